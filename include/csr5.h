@@ -403,6 +403,170 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
                              const double *val, const double *x, double *y, int32_t lanes_per_row,
                              void *hip_stream);
 
+/* ==========================================================================
+ * 5. Products of a layer of experts (large language models).  A router's choice
+ *    is a sparse matrix of tokens x experts with k entries per row; grouped by
+ *    expert it is that matrix in CSR, with offset[] for row_ptr, the experts'
+ *    products are a block-sparse product over those offsets, and the way back to
+ *    the tokens is a sparse times dense product.
+ *
+ * Matrices are row-major with a row stride in elements (ld..., at least the number
+ * of columns): rows may be views into wider arrays, and no address has to be aligned to
+ * more than its element; 16-byte aligned addresses and rows (ld * element size a
+ * multiple of 16) get the fast kernels.  dtype names the 16- or 32-bit type of a
+ * call's matrices; 8-bit values are OCP e4m3 (finite, largest 448) in uint8_t.
+ * Sums, softmax, norms and scales are held in 32 bits, and a result is rounded
+ * once.  Every call only enqueues kernels on the stream, allocates nothing, waits for
+ * nothing, and may be captured into a graph.  Results do not depend on timing: no call adds
+ * atomically.  Outputs must not overlap inputs unless a comment says that they may.
+ *
+ * Whatever offset, source and place hold, no kernel leaves the arrays: offsets are
+ * clamped to [0, rows], a group that ends before it begins is empty, a source
+ * outside [0, x_rows) is a row of zeros and a place outside [0, rows) is no row.
+ * A size of 0 is fine: such a call writes what is left to write (or nothing).
+ * ========================================================================== */
+#define CSR5_DTYPE_BF16 2
+#define CSR5_DTYPE_F16 3
+
+#define CSR5_ROUTE_MAX_EXPERTS 1024
+#define CSR5_ROUTE_MAX_K 32
+#define CSR5_NORM_MAX_N 32768
+#define CSR5_F8_BLOCK 128 /* values of a row that share a scale */
+
+/*
+ * The router: for each token the k experts with the largest logits, in descending
+ * order (the lower expert first where two are equal), and the softmax over those k:
+ *   weight[t][j] = exp(l_j - l_0) / sum_i exp(l_i - l_0).
+ * An expert whose logit is -inf (masked) or NaN is never chosen.  Where fewer than k
+ * remain the rest of the k get expert -1, weight 0 and place -1; a token with a NaN
+ * has NaN weights.  The pairs (t, j), j < k, that have an expert are then grouped:
+ * rows [offset[e], offset[e+1]) belong to expert e, by token and j within it.
+ *   logits   dtype (BF16, F16, F32) [tokens][experts], row stride ld
+ *   expert   int32[tokens*k]      weight  float[tokens*k]
+ *   offset   int32[experts+1]     offset[experts]: the number of rows
+ *   source   int32[tokens*k]      the token of each row, -1 past the last one
+ *   place    int32[tokens*k]      the row of each pair
+ *   workspace  csr5_route_workspace_bytes bytes (0: may be NULL), free again after the call
+ * 1 <= k <= min(experts, CSR5_ROUTE_MAX_K), experts <= CSR5_ROUTE_MAX_EXPERTS and
+ * tokens*k < 2^31, else CSR5_ERANGE (workspace bytes: 0).
+ */
+size_t csr5_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t k);
+int csr5_route(int32_t tokens, int32_t experts, int32_t k, int dtype, const void *logits, int64_t ld,
+               int32_t *expert, float *weight, int32_t *offset, int32_t *source, int32_t *place,
+               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradient of the router's weights with respect to the logits:
+ *   dlogits[t][expert_j] = weight_j * (dweight_j - sum_i weight_i dweight_i), 0 elsewhere.
+ * A pair whose expert is outside [0, experts) gives nothing.
+ */
+int csr5_route_backward(int32_t tokens, int32_t experts, int32_t k, int dtype, const int32_t *expert,
+                        const float *weight, const float *dweight, void *dlogits, int64_t ld,
+                        void *hip_stream);
+
+/*
+ * Back to the tokens: y[t] = residual[t] + sum_j weight[t][j] * z[place[t][j]], with j
+ * ascending.  z[rows][n], y and residual [tokens][n] in dtype (BF16, F16, F32);
+ * residual may be NULL, and y may be residual; weight may be NULL: ones (so the
+ * gradients of gathered rows are added up, see csr5_grouped_gemm_dx).
+ */
+int csr5_combine(int32_t tokens, int32_t k, int32_t rows, int32_t n, int dtype, const void *z, int64_t ldz,
+                 const int32_t *place, const float *weight, const void *residual, int64_t ldr, void *y,
+                 int64_t ldy, void *hip_stream);
+
+/*
+ * Gradients of csr5_combine (that of the residual is dy itself):
+ *   dz[place[t][j]] = weight[t][j] * dy[t],   dweight[t][j] = dy[t] . z[place[t][j]]
+ * (0 for a pair without a row).  Rows of dz that no place names stay as they are; place names
+ * a row at most once.  dz may be z.
+ */
+int csr5_combine_backward(int32_t tokens, int32_t k, int32_t rows, int32_t n, int dtype, const void *dy,
+                          int64_t lddy, const void *z, int64_t ldz, const int32_t *place,
+                          const float *weight, void *dz, int64_t lddz, float *dweight,
+                          void *hip_stream);
+
+/*
+ * Products grouped by expert, groups of any sizes.  Row r of group g, that is
+ * offset[g] <= r < offset[g+1]:
+ *   csr5_grouped_gemm     y[r]  = w[g] x[source[r]]          y [rows][n]
+ *   csr5_grouped_gemm_dx  dx[r] = w[g]^T dy[r]               dx[rows][k]
+ *   csr5_grouped_gemm_dw  dw[g] = sum_r dy[r] x[source[r]]^T dw[groups][n][k]
+ * x[x_rows][k]; source int32[rows], or NULL: row r itself (x_rows >= rows then);
+ * w[g] is n x k with row stride ldw, and begins w_group elements after w[g-1]; dw
+ * likewise.  dtype BF16 or F16 for all matrices of a call.  Rows in no group are
+ * left as they are; dw of an empty group is 0.
+ */
+int csr5_grouped_gemm(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t *offset,
+                      const void *x, int32_t x_rows, int64_t ldx, const int32_t *source, const void *w,
+                      int64_t ldw, int64_t w_group, void *y, int64_t ldy, void *hip_stream);
+int csr5_grouped_gemm_dx(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t *offset,
+                         const void *dy, int64_t lddy, const void *w, int64_t ldw, int64_t w_group,
+                         void *dx, int64_t lddx, void *hip_stream);
+int csr5_grouped_gemm_dw(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t *offset,
+                         const void *dy, int64_t lddy, const void *x, int32_t x_rows, int64_t ldx,
+                         const int32_t *source, void *dw, int64_t lddw, int64_t dw_group,
+                         void *hip_stream);
+
+/*
+ * 8-bit values with a scale for each block of block_rows x 128 values (block_rows 1 or
+ * 128; the blocks at the right and lower edge may be smaller):
+ *   scale = max(max|x| / 448, 2^-126),   q = x / scale, rounded to the nearest e4m3
+ * The scale of block (i, b) is at scale[i*scale_row + b*scale_block].  A block with an
+ * infinity or a NaN has such a scale.  x[rows][n] in dtype (BF16, F16, F32).
+ */
+int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const void *x, int64_t ldx,
+                  uint8_t *q, int64_t ldq, float *scale, int64_t scale_row, int64_t scale_block,
+                  void *hip_stream);
+
+/*
+ * Product in 8 bits: y[i][j] = sum over blocks b of 128 of
+ *   x_scale(i, b) * w_scale(j / w_rows, b) * sum_{c in b} x[i][c] w[j][c],
+ * each block's sum in 32 bits before it is scaled.  x[m][k], w[n][k]; w_rows is 128
+ * (scales of csr5_quantise with block_rows 128: weights) or 1 (both operands are
+ * quantised by rows, as the gradient of a weight needs it).  x_scale(i, b) is at
+ * x_scale[i*xs_row + b*xs_block], w_scale at w_scale[(j/w_rows)*ws_row + b*ws_block].
+ * dtype (BF16, F16, F32) is y's.
+ * Grouped by expert: as csr5_grouped_gemm; the scales of x go with its rows (by source),
+ * those of w[g] begin ws_group elements after those of w[g-1].
+ */
+int csr5_gemm_f8(int32_t m, int32_t n, int32_t k, int dtype, const uint8_t *x, int64_t ldx,
+                 const float *x_scale, int64_t xs_row, int64_t xs_block, const uint8_t *w, int64_t ldw,
+                 const float *w_scale, int32_t w_rows, int64_t ws_row, int64_t ws_block, void *y,
+                 int64_t ldy, void *hip_stream);
+int csr5_grouped_gemm_f8(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t *offset,
+                         const uint8_t *x, int32_t x_rows, int64_t ldx, const float *x_scale,
+                         int64_t xs_row, int64_t xs_block, const int32_t *source, const uint8_t *w,
+                         int64_t ldw, int64_t w_group, const float *w_scale, int32_t w_rows,
+                         int64_t ws_row, int64_t ws_block, int64_t ws_group, void *y, int64_t ldy,
+                         void *hip_stream);
+
+/*
+ * Root-mean-square norm of a row, with the residual's addition before it:
+ *   h = x + residual,   rstd = 1 / sqrt(mean(h^2) + eps),   y = h * rstd * gain
+ * x, residual (may be NULL), gain[n] (may be NULL: ones), h and y in dtype (BF16,
+ * F16, F32).  Outputs, each of which may be NULL: h (may be x or residual), y (may
+ * be x), q with scale (y in 8 bits as by csr5_quantise with block_rows 1, from y before its
+ * rounding), rstd float[rows].  The norm is that of h before its rounding.
+ * n <= CSR5_NORM_MAX_N, else CSR5_ERANGE.
+ */
+int csr5_rmsnorm(int32_t rows, int32_t n, int dtype, const void *x, int64_t ldx, const void *residual,
+                 int64_t ldr, const void *gain, float eps, void *h, int64_t ldh, void *y, int64_t ldy,
+                 uint8_t *q, int64_t ldq, float *scale, int64_t scale_row, int64_t scale_block,
+                 float *rstd, void *hip_stream);
+
+/*
+ * Its gradients, from dy (of y) and residual_grad (of h from elsewhere, may be NULL):
+ *   dh = rstd * (u - v * mean(u * v)) + residual_grad with u = dy * gain, v = h * rstd;
+ *   dgain[n] = sum over rows of dy * v, in float (may be NULL).
+ * dh is the gradient of x and of the residual alike; it may be dy or residual_grad.
+ * workspace: csr5_rmsnorm_workspace_bytes bytes, free again after the call.
+ */
+size_t csr5_rmsnorm_workspace_bytes(int32_t rows, int32_t n);
+int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void *h, int64_t ldh, const void *gain,
+                          const float *rstd, const void *dy, int64_t lddy, const void *residual_grad,
+                          int64_t ldrg, void *dh, int64_t lddh, float *dgain, void *workspace,
+                          size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,8 @@ CSR5_FLAG_AUX_TWO_KERNELS, CSR5_FLAG_AUX_ONE_KERNEL = 2, 4
 CSR5_STATUS_BAD_ROW_PTR, CSR5_STATUS_BAD_COL_IDX, CSR5_STATUS_HAS_DIRTY = 1, 2, 4
 CSR5_STATUS_HAS_EMPTY_ROWS = 8
 CSR5_ARRAY_TILE_PTR, CSR5_ARRAY_TILE_DESC, CSR5_ARRAY_EMPTY_OFFSET_PTR, CSR5_ARRAY_EMPTY_OFFSET = 0, 1, 2, 3
+CSR5_DTYPE_F64, CSR5_DTYPE_F32, CSR5_DTYPE_BF16, CSR5_DTYPE_F16 = range(4)
+CSR5_ROUTE_MAX_EXPERTS, CSR5_ROUTE_MAX_K, CSR5_NORM_MAX_N, CSR5_F8_BLOCK = 1024, 32, 32768, 128
 CSR5_KERNEL_TILES, CSR5_KERNEL_PARTS, CSR5_KERNEL_WINDOW, CSR5_KERNEL_GATHERED, CSR5_KERNEL_PAIRS = range(5)
 
 # every symbol include/csr5.h declares
@@ -37,6 +39,9 @@ SYMBOLS = [
     "csr5_read_array", "csr5_strerror", "csr5_baseline_csr_scalar", "csr5_baseline_csr_vector",
     "csr5s_convert_ex", "csr5s_spmv_ex", "csr5s_spmv_profile",
     "csr5l_workspace_bytes", "csr5l_convert_ex", "csr5l_get_arrays",
+    "csr5_route_workspace_bytes", "csr5_route", "csr5_route_backward", "csr5_combine", "csr5_combine_backward",
+    "csr5_grouped_gemm", "csr5_grouped_gemm_dx", "csr5_grouped_gemm_dw", "csr5_quantise", "csr5_gemm_f8",
+    "csr5_grouped_gemm_f8", "csr5_rmsnorm", "csr5_rmsnorm_workspace_bytes", "csr5_rmsnorm_backward",
 ]
 
 
@@ -111,6 +116,27 @@ def load():
     lib.csr5_baseline_csr_scalar.argtypes = [i32, vp, vp, vp, vp, vp, vp]
     lib.csr5_baseline_csr_vector.restype = C.c_int
     lib.csr5_baseline_csr_vector.argtypes = [i32, i32, vp, vp, vp, vp, vp, i32, vp]
+    layer = {
+        "csr5_route": [i32, i32, i32, C.c_int, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp],
+        "csr5_route_backward": [i32, i32, i32, C.c_int, vp, vp, vp, vp, i64, vp],
+        "csr5_combine": [i32, i32, i32, i32, C.c_int, vp, i64, vp, vp, vp, i64, vp, i64, vp],
+        "csr5_combine_backward": [i32, i32, i32, i32, C.c_int, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp],
+        "csr5_grouped_gemm": [i32, i32, i32, i32, C.c_int, vp, vp, i32, i64, vp, vp, i64, i64, vp, i64, vp],
+        "csr5_grouped_gemm_dx": [i32, i32, i32, i32, C.c_int, vp, vp, i64, vp, i64, i64, vp, i64, vp],
+        "csr5_grouped_gemm_dw": [i32, i32, i32, i32, C.c_int, vp, vp, i64, vp, i32, i64, vp, vp, i64, i64, vp],
+        "csr5_quantise": [i32, i32, i32, C.c_int, vp, i64, vp, i64, vp, i64, i64, vp],
+        "csr5_gemm_f8": [i32, i32, i32, C.c_int, vp, i64, vp, i64, i64, vp, i64, vp, i32, i64, i64, vp, i64, vp],
+        "csr5_grouped_gemm_f8": [i32, i32, i32, i32, C.c_int, vp, vp, i32, i64, vp, i64, i64, vp, vp, i64, i64, vp, i32, i64, i64, i64, vp, i64, vp],
+        "csr5_rmsnorm": [i32, i32, C.c_int, vp, i64, vp, i64, vp, C.c_float, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, vp],
+        "csr5_rmsnorm_backward": [i32, i32, C.c_int, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp],
+    }
+    for name, argtypes in layer.items():
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = argtypes
+    lib.csr5_route_workspace_bytes.restype = sz
+    lib.csr5_route_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.csr5_rmsnorm_workspace_bytes.restype = sz
+    lib.csr5_rmsnorm_workspace_bytes.argtypes = [i32, i32]
     lib.csr5_strerror.restype = C.c_char_p
     lib.csr5_strerror.argtypes = [C.c_int]
     _lib = lib
@@ -401,3 +427,229 @@ def csr5_read_array(h, which, wide=False):
     _chk(load().csr5_read_array(h, which, out.ctypes.data_as(C.c_void_p), out.nbytes),
          "csr5_read_array", True)
     return out
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Products of a layer of experts (section 5 of the header).  Matrices are 2-D tensors whose rows are contiguous (views
+# into wider ones are fine), weights of experts 3-D ones; sizes are taken from the tensors, and what the library cannot
+# see (element types, lengths) is checked here.  8-bit values are float8_e4m3fn or uint8 tensors.
+# ---------------------------------------------------------------------------------------------------------------------
+_TYPE_CODES: dict = {}      # 16- and 32-bit floating types -> dtype codes; filled on first use
+_F8_TYPES: tuple = ()
+
+
+def _code(t, name):
+    if not _TYPE_CODES:
+        import torch
+        global _F8_TYPES
+        load()
+        _F8_TYPES = (torch.float8_e4m3fn, torch.uint8)
+        _TYPE_CODES.update({torch.bfloat16: CSR5_DTYPE_BF16, torch.float16: CSR5_DTYPE_F16, torch.float32: CSR5_DTYPE_F32})
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected dtype bfloat16, float16 or float32, got {t.dtype}")
+    return code
+
+
+def _matrix(t, dtype, rows, cols, name):
+    """Address and row stride of a matrix of `dtype` (None: 8-bit values) with exactly this shape."""
+    if t.dtype is not dtype and not (dtype is None and t.dtype in _F8_TYPES):
+        raise ValueError(f"{name}: expected dtype {dtype or 'float8_e4m3fn or uint8'}, got {t.dtype}")
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
+    ld, step = t.stride()
+    if not t.is_cuda or (step != 1 and cols > 1):
+        raise ValueError(f"{name}: expected a GPU tensor with contiguous rows")
+    return t.data_ptr() or None, ld if rows > 1 else max(ld, cols)
+
+
+def _experts(t, dtype, groups, n, k, name):
+    """Address, row stride and expert stride of weights [groups, n, k]."""
+    if t.dtype is not dtype and not (dtype is None and t.dtype in _F8_TYPES):
+        raise ValueError(f"{name}: expected dtype {dtype or 'float8_e4m3fn or uint8'}, got {t.dtype}")
+    if t.shape != (groups, n, k):
+        raise ValueError(f"{name}: expected shape {(groups, n, k)}, got {tuple(t.shape)}")
+    group, ld, step = t.stride()
+    if not t.is_cuda or (step != 1 and k > 1):
+        raise ValueError(f"{name}: expected a GPU tensor with contiguous rows")
+    return t.data_ptr() or None, ld if n > 1 else max(ld, k), group
+
+
+def _scales(t, dims, name):
+    """Address and strides of float32 scales of exactly this shape, in any layout."""
+    if _TYPE_CODES.get(t.dtype) != CSR5_DTYPE_F32 or not t.is_cuda:
+        raise ValueError(f"{name}: expected a float32 GPU tensor, got {t.dtype}")
+    if t.shape != dims:
+        raise ValueError(f"{name}: expected shape {dims}, got {tuple(t.shape)}")
+    return (t.data_ptr() or None, *t.stride())
+
+
+def _f8_blocks(n):
+    return -(-n // CSR5_F8_BLOCK)
+
+
+def _space(t):
+    """Address and bytes of a workspace (None: none)."""
+    return (None, 0) if t is None else (_arr(t, ["u8"], 0, "workspace"), t.numel())
+
+
+def csr5_route_workspace_bytes(tokens, experts, k):
+    return int(load().csr5_route_workspace_bytes(int(tokens), int(experts), int(k)))
+
+
+def csr5_route(logits, k, expert, weight, offset, source, place, workspace=None, stream=None, check=True):
+    """The k experts of each row of `logits` [tokens, experts], their softmax, and the pairs grouped by expert.  Writes
+    expert, place (int32) and weight (float32) [tokens * k], source (int32) [tokens * k] and offset (int32)
+    [experts + 1]; `workspace` (uint8) has csr5_route_workspace_bytes bytes."""
+    code = _code(logits, "logits")
+    tokens, experts = logits.shape
+    pairs = tokens * k
+    return _chk(load().csr5_route(tokens, experts, k, code, *_matrix(logits, logits.dtype, tokens, experts, "logits"),
+                                  _arr(expert, ["i32"], pairs, "expert"), _arr(weight, ["f32"], pairs, "weight"),
+                                  _arr(offset, ["i32"], experts + 1, "offset"), _arr(source, ["i32"], pairs, "source"),
+                                  _arr(place, ["i32"], pairs, "place"), *_space(workspace), _stream(stream)), "csr5_route", check)
+
+
+def csr5_route_backward(expert, weight, dweight, dlogits, stream=None, check=True):
+    """Writes dlogits [tokens, experts] from expert, weight and dweight [tokens, k]."""
+    code = _code(dlogits, "dlogits")
+    tokens, experts = dlogits.shape
+    k = expert.shape[1]
+    return _chk(load().csr5_route_backward(tokens, experts, k, code, _arr(expert, ["i32"], tokens * k, "expert"),
+                                           _arr(weight, ["f32"], tokens * k, "weight"), _arr(dweight, ["f32"], tokens * k, "dweight"),
+                                           *_matrix(dlogits, dlogits.dtype, tokens, experts, "dlogits"), _stream(stream)),
+                "csr5_route_backward", check)
+
+
+def csr5_combine(z, place, y, weight=None, residual=None, stream=None, check=True):
+    """y[t] = residual[t] + sum_j weight[t, j] * z[place[t, j]]; place and weight [tokens, k], z [rows, n]."""
+    code, dt = _code(z, "z"), z.dtype
+    rows, n = z.shape
+    tokens, k = place.shape
+    res = (None, 0) if residual is None else _matrix(residual, dt, tokens, n, "residual")
+    return _chk(load().csr5_combine(tokens, k, rows, n, code, *_matrix(z, dt, rows, n, "z"), _arr(place, ["i32"], tokens * k, "place"),
+                                    _arr(weight, ["f32"], tokens * k, "weight"), *res, *_matrix(y, dt, tokens, n, "y"), _stream(stream)),
+                "csr5_combine", check)
+
+
+def csr5_combine_backward(dy, z, place, weight, dz, dweight, stream=None, check=True):
+    """Writes dz [rows, n] and dweight [tokens, k]."""
+    code, dt = _code(z, "z"), z.dtype
+    rows, n = z.shape
+    tokens, k = place.shape
+    return _chk(load().csr5_combine_backward(tokens, k, rows, n, code, *_matrix(dy, dt, tokens, n, "dy"), *_matrix(z, dt, rows, n, "z"),
+                                             _arr(place, ["i32"], tokens * k, "place"), _arr(weight, ["f32"], tokens * k, "weight"),
+                                             *_matrix(dz, dt, rows, n, "dz"), _arr(dweight, ["f32"], tokens * k, "dweight"),
+                                             _stream(stream)), "csr5_combine_backward", check)
+
+
+def _source(source, rows, x_rows):
+    if source is None:
+        if x_rows < rows:
+            raise ValueError(f"x: needs {rows} rows without source, has {x_rows}")
+        return None
+    return _arr(source, ["i32"], rows, "source")
+
+
+def csr5_grouped_gemm(x, w, offset, y, source=None, stream=None, check=True):
+    """y[r] = w[g] x[source[r]] for the rows r of each group g; x [x_rows, k], w [groups, n, k], y [rows, n]."""
+    code, dt = _code(x, "x"), x.dtype
+    x_rows, k = x.shape
+    groups, n = w.shape[0], w.shape[1]
+    rows = y.shape[0]
+    px, ldx = _matrix(x, dt, x_rows, k, "x")
+    return _chk(load().csr5_grouped_gemm(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), px, x_rows, ldx, _source(source, rows, x_rows),
+                                         *_experts(w, dt, groups, n, k, "w"), *_matrix(y, dt, rows, n, "y"), _stream(stream)),
+                "csr5_grouped_gemm", check)
+
+
+def csr5_grouped_gemm_dx(dy, w, offset, dx, stream=None, check=True):
+    """dx[r] = w[g]^T dy[r] for the rows r of each group g; dy [rows, n], w [groups, n, k], dx [rows, k]."""
+    code, dt = _code(dy, "dy"), dy.dtype
+    rows, n = dy.shape
+    groups, k = w.shape[0], w.shape[2]
+    return _chk(load().csr5_grouped_gemm_dx(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), *_matrix(dy, dt, rows, n, "dy"),
+                                            *_experts(w, dt, groups, n, k, "w"), *_matrix(dx, dt, rows, k, "dx"), _stream(stream)),
+                "csr5_grouped_gemm_dx", check)
+
+
+def csr5_grouped_gemm_dw(dy, x, offset, dw, source=None, stream=None, check=True):
+    """dw[g] = sum over the rows r of group g of dy[r] x[source[r]]^T; dy [rows, n], x [x_rows, k], dw [groups, n, k]."""
+    code, dt = _code(dy, "dy"), dy.dtype
+    rows, n = dy.shape
+    x_rows, k = x.shape
+    groups = dw.shape[0]
+    px, ldx = _matrix(x, dt, x_rows, k, "x")
+    return _chk(load().csr5_grouped_gemm_dw(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), *_matrix(dy, dt, rows, n, "dy"),
+                                            px, x_rows, ldx, _source(source, rows, x_rows), *_experts(dw, dt, groups, n, k, "dw"),
+                                            _stream(stream)), "csr5_grouped_gemm_dw", check)
+
+
+def csr5_quantise(x, q, scale, block_rows=1, stream=None, check=True):
+    """q [rows, n] in 8 bits and scale [ceil(rows / block_rows), ceil(n / 128)] of x [rows, n]; block_rows 1 or 128."""
+    code = _code(x, "x")
+    rows, n = x.shape
+    return _chk(load().csr5_quantise(rows, n, block_rows, code, *_matrix(x, x.dtype, rows, n, "x"), *_matrix(q, None, rows, n, "q"),
+                                     *_scales(scale, (-(-rows // block_rows), _f8_blocks(n)), "scale"), _stream(stream)), "csr5_quantise", check)
+
+
+def csr5_gemm_f8(x, x_scale, w, w_scale, y, w_rows=CSR5_F8_BLOCK, stream=None, check=True):
+    """y [m, n] = x [m, k] times w [n, k] transposed, both in 8 bits, with x_scale [m, ceil(k / 128)] and w_scale
+    [ceil(n / w_rows), ceil(k / 128)]; w_rows 128 or 1."""
+    code = _code(y, "y")
+    (m, k), n = x.shape, w.shape[0]
+    b = _f8_blocks(k)
+    pw, ldw = _matrix(w, None, n, k, "w")
+    ps, *ws = _scales(w_scale, (-(-n // w_rows), b), "w_scale")
+    return _chk(load().csr5_gemm_f8(m, n, k, code, *_matrix(x, None, m, k, "x"), *_scales(x_scale, (m, b), "x_scale"), pw, ldw, ps, w_rows, *ws,
+                                    *_matrix(y, y.dtype, m, n, "y"), _stream(stream)), "csr5_gemm_f8", check)
+
+
+def csr5_grouped_gemm_f8(x, x_scale, w, w_scale, offset, y, w_rows=CSR5_F8_BLOCK, source=None, stream=None, check=True):
+    """csr5_grouped_gemm in 8 bits: x_scale [x_rows, ceil(k / 128)], w_scale [groups, ceil(n / w_rows), ceil(k / 128)]."""
+    code = _code(y, "y")
+    x_rows, k = x.shape
+    groups, n = w.shape[0], w.shape[1]
+    rows, b = y.shape[0], _f8_blocks(k)
+    px, ldx = _matrix(x, None, x_rows, k, "x")
+    ps, ws_group, ws_row, ws_block = _scales(w_scale, (groups, -(-n // w_rows), b), "w_scale")
+    return _chk(load().csr5_grouped_gemm_f8(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), px, x_rows, ldx,
+                                            *_scales(x_scale, (x_rows, b), "x_scale"), _source(source, rows, x_rows),
+                                            *_experts(w, None, groups, n, k, "w"), ps, w_rows, ws_row, ws_block, ws_group,
+                                            *_matrix(y, y.dtype, rows, n, "y"), _stream(stream)), "csr5_grouped_gemm_f8", check)
+
+
+def csr5_rmsnorm(x, gain, eps, residual=None, h=None, y=None, q=None, scale=None, rstd=None, stream=None, check=True):
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain by rows of x [rows, n]; writes those of h, y, q with scale
+    [rows, ceil(n / 128)], and rstd [rows] that are given.  gain (or None: ones) [n]."""
+    code, dt = _code(x, "x"), x.dtype
+    rows, n = x.shape
+    if gain is not None and (gain.dtype is not dt or gain.shape != (n,) or not gain.is_cuda or not gain.is_contiguous()):
+        raise ValueError(f"gain: expected a contiguous GPU tensor of {n} values of {dt}")
+    if (q is None) != (scale is None):
+        raise ValueError("q and scale: both or neither")
+    none = (None, 0)
+    return _chk(load().csr5_rmsnorm(rows, n, code, *_matrix(x, dt, rows, n, "x"), *(none if residual is None else _matrix(residual, dt, rows, n, "residual")),
+                                    None if gain is None else gain.data_ptr() or None, eps,
+                                    *(none if h is None else _matrix(h, dt, rows, n, "h")), *(none if y is None else _matrix(y, dt, rows, n, "y")),
+                                    *(none if q is None else _matrix(q, None, rows, n, "q")),
+                                    *((None, 0, 0) if q is None else _scales(scale, (rows, _f8_blocks(n)), "scale")),
+                                    _arr(rstd, ["f32"], rows, "rstd"), _stream(stream)), "csr5_rmsnorm", check)
+
+
+def csr5_rmsnorm_workspace_bytes(rows, n):
+    return int(load().csr5_rmsnorm_workspace_bytes(int(rows), int(n)))
+
+
+def csr5_rmsnorm_backward(h, gain, rstd, dy, dh, dgain=None, workspace=None, residual_grad=None, stream=None, check=True):
+    """dh [rows, n] (of x and the residual alike) and dgain [n] (float32) from dy and residual_grad [rows, n]; `workspace`
+    (uint8, needed for dgain) has csr5_rmsnorm_workspace_bytes bytes."""
+    code, dt = _code(h, "h"), h.dtype
+    rows, n = h.shape
+    if gain is not None and (gain.dtype is not dt or gain.shape != (n,) or not gain.is_cuda or not gain.is_contiguous()):
+        raise ValueError(f"gain: expected a contiguous GPU tensor of {n} values of {dt}")
+    return _chk(load().csr5_rmsnorm_backward(rows, n, code, *_matrix(h, dt, rows, n, "h"), None if gain is None else gain.data_ptr() or None,
+                                             _arr(rstd, ["f32"], rows, "rstd"), *_matrix(dy, dt, rows, n, "dy"),
+                                             *((None, 0) if residual_grad is None else _matrix(residual_grad, dt, rows, n, "residual_grad")),
+                                             *_matrix(dh, dt, rows, n, "dh"), _arr(dgain, ["f32"], n, "dgain"), *_space(workspace),
+                                             _stream(stream)), "csr5_rmsnorm_backward", check)

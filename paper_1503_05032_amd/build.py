@@ -8,13 +8,13 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = [os.path.join(PKG, "csrc", "csr5.hip")]
-HEADERS = [os.path.join(PKG, "csrc", name) for name in ("row_share.h", "far_lists.h")]
+SRC = [os.path.join(PKG, "csrc", name) for name in ("csr5.hip", "experts.hip", "grouped.hip")]
+HEADERS = [os.path.join(PKG, "csrc", name) for name in ("row_share.h", "far_lists.h", "numbers.h")]
 INC = os.path.join(ROOT, "include")
 OUT = os.path.join(PKG, "libcsr5.so")
 
 FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-shared", "-fPIC",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
     "-munsafe-fp-atomics",            # hardware fp64 atomic add (memory is coarse-grained)
     # packed-fp32 instructions are switched off: some forms misbehave on this hardware
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -30,12 +30,27 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = True, extra=()) -> str:
+    """Compiles every source, side by side, and links them."""
     tmp = OUT + f".tmp{os.getpid()}"
-    cmd = [hipcc(), *FLAGS, *extra, "-I", INC, "-o", tmp, *SRC]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, OUT)
+    objects = [f"{tmp}.{os.path.basename(src)}.o" for src in SRC]
+
+    def start(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return subprocess.Popen(cmd, stdin=subprocess.DEVNULL)
+
+    try:
+        running = [start([hipcc(), *FLAGS, *extra, "-I", INC, "-c", src, "-o", obj]) for src, obj in zip(SRC, objects)]
+        codes = [p.wait() for p in running]
+        if any(codes):
+            raise subprocess.CalledProcessError(next(c for c in codes if c), running[0].args[0])
+        if start([hipcc(), *FLAGS, *extra, "-shared", "-o", tmp, *objects]).wait():
+            raise RuntimeError("linking libcsr5.so failed")
+        os.replace(tmp, OUT)
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     return OUT
 
 

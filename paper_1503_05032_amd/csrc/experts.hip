@@ -1,0 +1,665 @@
+// libcsr5: what stands around the products of a layer of experts -- the router, the way back to the tokens, the
+// root-mean-square norm and the quantisation to 8 bits.  All of it is bound by memory or by latency; the products
+// are in grouped.hip.  The C ABI is declared in include/csr5.h.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "csr5.h"
+#include "numbers.h"
+
+namespace {
+
+// Calls f with a value of the type that dtype names.
+template <typename F> int with_type(int dtype, F f) {
+    switch (dtype) {
+        case CSR5_DTYPE_BF16: return f(bf16());
+        case CSR5_DTYPE_F16: return f(f16());
+        case CSR5_DTYPE_F32: return f(float());
+        default: return CSR5_EINVAL;
+    }
+}
+size_t type_bytes(int dtype) { return dtype == CSR5_DTYPE_F32 ? 4 : dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16 ? 2 : 0; }
+
+// What the lanes of this wavefront wrote to LDS before is what they read after it (their LDS accesses are in order).
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The sum of v over the workgroup, for everybody.  `part` holds a word per wavefront and is not used again before the
+// next barrier.
+template <int TPB> __device__ __forceinline__ float group_sum(float v, float* part) {
+    v = lanes_sum<64>(v);
+    if (TPB == 64) return v;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPB / 64; w++) v += part[w];
+    return v;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Root-mean-square norm.  One workgroup per row, which it holds in registers between the sum of squares and the
+// output: x and the residual are read once.  8 neighbouring values per thread, so a block of 128 values that share a
+// scale is 16 neighbouring lanes.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T> struct NormArgs {
+    int n;
+    const T *x, *residual, *gain;
+    int64_t ldx, ldr;
+    float eps;
+    T *h, *y;
+    int64_t ldh, ldy;
+    uint8_t* q;
+    int64_t ldq;
+    float* scale;
+    int64_t scale_row, scale_block;
+    float* rstd;
+};
+
+template <typename T, int TPB, int NV, bool VEC> __global__ __launch_bounds__(TPB) void k_rmsnorm(NormArgs<T> a) {
+    __shared__ float part[TPB / 64];
+    const int64_t row = blockIdx.x;
+    float v[NV][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < NV; c++) {
+        const int col = (c * TPB + int(threadIdx.x)) * 8;
+        load_values<8, VEC>(a.x + row * a.ldx + col, a.n - col, v[c]);
+        if (a.residual) {
+            float r[8];
+            load_values<8, VEC>(a.residual + row * a.ldr + col, a.n - col, r);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[c][i] += r[i];
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < NV; c++) {
+        const int col = (c * TPB + int(threadIdx.x)) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum += v[c][i] * v[c][i];
+        if (a.h) store_values<8, VEC>(a.h + row * a.ldh + col, a.n - col, v[c]);
+    }
+    const float rstd = 1.f / sqrtf(group_sum<TPB>(sum, part) / float(a.n) + a.eps);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int c = 0; c < NV; c++) {
+        const int col = (c * TPB + int(threadIdx.x)) * 8;
+        float g[8];
+        if (a.gain) load_values<8, VEC>(a.gain + col, a.n - col, g);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[c][i] = a.gain ? v[c][i] * rstd * g[i] : v[c][i] * rstd;
+        if (a.y) store_values<8, VEC>(a.y + row * a.ldy + col, a.n - col, v[c]);
+        if (a.q) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) most = max(most, i < a.n - col ? magnitude(v[c][i]) : 0u);
+            const Scale s = f8_scale(lanes_max<16>(most));
+            if (col < a.n) {
+                f8_store<VEC>(a.q + row * a.ldq + col, a.n - col, v[c], s);
+                if ((threadIdx.x & 15) == 0) a.scale[row * a.scale_row + (col / CSR5_F8_BLOCK) * a.scale_block] = s.scale;
+            }
+        }
+    }
+}
+
+// Its gradients.  A workgroup takes rows by turns and keeps its share of the gain's gradient in registers; the shares
+// go to the workspace and are added up by k_columns in a fixed order.
+constexpr int NORM_GROUPS = 1024;
+template <typename T> struct NormBackArgs {
+    int rows, n;
+    const T *h, *gain, *dy, *residual_grad;
+    int64_t ldh, lddy, ldrg;
+    const float* rstd;
+    T* dh;
+    int64_t lddh;
+    float* share;           // [gridDim.x][n], NULL: not wanted
+};
+
+template <typename T, int TPB, int NV, bool VEC> __global__ __launch_bounds__(TPB) void k_rmsnorm_back(NormBackArgs<T> a) {
+    __shared__ float part[2][TPB / 64];
+    float gain[NV][8], share[NV][8];
+#pragma unroll
+    for (int c = 0; c < NV; c++) {
+        const int col = (c * TPB + int(threadIdx.x)) * 8;
+        if (a.gain) load_values<8, VEC>(a.gain + col, a.n - col, gain[c]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            share[c][i] = 0.f;
+            if (!a.gain) gain[c][i] = 1.f;
+        }
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const float r = a.rstd[row];
+        float v[NV][8], u[NV][8], sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < NV; c++) {
+            const int col = (c * TPB + int(threadIdx.x)) * 8;
+            load_values<8, VEC>(a.h + row * a.ldh + col, a.n - col, v[c]);
+            load_values<8, VEC>(a.dy + row * a.lddy + col, a.n - col, u[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < NV; c++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                v[c][i] *= r;
+                share[c][i] += u[c][i] * v[c][i];
+                u[c][i] *= gain[c][i];
+                sum += u[c][i] * v[c][i];
+            }
+        const float mean = group_sum<TPB>(sum, part[turn]) / float(a.n);
+#pragma unroll
+        for (int c = 0; c < NV; c++) {
+            const int col = (c * TPB + int(threadIdx.x)) * 8;
+            float d[8];
+            if (a.residual_grad) load_values<8, VEC>(a.residual_grad + row * a.ldrg + col, a.n - col, d);
+#pragma unroll
+            for (int i = 0; i < 8; i++) d[i] = r * (u[c][i] - v[c][i] * mean) + (a.residual_grad ? d[i] : 0.f);
+            store_values<8, VEC>(a.dh + row * a.lddh + col, a.n - col, d);
+        }
+    }
+    if (a.share)
+#pragma unroll
+        for (int c = 0; c < NV; c++) {
+            const int col = (c * TPB + int(threadIdx.x)) * 8;
+            store_values<8, false>(a.share + int64_t(blockIdx.x) * a.n + col, a.n - col, share[c]);
+        }
+}
+
+// out[col] = sum over `rows` rows; 32 columns and 32 rows side by side.
+__global__ __launch_bounds__(1024) void k_columns(int rows, int n, const float* in, float* out) {
+    __shared__ float part[32][33];
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = int(blockIdx.x) * 32 + c;
+    float sum = 0.f;
+    if (col < n)
+        for (int i = r; i < rows; i += 32) sum += in[int64_t(i) * n + col];
+    part[r][c] = sum;
+    __syncthreads();
+    if (r == 0 && col < n) {
+        for (int i = 1; i < 32; i++) sum += part[i][c];
+        out[col] = sum;
+    }
+}
+
+// The shapes of the norm's kernels: threads of a row's workgroup, and how many times 8 values a thread holds.
+template <typename F> void norm_shape(int n, F f) {
+    using std::integral_constant;
+    if (n <= 512) f(integral_constant<int, 64>(), integral_constant<int, 1>());
+    else if (n <= 2048) f(integral_constant<int, 256>(), integral_constant<int, 1>());
+    else if (n <= 4096) f(integral_constant<int, 256>(), integral_constant<int, 2>());
+    else if (n <= 8192) f(integral_constant<int, 1024>(), integral_constant<int, 1>());
+    else if (n <= 16384) f(integral_constant<int, 1024>(), integral_constant<int, 2>());
+    else f(integral_constant<int, 1024>(), integral_constant<int, 4>());
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Quantisation.  ROWS = 1: 16 lanes per block of 128 values; ROWS = 128: a workgroup per block of 128 x 128.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T, int ROWS, bool VEC>
+__global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, int64_t ldx, uint8_t* q, int64_t ldq, float* scale, int64_t scale_row, int64_t scale_block) {
+    constexpr int PASSES = ROWS == 1 ? 1 : 8;
+    const int blocks = (n + CSR5_F8_BLOCK - 1) / CSR5_F8_BLOCK, lane = threadIdx.x & 15, line = threadIdx.x >> 4;
+    int64_t row0;
+    int b;
+    if (ROWS == 1) {
+        const int64_t at = int64_t(blockIdx.x) * 16 + line;
+        row0 = at / blocks, b = int(at % blocks);
+        if (row0 >= rows) return;
+    } else {
+        row0 = int64_t(blockIdx.x / blocks) * ROWS + line, b = int(blockIdx.x % blocks);
+    }
+    const int col = b * CSR5_F8_BLOCK + lane * 8;
+    float v[PASSES][8];
+    uint32_t most = 0;
+#pragma unroll
+    for (int p = 0; p < PASSES; p++) {
+        const int64_t row = row0 + p * 16;
+        load_values<8, VEC>(x + row * ldx + col, row < rows ? n - col : 0, v[p]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) most = max(most, magnitude(v[p][i]));
+    }
+    if (ROWS == 1) {
+        most = lanes_max<16>(most);
+    } else {
+        __shared__ uint32_t part[4];
+        most = lanes_max<64>(most);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+        __syncthreads();
+        most = max(max(part[0], part[1]), max(part[2], part[3]));
+    }
+    const Scale s = f8_scale(most);
+#pragma unroll
+    for (int p = 0; p < PASSES; p++) {
+        const int64_t row = row0 + p * 16;
+        if (row < rows && col < n) f8_store<VEC>(q + row * ldq + col, n - col, v[p], s);
+    }
+    if (lane == 0 && (ROWS == 1 || line == 0)) scale[row0 / ROWS * scale_row + b * scale_block] = s.scale;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// The router.  A wavefront per token; a lane holds V neighbouring logits, so among equal ones the lowest lane, and in
+// it the lowest value, is the lowest expert.  k rounds of: largest of the wavefront, who has it first, take it out.
+//
+// Grouping is a counting sort, stable by pair: every workgroup counts the experts of its chunk of tokens; then each
+// adds up, per expert, the counts of all chunks and of those before it, and hands out rows to its pairs in order.
+// Tokens of one chunk: one workgroup does both.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int ROUTE_CHUNKS = 256;       // at most, each a workgroup
+constexpr int ROUTE_WAVES = 16;
+constexpr int ROUTE_ONE = 64;           // tokens that a single workgroup routes
+
+struct RouteArgs {
+    int tokens, experts, k, chunk, chunks;      // chunk: tokens of a workgroup
+    const void* logits;
+    int64_t ld;
+    int32_t* expert;
+    float* weight;
+    int32_t *offset, *source, *place;
+    int32_t* count;                             // [chunks][experts]
+};
+
+template <typename T, int V> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int32_t* count) {
+    const int lane = threadIdx.x & 63;
+    const T* row = static_cast<const T*>(a.logits) + t * a.ld;
+    float v[V];
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int e = lane * V + i;
+        v[i] = e < a.experts ? float(row[e]) : -INFINITY;
+        if (v[i] != v[i]) nan = true, v[i] = -INFINITY;
+    }
+    nan = __any(nan);
+    float mine = -INFINITY;         // of lane j: the j-th largest
+    int which = -1;
+    for (int j = 0; j < a.k; j++) {
+        float most = v[0];
+#pragma unroll
+        for (int i = 1; i < V; i++) most = fmaxf(most, v[i]);
+        float all = most;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
+        if (all == -INFINITY) break;
+        const int first = __ffsll((unsigned long long)__ballot(most == all)) - 1;
+        int at = 0;
+#pragma unroll
+        for (int i = V - 1; i >= 0; i--)
+            if (v[i] == all) at = i;
+        if (lane == first) {
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if (i == at) v[i] = -INFINITY;
+        }
+        at = __shfl(at, first);
+        if (lane == j) mine = all, which = first * V + at;
+    }
+    const float top = __shfl(mine, 0);
+    float w = which >= 0 ? expf(mine - top) : 0.f;
+    w = w / fmaxf(lanes_sum<64>(w), 1.f);       // the largest is exp(0): the sum is 1 at least where there is one
+    if (top == INFINITY || nan) w = NAN;
+    if (lane < a.k) {
+        a.expert[t * a.k + lane] = which;
+        a.weight[t * a.k + lane] = w;
+        if (which >= 0) atomicAdd(&count[which], 1);        // in LDS; a count does not depend on the order
+    }
+}
+
+// Lanes whose `e` is this lane's, among those with `in`.
+__device__ __forceinline__ uint64_t same_as(int e, bool in, int bits) {
+    uint64_t m = __ballot(in);
+    for (int b = 0; b < bits; b++) {
+        const uint64_t set = __ballot((e >> b) & 1);
+        m &= (e >> b) & 1 ? set : ~set;
+    }
+    return m;
+}
+
+// LDS: [ROUTE_WAVES + 1][experts] words
+template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds__(ROUTE_WAVES * 64) void k_route(RouteArgs a) {
+    extern __shared__ int32_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
+    int32_t* const total = lds + ROUTE_WAVES * E;
+    const int64_t t0 = int64_t(blockIdx.x) * a.chunk;
+    const int64_t t1 = min(t0 + a.chunk, int64_t(a.tokens));
+    if (CHOOSE) {
+        for (int e = tid; e < E; e += ROUTE_WAVES * 64) total[e] = 0;
+        __syncthreads();
+        for (int64_t t = t0 + wave; t < t1; t += ROUTE_WAVES) route_token<T, V>(a, t, total);
+        __syncthreads();
+        if (!GROUP)
+            for (int e = tid; e < E; e += ROUTE_WAVES * 64) a.count[int64_t(blockIdx.x) * E + e] = total[e];
+    }
+    if (!GROUP) return;
+    // before[e]: rows of expert e in earlier chunks; total[e]: in all chunks
+    __shared__ int32_t sums[ROUTE_WAVES];
+    int32_t before = 0;
+    if (!CHOOSE) {
+        for (int e = tid; e < E; e += ROUTE_WAVES * 64) {
+            int32_t sum = 0;
+            for (int c = 0; c < a.chunks; c++) {
+                const int32_t x = a.count[int64_t(c) * E + e];
+                sum += x;
+                before += c < int(blockIdx.x) ? x : 0;
+            }
+            total[e] = sum;
+        }
+    }
+    // each wavefront's own share of the chunk's pairs, in order
+    const int64_t p0 = t0 * a.k, pairs = (t1 - t0) * a.k;
+    const int64_t share = (pairs + ROUTE_WAVES * 64 - 1) / (ROUTE_WAVES * 64) * 64;
+    const int64_t first = p0 + min(int64_t(wave) * share, pairs), last = p0 + min(int64_t(wave + 1) * share, pairs);
+    int32_t* const mine = lds + wave * E;
+    for (int e = lane; e < E; e += 64) mine[e] = 0;
+    __syncthreads();
+    for (int64_t p = first + lane; p < last; p += 64) {
+        const int e = a.expert[p];
+        if (e >= 0) atomicAdd(&mine[e], 1);
+    }
+    // exclusive sum of total over the experts: one expert per thread (experts <= threads)
+    const int32_t n = tid < E ? total[tid] : 0;
+    int32_t upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int32_t rows = 0;
+    for (int w = 0; w < ROUTE_WAVES; w++) {
+        if (w < wave) upto += sums[w];
+        rows += sums[w];
+    }
+    if (tid < E) {
+        if (blockIdx.x == 0) a.offset[tid + 1] = upto;
+        int32_t at = upto - n + before;
+        for (int w = 0; w < ROUTE_WAVES; w++) {         // where each wavefront's pairs of this expert begin
+            const int32_t x = lds[w * E + tid];
+            lds[w * E + tid] = at;
+            at += x;
+        }
+    }
+    if (blockIdx.x == 0 && tid == 0) a.offset[0] = 0;
+    __syncthreads();
+    const int bits = 32 - __clz(max(E - 1, 1));
+    for (int64_t p = first + lane; p - lane < last; p += 64) {
+        const int e = p < last ? a.expert[p] : -1;
+        const uint64_t same = same_as(e, e >= 0, bits);
+        int32_t at = -1;
+        if (e >= 0) {
+            const int32_t base = mine[e];
+            at = base + __popcll(same & ((1ull << lane) - 1));
+            a.source[at] = int32_t(p / a.k);
+            wave_order();
+            if (63 - __clzll(same) == lane) mine[e] = at + 1;       // the last of its expert, after every lane's read
+        }
+        wave_order();
+        if (p < last) a.place[p] = at;
+    }
+    for (int64_t r = rows + p0 + tid; r < min(rows + p0 + pairs, int64_t(a.tokens) * a.k); r += ROUTE_WAVES * 64) a.source[r] = -1;
+}
+
+int route_chunk(int32_t tokens) { return tokens <= ROUTE_ONE ? max(tokens, 1) : max(divide_up(tokens, ROUTE_CHUNKS), ROUTE_WAVES); }
+bool route_fits(int32_t tokens, int32_t experts, int32_t k) {
+    return experts <= CSR5_ROUTE_MAX_EXPERTS && k >= 1 && k <= experts && k <= CSR5_ROUTE_MAX_K && int64_t(tokens) * k <= INT32_MAX;
+}
+
+// A wavefront per token: the row in LDS, zeros with k entries.
+template <typename T> __global__ __launch_bounds__(256) void k_route_back(int tokens, int experts, int k, const int32_t* expert, const float* weight, const float* dweight, T* dlogits, int64_t ld) {
+    __shared__ float rows[4][CSR5_ROUTE_MAX_EXPERTS];
+    const int lane = threadIdx.x & 63;
+    float* const row = rows[threadIdx.x >> 6];
+    const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (t >= tokens) return;                            // no barrier below: a wavefront's LDS accesses are in order
+    for (int e = lane; e < experts; e += 64) row[e] = 0.f;
+    wave_order();
+    float w = 0.f, d = 0.f;
+    int e = -1;
+    if (lane < k) e = expert[t * k + lane], w = weight[t * k + lane], d = dweight[t * k + lane];
+    if (uint32_t(e) >= uint32_t(experts)) e = -1, w = 0.f, d = 0.f;
+    const float mean = lanes_sum<64>(w * d);
+    if (e >= 0) row[e] = w * (d - mean);
+    wave_order();
+    for (int i = lane; i < experts; i += 64) dlogits[t * ld + i] = T(row[i]);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Back to the tokens.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_combine(int k, int rows, int n, const T* z, int64_t ldz, const int32_t* place, const float* weight, const T* residual, int64_t ldr, T* y, int64_t ldy) {
+    const int64_t t = blockIdx.x;
+    const int col = (int(blockIdx.y) * 256 + int(threadIdx.x)) * 8;
+    if (col >= n) return;
+    float sum[8] = {};
+    if (residual) load_values<8, VEC>(residual + t * ldr + col, n - col, sum);
+    for (int j = 0; j < k; j++) {
+        const int32_t r = place[t * k + j];
+        if (uint32_t(r) >= uint32_t(rows)) continue;
+        const float w = weight ? weight[t * k + j] : 1.f;
+        float v[8];
+        load_values<8, VEC>(z + r * ldz + col, n - col, v);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum[i] += w * v[i];
+    }
+    store_values<8, VEC>(y + t * ldy + col, n - col, sum);
+}
+
+// A wavefront per pair: dz and the sum for dweight in one pass over the row of z.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_combine_back(int64_t pairs, int k, int rows, int n, const T* dy, int64_t lddy, const T* z, int64_t ldz, const int32_t* place, const float* weight, T* dz, int64_t lddz, float* dweight) {
+    const int lane = threadIdx.x & 63;
+    const int64_t p = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (p >= pairs) return;
+    const int32_t r = place[p];
+    float sum = 0.f;
+    if (uint32_t(r) < uint32_t(rows)) {
+        const float w = weight[p];
+        for (int col = lane * 8; col < n; col += 512) {
+            float d[8], v[8];
+            load_values<8, VEC>(dy + p / k * lddy + col, n - col, d);
+            load_values<8, VEC>(z + r * ldz + col, n - col, v);
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum += d[i] * v[i], d[i] *= w;
+            store_values<8, VEC>(dz + r * lddz + col, n - col, d);
+        }
+    }
+    sum = lanes_sum<64>(sum);
+    if (lane == 0) dweight[p] = sum;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t csr5_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t k) {
+    if (tokens < 0 || experts < 0 || !route_fits(tokens, experts, k)) return 0;
+    const int chunks = divide_up(tokens, route_chunk(tokens));
+    return chunks <= 1 ? 0 : size_t(chunks) * size_t(experts) * 4;
+}
+
+int csr5_route(int32_t tokens, int32_t experts, int32_t k, int dtype, const void* logits, int64_t ld, int32_t* expert, float* weight,
+               int32_t* offset, int32_t* source, int32_t* place, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || tokens < 0 || experts < 0 || !offset) return CSR5_EINVAL;
+    if (!route_fits(tokens, experts, k)) return CSR5_ERANGE;
+    if (!rows_ok(logits, tokens, ld, experts, size) || (tokens > 0 && (!expert || !weight || !source || !place))) return CSR5_EINVAL;
+    const size_t need = csr5_route_workspace_bytes(tokens, experts, k);
+    if (need && (!workspace || workspace_bytes < need)) return CSR5_ENOMEM;
+    if (reinterpret_cast<uintptr_t>(workspace) & 3) return CSR5_EINVAL;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    RouteArgs a{tokens, experts, k, route_chunk(tokens), 0, logits, ld, expert, weight, offset, source, place, static_cast<int32_t*>(workspace)};
+    a.chunks = max(divide_up(tokens, a.chunk), 1);
+    const size_t lds = size_t(ROUTE_WAVES + 1) * size_t(experts) * 4;
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        auto go = [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            if (a.chunks == 1) {
+                k_route<T, V, true, true><<<1, ROUTE_WAVES * 64, lds, s>>>(a);
+            } else {
+                k_route<T, V, true, false><<<a.chunks, ROUTE_WAVES * 64, lds, s>>>(a);
+                k_route<T, V, false, true><<<a.chunks, ROUTE_WAVES * 64, lds, s>>>(a);
+            }
+        };
+        if (experts <= 64) go(std::integral_constant<int, 1>());
+        else if (experts <= 128) go(std::integral_constant<int, 2>());
+        else if (experts <= 256) go(std::integral_constant<int, 4>());
+        else if (experts <= 512) go(std::integral_constant<int, 8>());
+        else go(std::integral_constant<int, 16>());
+        return launched();
+    });
+}
+
+int csr5_route_backward(int32_t tokens, int32_t experts, int32_t k, int dtype, const int32_t* expert, const float* weight,
+                        const float* dweight, void* dlogits, int64_t ld, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || tokens < 0 || experts < 0) return CSR5_EINVAL;
+    if (!route_fits(tokens, experts, k)) return CSR5_ERANGE;
+    if (!rows_ok(dlogits, tokens, ld, experts, size) || (tokens > 0 && (!expert || !weight || !dweight))) return CSR5_EINVAL;
+    if (tokens == 0) return CSR5_OK;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        k_route_back<T><<<divide_up(tokens, 4), 256, 0, s>>>(tokens, experts, k, expert, weight, dweight, static_cast<T*>(dlogits), ld);
+        return launched();
+    });
+}
+
+int csr5_combine(int32_t tokens, int32_t k, int32_t rows, int32_t n, int dtype, const void* z, int64_t ldz, const int32_t* place,
+                 const float* weight, const void* residual, int64_t ldr, void* y, int64_t ldy, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || tokens < 0 || k < 0 || rows < 0 || n < 0) return CSR5_EINVAL;
+    if (int64_t(tokens) * k > INT32_MAX) return CSR5_ERANGE;
+    if (!rows_ok(z, rows, ldz, n, size) || !rows_ok(y, tokens, ldy, n, size) || (residual && !rows_ok(residual, tokens, ldr, n, size))) return CSR5_EINVAL;
+    if (tokens == 0 || n == 0) return CSR5_OK;
+    if (k > 0 && !place) return CSR5_EINVAL;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        const dim3 grid(tokens, divide_up(n, 2048));
+        auto go = [&](auto v) {
+            k_combine<T, decltype(v)::value><<<grid, 256, 0, s>>>(k, rows, n, static_cast<const T*>(z), ldz, place, weight, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy);
+        };
+        if (aligned(z, ldz, size, 8 * size) && aligned(y, ldy, size, 8 * size) && (!residual || aligned(residual, ldr, size, 8 * size))) go(std::true_type());
+        else go(std::false_type());
+        return launched();
+    });
+}
+
+int csr5_combine_backward(int32_t tokens, int32_t k, int32_t rows, int32_t n, int dtype, const void* dy, int64_t lddy, const void* z,
+                          int64_t ldz, const int32_t* place, const float* weight, void* dz, int64_t lddz, float* dweight, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || tokens < 0 || k < 0 || rows < 0 || n < 0) return CSR5_EINVAL;
+    if (int64_t(tokens) * k > INT32_MAX) return CSR5_ERANGE;
+    if (!rows_ok(z, rows, ldz, n, size) || !rows_ok(dy, tokens, lddy, n, size) || !rows_ok(dz, rows, lddz, n, size)) return CSR5_EINVAL;
+    const int64_t pairs = int64_t(tokens) * k;
+    if (pairs == 0) return CSR5_OK;
+    if (!place || !weight || !dweight) return CSR5_EINVAL;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        auto go = [&](auto v) {
+            k_combine_back<T, decltype(v)::value><<<divide_up(pairs, 4), 256, 0, s>>>(pairs, k, rows, n, static_cast<const T*>(dy), lddy, static_cast<const T*>(z), ldz, place, weight, static_cast<T*>(dz), lddz, dweight);
+        };
+        if (aligned(z, ldz, size, 8 * size) && aligned(dy, lddy, size, 8 * size) && aligned(dz, lddz, size, 8 * size)) go(std::true_type());
+        else go(std::false_type());
+        return launched();
+    });
+}
+
+int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const void* x, int64_t ldx, uint8_t* q, int64_t ldq, float* scale,
+                  int64_t scale_row, int64_t scale_block, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || rows < 0 || n < 0 || (block_rows != 1 && block_rows != CSR5_F8_BLOCK)) return CSR5_EINVAL;
+    if (!rows_ok(x, rows, ldx, n, size) || !rows_ok(q, rows, ldq, n, 1)) return CSR5_EINVAL;
+    if (rows == 0 || n == 0) return CSR5_OK;
+    if (!scale || (reinterpret_cast<uintptr_t>(scale) & 3)) return CSR5_EINVAL;
+    const int64_t blocks = divide_up(n, CSR5_F8_BLOCK);
+    const int64_t groups = block_rows == 1 ? (int64_t(rows) * blocks + 15) / 16 : divide_up(rows, CSR5_F8_BLOCK) * blocks;
+    if (groups > INT32_MAX) return CSR5_ERANGE;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        auto go = [&](auto r, auto v) {
+            k_quantise<T, decltype(r)::value, decltype(v)::value><<<uint32_t(groups), 256, 0, s>>>(rows, n, static_cast<const T*>(x), ldx, q, ldq, scale, scale_row, scale_block);
+        };
+        auto by = [&](auto v) {
+            if (block_rows == 1) go(std::integral_constant<int, 1>(), v);
+            else go(std::integral_constant<int, CSR5_F8_BLOCK>(), v);
+        };
+        if (aligned(x, ldx, size, 8 * size) && aligned(q, ldq, 1, 8)) by(std::true_type());
+        else by(std::false_type());
+        return launched();
+    });
+}
+
+int csr5_rmsnorm(int32_t rows, int32_t n, int dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* gain,
+                 float eps, void* h, int64_t ldh, void* y, int64_t ldy, uint8_t* q, int64_t ldq, float* scale, int64_t scale_row,
+                 int64_t scale_block, float* rstd, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || rows < 0 || n < 0) return CSR5_EINVAL;
+    if (n > CSR5_NORM_MAX_N) return CSR5_ERANGE;
+    if (!rows_ok(x, rows, ldx, n, size) || (residual && !rows_ok(residual, rows, ldr, n, size)) || (h && !rows_ok(h, rows, ldh, n, size)) ||
+        (y && !rows_ok(y, rows, ldy, n, size)) || (q && (!rows_ok(q, rows, ldq, n, 1) || !scale)) || (reinterpret_cast<uintptr_t>(gain) % size))
+        return CSR5_EINVAL;
+    if (rows == 0 || n == 0) return CSR5_OK;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        const NormArgs<T> a{n, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<const T*>(gain), ldx, ldr, eps,
+                            static_cast<T*>(h), static_cast<T*>(y), ldh, ldy, q, ldq, scale, scale_row, scale_block, rstd};
+        const size_t wide = 8 * size;
+        const bool v = aligned(x, ldx, size, wide) && (!residual || aligned(residual, ldr, size, wide)) && aligned(gain, 0, size, wide) &&
+                       (!h || aligned(h, ldh, size, wide)) && (!y || aligned(y, ldy, size, wide)) && (!q || aligned(q, ldq, 1, 8));
+        norm_shape(n, [&](auto tpb, auto nv) {
+            constexpr int TPB = decltype(tpb)::value, NV = decltype(nv)::value;
+            if (v) k_rmsnorm<T, TPB, NV, true><<<rows, TPB, 0, s>>>(a);
+            else k_rmsnorm<T, TPB, NV, false><<<rows, TPB, 0, s>>>(a);
+        });
+        return launched();
+    });
+}
+
+size_t csr5_rmsnorm_workspace_bytes(int32_t rows, int32_t n) {
+    if (rows < 0 || n < 0 || n > CSR5_NORM_MAX_N) return 0;
+    return size_t(rows < NORM_GROUPS ? rows : NORM_GROUPS) * size_t(n) * 4;
+}
+
+int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void* h, int64_t ldh, const void* gain, const float* rstd, const void* dy,
+                          int64_t lddy, const void* residual_grad, int64_t ldrg, void* dh, int64_t lddh, float* dgain, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+    const size_t size = type_bytes(dtype);
+    if (!size || rows < 0 || n < 0) return CSR5_EINVAL;
+    if (n > CSR5_NORM_MAX_N) return CSR5_ERANGE;
+    if (!rows_ok(h, rows, ldh, n, size) || !rows_ok(dy, rows, lddy, n, size) || !rows_ok(dh, rows, lddh, n, size) ||
+        (residual_grad && !rows_ok(residual_grad, rows, ldrg, n, size)) || (reinterpret_cast<uintptr_t>(gain) % size) || (rows > 0 && !rstd))
+        return CSR5_EINVAL;
+    if (dgain && rows > 0 && n > 0 && (!workspace || workspace_bytes < csr5_rmsnorm_workspace_bytes(rows, n))) return CSR5_ENOMEM;
+    if (reinterpret_cast<uintptr_t>(workspace) & 3) return CSR5_EINVAL;
+    if (n == 0 || (rows == 0 && !dgain)) return CSR5_OK;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const int groups = rows < NORM_GROUPS ? rows : NORM_GROUPS;
+    return with_type(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        const NormBackArgs<T> a{rows, n, static_cast<const T*>(h), static_cast<const T*>(gain), static_cast<const T*>(dy), static_cast<const T*>(residual_grad),
+                                ldh, lddy, ldrg, rstd, static_cast<T*>(dh), lddh, dgain ? static_cast<float*>(workspace) : nullptr};
+        const size_t wide = 8 * size;
+        const bool v = aligned(h, ldh, size, wide) && aligned(dy, lddy, size, wide) && aligned(dh, lddh, size, wide) && aligned(gain, 0, size, wide) &&
+                       (!residual_grad || aligned(residual_grad, ldrg, size, wide));
+        if (rows > 0)
+            norm_shape(n, [&](auto tpb, auto nv) {
+                constexpr int TPB = decltype(tpb)::value, NV = decltype(nv)::value;
+                if (v) k_rmsnorm_back<T, TPB, NV, true><<<groups, TPB, 0, s>>>(a);
+                else k_rmsnorm_back<T, TPB, NV, false><<<groups, TPB, 0, s>>>(a);
+            });
+        if (dgain) k_columns<<<divide_up(n, 32), 1024, 0, s>>>(rows > 0 ? groups : 0, n, static_cast<const float*>(workspace), dgain);
+        return launched();
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,343 @@
+// libcsr5: products of a layer of experts -- grouped by expert over ragged groups, in 16 bits with their gradients and in
+// 8 bits with a scale for each block of 128.  The C ABI is declared in include/csr5.h.
+//
+// Every product here is out[i][j] = sum_c X[i][c] W[j][c]:
+//
+//   FWD   y = x w^T      i: rows of a group    j: n      c: k       X, W as they lie in memory
+//   DX    dx = dy w      i: rows of a group    j: k      c: n       W lies with j contiguous: transposed on the way
+//   DW    dw = dy^T x    i: n                  j: k      c: rows    both transposed on the way
+//
+// The matrix instructions take W for their first operand and X for their second, so that a lane of the result holds
+// four neighbouring columns j of one row i (one row's scale, one 8-byte store).
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "csr5.h"
+#include "numbers.h"
+
+namespace {
+
+enum { FWD, DX, DW };
+
+typedef uint8_t f8;
+template <typename T> constexpr bool is_f8 = std::is_same<T, f8>::value;
+
+struct Product {
+    const void* x;              // FWD: x; DX, DW: dy
+    int64_t ldx;
+    const void* w;              // FWD, DX: w; DW: x
+    int64_t ldw, w_group;
+    void* y;
+    int64_t ldy, y_group;       // y_group: DW
+    const int32_t* offset;      // NULL: one group of all rows
+    const int32_t* source;      // of the rows of x, wherever x is; NULL: themselves
+    int32_t source_rows;        // rows that a source may name
+    int32_t groups, rows;
+    int32_t out_rows;           // DW: n
+    int32_t cols, depth;        // j and c (DW: depth is the group's)
+    const float *xs, *ws;       // 8 bits: the scales
+    int64_t xs_row, xs_block, ws_row, ws_block, ws_group;
+    int32_t w_rows;
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+// Which rows
+// ---------------------------------------------------------------------------------------------------------------
+struct Span {
+    int group;
+    int32_t first, last;        // rows [first, last) of the group that are this workgroup's
+};
+
+__device__ __forceinline__ int32_t offset_at(const Product& a, int g) { return min(max(a.offset[g], 0), a.rows); }
+__device__ __forceinline__ Span group_span(const Product& a, int g) {
+    if (!a.offset) return {0, 0, a.rows};
+    const int32_t first = offset_at(a, g);
+    return {g, first, max(offset_at(a, g + 1), first)};
+}
+
+// The t-th tile of BM rows, counted through the groups in order; group -1: there are fewer.  The whole wavefront takes part:
+// a lane per group.  At most rows / BM + groups tiles.
+template <int BM> __device__ __forceinline__ Span find_tile(const Product& a, int32_t t) {
+    if (!a.offset) {
+        const int64_t first = int64_t(t) * BM;
+        return {first < a.rows ? 0 : -1, int32_t(min(first, int64_t(a.rows))), int32_t(min(first + BM, int64_t(a.rows)))};
+    }
+    const int lane = threadIdx.x & 63;
+    int32_t before = 0;
+    for (int g0 = 0; g0 < a.groups; g0 += 64) {
+        const int g = g0 + lane;
+        Span s{-1, 0, 0};
+        if (g < a.groups) s = group_span(a, g);
+        const int32_t tiles = (s.last - s.first + BM - 1) / BM;
+        int32_t upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const uint64_t past = __ballot(before + upto > t);
+        if (past) {
+            const int l = __ffsll((unsigned long long)past) - 1;
+            const int32_t first = __shfl(s.first, l) + (t - before - __shfl(upto - tiles, l)) * BM;
+            return {g0 + l, first, min(first + BM, __shfl(s.last, l))};
+        }
+        before += __shfl(upto, 63);
+    }
+    return {-1, 0, 0};
+}
+
+__device__ __forceinline__ int64_t source_of(const Product& a, int64_t row) {       // -1: a row of zeros
+    const int64_t r = a.source ? a.source[row] : row;
+    return r >= 0 && r < a.source_rows ? r : -1;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// The matrix instructions: 16 x 16 results from 16 bytes (8 bits: 32) of each lane
+// ---------------------------------------------------------------------------------------------------------------
+typedef vec<float, 4> f32x4;
+typedef vec<bf16, 8> bf16x8;
+typedef vec<f16, 8> f16x8;
+
+__device__ __forceinline__ f32x4 multiply(const uint4& w, const uint4& x, f32x4 acc, bf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(const uint4& w, const uint4& x, f32x4 acc, f16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), acc, 0, 0, 0);
+}
+// 8 e4m3 values in 16 bits, exactly
+__device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b) {
+    const vec<float, 2> v[4] = {__builtin_amdgcn_cvt_pk_f32_fp8(int(a), false), __builtin_amdgcn_cvt_pk_f32_fp8(int(a), true),
+                                __builtin_amdgcn_cvt_pk_f32_fp8(int(b), false), __builtin_amdgcn_cvt_pk_f32_fp8(int(b), true)};
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = bf16(v[i / 2][i % 2]);
+    return r;
+}
+// In 8 bits: by the instruction for 16, which adds up in 32 bits.  That for 8 bits adds products in units of 2^-15 or so of
+// the largest one (1 or 3.5 beside 448 * 448 is lost, measured); few products and odd sizes would show it.
+__device__ __forceinline__ f32x4 multiply(const uint4& w, const uint4& x, f32x4 acc, f8) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.x, w.y), widen(x.x, x.y), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.z, w.w), widen(x.z, x.w), acc, 0, 0, 0);
+}
+
+// Four neighbouring values of a row of y.
+template <typename Y, bool VEC> __device__ __forceinline__ void store_four(Y* p, int have, f32x4 v) {
+    const float f[4] = {v[0], v[1], v[2], v[3]};
+    store_values<4, VEC>(p, have, f);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// The plain kernel: right for any strides, alignment and sizes.  128 x 128 results per workgroup of four wavefronts; the
+// depth goes by in steps of 128 bytes (in 8 bits a block of scales) through registers into LDS, where rows of both
+// operands are contiguous along it.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int PLAIN_TILE = 128;
+constexpr int PLAIN_PITCH = 128 + 16;       // bytes of a row in LDS
+
+template <typename T, typename Y, int OP> __global__ __launch_bounds__(256) void k_product_plain(Product a) {
+    constexpr int SIZE = sizeof(T), STEP = 128 / SIZE;
+    __shared__ __align__(16) uint8_t lds[2][PLAIN_TILE * PLAIN_PITCH];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int col_tiles = (a.cols + PLAIN_TILE - 1) / PLAIN_TILE;
+    const int j0 = int(blockIdx.x % col_tiles) * PLAIN_TILE;
+    Span s;
+    int32_t i0;                             // first row of the results
+    int32_t i_end, depth;
+    if (OP == DW) {
+        const int row_tiles = (a.out_rows + PLAIN_TILE - 1) / PLAIN_TILE;
+        s = group_span(a, int(blockIdx.x / col_tiles / row_tiles));
+        i0 = int32_t(blockIdx.x / col_tiles % row_tiles) * PLAIN_TILE;
+        i_end = a.out_rows, depth = s.last - s.first;
+    } else {
+        s = find_tile<PLAIN_TILE>(a, int32_t(blockIdx.x / col_tiles));
+        if (s.group < 0) return;
+        i0 = s.first, i_end = s.last, depth = a.depth;
+    }
+    const T* const w = static_cast<const T*>(a.w) + (OP == DW ? 0 : s.group * a.w_group);
+
+    // One value of each operand, 0 outside.
+    auto x_at = [&](int32_t i, int32_t c) -> T {
+        if (i >= i_end || c >= depth) return T(0);
+        if (OP == DW) return static_cast<const T*>(a.x)[int64_t(s.first + c) * a.ldx + i];
+        const int64_t r = OP == FWD ? source_of(a, i) : i;
+        return r < 0 ? T(0) : static_cast<const T*>(a.x)[r * a.ldx + c];
+    };
+    auto w_at = [&](int32_t j, int32_t c) -> T {
+        if (j >= a.cols || c >= depth) return T(0);
+        if (OP == FWD) return w[int64_t(j) * a.ldw + c];
+        if (OP == DX) return w[int64_t(c) * a.ldw + j];
+        const int64_t r = source_of(a, s.first + c);
+        return r < 0 ? T(0) : w[r * a.ldw + j];
+    };
+    f32x4 acc[4][4] = {};                   // [j][i] of this wavefront's 64 x 64
+    const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64;
+    for (int32_t c0 = 0; c0 < depth; c0 += STEP) {
+        // neighbouring threads along what is contiguous in memory
+        for (int e = tid; e < PLAIN_TILE * STEP; e += 256) {
+            const int i = OP == DW ? e % PLAIN_TILE : e / STEP, c = OP == DW ? e / PLAIN_TILE : e % STEP;
+            *reinterpret_cast<T*>(&lds[0][i * PLAIN_PITCH + c * SIZE]) = x_at(i0 + i, c0 + c);
+        }
+        for (int e = tid; e < PLAIN_TILE * STEP; e += 256) {
+            const int j = OP != FWD ? e % PLAIN_TILE : e / STEP, c = OP != FWD ? e / PLAIN_TILE : e % STEP;
+            *reinterpret_cast<T*>(&lds[1][j * PLAIN_PITCH + c * SIZE]) = w_at(j0 + j, c0 + c);
+        }
+        __syncthreads();
+        f32x4 part[4][4] = {};
+#pragma unroll
+        for (int k = 0; k < 128; k += 64) {
+            uint4 xv[4], wv[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                xv[i] = *reinterpret_cast<const uint4*>(&lds[0][(wi + i * 16 + (lane & 15)) * PLAIN_PITCH + k + (lane >> 4) * 16]);
+                wv[i] = *reinterpret_cast<const uint4*>(&lds[1][(wj + i * 16 + (lane & 15)) * PLAIN_PITCH + k + (lane >> 4) * 16]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    f32x4& to = is_f8<T> ? part[j][i] : acc[j][i];
+                    to = multiply(wv[j], xv[i], to, T());
+                }
+        }
+        if (is_f8<T>) {
+            const int b = c0 / CSR5_F8_BLOCK;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int32_t row = i0 + wi + i * 16 + (lane & 15);
+                const int64_t r = row < i_end ? source_of(a, row) : -1;
+                const float xs = r < 0 ? 0.f : a.xs[r * a.xs_row + b * a.xs_block];
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        const int32_t col = j0 + wj + j * 16 + (lane >> 4) * 4 + q;
+                        const float ws = col < a.cols ? a.ws[s.group * a.ws_group + col / a.w_rows * a.ws_row + b * a.ws_block] : 0.f;
+                        acc[j][i][q] += part[j][i][q] * (xs * ws);
+                    }
+            }
+        }
+        __syncthreads();
+    }
+    Y* const y = static_cast<Y*>(a.y) + (OP == DW ? s.group * a.y_group : 0);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int32_t row = i0 + wi + i * 16 + (lane & 15);
+        if (row >= i_end) continue;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int32_t col = j0 + wj + j * 16 + (lane >> 4) * 4;
+            store_four<Y, false>(y + int64_t(row) * a.ldy + col, a.cols - col, acc[j][i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T, typename Y, int OP> int launch_plain(const Product& a, hipStream_t s) {
+    const int64_t cols = divide_up(a.cols, PLAIN_TILE);
+    const int64_t tiles = OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, PLAIN_TILE) : int64_t(divide_up(a.rows, PLAIN_TILE)) + (a.offset ? a.groups : 0);
+    if (tiles * cols > INT32_MAX) return CSR5_ERANGE;
+    k_product_plain<T, Y, OP><<<uint32_t(tiles * cols), 256, 0, s>>>(a);
+    return launched();
+}
+
+template <typename T, typename Y, int OP> int launch(const Product& a, hipStream_t s) { return launch_plain<T, Y, OP>(a, s); }
+
+bool half_type(int dtype) { return dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16; }
+template <int OP> int launch_half(int dtype, const Product& a, void* hip_stream) {
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    return dtype == CSR5_DTYPE_BF16 ? launch<bf16, bf16, OP>(a, s) : launch<f16, f16, OP>(a, s);
+}
+
+int launch_f8(int dtype, const Product& a, void* hip_stream) {
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    switch (dtype) {
+        case CSR5_DTYPE_BF16: return launch<f8, bf16, FWD>(a, s);
+        case CSR5_DTYPE_F16: return launch<f8, f16, FWD>(a, s);
+        default: return launch<f8, float, FWD>(a, s);
+    }
+}
+
+bool groups_ok(int32_t groups, int32_t rows, int32_t n, int32_t k, const int32_t* offset) {
+    return groups >= 0 && rows >= 0 && n >= 0 && k >= 0 && (groups == 0 || offset) && !(reinterpret_cast<uintptr_t>(offset) & 3);
+}
+// what `source` may name is there
+bool source_ok(int32_t rows, int32_t x_rows, const int32_t* source) {
+    return x_rows >= 0 && (source || x_rows >= rows) && !(reinterpret_cast<uintptr_t>(source) & 3);
+}
+
+}  // namespace
+
+extern "C" {
+
+int csr5_grouped_gemm(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const void* x, int32_t x_rows,
+                      int64_t ldx, const int32_t* source, const void* w, int64_t ldw, int64_t w_group, void* y, int64_t ldy, void* hip_stream) {
+    if (!half_type(dtype) || !groups_ok(groups, rows, n, k, offset) || !source_ok(rows, x_rows, source)) return CSR5_EINVAL;
+    if (!rows_ok(x, x_rows, ldx, k, 2) || !rows_ok(w, int64_t(groups) * n, ldw, k, 2) || !rows_ok(y, rows, ldy, n, 2)) return CSR5_EINVAL;
+    if (groups == 0 || rows == 0 || n == 0) return CSR5_OK;
+    Product a{};
+    a.x = x, a.ldx = ldx, a.w = w, a.ldw = ldw, a.w_group = w_group, a.y = y, a.ldy = ldy;
+    a.offset = offset, a.source = source, a.source_rows = x_rows, a.groups = groups, a.rows = rows, a.cols = n, a.depth = k;
+    return launch_half<FWD>(dtype, a, hip_stream);
+}
+
+int csr5_grouped_gemm_dx(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const void* dy, int64_t lddy,
+                         const void* w, int64_t ldw, int64_t w_group, void* dx, int64_t lddx, void* hip_stream) {
+    if (!half_type(dtype) || !groups_ok(groups, rows, n, k, offset)) return CSR5_EINVAL;
+    if (!rows_ok(dy, rows, lddy, n, 2) || !rows_ok(w, int64_t(groups) * n, ldw, k, 2) || !rows_ok(dx, rows, lddx, k, 2)) return CSR5_EINVAL;
+    if (groups == 0 || rows == 0 || k == 0) return CSR5_OK;
+    Product a{};
+    a.x = dy, a.ldx = lddy, a.w = w, a.ldw = ldw, a.w_group = w_group, a.y = dx, a.ldy = lddx;
+    a.offset = offset, a.groups = groups, a.rows = rows, a.cols = k, a.depth = n;
+    return launch_half<DX>(dtype, a, hip_stream);
+}
+
+int csr5_grouped_gemm_dw(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const void* dy, int64_t lddy,
+                         const void* x, int32_t x_rows, int64_t ldx, const int32_t* source, void* dw, int64_t lddw, int64_t dw_group, void* hip_stream) {
+    if (!half_type(dtype) || !groups_ok(groups, rows, n, k, offset) || !source_ok(rows, x_rows, source)) return CSR5_EINVAL;
+    if (!rows_ok(dy, rows, lddy, n, 2) || !rows_ok(x, x_rows, ldx, k, 2) || !rows_ok(dw, int64_t(groups) * n, lddw, k, 2)) return CSR5_EINVAL;
+    if (groups == 0 || n == 0 || k == 0) return CSR5_OK;
+    Product a{};
+    a.x = dy, a.ldx = lddy, a.w = x, a.ldw = ldx, a.y = dw, a.ldy = lddw, a.y_group = dw_group;
+    a.offset = offset, a.source = source, a.source_rows = x_rows, a.groups = groups, a.rows = rows, a.out_rows = n, a.cols = k;
+    return launch_half<DW>(dtype, a, hip_stream);
+}
+
+int csr5_grouped_gemm_f8(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const uint8_t* x, int32_t x_rows,
+                         int64_t ldx, const float* x_scale, int64_t xs_row, int64_t xs_block, const int32_t* source, const uint8_t* w, int64_t ldw,
+                         int64_t w_group, const float* w_scale, int32_t w_rows, int64_t ws_row, int64_t ws_block, int64_t ws_group, void* y,
+                         int64_t ldy, void* hip_stream) {
+    const size_t size = half_type(dtype) ? 2 : 4;
+    if (!(half_type(dtype) || dtype == CSR5_DTYPE_F32) || !groups_ok(groups, rows, n, k, offset) || !source_ok(rows, x_rows, source)) return CSR5_EINVAL;
+    if (w_rows != 1 && w_rows != CSR5_F8_BLOCK) return CSR5_EINVAL;
+    if (!rows_ok(x, x_rows, ldx, k, 1) || !rows_ok(w, int64_t(groups) * n, ldw, k, 1) || !rows_ok(y, rows, ldy, n, size)) return CSR5_EINVAL;
+    if (groups == 0 || rows == 0 || n == 0) return CSR5_OK;
+    if (k > 0 && (!x_scale || !w_scale || ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale)) & 3))) return CSR5_EINVAL;
+    Product a{};
+    a.x = x, a.ldx = ldx, a.w = w, a.ldw = ldw, a.w_group = w_group, a.y = y, a.ldy = ldy;
+    a.offset = offset, a.source = source, a.source_rows = x_rows, a.groups = groups, a.rows = rows, a.cols = n, a.depth = k;
+    a.xs = x_scale, a.xs_row = xs_row, a.xs_block = xs_block;
+    a.ws = w_scale, a.ws_row = ws_row, a.ws_block = ws_block, a.ws_group = ws_group, a.w_rows = w_rows;
+    return launch_f8(dtype, a, hip_stream);
+}
+
+int csr5_gemm_f8(int32_t m, int32_t n, int32_t k, int dtype, const uint8_t* x, int64_t ldx, const float* x_scale, int64_t xs_row, int64_t xs_block,
+                 const uint8_t* w, int64_t ldw, const float* w_scale, int32_t w_rows, int64_t ws_row, int64_t ws_block, void* y, int64_t ldy,
+                 void* hip_stream) {
+    const size_t size = half_type(dtype) ? 2 : 4;
+    if (!(half_type(dtype) || dtype == CSR5_DTYPE_F32) || m < 0 || n < 0 || k < 0 || (w_rows != 1 && w_rows != CSR5_F8_BLOCK)) return CSR5_EINVAL;
+    if (!rows_ok(x, m, ldx, k, 1) || !rows_ok(w, n, ldw, k, 1) || !rows_ok(y, m, ldy, n, size)) return CSR5_EINVAL;
+    if (m == 0 || n == 0) return CSR5_OK;
+    if (k > 0 && (!x_scale || !w_scale || ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale)) & 3))) return CSR5_EINVAL;
+    Product a{};
+    a.x = x, a.ldx = ldx, a.w = w, a.ldw = ldw, a.y = y, a.ldy = ldy;
+    a.source_rows = m, a.groups = 1, a.rows = m, a.cols = n, a.depth = k;
+    a.xs = x_scale, a.xs_row = xs_row, a.xs_block = xs_block;
+    a.ws = w_scale, a.ws_row = ws_row, a.ws_block = ws_block, a.w_rows = w_rows;
+    return launch_f8(dtype, a, hip_stream);
+}
+
+}  // extern "C"

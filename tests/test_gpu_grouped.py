@@ -1,0 +1,218 @@
+"""Products grouped by expert and products in 8 bits against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from layer_util import DEV, EPS32, close, matrix, meaning, offsets, place_in, quantised, room, untouched
+from paper_1503_05032_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+HALF = [torch.bfloat16, torch.float16]
+ids = lambda t: str(t).replace("torch.", "")  # noqa: E731
+
+GROUPS = {
+    "one": [1],
+    "singles": [1, 0, 1, 1, 0],
+    "edges": [127, 128, 129, 0, 15, 16, 17],
+    "large": [255, 1, 257, 0, 64],
+    "lopsided": [0, 0, 700, 3, 0],
+    "none": [0, 0, 0],
+}
+SHAPES = [(1, 1, "plain"), (17, 33, "odd"), (128, 64, "plain"), (136, 200, "wide"), (264, 328, "plain"), (300, 129, "odd"), (512, 640, "plain")]
+
+
+def experts(gen, groups, n, k, dtype, layout, scale=1.0):
+    """Weights [groups, n, k], a view whose surroundings are NaN unless "plain"."""
+    if layout == "plain":
+        return (torch.randn(groups, n, k, generator=gen) * scale).to(dtype).to(DEV)
+    flat = matrix(gen, groups * n, k, dtype, layout, scale)
+    return flat.unflatten(0, (groups, n))
+
+
+def source_for(gen, rows, x_rows, bad=True):
+    s = torch.randint(0, x_rows, (rows,), generator=gen, dtype=torch.int32)
+    if bad and rows > 4:
+        s[1], s[3] = -1, x_rows             # rows of zeros
+    return s
+
+
+def taken(x, source, rows):
+    """The rows of x that the products see, in 64 bits."""
+    x = x.double().cpu()
+    if source is None:
+        return x[:rows]
+    s = source.long()
+    there = (s >= 0) & (s < x.shape[0])
+    return x[torch.where(there, s, 0)] * there[:, None]
+
+
+def spans(sizes):
+    at = 0
+    for g, c in enumerate(sizes):
+        yield g, at, at + c
+        at += c
+
+
+@pytest.mark.parametrize("dtype", HALF, ids=ids)
+@pytest.mark.parametrize("groups", GROUPS)
+@pytest.mark.parametrize("n,k,layout", SHAPES)
+def test_grouped(dtype, groups, n, k, layout):
+    sizes = GROUPS[groups]
+    g = torch.Generator().manual_seed(n * k)
+    rows, tail = sum(sizes), 3                              # rows in no group stay as they are
+    offset = offsets(sizes)
+    w = experts(g, len(sizes), n, k, dtype, layout)
+    wc = w.double().cpu()
+    x = matrix(g, rows + tail, k, dtype, layout)
+    source = source_for(g, rows + tail, rows + tail)
+    for s in (None, source):
+        big, y = room(rows + tail, n, dtype, layout)
+        B.csr5_grouped_gemm(x, w, offset, y, source=None if s is None else s.to(DEV))
+        untouched(big, rows + tail, n, layout)
+        xc = taken(x, s, rows + tail)
+        ref, size = torch.full((rows + tail, n), 77.0, dtype=torch.float64).to(dtype).double(), torch.zeros(rows + tail, n, dtype=torch.float64)
+        for i, a, b in spans(sizes):
+            ref[a:b], size[a:b] = xc[a:b] @ wc[i].T, xc[a:b].abs() @ wc[i].T.abs()
+        close(y, ref, dtype, (k + 8) * EPS32 * size, "y")
+        dy = matrix(g, rows + tail, n, dtype, layout)
+        dyc = dy.double().cpu()
+        big, dx = room(rows + tail, k, dtype, layout)
+        B.csr5_grouped_gemm_dx(dy, w, offset, dx)
+        untouched(big, rows + tail, k, layout)
+        ref, size = torch.full((rows + tail, k), 77.0, dtype=torch.float64).to(dtype).double(), torch.zeros(rows + tail, k, dtype=torch.float64)
+        for i, a, b in spans(sizes):
+            ref[a:b], size[a:b] = dyc[a:b] @ wc[i], dyc[a:b].abs() @ wc[i].abs()
+        close(dx, ref, dtype, (n + 8) * EPS32 * size, "dx")
+        big, dw = room(len(sizes) * n, k, dtype, layout)
+        B.csr5_grouped_gemm_dw(dy, x, offset, dw.unflatten(0, (len(sizes), n)), source=None if s is None else s.to(DEV))
+        untouched(big, len(sizes) * n, k, layout)
+        ref, size = torch.zeros(len(sizes) * n, k, dtype=torch.float64), torch.zeros(len(sizes) * n, k, dtype=torch.float64)
+        for i, a, b in spans(sizes):
+            ref[i * n:(i + 1) * n], size[i * n:(i + 1) * n] = dyc[a:b].T @ xc[a:b], dyc[a:b].T.abs() @ xc[a:b].abs()
+        close(dw, ref, dtype, (max(sizes) + 8) * EPS32 * size, "dw")
+
+
+@pytest.mark.parametrize("dtype", HALF, ids=ids)
+def test_grouped_gradients_are_those_of_differences(dtype):
+    """With small whole numbers every sum is exact, and so is a difference of the (linear) product: it has to equal the
+    gradients' prediction bit by bit."""
+    g = torch.Generator().manual_seed(11)
+    sizes, n, k = [3, 0, 20, 1], 24, 40
+    rows, groups = sum(sizes), 4
+    draw = lambda *shape: torch.randint(-1, 2, shape, generator=g).to(dtype).to(DEV)  # noqa: E731
+    x, w, dy, offset = draw(9, k), draw(groups, n, k), draw(rows, n), offsets(sizes)
+    source = source_for(g, rows, 9, bad=False).to(DEV)
+
+    def product(x, w):
+        y = torch.zeros(rows, n, dtype=dtype, device=DEV)
+        B.csr5_grouped_gemm(x, w, offset, y, source=source)
+        return y.double()
+
+    dx, dw = torch.zeros(rows, k, dtype=dtype, device=DEV), torch.zeros_like(w)
+    B.csr5_grouped_gemm_dx(dy, w, offset, dx)
+    B.csr5_grouped_gemm_dw(dy, x, offset, dw, source=source)
+    for _ in range(3):
+        ex, ew = draw(9, k), draw(groups, n, k)
+        moved = ((product(x + ex, w) - product(x, w)) * dy.double()).sum()
+        assert moved == (dx.double() * ex[source.long()].double()).sum()
+        moved = ((product(x, w + ew) - product(x, w)) * dy.double()).sum()
+        assert moved == (dw.double() * ew.double()).sum()
+
+
+@pytest.mark.parametrize("offset", [[0, 5, 3, 9, 40], [-4, 2, 2, 1000, 6], [9, 9, 9, 9, 9], [0, 0, 0, 0, 30]])
+def test_offsets_outside_stay_inside(offset):
+    """Clamped to the rows; a group that ends before it begins is empty."""
+    g = torch.Generator().manual_seed(0)
+    rows, n, k = 30, 32, 48
+    x, w = matrix(g, rows, k, torch.bfloat16), experts(g, 4, n, k, torch.bfloat16, "plain")
+    o = torch.tensor(offset, dtype=torch.int32, device=DEV)
+    big, y = room(rows, n, torch.bfloat16)
+    B.csr5_grouped_gemm(x, w, o, y)
+    untouched(big, rows, n, "plain")
+    dw = torch.empty(4, n, k, dtype=torch.bfloat16, device=DEV)
+    B.csr5_grouped_gemm_dw(y, x, o, dw)
+    c = [min(max(v, 0), rows) for v in offset]
+    for i in range(4):
+        if c[i + 1] <= c[i]:
+            assert (dw[i] == 0).all()
+
+
+def test_masked_rows_do_not_spread():
+    """A NaN or infinity in a row of x stays in that row's results; rows in no group are not read."""
+    g = torch.Generator().manual_seed(0)
+    for k in (64, 72, 100, 128):
+        x, w = matrix(g, 40, k, torch.bfloat16), experts(g, 2, 256, k, torch.bfloat16, "plain")
+        offset = offsets([17, 20])
+        x[5], x[38] = math.nan, math.nan
+        y = torch.zeros(40, 256, dtype=torch.bfloat16, device=DEV)
+        B.csr5_grouped_gemm(x, w, offset, y)
+        bad = torch.isnan(y).any(1).cpu()
+        assert bad[5] and bad.sum() == 1 and (y[37:] == 0).all()
+        dy = matrix(g, 40, 256, torch.bfloat16)
+        dy[37:] = math.inf
+        x[5] = 0
+        dw = torch.empty(2, 256, k, dtype=torch.bfloat16, device=DEV)
+        B.csr5_grouped_gemm_dw(dy, x, offset, dw)
+        assert torch.isfinite(dw).all()
+
+
+# ---------------------------------------------------------------------------------------------------------------- 8 bits
+def f8_operand(gen, rows, k, block_rows, layout):
+    q, scale = quantised(torch.randn(rows, k, generator=gen) * 2, block_rows)
+    return place_in(q, layout), scale.to(DEV), meaning(q, scale, block_rows)
+
+
+F8_SHAPES = [(1, 1, 1, "plain"), (5, 33, 17, "odd"), (16, 128, 128, "plain"), (17, 130, 144, "wide"), (33, 257, 260, "plain"), (129, 384, 512, "wide"),
+             (200, 129, 399, "odd"), (260, 264, 1040, "plain"), (8, 1024, 2048, "plain")]
+
+
+@pytest.mark.parametrize("dtype", HALF + [torch.float32], ids=ids)
+@pytest.mark.parametrize("w_rows", [128, 1])
+@pytest.mark.parametrize("m,n,k,layout", F8_SHAPES)
+def test_f8(dtype, w_rows, m, n, k, layout):
+    g = torch.Generator().manual_seed(m + n + k)
+    x, xs, xc = f8_operand(g, m, k, 1, layout)
+    w, ws, wc = f8_operand(g, n, k, w_rows, layout)
+    ref, slack = xc @ wc.T, (k + 8) * EPS32 * (xc.abs() @ wc.T.abs())
+    for scales in (xs, xs.T.contiguous().T):                            # in either order
+        big, y = room(m, n, dtype, layout)
+        B.csr5_gemm_f8(x, scales, w, ws, y, w_rows=w_rows)
+        untouched(big, m, n, layout)
+        close(y, ref, dtype, slack)
+
+
+@pytest.mark.parametrize("w_rows", [128, 1])
+@pytest.mark.parametrize("groups", GROUPS)
+@pytest.mark.parametrize("n,k,layout", [(33, 17, "odd"), (128, 128, "plain"), (264, 400, "wide"), (384, 512, "plain")])
+def test_grouped_f8(w_rows, groups, n, k, layout):
+    sizes = GROUPS[groups]
+    g = torch.Generator().manual_seed(n + k)
+    rows, tail, x_rows = sum(sizes), 2, max(sum(sizes) // 2, 1)
+    operands = [f8_operand(g, n, k, w_rows, "plain") for _ in sizes]
+    flat = place_in(torch.cat([o[0].cpu() for o in operands]), layout)
+    w, ws = flat.unflatten(0, (len(sizes), n)), torch.stack([o[1] for o in operands])
+    x, xs, xc = f8_operand(g, x_rows, k, 1, layout)
+    source = source_for(g, rows + tail, x_rows)
+    xs[0] = 1e30 if x_rows > 1 else 1.0     # a large scale belongs to its row alone
+    xc = meaning(x.cpu(), xs.cpu(), 1)
+    big, y = room(rows + tail, n, torch.bfloat16, layout)
+    B.csr5_grouped_gemm_f8(x, xs, w, ws, offsets(sizes), y, w_rows=w_rows, source=source.to(DEV))
+    untouched(big, rows + tail, n, layout)
+    seen = taken(xc, source, rows + tail)
+    ref, size = torch.full((rows + tail, n), 77.0, dtype=torch.float64), torch.zeros(rows + tail, n, dtype=torch.float64)
+    ref = ref.to(torch.bfloat16).double()
+    for i, a, b in spans(sizes):
+        ref[a:b], size[a:b] = seen[a:b] @ operands[i][2].T, seen[a:b].abs() @ operands[i][2].T.abs()
+    close(y, ref, torch.bfloat16, (k + 8) * EPS32 * size)
+
+
+def test_products_of_depth_zero_are_zero():
+    y = torch.full((5, 40), 7.0, dtype=torch.bfloat16, device=DEV)
+    x, w = torch.empty(5, 0, dtype=torch.bfloat16, device=DEV), torch.empty(2, 40, 0, dtype=torch.bfloat16, device=DEV)
+    B.csr5_grouped_gemm(x, w, offsets([2, 3]), y)
+    assert (y == 0).all()
+    y.fill_(7.0)
+    e = lambda *s: torch.empty(*s, device=DEV)  # noqa: E731
+    B.csr5_gemm_f8(x.to(torch.float8_e4m3fn), e(5, 0), w[0].to(torch.float8_e4m3fn), e(1, 0), y)
+    assert (y == 0).all()
