@@ -234,6 +234,253 @@ template <typename T, typename Y, int OP> __global__ __launch_bounds__(256) void
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// The tiled kernel, for rows of whole 16-byte chunks.  BI x BJ results per workgroup of WI x WJ wavefronts; the depth goes by
+// in steps of 128 bytes, from memory straight into LDS, one step ahead of the matrix instructions.
+//
+// A tile whose rows are contiguous along the depth (straight) lies in LDS as rows of 128 bytes; one whose rows are
+// contiguous along i or j (turned: W of DX, both of DW) as 64 rows of the tile's width, and is turned by the LDS read.  A
+// wavefront's load fills 1024 contiguous bytes of LDS; which 16 bytes of memory each lane asks for is what spreads the
+// reads over the banks:
+//   straight   chunk c of row r is at slot c ^ (r >> 1 & 7): the 16 rows that a read takes a chunk of fill all 64 banks
+//   turned     32-byte segment g of row c is at segment g ^ (c & 3 | c >> 1 & 4): so do the 8 rows of half a read
+// Chunks past the depth (or the row, where that is contiguous) come from 16 bytes of zeros; rows past the end are some
+// other row, and their results are not stored.
+// ---------------------------------------------------------------------------------------------------------------
+__device__ const uint4 ZEROS = {0, 0, 0, 0};
+
+__device__ __forceinline__ void to_lds(const void* from, void* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+__device__ __forceinline__ void word_to_lds(const void* from, void* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
+}
+// Every load of this wavefront into LDS has landed and every read of it has returned; then the others' too.
+__device__ __forceinline__ void all_landed() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+}
+
+template <typename T, int ROWS, int WAVES> struct Straight {        // ROWS rows of 128 bytes
+    static constexpr int LOADS = ROWS / 8 / WAVES;
+    static_assert(WAVES % 2 == 0, "bit 3 of a row is that of the wavefront, so a lane's chunk is the same in every load");
+    const uint8_t* p[LOADS];
+    int chunk;                  // of the step, that this lane asks for: the same in every load
+    template <typename Row> __device__ __forceinline__ void start(int lane, int wave, Row row) {
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) {
+            const int r = (q * WAVES + wave) * 8 + lane / 8;
+            chunk = (lane & 7) ^ ((r >> 1) & 7);
+            p[q] = row(r) + chunk * 16;
+        }
+    }
+    // left: bytes of a row from this step on
+    __device__ __forceinline__ void load(uint8_t* lds, int wave, int64_t left) {
+        const bool in = chunk * 16 < left;
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) {
+            to_lds(in ? p[q] : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+            p[q] += 128;
+        }
+    }
+    // 16 bytes of the row `first` + lane % 16; k: which half of the step
+    __device__ static __forceinline__ uint4 read(const uint8_t* lds, int first, int k, int lane) {
+        return *reinterpret_cast<const uint4*>(lds + (first + (lane & 15)) * 128 + (((k * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) * 16));
+    }
+};
+
+template <int COLS, int WAVES> struct Turned {                      // 64 rows of COLS 16-bit values
+    static constexpr int LOADS = COLS / 8 / WAVES, PITCH = COLS * 2, LANES = PITCH / 16, ROWS = 64 / LANES;    // lanes of a row, rows of a load
+    static_assert(COLS >= 128 && LANES <= 64, "a swizzle is over 256 bytes; a load is whole rows");
+    __device__ static __forceinline__ int row(int q, int lane, int wave) { return (q * WAVES + wave) * ROWS + lane / LANES; }
+    // first value of the 8 that this lane asks for in row c
+    __device__ static __forceinline__ int col(int c, int lane) {
+        const int slot = lane % LANES;
+        return (((slot >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (slot & 1) * 8;
+    }
+    __device__ static __forceinline__ uint4 read(const uint8_t* lds, int first, int k, int lane) {
+        const int li = lane & 15, q = lane >> 4, c = k * 32 + q * 8 + (li >> 2);
+        const uint8_t* at = lds + c * PITCH + (((first >> 4) ^ ((li >> 2) | (q & 1) << 2)) * 32) + (li & 3) * 8;
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * PITCH));
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+};
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// What a workgroup with index `b` of `total` computes, in an order that suits the caches: workgroups go to the 8 XCDs by
+// turns, so each XCD gets a contiguous part of the order, and in it 8 tiles of rows go with one tile of columns after the
+// other.  Past the last tile: i or j past its end.
+__device__ __forceinline__ void tile_order(int64_t b, int64_t row_tiles, int64_t col_tiles, int64_t& i, int64_t& j) {
+    const int64_t total = row_tiles * col_tiles, per = (total + 7) / 8, at = (b & 7) * per + (b >> 3);
+    const int64_t strip = at / (8 * col_tiles), in = at - strip * 8 * col_tiles, high = min(int64_t(8), row_tiles - strip * 8);
+    j = high > 0 ? in / high : 0, i = high > 0 && (b >> 3) < per ? strip * 8 + in % high : row_tiles;
+}
+
+template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ, bool W1>
+__global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_tiles, int col_tiles) {
+    constexpr int SIZE = sizeof(T), STEP = 128 / SIZE, WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16;
+    constexpr bool F8 = is_f8<T>, X_TURNED = OP == DW, W_TURNED = OP != FWD;
+    static_assert(!F8 || (BI + BJ == WAVES * 64 && OP == FWD), "a thread per scale");
+    __shared__ __align__(16) uint8_t x0[BI * 128], x1[BI * 128], w0[BJ * 128], w1[BJ * 128];
+    __shared__ float s0[F8 ? BI + BJ : 1], s1[F8 ? BI + BJ : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    int64_t it, jt;
+    tile_order(blockIdx.x, row_tiles, col_tiles, it, jt);
+    if (it >= row_tiles || jt >= col_tiles) return;
+    const int32_t j0 = int32_t(jt) * BJ;
+    Span s;
+    int32_t i0, i_end, depth;
+    if (OP == DW) {
+        const int tiles = (a.out_rows + BI - 1) / BI;
+        s = group_span(a, int(it / tiles));
+        i0 = int32_t(it % tiles) * BI, i_end = a.out_rows, depth = s.last - s.first;
+    } else {
+        s = find_tile<BI>(a, int32_t(it));
+        if (s.group < 0) return;
+        i0 = s.first, i_end = s.last, depth = a.depth;
+    }
+    const T* const w = static_cast<const T*>(a.w) + (OP == DW ? 0 : s.group * a.w_group);
+    const T* const x = static_cast<const T*>(a.x);
+
+    Straight<T, BI, WAVES> sx;
+    Straight<T, BJ, WAVES> sw;
+    if (!X_TURNED)
+        sx.start(lane, wave, [&](int r) {
+            const int32_t i = min(i0 + r, i_end - 1);
+            const int64_t at = OP == FWD ? max(source_of(a, i), int64_t(0)) : i;
+            return reinterpret_cast<const uint8_t*>(x + at * a.ldx);
+        });
+    if (!W_TURNED)
+        sw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(j0 + r, a.cols - 1)) * a.ldw); });
+    const float* scale = nullptr;
+    int64_t scale_step = 0;
+    if (F8) {
+        if (tid < BI) {
+            scale = a.xs + max(source_of(a, min(i0 + tid, i_end - 1)), int64_t(0)) * a.xs_row, scale_step = a.xs_block;
+        } else {
+            scale = a.ws + s.group * a.ws_group + min(j0 + tid - BI, a.cols - 1) / a.w_rows * a.ws_row, scale_step = a.ws_block;
+        }
+    }
+
+    // the step from c0 on, into these tiles
+    auto load = [&](int32_t c0, uint8_t* xt, uint8_t* wt, float* st) {
+        if constexpr (X_TURNED) {
+            using X = Turned<BI, WAVES>;
+#pragma unroll
+            for (int q = 0; q < X::LOADS; q++) {
+                const int c = X::row(q, lane, wave), i = i0 + X::col(c, lane);
+                const T* p = x + int64_t(s.first + c0 + c) * a.ldx + i;
+                to_lds(c0 + c < depth && i < i_end ? static_cast<const void*>(p) : &ZEROS, xt + (q * WAVES + wave) * 1024);
+            }
+        } else {
+            sx.load(xt, wave, int64_t(depth - c0) * SIZE);
+        }
+        if constexpr (W_TURNED) {
+            using W = Turned<BJ, WAVES>;
+#pragma unroll
+            for (int q = 0; q < W::LOADS; q++) {
+                const int c = W::row(q, lane, wave), j = j0 + W::col(c, lane);
+                int64_t r = c0 + c;
+                if (OP == DW) r = r < depth ? source_of(a, s.first + r) : -1;
+                const bool in = OP == DW ? r >= 0 : r < depth;
+                to_lds(in && j < a.cols ? static_cast<const void*>(w + r * a.ldw + j) : &ZEROS, wt + (q * WAVES + wave) * 1024);
+            }
+        } else {
+            sw.load(wt, wave, int64_t(depth - c0) * SIZE);
+        }
+        if (F8) {
+            word_to_lds(scale, st + wave * 64);
+            scale += scale_step;
+        }
+    };
+
+    f32x4 acc[TJ][TI] = {};
+    const int wi = wave / WJ * (TI * 16), wj = wave % WJ * (TJ * 16);      // this wavefront's part of the tile
+    const bool some = i0 + wi < i_end;                                     // ... has a row
+    auto multiply_step = [&](const uint8_t* xt, const uint8_t* wt, const float* st) {
+        if (!some) return;
+        if constexpr (F8) {
+            i32x8 wv[TJ], xv[TI];
+            float xs[TI], ws[TJ][4];
+            auto both = [](uint4 lo, uint4 hi) { return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; };
+#pragma unroll
+            for (int j = 0; j < TJ; j++) wv[j] = both(Straight<T, BJ, WAVES>::read(wt, wj + j * 16, 0, lane), Straight<T, BJ, WAVES>::read(wt, wj + j * 16, 1, lane));
+#pragma unroll
+            for (int i = 0; i < TI; i++) {
+                xv[i] = both(Straight<T, BI, WAVES>::read(xt, wi + i * 16, 0, lane), Straight<T, BI, WAVES>::read(xt, wi + i * 16, 1, lane));
+                xs[i] = st[wi + i * 16 + (lane & 15)];
+            }
+            if (W1) {
+#pragma unroll
+                for (int j = 0; j < TJ; j++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) ws[j][q] = st[BI + wj + j * 16 + (lane >> 4) * 4 + q];
+            } else {
+                const float one = st[BI + wj];          // TJ * 16 columns that begin at a multiple of that, within 128
+#pragma unroll
+                for (int i = 0; i < TI; i++) xs[i] *= one;
+            }
+#pragma unroll
+            for (int i = 0; i < TI; i++)
+#pragma unroll
+                for (int j = 0; j < TJ; j++) {
+                    const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv[i], f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+#pragma unroll
+                    for (int q = 0; q < 4; q++) acc[j][i][q] = fmaf(part[q], W1 ? xs[i] * ws[j][q] : xs[i], acc[j][i][q]);
+                }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                uint4 wv[TJ], xv[TI];
+#pragma unroll
+                for (int j = 0; j < TJ; j++) {
+                    if constexpr (W_TURNED) wv[j] = Turned<BJ, WAVES>::read(wt, wj + j * 16, k, lane);
+                    else wv[j] = Straight<T, BJ, WAVES>::read(wt, wj + j * 16, k, lane);
+                }
+#pragma unroll
+                for (int i = 0; i < TI; i++) {
+                    if constexpr (X_TURNED) xv[i] = Turned<BI, WAVES>::read(xt, wi + i * 16, k, lane);
+                    else xv[i] = Straight<T, BI, WAVES>::read(xt, wi + i * 16, k, lane);
+                }
+#pragma unroll
+                for (int i = 0; i < TI; i++)
+#pragma unroll
+                    for (int j = 0; j < TJ; j++) acc[j][i] = multiply(wv[j], xv[i], acc[j][i], T());
+            }
+        }
+    };
+
+    if (depth > 0) load(0, x0, w0, s0);
+    for (int32_t c0 = 0; c0 < depth; c0 += 2 * STEP) {
+        all_landed();
+        if (c0 + STEP < depth) load(c0 + STEP, x1, w1, s1);
+        multiply_step(x0, w0, s0);
+        all_landed();
+        if (c0 + STEP >= depth) break;
+        if (c0 + 2 * STEP < depth) load(c0 + 2 * STEP, x0, w0, s0);
+        multiply_step(x1, w1, s1);
+    }
+
+    Y* const y = static_cast<Y*>(a.y) + (OP == DW ? s.group * a.y_group : 0);
+#pragma unroll
+    for (int i = 0; i < TI; i++) {
+        const int32_t row = i0 + wi + i * 16 + (lane & 15);
+        if (row >= i_end) continue;
+        const bool zero = OP == FWD && a.source && source_of(a, row) < 0;
+#pragma unroll
+        for (int j = 0; j < TJ; j++) {
+            const int32_t col = j0 + wj + j * 16 + (lane >> 4) * 4;
+            store_four<Y, true>(y + int64_t(row) * a.ldy + col, a.cols - col, zero ? f32x4{0, 0, 0, 0} : acc[j][i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, typename Y, int OP> int launch_plain(const Product& a, hipStream_t s) {
@@ -244,7 +491,30 @@ template <typename T, typename Y, int OP> int launch_plain(const Product& a, hip
     return launched();
 }
 
-template <typename T, typename Y, int OP> int launch(const Product& a, hipStream_t s) { return launch_plain<T, Y, OP>(a, s); }
+template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int launch_tiled(const Product& a, hipStream_t s) {
+    const int64_t cols = divide_up(a.cols, BJ);
+    const int64_t rows = OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : int64_t(divide_up(a.rows, BI)) + (a.offset ? a.groups : 0);
+    const int64_t grid = (rows * cols + 7) / 8 * 8;
+    if (grid > INT32_MAX) return CSR5_ERANGE;
+    if (is_f8<T> && a.w_rows == 1) k_product<T, Y, OP, BI, BJ, WI, WJ, is_f8<T>><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+    else k_product<T, Y, OP, BI, BJ, WI, WJ, false><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+    return launched();
+}
+
+// Rows of whole 16-byte chunks, at 16-byte addresses; results at addresses of four values.
+template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
+    constexpr int SIZE = sizeof(T);
+    auto whole = [](int64_t n) { return n * SIZE % 16 == 0; };
+    return aligned(a.x, a.ldx, SIZE, 16) && aligned(a.w, a.ldw, SIZE, 16) && whole(a.w_group) && aligned(a.y, a.ldy, sizeof(Y), 4 * sizeof(Y)) &&
+           a.y_group % 4 == 0 && (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
+}
+
+template <typename T, typename Y, int OP> int launch(const Product& a, hipStream_t s) {
+    if (!chunks_fit<T, Y, OP>(a)) return launch_plain<T, Y, OP>(a, s);
+    const int64_t height = OP == DW ? a.out_rows : a.rows / a.groups;
+    if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4>(a, s);
+    return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
+}
 
 bool half_type(int dtype) { return dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16; }
 template <int OP> int launch_half(int dtype, const Product& a, void* hip_stream) {
