@@ -405,34 +405,44 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
     auto multiply_step = [&](const uint8_t* xt, const uint8_t* wt, const float* st) {
         if (!some) return;
         if constexpr (F8) {
-            i32x8 wv[TJ], xv[TI];
-            float xs[TI], ws[TJ][4];
+            using X = Straight<T, BI, WAVES>;
+            using W = Straight<T, BJ, WAVES>;
             auto both = [](uint4 lo, uint4 hi) { return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; };
+            i32x8 wv[TJ], xv = both(X::read(xt, wi, 0, lane), X::read(xt, wi, 1, lane));
+            f32x4 ws[W1 ? TJ : 1];
 #pragma unroll
-            for (int j = 0; j < TJ; j++) wv[j] = both(Straight<T, BJ, WAVES>::read(wt, wj + j * 16, 0, lane), Straight<T, BJ, WAVES>::read(wt, wj + j * 16, 1, lane));
-#pragma unroll
-            for (int i = 0; i < TI; i++) {
-                xv[i] = both(Straight<T, BI, WAVES>::read(xt, wi + i * 16, 0, lane), Straight<T, BI, WAVES>::read(xt, wi + i * 16, 1, lane));
-                xs[i] = st[wi + i * 16 + (lane & 15)];
-            }
+            for (int j = 0; j < TJ; j++) wv[j] = both(W::read(wt, wj + j * 16, 0, lane), W::read(wt, wj + j * 16, 1, lane));
             if (W1) {
 #pragma unroll
-                for (int j = 0; j < TJ; j++)
-#pragma unroll
-                    for (int q = 0; q < 4; q++) ws[j][q] = st[BI + wj + j * 16 + (lane >> 4) * 4 + q];
-            } else {
-                const float one = st[BI + wj];          // TJ * 16 columns that begin at a multiple of that, within 128
-#pragma unroll
-                for (int i = 0; i < TI; i++) xs[i] *= one;
+                for (int j = 0; j < TJ; j++) ws[j] = *reinterpret_cast<const f32x4*>(st + BI + wj + j * 16 + (lane >> 4) * 4);
             }
+            const float one = W1 ? 1.f : st[BI + wj];       // TJ * 16 columns that begin at a multiple of that: within 128
+            // A row of tiles at a time, the sums of the one before it scaled and added beside it.  Nothing moves between
+            // rows: the compiler would keep more of them in flight than there are registers.
+            f32x4 part[2][TJ];
+            float xs = st[wi + (lane & 15)] * one, before = 0.f;
 #pragma unroll
-            for (int i = 0; i < TI; i++)
-#pragma unroll
-                for (int j = 0; j < TJ; j++) {
-                    const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv[i], f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-#pragma unroll
-                    for (int q = 0; q < 4; q++) acc[j][i][q] = fmaf(part[q], W1 ? xs[i] * ws[j][q] : xs[i], acc[j][i][q]);
+            for (int i = 0; i <= TI; i++) {
+                i32x8 next = xv;
+                if (i + 1 < TI) {
+                    next = both(X::read(xt, wi + i * 16 + 16, 0, lane), X::read(xt, wi + i * 16 + 16, 1, lane));
                 }
+                if (i < TI) {
+#pragma unroll
+                    for (int j = 0; j < TJ; j++)
+                        part[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                }
+                if (i > 0) {
+#pragma unroll
+                    for (int j = 0; j < TJ; j++)
+#pragma unroll
+                        for (int q = 0; q < 4; q++)
+                            acc[j][i - 1][q] = fmaf(part[~i & 1][j][q], W1 ? before * ws[j][q] : before, acc[j][i - 1][q]);
+                }
+                xv = next, before = xs;
+                if (i + 1 < TI) xs = st[wi + i * 16 + 16 + (lane & 15)] * one;
+                __builtin_amdgcn_sched_barrier(0);
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < 2; k++) {
