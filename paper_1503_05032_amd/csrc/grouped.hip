@@ -491,6 +491,94 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// Few rows (a step of serving): bound by reading the weights once.  A workgroup of 8 wavefronts has 16 columns and 16 TI rows;
+// its wavefronts take the steps of the depth by turns, several at a time, from memory straight into the registers of the
+// matrix instructions (a load takes 64 contiguous bytes of 16 rows), and add up their sums in LDS in a fixed order.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int FEW_WAVES = 8;
+constexpr int FEW1 = 16, FEW2 = 32;
+
+template <typename T, typename Y, int TI, bool W1> __global__ __launch_bounds__(FEW_WAVES * 64) void k_product_few(Product a, int col_tiles) {
+    constexpr int SIZE = sizeof(T), STEP = 128 / SIZE, AHEAD = 4;
+    constexpr bool F8 = is_f8<T>;
+    __shared__ __align__(16) f32x4 sums[FEW_WAVES][TI][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, q = lane >> 4;
+    const Span s = find_tile<16 * TI>(a, int32_t(blockIdx.x / col_tiles));
+    if (s.group < 0) return;
+    const int32_t j0 = int32_t(blockIdx.x % col_tiles) * 16;
+    const uint8_t* const w = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.w) + s.group * a.w_group + int64_t(min(j0 + li, a.cols - 1)) * a.ldw);
+    const uint8_t* x[TI];
+    const float *xs[TI], *ws[4];
+#pragma unroll
+    for (int i = 0; i < TI; i++) {
+        const int64_t r = max(source_of(a, min(s.first + i * 16 + li, s.last - 1)), int64_t(0));
+        x[i] = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.x) + r * a.ldx);
+        if (F8) xs[i] = a.xs + r * a.xs_row;
+    }
+    if (F8) {
+#pragma unroll
+        for (int c = 0; c < (W1 ? 4 : 1); c++) ws[c] = a.ws + s.group * a.ws_group + (W1 ? min(j0 + q * 4 + c, a.cols - 1) : j0 / CSR5_F8_BLOCK) * a.ws_row;
+    }
+    const int64_t bytes = int64_t(a.depth) * SIZE;
+    const int steps = (a.depth + STEP - 1) / STEP;
+    f32x4 acc[TI] = {};
+    for (int at = wave; at < steps; at += FEW_WAVES * AHEAD) {
+        uint4 wv[AHEAD][2], xv[AHEAD][TI][2];
+        float xf[AHEAD][TI], wf[AHEAD][4];
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) {
+            const int b = at + u * FEW_WAVES;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const int64_t o = int64_t(b) * 128 + k * 64 + q * 16;
+                const bool in = o < bytes;
+                wv[u][k] = *reinterpret_cast<const uint4*>(in ? w + o : reinterpret_cast<const uint8_t*>(&ZEROS));
+#pragma unroll
+                for (int i = 0; i < TI; i++) xv[u][i][k] = *reinterpret_cast<const uint4*>(in ? x[i] + o : reinterpret_cast<const uint8_t*>(&ZEROS));
+            }
+            if (F8) {
+                const int64_t block = min(b, steps - 1);
+#pragma unroll
+                for (int i = 0; i < TI; i++) xf[u][i] = xs[i][block * a.xs_block];
+#pragma unroll
+                for (int c = 0; c < (W1 ? 4 : 1); c++) wf[u][c] = ws[c][block * a.ws_block];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++)
+#pragma unroll
+            for (int i = 0; i < TI; i++) {
+                if constexpr (F8) {
+                    const uint4 wl = wv[u][0], wh = wv[u][1], xl = xv[u][i][0], xh = xv[u][i][1];
+                    const i32x8 w8 = {int(wl.x), int(wl.y), int(wl.z), int(wl.w), int(wh.x), int(wh.y), int(wh.z), int(wh.w)};
+                    const i32x8 x8 = {int(xl.x), int(xl.y), int(xl.z), int(xl.w), int(xh.x), int(xh.y), int(xh.z), int(xh.w)};
+                    const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                    if (at + u * FEW_WAVES < steps) {           // past the depth: a NaN scale of the last block counts once
+#pragma unroll
+                        for (int c = 0; c < 4; c++) acc[i][c] = fmaf(part[c], xf[u][i] * wf[u][W1 ? c : 0], acc[i][c]);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; k++) acc[i] = multiply(wv[u][k], xv[u][i][k], acc[i], T());
+                }
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < TI; i++) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    // a thread per four columns of a row
+    for (int e = tid; e < TI * 64; e += FEW_WAVES * 64) {
+        f32x4 sum = sums[0][e / 64][e % 64];
+#pragma unroll
+        for (int v = 1; v < FEW_WAVES; v++) sum += sums[v][e / 64][e % 64];
+        const int32_t row = s.first + e / 64 * 16 + (e & 15), col = j0 + (e % 64 >> 4) * 4;
+        if (row >= s.last || col >= a.cols) continue;
+        if (a.source && source_of(a, row) < 0) sum = f32x4{0, 0, 0, 0};
+        store_four<Y, true>(static_cast<Y*>(a.y) + int64_t(row) * a.ldy + col, a.cols - col, sum);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, typename Y, int OP> int launch_plain(const Product& a, hipStream_t s) {
@@ -511,6 +599,14 @@ template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int la
     return launched();
 }
 
+template <typename T, typename Y, int TI> int launch_few(const Product& a, hipStream_t s) {
+    const int64_t cols = divide_up(a.cols, 16), rows = int64_t(divide_up(a.rows, 16 * TI)) + (a.offset ? a.groups : 0);
+    if (rows * cols > INT32_MAX) return CSR5_ERANGE;
+    if (is_f8<T> && a.w_rows == 1) k_product_few<T, Y, TI, is_f8<T>><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
+    else k_product_few<T, Y, TI, false><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
+    return launched();
+}
+
 // Rows of whole 16-byte chunks, at 16-byte addresses; results at addresses of four values.
 template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
     constexpr int SIZE = sizeof(T);
@@ -522,6 +618,10 @@ template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
 template <typename T, typename Y, int OP> int launch(const Product& a, hipStream_t s) {
     if (!chunks_fit<T, Y, OP>(a)) return launch_plain<T, Y, OP>(a, s);
     const int64_t height = OP == DW ? a.out_rows : a.rows / a.groups;
+    if constexpr (OP == FWD) {
+        if (height <= FEW1) return launch_few<T, Y, 1>(a, s);
+        if (height <= FEW2) return launch_few<T, Y, 2>(a, s);
+    }
     if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4>(a, s);
     return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
 }
