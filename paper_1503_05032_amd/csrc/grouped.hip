@@ -248,16 +248,25 @@ template <typename T, typename Y, int OP> __global__ __launch_bounds__(256) void
 // ---------------------------------------------------------------------------------------------------------------
 __device__ const uint4 ZEROS = {0, 0, 0, 0};
 
-__device__ __forceinline__ void to_lds(const void* from, void* lds) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+// 16 (4) bytes of each lane's address to lds + 16 (4) * lane; lds is the same for the whole wavefront.  In assembly because
+// the compiler, which knows these loads as writes to all of LDS, would wait for the next step's before it reads this one's;
+// they write no vector register, and the compiler keeps nothing in m0 (hence no warning that it would not be kept).  What
+// waits for them is all_landed().
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ uint32_t lds_address(const void* lds) { return uint32_t(uintptr_t((const __attribute__((address_space(3))) void*)lds)); }
+__device__ __forceinline__ void to_lds(const void* from, const void* lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(lds)), "v"(from) : "memory", "m0");
 }
-__device__ __forceinline__ void word_to_lds(const void* from, void* lds) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
+__device__ __forceinline__ void word_to_lds(const void* from, const void* lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(lds)), "v"(from) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // Every load of this wavefront into LDS has landed and every read of it has returned; then the others' too.
 __device__ __forceinline__ void all_landed() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 template <typename T, int ROWS, int WAVES> struct Straight {        // ROWS rows of 128 bytes
@@ -291,11 +300,44 @@ template <typename T, int ROWS, int WAVES> struct Straight {        // ROWS rows
 template <int COLS, int WAVES> struct Turned {                      // 64 rows of COLS 16-bit values
     static constexpr int LOADS = COLS / 8 / WAVES, PITCH = COLS * 2, LANES = PITCH / 16, ROWS = 64 / LANES;    // lanes of a row, rows of a load
     static_assert(COLS >= 128 && LANES <= 64, "a swizzle is over 256 bytes; a load is whole rows");
-    __device__ static __forceinline__ int row(int q, int lane, int wave) { return (q * WAVES + wave) * ROWS + lane / LANES; }
-    // first value of the 8 that this lane asks for in row c
-    __device__ static __forceinline__ int col(int c, int lane) {
-        const int slot = lane % LANES;
-        return (((slot >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (slot & 1) * 8;
+    static_assert(WAVES * ROWS % 16 == 0, "bits 0, 1 and 3 of a row are the same in every load of a lane");
+    const uint8_t* p;           // without source: this lane's chunk of the step's row of load 0
+    int64_t pitch;              // bytes of a row in memory
+    int32_t next[LOADS];        // with source: what it says for the next step
+    int c;                      // row of load 0 within a step
+    bool in;                    // the chunk is within the row
+    __device__ static __forceinline__ int row(int q) { return q * WAVES * ROWS; }
+    // values: address of row 0, value 0; first: the tile's first value in it; width: values of a row
+    template <typename T> __device__ __forceinline__ void start(int lane, int wave, const T* values, int64_t ld, int first, int width) {
+        c = wave * ROWS + lane / LANES;
+        const int slot = lane % LANES, col = first + (((slot >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (slot & 1) * 8;
+        in = col < width, pitch = ld * sizeof(T);
+        p = reinterpret_cast<const uint8_t*>(values + col);
+    }
+    __device__ __forceinline__ void by_row() { p += c * pitch; }
+    // source: from the step's first row on; left: its rows
+    __device__ __forceinline__ void by_source(const int32_t* source, int left) {
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) next[q] = source[min(c + row(q), max(left - 1, 0))];
+    }
+    // left: rows from this step on
+    __device__ __forceinline__ void load(uint8_t* lds, int wave, int left) {
+#pragma unroll
+        for (int q = 0; q < LOADS; q++)
+            to_lds(in && c + row(q) < left ? p + row(q) * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+        p += 64 * pitch;
+    }
+    // what by_source() asked for a step ago, of `rows` rows
+    __device__ __forceinline__ void load_by_source(uint8_t* lds, int wave, int left, int32_t rows) {
+        // they are here since the last all_landed(); used before the first load, so that the compiler's own wait for them
+        // waits for nothing else
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) asm volatile("" : "+v"(next[q]));
+#pragma unroll
+        for (int q = 0; q < LOADS; q++) {
+            const bool there = in && c + row(q) < left && uint32_t(next[q]) < uint32_t(rows);
+            to_lds(there ? p + next[q] * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+        }
     }
     __device__ static __forceinline__ uint4 read(const uint8_t* lds, int first, int k, int lane) {
         const int li = lane & 15, q = lane >> 4, c = k * 32 + q * 8 + (li >> 2);
@@ -347,16 +389,25 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
     const T* const w = static_cast<const T*>(a.w) + (OP == DW ? 0 : s.group * a.w_group);
     const T* const x = static_cast<const T*>(a.x);
 
-    Straight<T, BI, WAVES> sx;
-    Straight<T, BJ, WAVES> sw;
-    if (!X_TURNED)
-        sx.start(lane, wave, [&](int r) {
+    std::conditional_t<X_TURNED, Turned<BI, WAVES>, Straight<T, BI, WAVES>> tx;
+    std::conditional_t<W_TURNED, Turned<BJ, WAVES>, Straight<T, BJ, WAVES>> tw;
+    if constexpr (X_TURNED) {
+        tx.start(lane, wave, x + int64_t(s.first) * a.ldx, a.ldx, i0, i_end);
+        tx.by_row();
+    } else {
+        tx.start(lane, wave, [&](int r) {
             const int32_t i = min(i0 + r, i_end - 1);
             const int64_t at = OP == FWD ? max(source_of(a, i), int64_t(0)) : i;
             return reinterpret_cast<const uint8_t*>(x + at * a.ldx);
         });
-    if (!W_TURNED)
-        sw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(j0 + r, a.cols - 1)) * a.ldw); });
+    }
+    if constexpr (W_TURNED) {
+        tw.start(lane, wave, OP == DW && !a.source ? w + int64_t(s.first) * a.ldw : w, a.ldw, j0, a.cols);
+        if (OP == DW && a.source && depth > 0) tw.by_source(a.source + s.first, depth);
+        else tw.by_row();
+    } else {
+        tw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(j0 + r, a.cols - 1)) * a.ldw); });
+    }
     const float* scale = nullptr;
     int64_t scale_step = 0;
     if (F8) {
@@ -369,30 +420,18 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
 
     // the step from c0 on, into these tiles
     auto load = [&](int32_t c0, uint8_t* xt, uint8_t* wt, float* st) {
-        if constexpr (X_TURNED) {
-            using X = Turned<BI, WAVES>;
-#pragma unroll
-            for (int q = 0; q < X::LOADS; q++) {
-                const int c = X::row(q, lane, wave), i = i0 + X::col(c, lane);
-                const T* p = x + int64_t(s.first + c0 + c) * a.ldx + i;
-                to_lds(c0 + c < depth && i < i_end ? static_cast<const void*>(p) : &ZEROS, xt + (q * WAVES + wave) * 1024);
+        if (OP == DW && a.source) {
+            if constexpr (OP == DW) {
+                tw.load_by_source(wt, wave, depth - c0, a.source_rows);
+                if (c0 + STEP < depth) tw.by_source(a.source + s.first + c0 + STEP, depth - c0 - STEP);
             }
+        } else if constexpr (W_TURNED) {
+            tw.load(wt, wave, depth - c0);
         } else {
-            sx.load(xt, wave, int64_t(depth - c0) * SIZE);
+            tw.load(wt, wave, int64_t(depth - c0) * SIZE);
         }
-        if constexpr (W_TURNED) {
-            using W = Turned<BJ, WAVES>;
-#pragma unroll
-            for (int q = 0; q < W::LOADS; q++) {
-                const int c = W::row(q, lane, wave), j = j0 + W::col(c, lane);
-                int64_t r = c0 + c;
-                if (OP == DW) r = r < depth ? source_of(a, s.first + r) : -1;
-                const bool in = OP == DW ? r >= 0 : r < depth;
-                to_lds(in && j < a.cols ? static_cast<const void*>(w + r * a.ldw + j) : &ZEROS, wt + (q * WAVES + wave) * 1024);
-            }
-        } else {
-            sw.load(wt, wave, int64_t(depth - c0) * SIZE);
-        }
+        if constexpr (X_TURNED) tx.load(xt, wave, depth - c0);
+        else tx.load(xt, wave, int64_t(depth - c0) * SIZE);
         if (F8) {
             word_to_lds(scale, st + wave * 64);
             scale += scale_step;
