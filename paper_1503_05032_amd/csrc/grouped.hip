@@ -57,6 +57,11 @@ __device__ __forceinline__ Span group_span(const Product& a, int g) {
     return {g, first, max(offset_at(a, g + 1), first)};
 }
 
+// The same in every lane, for the compiler to know.
+__device__ __forceinline__ Span uniform(Span s) {
+    return {__builtin_amdgcn_readfirstlane(s.group), __builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.last)};
+}
+
 // The t-th tile of BM rows, counted through the groups in order; group -1: there are fewer.  The whole wavefront takes part:
 // a lane per group.  At most rows / BM + groups tiles.
 template <int BM> __device__ __forceinline__ Span find_tile(const Product& a, int32_t t) {
@@ -81,7 +86,7 @@ template <int BM> __device__ __forceinline__ Span find_tile(const Product& a, in
         if (past) {
             const int l = __ffsll((unsigned long long)past) - 1;
             const int32_t first = __shfl(s.first, l) + (t - before - __shfl(upto - tiles, l)) * BM;
-            return {g0 + l, first, min(first + BM, __shfl(s.last, l))};
+            return uniform({g0 + l, first, min(first + BM, __shfl(s.last, l))});
         }
         before += __shfl(upto, 63);
     }
@@ -234,24 +239,26 @@ template <typename T, typename Y, int OP> __global__ __launch_bounds__(256) void
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// The tiled kernel, for rows of whole 16-byte chunks.  BI x BJ results per workgroup of WI x WJ wavefronts; the depth goes by
-// in steps of 128 bytes, from memory straight into LDS, one step ahead of the matrix instructions.
+// The tiled kernels, for rows of whole 16-byte chunks.  BI x BJ results per workgroup of WI x WJ wavefronts; the depth goes by
+// in steps, from memory straight into slots of LDS, ahead of the matrix instructions.
 //
-// A tile whose rows are contiguous along the depth (straight) lies in LDS as rows of 128 bytes; one whose rows are
-// contiguous along i or j (turned: W of DX, both of DW) as 64 rows of the tile's width, and is turned by the LDS read.  A
-// wavefront's load fills 1024 contiguous bytes of LDS; which 16 bytes of memory each lane asks for is what spreads the
-// reads over the banks:
-//   straight   chunk c of row r is at slot c ^ (r >> 1 & 7): the 16 rows that a read takes a chunk of fill all 64 banks
-//   turned     32-byte segment g of row c is at segment g ^ (c & 3 | c >> 1 & 4): so do the 8 rows of half a read
+// A tile whose rows are contiguous along the depth (Straight) lies in a slot as rows of one step (64 bytes; 128 in 8 bits);
+// one whose rows are contiguous along i or j (Turned: W of DX, both of DW) as 32 rows of the tile's width, and is turned by
+// the LDS read.  A wavefront's load fills 1024 contiguous bytes of a slot; which 16 bytes of memory each lane asks for is
+// what spreads the reads over the 64 banks (no conflicts counted):
+//   Straight   chunk c of row r is at place c ^ (-(r >> 2) & 3), of 128 bytes c ^ (r >> 1 & 7).  A 16-byte read is served
+//              for 16 lanes at a time, but not for neighbouring ones (0-3, 12-15 and 20-27 first): with r >> 2 for
+//              -(r >> 2) half of the time went on conflicts
+//   Turned     32-byte segment g of row c is at segment g ^ (c & 3 | c >> 1 & 4): so do the 8 rows of half a read
 // Chunks past the depth (or the row, where that is contiguous) come from 16 bytes of zeros; rows past the end are some
 // other row, and their results are not stored.
 // ---------------------------------------------------------------------------------------------------------------
 __device__ const uint4 ZEROS = {0, 0, 0, 0};
 
 // 16 (4) bytes of each lane's address to lds + 16 (4) * lane; lds is the same for the whole wavefront.  In assembly because
-// the compiler, which knows these loads as writes to all of LDS, would wait for the next step's before it reads this one's;
+// the compiler, which knows these loads as writes to all of LDS, would wait for later steps' before it reads this one's;
 // they write no vector register, and the compiler keeps nothing in m0 (hence no warning that it would not be kept).  What
-// waits for them is all_landed().
+// waits for them is landed().
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ uint32_t lds_address(const void* lds) { return uint32_t(uintptr_t((const __attribute__((address_space(3))) void*)lds)); }
@@ -262,90 +269,90 @@ __device__ __forceinline__ void word_to_lds(const void* from, const void* lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(lds)), "v"(from) : "memory", "m0");
 }
 #pragma clang diagnostic pop
-// Every load of this wavefront into LDS has landed and every read of it has returned; then the others' too.
-__device__ __forceinline__ void all_landed() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+// This wavefront's loads into LDS have landed but for the last LATER, and its reads of LDS have returned; then the others' too.
+template <int LATER> __device__ __forceinline__ void landed() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-template <typename T, int ROWS, int WAVES> struct Straight {        // ROWS rows of 128 bytes
-    static constexpr int LOADS = ROWS / 8 / WAVES;
-    static_assert(WAVES % 2 == 0, "bit 3 of a row is that of the wavefront, so a lane's chunk is the same in every load");
+template <int HEIGHT, int WAVES, int WIDTH> struct Straight {       // HEIGHT rows of WIDTH bytes
+    static constexpr int LANES = WIDTH / 16, EACH = 64 / LANES, LOADS = HEIGHT / EACH / WAVES, READS = 1;   // lanes of a row, rows of a load
+    static_assert(WIDTH == 64 || (WIDTH == 128 && WAVES % 2 == 0), "a lane's chunk is the same in every load");
     const uint8_t* p[LOADS];
-    int chunk;                  // of the step, that this lane asks for: the same in every load
+    int chunk;                  // of the step, that this lane asks for
+    __device__ static __forceinline__ int turn(int r) { return WIDTH == 64 ? -(r >> 2) & 3 : (r >> 1) & 7; }
     template <typename Row> __device__ __forceinline__ void start(int lane, int wave, Row row) {
+        chunk = (lane % LANES) ^ turn(wave * EACH + lane / LANES);
 #pragma unroll
-        for (int q = 0; q < LOADS; q++) {
-            const int r = (q * WAVES + wave) * 8 + lane / 8;
-            chunk = (lane & 7) ^ ((r >> 1) & 7);
-            p[q] = row(r) + chunk * 16;
-        }
+        for (int q = 0; q < LOADS; q++) p[q] = row((q * WAVES + wave) * EACH + lane / LANES) + chunk * 16;
     }
     // left: bytes of a row from this step on
-    __device__ __forceinline__ void load(uint8_t* lds, int wave, int64_t left) {
-        const bool in = chunk * 16 < left;
-#pragma unroll
-        for (int q = 0; q < LOADS; q++) {
-            to_lds(in ? p[q] : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-            p[q] += 128;
-        }
+    __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int64_t left) {
+        to_lds(chunk * 16 < left ? p[q] : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+        p[q] += WIDTH;
     }
-    // 16 bytes of the row `first` + lane % 16; k: which half of the step
-    __device__ static __forceinline__ uint4 read(const uint8_t* lds, int first, int k, int lane) {
-        return *reinterpret_cast<const uint4*>(lds + (first + (lane & 15)) * 128 + (((k * 4 + (lane >> 4)) ^ ((lane >> 1) & 7)) * 16));
+    // Where in a slot this lane reads the first of the 16 x 64 bytes of rows from `first` on (a multiple of a wavefront's
+    // share), and the e-th from there on of its 64 bytes k, given the address of that in a slot.
+    __device__ static __forceinline__ uint32_t where(int first, int lane) { return (first + (lane & 15)) * WIDTH + (((lane >> 4) ^ turn(lane & 15)) * 16); }
+    __device__ static __forceinline__ uint4 read(uint32_t at, int e, int k) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)uintptr_t((at ^ (k * 64)) + e * 16 * WIDTH);
+        return make_uint4(v[0], v[1], v[2], v[3]);
     }
 };
 
-template <int COLS, int WAVES> struct Turned {                      // 64 rows of COLS 16-bit values
-    static constexpr int LOADS = COLS / 8 / WAVES, PITCH = COLS * 2, LANES = PITCH / 16, ROWS = 64 / LANES;    // lanes of a row, rows of a load
+template <int COLS, int WAVES> struct Turned {                      // 32 rows of COLS 16-bit values
+    static constexpr int PITCH = COLS * 2, LANES = PITCH / 16, EACH = 64 / LANES, LOADS = 32 / EACH / WAVES, READS = 2;  // lanes of a row, rows of a load
     static_assert(COLS >= 128 && LANES <= 64, "a swizzle is over 256 bytes; a load is whole rows");
-    static_assert(WAVES * ROWS % 16 == 0, "bits 0, 1 and 3 of a row are the same in every load of a lane");
-    const uint8_t* p;           // without source: this lane's chunk of the step's row of load 0
+    static_assert(WAVES * EACH % 16 == 0, "bits 0, 1 and 3 of a row are the same in every load of a lane");
+    const uint8_t* p;           // this lane's chunk: of its row in load 0; with source: of row 0
     int64_t pitch;              // bytes of a row in memory
-    int32_t next[LOADS];        // with source: what it says for the next step
+    int32_t next[LOADS][EACH];  // with source: what it says for the next step, the same in every lane
     int c;                      // row of load 0 within a step
     bool in;                    // the chunk is within the row
-    __device__ static __forceinline__ int row(int q) { return q * WAVES * ROWS; }
     // values: address of row 0, value 0; first: the tile's first value in it; width: values of a row
     template <typename T> __device__ __forceinline__ void start(int lane, int wave, const T* values, int64_t ld, int first, int width) {
-        c = wave * ROWS + lane / LANES;
-        const int slot = lane % LANES, col = first + (((slot >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (slot & 1) * 8;
+        c = wave * EACH + lane / LANES;
+        const int place = lane % LANES, col = first + (((place >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (place & 1) * 8;
         in = col < width, pitch = ld * sizeof(T);
         p = reinterpret_cast<const uint8_t*>(values + col);
     }
     __device__ __forceinline__ void by_row() { p += c * pitch; }
-    // source: from the step's first row on; left: its rows
-    __device__ __forceinline__ void by_source(const int32_t* source, int left) {
-#pragma unroll
-        for (int q = 0; q < LOADS; q++) next[q] = source[min(c + row(q), max(left - 1, 0))];
-    }
     // left: rows from this step on
-    __device__ __forceinline__ void load(uint8_t* lds, int wave, int left) {
+    __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int left) {
+        const int at = q * WAVES * EACH;
+        to_lds(in && c + at < left ? p + at * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+        if (q == LOADS - 1) p += 32 * pitch;
+    }
+    // source: from the step's first row on; left: its rows.  Scalar loads: they do not wait with the loads into LDS.
+    __device__ __forceinline__ void by_source(const int32_t* source, int left, int wave) {
+        typedef const __attribute__((address_space(4))) int32_t* constant;
 #pragma unroll
         for (int q = 0; q < LOADS; q++)
-            to_lds(in && c + row(q) < left ? p + row(q) * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-        p += 64 * pitch;
-    }
-    // what by_source() asked for a step ago, of `rows` rows
-    __device__ __forceinline__ void load_by_source(uint8_t* lds, int wave, int left, int32_t rows) {
-        // they are here since the last all_landed(); used before the first load, so that the compiler's own wait for them
-        // waits for nothing else
 #pragma unroll
-        for (int q = 0; q < LOADS; q++) asm volatile("" : "+v"(next[q]));
-#pragma unroll
-        for (int q = 0; q < LOADS; q++) {
-            const bool there = in && c + row(q) < left && uint32_t(next[q]) < uint32_t(rows);
-            to_lds(there ? p + next[q] * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-        }
+            for (int r = 0; r < EACH; r++) next[q][r] = left > 0 ? ((constant)(uintptr_t)source)[min((q * WAVES + wave) * EACH + r, left - 1)] : -1;
     }
-    __device__ static __forceinline__ uint4 read(const uint8_t* lds, int first, int k, int lane) {
-        const int li = lane & 15, q = lane >> 4, c = k * 32 + q * 8 + (li >> 2);
-        const uint8_t* at = lds + c * PITCH + (((first >> 4) ^ ((li >> 2) | (q & 1) << 2)) * 32) + (li & 3) * 8;
+    // what by_source() asked for a step ago; rows: that a source may name
+    __device__ __forceinline__ void load_by_source(int q, uint8_t* lds, int lane, int wave, int left, int32_t rows) {
+        int32_t r = next[q][0];
+#pragma unroll
+        for (int e = 1; e < EACH; e++) r = lane / LANES == e ? next[q][e] : r;
+        const bool there = in && c + q * WAVES * EACH < left && uint32_t(r) < uint32_t(rows);
+        to_lds(there ? p + r * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+    }
+    // As Straight's, for 16 columns from `first` on; slots and rows are multiples of 256 bytes, so the e-th segment's place is
+    // another pattern in bits 5 to 7.
+    __device__ static __forceinline__ uint32_t where(int first, int lane) {
+        const int li = lane & 15, q = lane >> 4;
+        return (q * 8 + (li >> 2)) * PITCH + (((first >> 4) ^ ((li >> 2) | (q & 1) << 2)) * 32) + (li & 3) * 8;
+    }
+    __device__ static __forceinline__ uint4 read(uint32_t at, int e, int) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * PITCH));
+        at ^= e * 32;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at)),
+                    hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at + 4 * PITCH));
         const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
         return make_uint4(a.x, a.y, b.x, b.y);
     }
@@ -353,180 +360,270 @@ template <int COLS, int WAVES> struct Turned {                      // 64 rows o
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// What a workgroup with index `b` of `total` computes, in an order that suits the caches: workgroups go to the 8 XCDs by
-// turns, so each XCD gets a contiguous part of the order, and in it 8 tiles of rows go with one tile of columns after the
-// other.  Past the last tile: i or j past its end.
-__device__ __forceinline__ void tile_order(int64_t b, int64_t row_tiles, int64_t col_tiles, int64_t& i, int64_t& j) {
-    const int64_t total = row_tiles * col_tiles, per = (total + 7) / 8, at = (b & 7) * per + (b >> 3);
-    const int64_t strip = at / (8 * col_tiles), in = at - strip * 8 * col_tiles, high = min(int64_t(8), row_tiles - strip * 8);
-    j = high > 0 ? in / high : 0, i = high > 0 && (b >> 3) < per ? strip * 8 + in % high : row_tiles;
+// What a workgroup with index `b` computes, in an order that suits the caches: workgroups go to the 8 XCDs by turns, so
+// each XCD gets a contiguous part of the order, and in it 8 tiles of rows go with one tile of columns after the other.
+// False: nothing.
+__device__ __forceinline__ bool tile_order(int64_t b, int row_tiles, int col_tiles, int32_t& i, int32_t& j) {
+    const int64_t total = int64_t(row_tiles) * col_tiles, per = (total + 7) / 8, at = (b & 7) * per + (b >> 3);
+    if ((b >> 3) >= per || at >= total) return false;
+    const int32_t strip = int32_t(at / (8 * int64_t(col_tiles))), in = int32_t(at - int64_t(strip) * 8 * col_tiles), high = min(8, row_tiles - strip * 8);
+    i = strip * 8 + in % high, j = in / high;
+    return true;
 }
 
-template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ, bool W1>
-__global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_tiles, int col_tiles) {
-    constexpr int SIZE = sizeof(T), STEP = 128 / SIZE, WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16;
-    constexpr bool F8 = is_f8<T>, X_TURNED = OP == DW, W_TURNED = OP != FWD;
-    static_assert(!F8 || (BI + BJ == WAVES * 64 && OP == FWD), "a thread per scale");
-    __shared__ __align__(16) uint8_t x0[BI * 128], x1[BI * 128], w0[BJ * 128], w1[BJ * 128];
-    __shared__ float s0[F8 ? BI + BJ : 1], s1[F8 ? BI + BJ : 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    int64_t it, jt;
-    tile_order(blockIdx.x, row_tiles, col_tiles, it, jt);
-    if (it >= row_tiles || jt >= col_tiles) return;
-    const int32_t j0 = int32_t(jt) * BJ;
+// The rows, columns and depth of a workgroup's tile.
+struct Tile {
     Span s;
-    int32_t i0, i_end, depth;
+    int32_t i0, i_end, j0, depth;
+};
+template <int OP, int BI, int BJ> __device__ __forceinline__ bool find(const Product& a, int row_tiles, int col_tiles, Tile& t) {
+    int32_t it, jt;
+    if (!tile_order(blockIdx.x, row_tiles, col_tiles, it, jt)) return false;
+    t.j0 = jt * BJ;
     if (OP == DW) {
         const int tiles = (a.out_rows + BI - 1) / BI;
-        s = group_span(a, int(it / tiles));
-        i0 = int32_t(it % tiles) * BI, i_end = a.out_rows, depth = s.last - s.first;
+        t.s = group_span(a, it / tiles);
+        t.i0 = it % tiles * BI, t.i_end = a.out_rows, t.depth = t.s.last - t.s.first;
     } else {
-        s = find_tile<BI>(a, int32_t(it));
-        if (s.group < 0) return;
-        i0 = s.first, i_end = s.last, depth = a.depth;
+        t.s = find_tile<BI>(a, it);
+        t.i0 = t.s.first, t.i_end = t.s.last, t.depth = a.depth;
     }
-    const T* const w = static_cast<const T*>(a.w) + (OP == DW ? 0 : s.group * a.w_group);
-    const T* const x = static_cast<const T*>(a.x);
+    return t.s.group >= 0;
+}
 
-    std::conditional_t<X_TURNED, Turned<BI, WAVES>, Straight<T, BI, WAVES>> tx;
-    std::conditional_t<W_TURNED, Turned<BJ, WAVES>, Straight<T, BJ, WAVES>> tw;
+// A wavefront's 16 TI x 16 TJ results from row i0 and column j0 on.
+template <int OP, typename Y, int TI, int TJ> __device__ __forceinline__ void store_tile(const Product& a, const Tile& t, int32_t i0, int32_t j0, int lane, const f32x4 (&acc)[TJ][TI]) {
+    Y* const y = static_cast<Y*>(a.y) + (OP == DW ? t.s.group * a.y_group : 0);
+#pragma unroll
+    for (int i = 0; i < TI; i++) {
+        const int32_t row = i0 + i * 16 + (lane & 15);
+        if (row >= t.i_end) continue;
+        const bool zero = OP == FWD && a.source && source_of(a, row) < 0;
+#pragma unroll
+        for (int j = 0; j < TJ; j++) {
+            const int32_t col = j0 + j * 16 + (lane >> 4) * 4;
+            store_four<Y, true>(y + int64_t(row) * a.ldy + col, a.cols - col, zero ? f32x4{0, 0, 0, 0} : acc[j][i]);
+        }
+    }
+}
+
+// 16 bits.  A step is 32 values of the depth, a block of work the step's products: TI rows of TJ matrix instructions each.
+// The operands of block b + 1 are read from its slot while block b is multiplied; the slot of block b, read the block
+// before, is filled with step b + SLOTS meanwhile: a load has SLOTS - 1 blocks to land.  Reads and loads are dealt out between
+// the rows of products (together at a block's start they held up the products: 8192^3 took 1.05 ms).
+template <typename T, int OP, int BI, int BJ, int WI, int WJ, int SLOTS>
+__global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_tiles, int col_tiles) {
+    constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, SLOT = (BI + BJ) * 64;
+    constexpr bool X_TURNED = OP == DW, W_TURNED = OP != FWD;
+    using X = std::conditional_t<X_TURNED, Turned<BI, WAVES>, Straight<BI, WAVES, 64>>;
+    using W = std::conditional_t<W_TURNED, Turned<BJ, WAVES>, Straight<BJ, WAVES, 64>>;
+    constexpr int LOADS = X::LOADS + W::LOADS;
+    static_assert(LOADS <= TI && TI > 2, "at most one load beside a row");
+    __shared__ __align__(16) uint8_t lds[SLOTS * SLOT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Tile t;
+    if (!find<OP, BI, BJ>(a, row_tiles, col_tiles, t)) return;
+    const T* const w = static_cast<const T*>(a.w) + (OP == DW ? 0 : t.s.group * a.w_group);
+    const T* const x = static_cast<const T*>(a.x);
+    const bool by_source = OP == DW && a.source;
+    X tx;
+    W tw;
     if constexpr (X_TURNED) {
-        tx.start(lane, wave, x + int64_t(s.first) * a.ldx, a.ldx, i0, i_end);
+        tx.start(lane, wave, x + int64_t(t.s.first) * a.ldx, a.ldx, t.i0, t.i_end);
         tx.by_row();
     } else {
         tx.start(lane, wave, [&](int r) {
-            const int32_t i = min(i0 + r, i_end - 1);
-            const int64_t at = OP == FWD ? max(source_of(a, i), int64_t(0)) : i;
-            return reinterpret_cast<const uint8_t*>(x + at * a.ldx);
+            const int32_t i = min(t.i0 + r, t.i_end - 1);
+            return reinterpret_cast<const uint8_t*>(x + (OP == FWD ? max(source_of(a, i), int64_t(0)) : i) * a.ldx);
         });
     }
     if constexpr (W_TURNED) {
-        tw.start(lane, wave, OP == DW && !a.source ? w + int64_t(s.first) * a.ldw : w, a.ldw, j0, a.cols);
-        if (OP == DW && a.source && depth > 0) tw.by_source(a.source + s.first, depth);
+        tw.start(lane, wave, OP == DW && !by_source ? w + int64_t(t.s.first) * a.ldw : w, a.ldw, t.j0, a.cols);
+        if (by_source) tw.by_source(a.source + t.s.first, t.depth, wave);
         else tw.by_row();
     } else {
-        tw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(j0 + r, a.cols - 1)) * a.ldw); });
+        tw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(t.j0 + r, a.cols - 1)) * a.ldw); });
     }
-    const float* scale = nullptr;
-    int64_t scale_step = 0;
-    if (F8) {
-        if (tid < BI) {
-            scale = a.xs + max(source_of(a, min(i0 + tid, i_end - 1)), int64_t(0)) * a.xs_row, scale_step = a.xs_block;
-        } else {
-            scale = a.ws + s.group * a.ws_group + min(j0 + tid - BI, a.cols - 1) / a.w_rows * a.ws_row, scale_step = a.ws_block;
+    // part `part` of the loads of the step from c0 on (past the depth: zeros)
+    auto load = [&](int part, uint8_t* slot, int32_t c0) {
+        const int32_t left = t.depth - c0;
+        if (part < X::LOADS) {
+            if constexpr (X_TURNED) tx.load(part, slot, wave, left);
+            else tx.load(part, slot, wave, int64_t(left) * 2);
+            return;
         }
-    }
-
-    // the step from c0 on, into these tiles
-    auto load = [&](int32_t c0, uint8_t* xt, uint8_t* wt, float* st) {
-        if (OP == DW && a.source) {
-            if constexpr (OP == DW) {
-                tw.load_by_source(wt, wave, depth - c0, a.source_rows);
-                if (c0 + STEP < depth) tw.by_source(a.source + s.first + c0 + STEP, depth - c0 - STEP);
+        const int q = part - X::LOADS;
+        slot += BI * 64;
+        if constexpr (OP == DW) {
+            if (by_source) {
+                tw.load_by_source(q, slot, lane, wave, left, a.source_rows);
+                if (q == W::LOADS - 1) tw.by_source(a.source + t.s.first + c0 + 32, left - 32, wave);
+            } else {
+                tw.load(q, slot, wave, left);
             }
         } else if constexpr (W_TURNED) {
-            tw.load(wt, wave, depth - c0);
+            tw.load(q, slot, wave, left);
         } else {
-            tw.load(wt, wave, int64_t(depth - c0) * SIZE);
-        }
-        if constexpr (X_TURNED) tx.load(xt, wave, depth - c0);
-        else tx.load(xt, wave, int64_t(depth - c0) * SIZE);
-        if (F8) {
-            word_to_lds(scale, st + wave * 64);
-            scale += scale_step;
+            tw.load(q, slot, wave, int64_t(left) * 2);
         }
     };
 
     f32x4 acc[TJ][TI] = {};
     const int wi = wave / WJ * (TI * 16), wj = wave % WJ * (TJ * 16);      // this wavefront's part of the tile
-    const bool some = i0 + wi < i_end;                                     // ... has a row
-    auto multiply_step = [&](const uint8_t* xt, const uint8_t* wt, const float* st) {
-        if (!some) return;
-        if constexpr (F8) {
-            using X = Straight<T, BI, WAVES>;
-            using W = Straight<T, BJ, WAVES>;
-            auto both = [](uint4 lo, uint4 hi) { return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; };
-            i32x8 wv[TJ], xv = both(X::read(xt, wi, 0, lane), X::read(xt, wi, 1, lane));
-            f32x4 ws[W1 ? TJ : 1];
+    const bool some = t.i0 + wi < t.i_end;                                 // ... has a row
+    // X's rows but the last are read into the registers of the rows just multiplied; W's and the last have two sets.
+    struct Operands {
+        uint4 w[TJ], last;
+    };
+    uint4 rows[TI - 1];
+    const uint32_t x_at = X::where(wi, lane), w_at = BI * 64 + W::where(wj, lane);
+    auto block = [&](const Operands& now, Operands& next, uint8_t* free, const uint8_t* ready, int32_t c0) {
+        if (some) {
+            const uint32_t slot = lds_address(ready);
 #pragma unroll
-            for (int j = 0; j < TJ; j++) wv[j] = both(W::read(wt, wj + j * 16, 0, lane), W::read(wt, wj + j * 16, 1, lane));
-            if (W1) {
+            for (int i = 0; i < TI; i++) {
+                constexpr int EACH = TJ > 2 ? TJ / 2 : 1;
+                if (i * EACH < TJ)
 #pragma unroll
-                for (int j = 0; j < TJ; j++) ws[j] = *reinterpret_cast<const f32x4*>(st + BI + wj + j * 16 + (lane >> 4) * 4);
-            }
-            const float one = W1 ? 1.f : st[BI + wj];       // TJ * 16 columns that begin at a multiple of that: within 128
-            // A row of tiles at a time, the sums of the one before it scaled and added beside it.  Nothing moves between
-            // rows: the compiler would keep more of them in flight than there are registers.
-            f32x4 part[2][TJ];
-            float xs = st[wi + (lane & 15)] * one, before = 0.f;
+                    for (int j = i * EACH; j < (i + 1) * EACH; j++) next.w[j] = W::read(slot + w_at, j, 0);
+                if (i == 2) next.last = X::read(slot + x_at, TI - 1, 0);
+                if (i > 0) rows[i - 1] = X::read(slot + x_at, i - 1, 0);
+                if (i < LOADS) load(i, free, c0 + SLOTS * 32);
 #pragma unroll
-            for (int i = 0; i <= TI; i++) {
-                i32x8 next = xv;
-                if (i + 1 < TI) {
-                    next = both(X::read(xt, wi + i * 16 + 16, 0, lane), X::read(xt, wi + i * 16 + 16, 1, lane));
-                }
-                if (i < TI) {
-#pragma unroll
-                    for (int j = 0; j < TJ; j++)
-                        part[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-                }
-                if (i > 0) {
-#pragma unroll
-                    for (int j = 0; j < TJ; j++)
-#pragma unroll
-                        for (int q = 0; q < 4; q++)
-                            acc[j][i - 1][q] = fmaf(part[~i & 1][j][q], W1 ? before * ws[j][q] : before, acc[j][i - 1][q]);
-                }
-                xv = next, before = xs;
-                if (i + 1 < TI) xs = st[wi + i * 16 + 16 + (lane & 15)] * one;
+                for (int j = 0; j < TJ; j++) acc[j][i] = multiply(now.w[j], i < TI - 1 ? rows[i] : now.last, acc[j][i], T());
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-                uint4 wv[TJ], xv[TI];
-#pragma unroll
-                for (int j = 0; j < TJ; j++) {
-                    if constexpr (W_TURNED) wv[j] = Turned<BJ, WAVES>::read(wt, wj + j * 16, k, lane);
-                    else wv[j] = Straight<T, BJ, WAVES>::read(wt, wj + j * 16, k, lane);
-                }
-#pragma unroll
-                for (int i = 0; i < TI; i++) {
-                    if constexpr (X_TURNED) xv[i] = Turned<BI, WAVES>::read(xt, wi + i * 16, k, lane);
-                    else xv[i] = Straight<T, BI, WAVES>::read(xt, wi + i * 16, k, lane);
-                }
-#pragma unroll
-                for (int i = 0; i < TI; i++)
-#pragma unroll
-                    for (int j = 0; j < TJ; j++) acc[j][i] = multiply(wv[j], xv[i], acc[j][i], T());
-            }
+            for (int i = 0; i < LOADS; i++) load(i, free, c0 + SLOTS * 32);
         }
+        landed<(SLOTS - 2) * LOADS>();
+    };
+    if (t.depth > 0) {
+        Operands even, odd;
+#pragma unroll
+        for (int s = 0; s < SLOTS; s++)
+#pragma unroll
+            for (int i = 0; i < LOADS; i++) load(i, lds + s * SLOT, s * 32);
+        landed<(SLOTS - 2) * LOADS>();
+#pragma unroll
+        for (int j = 0; j < TJ; j++) even.w[j] = W::read(lds_address(lds) + w_at, j, 0);
+#pragma unroll
+        for (int i = 0; i < TI - 1; i++) rows[i] = X::read(lds_address(lds) + x_at, i, 0);
+        even.last = X::read(lds_address(lds) + x_at, TI - 1, 0);
+        uint8_t *free = lds, *ready = lds + SLOT;
+        auto after = [&](uint8_t* slot) { return slot == lds + (SLOTS - 1) * SLOT ? lds : slot + SLOT; };
+        for (int32_t c0 = 0; c0 < t.depth; c0 += 64) {
+            block(even, odd, free, ready, c0);
+            if (c0 + 32 >= t.depth) break;
+            free = ready, ready = after(ready);
+            block(odd, even, free, ready, c0 + 32);
+            free = ready, ready = after(ready);
+        }
+        landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
+    }
+    store_tile<OP, T, TI, TJ>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
+}
+
+// 8 bits.  A step is a block of 128 values: one matrix instruction per 16 x 16 results, whose sum is scaled and added in 32
+// bits.  Two slots, the scales beside the values; the loads of a step are dealt out between the rows of products of the one
+// before.  W1: a scale per row of w.
+template <typename Y, int BI, int BJ, int WI, int WJ, bool W1>
+__global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int row_tiles, int col_tiles) {
+    constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, SLOT = (BI + BJ) * (128 + 4), SCALES = (BI + BJ) * 128;
+    static_assert(BI + BJ == WAVES * 64, "a thread per scale");
+    using X = Straight<BI, WAVES, 128>;
+    using W = Straight<BJ, WAVES, 128>;
+    constexpr int LOADS = X::LOADS + W::LOADS, EACH = (LOADS + TI - 1) / TI;
+    __shared__ __align__(16) uint8_t lds[2 * SLOT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    Tile t;
+    if (!find<FWD, BI, BJ>(a, row_tiles, col_tiles, t)) return;
+    const uint8_t* const w = static_cast<const uint8_t*>(a.w) + t.s.group * a.w_group;
+    const uint8_t* const x = static_cast<const uint8_t*>(a.x);
+    X tx;
+    W tw;
+    tx.start(lane, wave, [&](int r) { return x + max(source_of(a, min(t.i0 + r, t.i_end - 1)), int64_t(0)) * a.ldx; });
+    tw.start(lane, wave, [&](int r) { return w + int64_t(min(t.j0 + r, a.cols - 1)) * a.ldw; });
+    const float* scale;
+    int64_t scale_step;
+    if (tid < BI) {
+        scale = a.xs + max(source_of(a, min(t.i0 + tid, t.i_end - 1)), int64_t(0)) * a.xs_row, scale_step = a.xs_block;
+    } else {
+        scale = a.ws + t.s.group * a.ws_group + min(t.j0 + tid - BI, a.cols - 1) / a.w_rows * a.ws_row, scale_step = a.ws_block;
+    }
+    auto load = [&](int part, uint8_t* slot, int32_t c0) {
+        if (part == 0) {
+            word_to_lds(c0 < t.depth ? static_cast<const void*>(scale) : &ZEROS, slot + SCALES + wave * 256);
+            scale += scale_step;
+        }
+        if (part < X::LOADS) tx.load(part, slot, wave, t.depth - c0);
+        else tw.load(part - X::LOADS, slot + BI * 128, wave, t.depth - c0);
     };
 
-    if (depth > 0) load(0, x0, w0, s0);
-    for (int32_t c0 = 0; c0 < depth; c0 += 2 * STEP) {
-        all_landed();
-        if (c0 + STEP < depth) load(c0 + STEP, x1, w1, s1);
-        multiply_step(x0, w0, s0);
-        all_landed();
-        if (c0 + STEP >= depth) break;
-        if (c0 + 2 * STEP < depth) load(c0 + 2 * STEP, x0, w0, s0);
-        multiply_step(x1, w1, s1);
-    }
-
-    Y* const y = static_cast<Y*>(a.y) + (OP == DW ? s.group * a.y_group : 0);
+    f32x4 acc[TJ][TI] = {};
+    const int wi = wave / WJ * (TI * 16), wj = wave % WJ * (TJ * 16);
+    const bool some = t.i0 + wi < t.i_end;
+    auto both = [](uint4 lo, uint4 hi) { return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; };
+    const uint32_t x_at = X::where(wi, lane), w_at = BI * 128 + W::where(wj, lane);
+    // the step in slot `ready`, and the loads of the one from c0 on (past the depth: zeros) into the slot `free`
+    auto step = [&](const uint8_t* ready, uint8_t* free, int32_t c0) {
+        if (!some) {
 #pragma unroll
-    for (int i = 0; i < TI; i++) {
-        const int32_t row = i0 + wi + i * 16 + (lane & 15);
-        if (row >= i_end) continue;
-        const bool zero = OP == FWD && a.source && source_of(a, row) < 0;
-#pragma unroll
-        for (int j = 0; j < TJ; j++) {
-            const int32_t col = j0 + wj + j * 16 + (lane >> 4) * 4;
-            store_four<Y, true>(y + int64_t(row) * a.ldy + col, a.cols - col, zero ? f32x4{0, 0, 0, 0} : acc[j][i]);
+            for (int p = 0; p < LOADS; p++) load(p, free, c0);
+            return;
         }
+        const uint32_t x_in = lds_address(ready) + x_at, w_in = lds_address(ready) + w_at;
+        const float* const xs_at = reinterpret_cast<const float*>(ready + SCALES) + wi + (lane & 15);
+        const float* const ws_at = reinterpret_cast<const float*>(ready + SCALES) + BI + wj;
+        i32x8 wv[TJ], xv = both(X::read(x_in, 0, 0), X::read(x_in, 0, 1));
+        f32x4 ws[W1 ? TJ : 1];
+#pragma unroll
+        for (int j = 0; j < TJ; j++) wv[j] = both(W::read(w_in, j, 0), W::read(w_in, j, 1));
+        if (W1) {
+#pragma unroll
+            for (int j = 0; j < TJ; j++) ws[j] = *reinterpret_cast<const f32x4*>(ws_at + j * 16 + (lane >> 4) * 4);
+        }
+        const float one = W1 ? 1.f : *ws_at;            // TJ * 16 columns that begin at a multiple of that: within 128
+        // A row of products at a time, the sums of the one before it scaled and added beside it.  Nothing moves between
+        // rows: the compiler would keep more of them in flight than there are registers.
+        f32x4 part[2][TJ];
+        float xs = xs_at[0] * one, before = 0.f;
+#pragma unroll
+        for (int i = 0; i <= TI; i++) {
+            i32x8 next = xv;
+            if (i + 1 < TI) next = both(X::read(x_in, i + 1, 0), X::read(x_in, i + 1, 1));
+#pragma unroll
+            for (int p = i * EACH; p < min((i + 1) * EACH, LOADS); p++) load(p, free, c0);
+            if (i < TI) {
+#pragma unroll
+                for (int j = 0; j < TJ; j++)
+                    part[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+            }
+            if (i > 0) {
+#pragma unroll
+                for (int j = 0; j < TJ; j++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++) acc[j][i - 1][q] = fmaf(part[~i & 1][j][q], W1 ? before * ws[j][q] : before, acc[j][i - 1][q]);
+            }
+            xv = next, before = xs;
+            if (i + 1 < TI) xs = xs_at[i * 16 + 16] * one;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (t.depth > 0) {
+#pragma unroll
+        for (int p = 0; p < LOADS; p++) load(p, lds, 0);
+        for (int32_t c0 = 0; c0 < t.depth; c0 += 256) {
+            landed<0>();
+            step(lds, lds + SLOT, c0 + 128);
+            if (c0 + 128 >= t.depth) break;
+            landed<0>();
+            step(lds + SLOT, lds, c0 + 256);
+        }
+        landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
+    store_tile<FWD, Y, TI, TJ>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -628,13 +725,17 @@ template <typename T, typename Y, int OP> int launch_plain(const Product& a, hip
     return launched();
 }
 
-template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int launch_tiled(const Product& a, hipStream_t s) {
+template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ, int SLOTS> int launch_tiled(const Product& a, hipStream_t s) {
     const int64_t cols = divide_up(a.cols, BJ);
     const int64_t rows = OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : int64_t(divide_up(a.rows, BI)) + (a.offset ? a.groups : 0);
     const int64_t grid = (rows * cols + 7) / 8 * 8;
     if (grid > INT32_MAX) return CSR5_ERANGE;
-    if (is_f8<T> && a.w_rows == 1) k_product<T, Y, OP, BI, BJ, WI, WJ, is_f8<T>><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
-    else k_product<T, Y, OP, BI, BJ, WI, WJ, false><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+    if constexpr (is_f8<T>) {
+        if (a.w_rows == 1) k_product_f8<Y, BI, BJ, WI, WJ, true><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+        else k_product_f8<Y, BI, BJ, WI, WJ, false><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+    } else {
+        k_product<T, OP, BI, BJ, WI, WJ, SLOTS><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+    }
     return launched();
 }
 
@@ -661,8 +762,8 @@ template <typename T, typename Y, int OP> int launch(const Product& a, hipStream
         if (height <= FEW1) return launch_few<T, Y, 1>(a, s);
         if (height <= FEW2) return launch_few<T, Y, 2>(a, s);
     }
-    if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4>(a, s);
-    return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
+    if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4, 5>(a, s);
+    return launch_tiled<T, Y, OP, 128, 128, 2, 2, 4>(a, s);
 }
 
 bool half_type(int dtype) { return dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16; }
