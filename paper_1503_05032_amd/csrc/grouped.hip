@@ -240,15 +240,13 @@ template <typename T, typename Y, int OP> __global__ __launch_bounds__(256) void
 
 // ---------------------------------------------------------------------------------------------------------------
 // The tiled kernels, for rows of whole 16-byte chunks.  BI x BJ results per workgroup of WI x WJ wavefronts; the depth goes by
-// in steps, from memory straight into slots of LDS, ahead of the matrix instructions.
+// in steps of 128 bytes, from memory straight into LDS, ahead of the matrix instructions.
 //
-// A tile whose rows are contiguous along the depth (Straight) lies in a slot as rows of one step (64 bytes; 128 in 8 bits);
-// one whose rows are contiguous along i or j (Turned: W of DX, both of DW) as 32 rows of the tile's width, and is turned by
-// the LDS read.  A wavefront's load fills 1024 contiguous bytes of a slot; which 16 bytes of memory each lane asks for is
-// what spreads the reads over the 64 banks (no conflicts counted):
-//   Straight   chunk c of row r is at place c ^ (-(r >> 2) & 3), of 128 bytes c ^ (r >> 1 & 7).  A 16-byte read is served
-//              for 16 lanes at a time, but not for neighbouring ones (0-3, 12-15 and 20-27 first): with r >> 2 for
-//              -(r >> 2) half of the time went on conflicts
+// A tile whose rows are contiguous along the depth (Straight) lies in LDS as rows of one step, 128 bytes: whole lines (64
+// bytes a step took twice the requests to the L2); one whose rows are contiguous along i or j (Turned: W of DX, both of DW)
+// as 64 rows of the tile's width, and is turned by the LDS read.  A wavefront's load fills 1024 contiguous bytes of LDS;
+// which 16 bytes of memory each lane asks for is what spreads the reads over the 64 banks (no conflicts counted):
+//   Straight   chunk c of row r is at place c ^ (r >> 1 & 7): the 16 rows that a read takes a chunk of fill all banks
 //   Turned     32-byte segment g of row c is at segment g ^ (c & 3 | c >> 1 & 4): so do the 8 rows of half a read
 // Chunks past the depth (or the row, where that is contiguous) come from 16 bytes of zeros; rows past the end are some
 // other row, and their results are not stored.
@@ -276,39 +274,39 @@ template <int LATER> __device__ __forceinline__ void landed() {
     asm volatile("" ::: "memory");
 }
 
-template <int HEIGHT, int WAVES, int WIDTH> struct Straight {       // HEIGHT rows of WIDTH bytes
-    static constexpr int LANES = WIDTH / 16, EACH = 64 / LANES, LOADS = HEIGHT / EACH / WAVES, READS = 1;   // lanes of a row, rows of a load
-    static_assert(WIDTH == 64 || (WIDTH == 128 && WAVES % 2 == 0), "a lane's chunk is the same in every load");
+template <int HEIGHT, int WAVES> struct Straight {                  // HEIGHT rows of 128 bytes
+    static constexpr int LOADS = HEIGHT / 8 / WAVES;
+    static_assert(WAVES % 2 == 0, "bit 3 of a row is that of the wavefront, so a lane's chunk is the same in every load");
     const uint8_t* p[LOADS];
     int chunk;                  // of the step, that this lane asks for
-    __device__ static __forceinline__ int turn(int r) { return WIDTH == 64 ? -(r >> 2) & 3 : (r >> 1) & 7; }
     template <typename Row> __device__ __forceinline__ void start(int lane, int wave, Row row) {
-        chunk = (lane % LANES) ^ turn(wave * EACH + lane / LANES);
+        chunk = (lane & 7) ^ (((wave * 8 + lane / 8) >> 1) & 7);
 #pragma unroll
-        for (int q = 0; q < LOADS; q++) p[q] = row((q * WAVES + wave) * EACH + lane / LANES) + chunk * 16;
+        for (int q = 0; q < LOADS; q++) p[q] = row((q * WAVES + wave) * 8 + lane / 8) + chunk * 16;
     }
     // left: bytes of a row from this step on
     __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int64_t left) {
         to_lds(chunk * 16 < left ? p[q] : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-        p[q] += WIDTH;
+        p[q] += 128;
     }
-    // Where in a slot this lane reads the first of the 16 x 64 bytes of rows from `first` on (a multiple of a wavefront's
-    // share), and the e-th from there on of its 64 bytes k, given the address of that in a slot.
-    __device__ static __forceinline__ uint32_t where(int first, int lane) { return (first + (lane & 15)) * WIDTH + (((lane >> 4) ^ turn(lane & 15)) * 16); }
+    // Where in a tile this lane reads the first of the 16 x 64 bytes of rows from `first` on (a multiple of a wavefront's
+    // share), and the e-th from there on of its 64 bytes k, given the address of that in a tile.
+    __device__ static __forceinline__ uint32_t where(int first, int lane) { return (first + (lane & 15)) * 128 + (((lane >> 4) ^ ((lane >> 1) & 7)) * 16); }
     __device__ static __forceinline__ uint4 read(uint32_t at, int e, int k) {
         typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)uintptr_t((at ^ (k * 64)) + e * 16 * WIDTH);
+        const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)uintptr_t((at ^ (k * 64)) + e * 2048);
         return make_uint4(v[0], v[1], v[2], v[3]);
     }
 };
 
-template <int COLS, int WAVES> struct Turned {                      // 32 rows of COLS 16-bit values
-    static constexpr int PITCH = COLS * 2, LANES = PITCH / 16, EACH = 64 / LANES, LOADS = 32 / EACH / WAVES, READS = 2;  // lanes of a row, rows of a load
+template <int COLS, int WAVES> struct Turned {                      // 64 rows of COLS 16-bit values
+    static constexpr int PITCH = COLS * 2, LANES = PITCH / 16, EACH = 64 / LANES, LOADS = 64 / EACH / WAVES;     // lanes of a row, rows of a load
     static_assert(COLS >= 128 && LANES <= 64, "a swizzle is over 256 bytes; a load is whole rows");
     static_assert(WAVES * EACH % 16 == 0, "bits 0, 1 and 3 of a row are the same in every load of a lane");
     const uint8_t* p;           // this lane's chunk: of its row in load 0; with source: of row 0
     int64_t pitch;              // bytes of a row in memory
     int32_t next[LOADS][EACH];  // with source: what it says for the next step, the same in every lane
+    int32_t from[LOADS];        // ... and for this one, for this lane's row
     int c;                      // row of load 0 within a step
     bool in;                    // the chunk is within the row
     // values: address of row 0, value 0; first: the tile's first value in it; width: values of a row
@@ -323,7 +321,7 @@ template <int COLS, int WAVES> struct Turned {                      // 32 rows o
     __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int left) {
         const int at = q * WAVES * EACH;
         to_lds(in && c + at < left ? p + at * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-        if (q == LOADS - 1) p += 32 * pitch;
+        if (q == LOADS - 1) p += 64 * pitch;
     }
     // source: from the step's first row on; left: its rows.  Scalar loads: they do not wait with the loads into LDS.
     __device__ __forceinline__ void by_source(const int32_t* source, int left, int wave) {
@@ -333,13 +331,21 @@ template <int COLS, int WAVES> struct Turned {                      // 32 rows o
 #pragma unroll
             for (int r = 0; r < EACH; r++) next[q][r] = left > 0 ? ((constant)(uintptr_t)source)[min((q * WAVES + wave) * EACH + r, left - 1)] : -1;
     }
-    // what by_source() asked for a step ago; rows: that a source may name
-    __device__ __forceinline__ void load_by_source(int q, uint8_t* lds, int lane, int wave, int left, int32_t rows) {
-        int32_t r = next[q][0];
+    // Before the first of a step's loads, after the wait of landed(): the compiler's own wait for them goes here, where it
+    // is for nothing.
+    __device__ __forceinline__ void here(int lane) {
 #pragma unroll
-        for (int e = 1; e < EACH; e++) r = lane / LANES == e ? next[q][e] : r;
-        const bool there = in && c + q * WAVES * EACH < left && uint32_t(r) < uint32_t(rows);
-        to_lds(there ? p + r * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+        for (int q = 0; q < LOADS; q++) {
+            from[q] = next[q][0];
+#pragma unroll
+            for (int e = 1; e < EACH; e++) from[q] = lane / LANES == e ? next[q][e] : from[q];
+            asm volatile("" : "+v"(from[q]));
+        }
+    }
+    // what by_source() asked for a step ago; rows: that a source may name
+    __device__ __forceinline__ void load_by_source(int q, uint8_t* lds, int wave, int left, int32_t rows) {
+        const bool there = in && c + q * WAVES * EACH < left && uint32_t(from[q]) < uint32_t(rows);
+        to_lds(there ? p + from[q] * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
     }
     // As Straight's, for 16 columns from `first` on; slots and rows are multiples of 256 bytes, so the e-th segment's place is
     // another pattern in bits 5 to 7.
@@ -347,10 +353,10 @@ template <int COLS, int WAVES> struct Turned {                      // 32 rows o
         const int li = lane & 15, q = lane >> 4;
         return (q * 8 + (li >> 2)) * PITCH + (((first >> 4) ^ ((li >> 2) | (q & 1) << 2)) * 32) + (li & 3) * 8;
     }
-    __device__ static __forceinline__ uint4 read(uint32_t at, int e, int) {
+    __device__ static __forceinline__ uint4 read(uint32_t at, int e, int k) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-        at ^= e * 32;
+        at = (at ^ (e * 32)) + k * 32 * PITCH;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at)),
                     hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at + 4 * PITCH));
         const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
@@ -382,7 +388,7 @@ template <int OP, int BI, int BJ> __device__ __forceinline__ bool find(const Pro
     t.j0 = jt * BJ;
     if (OP == DW) {
         const int tiles = (a.out_rows + BI - 1) / BI;
-        t.s = group_span(a, it / tiles);
+        t.s = uniform(group_span(a, it / tiles));
         t.i0 = it % tiles * BI, t.i_end = a.out_rows, t.depth = t.s.last - t.s.first;
     } else {
         t.s = find_tile<BI>(a, it);
@@ -407,19 +413,21 @@ template <int OP, typename Y, int TI, int TJ> __device__ __forceinline__ void st
     }
 }
 
-// 16 bits.  A step is 32 values of the depth, a block of work the step's products: TI rows of TJ matrix instructions each.
-// The operands of block b + 1 are read from its slot while block b is multiplied; the slot of block b, read the block
-// before, is filled with step b + SLOTS meanwhile: a load has SLOTS - 1 blocks to land.  Reads and loads are dealt out between
-// the rows of products (together at a block's start they held up the products: 8192^3 took 1.05 ms).
-template <typename T, int OP, int BI, int BJ, int WI, int WJ, int SLOTS>
+// 16 bits.  A step is 64 values of the depth, in two halves of TI rows of TJ matrix instructions.  The operands of a half are
+// read while the one before it is multiplied.  After the first half of step s both tiles of s have been read: at the
+// barrier there, those of step s + 1 have to have landed.  LDS is a ring of five tiles, w 0, x 0, w 1, x 1 and so on; in the
+// second half of step s the tiles x s + 2 and w s + 3 are asked for, in the places of w s and x s.  So half of the loads
+// have a step to land, the others two.  Reads and loads are dealt out between the rows of products: together they held them up.
+template <typename T, int OP, int BI, int BJ, int WI, int WJ>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_tiles, int col_tiles) {
-    constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, SLOT = (BI + BJ) * 64;
+    constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, TILE = BI * 128, RING = 5;
+    static_assert(BI == BJ && TI >= 4 && TJ % 2 == 0, "places of a ring");
     constexpr bool X_TURNED = OP == DW, W_TURNED = OP != FWD;
-    using X = std::conditional_t<X_TURNED, Turned<BI, WAVES>, Straight<BI, WAVES, 64>>;
-    using W = std::conditional_t<W_TURNED, Turned<BJ, WAVES>, Straight<BJ, WAVES, 64>>;
-    constexpr int LOADS = X::LOADS + W::LOADS;
-    static_assert(LOADS <= TI && TI > 2, "at most one load beside a row");
-    __shared__ __align__(16) uint8_t lds[SLOTS * SLOT];
+    using X = std::conditional_t<X_TURNED, Turned<BI, WAVES>, Straight<BI, WAVES>>;
+    using W = std::conditional_t<W_TURNED, Turned<BJ, WAVES>, Straight<BJ, WAVES>>;
+    constexpr int LOADS = X::LOADS, EACH = 2 * LOADS / TI;      // loads of a tile, loads beside a row
+    static_assert(X::LOADS == W::LOADS && 2 * LOADS % TI == 0, "loads are dealt out evenly");
+    __shared__ __align__(1024) uint8_t lds[RING * TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Tile t;
     if (!find<OP, BI, BJ>(a, row_tiles, col_tiles, t)) return;
@@ -444,81 +452,101 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
     } else {
         tw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(t.j0 + r, a.cols - 1)) * a.ldw); });
     }
-    // part `part` of the loads of the step from c0 on (past the depth: zeros)
-    auto load = [&](int part, uint8_t* slot, int32_t c0) {
-        const int32_t left = t.depth - c0;
-        if (part < X::LOADS) {
-            if constexpr (X_TURNED) tx.load(part, slot, wave, left);
-            else tx.load(part, slot, wave, int64_t(left) * 2);
-            return;
-        }
-        const int q = part - X::LOADS;
-        slot += BI * 64;
+    // load q of the tile of the step from c0 on (past the depth: zeros)
+    auto load_x = [&](int q, uint8_t* tile, int32_t c0) {
+        if constexpr (X_TURNED) tx.load(q, tile, wave, t.depth - c0);
+        else tx.load(q, tile, wave, int64_t(t.depth - c0) * 2);
+    };
+    auto load_w = [&](int q, uint8_t* tile, int32_t c0) {
         if constexpr (OP == DW) {
             if (by_source) {
-                tw.load_by_source(q, slot, lane, wave, left, a.source_rows);
-                if (q == W::LOADS - 1) tw.by_source(a.source + t.s.first + c0 + 32, left - 32, wave);
+                tw.load_by_source(q, tile, wave, t.depth - c0, a.source_rows);
+                if (q == LOADS - 1) tw.by_source(a.source + t.s.first + c0 + 64, t.depth - c0 - 64, wave);
             } else {
-                tw.load(q, slot, wave, left);
+                tw.load(q, tile, wave, t.depth - c0);
             }
         } else if constexpr (W_TURNED) {
-            tw.load(q, slot, wave, left);
+            tw.load(q, tile, wave, t.depth - c0);
         } else {
-            tw.load(q, slot, wave, int64_t(left) * 2);
+            tw.load(q, tile, wave, int64_t(t.depth - c0) * 2);
+        }
+    };
+    auto load_row = [&](int i, uint8_t* xt, uint8_t* wt, int32_t c0) {      // those beside row i: x of the step from c0 on, w of the next
+#pragma unroll
+        for (int p = i * EACH; p < (i + 1) * EACH; p++) {
+            if (p < LOADS) load_x(p, xt, c0);
+            else load_w(p - LOADS, wt, c0 + 64);
         }
     };
 
     f32x4 acc[TJ][TI] = {};
     const int wi = wave / WJ * (TI * 16), wj = wave % WJ * (TJ * 16);      // this wavefront's part of the tile
     const bool some = t.i0 + wi < t.i_end;                                 // ... has a row
-    // X's rows but the last are read into the registers of the rows just multiplied; W's and the last have two sets.
+    const uint32_t x_at = X::where(wi, lane), w_at = W::where(wj, lane);
+    // X's rows but the last two are read into the registers of the rows just multiplied; W's and those have two sets.
     struct Operands {
-        uint4 w[TJ], last;
+        uint4 w[TJ], last[2];
     };
-    uint4 rows[TI - 1];
-    const uint32_t x_at = X::where(wi, lane), w_at = BI * 64 + W::where(wj, lane);
-    auto block = [&](const Operands& now, Operands& next, uint8_t* free, const uint8_t* ready, int32_t c0) {
-        if (some) {
-            const uint32_t slot = lds_address(ready);
+    uint4 rows[TI - 2];
+    // A half: its products, the reads of the half k from these tiles, and the loads into x_free, w_free if LOAD.
+    auto half = [&](auto load, const Operands& now, Operands& next, const uint8_t* xt, const uint8_t* wt, int k, uint8_t* x_free, uint8_t* w_free, int32_t c0) {
+        constexpr bool LOAD = decltype(load)::value;
+        if (!some) {
+            if (LOAD)
 #pragma unroll
-            for (int i = 0; i < TI; i++) {
-                constexpr int EACH = TJ > 2 ? TJ / 2 : 1;
-                if (i * EACH < TJ)
-#pragma unroll
-                    for (int j = i * EACH; j < (i + 1) * EACH; j++) next.w[j] = W::read(slot + w_at, j, 0);
-                if (i == 2) next.last = X::read(slot + x_at, TI - 1, 0);
-                if (i > 0) rows[i - 1] = X::read(slot + x_at, i - 1, 0);
-                if (i < LOADS) load(i, free, c0 + SLOTS * 32);
-#pragma unroll
-                for (int j = 0; j < TJ; j++) acc[j][i] = multiply(now.w[j], i < TI - 1 ? rows[i] : now.last, acc[j][i], T());
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; i++) load(i, free, c0 + SLOTS * 32);
+                for (int i = 0; i < TI; i++) load_row(i, x_free, w_free, c0);
+            return;
         }
-        landed<(SLOTS - 2) * LOADS>();
+        const uint32_t xr = lds_address(xt) + x_at, wr = lds_address(wt) + w_at;
+#pragma unroll
+        for (int i = 0; i < TI; i++) {
+            if (i < 2)
+#pragma unroll
+                for (int j = i * TJ / 2; j < (i + 1) * TJ / 2; j++) next.w[j] = W::read(wr, j, k);
+            else if (i < 4) next.last[i - 2] = X::read(xr, TI - 4 + i, k);
+            if (i > 0 && i < TI - 1) rows[i - 1] = X::read(xr, i - 1, k);
+            if (LOAD) load_row(i, x_free, w_free, c0);
+#pragma unroll
+            for (int j = 0; j < TJ; j++) acc[j][i] = multiply(now.w[j], i < TI - 2 ? rows[i] : now.last[i - TI + 2], acc[j][i], T());
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     if (t.depth > 0) {
         Operands even, odd;
+        // tiles in the ring: w 0, x 0, w 1, x 1, w 2
+        uint8_t* place[RING] = {lds, lds + TILE, lds + 2 * TILE, lds + 3 * TILE, lds + 4 * TILE};
 #pragma unroll
-        for (int s = 0; s < SLOTS; s++)
+        for (int s = 0; s < RING; s++) {
 #pragma unroll
-            for (int i = 0; i < LOADS; i++) load(i, lds + s * SLOT, s * 32);
-        landed<(SLOTS - 2) * LOADS>();
+            for (int q = 0; q < LOADS; q++) {
+                if (s & 1) {
+                    load_x(q, place[s], s / 2 * 64);
+                } else {
+                    if constexpr (OP == DW) {
+                        if (by_source && q == 0) tw.here(lane);
+                    }
+                    load_w(q, place[s], s / 2 * 64);
+                }
+            }
+        }
+        landed<3 * LOADS>();
+        const uint32_t xr = lds_address(place[1]) + x_at, wr = lds_address(place[0]) + w_at;
 #pragma unroll
-        for (int j = 0; j < TJ; j++) even.w[j] = W::read(lds_address(lds) + w_at, j, 0);
+        for (int j = 0; j < TJ; j++) even.w[j] = W::read(wr, j, 0);
 #pragma unroll
-        for (int i = 0; i < TI - 1; i++) rows[i] = X::read(lds_address(lds) + x_at, i, 0);
-        even.last = X::read(lds_address(lds) + x_at, TI - 1, 0);
-        uint8_t *free = lds, *ready = lds + SLOT;
-        auto after = [&](uint8_t* slot) { return slot == lds + (SLOTS - 1) * SLOT ? lds : slot + SLOT; };
+        for (int i = 0; i < TI - 2; i++) rows[i] = X::read(xr, i, 0);
+        even.last[0] = X::read(xr, TI - 2, 0), even.last[1] = X::read(xr, TI - 1, 0);
+        uint8_t *w_now = place[0], *x_now = place[1], *w_next = place[2], *x_next = place[3], *w_after = place[4];
         for (int32_t c0 = 0; c0 < t.depth; c0 += 64) {
-            block(even, odd, free, ready, c0);
-            if (c0 + 32 >= t.depth) break;
-            free = ready, ready = after(ready);
-            block(odd, even, free, ready, c0 + 32);
-            free = ready, ready = after(ready);
+            half(std::false_type(), even, odd, x_now, w_now, 1, nullptr, nullptr, 0);
+            landed<LOADS>();                    // all but the loads of w_after
+            if constexpr (OP == DW) {
+                if (by_source) tw.here(lane);
+            }
+            // x of the step after the next goes to w_now, w of the one after that to x_now
+            half(std::true_type(), odd, even, x_next, w_next, 0, w_now, x_now, c0 + 128);
+            uint8_t *const xa = w_now, *const wa = x_now;
+            w_now = w_next, x_now = x_next, w_next = w_after, x_next = xa, w_after = wa;
         }
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
@@ -532,8 +560,8 @@ template <typename Y, int BI, int BJ, int WI, int WJ, bool W1>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int row_tiles, int col_tiles) {
     constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, SLOT = (BI + BJ) * (128 + 4), SCALES = (BI + BJ) * 128;
     static_assert(BI + BJ == WAVES * 64, "a thread per scale");
-    using X = Straight<BI, WAVES, 128>;
-    using W = Straight<BJ, WAVES, 128>;
+    using X = Straight<BI, WAVES>;
+    using W = Straight<BJ, WAVES>;
     constexpr int LOADS = X::LOADS + W::LOADS, EACH = (LOADS + TI - 1) / TI;
     __shared__ __align__(16) uint8_t lds[2 * SLOT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -725,7 +753,7 @@ template <typename T, typename Y, int OP> int launch_plain(const Product& a, hip
     return launched();
 }
 
-template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ, int SLOTS> int launch_tiled(const Product& a, hipStream_t s) {
+template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int launch_tiled(const Product& a, hipStream_t s) {
     const int64_t cols = divide_up(a.cols, BJ);
     const int64_t rows = OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : int64_t(divide_up(a.rows, BI)) + (a.offset ? a.groups : 0);
     const int64_t grid = (rows * cols + 7) / 8 * 8;
@@ -734,7 +762,7 @@ template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ, int SL
         if (a.w_rows == 1) k_product_f8<Y, BI, BJ, WI, WJ, true><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
         else k_product_f8<Y, BI, BJ, WI, WJ, false><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
     } else {
-        k_product<T, OP, BI, BJ, WI, WJ, SLOTS><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+        k_product<T, OP, BI, BJ, WI, WJ><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
     }
     return launched();
 }
@@ -762,8 +790,8 @@ template <typename T, typename Y, int OP> int launch(const Product& a, hipStream
         if (height <= FEW1) return launch_few<T, Y, 1>(a, s);
         if (height <= FEW2) return launch_few<T, Y, 2>(a, s);
     }
-    if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4, 5>(a, s);
-    return launch_tiled<T, Y, OP, 128, 128, 2, 2, 4>(a, s);
+    if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4>(a, s);
+    return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
 }
 
 bool half_type(int dtype) { return dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16; }
