@@ -40,6 +40,7 @@ struct Product {
     const float *xs, *ws;       // 8 bits: the scales
     int64_t xs_row, xs_block, ws_row, ws_block, ws_group;
     int32_t w_rows;
+    bool far;                   // bytes from the beginning of x to a row that a source names may pass 32 bits
 };
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -259,12 +260,27 @@ __device__ const uint4 ZEROS = {0, 0, 0, 0};
 // waits for them is landed().
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ uint32_t lds_address(const void* lds) { return uint32_t(uintptr_t((const __attribute__((address_space(3))) void*)lds)); }
+__device__ __forceinline__ uint32_t lds_address(const void* lds) {
+    return __builtin_amdgcn_readfirstlane(uint32_t(uintptr_t((const __attribute__((address_space(3))) void*)lds)));
+}
+// An address that is the same in every lane, for the compiler to know.
+template <typename P> __device__ __forceinline__ P* same(P* p) {
+    const uint64_t v = reinterpret_cast<uintptr_t>(p);
+    // the builtin's result is signed
+    const uint32_t low = uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(v))), high = uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(v >> 32)));
+    return reinterpret_cast<P*>(uint64_t(low) | uint64_t(high) << 32);
+}
 __device__ __forceinline__ void to_lds(const void* from, const void* lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(lds)), "v"(from) : "memory", "m0");
 }
+__device__ __forceinline__ void to_lds(const void* base, uint32_t offset, const void* lds) {      // base: the same in every lane
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_address(lds)), "v"(offset), "s"(same(base)) : "memory", "m0");
+}
 __device__ __forceinline__ void word_to_lds(const void* from, const void* lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(lds)), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void word_to_lds(const void* base, uint32_t offset, const void* lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_address(lds)), "v"(offset), "s"(same(base)) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 // This wavefront's loads into LDS have landed but for the last LATER, and its reads of LDS have returned; then the others' too.
@@ -277,17 +293,22 @@ template <int LATER> __device__ __forceinline__ void landed() {
 template <int HEIGHT, int WAVES> struct Straight {                  // HEIGHT rows of 128 bytes
     static constexpr int LOADS = HEIGHT / 8 / WAVES;
     static_assert(WAVES % 2 == 0, "bit 3 of a row is that of the wavefront, so a lane's chunk is the same in every load");
-    const uint8_t* p[LOADS];
-    int chunk;                  // of the step, that this lane asks for
-    template <typename Row> __device__ __forceinline__ void start(int lane, int wave, Row row) {
+    const uint8_t* base;        // moves on with the steps, the same in every lane
+    uint32_t offset[LOADS];     // from it, in 16 bytes
+    int chunk;                  // of a step, that this lane asks for
+    // row(r): bytes from `at` to the tile's row r
+    template <typename Row> __device__ __forceinline__ void start(int lane, int wave, const void* at, Row row) {
+        base = same(static_cast<const uint8_t*>(at));
         chunk = (lane & 7) ^ (((wave * 8 + lane / 8) >> 1) & 7);
 #pragma unroll
-        for (int q = 0; q < LOADS; q++) p[q] = row((q * WAVES + wave) * 8 + lane / 8) + chunk * 16;
+        for (int q = 0; q < LOADS; q++) offset[q] = uint32_t(uint64_t(row((q * WAVES + wave) * 8 + lane / 8)) >> 4) + chunk;
     }
-    // left: bytes of a row from this step on
-    __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int64_t left) {
-        to_lds(chunk * 16 < left ? p[q] : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-        p[q] += 128;
+    // left: bytes of a row from this step on.  FAST: a whole step, and no offset passes 32 bits.
+    template <bool FAST> __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int64_t left) {
+        uint8_t* const to = lds + (q * WAVES + wave) * 1024;
+        if (FAST) to_lds(base, offset[q] << 4, to);
+        else to_lds(chunk * 16 < left ? base + (uint64_t(offset[q]) << 4) : reinterpret_cast<const uint8_t*>(&ZEROS), to);
+        if (q == LOADS - 1) base += 128;
     }
     // Where in a tile this lane reads the first of the 16 x 64 bytes of rows from `first` on (a multiple of a wavefront's
     // share), and the e-th from there on of its 64 bytes k, given the address of that in a tile.
@@ -303,25 +324,25 @@ template <int COLS, int WAVES> struct Turned {                      // 64 rows o
     static constexpr int PITCH = COLS * 2, LANES = PITCH / 16, EACH = 64 / LANES, LOADS = 64 / EACH / WAVES;     // lanes of a row, rows of a load
     static_assert(COLS >= 128 && LANES <= 64, "a swizzle is over 256 bytes; a load is whole rows");
     static_assert(WAVES * EACH % 16 == 0, "bits 0, 1 and 3 of a row are the same in every load of a lane");
-    const uint8_t* p;           // this lane's chunk: of its row in load 0; with source: of row 0
+    const uint8_t* base;        // row 0 of the next step (with source: of all), the same in every lane
     int64_t pitch;              // bytes of a row in memory
     int32_t next[LOADS][EACH];  // with source: what it says for the next step, the same in every lane
     int32_t from[LOADS];        // ... and for this one, for this lane's row
     int c;                      // row of load 0 within a step
-    bool in;                    // the chunk is within the row
-    // values: address of row 0, value 0; first: the tile's first value in it; width: values of a row
+    uint32_t col;               // where this lane's chunk begins in a row, in bytes; past its end: at its last chunk
+    // values: row 0; first: the tile's first value in it; width: values of a row
     template <typename T> __device__ __forceinline__ void start(int lane, int wave, const T* values, int64_t ld, int first, int width) {
         c = wave * EACH + lane / LANES;
-        const int place = lane % LANES, col = first + (((place >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (place & 1) * 8;
-        in = col < width, pitch = ld * sizeof(T);
-        p = reinterpret_cast<const uint8_t*>(values + col);
+        const int place = lane % LANES, at = first + (((place >> 1) ^ ((c & 3) | (c >> 1 & 4))) << 4) + (place & 1) * 8;
+        base = same(reinterpret_cast<const uint8_t*>(values)), pitch = ld * sizeof(T), col = min(at, width - 8) * sizeof(T);
     }
-    __device__ __forceinline__ void by_row() { p += c * pitch; }
-    // left: rows from this step on
-    __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int left) {
-        const int at = q * WAVES * EACH;
-        to_lds(in && c + at < left ? p + at * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
-        if (q == LOADS - 1) p += 64 * pitch;
+    // left: rows from this step on.  FAST: a whole step.
+    template <bool FAST> __device__ __forceinline__ void load(int q, uint8_t* lds, int wave, int left) {
+        const int at = c + q * WAVES * EACH;
+        uint8_t* const to = lds + (q * WAVES + wave) * 1024;
+        if (FAST) to_lds(base, uint32_t(at) * uint32_t(pitch) + col, to);
+        else to_lds(at < left ? base + at * pitch + col : reinterpret_cast<const uint8_t*>(&ZEROS), to);
+        if (q == LOADS - 1) base += 64 * pitch;
     }
     // source: from the step's first row on; left: its rows.  Scalar loads: they do not wait with the loads into LDS.
     __device__ __forceinline__ void by_source(const int32_t* source, int left, int wave) {
@@ -344,8 +365,8 @@ template <int COLS, int WAVES> struct Turned {                      // 64 rows o
     }
     // what by_source() asked for a step ago; rows: that a source may name
     __device__ __forceinline__ void load_by_source(int q, uint8_t* lds, int wave, int left, int32_t rows) {
-        const bool there = in && c + q * WAVES * EACH < left && uint32_t(from[q]) < uint32_t(rows);
-        to_lds(there ? p + from[q] * pitch : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+        const bool there = c + q * WAVES * EACH < left && uint32_t(from[q]) < uint32_t(rows);
+        to_lds(there ? base + from[q] * pitch + col : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
     }
     // As Straight's, for 16 columns from `first` on; slots and rows are multiples of 256 bytes, so the e-th segment's place is
     // another pattern in bits 5 to 7.
@@ -373,7 +394,7 @@ __device__ __forceinline__ bool tile_order(int64_t b, int row_tiles, int col_til
     const int64_t total = int64_t(row_tiles) * col_tiles, per = (total + 7) / 8, at = (b & 7) * per + (b >> 3);
     if ((b >> 3) >= per || at >= total) return false;
     const int32_t strip = int32_t(at / (8 * int64_t(col_tiles))), in = int32_t(at - int64_t(strip) * 8 * col_tiles), high = min(8, row_tiles - strip * 8);
-    i = strip * 8 + in % high, j = in / high;
+    i = __builtin_amdgcn_readfirstlane(strip * 8 + in % high), j = __builtin_amdgcn_readfirstlane(in / high);
     return true;
 }
 
@@ -413,6 +434,21 @@ template <int OP, typename Y, int TI, int TJ> __device__ __forceinline__ void st
     }
 }
 
+// Where a straight tile's rows are.  With a source, from the beginning of x on; then an offset may pass 32 bits (a.far).
+template <typename T, int OP, typename X> __device__ __forceinline__ void start_x(const Product& a, const Tile& t, int lane, int wave, X& tx) {
+    const T* const x = static_cast<const T*>(a.x);
+    const int64_t pitch = a.ldx * int64_t(sizeof(T));
+    const bool by_source = OP == FWD && a.source;
+    tx.start(lane, wave, by_source ? x : x + int64_t(t.i0) * a.ldx, [&](int r) {
+        const int32_t i = min(t.i0 + r, t.i_end - 1);
+        return (by_source ? max(source_of(a, i), int64_t(0)) : i - t.i0) * pitch;
+    });
+}
+template <typename T, typename W> __device__ __forceinline__ void start_w(const Product& a, const Tile& t, int lane, int wave, W& tw) {
+    const T* const w = static_cast<const T*>(a.w) + t.s.group * a.w_group + int64_t(t.j0) * a.ldw;
+    tw.start(lane, wave, w, [&](int r) { return min(r, a.cols - 1 - t.j0) * (a.ldw * int64_t(sizeof(T))); });
+}
+
 // 16 bits.  A step is 64 values of the depth, in two halves of TI rows of TJ matrix instructions.  The operands of a half are
 // read while the one before it is multiplied.  After the first half of step s both tiles of s have been read: at the
 // barrier there, those of step s + 1 have to have landed.  LDS is a ring of five tiles, w 0, x 0, w 1, x 1 and so on; in the
@@ -438,63 +474,57 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
     W tw;
     if constexpr (X_TURNED) {
         tx.start(lane, wave, x + int64_t(t.s.first) * a.ldx, a.ldx, t.i0, t.i_end);
-        tx.by_row();
     } else {
-        tx.start(lane, wave, [&](int r) {
-            const int32_t i = min(t.i0 + r, t.i_end - 1);
-            return reinterpret_cast<const uint8_t*>(x + (OP == FWD ? max(source_of(a, i), int64_t(0)) : i) * a.ldx);
-        });
+        start_x<T, OP>(a, t, lane, wave, tx);
     }
     if constexpr (W_TURNED) {
         tw.start(lane, wave, OP == DW && !by_source ? w + int64_t(t.s.first) * a.ldw : w, a.ldw, t.j0, a.cols);
         if (by_source) tw.by_source(a.source + t.s.first, t.depth, wave);
-        else tw.by_row();
     } else {
-        tw.start(lane, wave, [&](int r) { return reinterpret_cast<const uint8_t*>(w + int64_t(min(t.j0 + r, a.cols - 1)) * a.ldw); });
+        start_w<T>(a, t, lane, wave, tw);
     }
     // load q of the tile of the step from c0 on (past the depth: zeros)
-    auto load_x = [&](int q, uint8_t* tile, int32_t c0) {
-        if constexpr (X_TURNED) tx.load(q, tile, wave, t.depth - c0);
-        else tx.load(q, tile, wave, int64_t(t.depth - c0) * 2);
+    auto load_x = [&](auto fast, int q, uint8_t* tile, int32_t c0) __attribute__((always_inline)) {
+        constexpr bool FAST = decltype(fast)::value;
+        if constexpr (X_TURNED) tx.template load<FAST>(q, tile, wave, t.depth - c0);
+        else tx.template load<FAST>(q, tile, wave, int64_t(t.depth - c0) * 2);
     };
-    auto load_w = [&](int q, uint8_t* tile, int32_t c0) {
+    auto load_w = [&](auto fast, int q, uint8_t* tile, int32_t c0) __attribute__((always_inline)) {
+        constexpr bool FAST = decltype(fast)::value;
         if constexpr (OP == DW) {
             if (by_source) {
                 tw.load_by_source(q, tile, wave, t.depth - c0, a.source_rows);
                 if (q == LOADS - 1) tw.by_source(a.source + t.s.first + c0 + 64, t.depth - c0 - 64, wave);
-            } else {
-                tw.load(q, tile, wave, t.depth - c0);
+                return;
             }
-        } else if constexpr (W_TURNED) {
-            tw.load(q, tile, wave, t.depth - c0);
-        } else {
-            tw.load(q, tile, wave, int64_t(t.depth - c0) * 2);
         }
+        if constexpr (W_TURNED) tw.template load<FAST>(q, tile, wave, t.depth - c0);
+        else tw.template load<FAST>(q, tile, wave, int64_t(t.depth - c0) * 2);
     };
-    auto load_row = [&](int i, uint8_t* xt, uint8_t* wt, int32_t c0) {      // those beside row i: x of the step from c0 on, w of the next
+    auto load_row = [&](auto fast, int i, uint8_t* xt, uint8_t* wt, int32_t c0) __attribute__((always_inline)) {     // those beside row i: x of the step from c0 on, w of the next
 #pragma unroll
         for (int p = i * EACH; p < (i + 1) * EACH; p++) {
-            if (p < LOADS) load_x(p, xt, c0);
-            else load_w(p - LOADS, wt, c0 + 64);
+            if (p < LOADS) load_x(fast, p, xt, c0);
+            else load_w(fast, p - LOADS, wt, c0 + 64);
         }
     };
 
     f32x4 acc[TJ][TI] = {};
     const int wi = wave / WJ * (TI * 16), wj = wave % WJ * (TJ * 16);      // this wavefront's part of the tile
-    const bool some = t.i0 + wi < t.i_end;                                 // ... has a row
+    const bool some = __builtin_amdgcn_readfirstlane(t.i0 + wi < t.i_end); // ... has a row
     const uint32_t x_at = X::where(wi, lane), w_at = W::where(wj, lane);
     // X's rows but the last two are read into the registers of the rows just multiplied; W's and those have two sets.
     struct Operands {
         uint4 w[TJ], last[2];
     };
     uint4 rows[TI - 2];
-    // A half: its products, the reads of the half k from these tiles, and the loads into x_free, w_free if LOAD.
-    auto half = [&](auto load, const Operands& now, Operands& next, const uint8_t* xt, const uint8_t* wt, int k, uint8_t* x_free, uint8_t* w_free, int32_t c0) {
+    // A half: its products, the reads of the half k from these tiles, and, LOAD, the loads into x_free, w_free.
+    auto half = [&](auto load, auto fast, const Operands& now, Operands& next, const uint8_t* xt, const uint8_t* wt, int k, uint8_t* x_free, uint8_t* w_free, int32_t c0) __attribute__((always_inline)) {
         constexpr bool LOAD = decltype(load)::value;
         if (!some) {
             if (LOAD)
 #pragma unroll
-                for (int i = 0; i < TI; i++) load_row(i, x_free, w_free, c0);
+                for (int i = 0; i < TI; i++) load_row(fast, i, x_free, w_free, c0);
             return;
         }
         const uint32_t xr = lds_address(xt) + x_at, wr = lds_address(wt) + w_at;
@@ -505,7 +535,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
                 for (int j = i * TJ / 2; j < (i + 1) * TJ / 2; j++) next.w[j] = W::read(wr, j, k);
             else if (i < 4) next.last[i - 2] = X::read(xr, TI - 4 + i, k);
             if (i > 0 && i < TI - 1) rows[i - 1] = X::read(xr, i - 1, k);
-            if (LOAD) load_row(i, x_free, w_free, c0);
+            if (LOAD) load_row(fast, i, x_free, w_free, c0);
 #pragma unroll
             for (int j = 0; j < TJ; j++) acc[j][i] = multiply(now.w[j], i < TI - 2 ? rows[i] : now.last[i - TI + 2], acc[j][i], T());
             __builtin_amdgcn_sched_barrier(0);
@@ -520,12 +550,12 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
 #pragma unroll
             for (int q = 0; q < LOADS; q++) {
                 if (s & 1) {
-                    load_x(q, place[s], s / 2 * 64);
+                    load_x(std::false_type(), q, place[s], s / 2 * 64);
                 } else {
                     if constexpr (OP == DW) {
                         if (by_source && q == 0) tw.here(lane);
                     }
-                    load_w(q, place[s], s / 2 * 64);
+                    load_w(std::false_type(), q, place[s], s / 2 * 64);
                 }
             }
         }
@@ -537,118 +567,142 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
         for (int i = 0; i < TI - 2; i++) rows[i] = X::read(xr, i, 0);
         even.last[0] = X::read(xr, TI - 2, 0), even.last[1] = X::read(xr, TI - 1, 0);
         uint8_t *w_now = place[0], *x_now = place[1], *w_next = place[2], *x_next = place[3], *w_after = place[4];
-        for (int32_t c0 = 0; c0 < t.depth; c0 += 64) {
-            half(std::false_type(), even, odd, x_now, w_now, 1, nullptr, nullptr, 0);
+        auto step = [&](auto fast, int32_t c0) __attribute__((always_inline)) {
+            half(std::false_type(), fast, even, odd, x_now, w_now, 1, nullptr, nullptr, 0);
             landed<LOADS>();                    // all but the loads of w_after
             if constexpr (OP == DW) {
                 if (by_source) tw.here(lane);
             }
             // x of the step after the next goes to w_now, w of the one after that to x_now
-            half(std::true_type(), odd, even, x_next, w_next, 0, w_now, x_now, c0 + 128);
+            half(std::true_type(), fast, odd, even, x_next, w_next, 0, w_now, x_now, c0 + 128);
             uint8_t *const xa = w_now, *const wa = x_now;
             w_now = w_next, x_now = x_next, w_next = w_after, x_next = xa, w_after = wa;
-        }
+        };
+        int32_t c0 = 0;
+        if (!a.far)
+            for (; c0 + 256 <= t.depth; c0 += 64) step(std::true_type(), c0);
+        for (; c0 < t.depth; c0 += 64) step(std::false_type(), c0);
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
     store_tile<OP, T, TI, TJ>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
 }
 
-// 8 bits.  A step is a block of 128 values: one matrix instruction per 16 x 16 results, whose sum is scaled and added in 32
-// bits.  Two slots, the scales beside the values; the loads of a step are dealt out between the rows of products of the one
-// before.  W1: a scale per row of w.
-template <typename Y, int BI, int BJ, int WI, int WJ, bool W1>
+// 8 bits.  A step is a block of 128 values: one matrix instruction per 16 x 16 results, which starts from 0 (its own sum is
+// exact to 2^-15 or so of the largest product) and whose result is scaled and added in 32 bits, beside the instructions of
+// the next row of tiles.  LDS holds two tiles of w, XRING of x and three sets of scales.  Two rows of tiles before a step's
+// end everything of the step has been read; at the barrier there the next step has to have landed, and its first operands
+// are read beside the last two rows.  From there on the loads of w s + 2 are asked for, then, XRING = 3, of x s + 3: that
+// half of the loads has two steps to land.  W1: a scale per row of w.
+template <typename Y, int BI, int BJ, int WI, int WJ, int XRING, bool W1>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int row_tiles, int col_tiles) {
-    constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, SLOT = (BI + BJ) * (128 + 4), SCALES = (BI + BJ) * 128;
-    static_assert(BI + BJ == WAVES * 64, "a thread per scale");
+    constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16;
+    static_assert(BI + BJ <= WAVES * 64 && 128 % (TJ * 16) == 0 && TI >= 4, "a thread per scale; a wavefront's columns share one");
     using X = Straight<BI, WAVES>;
     using W = Straight<BJ, WAVES>;
-    constexpr int LOADS = X::LOADS + W::LOADS, EACH = (LOADS + TI - 1) / TI;
-    __shared__ __align__(16) uint8_t lds[2 * SLOT];
+    constexpr int LOADS = W::LOADS + 1 + X::LOADS, EACH = (LOADS + TI - 2) / (TI - 1), SETS = TI % 3 ? 4 : 3;
+    constexpr int X_TILE = BI * 128, W_TILE = BJ * 128, S_TILE = WAVES * 256;
+    __shared__ __align__(1024) uint8_t lds[XRING * X_TILE + 2 * W_TILE + 3 * S_TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Tile t;
     if (!find<FWD, BI, BJ>(a, row_tiles, col_tiles, t)) return;
-    const uint8_t* const w = static_cast<const uint8_t*>(a.w) + t.s.group * a.w_group;
-    const uint8_t* const x = static_cast<const uint8_t*>(a.x);
     X tx;
     W tw;
-    tx.start(lane, wave, [&](int r) { return x + max(source_of(a, min(t.i0 + r, t.i_end - 1)), int64_t(0)) * a.ldx; });
-    tw.start(lane, wave, [&](int r) { return w + int64_t(min(t.j0 + r, a.cols - 1)) * a.ldw; });
-    const float* scale;
-    int64_t scale_step;
-    if (tid < BI) {
-        scale = a.xs + max(source_of(a, min(t.i0 + tid, t.i_end - 1)), int64_t(0)) * a.xs_row, scale_step = a.xs_block;
-    } else {
-        scale = a.ws + t.s.group * a.ws_group + min(t.j0 + tid - BI, a.cols - 1) / a.w_rows * a.ws_row, scale_step = a.ws_block;
-    }
-    auto load = [&](int part, uint8_t* slot, int32_t c0) {
-        if (part == 0) {
-            word_to_lds(c0 < t.depth ? static_cast<const void*>(scale) : &ZEROS, slot + SCALES + wave * 256);
-            scale += scale_step;
-        }
-        if (part < X::LOADS) tx.load(part, slot, wave, t.depth - c0);
-        else tw.load(part - X::LOADS, slot + BI * 128, wave, t.depth - c0);
+    start_x<f8, FWD>(a, t, lane, wave, tx);
+    start_w<f8>(a, t, lane, wave, tw);
+    // A thread's scale: the first wavefronts' of x, the next ones' of w (whatever the last ones get is not used).
+    const bool of_x = wave * 64 < BI;
+    const float* scale = same(of_x ? a.xs : a.ws + t.s.group * a.ws_group);
+    const int64_t scale_step = of_x ? a.xs_block : a.ws_block;
+    const int64_t scale_at = of_x ? max(source_of(a, min(t.i0 + tid, t.i_end - 1)), int64_t(0)) * a.xs_row : min(t.j0 + tid - BI, a.cols - 1) / a.w_rows * a.ws_row;
+    auto load_scales = [&](auto fast, uint8_t* tile, int32_t c0) __attribute__((always_inline)) {
+        if (decltype(fast)::value) word_to_lds(scale, uint32_t(scale_at) * 4, tile + wave * 256);
+        else word_to_lds(c0 < t.depth ? static_cast<const void*>(scale + scale_at) : &ZEROS, tile + wave * 256);
+        scale += scale_step;
     };
 
     f32x4 acc[TJ][TI] = {};
     const int wi = wave / WJ * (TI * 16), wj = wave % WJ * (TJ * 16);
-    const bool some = t.i0 + wi < t.i_end;
+    const uint32_t x_at = X::where(wi, lane), w_at = W::where(wj, lane);
     auto both = [](uint4 lo, uint4 hi) { return i32x8{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)}; };
-    const uint32_t x_at = X::where(wi, lane), w_at = BI * 128 + W::where(wj, lane);
-    // the step in slot `ready`, and the loads of the one from c0 on (past the depth: zeros) into the slot `free`
-    auto step = [&](const uint8_t* ready, uint8_t* free, int32_t c0) {
-        if (!some) {
-#pragma unroll
-            for (int p = 0; p < LOADS; p++) load(p, free, c0);
-            return;
-        }
-        const uint32_t x_in = lds_address(ready) + x_at, w_in = lds_address(ready) + w_at;
-        const float* const xs_at = reinterpret_cast<const float*>(ready + SCALES) + wi + (lane & 15);
-        const float* const ws_at = reinterpret_cast<const float*>(ready + SCALES) + BI + wj;
-        i32x8 wv[TJ], xv = both(X::read(x_in, 0, 0), X::read(x_in, 0, 1));
-        f32x4 ws[W1 ? TJ : 1];
-#pragma unroll
-        for (int j = 0; j < TJ; j++) wv[j] = both(W::read(w_in, j, 0), W::read(w_in, j, 1));
-        if (W1) {
-#pragma unroll
-            for (int j = 0; j < TJ; j++) ws[j] = *reinterpret_cast<const f32x4*>(ws_at + j * 16 + (lane >> 4) * 4);
-        }
-        const float one = W1 ? 1.f : *ws_at;            // TJ * 16 columns that begin at a multiple of that: within 128
-        // A row of products at a time, the sums of the one before it scaled and added beside it.  Nothing moves between
-        // rows: the compiler would keep more of them in flight than there are registers.
-        f32x4 part[2][TJ];
-        float xs = xs_at[0] * one, before = 0.f;
-#pragma unroll
-        for (int i = 0; i <= TI; i++) {
-            i32x8 next = xv;
-            if (i + 1 < TI) next = both(X::read(x_in, i + 1, 0), X::read(x_in, i + 1, 1));
-#pragma unroll
-            for (int p = i * EACH; p < min((i + 1) * EACH, LOADS); p++) load(p, free, c0);
-            if (i < TI) {
-#pragma unroll
-                for (int j = 0; j < TJ; j++)
-                    part[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-            }
-            if (i > 0) {
-#pragma unroll
-                for (int j = 0; j < TJ; j++)
-#pragma unroll
-                    for (int q = 0; q < 4; q++) acc[j][i - 1][q] = fmaf(part[~i & 1][j][q], W1 ? before * ws[j][q] : before, acc[j][i - 1][q]);
-            }
-            xv = next, before = xs;
-            if (i + 1 < TI) xs = xs_at[i * 16 + 16] * one;
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
     if (t.depth > 0) {
+        uint8_t *x_now = lds, *x_next = lds + X_TILE, *x_free = lds + (XRING - 1) * X_TILE;
+        uint8_t *w_now = lds + XRING * X_TILE, *w_next = w_now + W_TILE;
+        uint8_t *s_now = w_next + W_TILE, *s_next = s_now + S_TILE, *s_after = s_next + S_TILE;
+        // Turn `turn` of the loads that a step's barrier lets go: w and the scales of the step from c0 on, then x of that
+        // or, XRING = 3, the next one.
+        auto load = [&](auto fast, int turn, uint8_t* wt, uint8_t* st, uint8_t* xt, int32_t c0) __attribute__((always_inline)) {
+            constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
-        for (int p = 0; p < LOADS; p++) load(p, lds, 0);
-        for (int32_t c0 = 0; c0 < t.depth; c0 += 256) {
-            landed<0>();
-            step(lds, lds + SLOT, c0 + 128);
-            if (c0 + 128 >= t.depth) break;
-            landed<0>();
-            step(lds + SLOT, lds, c0 + 256);
-        }
+            for (int p = turn * EACH; p < min((turn + 1) * EACH, LOADS); p++) {
+                if (p < W::LOADS) tw.template load<FAST>(p, wt, wave, t.depth - c0);
+                else if (p == W::LOADS) load_scales(fast, st, c0);
+                else tx.template load<FAST>(p - W::LOADS - 1, xt, wave, t.depth - c0 - (XRING - 2) * 128);
+            }
+        };
+        // As a step finds it: step 0 (of x, XRING = 3, step 1 too), and the first two turns of what comes next.
+#pragma unroll
+        for (int q = 0; q < W::LOADS; q++) tw.template load<false>(q, w_now, wave, t.depth);
+        load_scales(std::false_type(), s_now, 0);
+#pragma unroll
+        for (int r = 0; r < XRING - 1; r++)
+#pragma unroll
+            for (int q = 0; q < X::LOADS; q++) tx.template load<false>(q, lds + r * X_TILE, wave, t.depth - r * 128);
+        landed<0>();
+        load(std::false_type(), 0, w_next, s_next, x_free, 128);
+        load(std::false_type(), 1, w_next, s_next, x_free, 128);
+        i32x8 wv[TJ], xv[SETS];         // w's operands, x's two rows ahead of the products
+        f32x4 part[2][TJ] = {}, ws[W1 ? TJ : 1] = {}, ws_before[W1 ? TJ : 1];
+        float before = 0.f, one_before = 0.f;       // x's scale of the row of tiles before, w's
+#pragma unroll
+        for (int j = 0; j < TJ; j++) wv[j] = both(W::read(lds_address(w_now) + w_at, j, 0), W::read(lds_address(w_now) + w_at, j, 1));
+#pragma unroll
+        for (int i = 0; i < 2; i++) xv[i] = both(X::read(lds_address(x_now) + x_at, i, 0), X::read(lds_address(x_now) + x_at, i, 1));
+        auto step = [&](auto fast, int32_t c0) __attribute__((always_inline)) {
+            const float* const xs_at = reinterpret_cast<const float*>(s_now) + wi + (lane & 15);
+            const float* const ws_at = reinterpret_cast<const float*>(s_now) + BI + wj;
+            float one = 1.f;
+            if (W1) {
+#pragma unroll
+                for (int j = 0; j < TJ; j++) ws_before[W1 ? j : 0] = ws[W1 ? j : 0], ws[W1 ? j : 0] = *reinterpret_cast<const f32x4*>(ws_at + j * 16 + (lane >> 4) * 4);
+            } else {
+                one = *ws_at;
+            }
+#pragma unroll
+            for (int i = 0; i < TI; i++) {
+                if (i == TI - 2) landed<(XRING - 2) * X::LOADS>();
+                // From the barrier on the loads into what has been read: w_now, the scales of the step before, x_now.
+                if (i >= TI - 2) load(fast, i - (TI - 2), w_now, s_after, x_now, c0 + 256);
+                else load(fast, i + 2, w_next, s_next, x_free, c0 + 128);
+                const uint32_t xr = lds_address(i < TI - 2 ? x_now : x_next) + x_at, wr = lds_address(w_next) + w_at;
+                const int e = i < TI - 2 ? i + 2 : i - (TI - 2);
+                xv[(i + 2) % SETS] = both(X::read(xr, e, 0), X::read(xr, e, 1));
+                const float by_x = before * one_before, xs = xs_at[i * 16];
+#pragma unroll
+                for (int j = 0; j < TJ; j++) {
+                    // scales 0: the form of the instruction without scales
+                    part[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv[i % SETS], f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+                    if (i == TI - 1) wv[j] = both(W::read(wr, j, 0), W::read(wr, j, 1));
+                    f32x4& to = acc[j][(i + TI - 1) % TI];
+                    const f32x4 by = i > 0 ? ws[W1 ? j : 0] : ws_before[W1 ? j : 0];
+#pragma unroll
+                    for (int q = 0; q < 4; q++) to[q] = fmaf(part[~i & 1][j][q], W1 ? before * by[q] : by_x, to[q]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                before = xs, one_before = one;
+            }
+            uint8_t *const w_old = w_now, *const x_old = x_now, *const s_old = s_now;
+            w_now = w_next, w_next = w_old;
+            s_now = s_next, s_next = s_after, s_after = s_old;
+            x_now = x_next, x_next = XRING == 3 ? x_free : x_old, x_free = x_old;
+        };
+        int32_t c0 = 0;
+        if (!a.far)
+            for (; c0 + 128 * (XRING + 1) <= t.depth; c0 += 128) step(std::true_type(), c0);
+        for (; c0 < t.depth; c0 += 128) step(std::false_type(), c0);
+#pragma unroll
+        for (int j = 0; j < TJ; j++)        // the last row of tiles
+#pragma unroll
+            for (int q = 0; q < 4; q++) acc[j][TI - 1][q] = fmaf(part[(TI - 1) & 1][j][q], W1 ? before * ws[W1 ? j : 0][q] : before * one_before, acc[j][TI - 1][q]);
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
     store_tile<FWD, Y, TI, TJ>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
@@ -759,8 +813,9 @@ template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int la
     const int64_t grid = (rows * cols + 7) / 8 * 8;
     if (grid > INT32_MAX) return CSR5_ERANGE;
     if constexpr (is_f8<T>) {
-        if (a.w_rows == 1) k_product_f8<Y, BI, BJ, WI, WJ, true><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
-        else k_product_f8<Y, BI, BJ, WI, WJ, false><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+        constexpr int XRING = BI > 128 ? 3 : 2;         // 128 x 128: two workgroups on a CU
+        if (a.w_rows == 1) k_product_f8<Y, BI, BJ, WI, WJ, XRING, true><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
+        else k_product_f8<Y, BI, BJ, WI, WJ, XRING, false><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
     } else {
         k_product<T, OP, BI, BJ, WI, WJ><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
     }
@@ -775,22 +830,32 @@ template <typename T, typename Y, int TI> int launch_few(const Product& a, hipSt
     return launched();
 }
 
-// Rows of whole 16-byte chunks, at 16-byte addresses; results at addresses of four values.
+// Offsets that do not fit 32 bits.
+constexpr int64_t MOST_BYTES = int64_t(1) << 32;
+bool far(const Product& a, int64_t size) {
+    auto past = [](int64_t rows, int64_t pitch) { return pitch < 0 || rows * pitch >= MOST_BYTES; };
+    return (a.source && past(a.source_rows, a.ldx * size)) || past(a.source_rows, a.xs_row * 4) || past(a.cols, a.ws_row * 4);
+}
+
+// Rows of whole 16-byte chunks, at 16-byte addresses, a tile of which offsets of 32 bits reach; results at addresses of four
+// values.
 template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
     constexpr int SIZE = sizeof(T);
     auto whole = [](int64_t n) { return n * SIZE % 16 == 0; };
     return aligned(a.x, a.ldx, SIZE, 16) && aligned(a.w, a.ldw, SIZE, 16) && whole(a.w_group) && aligned(a.y, a.ldy, sizeof(Y), 4 * sizeof(Y)) &&
-           a.y_group % 4 == 0 && (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
+           a.y_group % 4 == 0 && a.ldx * SIZE < MOST_BYTES / 256 && a.ldw * SIZE < MOST_BYTES / 256 && (!a.source || int64_t(a.source_rows) * a.ldx * SIZE < 16 * MOST_BYTES) &&
+           (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
 }
 
-template <typename T, typename Y, int OP> int launch(const Product& a, hipStream_t s) {
+template <typename T, typename Y, int OP> int launch(Product a, hipStream_t s) {
     if (!chunks_fit<T, Y, OP>(a)) return launch_plain<T, Y, OP>(a, s);
+    a.far = far(a, sizeof(T));
     const int64_t height = OP == DW ? a.out_rows : a.rows / a.groups;
     if constexpr (OP == FWD) {
         if (height <= FEW1) return launch_few<T, Y, 1>(a, s);
         if (height <= FEW2) return launch_few<T, Y, 2>(a, s);
     }
-    if (height >= 192) return launch_tiled<T, Y, OP, 256, 256, 2, 4>(a, s);
+    if (height >= 192) return launch_tiled<T, Y, OP, is_f8<T> ? 192 : 256, 256, 2, 4>(a, s);
     return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
 }
 
