@@ -448,7 +448,7 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
  *   place    int32[tokens*k]      the row of each pair
  *   workspace  csr5_route_workspace_bytes bytes (0: may be NULL), free again after the call
  * 1 <= k <= min(experts, CSR5_ROUTE_MAX_K), experts <= CSR5_ROUTE_MAX_EXPERTS and
- * tokens*k < 2^31, else CSR5_ERANGE (workspace bytes: 0).
+ * tokens*k < 2^31 - 2^16, else CSR5_ERANGE (workspace bytes: 0).
  */
 size_t csr5_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t k);
 int csr5_route(int32_t tokens, int32_t experts, int32_t k, int dtype, const void *logits, int64_t ld,

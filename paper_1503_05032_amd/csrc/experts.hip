@@ -28,24 +28,26 @@ __device__ __forceinline__ void wave_order() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// The sum of v over the workgroup, for everybody.  `part` holds a word per wavefront and is not used again before the
-// next barrier.
-template <int TPB> __device__ __forceinline__ float group_sum(float v, float* part) {
-    v = lanes_sum<64>(v);
-    if (TPB == 64) return v;
+// The sum of v over the workgroup, for everybody, in a fixed order.  `part` holds a word per wavefront and is not used again
+// before the next barrier.
+__device__ __forceinline__ float group_sum(float v, float* part) {
+    v = wave_sum(v);
+    const int waves = blockDim.x >> 6;
+    if (waves == 1) return v;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.f;
-#pragma unroll
-    for (int w = 0; w < TPB / 64; w++) v += part[w];
+    for (int w = 0; w < waves; w++) v += part[w];
     return v;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
 // Root-mean-square norm.  One workgroup per row, which it holds in registers between the sum of squares and the
 // output: x and the residual are read once.  8 neighbouring values per thread, so a block of 128 values that share a
-// scale is 16 neighbouring lanes.
+// scale is 16 neighbouring lanes; as many threads as the row has eights, up to 1024, then NV eights per thread.
 // ---------------------------------------------------------------------------------------------------------------
+constexpr int NORM_THREADS = 1024;
+
 template <typename T> struct NormArgs {
     int n;
     const T *x, *residual, *gain;
@@ -60,14 +62,14 @@ template <typename T> struct NormArgs {
     float* rstd;
 };
 
-template <typename T, int TPB, int NV, bool VEC> __global__ __launch_bounds__(TPB) void k_rmsnorm(NormArgs<T> a) {
-    __shared__ float part[TPB / 64];
+template <typename T, int NV, bool VEC> __global__ __launch_bounds__(NORM_THREADS) void k_rmsnorm(NormArgs<T> a) {
+    __shared__ float part[NORM_THREADS / 64];
     const int64_t row = blockIdx.x;
     float v[NV][8];
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < NV; c++) {
-        const int col = (c * TPB + int(threadIdx.x)) * 8;
+        const int col = (c * int(blockDim.x) + int(threadIdx.x)) * 8;
         load_values<8, VEC>(a.x + row * a.ldx + col, a.n - col, v[c]);
         if (a.residual) {
             float r[8];
@@ -78,16 +80,16 @@ template <typename T, int TPB, int NV, bool VEC> __global__ __launch_bounds__(TP
     }
 #pragma unroll
     for (int c = 0; c < NV; c++) {
-        const int col = (c * TPB + int(threadIdx.x)) * 8;
+        const int col = (c * int(blockDim.x) + int(threadIdx.x)) * 8;
 #pragma unroll
         for (int i = 0; i < 8; i++) sum += v[c][i] * v[c][i];
         if (a.h) store_values<8, VEC>(a.h + row * a.ldh + col, a.n - col, v[c]);
     }
-    const float rstd = 1.f / sqrtf(group_sum<TPB>(sum, part) / float(a.n) + a.eps);
+    const float rstd = 1.f / sqrtf(group_sum(sum, part) / float(a.n) + a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int c = 0; c < NV; c++) {
-        const int col = (c * TPB + int(threadIdx.x)) * 8;
+        const int col = (c * int(blockDim.x) + int(threadIdx.x)) * 8;
         float g[8];
         if (a.gain) load_values<8, VEC>(a.gain + col, a.n - col, g);
 #pragma unroll
@@ -119,55 +121,58 @@ template <typename T> struct NormBackArgs {
     float* share;           // [gridDim.x][n], NULL: not wanted
 };
 
-template <typename T, int TPB, int NV, bool VEC> __global__ __launch_bounds__(TPB) void k_rmsnorm_back(NormBackArgs<T> a) {
-    __shared__ float part[2][TPB / 64];
+// The next row's h and dy are asked for before this row's sum.
+template <typename T, int NV, bool VEC> __global__ __launch_bounds__(NORM_THREADS) void k_rmsnorm_back(NormBackArgs<T> a) {
+    __shared__ float part[2][NORM_THREADS / 64];
     float gain[NV][8], share[NV][8];
+    auto at = [](int c) { return (c * int(blockDim.x) + int(threadIdx.x)) * 8; };
 #pragma unroll
     for (int c = 0; c < NV; c++) {
-        const int col = (c * TPB + int(threadIdx.x)) * 8;
-        if (a.gain) load_values<8, VEC>(a.gain + col, a.n - col, gain[c]);
+        if (a.gain) load_values<8, VEC>(a.gain + at(c), a.n - at(c), gain[c]);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             share[c][i] = 0.f;
             if (!a.gain) gain[c][i] = 1.f;
         }
     }
+    vec<T, 8> h[NV], dy[NV];
+    auto ask = [&](int64_t row) {
+#pragma unroll
+        for (int c = 0; c < NV; c++) {
+            h[c] = eight_values<VEC>(a.h + row * a.ldh + at(c), a.n - at(c));
+            dy[c] = eight_values<VEC>(a.dy + row * a.lddy + at(c), a.n - at(c));
+        }
+    };
+    if (blockIdx.x < a.rows) ask(blockIdx.x);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const float r = a.rstd[row];
         float v[NV][8], u[NV][8], sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < NV; c++) {
-            const int col = (c * TPB + int(threadIdx.x)) * 8;
-            load_values<8, VEC>(a.h + row * a.ldh + col, a.n - col, v[c]);
-            load_values<8, VEC>(a.dy + row * a.lddy + col, a.n - col, u[c]);
-        }
-#pragma unroll
         for (int c = 0; c < NV; c++)
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                v[c][i] *= r;
+                v[c][i] = float(h[c][i]) * r, u[c][i] = float(dy[c][i]);
                 share[c][i] += u[c][i] * v[c][i];
                 u[c][i] *= gain[c][i];
                 sum += u[c][i] * v[c][i];
             }
-        const float mean = group_sum<TPB>(sum, part[turn]) / float(a.n);
+        float d[NV][8];
+        if (a.residual_grad)
+#pragma unroll
+            for (int c = 0; c < NV; c++) load_values<8, VEC>(a.residual_grad + row * a.ldrg + at(c), a.n - at(c), d[c]);
+        if (row + gridDim.x < a.rows) ask(row + gridDim.x);
+        const float mean = group_sum(sum, part[turn]) / float(a.n);
 #pragma unroll
         for (int c = 0; c < NV; c++) {
-            const int col = (c * TPB + int(threadIdx.x)) * 8;
-            float d[8];
-            if (a.residual_grad) load_values<8, VEC>(a.residual_grad + row * a.ldrg + col, a.n - col, d);
 #pragma unroll
-            for (int i = 0; i < 8; i++) d[i] = r * (u[c][i] - v[c][i] * mean) + (a.residual_grad ? d[i] : 0.f);
-            store_values<8, VEC>(a.dh + row * a.lddh + col, a.n - col, d);
+            for (int i = 0; i < 8; i++) d[c][i] = r * (u[c][i] - v[c][i] * mean) + (a.residual_grad ? d[c][i] : 0.f);
+            store_values<8, VEC>(a.dh + row * a.lddh + at(c), a.n - at(c), d[c]);
         }
     }
     if (a.share)
 #pragma unroll
-        for (int c = 0; c < NV; c++) {
-            const int col = (c * TPB + int(threadIdx.x)) * 8;
-            store_values<8, false>(a.share + int64_t(blockIdx.x) * a.n + col, a.n - col, share[c]);
-        }
+        for (int c = 0; c < NV; c++) store_values<8, false>(a.share + int64_t(blockIdx.x) * a.n + at(c), a.n - at(c), share[c]);
 }
 
 // out[col] = sum over `rows` rows; 32 columns and 32 rows side by side.
@@ -176,6 +181,7 @@ __global__ __launch_bounds__(1024) void k_columns(int rows, int n, const float* 
     const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = int(blockIdx.x) * 32 + c;
     float sum = 0.f;
     if (col < n)
+#pragma unroll 8
         for (int i = r; i < rows; i += 32) sum += in[int64_t(i) * n + col];
     part[r][c] = sum;
     __syncthreads();
@@ -185,15 +191,12 @@ __global__ __launch_bounds__(1024) void k_columns(int rows, int n, const float* 
     }
 }
 
-// The shapes of the norm's kernels: threads of a row's workgroup, and how many times 8 values a thread holds.
+// Threads of a row's workgroup, and how many times 8 values a thread holds.
 template <typename F> void norm_shape(int n, F f) {
-    using std::integral_constant;
-    if (n <= 512) f(integral_constant<int, 64>(), integral_constant<int, 1>());
-    else if (n <= 2048) f(integral_constant<int, 256>(), integral_constant<int, 1>());
-    else if (n <= 4096) f(integral_constant<int, 256>(), integral_constant<int, 2>());
-    else if (n <= 8192) f(integral_constant<int, 1024>(), integral_constant<int, 1>());
-    else if (n <= 16384) f(integral_constant<int, 1024>(), integral_constant<int, 2>());
-    else f(integral_constant<int, 1024>(), integral_constant<int, 4>());
+    const int eights = divide_up(n, 8), threads = eights >= NORM_THREADS ? NORM_THREADS : divide_up(eights, 64) * 64;
+    if (eights <= NORM_THREADS) f(threads, std::integral_constant<int, 1>());
+    else if (eights <= 2 * NORM_THREADS) f(threads, std::integral_constant<int, 2>());
+    else f(threads, std::integral_constant<int, 4>());
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -241,8 +244,10 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// The router.  A wavefront per token; a lane holds V neighbouring logits, so among equal ones the lowest lane, and in
-// it the lowest value, is the lowest expert.  k rounds of: largest of the wavefront, who has it first, take it out.
+// The router.  A wavefront per token; a lane holds V neighbouring logits.  k rounds of: largest of the wavefront, who has it
+// first, take it out.  Logits are compared as whole numbers in the floats' order, 0 for what is never chosen (-inf, NaN);
+// 16-bit ones carry their expert in the low half, so that the largest is the lowest expert's of the largest and names it.
+// Bound by instructions, about 20 a round.
 //
 // Grouping is a counting sort, stable by pair: every workgroup counts the experts of its chunk of tokens; then each
 // adds up, per expert, the counts of all chunks and of those before it, and hands out rows to its pairs in order.
@@ -256,51 +261,79 @@ struct RouteArgs {
     int tokens, experts, k, chunk, chunks;      // chunk: tokens of a workgroup
     const void* logits;
     int64_t ld;
+    bool vec;                                   // rows may be read V values at a time
     int32_t* expert;
     float* weight;
     int32_t *offset, *source, *place;
     int32_t* count;                             // [chunks][experts]
 };
 
-template <typename T, int V> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int32_t* count) {
+template <typename T, int V> __device__ __forceinline__ void route_load(const RouteArgs& a, int64_t t, float (&v)[V]) {
+    const int e = (threadIdx.x & 63) * V, have = max(a.experts - e, 0);
+    const T* const row = static_cast<const T*>(a.logits) + t * a.ld + (have ? e : 0);
+    if (a.vec && have >= V) {
+        load_values<V, true>(row, V, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = i < have ? float(row[i]) : -INFINITY;
+    }
+}
+
+template <typename T, int V> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, const float (&logit)[V], int32_t* count) {
+    constexpr bool PACKED = sizeof(T) == 2;
     const int lane = threadIdx.x & 63;
-    const T* row = static_cast<const T*>(a.logits) + t * a.ld;
-    float v[V];
+    uint32_t key[V];
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        const int e = lane * V + i;
-        v[i] = e < a.experts ? float(row[e]) : -INFINITY;
-        if (v[i] != v[i]) nan = true, v[i] = -INFINITY;
+        const float f = logit[i] + 0.f;                 // -0 and 0 are equal
+        const uint32_t bits = __float_as_uint(f), order = bits >> 31 ? ~bits : bits | 0x80000000u;
+        nan |= f != f;
+        key[i] = f > -INFINITY ? (PACKED ? (order & 0xffff0000u) | (0xffffu - uint32_t(lane * V + i)) : order) : 0u;
+        if constexpr (std::is_same<T, f16>::value) {    // 16 bits of its own: those of the float's are not all in the upper half
+            const uint32_t half = __builtin_bit_cast(uint16_t, f16(f)), h = half >> 15 ? ~half & 0xffffu : half | 0x8000u;
+            key[i] = f > -INFINITY ? h << 16 | (0xffffu - uint32_t(lane * V + i)) : 0u;
+        }
     }
     nan = __any(nan);
-    float mine = -INFINITY;         // of lane j: the j-th largest
+    uint32_t mine = 0;              // of lane j: the key of the j-th largest, and its expert
     int which = -1;
     for (int j = 0; j < a.k; j++) {
-        float most = v[0];
+        uint32_t most = key[0];
 #pragma unroll
-        for (int i = 1; i < V; i++) most = fmaxf(most, v[i]);
-        float all = most;
+        for (int i = 1; i < V; i++) most = max(most, key[i]);
+        const uint32_t all = wave_max(most);
+        if (all == 0) break;
+        int e;
+        if (PACKED) {
+            e = int(0xffffu - (all & 0xffffu));
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
-        if (all == -INFINITY) break;
-        const int first = __ffsll((unsigned long long)__ballot(most == all)) - 1;
-        int at = 0;
+            for (int i = 0; i < V; i++) key[i] = key[i] == all ? 0u : key[i];
+        } else {
+            const int first = __ffsll((unsigned long long)__ballot(most == all)) - 1;
+            int at = 0;
 #pragma unroll
-        for (int i = V - 1; i >= 0; i--)
-            if (v[i] == all) at = i;
-        if (lane == first) {
+            for (int i = V - 1; i >= 0; i--) at = key[i] == all ? i : at;
 #pragma unroll
-            for (int i = 0; i < V; i++)
-                if (i == at) v[i] = -INFINITY;
+            for (int i = 0; i < V; i++) key[i] = lane == first && i == at ? 0u : key[i];
+            e = first * V + __builtin_amdgcn_readlane(at, first);
         }
-        at = __shfl(at, first);
-        if (lane == j) mine = all, which = first * V + at;
+        if (lane == j) mine = all, which = e;
     }
-    const float top = __shfl(mine, 0);
-    float w = which >= 0 ? expf(mine - top) : 0.f;
-    w = w / fmaxf(lanes_sum<64>(w), 1.f);       // the largest is exp(0): the sum is 1 at least where there is one
-    if (top == INFINITY || nan) w = NAN;
+    auto value = [](uint32_t all) {
+        if constexpr (std::is_same<T, f16>::value) {
+            const uint32_t h = all >> 16;
+            return float(__builtin_bit_cast(f16, uint16_t(h & 0x8000u ? h & 0x7fffu : ~h)));
+        }
+        const uint32_t order = PACKED ? all & 0xffff0000u : all;
+        // a packed negative number's lower half comes back as ones: cut
+        const uint32_t bits = order >> 31 ? order & 0x7fffffffu : ~order;
+        return __uint_as_float(PACKED ? bits & 0xffff0000u : bits);
+    };
+    const float top = value(uint32_t(__builtin_amdgcn_readlane(int(mine), 0)));
+    float w = which >= 0 ? expf(value(mine) - top) : 0.f;
+    w = w / fmaxf(wave_sum(w), 1.f);            // the largest is exp(0): the sum is 1 at least where there is one
+    if (nan || top == INFINITY) w = NAN;
     if (lane < a.k) {
         a.expert[t * a.k + lane] = which;
         a.weight[t * a.k + lane] = w;
@@ -318,47 +351,57 @@ __device__ __forceinline__ uint64_t same_as(int e, bool in, int bits) {
     return m;
 }
 
-// LDS: [ROUTE_WAVES + 1][experts] words
+// LDS: [ROUTE_WAVES + 2][experts] words
 template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds__(ROUTE_WAVES * 64) void k_route(RouteArgs a) {
     extern __shared__ int32_t lds[];
+    constexpr int THREADS = ROUTE_WAVES * 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
-    int32_t* const total = lds + ROUTE_WAVES * E;
-    const int64_t t0 = int64_t(blockIdx.x) * a.chunk;
-    const int64_t t1 = min(t0 + a.chunk, int64_t(a.tokens));
+    int32_t *const total = lds + ROUTE_WAVES * E, *const before = total + E;     // rows of an expert in all chunks, in earlier ones
+    const int32_t t0 = int32_t(blockIdx.x) * a.chunk, t1 = min(t0 + a.chunk, a.tokens);
+    for (int e = tid; e < 2 * E; e += THREADS) total[e] = 0;
+    __syncthreads();
     if (CHOOSE) {
-        for (int e = tid; e < E; e += ROUTE_WAVES * 64) total[e] = 0;
-        __syncthreads();
-        for (int64_t t = t0 + wave; t < t1; t += ROUTE_WAVES) route_token<T, V>(a, t, total);
+        float v[V], next[V] = {};
+        if (t0 + wave < t1) route_load<T, V>(a, t0 + wave, v);
+        for (int32_t t = t0 + wave; t < t1; t += ROUTE_WAVES) {
+            if (t + ROUTE_WAVES < t1) route_load<T, V>(a, t + ROUTE_WAVES, next);
+            route_token<T, V>(a, t, v, total);
+#pragma unroll
+            for (int i = 0; i < V; i++) v[i] = next[i];
+        }
         __syncthreads();
         if (!GROUP)
-            for (int e = tid; e < E; e += ROUTE_WAVES * 64) a.count[int64_t(blockIdx.x) * E + e] = total[e];
+            for (int e = tid; e < E; e += THREADS) a.count[int64_t(blockIdx.x) * E + e] = total[e];
     }
     if (!GROUP) return;
-    // before[e]: rows of expert e in earlier chunks; total[e]: in all chunks
     __shared__ int32_t sums[ROUTE_WAVES];
-    int32_t before = 0;
     if (!CHOOSE) {
-        for (int e = tid; e < E; e += ROUTE_WAVES * 64) {
-            int32_t sum = 0;
-            for (int c = 0; c < a.chunks; c++) {
+        // several threads per expert, each some of the chunks
+        const int parts = THREADS / E, e = tid % E, part = tid / E;
+        if (part < parts) {
+            int32_t sum = 0, earlier = 0;
+#pragma unroll 8
+            for (int c = part; c < a.chunks; c += parts) {
                 const int32_t x = a.count[int64_t(c) * E + e];
                 sum += x;
-                before += c < int(blockIdx.x) ? x : 0;
+                earlier += c < int(blockIdx.x) ? x : 0;
             }
-            total[e] = sum;
+            atomicAdd(&total[e], sum);              // whole numbers, in LDS
+            atomicAdd(&before[e], earlier);
         }
     }
     // each wavefront's own share of the chunk's pairs, in order
-    const int64_t p0 = t0 * a.k, pairs = (t1 - t0) * a.k;
-    const int64_t share = (pairs + ROUTE_WAVES * 64 - 1) / (ROUTE_WAVES * 64) * 64;
-    const int64_t first = p0 + min(int64_t(wave) * share, pairs), last = p0 + min(int64_t(wave + 1) * share, pairs);
+    const int32_t p0 = t0 * a.k, pairs = max(t1 - t0, 0) * a.k;
+    const int32_t share = (pairs + THREADS - 1) / THREADS * 64;
+    const int32_t first = p0 + min(wave * share, pairs), last = p0 + min((wave + 1) * share, pairs);
     int32_t* const mine = lds + wave * E;
     for (int e = lane; e < E; e += 64) mine[e] = 0;
-    __syncthreads();
-    for (int64_t p = first + lane; p < last; p += 64) {
+    wave_order();
+    for (int32_t p = first + lane; p < last; p += 64) {
         const int e = a.expert[p];
         if (e >= 0) atomicAdd(&mine[e], 1);
     }
+    __syncthreads();
     // exclusive sum of total over the experts: one expert per thread (experts <= threads)
     const int32_t n = tid < E ? total[tid] : 0;
     int32_t upto = n;
@@ -376,7 +419,7 @@ template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds
     }
     if (tid < E) {
         if (blockIdx.x == 0) a.offset[tid + 1] = upto;
-        int32_t at = upto - n + before;
+        int32_t at = upto - n + before[tid];
         for (int w = 0; w < ROUTE_WAVES; w++) {         // where each wavefront's pairs of this expert begin
             const int32_t x = lds[w * E + tid];
             lds[w * E + tid] = at;
@@ -386,26 +429,27 @@ template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds
     if (blockIdx.x == 0 && tid == 0) a.offset[0] = 0;
     __syncthreads();
     const int bits = 32 - __clz(max(E - 1, 1));
-    for (int64_t p = first + lane; p - lane < last; p += 64) {
+    for (int32_t p = first + lane; p - lane < last; p += 64) {
         const int e = p < last ? a.expert[p] : -1;
         const uint64_t same = same_as(e, e >= 0, bits);
         int32_t at = -1;
         if (e >= 0) {
             const int32_t base = mine[e];
             at = base + __popcll(same & ((1ull << lane) - 1));
-            a.source[at] = int32_t(p / a.k);
+            a.source[at] = int32_t(uint32_t(p) / uint32_t(a.k));
             wave_order();
             if (63 - __clzll(same) == lane) mine[e] = at + 1;       // the last of its expert, after every lane's read
         }
         wave_order();
         if (p < last) a.place[p] = at;
     }
-    for (int64_t r = rows + p0 + tid; r < min(rows + p0 + pairs, int64_t(a.tokens) * a.k); r += ROUTE_WAVES * 64) a.source[r] = -1;
+    const int32_t end = min(a.tokens * a.k - rows, p0 + pairs);
+    for (int32_t r = p0 + tid; r < end; r += THREADS) a.source[rows + r] = -1;
 }
 
 int route_chunk(int32_t tokens) { return tokens <= ROUTE_ONE ? max(tokens, 1) : max(divide_up(tokens, ROUTE_CHUNKS), ROUTE_WAVES); }
 bool route_fits(int32_t tokens, int32_t experts, int32_t k) {
-    return experts <= CSR5_ROUTE_MAX_EXPERTS && k >= 1 && k <= experts && k <= CSR5_ROUTE_MAX_K && int64_t(tokens) * k <= INT32_MAX;
+    return experts <= CSR5_ROUTE_MAX_EXPERTS && k >= 1 && k <= experts && k <= CSR5_ROUTE_MAX_K && int64_t(tokens) * k <= INT32_MAX - 65536;    // loops count past the end
 }
 
 // A wavefront per token: the row in LDS, zeros with k entries.
@@ -421,7 +465,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_route_back(int to
     int e = -1;
     if (lane < k) e = expert[t * k + lane], w = weight[t * k + lane], d = dweight[t * k + lane];
     if (uint32_t(e) >= uint32_t(experts)) e = -1, w = 0.f, d = 0.f;
-    const float mean = lanes_sum<64>(w * d);
+    const float mean = wave_sum(w * d);
     if (e >= 0) row[e] = w * (d - mean);
     wave_order();
     for (int i = lane; i < experts; i += 64) dlogits[t * ld + i] = T(row[i]);
@@ -468,7 +512,7 @@ __global__ __launch_bounds__(256) void k_combine_back(int64_t pairs, int k, int 
             store_values<8, VEC>(dz + r * lddz + col, n - col, d);
         }
     }
-    sum = lanes_sum<64>(sum);
+    sum = wave_sum(sum);
     if (lane == 0) dweight[p] = sum;
 }
 
@@ -492,13 +536,14 @@ int csr5_route(int32_t tokens, int32_t experts, int32_t k, int dtype, const void
     if (need && (!workspace || workspace_bytes < need)) return CSR5_ENOMEM;
     if (reinterpret_cast<uintptr_t>(workspace) & 3) return CSR5_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    RouteArgs a{tokens, experts, k, route_chunk(tokens), 0, logits, ld, expert, weight, offset, source, place, static_cast<int32_t*>(workspace)};
+    RouteArgs a{tokens, experts, k, route_chunk(tokens), 0, logits, ld, false, expert, weight, offset, source, place, static_cast<int32_t*>(workspace)};
     a.chunks = max(divide_up(tokens, a.chunk), 1);
-    const size_t lds = size_t(ROUTE_WAVES + 1) * size_t(experts) * 4;
+    const size_t lds = size_t(ROUTE_WAVES + 2) * size_t(experts) * 4;
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         auto go = [&](auto width) {
             constexpr int V = decltype(width)::value;
+            a.vec = aligned(logits, ld, size, V * size);
             if (a.chunks == 1) {
                 k_route<T, V, true, true><<<1, ROUTE_WAVES * 64, lds, s>>>(a);
             } else {
@@ -616,10 +661,10 @@ int csr5_rmsnorm(int32_t rows, int32_t n, int dtype, const void* x, int64_t ldx,
         const size_t wide = 8 * size;
         const bool v = aligned(x, ldx, size, wide) && (!residual || aligned(residual, ldr, size, wide)) && aligned(gain, 0, size, wide) &&
                        (!h || aligned(h, ldh, size, wide)) && (!y || aligned(y, ldy, size, wide)) && (!q || aligned(q, ldq, 1, 8));
-        norm_shape(n, [&](auto tpb, auto nv) {
-            constexpr int TPB = decltype(tpb)::value, NV = decltype(nv)::value;
-            if (v) k_rmsnorm<T, TPB, NV, true><<<rows, TPB, 0, s>>>(a);
-            else k_rmsnorm<T, TPB, NV, false><<<rows, TPB, 0, s>>>(a);
+        norm_shape(n, [&](int threads, auto nv) {
+            constexpr int NV = decltype(nv)::value;
+            if (v) k_rmsnorm<T, NV, true><<<rows, threads, 0, s>>>(a);
+            else k_rmsnorm<T, NV, false><<<rows, threads, 0, s>>>(a);
         });
         return launched();
     });
@@ -652,10 +697,10 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void* h, int
         const bool v = aligned(h, ldh, size, wide) && aligned(dy, lddy, size, wide) && aligned(dh, lddh, size, wide) && aligned(gain, 0, size, wide) &&
                        (!residual_grad || aligned(residual_grad, ldrg, size, wide));
         if (rows > 0)
-            norm_shape(n, [&](auto tpb, auto nv) {
-                constexpr int TPB = decltype(tpb)::value, NV = decltype(nv)::value;
-                if (v) k_rmsnorm_back<T, TPB, NV, true><<<groups, TPB, 0, s>>>(a);
-                else k_rmsnorm_back<T, TPB, NV, false><<<groups, TPB, 0, s>>>(a);
+            norm_shape(n, [&](int threads, auto nv) {
+                constexpr int NV = decltype(nv)::value;
+                if (v) k_rmsnorm_back<T, NV, true><<<groups, threads, 0, s>>>(a);
+                else k_rmsnorm_back<T, NV, false><<<groups, threads, 0, s>>>(a);
             });
         if (dgain) k_columns<<<divide_up(n, 32), 1024, 0, s>>>(rows > 0 ? groups : 0, n, static_cast<const float*>(workspace), dgain);
         return launched();

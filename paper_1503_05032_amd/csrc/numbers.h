@@ -27,6 +27,15 @@ template <int N, bool VEC, typename T> __device__ __forceinline__ void load_valu
     }
 }
 
+// Eight of them as they are.
+template <bool VEC, typename T> __device__ __forceinline__ vec<T, 8> eight_values(const T* p, int have) {
+    if (VEC && have >= 8) return *reinterpret_cast<const vec<T, 8>*>(p);
+    vec<T, 8> v;
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = i < have ? p[i] : T(0.f);
+    return v;
+}
+
 // Rounds to the nearest T, ties to even.
 template <int N, bool VEC, typename T> __device__ __forceinline__ void store_values(T* p, int have, const float (&in)[N]) {
     if (VEC && have >= N) {
@@ -93,6 +102,27 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 #pragma unroll
     for (int d = 1; d < LANES; d *= 2) v = max(v, uint32_t(__shfl_xor(int(v), d)));
     return v;
+}
+
+// Over the whole wavefront, by data-parallel moves: row shifts by 1, 2, 4 and 8, then the last lane of a row of 16 to the
+// next row and of the first half to the second; lane 63 has it all.  (A shuffle through LDS takes some 100 cycles a step.)
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t identity) {
+    return uint32_t(__builtin_amdgcn_update_dpp(int(identity), int(v), CTRL, ROWS, 0xf, false));
+}
+template <typename F> __device__ __forceinline__ uint32_t wave_all(uint32_t v, uint32_t identity, F f) {
+    v = f(v, moved<0x111, 0xf>(v, identity));
+    v = f(v, moved<0x112, 0xf>(v, identity));
+    v = f(v, moved<0x114, 0xf>(v, identity));
+    v = f(v, moved<0x118, 0xf>(v, identity));
+    v = f(v, moved<0x142, 0xa>(v, identity));
+    v = f(v, moved<0x143, 0xc>(v, identity));
+    return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    return wave_all(v, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return __uint_as_float(wave_all(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
 inline bool aligned(const void* p, int64_t ld, size_t element, size_t bytes) {
