@@ -22,12 +22,6 @@ template <typename F> int with_type(int dtype, F f) {
 }
 size_t type_bytes(int dtype) { return dtype == CSR5_DTYPE_F32 ? 4 : dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16 ? 2 : 0; }
 
-// What the lanes of this wavefront wrote to LDS before is what they read after it (their LDS accesses are in order).
-__device__ __forceinline__ void wave_order() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // The sum of v over the workgroup, for everybody, in a fixed order.  `part` holds a word per wavefront and is not used again
 // before the next barrier.
 __device__ __forceinline__ float group_sum(float v, float* part) {
@@ -404,12 +398,7 @@ template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds
     __syncthreads();
     // exclusive sum of total over the experts: one expert per thread (experts <= threads)
     const int32_t n = tid < E ? total[tid] : 0;
-    int32_t upto = n;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int32_t o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-    }
+    int32_t upto = wave_prefix(n);
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     int32_t rows = 0;

@@ -77,21 +77,46 @@ template <int BM> __device__ __forceinline__ Span find_tile(const Product& a, in
         Span s{-1, 0, 0};
         if (g < a.groups) s = group_span(a, g);
         const int32_t tiles = (s.last - s.first + BM - 1) / BM;
-        int32_t upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
+        const int32_t upto = wave_prefix(tiles);
         const uint64_t past = __ballot(before + upto > t);
         if (past) {
             const int l = __ffsll((unsigned long long)past) - 1;
-            const int32_t first = __shfl(s.first, l) + (t - before - __shfl(upto - tiles, l)) * BM;
-            return uniform({g0 + l, first, min(first + BM, __shfl(s.last, l))});
+            const int32_t first = __builtin_amdgcn_readlane(s.first, l) + (t - before - __builtin_amdgcn_readlane(upto - tiles, l)) * BM;
+            return uniform({g0 + l, first, min(first + BM, __builtin_amdgcn_readlane(s.last, l))});
         }
-        before += __shfl(upto, 63);
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return {-1, 0, 0};
+}
+// How many there are; `most`: of dense rows.
+template <int BM> __device__ __forceinline__ int32_t count_tiles(const Product& a, int32_t most) {
+    if (!a.offset) return most;
+    int32_t all = 0;
+    for (int g0 = 0; g0 < a.groups; g0 += 64) {
+        const int g = g0 + int(threadIdx.x & 63);
+        int32_t tiles = 0;
+        if (g < a.groups) {
+            const Span s = group_span(a, g);
+            tiles = (s.last - s.first + BM - 1) / BM;
+        }
+        all += __builtin_amdgcn_readlane(wave_prefix(tiles), 63);
+    }
+    return all;
+}
+// The group with the rank-th most rows (the rank-th, where there are more than 64).
+__device__ __forceinline__ int largest_group(const Product& a, int rank) {
+    if (a.groups > 64) return rank;
+    const int lane = threadIdx.x & 63;
+    int32_t rows = -1, above = 0;
+    if (lane < a.groups) {
+        const Span s = group_span(a, lane);
+        rows = s.last - s.first;
+    }
+    for (int g = 0; g < a.groups; g++) {
+        const int32_t other = __builtin_amdgcn_readlane(rows, g);
+        above += other > rows || (other == rows && g < lane);
+    }
+    return __ffsll((unsigned long long)__ballot(lane < a.groups && above == rank)) - 1;
 }
 
 __device__ __forceinline__ int64_t source_of(const Product& a, int64_t row) {       // -1: a row of zeros
@@ -387,50 +412,81 @@ template <int COLS, int WAVES> struct Turned {                      // 64 rows o
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// What a workgroup with index `b` computes, in an order that suits the caches: workgroups go to the 8 XCDs by turns, so
-// each XCD gets a contiguous part of the order, and in it 8 tiles of rows go with one tile of columns after the other.
-// False: nothing.
-__device__ __forceinline__ bool tile_order(int64_t b, int row_tiles, int col_tiles, int32_t& i, int32_t& j) {
-    const int64_t total = int64_t(row_tiles) * col_tiles, per = (total + 7) / 8, at = (b & 7) * per + (b >> 3);
-    if ((b >> 3) >= per || at >= total) return false;
-    const int32_t strip = int32_t(at / (8 * int64_t(col_tiles))), in = int32_t(at - int64_t(strip) * 8 * col_tiles), high = min(8, row_tiles - strip * 8);
+// The order of the tiles, which suits the caches: 8 tiles of rows go with one tile of columns after the other.
+__device__ __forceinline__ void tile_at(int32_t at, int row_tiles, int col_tiles, int32_t& i, int32_t& j) {
+    const int32_t strip = at / (8 * col_tiles), in = at - strip * 8 * col_tiles, high = min(8, row_tiles - strip * 8);
     i = __builtin_amdgcn_readfirstlane(strip * 8 + in % high), j = __builtin_amdgcn_readfirstlane(in / high);
-    return true;
 }
 
-// The rows, columns and depth of a workgroup's tile.
+// The rows, columns and depth of a workgroup's tile.  Workgroups go to the 8 XCDs by turns, so each XCD gets a contiguous part
+// of the order: of the tiles that there are, which is for the device to say (with a part of the most that there can be, one
+// XCD had mostly tiles that there were not).  DW: of each group's, the groups with most rows first, as a tile takes as long
+// as its group has rows.
 struct Tile {
     Span s;
     int32_t i0, i_end, j0, depth;
 };
 template <int OP, int BI, int BJ> __device__ __forceinline__ bool find(const Product& a, int row_tiles, int col_tiles, Tile& t) {
+    const int32_t xcd = blockIdx.x & 7, m = blockIdx.x >> 3;
     int32_t it, jt;
-    if (!tile_order(blockIdx.x, row_tiles, col_tiles, it, jt)) return false;
-    t.j0 = jt * BJ;
     if (OP == DW) {
-        const int tiles = (a.out_rows + BI - 1) / BI;
-        t.s = uniform(group_span(a, it / tiles));
-        t.i0 = it % tiles * BI, t.i_end = a.out_rows, t.depth = t.s.last - t.s.first;
+        const int32_t total = row_tiles * col_tiles, per = (total + 7) / 8, at = xcd * per + m % per;
+        if (at >= total) return false;
+        t.s.group = largest_group(a, m / per);
+        if (t.s.group < 0 || t.s.group >= a.groups) return false;
+        tile_at(at, row_tiles, col_tiles, it, jt);
+        t.s = uniform(group_span(a, t.s.group));
+        t.i0 = it * BI, t.i_end = a.out_rows, t.depth = t.s.last - t.s.first;
     } else {
+        row_tiles = __builtin_amdgcn_readfirstlane(min(count_tiles<BI>(a, row_tiles), row_tiles));
+        const int32_t total = row_tiles * col_tiles, per = (total + 7) / 8, at = xcd * per + m;
+        if (m >= per || at >= total) return false;
+        tile_at(at, row_tiles, col_tiles, it, jt);
         t.s = find_tile<BI>(a, it);
         t.i0 = t.s.first, t.i_end = t.s.last, t.depth = a.depth;
     }
+    t.j0 = jt * BJ;
     return t.s.group >= 0;
 }
 
-// A wavefront's 16 TI x 16 TJ results from row i0 and column j0 on.
-template <int OP, typename Y, int TI, int TJ> __device__ __forceinline__ void store_tile(const Product& a, const Tile& t, int32_t i0, int32_t j0, int lane, const f32x4 (&acc)[TJ][TI]) {
+// A wavefront's 16 TI x 16 TJ results from row i0 and column j0 on, by way of `room`, its ROOM bytes of LDS: a lane has four
+// columns of a row, a line of memory is 32 lanes' (8-byte stores of 16 rows at a time took 3 us longer a tile).
+template <int OP, typename Y, int ROOM, int TI, int TJ> __device__ __forceinline__ void store_tile(const Product& a, const Tile& t, int32_t i0, int32_t j0, int lane, uint8_t* room, const f32x4 (&acc)[TJ][TI]) {
+    constexpr int SIZE = sizeof(Y), PITCH = TJ * 16 * SIZE + 16, MOST = ROOM / (16 * PITCH), BATCH = MOST < TI ? MOST : TI;    // tiles at a time
+    constexpr int LANES = TJ * 16 * SIZE / 16, EACH = 64 / LANES, VALUES = 16 / SIZE;                       // lanes of a row, rows of a store
+    static_assert(BATCH >= 1 && 64 % LANES == 0, "a row of tiles fits");
     Y* const y = static_cast<Y*>(a.y) + (OP == DW ? t.s.group * a.y_group : 0);
+    bool zero[TI] = {};
+    if (OP == FWD && a.source)
 #pragma unroll
-    for (int i = 0; i < TI; i++) {
-        const int32_t row = i0 + i * 16 + (lane & 15);
-        if (row >= t.i_end) continue;
-        const bool zero = OP == FWD && a.source && source_of(a, row) < 0;
+        for (int i = 0; i < TI; i++) zero[i] = source_of(a, min(i0 + i * 16 + (lane & 15), t.i_end - 1)) < 0;
 #pragma unroll
-        for (int j = 0; j < TJ; j++) {
-            const int32_t col = j0 + j * 16 + (lane >> 4) * 4;
-            store_four<Y, true>(y + int64_t(row) * a.ldy + col, a.cols - col, zero ? f32x4{0, 0, 0, 0} : acc[j][i]);
+    for (int b = 0; b < TI; b += BATCH) {
+#pragma unroll
+        for (int i = b; i < min(b + BATCH, TI); i++)
+#pragma unroll
+            for (int j = 0; j < TJ; j++)
+                store_four<Y, true>(reinterpret_cast<Y*>(room + ((i - b) * 16 + (lane & 15)) * PITCH) + j * 16 + (lane >> 4) * 4, 4, zero[i] ? f32x4{0, 0, 0, 0} : acc[j][i]);
+        wave_order();
+#pragma unroll
+        for (int r = 0; r < min(BATCH, TI - b) * 16; r += EACH) {
+            const int at = r + lane / LANES;
+            const int32_t row = i0 + b * 16 + at, col = j0 + lane % LANES * VALUES;
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(8)));        // y may be aligned to 8 bytes only
+            const u32x4 v = *reinterpret_cast<const u32x4*>(room + at * PITCH + lane % LANES * 16);
+            if (row >= t.i_end || col >= a.cols) continue;
+            Y* const p = y + int64_t(row) * a.ldy + col;
+            if (col + VALUES <= a.cols) {
+                *reinterpret_cast<u32x4*>(p) = v;
+            } else {
+                typedef vec<Y, VALUES> values_type;
+                const values_type values = *reinterpret_cast<const values_type*>(&v);
+#pragma unroll
+                for (int e = 0; e < VALUES; e++)
+                    if (col + e < a.cols) p[e] = values[e];
+            }
         }
+        wave_order();
     }
 }
 
@@ -584,7 +640,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
         for (; c0 < t.depth; c0 += 64) step(std::false_type(), c0);
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
-    store_tile<OP, T, TI, TJ>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
+    store_tile<OP, T, RING * TILE / WAVES>(a, t, t.i0 + wi, t.j0 + wj, lane, lds + wave * (RING * TILE / WAVES), acc);
 }
 
 // 8 bits.  A step is a block of 128 values: one matrix instruction per 16 x 16 results, which starts from 0 (its own sum is
@@ -705,7 +761,8 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int r
             for (int q = 0; q < 4; q++) acc[j][TI - 1][q] = fmaf(part[(TI - 1) & 1][j][q], W1 ? before * ws[W1 ? j : 0][q] : before * one_before, acc[j][TI - 1][q]);
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
-    store_tile<FWD, Y, TI, TJ>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
+    constexpr int ROOM = int(sizeof(lds)) / WAVES / 16 * 16;
+    store_tile<FWD, Y, ROOM>(a, t, t.i0 + wi, t.j0 + wj, lane, lds + wave * ROOM, acc);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -809,8 +866,8 @@ template <typename T, typename Y, int OP> int launch_plain(const Product& a, hip
 
 template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int launch_tiled(const Product& a, hipStream_t s) {
     const int64_t cols = divide_up(a.cols, BJ);
-    const int64_t rows = OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : int64_t(divide_up(a.rows, BI)) + (a.offset ? a.groups : 0);
-    const int64_t grid = (rows * cols + 7) / 8 * 8;
+    const int64_t rows = OP == DW ? int64_t(divide_up(a.out_rows, BI)) : int64_t(divide_up(a.rows, BI)) + (a.offset ? a.groups : 0);
+    const int64_t grid = (rows * cols + 7) / 8 * 8 * (OP == DW ? a.groups : 1);
     if (grid > INT32_MAX) return CSR5_ERANGE;
     if constexpr (is_f8<T>) {
         constexpr int XRING = BI > 128 ? 3 : 2;         // 128 x 128: two workgroups on a CU

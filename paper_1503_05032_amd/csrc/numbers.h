@@ -109,20 +109,32 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t identity) {
     return uint32_t(__builtin_amdgcn_update_dpp(int(identity), int(v), CTRL, ROWS, 0xf, false));
 }
-template <typename F> __device__ __forceinline__ uint32_t wave_all(uint32_t v, uint32_t identity, F f) {
+// With sums, a lane has those up to itself.
+template <typename F> __device__ __forceinline__ uint32_t wave_upto(uint32_t v, uint32_t identity, F f) {
     v = f(v, moved<0x111, 0xf>(v, identity));
     v = f(v, moved<0x112, 0xf>(v, identity));
     v = f(v, moved<0x114, 0xf>(v, identity));
     v = f(v, moved<0x118, 0xf>(v, identity));
     v = f(v, moved<0x142, 0xa>(v, identity));
-    v = f(v, moved<0x143, 0xc>(v, identity));
-    return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+    return f(v, moved<0x143, 0xc>(v, identity));
+}
+template <typename F> __device__ __forceinline__ uint32_t wave_all(uint32_t v, uint32_t identity, F f) {
+    return uint32_t(__builtin_amdgcn_readlane(int(wave_upto(v, identity, f)), 63));
+}
+__device__ __forceinline__ int32_t wave_prefix(int32_t v) {
+    return int32_t(wave_upto(uint32_t(v), 0u, [](uint32_t a, uint32_t b) { return a + b; }));
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return wave_all(v, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float(wave_all(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+
+// What the lanes of this wavefront wrote to LDS before is what they read after it (their LDS accesses are in order).
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 inline bool aligned(const void* p, int64_t ld, size_t element, size_t bytes) {
