@@ -238,10 +238,12 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// The router.  A wavefront per token; a lane holds V neighbouring logits.  k rounds of: largest of the wavefront, who has it
-// first, take it out.  Logits are compared as whole numbers in the floats' order, 0 for what is never chosen (-inf, NaN);
-// 16-bit ones carry their expert in the low half, so that the largest is the lowest expert's of the largest and names it.
-// Bound by instructions, about 20 a round.
+// The router.  A token's logits lie over LANES lanes, V neighbouring ones in each: 16 lanes, four tokens to a wavefront, for
+// up to 256 experts and k up to 16, otherwise all 64.  k rounds of: largest of the token, who has it first, take it out.
+// Logits are compared as whole numbers in the floats' order, 0 for what is never chosen (-inf, NaN); 16-bit ones carry their
+// expert in the low half, so that the largest is the lowest expert's of the largest and names it.  Bound by instructions:
+// 256 experts in 16 bits take about 45 a round, for four tokens (a wavefront per token: 25 for one; 32768 tokens, 8 of 256
+// experts, took 23 us).
 //
 // Grouping is a counting sort, stable by pair: every workgroup counts the experts of its chunk of tokens; then each
 // adds up, per expert, the counts of all chunks and of those before it, and hands out rows to its pairs in order.
@@ -250,6 +252,7 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
 constexpr int ROUTE_CHUNKS = 256;       // at most, each a workgroup
 constexpr int ROUTE_WAVES = 16;
 constexpr int ROUTE_ONE = 64;           // tokens that a single workgroup routes
+constexpr int ROUTE_FEW = 32;           // ... by a wavefront each: 24 tokens of 128 experts take 6.0 us, four to a wavefront 7.3
 
 struct RouteArgs {
     int tokens, experts, k, chunk, chunks;      // chunk: tokens of a workgroup
@@ -260,22 +263,31 @@ struct RouteArgs {
     float* weight;
     int32_t *offset, *source, *place;
     int32_t* count;                             // [chunks][experts]
+    bool fours;                                 // ... whose rows may be read four at a time
 };
 
-template <typename T, int V> __device__ __forceinline__ void route_load(const RouteArgs& a, int64_t t, float (&v)[V]) {
-    const int e = (threadIdx.x & 63) * V, have = max(a.experts - e, 0);
+template <typename T, int V, int LANES> __device__ __forceinline__ void route_load(const RouteArgs& a, int64_t t, float (&v)[V]) {
+    const int e = int(threadIdx.x % LANES) * V, have = max(a.experts - e, 0);
     const T* const row = static_cast<const T*>(a.logits) + t * a.ld + (have ? e : 0);
     if (a.vec && have >= V) {
-        load_values<V, true>(row, V, v);
+        constexpr int N = V * sizeof(T) > 16 ? 16 / sizeof(T) : V;
+#pragma unroll
+        for (int i = 0; i < V; i += N) {
+            float part[N];
+            load_values<N, true>(row + i, N, part);
+#pragma unroll
+            for (int j = 0; j < N; j++) v[i + j] = part[j];
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < V; i++) v[i] = i < have ? float(row[i]) : -INFINITY;
     }
 }
 
-template <typename T, int V> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, const float (&logit)[V], int32_t* count) {
-    constexpr bool PACKED = sizeof(T) == 2;
-    const int lane = threadIdx.x & 63;
+// `there`: this lane's token is one.
+template <typename T, int V, int LANES> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool there, const float (&logit)[V], int32_t* count) {
+    constexpr bool PACKED = sizeof(T) == 2, ROW = LANES == 16;
+    const int lane = threadIdx.x % LANES, row = threadIdx.x & 48;
     uint32_t key[V];
     bool nan = false;
 #pragma unroll
@@ -289,30 +301,33 @@ template <typename T, int V> __device__ __forceinline__ void route_token(const R
             key[i] = f > -INFINITY ? h << 16 | (0xffffu - uint32_t(lane * V + i)) : 0u;
         }
     }
-    nan = __any(nan);
-    uint32_t mine = 0;              // of lane j: the key of the j-th largest, and its expert
+    const uint64_t nans = __ballot(nan);
+    nan = ROW ? (nans >> row) & 0xffff : nans != 0;
+    uint32_t mine = 0, best = 0;    // of lane j: the key of the j-th largest, and its expert; the largest's key
     int which = -1;
     for (int j = 0; j < a.k; j++) {
         uint32_t most = key[0];
 #pragma unroll
         for (int i = 1; i < V; i++) most = max(most, key[i]);
-        const uint32_t all = wave_max(most);
-        if (all == 0) break;
+        const uint32_t all = ROW ? row_max(most) : wave_max(most);
+        if (!__any(all != 0)) break;
         int e;
         if (PACKED) {
             e = int(0xffffu - (all & 0xffffu));
 #pragma unroll
             for (int i = 0; i < V; i++) key[i] = key[i] == all ? 0u : key[i];
         } else {
-            const int first = __ffsll((unsigned long long)__ballot(most == all)) - 1;
+            const uint64_t have = __ballot(most == all);
+            const int first = ROW ? __ffs(uint32_t(have >> row) & 0xffffu) - 1 : __ffsll((unsigned long long)have) - 1;
             int at = 0;
 #pragma unroll
             for (int i = V - 1; i >= 0; i--) at = key[i] == all ? i : at;
 #pragma unroll
             for (int i = 0; i < V; i++) key[i] = lane == first && i == at ? 0u : key[i];
-            e = first * V + __builtin_amdgcn_readlane(at, first);
+            e = first * V + __shfl(at, (ROW ? row : 0) + first);
         }
-        if (lane == j) mine = all, which = e;
+        if (j == 0) best = all;
+        if (lane == j && all != 0) mine = all, which = e;
     }
     auto value = [](uint32_t all) {
         if constexpr (std::is_same<T, f16>::value) {
@@ -324,11 +339,12 @@ template <typename T, int V> __device__ __forceinline__ void route_token(const R
         const uint32_t bits = order >> 31 ? order & 0x7fffffffu : ~order;
         return __uint_as_float(PACKED ? bits & 0xffff0000u : bits);
     };
-    const float top = value(uint32_t(__builtin_amdgcn_readlane(int(mine), 0)));
+    const float top = value(best);
     float w = which >= 0 ? expf(value(mine) - top) : 0.f;
-    w = w / fmaxf(wave_sum(w), 1.f);            // the largest is exp(0): the sum is 1 at least where there is one
+    const float sum = ROW ? row_sum(w) : wave_sum(w);
+    w = w / fmaxf(sum, 1.f);                    // the largest is exp(0): the sum is 1 at least where there is one
     if (nan || top == INFINITY) w = NAN;
-    if (lane < a.k) {
+    if (there && lane < a.k) {
         a.expert[t * a.k + lane] = which;
         a.weight[t * a.k + lane] = w;
         if (which >= 0) atomicAdd(&count[which], 1);        // in LDS; a count does not depend on the order
@@ -346,7 +362,7 @@ __device__ __forceinline__ uint64_t same_as(int e, bool in, int bits) {
 }
 
 // LDS: [ROUTE_WAVES + 2][experts] words
-template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds__(ROUTE_WAVES * 64) void k_route(RouteArgs a) {
+template <typename T, int V, int LANES, bool CHOOSE, bool GROUP> __global__ __launch_bounds__(ROUTE_WAVES * 64) void k_route(RouteArgs a) {
     extern __shared__ int32_t lds[];
     constexpr int THREADS = ROUTE_WAVES * 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
@@ -354,15 +370,19 @@ template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds
     const int32_t t0 = int32_t(blockIdx.x) * a.chunk, t1 = min(t0 + a.chunk, a.tokens);
     for (int e = tid; e < 2 * E; e += THREADS) total[e] = 0;
     __syncthreads();
-    if (CHOOSE) {
+    if (CHOOSE && t0 < t1) {
+        constexpr int STEP = THREADS / LANES;           // tokens of the workgroup at a time
         float v[V], next[V] = {};
-        if (t0 + wave < t1) route_load<T, V>(a, t0 + wave, v);
-        for (int32_t t = t0 + wave; t < t1; t += ROUTE_WAVES) {
-            if (t + ROUTE_WAVES < t1) route_load<T, V>(a, t + ROUTE_WAVES, next);
-            route_token<T, V>(a, t, v, total);
+        const int32_t mine = t0 + tid / LANES;
+        route_load<T, V, LANES>(a, min(mine, a.tokens - 1), v);
+        for (int32_t t = mine; t - tid / LANES < t1; t += STEP) {     // the same number of turns for everybody
+            route_load<T, V, LANES>(a, min(t + STEP, a.tokens - 1), next);
+            route_token<T, V, LANES>(a, t, t < t1, v, total);
 #pragma unroll
             for (int i = 0; i < V; i++) v[i] = next[i];
         }
+    }
+    if (CHOOSE) {
         __syncthreads();
         if (!GROUP)
             for (int e = tid; e < E; e += THREADS) a.count[int64_t(blockIdx.x) * E + e] = total[e];
@@ -370,19 +390,29 @@ template <typename T, int V, bool CHOOSE, bool GROUP> __global__ __launch_bounds
     if (!GROUP) return;
     __shared__ int32_t sums[ROUTE_WAVES];
     if (!CHOOSE) {
-        // several threads per expert, each some of the chunks
-        const int parts = THREADS / E, e = tid % E, part = tid / E;
-        if (part < parts) {
-            int32_t sum = 0, earlier = 0;
+        // several threads per expert (per four), each some of the chunks
+        auto add_up = [&](auto width) {
+            constexpr int N = decltype(width)::value;
+            const int parts = THREADS / (E / N), e = tid % (E / N) * N, part = tid / (E / N);
+            if (part >= parts) return;
+            int32_t sum[N] = {}, earlier[N] = {};
 #pragma unroll 8
             for (int c = part; c < a.chunks; c += parts) {
-                const int32_t x = a.count[int64_t(c) * E + e];
-                sum += x;
-                earlier += c < int(blockIdx.x) ? x : 0;
+                const vec<int32_t, N> x = *reinterpret_cast<const vec<int32_t, N>*>(a.count + int64_t(c) * E + e);
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    const int32_t v = N == 1 ? x[0] : x[i];
+                    sum[i] += v, earlier[i] += c < int(blockIdx.x) ? v : 0;
+                }
             }
-            atomicAdd(&total[e], sum);              // whole numbers, in LDS
-            atomicAdd(&before[e], earlier);
-        }
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                atomicAdd(&total[e + i], sum[i]);              // whole numbers, in LDS
+                atomicAdd(&before[e + i], earlier[i]);
+            }
+        };
+        if (a.fours) add_up(std::integral_constant<int, 4>());
+        else add_up(std::integral_constant<int, 1>());
     }
     // each wavefront's own share of the chunk's pairs, in order
     const int32_t p0 = t0 * a.k, pairs = max(t1 - t0, 0) * a.k;
@@ -525,26 +555,31 @@ int csr5_route(int32_t tokens, int32_t experts, int32_t k, int dtype, const void
     if (need && (!workspace || workspace_bytes < need)) return CSR5_ENOMEM;
     if (reinterpret_cast<uintptr_t>(workspace) & 3) return CSR5_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    RouteArgs a{tokens, experts, k, route_chunk(tokens), 0, logits, ld, false, expert, weight, offset, source, place, static_cast<int32_t*>(workspace)};
+    RouteArgs a{tokens, experts, k, route_chunk(tokens), 0, logits, ld, false, expert, weight, offset, source, place, static_cast<int32_t*>(workspace), experts % 4 == 0 && (reinterpret_cast<uintptr_t>(workspace) & 15) == 0};
     a.chunks = max(divide_up(tokens, a.chunk), 1);
     const size_t lds = size_t(ROUTE_WAVES + 2) * size_t(experts) * 4;
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        auto go = [&](auto width) {
-            constexpr int V = decltype(width)::value;
-            a.vec = aligned(logits, ld, size, V * size);
+        auto go = [&](auto width, auto lanes) {
+            constexpr int V = decltype(width)::value, LANES = decltype(lanes)::value;
+            a.vec = aligned(logits, ld, size, V * size < 16 ? V * size : 16);
             if (a.chunks == 1) {
-                k_route<T, V, true, true><<<1, ROUTE_WAVES * 64, lds, s>>>(a);
+                k_route<T, V, LANES, true, true><<<1, ROUTE_WAVES * 64, lds, s>>>(a);
             } else {
-                k_route<T, V, true, false><<<a.chunks, ROUTE_WAVES * 64, lds, s>>>(a);
-                k_route<T, V, false, true><<<a.chunks, ROUTE_WAVES * 64, lds, s>>>(a);
+                k_route<T, V, LANES, true, false><<<a.chunks, ROUTE_WAVES * 64, lds, s>>>(a);
+                k_route<T, V, LANES, false, true><<<a.chunks, ROUTE_WAVES * 64, lds, s>>>(a);
             }
         };
-        if (experts <= 64) go(std::integral_constant<int, 1>());
-        else if (experts <= 128) go(std::integral_constant<int, 2>());
-        else if (experts <= 256) go(std::integral_constant<int, 4>());
-        else if (experts <= 512) go(std::integral_constant<int, 8>());
-        else go(std::integral_constant<int, 16>());
+        using std::integral_constant;
+        if (k <= 16 && experts <= 256 && tokens > ROUTE_FEW) {
+            if (experts <= 64) go(integral_constant<int, 4>(), integral_constant<int, 16>());
+            else if (experts <= 128) go(integral_constant<int, 8>(), integral_constant<int, 16>());
+            else go(integral_constant<int, 16>(), integral_constant<int, 16>());
+        } else {
+            if (experts <= 64) go(integral_constant<int, 1>(), integral_constant<int, 64>());
+            else if (experts <= 256) go(integral_constant<int, 4>(), integral_constant<int, 64>());
+            else go(integral_constant<int, 16>(), integral_constant<int, 64>());
+        }
         return launched();
     });
 }

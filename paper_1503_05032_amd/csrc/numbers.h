@@ -124,6 +124,19 @@ template <typename F> __device__ __forceinline__ uint32_t wave_all(uint32_t v, u
 __device__ __forceinline__ int32_t wave_prefix(int32_t v) {
     return int32_t(wave_upto(uint32_t(v), 0u, [](uint32_t a, uint32_t b) { return a + b; }));
 }
+// Over each row of 16 lanes, by rotations: every lane has the result.
+template <typename F> __device__ __forceinline__ uint32_t row_all(uint32_t v, F f) {
+    v = f(v, moved<0x128, 0xf>(v, v));
+    v = f(v, moved<0x124, 0xf>(v, v));
+    v = f(v, moved<0x122, 0xf>(v, v));
+    return f(v, moved<0x121, 0xf>(v, v));
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    return row_all(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ float row_sum(float v) {
+    return __uint_as_float(row_all(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return wave_all(v, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
