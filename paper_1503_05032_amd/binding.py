@@ -475,17 +475,20 @@ def _experts(t, dtype, groups, n, k, name):
     return t.data_ptr() or None, ld if n > 1 else max(ld, k), group
 
 
-def _scales(t, dims, name):
-    """Address and strides of float32 scales of exactly this shape, in any layout."""
-    if _TYPE_CODES.get(t.dtype) != CSR5_DTYPE_F32 or not t.is_cuda:
-        raise ValueError(f"{name}: expected a float32 GPU tensor, got {t.dtype}")
-    if t.shape != dims:
-        raise ValueError(f"{name}: expected shape {dims}, got {tuple(t.shape)}")
-    return (t.data_ptr() or None, *t.stride())
+_marshal = None     # csrc/marshal.cpp: takes the tensors of a serving step's calls apart (and makes the same checks)
 
 
-def _f8_blocks(n):
-    return -(-n // CSR5_F8_BLOCK)
+def _native():
+    global _marshal
+    if _marshal is None:
+        load()
+        path = os.path.join(_PKG, "_marshal.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python {os.path.join(_PKG, 'build.py')}` (there is no fallback)")
+        from . import _marshal as module
+        module.set_current_stream(lambda: _stream(None))
+        _marshal = module
+    return _marshal
 
 
 def _space(t):
@@ -501,13 +504,7 @@ def csr5_route(logits, k, expert, weight, offset, source, place, workspace=None,
     """The k experts of each row of `logits` [tokens, experts], their softmax, and the pairs grouped by expert.  Writes
     expert, place (int32) and weight (float32) [tokens * k], source (int32) [tokens * k] and offset (int32)
     [experts + 1]; `workspace` (uint8) has csr5_route_workspace_bytes bytes."""
-    code = _code(logits, "logits")
-    tokens, experts = logits.shape
-    pairs = tokens * k
-    return _chk(load().csr5_route(tokens, experts, k, code, *_matrix(logits, logits.dtype, tokens, experts, "logits"),
-                                  _arr(expert, ["i32"], pairs, "expert"), _arr(weight, ["f32"], pairs, "weight"),
-                                  _arr(offset, ["i32"], experts + 1, "offset"), _arr(source, ["i32"], pairs, "source"),
-                                  _arr(place, ["i32"], pairs, "place"), *_space(workspace), _stream(stream)), "csr5_route", check)
+    return _chk(_native().route(logits, k, expert, weight, offset, source, place, workspace, stream), "csr5_route", check)
 
 
 def csr5_route_backward(expert, weight, dweight, dlogits, stream=None, check=True):
@@ -523,13 +520,7 @@ def csr5_route_backward(expert, weight, dweight, dlogits, stream=None, check=Tru
 
 def csr5_combine(z, place, y, weight=None, residual=None, stream=None, check=True):
     """y[t] = residual[t] + sum_j weight[t, j] * z[place[t, j]]; place and weight [tokens, k], z [rows, n]."""
-    code, dt = _code(z, "z"), z.dtype
-    rows, n = z.shape
-    tokens, k = place.shape
-    res = (None, 0) if residual is None else _matrix(residual, dt, tokens, n, "residual")
-    return _chk(load().csr5_combine(tokens, k, rows, n, code, *_matrix(z, dt, rows, n, "z"), _arr(place, ["i32"], tokens * k, "place"),
-                                    _arr(weight, ["f32"], tokens * k, "weight"), *res, *_matrix(y, dt, tokens, n, "y"), _stream(stream)),
-                "csr5_combine", check)
+    return _chk(_native().combine(z, place, y, weight, residual, stream), "csr5_combine", check)
 
 
 def csr5_combine_backward(dy, z, place, weight, dz, dweight, stream=None, check=True):
@@ -553,14 +544,7 @@ def _source(source, rows, x_rows):
 
 def csr5_grouped_gemm(x, w, offset, y, source=None, stream=None, check=True):
     """y[r] = w[g] x[source[r]] for the rows r of each group g; x [x_rows, k], w [groups, n, k], y [rows, n]."""
-    code, dt = _code(x, "x"), x.dtype
-    x_rows, k = x.shape
-    groups, n = w.shape[0], w.shape[1]
-    rows = y.shape[0]
-    px, ldx = _matrix(x, dt, x_rows, k, "x")
-    return _chk(load().csr5_grouped_gemm(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), px, x_rows, ldx, _source(source, rows, x_rows),
-                                         *_experts(w, dt, groups, n, k, "w"), *_matrix(y, dt, rows, n, "y"), _stream(stream)),
-                "csr5_grouped_gemm", check)
+    return _chk(_native().grouped_gemm(x, w, offset, y, source, stream), "csr5_grouped_gemm", check)
 
 
 def csr5_grouped_gemm_dx(dy, w, offset, dx, stream=None, check=True):
@@ -587,54 +571,24 @@ def csr5_grouped_gemm_dw(dy, x, offset, dw, source=None, stream=None, check=True
 
 def csr5_quantise(x, q, scale, block_rows=1, stream=None, check=True):
     """q [rows, n] in 8 bits and scale [ceil(rows / block_rows), ceil(n / 128)] of x [rows, n]; block_rows 1 or 128."""
-    code = _code(x, "x")
-    rows, n = x.shape
-    return _chk(load().csr5_quantise(rows, n, block_rows, code, *_matrix(x, x.dtype, rows, n, "x"), *_matrix(q, None, rows, n, "q"),
-                                     *_scales(scale, (-(-rows // block_rows), _f8_blocks(n)), "scale"), _stream(stream)), "csr5_quantise", check)
+    return _chk(_native().quantise(x, q, scale, block_rows, stream), "csr5_quantise", check)
 
 
 def csr5_gemm_f8(x, x_scale, w, w_scale, y, w_rows=CSR5_F8_BLOCK, stream=None, check=True):
     """y [m, n] = x [m, k] times w [n, k] transposed, both in 8 bits, with x_scale [m, ceil(k / 128)] and w_scale
     [ceil(n / w_rows), ceil(k / 128)]; w_rows 128 or 1."""
-    code = _code(y, "y")
-    (m, k), n = x.shape, w.shape[0]
-    b = _f8_blocks(k)
-    pw, ldw = _matrix(w, None, n, k, "w")
-    ps, *ws = _scales(w_scale, (-(-n // w_rows), b), "w_scale")
-    return _chk(load().csr5_gemm_f8(m, n, k, code, *_matrix(x, None, m, k, "x"), *_scales(x_scale, (m, b), "x_scale"), pw, ldw, ps, w_rows, *ws,
-                                    *_matrix(y, y.dtype, m, n, "y"), _stream(stream)), "csr5_gemm_f8", check)
+    return _chk(_native().gemm_f8(x, x_scale, w, w_scale, y, w_rows, stream), "csr5_gemm_f8", check)
 
 
 def csr5_grouped_gemm_f8(x, x_scale, w, w_scale, offset, y, w_rows=CSR5_F8_BLOCK, source=None, stream=None, check=True):
     """csr5_grouped_gemm in 8 bits: x_scale [x_rows, ceil(k / 128)], w_scale [groups, ceil(n / w_rows), ceil(k / 128)]."""
-    code = _code(y, "y")
-    x_rows, k = x.shape
-    groups, n = w.shape[0], w.shape[1]
-    rows, b = y.shape[0], _f8_blocks(k)
-    px, ldx = _matrix(x, None, x_rows, k, "x")
-    ps, ws_group, ws_row, ws_block = _scales(w_scale, (groups, -(-n // w_rows), b), "w_scale")
-    return _chk(load().csr5_grouped_gemm_f8(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), px, x_rows, ldx,
-                                            *_scales(x_scale, (x_rows, b), "x_scale"), _source(source, rows, x_rows),
-                                            *_experts(w, None, groups, n, k, "w"), ps, w_rows, ws_row, ws_block, ws_group,
-                                            *_matrix(y, y.dtype, rows, n, "y"), _stream(stream)), "csr5_grouped_gemm_f8", check)
+    return _chk(_native().grouped_gemm_f8(x, x_scale, w, w_scale, offset, y, w_rows, source, stream), "csr5_grouped_gemm_f8", check)
 
 
 def csr5_rmsnorm(x, gain, eps, residual=None, h=None, y=None, q=None, scale=None, rstd=None, stream=None, check=True):
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain by rows of x [rows, n]; writes those of h, y, q with scale
     [rows, ceil(n / 128)], and rstd [rows] that are given.  gain (or None: ones) [n]."""
-    code, dt = _code(x, "x"), x.dtype
-    rows, n = x.shape
-    if gain is not None and (gain.dtype is not dt or gain.shape != (n,) or not gain.is_cuda or not gain.is_contiguous()):
-        raise ValueError(f"gain: expected a contiguous GPU tensor of {n} values of {dt}")
-    if (q is None) != (scale is None):
-        raise ValueError("q and scale: both or neither")
-    none = (None, 0)
-    return _chk(load().csr5_rmsnorm(rows, n, code, *_matrix(x, dt, rows, n, "x"), *(none if residual is None else _matrix(residual, dt, rows, n, "residual")),
-                                    None if gain is None else gain.data_ptr() or None, eps,
-                                    *(none if h is None else _matrix(h, dt, rows, n, "h")), *(none if y is None else _matrix(y, dt, rows, n, "y")),
-                                    *(none if q is None else _matrix(q, None, rows, n, "q")),
-                                    *((None, 0, 0) if q is None else _scales(scale, (rows, _f8_blocks(n)), "scale")),
-                                    _arr(rstd, ["f32"], rows, "rstd"), _stream(stream)), "csr5_rmsnorm", check)
+    return _chk(_native().rmsnorm(x, gain, eps, residual, h, y, q, scale, rstd, stream), "csr5_rmsnorm", check)
 
 
 def csr5_rmsnorm_workspace_bytes(rows, n):

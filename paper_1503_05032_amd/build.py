@@ -1,4 +1,5 @@
-"""Builds libcsr5.so (HIP, gfx950) in-tree with hipcc.  No torch involved."""
+"""Builds libcsr5.so (HIP, gfx950) in-tree with hipcc, no torch involved, and next to it _marshal.so, which takes torch's
+tensors apart for the calls of a serving step."""
 from __future__ import annotations
 
 import os
@@ -12,6 +13,8 @@ SRC = [os.path.join(PKG, "csrc", name) for name in ("csr5.hip", "experts.hip", "
 HEADERS = [os.path.join(PKG, "csrc", name) for name in ("row_share.h", "far_lists.h", "numbers.h")]
 INC = os.path.join(ROOT, "include")
 OUT = os.path.join(PKG, "libcsr5.so")
+MARSHAL_SRC = os.path.join(PKG, "csrc", "marshal.cpp")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
@@ -51,14 +54,33 @@ def build(verbose: bool = True, extra=()) -> str:
         for obj in objects:
             if os.path.exists(obj):
                 os.remove(obj)
+    build_marshal(verbose)
     return OUT
 
 
+def build_marshal(verbose: bool = True) -> str:
+    """_marshal.so, against this interpreter's and torch's headers."""
+    import sysconfig
+
+    import torch
+    t = os.path.dirname(torch.__file__)
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", INC, "-I", os.path.join(t, "include"), "-I", os.path.join(t, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], MARSHAL_SRC, "-o", tmp, "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+           "-L", PKG, "-l:libcsr5.so", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd, stdin=subprocess.DEVNULL)
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 def is_stale() -> bool:
-    if not os.path.exists(OUT):
+    if not os.path.exists(OUT) or not os.path.exists(MARSHAL):
         return True
-    t = os.path.getmtime(OUT)
-    deps = SRC + HEADERS + [os.path.join(INC, "csr5.h")]
+    t = min(os.path.getmtime(OUT), os.path.getmtime(MARSHAL))
+    deps = SRC + HEADERS + [MARSHAL_SRC] + [os.path.join(INC, "csr5.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
