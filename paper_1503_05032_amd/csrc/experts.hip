@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
 constexpr int ROUTE_CHUNKS = 256;       // at most, each a workgroup
 constexpr int ROUTE_WAVES = 16;
 constexpr int ROUTE_ONE = 64;           // tokens that a single workgroup routes
-constexpr int ROUTE_FEW = 32;           // ... by a wavefront each: 24 tokens of 128 experts take 6.0 us, four to a wavefront 7.3
+constexpr int ROUTE_FEW = 16;           // ... by a wavefront each: 8 of 128 take 6.2 us so, four to a wavefront 7.3; 24 would take turns, 9.2 against 7.4
 
 struct RouteArgs {
     int tokens, experts, k, chunk, chunks;      // chunk: tokens of a workgroup
@@ -284,8 +284,8 @@ template <typename T, int V, int LANES> __device__ __forceinline__ void route_lo
     }
 }
 
-// `there`: this lane's token is one.
-template <typename T, int V, int LANES> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool there, const float (&logit)[V], int32_t* count) {
+// `there`: this lane's token is one.  chosen: also has the experts, in LDS, where it is not NULL.
+template <typename T, int V, int LANES> __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, bool there, const float (&logit)[V], int32_t* count, int32_t* chosen) {
     constexpr bool PACKED = sizeof(T) == 2, ROW = LANES == 16;
     const int lane = threadIdx.x % LANES, row = threadIdx.x & 48;
     uint32_t key[V];
@@ -347,6 +347,7 @@ template <typename T, int V, int LANES> __device__ __forceinline__ void route_to
     if (there && lane < a.k) {
         a.expert[t * a.k + lane] = which;
         a.weight[t * a.k + lane] = w;
+        if (chosen) chosen[t * a.k + lane] = which;
         if (which >= 0) atomicAdd(&count[which], 1);        // in LDS; a count does not depend on the order
     }
 }
@@ -361,12 +362,13 @@ __device__ __forceinline__ uint64_t same_as(int e, bool in, int bits) {
     return m;
 }
 
-// LDS: [ROUTE_WAVES + 2][experts] words
+// LDS: [ROUTE_WAVES + 2][experts] words, and one per pair where a single workgroup does it all
 template <typename T, int V, int LANES, bool CHOOSE, bool GROUP> __global__ __launch_bounds__(ROUTE_WAVES * 64) void k_route(RouteArgs a) {
     extern __shared__ int32_t lds[];
     constexpr int THREADS = ROUTE_WAVES * 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.experts;
     int32_t *const total = lds + ROUTE_WAVES * E, *const before = total + E;     // rows of an expert in all chunks, in earlier ones
+    int32_t* const chosen = before + E;                                          // a single workgroup's pairs' experts
     const int32_t t0 = int32_t(blockIdx.x) * a.chunk, t1 = min(t0 + a.chunk, a.tokens);
     for (int e = tid; e < 2 * E; e += THREADS) total[e] = 0;
     __syncthreads();
@@ -377,7 +379,7 @@ template <typename T, int V, int LANES, bool CHOOSE, bool GROUP> __global__ __la
         route_load<T, V, LANES>(a, min(mine, a.tokens - 1), v);
         for (int32_t t = mine; t - tid / LANES < t1; t += STEP) {     // the same number of turns for everybody
             route_load<T, V, LANES>(a, min(t + STEP, a.tokens - 1), next);
-            route_token<T, V, LANES>(a, t, t < t1, v, total);
+            route_token<T, V, LANES>(a, t, t < t1, v, total, GROUP ? chosen : nullptr);
 #pragma unroll
             for (int i = 0; i < V; i++) v[i] = next[i];
         }
@@ -421,8 +423,9 @@ template <typename T, int V, int LANES, bool CHOOSE, bool GROUP> __global__ __la
     int32_t* const mine = lds + wave * E;
     for (int e = lane; e < E; e += 64) mine[e] = 0;
     wave_order();
+    const int32_t* const expert = CHOOSE ? chosen : a.expert;
     for (int32_t p = first + lane; p < last; p += 64) {
-        const int e = a.expert[p];
+        const int e = expert[p];
         if (e >= 0) atomicAdd(&mine[e], 1);
     }
     __syncthreads();
@@ -449,7 +452,7 @@ template <typename T, int V, int LANES, bool CHOOSE, bool GROUP> __global__ __la
     __syncthreads();
     const int bits = 32 - __clz(max(E - 1, 1));
     for (int32_t p = first + lane; p - lane < last; p += 64) {
-        const int e = p < last ? a.expert[p] : -1;
+        const int e = p < last ? expert[p] : -1;
         const uint64_t same = same_as(e, e >= 0, bits);
         int32_t at = -1;
         if (e >= 0) {
@@ -557,7 +560,7 @@ int csr5_route(int32_t tokens, int32_t experts, int32_t k, int dtype, const void
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     RouteArgs a{tokens, experts, k, route_chunk(tokens), 0, logits, ld, false, expert, weight, offset, source, place, static_cast<int32_t*>(workspace), experts % 4 == 0 && (reinterpret_cast<uintptr_t>(workspace) & 15) == 0};
     a.chunks = max(divide_up(tokens, a.chunk), 1);
-    const size_t lds = size_t(ROUTE_WAVES + 2) * size_t(experts) * 4;
+    const size_t lds = (size_t(ROUTE_WAVES + 2) * size_t(experts) + (a.chunks == 1 ? size_t(tokens) * size_t(k) : 0)) * 4;
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         auto go = [&](auto width, auto lanes) {

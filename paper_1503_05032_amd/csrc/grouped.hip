@@ -353,6 +353,7 @@ template <int COLS, int WAVES> struct Turned {                      // 64 rows o
     int64_t pitch;              // bytes of a row in memory
     int32_t next[LOADS][EACH];  // with source: what it says for the next step, the same in every lane
     int32_t from[LOADS];        // ... and for this one, for this lane's row
+    bool all_named;             // ... of which every one is a row
     int c;                      // row of load 0 within a step
     uint32_t col;               // where this lane's chunk begins in a row, in bytes; past its end: at its last chunk
     // values: row 0; first: the tile's first value in it; width: values of a row
@@ -379,19 +380,28 @@ template <int COLS, int WAVES> struct Turned {                      // 64 rows o
     }
     // Before the first of a step's loads, after the wait of landed(): the compiler's own wait for them goes here, where it
     // is for nothing.
-    __device__ __forceinline__ void here(int lane) {
+    // rows: that a source may name
+    __device__ __forceinline__ void here(int lane, int32_t rows) {
+        bool named = true;
 #pragma unroll
         for (int q = 0; q < LOADS; q++) {
             from[q] = next[q][0];
 #pragma unroll
             for (int e = 1; e < EACH; e++) from[q] = lane / LANES == e ? next[q][e] : from[q];
             asm volatile("" : "+v"(from[q]));
+            named = named && uint32_t(from[q]) < uint32_t(rows);
         }
+        all_named = __all(named);
     }
-    // what by_source() asked for a step ago; rows: that a source may name
-    __device__ __forceinline__ void load_by_source(int q, uint8_t* lds, int wave, int left, int32_t rows) {
-        const bool there = c + q * WAVES * EACH < left && uint32_t(from[q]) < uint32_t(rows);
-        to_lds(there ? base + from[q] * pitch + col : reinterpret_cast<const uint8_t*>(&ZEROS), lds + (q * WAVES + wave) * 1024);
+    // what by_source() asked for a step ago
+    template <bool FAST> __device__ __forceinline__ void load_by_source(int q, uint8_t* lds, int wave, int left, int32_t rows) {
+        uint8_t* const to = lds + (q * WAVES + wave) * 1024;
+        if (FAST && all_named) {
+            to_lds(base, uint32_t(from[q]) * uint32_t(pitch) + col, to);
+        } else {
+            const bool there = c + q * WAVES * EACH < left && uint32_t(from[q]) < uint32_t(rows);
+            to_lds(there ? base + from[q] * pitch + col : reinterpret_cast<const uint8_t*>(&ZEROS), to);
+        }
     }
     // As Straight's, for 16 columns from `first` on; slots and rows are multiples of 256 bytes, so the e-th segment's place is
     // another pattern in bits 5 to 7.
@@ -549,7 +559,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
         constexpr bool FAST = decltype(fast)::value;
         if constexpr (OP == DW) {
             if (by_source) {
-                tw.load_by_source(q, tile, wave, t.depth - c0, a.source_rows);
+                tw.template load_by_source<FAST>(q, tile, wave, t.depth - c0, a.source_rows);
                 if (q == LOADS - 1) tw.by_source(a.source + t.s.first + c0 + 64, t.depth - c0 - 64, wave);
                 return;
             }
@@ -609,7 +619,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
                     load_x(std::false_type(), q, place[s], s / 2 * 64);
                 } else {
                     if constexpr (OP == DW) {
-                        if (by_source && q == 0) tw.here(lane);
+                        if (by_source && q == 0) tw.here(lane, a.source_rows);
                     }
                     load_w(std::false_type(), q, place[s], s / 2 * 64);
                 }
@@ -627,7 +637,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
             half(std::false_type(), fast, even, odd, x_now, w_now, 1, nullptr, nullptr, 0);
             landed<LOADS>();                    // all but the loads of w_after
             if constexpr (OP == DW) {
-                if (by_source) tw.here(lane);
+                if (by_source) tw.here(lane, a.source_rows);
             }
             // x of the step after the next goes to w_now, w of the one after that to x_now
             half(std::true_type(), fast, odd, even, x_next, w_next, 0, w_now, x_now, c0 + 128);
@@ -771,35 +781,39 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int r
 // matrix instructions (a load takes 64 contiguous bytes of 16 rows), and add up their sums in LDS in a fixed order.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int FEW_WAVES = 8;
-constexpr int FEW1 = 16, FEW2 = 32;
+// 8 bits: 32 columns to a workgroup where that still makes 256 of them (8 x 8192 x 4096 10.2 us against 11.2 with 16; 8 x 4096 x
+// 14336 25 against 16).  16 bits: always (64 rows over 64 groups of 1536 x 2048 46 against 49).
+constexpr int FEW_WIDE = 32 * 256;
 
-template <typename T, typename Y, int TI, bool W1> __global__ __launch_bounds__(FEW_WAVES * 64) void k_product_few(Product a, int col_tiles) {
-    constexpr int SIZE = sizeof(T), STEP = 128 / SIZE, AHEAD = 4;
-    constexpr bool F8 = is_f8<T>;
-    __shared__ __align__(16) f32x4 sums[FEW_WAVES][TI][64];
+template <typename T, typename Y, int TI, int TJ, bool W1> __global__ __launch_bounds__(FEW_WAVES * 64) void k_product_few(Product a, int col_tiles) {
+    constexpr bool F8 = is_f8<T>, WIDE = F8 && TJ == 2;
+    constexpr int SIZE = sizeof(T), STEP = 128 / SIZE, AHEAD = WIDE ? 4 : 2, WS = W1 ? 4 : 1;
+    __shared__ __align__(16) f32x4 sums[FEW_WAVES][TJ][TI][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, q = lane >> 4;
     const Span s = find_tile<16 * TI>(a, int32_t(blockIdx.x / col_tiles));
     if (s.group < 0) return;
-    const int32_t j0 = int32_t(blockIdx.x % col_tiles) * 16;
-    const uint8_t* const w = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.w) + s.group * a.w_group + int64_t(min(j0 + li, a.cols - 1)) * a.ldw);
-    const uint8_t* x[TI];
-    const float *xs[TI], *ws[4];
+    const int32_t j0 = int32_t(blockIdx.x % col_tiles) * (16 * TJ);
+    const uint8_t *w[TJ], *x[TI];
+    const float *xs[TI], *ws[TJ][WS];
+#pragma unroll
+    for (int j = 0; j < TJ; j++) {
+        w[j] = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.w) + s.group * a.w_group + int64_t(min(j0 + j * 16 + li, a.cols - 1)) * a.ldw);
+        if (F8)
+#pragma unroll
+            for (int c = 0; c < WS; c++) ws[j][c] = a.ws + s.group * a.ws_group + min(j0 + j * 16 + (W1 ? q * 4 + c : 0), a.cols - 1) / a.w_rows * a.ws_row;
+    }
 #pragma unroll
     for (int i = 0; i < TI; i++) {
         const int64_t r = max(source_of(a, min(s.first + i * 16 + li, s.last - 1)), int64_t(0));
         x[i] = reinterpret_cast<const uint8_t*>(static_cast<const T*>(a.x) + r * a.ldx);
         if (F8) xs[i] = a.xs + r * a.xs_row;
     }
-    if (F8) {
-#pragma unroll
-        for (int c = 0; c < (W1 ? 4 : 1); c++) ws[c] = a.ws + s.group * a.ws_group + (W1 ? min(j0 + q * 4 + c, a.cols - 1) : j0 / CSR5_F8_BLOCK) * a.ws_row;
-    }
     const int64_t bytes = int64_t(a.depth) * SIZE;
     const int steps = (a.depth + STEP - 1) / STEP;
-    f32x4 acc[TI] = {};
+    f32x4 acc[TJ][TI] = {};
     for (int at = wave; at < steps; at += FEW_WAVES * AHEAD) {
-        uint4 wv[AHEAD][2], xv[AHEAD][TI][2];
-        float xf[AHEAD][TI], wf[AHEAD][4];
+        uint4 wv[AHEAD][TJ][2], xv[AHEAD][TI][2];
+        float xf[AHEAD][TI], wf[AHEAD][TJ][WS];
 #pragma unroll
         for (int u = 0; u < AHEAD; u++) {
             const int b = at + u * FEW_WAVES;
@@ -807,46 +821,56 @@ template <typename T, typename Y, int TI, bool W1> __global__ __launch_bounds__(
             for (int k = 0; k < 2; k++) {
                 const int64_t o = int64_t(b) * 128 + k * 64 + q * 16;
                 const bool in = o < bytes;
-                wv[u][k] = *reinterpret_cast<const uint4*>(in ? w + o : reinterpret_cast<const uint8_t*>(&ZEROS));
+#pragma unroll
+                for (int j = 0; j < TJ; j++) wv[u][j][k] = *reinterpret_cast<const uint4*>(in ? w[j] + o : reinterpret_cast<const uint8_t*>(&ZEROS));
 #pragma unroll
                 for (int i = 0; i < TI; i++) xv[u][i][k] = *reinterpret_cast<const uint4*>(in ? x[i] + o : reinterpret_cast<const uint8_t*>(&ZEROS));
             }
             if (F8) {
                 const int64_t block = min(b, steps - 1);
 #pragma unroll
-                for (int i = 0; i < TI; i++) xf[u][i] = xs[i][block * a.xs_block];
+                for (int i = 0; i < TI; i++) xf[u][i] = b < steps ? xs[i][block * a.xs_block] : 0.f;
 #pragma unroll
-                for (int c = 0; c < (W1 ? 4 : 1); c++) wf[u][c] = ws[c][block * a.ws_block];
+                for (int j = 0; j < TJ; j++)
+#pragma unroll
+                    for (int c = 0; c < WS; c++) wf[u][j][c] = b < steps ? ws[j][c][block * a.ws_block] : 0.f;
             }
         }
+        if (!WIDE) __builtin_amdgcn_sched_barrier(0);       // all loads before the first product: the compiler would keep fewer in flight
 #pragma unroll
         for (int u = 0; u < AHEAD; u++)
 #pragma unroll
-            for (int i = 0; i < TI; i++) {
-                if constexpr (F8) {
-                    const uint4 wl = wv[u][0], wh = wv[u][1], xl = xv[u][i][0], xh = xv[u][i][1];
-                    const i32x8 w8 = {int(wl.x), int(wl.y), int(wl.z), int(wl.w), int(wh.x), int(wh.y), int(wh.z), int(wh.w)};
-                    const i32x8 x8 = {int(xl.x), int(xl.y), int(xl.z), int(xl.w), int(xh.x), int(xh.y), int(xh.z), int(xh.w)};
-                    const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-                    if (at + u * FEW_WAVES < steps) {           // past the depth: a NaN scale of the last block counts once
+            for (int j = 0; j < TJ; j++)
 #pragma unroll
-                        for (int c = 0; c < 4; c++) acc[i][c] = fmaf(part[c], xf[u][i] * wf[u][W1 ? c : 0], acc[i][c]);
+                for (int i = 0; i < TI; i++) {
+                    if constexpr (F8) {
+                        const uint4 wl = wv[u][j][0], wh = wv[u][j][1], xl = xv[u][i][0], xh = xv[u][i][1];
+                        const i32x8 w8 = {int(wl.x), int(wl.y), int(wl.z), int(wl.w), int(wh.x), int(wh.y), int(wh.z), int(wh.w)};
+                        const i32x8 x8 = {int(xl.x), int(xl.y), int(xl.z), int(xl.w), int(xh.x), int(xh.y), int(xh.z), int(xh.w)};
+                        const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+                        // Past the depth products and scales are 0.  No branch around the sum: where one skipped what reads a
+                        // matrix instruction's result, the compiler wrote its registers again too early for the instruction,
+                        // whose write came after (one in some thousand results was wrong).
+#pragma unroll
+                        for (int c = 0; c < 4; c++) acc[j][i][c] = fmaf(part[c], xf[u][i] * wf[u][j][W1 ? c : 0], acc[j][i][c]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 2; k++) acc[j][i] = multiply(wv[u][j][k], xv[u][i][k], acc[j][i], T());
                     }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 2; k++) acc[i] = multiply(wv[u][k], xv[u][i][k], acc[i], T());
                 }
-            }
     }
 #pragma unroll
-    for (int i = 0; i < TI; i++) sums[wave][i][lane] = acc[i];
+    for (int j = 0; j < TJ; j++)
+#pragma unroll
+        for (int i = 0; i < TI; i++) sums[wave][j][i][lane] = acc[j][i];
     __syncthreads();
     // a thread per four columns of a row
-    for (int e = tid; e < TI * 64; e += FEW_WAVES * 64) {
-        f32x4 sum = sums[0][e / 64][e % 64];
+    for (int e = tid; e < TJ * TI * 64; e += FEW_WAVES * 64) {
+        const int l = e % 64, i = e / 64 % TI, j = e / 64 / TI;
+        f32x4 sum = sums[0][j][i][l];
 #pragma unroll
-        for (int v = 1; v < FEW_WAVES; v++) sum += sums[v][e / 64][e % 64];
-        const int32_t row = s.first + e / 64 * 16 + (e & 15), col = j0 + (e % 64 >> 4) * 4;
+        for (int v = 1; v < FEW_WAVES; v++) sum += sums[v][j][i][l];
+        const int32_t row = s.first + i * 16 + (l & 15), col = j0 + j * 16 + (l >> 4) * 4;
         if (row >= s.last || col >= a.cols) continue;
         if (a.source && source_of(a, row) < 0) sum = f32x4{0, 0, 0, 0};
         store_four<Y, true>(static_cast<Y*>(a.y) + int64_t(row) * a.ldy + col, a.cols - col, sum);
@@ -879,19 +903,23 @@ template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int la
     return launched();
 }
 
-template <typename T, typename Y, int TI> int launch_few(const Product& a, hipStream_t s) {
-    const int64_t cols = divide_up(a.cols, 16), rows = int64_t(divide_up(a.rows, 16 * TI)) + (a.offset ? a.groups : 0);
+template <typename T, typename Y, int TI, int TJ> int launch_few(const Product& a, hipStream_t s) {
+    const int64_t cols = divide_up(a.cols, 16 * TJ), rows = int64_t(divide_up(a.rows, 16 * TI)) + (a.offset ? a.groups : 0);
     if (rows * cols > INT32_MAX) return CSR5_ERANGE;
-    if (is_f8<T> && a.w_rows == 1) k_product_few<T, Y, TI, is_f8<T>><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
-    else k_product_few<T, Y, TI, false><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
+    if (is_f8<T> && a.w_rows == 1) k_product_few<T, Y, TI, TJ, is_f8<T>><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
+    else k_product_few<T, Y, TI, TJ, false><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
     return launched();
+}
+template <typename T, typename Y, int TI> int launch_few(const Product& a, hipStream_t s) {
+    if (!is_f8<T> || int64_t(a.cols) * divide_up(a.rows, 16 * TI) >= FEW_WIDE) return launch_few<T, Y, TI, 2>(a, s);
+    return launch_few<T, Y, TI, 1>(a, s);
 }
 
 // Offsets that do not fit 32 bits.
 constexpr int64_t MOST_BYTES = int64_t(1) << 32;
-bool far(const Product& a, int64_t size) {
+bool far(const Product& a, int64_t named_pitch) {
     auto past = [](int64_t rows, int64_t pitch) { return pitch < 0 || rows * pitch >= MOST_BYTES; };
-    return (a.source && past(a.source_rows, a.ldx * size)) || past(a.source_rows, a.xs_row * 4) || past(a.cols, a.ws_row * 4);
+    return (a.source && past(a.source_rows, named_pitch)) || past(a.source_rows, a.xs_row * 4) || past(a.cols, a.ws_row * 4);
 }
 
 // Rows of whole 16-byte chunks, at 16-byte addresses, a tile of which offsets of 32 bits reach; results at addresses of four
@@ -900,19 +928,33 @@ template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
     constexpr int SIZE = sizeof(T);
     auto whole = [](int64_t n) { return n * SIZE % 16 == 0; };
     return aligned(a.x, a.ldx, SIZE, 16) && aligned(a.w, a.ldw, SIZE, 16) && whole(a.w_group) && aligned(a.y, a.ldy, sizeof(Y), 4 * sizeof(Y)) &&
-           a.y_group % 4 == 0 && a.ldx * SIZE < MOST_BYTES / 256 && a.ldw * SIZE < MOST_BYTES / 256 && (!a.source || int64_t(a.source_rows) * a.ldx * SIZE < 16 * MOST_BYTES) &&
+           a.y_group % 4 == 0 && a.ldx * SIZE < MOST_BYTES / 256 && a.ldw * SIZE < MOST_BYTES / 256 && (OP != FWD || !a.source || int64_t(a.source_rows) * a.ldx * SIZE < 16 * MOST_BYTES) &&
            (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
 }
 
+// Which kernel.  Measured at k = 2048 and 4096, n = 1536 to 8192 (us in 16 bits, in 8):
+//   few rows    groups of up to 12 rows on average (8 bits: 4): 64 groups of 1536 x 2048 with 10 rows each 86 against 97 in
+//               128 x 128 tiles, with 16 rows 112 against 103; 8 bits with 6 rows 57 against 53; and where there are so few
+//               tiles that a step of their depth takes as long whatever they are: 128 rows of n = 2048 10 against 17 (10
+//               against 18), 64 of n = 8192 36 against 36 (24 against 32), 128 of n = 8192 64 against 35 (45 against 36)
+//   large tiles 256 rows and more where there are enough to go round the CUs: 4096 x 4096 x 2048 55 against 67, 2048 x 4096 x
+//               4096 78 against 61
+constexpr int FEW_ROWS16 = 12, FEW_ROWS8 = 4, FEW_AREA16 = 12288, FEW_AREA8 = 24576;
+constexpr int LARGE_TILES = 192;
+
 template <typename T, typename Y, int OP> int launch(Product a, hipStream_t s) {
+    constexpr bool F8 = is_f8<T>;
     if (!chunks_fit<T, Y, OP>(a)) return launch_plain<T, Y, OP>(a, s);
-    a.far = far(a, sizeof(T));
+    a.far = far(a, (OP == DW ? a.ldw : a.ldx) * int64_t(sizeof(T)));
     const int64_t height = OP == DW ? a.out_rows : a.rows / a.groups;
     if constexpr (OP == FWD) {
-        if (height <= FEW1) return launch_few<T, Y, 1>(a, s);
-        if (height <= FEW2) return launch_few<T, Y, 2>(a, s);
+        const int64_t tiles = divide_up(a.rows, 32) + (a.offset ? a.groups - 1 : 0);
+        if (height <= (F8 ? FEW_ROWS8 : FEW_ROWS16) || tiles * a.cols <= (F8 ? FEW_AREA8 : FEW_AREA16))
+            return height <= 16 ? launch_few<T, Y, 1>(a, s) : launch_few<T, Y, 2>(a, s);
     }
-    if (height >= 192) return launch_tiled<T, Y, OP, is_f8<T> ? 192 : 256, 256, 2, 4>(a, s);
+    constexpr int BI = F8 ? 192 : 256;
+    const int64_t large = (OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : a.rows / BI + (a.offset ? a.groups / 2 : 0)) * divide_up(a.cols, 256);
+    if (height >= 192 && large >= LARGE_TILES) return launch_tiled<T, Y, OP, BI, 256, 2, 4>(a, s);
     return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
 }
 
