@@ -216,3 +216,126 @@ def test_products_of_depth_zero_are_zero():
     e = lambda *s: torch.empty(*s, device=DEV)  # noqa: E731
     B.csr5_gemm_f8(x.to(torch.float8_e4m3fn), e(5, 0), w[0].to(torch.float8_e4m3fn), e(1, 0), y)
     assert (y == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------------------------- large tiles
+TALL = [700, 0, 1301]
+
+
+@pytest.mark.parametrize("dtype", HALF, ids=ids)
+@pytest.mark.parametrize("n,k", [(5640, 264), (5632, 40), (264, 5640), (2056, 2056)])
+def test_grouped_in_large_tiles(dtype, n, k):
+    """Enough rows and columns for the large tiles: of y with many columns, of dx with a large depth's, of dw."""
+    g = torch.Generator().manual_seed(n)
+    rows, groups = sum(TALL), len(TALL)
+    offset, w, x = offsets(TALL), experts(g, groups, n, k, dtype, "wide", k ** -0.5), matrix(g, rows, k, dtype, "wide")
+    source = source_for(g, rows, rows)
+    dy = matrix(g, rows, n, dtype, "wide")
+    big_y, y = room(rows, n, dtype, "wide")
+    big_x, dx = room(rows, k, dtype, "wide")
+    big_w, dw = room(groups * n, k, dtype, "wide")
+    B.csr5_grouped_gemm(x, w, offset, y, source=source.to(DEV))
+    B.csr5_grouped_gemm_dx(dy, w, offset, dx)
+    B.csr5_grouped_gemm_dw(dy, x, offset, dw.unflatten(0, (groups, n)), source=source.to(DEV))
+    for big, r, c in ((big_y, rows, n), (big_x, rows, k), (big_w, groups * n, k)):
+        untouched(big, r, c, "wide")
+    xc, wc, dyc = taken(x, source, rows), w.double().cpu(), dy.double().cpu()
+    for i, a, b in spans(TALL):
+        close(y[a:b], xc[a:b] @ wc[i].T, dtype, (k + 8) * EPS32 * (xc[a:b].abs() @ wc[i].T.abs()), "y")
+        close(dx[a:b], dyc[a:b] @ wc[i], dtype, (n + 8) * EPS32 * (dyc[a:b].abs() @ wc[i].abs()), "dx")
+        close(dw[i * n:(i + 1) * n], dyc[a:b].T @ xc[a:b], dtype, (b - a + 8) * EPS32 * (dyc[a:b].T.abs() @ xc[a:b].abs()), "dw")
+
+
+@pytest.mark.parametrize("w_rows", [128, 1])
+@pytest.mark.parametrize("n,k", [(5640, 272), (5632, 1040)])
+def test_f8_in_large_tiles(w_rows, n, k):
+    g = torch.Generator().manual_seed(n + k)
+    rows, groups = sum(TALL), len(TALL)
+    x, xs, xc = f8_operand(g, rows, k, 1, "wide")
+    operands = [f8_operand(g, n, k, w_rows, "plain") for _ in range(groups)]
+    w, ws = torch.stack([o[0] for o in operands]), torch.stack([o[1] for o in operands])
+    source = source_for(g, rows, rows)
+    for s in (None, source):
+        big, y = room(rows, n, torch.bfloat16, "wide")
+        B.csr5_grouped_gemm_f8(x, xs, w, ws, offsets(TALL), y, w_rows=w_rows, source=None if s is None else s.to(DEV))
+        untouched(big, rows, n, "wide")
+        seen = taken(xc, s, rows)
+        for i, a, b in spans(TALL):
+            close(y[a:b], seen[a:b] @ operands[i][2].T, torch.bfloat16, (k + 8) * EPS32 * (seen[a:b].abs() @ operands[i][2].T.abs()))
+
+
+@pytest.mark.parametrize("n", [64, 5632])
+def test_rows_past_32_bits(n):
+    """A source may name rows whose bytes from the beginning of x do not fit 32 bits."""
+    g = torch.Generator().manual_seed(n)
+    x_rows, k, rows, sizes = 70_000, 256, 2000, [1200, 800]
+    source = torch.randint(0, x_rows, (rows,), generator=g, dtype=torch.int32)
+    source[:5] = torch.tensor([x_rows - 1, 0, 65_535, 65_536, 65_537])
+    names = source.long().to(DEV)
+    offset = offsets(sizes)
+    some = torch.cat([torch.arange(0, 40), torch.arange(1190, 1230), torch.arange(1990, 2000)])
+    wide = torch.zeros(x_rows, 65_536, dtype=torch.uint8, device=DEV)          # rows 64 KiB apart: 4.6e9 bytes
+    values = (torch.randn(rows, k, generator=g)).to(torch.bfloat16)
+    x = wide.view(torch.bfloat16)[:, :k]
+    x[names] = values.to(DEV)
+    xc = x[names].double().cpu()
+    w = experts(g, 2, n, k, torch.bfloat16, "plain")
+    y, dw = torch.empty(rows, n, dtype=torch.bfloat16, device=DEV), torch.empty_like(w)
+    B.csr5_grouped_gemm(x, w, offset, y, source=source.to(DEV))
+    B.csr5_grouped_gemm_dw(y, x, offset, dw, source=source.to(DEV))
+    wc = w.double().cpu()
+    for i, a, b in spans(sizes):
+        at = some[(some >= a) & (some < b)]
+        close(y[at.to(DEV)], xc[at] @ wc[i].T, torch.bfloat16, (k + 8) * EPS32 * (xc[at].abs() @ wc[i].T.abs()), "y")
+        yc = y[a:b, :64].double().cpu()
+        close(dw[i, :64], yc.T @ xc[a:b], torch.bfloat16, (b - a + 8) * EPS32 * (yc.T.abs() @ xc[a:b].abs()), "dw")
+    q, scale = quantised(torch.randn(rows, k, generator=g), 1)
+    x8, xs = wide[:, :k], torch.zeros(x_rows, 2, device=DEV)
+    x8[names], xs[names] = q.view(torch.uint8).to(DEV), scale.to(DEV)
+    xc = meaning(x8[names].cpu().view(torch.float8_e4m3fn), xs[names].cpu(), 1)
+    w8, ws, w8c = f8_operand(g, n, k, 128, "plain")
+    B.csr5_grouped_gemm_f8(x8, xs, torch.stack([w8, w8]), torch.stack([ws, ws]), offset, y, source=source.to(DEV))
+    close(y[some.to(DEV)], xc[some] @ w8c.T, torch.bfloat16, (k + 8) * EPS32 * (xc[some].abs() @ w8c.T.abs()), "f8")
+
+
+def test_products_on_another_stream_and_in_a_graph():
+    """The calls go to the given stream, and captured ones give the same on every replay."""
+    g = torch.Generator().manual_seed(8)
+    sizes, n, k = [5, 0, 300, 40], 256, 384
+    rows = sum(sizes)
+    x, w, offset = matrix(g, rows, k, torch.bfloat16), experts(g, 4, n, k, torch.bfloat16, "plain"), offsets(sizes)
+    y, dx, dw = torch.empty(rows, n, dtype=torch.bfloat16, device=DEV), torch.empty_like(x), torch.empty_like(w)
+    q, scale = torch.empty(rows, k, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(rows, 3, device=DEV)
+    w8, ws, _ = f8_operand(g, n, k, 128, "plain")
+    y8 = torch.empty_like(y)
+
+    def work():
+        B.csr5_grouped_gemm(x, w, offset, y)
+        B.csr5_grouped_gemm_dx(y, w, offset, dx)
+        B.csr5_grouped_gemm_dw(y, x, offset, dw)
+        B.csr5_quantise(x, q, scale)
+        B.csr5_gemm_f8(q, scale, w8, ws, y8)
+
+    outs = (y, dx, dw, q.view(torch.uint8), scale, y8)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        work()
+    s.synchronize()
+    first = [t.clone() for t in outs]
+    work()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, outs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for turn in range(3):
+        x.copy_(torch.randn(rows, k, generator=g))
+        work()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs)), turn
