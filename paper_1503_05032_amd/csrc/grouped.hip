@@ -923,13 +923,13 @@ bool far(const Product& a, int64_t named_pitch) {
 }
 
 // Rows of whole 16-byte chunks, at 16-byte addresses, a tile of which offsets of 32 bits reach; results at addresses of four
-// values.
+// values; and a row of x to read in place of those that a source does not name.
 template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
     constexpr int SIZE = sizeof(T);
     auto whole = [](int64_t n) { return n * SIZE % 16 == 0; };
     return aligned(a.x, a.ldx, SIZE, 16) && aligned(a.w, a.ldw, SIZE, 16) && whole(a.w_group) && aligned(a.y, a.ldy, sizeof(Y), 4 * sizeof(Y)) &&
            a.y_group % 4 == 0 && a.ldx * SIZE < MOST_BYTES / 256 && a.ldw * SIZE < MOST_BYTES / 256 && (OP != FWD || !a.source || int64_t(a.source_rows) * a.ldx * SIZE < 16 * MOST_BYTES) &&
-           (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
+           (OP != FWD || a.source_rows > 0) && (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
 }
 
 // Which kernel.  Measured at k = 2048 and 4096, n = 1536 to 8192 (us in 16 bits, in 8):
@@ -1027,7 +1027,7 @@ int csr5_grouped_gemm_f8(int32_t groups, int32_t rows, int32_t n, int32_t k, int
     if (w_rows != 1 && w_rows != CSR5_F8_BLOCK) return CSR5_EINVAL;
     if (!rows_ok(x, x_rows, ldx, k, 1) || !rows_ok(w, int64_t(groups) * n, ldw, k, 1) || !rows_ok(y, rows, ldy, n, size)) return CSR5_EINVAL;
     if (groups == 0 || rows == 0 || n == 0) return CSR5_OK;
-    if (k > 0 && (!x_scale || !w_scale || ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale)) & 3))) return CSR5_EINVAL;
+    if (k > 0 && ((x_rows > 0 && !x_scale) || !w_scale || ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale)) & 3))) return CSR5_EINVAL;
     Product a{};
     a.x = x, a.ldx = ldx, a.w = w, a.ldw = ldw, a.w_group = w_group, a.y = y, a.ldy = ldy;
     a.offset = offset, a.source = source, a.source_rows = x_rows, a.groups = groups, a.rows = rows, a.cols = n, a.depth = k;

@@ -339,3 +339,21 @@ def test_products_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, outs)), turn
+
+
+@pytest.mark.parametrize("sizes", [[3, 2], [700, 600]])
+def test_sources_of_no_rows(sizes):
+    """x has no rows, so no source names one: zeros, and nothing of x or its scales is read."""
+    rows, n, k = sum(sizes), 8192, 256
+    source = torch.full((rows,), -1, dtype=torch.int32, device=DEV)
+    w = torch.ones(2, n, k, dtype=torch.bfloat16, device=DEV)
+    y = torch.ones(rows, n, dtype=torch.bfloat16, device=DEV)
+    B.csr5_grouped_gemm(w[0, :0], w, offsets(sizes), y, source=source)
+    assert not y.any()
+    y.fill_(1)
+    w8, ws = w.to(torch.float8_e4m3fn), torch.ones(2, n // 128, 2, device=DEV)
+    B.csr5_grouped_gemm_f8(w8[0, :0], ws[0, :0], w8, ws, offsets(sizes), y, source=source)
+    assert not y.any()
+    dw = torch.ones_like(w)
+    B.csr5_grouped_gemm_dw(y, w[0, :0], offsets(sizes), dw, source=source)
+    assert not dw.any()
