@@ -459,44 +459,45 @@ template <int OP, int BI, int BJ> __device__ __forceinline__ bool find(const Pro
     return t.s.group >= 0;
 }
 
-// A wavefront's 16 TI x 16 TJ results from row i0 and column j0 on, by way of `room`, its ROOM bytes of LDS: a lane has four
-// columns of a row, a line of memory is 32 lanes' (8-byte stores of 16 rows at a time took 3 us longer a tile).
-template <int OP, typename Y, int ROOM, int TI, int TJ> __device__ __forceinline__ void store_tile(const Product& a, const Tile& t, int32_t i0, int32_t j0, int lane, uint8_t* room, const f32x4 (&acc)[TJ][TI]) {
-    constexpr int SIZE = sizeof(Y), PITCH = TJ * 16 * SIZE + 16, MOST = ROOM / (16 * PITCH), BATCH = MOST < TI ? MOST : TI;    // tiles at a time
-    constexpr int LANES = TJ * 16 * SIZE / 16, EACH = 64 / LANES, VALUES = 16 / SIZE;                       // lanes of a row, rows of a store
-    static_assert(BATCH >= 1 && 64 % LANES == 0, "a row of tiles fits");
+// A wavefront's 16 TI x 16 TJ results from row i0 and column j0 on.  A lane has four columns of a row; in 16 bits, lanes of
+// neighbouring columns exchange halves, so that a store is 16 bytes of a lane and 64 contiguous ones of a row (8192 x 4096 x
+// 64, two rounds of tiles: 38.7 us with 8-byte stores, 21.8 so).
+template <int OP, typename Y, int TI, int TJ> __device__ __forceinline__ void store_tile(const Product& a, const Tile& t, int32_t i0, int32_t j0, int lane, const f32x4 (&acc)[TJ][TI]) {
+    constexpr int SIZE = sizeof(Y), VALUES = 16 / SIZE, TILES = 4 / SIZE;       // of a store: values, tiles of columns
+    static_assert(TJ % TILES == 0, "tiles of columns in pairs");
     Y* const y = static_cast<Y*>(a.y) + (OP == DW ? t.s.group * a.y_group : 0);
-    bool zero[TI] = {};
-    if (OP == FWD && a.source)
+    const int q = lane >> 4;
+    j0 += SIZE == 2 ? (q & 1) * 16 + (q >> 1) * 8 : q * 4;
 #pragma unroll
-        for (int i = 0; i < TI; i++) zero[i] = source_of(a, min(i0 + i * 16 + (lane & 15), t.i_end - 1)) < 0;
+    for (int i = 0; i < TI; i++) {
+        const int32_t row = i0 + i * 16 + (lane & 15);
+        const bool zero = OP == FWD && a.source && source_of(a, min(row, t.i_end - 1)) < 0;
 #pragma unroll
-    for (int b = 0; b < TI; b += BATCH) {
-#pragma unroll
-        for (int i = b; i < min(b + BATCH, TI); i++)
-#pragma unroll
-            for (int j = 0; j < TJ; j++)
-                store_four<Y, true>(reinterpret_cast<Y*>(room + ((i - b) * 16 + (lane & 15)) * PITCH) + j * 16 + (lane >> 4) * 4, 4, zero[i] ? f32x4{0, 0, 0, 0} : acc[j][i]);
-        wave_order();
-#pragma unroll
-        for (int r = 0; r < min(BATCH, TI - b) * 16; r += EACH) {
-            const int at = r + lane / LANES;
-            const int32_t row = i0 + b * 16 + at, col = j0 + lane % LANES * VALUES;
+        for (int j = 0; j < TJ; j += TILES) {
             typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(8)));        // y may be aligned to 8 bytes only
-            const u32x4 v = *reinterpret_cast<const u32x4*>(room + at * PITCH + lane % LANES * 16);
+            u32x4 v;
+            if constexpr (SIZE == 2) {
+                auto pack = [](f32x4 f) { return __builtin_bit_cast(uint2, vec<Y, 4>{Y(f[0]), Y(f[1]), Y(f[2]), Y(f[3])}); };
+                const uint2 l = pack(acc[j][i]), r = pack(acc[j + 1][i]);
+                // l's odd rows of 16 lanes change places with r's even ones
+                const auto x = __builtin_amdgcn_permlane16_swap(l.x, r.x, false, false), y = __builtin_amdgcn_permlane16_swap(l.y, r.y, false, false);
+                v = u32x4{x[0], y[0], x[1], y[1]};
+            } else {
+                v = __builtin_bit_cast(u32x4, acc[j][i]);
+            }
+            if (zero) v = u32x4{0, 0, 0, 0};
+            const int32_t col = j0 + j * 16;
             if (row >= t.i_end || col >= a.cols) continue;
             Y* const p = y + int64_t(row) * a.ldy + col;
             if (col + VALUES <= a.cols) {
                 *reinterpret_cast<u32x4*>(p) = v;
             } else {
-                typedef vec<Y, VALUES> values_type;
-                const values_type values = *reinterpret_cast<const values_type*>(&v);
+                const vec<Y, VALUES> values = __builtin_bit_cast(vec<Y, VALUES>, v);
 #pragma unroll
                 for (int e = 0; e < VALUES; e++)
                     if (col + e < a.cols) p[e] = values[e];
             }
         }
-        wave_order();
     }
 }
 
@@ -650,7 +651,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
         for (; c0 < t.depth; c0 += 64) step(std::false_type(), c0);
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
-    store_tile<OP, T, RING * TILE / WAVES>(a, t, t.i0 + wi, t.j0 + wj, lane, lds + wave * (RING * TILE / WAVES), acc);
+    store_tile<OP, T>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
 }
 
 // 8 bits.  A step is a block of 128 values: one matrix instruction per 16 x 16 results, which starts from 0 (its own sum is
@@ -771,8 +772,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int r
             for (int q = 0; q < 4; q++) acc[j][TI - 1][q] = fmaf(part[(TI - 1) & 1][j][q], W1 ? before * ws[W1 ? j : 0][q] : before * one_before, acc[j][TI - 1][q]);
         landed<0>();            // nothing is on its way to this LDS when it becomes another workgroup's
     }
-    constexpr int ROOM = int(sizeof(lds)) / WAVES / 16 * 16;
-    store_tile<FWD, Y, ROOM>(a, t, t.i0 + wi, t.j0 + wj, lane, lds + wave * ROOM, acc);
+    store_tile<FWD, Y>(a, t, t.i0 + wi, t.j0 + wj, lane, acc);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -911,8 +911,9 @@ template <typename T, typename Y, int TI, int TJ> int launch_few(const Product& 
     return launched();
 }
 template <typename T, typename Y, int TI> int launch_few(const Product& a, hipStream_t s) {
-    if (!is_f8<T> || int64_t(a.cols) * divide_up(a.rows, 16 * TI) >= FEW_WIDE) return launch_few<T, Y, TI, 2>(a, s);
-    return launch_few<T, Y, TI, 1>(a, s);
+    if constexpr (is_f8<T>)
+        if (int64_t(a.cols) * divide_up(a.rows, 16 * TI) < FEW_WIDE) return launch_few<T, Y, TI, 1>(a, s);
+    return launch_few<T, Y, TI, 2>(a, s);
 }
 
 // Offsets that do not fit 32 bits.
