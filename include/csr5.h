@@ -423,7 +423,8 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
  * Whatever offset, source and place hold, no kernel leaves the arrays: offsets are
  * clamped to [0, rows], a group that ends before it begins is empty, a source
  * outside [0, x_rows) is a row of zeros and a place outside [0, rows) is no row.
- * A size of 0 is fine: such a call writes what is left to write (or nothing).
+ * A size of 0 is fine: such a call writes what is left to write (or nothing).  One of
+ * 2^31 - 2^16 or more is CSR5_ERANGE where a kernel counts in 32 bits.
  * ========================================================================== */
 #define CSR5_DTYPE_BF16 2
 #define CSR5_DTYPE_F16 3
@@ -439,7 +440,7 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
  *   weight[t][j] = exp(l_j - l_0) / sum_i exp(l_i - l_0).
  * An expert whose logit is -inf (masked) or NaN is never chosen.  Where fewer than k
  * remain the rest of the k get expert -1, weight 0 and place -1; a token with a NaN
- * has NaN weights.  The pairs (t, j), j < k, that have an expert are then grouped:
+ * or +inf has NaN weights.  The pairs (t, j), j < k, that have an expert are then grouped:
  * rows [offset[e], offset[e+1]) belong to expert e, by token and j within it.
  *   logits   dtype (BF16, F16, F32) [tokens][experts], row stride ld
  *   expert   int32[tokens*k]      weight  float[tokens*k]
@@ -521,7 +522,9 @@ int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const 
 /*
  * Product in 8 bits: y[i][j] = sum over blocks b of 128 of
  *   x_scale(i, b) * w_scale(j / w_rows, b) * sum_{c in b} x[i][c] w[j][c],
- * each block's sum in 32 bits before it is scaled.  x[m][k], w[n][k]; w_rows is 128
+ * each block's sum before it is scaled, the blocks' sums in 32 bits.  (With 16-byte rows
+ * a block is one matrix instruction for 8 bits, which drops what is below 2^-15 or so of
+ * a block's largest product; otherwise it is summed in 32 bits.)  x[m][k], w[n][k]; w_rows is 128
  * (scales of csr5_quantise with block_rows 128: weights) or 1 (both operands are
  * quantised by rows, as the gradient of a weight needs it).  x_scale(i, b) is at
  * x_scale[i*xs_row + b*xs_block], w_scale at w_scale[(j/w_rows)*ws_row + b*ws_block].

@@ -43,7 +43,7 @@ __device__ __forceinline__ float group_sum(float v, float* part) {
 constexpr int NORM_THREADS = 1024;
 
 template <typename T> struct NormArgs {
-    int n;
+    int rows, n;
     const T *x, *residual, *gain;
     int64_t ldx, ldr;
     float eps;
@@ -58,7 +58,8 @@ template <typename T> struct NormArgs {
 
 template <typename T, int NV, bool VEC> __global__ __launch_bounds__(NORM_THREADS) void k_rmsnorm(NormArgs<T> a) {
     __shared__ float part[NORM_THREADS / 64];
-    const int64_t row = blockIdx.x;
+    const int64_t row = workgroup();
+    if (row >= a.rows) return;
     float v[NV][8];
     float sum = 0.f;
 #pragma unroll
@@ -203,11 +204,13 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
     int64_t row0;
     int b;
     if (ROWS == 1) {
-        const int64_t at = int64_t(blockIdx.x) * 16 + line;
+        const int64_t at = workgroup() * 16 + line;
         row0 = at / blocks, b = int(at % blocks);
         if (row0 >= rows) return;
     } else {
-        row0 = int64_t(blockIdx.x / blocks) * ROWS + line, b = int(blockIdx.x % blocks);
+        row0 = workgroup() / blocks * ROWS, b = int(workgroup() % blocks);
+        if (row0 >= rows) return;
+        row0 += line;
     }
     const int col = b * CSR5_F8_BLOCK + lane * 8;
     float v[PASSES][8];
@@ -471,7 +474,7 @@ template <typename T, int V, int LANES, bool CHOOSE, bool GROUP> __global__ __la
 
 int route_chunk(int32_t tokens) { return tokens <= ROUTE_ONE ? max(tokens, 1) : max(divide_up(tokens, ROUTE_CHUNKS), ROUTE_WAVES); }
 bool route_fits(int32_t tokens, int32_t experts, int32_t k) {
-    return experts <= CSR5_ROUTE_MAX_EXPERTS && k >= 1 && k <= experts && k <= CSR5_ROUTE_MAX_K && int64_t(tokens) * k <= INT32_MAX - 65536;    // loops count past the end
+    return experts <= CSR5_ROUTE_MAX_EXPERTS && k >= 1 && k <= experts && k <= CSR5_ROUTE_MAX_K && int64_t(tokens) * k <= MOST_SIZE;
 }
 
 // A wavefront per token: the row in LDS, zeros with k entries.
@@ -479,7 +482,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_route_back(int to
     __shared__ float rows[4][CSR5_ROUTE_MAX_EXPERTS];
     const int lane = threadIdx.x & 63;
     float* const row = rows[threadIdx.x >> 6];
-    const int64_t t = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t t = workgroup() * 4 + (threadIdx.x >> 6);
     if (t >= tokens) return;                            // no barrier below: a wavefront's LDS accesses are in order
     for (int e = lane; e < experts; e += 64) row[e] = 0.f;
     wave_order();
@@ -497,10 +500,10 @@ template <typename T> __global__ __launch_bounds__(256) void k_route_back(int to
 // Back to the tokens.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_combine(int k, int rows, int n, const T* z, int64_t ldz, const int32_t* place, const float* weight, const T* residual, int64_t ldr, T* y, int64_t ldy) {
-    const int64_t t = blockIdx.x;
-    const int col = (int(blockIdx.y) * 256 + int(threadIdx.x)) * 8;
-    if (col >= n) return;
+__global__ __launch_bounds__(256) void k_combine(int tokens, int k, int rows, int n, const T* z, int64_t ldz, const int32_t* place, const float* weight, const T* residual, int64_t ldr, T* y, int64_t ldy) {
+    const int64_t t = workgroup();
+    const int col = (int(blockIdx.z) * 256 + int(threadIdx.x)) * 8;
+    if (t >= tokens || col >= n) return;
     float sum[8] = {};
     if (residual) load_values<8, VEC>(residual + t * ldr + col, n - col, sum);
     for (int j = 0; j < k; j++) {
@@ -519,7 +522,7 @@ __global__ __launch_bounds__(256) void k_combine(int k, int rows, int n, const T
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_combine_back(int64_t pairs, int k, int rows, int n, const T* dy, int64_t lddy, const T* z, int64_t ldz, const int32_t* place, const float* weight, T* dz, int64_t lddz, float* dweight) {
     const int lane = threadIdx.x & 63;
-    const int64_t p = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t p = workgroup() * 4 + (threadIdx.x >> 6);
     if (p >= pairs) return;
     const int32_t r = place[p];
     float sum = 0.f;
@@ -597,7 +600,7 @@ int csr5_route_backward(int32_t tokens, int32_t experts, int32_t k, int dtype, c
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        k_route_back<T><<<divide_up(tokens, 4), 256, 0, s>>>(tokens, experts, k, expert, weight, dweight, static_cast<T*>(dlogits), ld);
+        k_route_back<T><<<workgroups(divide_up(tokens, 4)), 256, 0, s>>>(tokens, experts, k, expert, weight, dweight, static_cast<T*>(dlogits), ld);
         return launched();
     });
 }
@@ -606,16 +609,17 @@ int csr5_combine(int32_t tokens, int32_t k, int32_t rows, int32_t n, int dtype, 
                  const float* weight, const void* residual, int64_t ldr, void* y, int64_t ldy, void* hip_stream) {
     const size_t size = type_bytes(dtype);
     if (!size || tokens < 0 || k < 0 || rows < 0 || n < 0) return CSR5_EINVAL;
-    if (int64_t(tokens) * k > INT32_MAX) return CSR5_ERANGE;
+    if (int64_t(tokens) * k > INT32_MAX || n > MOST_SIZE) return CSR5_ERANGE;
     if (!rows_ok(z, rows, ldz, n, size) || !rows_ok(y, tokens, ldy, n, size) || (residual && !rows_ok(residual, tokens, ldr, n, size))) return CSR5_EINVAL;
     if (tokens == 0 || n == 0) return CSR5_OK;
     if (k > 0 && !place) return CSR5_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const dim3 grid(tokens, divide_up(n, 2048));
+        dim3 grid = workgroups(tokens);
+        grid.z = divide_up(n, 2048);
         auto go = [&](auto v) {
-            k_combine<T, decltype(v)::value><<<grid, 256, 0, s>>>(k, rows, n, static_cast<const T*>(z), ldz, place, weight, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy);
+            k_combine<T, decltype(v)::value><<<grid, 256, 0, s>>>(tokens, k, rows, n, static_cast<const T*>(z), ldz, place, weight, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy);
         };
         if (aligned(z, ldz, size, 8 * size) && aligned(y, ldy, size, 8 * size) && (!residual || aligned(residual, ldr, size, 8 * size))) go(std::true_type());
         else go(std::false_type());
@@ -627,7 +631,7 @@ int csr5_combine_backward(int32_t tokens, int32_t k, int32_t rows, int32_t n, in
                           int64_t ldz, const int32_t* place, const float* weight, void* dz, int64_t lddz, float* dweight, void* hip_stream) {
     const size_t size = type_bytes(dtype);
     if (!size || tokens < 0 || k < 0 || rows < 0 || n < 0) return CSR5_EINVAL;
-    if (int64_t(tokens) * k > INT32_MAX) return CSR5_ERANGE;
+    if (int64_t(tokens) * k > INT32_MAX || n > MOST_SIZE) return CSR5_ERANGE;
     if (!rows_ok(z, rows, ldz, n, size) || !rows_ok(dy, tokens, lddy, n, size) || !rows_ok(dz, rows, lddz, n, size)) return CSR5_EINVAL;
     const int64_t pairs = int64_t(tokens) * k;
     if (pairs == 0) return CSR5_OK;
@@ -636,7 +640,7 @@ int csr5_combine_backward(int32_t tokens, int32_t k, int32_t rows, int32_t n, in
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         auto go = [&](auto v) {
-            k_combine_back<T, decltype(v)::value><<<divide_up(pairs, 4), 256, 0, s>>>(pairs, k, rows, n, static_cast<const T*>(dy), lddy, static_cast<const T*>(z), ldz, place, weight, static_cast<T*>(dz), lddz, dweight);
+            k_combine_back<T, decltype(v)::value><<<workgroups(divide_up(pairs, 4)), 256, 0, s>>>(pairs, k, rows, n, static_cast<const T*>(dy), lddy, static_cast<const T*>(z), ldz, place, weight, static_cast<T*>(dz), lddz, dweight);
         };
         if (aligned(z, ldz, size, 8 * size) && aligned(dy, lddy, size, 8 * size) && aligned(dz, lddz, size, 8 * size)) go(std::true_type());
         else go(std::false_type());
@@ -648,17 +652,17 @@ int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const 
                   int64_t scale_row, int64_t scale_block, void* hip_stream) {
     const size_t size = type_bytes(dtype);
     if (!size || rows < 0 || n < 0 || (block_rows != 1 && block_rows != CSR5_F8_BLOCK)) return CSR5_EINVAL;
+    if (rows > MOST_SIZE || n > MOST_SIZE) return CSR5_ERANGE;
     if (!rows_ok(x, rows, ldx, n, size) || !rows_ok(q, rows, ldq, n, 1)) return CSR5_EINVAL;
     if (rows == 0 || n == 0) return CSR5_OK;
     if (!scale || (reinterpret_cast<uintptr_t>(scale) & 3)) return CSR5_EINVAL;
     const int64_t blocks = divide_up(n, CSR5_F8_BLOCK);
     const int64_t groups = block_rows == 1 ? (int64_t(rows) * blocks + 15) / 16 : divide_up(rows, CSR5_F8_BLOCK) * blocks;
-    if (groups > INT32_MAX) return CSR5_ERANGE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         auto go = [&](auto r, auto v) {
-            k_quantise<T, decltype(r)::value, decltype(v)::value><<<uint32_t(groups), 256, 0, s>>>(rows, n, static_cast<const T*>(x), ldx, q, ldq, scale, scale_row, scale_block);
+            k_quantise<T, decltype(r)::value, decltype(v)::value><<<workgroups(groups), 256, 0, s>>>(rows, n, static_cast<const T*>(x), ldx, q, ldq, scale, scale_row, scale_block);
         };
         auto by = [&](auto v) {
             if (block_rows == 1) go(std::integral_constant<int, 1>(), v);
@@ -683,15 +687,15 @@ int csr5_rmsnorm(int32_t rows, int32_t n, int dtype, const void* x, int64_t ldx,
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const NormArgs<T> a{n, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<const T*>(gain), ldx, ldr, eps,
+        const NormArgs<T> a{rows, n, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<const T*>(gain), ldx, ldr, eps,
                             static_cast<T*>(h), static_cast<T*>(y), ldh, ldy, q, ldq, scale, scale_row, scale_block, rstd};
         const size_t wide = 8 * size;
         const bool v = aligned(x, ldx, size, wide) && (!residual || aligned(residual, ldr, size, wide)) && aligned(gain, 0, size, wide) &&
                        (!h || aligned(h, ldh, size, wide)) && (!y || aligned(y, ldy, size, wide)) && (!q || aligned(q, ldq, 1, 8));
         norm_shape(n, [&](int threads, auto nv) {
             constexpr int NV = decltype(nv)::value;
-            if (v) k_rmsnorm<T, NV, true><<<rows, threads, 0, s>>>(a);
-            else k_rmsnorm<T, NV, false><<<rows, threads, 0, s>>>(a);
+            if (v) k_rmsnorm<T, NV, true><<<workgroups(rows), threads, 0, s>>>(a);
+            else k_rmsnorm<T, NV, false><<<workgroups(rows), threads, 0, s>>>(a);
         });
         return launched();
     });

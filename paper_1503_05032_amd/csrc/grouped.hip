@@ -977,6 +977,7 @@ int launch_f8(int dtype, const Product& a, void* hip_stream) {
 bool groups_ok(int32_t groups, int32_t rows, int32_t n, int32_t k, const int32_t* offset) {
     return groups >= 0 && rows >= 0 && n >= 0 && k >= 0 && (groups == 0 || offset) && !(reinterpret_cast<uintptr_t>(offset) & 3);
 }
+bool sizes_fit(int32_t groups, int32_t rows, int32_t n, int32_t k) { return max(max(groups, rows), max(n, k)) <= MOST_SIZE; }
 // what `source` may name is there
 bool source_ok(int32_t rows, int32_t x_rows, const int32_t* source) {
     return x_rows >= 0 && (source || x_rows >= rows) && !(reinterpret_cast<uintptr_t>(source) & 3);
@@ -989,6 +990,7 @@ extern "C" {
 int csr5_grouped_gemm(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const void* x, int32_t x_rows,
                       int64_t ldx, const int32_t* source, const void* w, int64_t ldw, int64_t w_group, void* y, int64_t ldy, void* hip_stream) {
     if (!half_type(dtype) || !groups_ok(groups, rows, n, k, offset) || !source_ok(rows, x_rows, source)) return CSR5_EINVAL;
+    if (!sizes_fit(groups, rows, n, k)) return CSR5_ERANGE;
     if (!rows_ok(x, x_rows, ldx, k, 2) || !rows_ok(w, int64_t(groups) * n, ldw, k, 2) || !rows_ok(y, rows, ldy, n, 2)) return CSR5_EINVAL;
     if (groups == 0 || rows == 0 || n == 0) return CSR5_OK;
     Product a{};
@@ -1000,6 +1002,7 @@ int csr5_grouped_gemm(int32_t groups, int32_t rows, int32_t n, int32_t k, int dt
 int csr5_grouped_gemm_dx(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const void* dy, int64_t lddy,
                          const void* w, int64_t ldw, int64_t w_group, void* dx, int64_t lddx, void* hip_stream) {
     if (!half_type(dtype) || !groups_ok(groups, rows, n, k, offset)) return CSR5_EINVAL;
+    if (!sizes_fit(groups, rows, n, k)) return CSR5_ERANGE;
     if (!rows_ok(dy, rows, lddy, n, 2) || !rows_ok(w, int64_t(groups) * n, ldw, k, 2) || !rows_ok(dx, rows, lddx, k, 2)) return CSR5_EINVAL;
     if (groups == 0 || rows == 0 || k == 0) return CSR5_OK;
     Product a{};
@@ -1011,6 +1014,7 @@ int csr5_grouped_gemm_dx(int32_t groups, int32_t rows, int32_t n, int32_t k, int
 int csr5_grouped_gemm_dw(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t* offset, const void* dy, int64_t lddy,
                          const void* x, int32_t x_rows, int64_t ldx, const int32_t* source, void* dw, int64_t lddw, int64_t dw_group, void* hip_stream) {
     if (!half_type(dtype) || !groups_ok(groups, rows, n, k, offset) || !source_ok(rows, x_rows, source)) return CSR5_EINVAL;
+    if (!sizes_fit(groups, rows, n, k)) return CSR5_ERANGE;
     if (!rows_ok(dy, rows, lddy, n, 2) || !rows_ok(x, x_rows, ldx, k, 2) || !rows_ok(dw, int64_t(groups) * n, lddw, k, 2)) return CSR5_EINVAL;
     if (groups == 0 || n == 0 || k == 0) return CSR5_OK;
     Product a{};
@@ -1025,6 +1029,7 @@ int csr5_grouped_gemm_f8(int32_t groups, int32_t rows, int32_t n, int32_t k, int
                          int64_t ldy, void* hip_stream) {
     const size_t size = half_type(dtype) ? 2 : 4;
     if (!(half_type(dtype) || dtype == CSR5_DTYPE_F32) || !groups_ok(groups, rows, n, k, offset) || !source_ok(rows, x_rows, source)) return CSR5_EINVAL;
+    if (!sizes_fit(groups, rows, n, k)) return CSR5_ERANGE;
     if (w_rows != 1 && w_rows != CSR5_F8_BLOCK) return CSR5_EINVAL;
     if (!rows_ok(x, x_rows, ldx, k, 1) || !rows_ok(w, int64_t(groups) * n, ldw, k, 1) || !rows_ok(y, rows, ldy, n, size)) return CSR5_EINVAL;
     if (groups == 0 || rows == 0 || n == 0) return CSR5_OK;
@@ -1042,6 +1047,7 @@ int csr5_gemm_f8(int32_t m, int32_t n, int32_t k, int dtype, const uint8_t* x, i
                  void* hip_stream) {
     const size_t size = half_type(dtype) ? 2 : 4;
     if (!(half_type(dtype) || dtype == CSR5_DTYPE_F32) || m < 0 || n < 0 || k < 0 || (w_rows != 1 && w_rows != CSR5_F8_BLOCK)) return CSR5_EINVAL;
+    if (!sizes_fit(1, m, n, k)) return CSR5_ERANGE;
     if (!rows_ok(x, m, ldx, k, 1) || !rows_ok(w, n, ldw, k, 1) || !rows_ok(y, m, ldy, n, size)) return CSR5_EINVAL;
     if (m == 0 || n == 0) return CSR5_OK;
     if (k > 0 && (!x_scale || !w_scale || ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale)) & 3))) return CSR5_EINVAL;

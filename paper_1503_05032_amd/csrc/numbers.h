@@ -160,6 +160,16 @@ inline bool rows_ok(const void* p, int64_t rows, int64_t ld, int64_t columns, si
 }
 inline int divide_up(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
+// The largest size that every loop may count past.
+constexpr int32_t MOST_SIZE = INT32_MAX - 65536;
+
+// n workgroups in two dimensions, as one holds 2^32 threads at most; the last ones may have nothing to do.
+inline dim3 workgroups(int64_t n) {
+    constexpr int64_t ROW = 1 << 20;
+    return dim3(uint32_t(n < ROW ? n : ROW), uint32_t((n + ROW - 1) / ROW));
+}
+__device__ __forceinline__ int64_t workgroup() { return int64_t(blockIdx.y) * gridDim.x + blockIdx.x; }
+
 inline int launched() { return hipGetLastError() == hipSuccess ? CSR5_OK : CSR5_EHIP; }
 
 }  // namespace

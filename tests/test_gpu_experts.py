@@ -398,3 +398,44 @@ def test_other_stream_and_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (*got.values(), y, dh, dgain))), turn
 
+
+
+# ---------------------------------------------------------------------------------------------------------------- very many rows
+def test_more_rows_than_one_dimension_of_a_grid_holds():
+    """A wavefront (or more) per row: 2^32 threads and more.  Every row is one of four, so the last ones are known."""
+    rows, n = 2 ** 26 + 3, 8
+    four = torch.tensor([[1, 2, 3, 4, 5, 6, 7, 8], [0] * 8, [-8, 4, 0, 1, 2, 0, 0, 0.5], [2] * 8], dtype=torch.bfloat16, device=DEV)
+    x = four.repeat(rows // 4 + 1, 1)[:rows]
+    ends = [0, 1, 2, 3, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 2 ** 24 + 2, 2 ** 26 - 1, 2 ** 26, 2 ** 26 + 1, 2 ** 26 + 2]
+    y = torch.full_like(x, 9)
+    B.csr5_rmsnorm(x, None, 1e-6, y=y)
+    small = torch.empty_like(four)
+    B.csr5_rmsnorm(four, None, 1e-6, y=small)
+    assert torch.equal(y, small.repeat(rows // 4 + 1, 1)[:rows])
+    place = torch.arange(rows, dtype=torch.int32, device=DEV).flip(0).view(rows, 1)
+    y.fill_(9)
+    B.csr5_combine(x, place, y)
+    assert torch.equal(y, x.flip(0))
+    weight, dweight = torch.full((rows, 1), 2.0, device=DEV), torch.full((rows, 1), 9.0, device=DEV)
+    y.fill_(9)
+    B.csr5_combine_backward(x, x, place, weight, y, dweight)
+    assert torch.equal(y, 2 * x.flip(0))
+    for r in ends:
+        assert dweight[r].item() == (x[r].float() * x[rows - 1 - r].float()).sum().item()
+    del place
+    expert = torch.arange(rows, dtype=torch.int32, device=DEV).remainder_(n).view(rows, 1)
+    y.fill_(9)
+    B.csr5_route_backward(expert, weight, dweight, y)
+    want = torch.zeros_like(y).scatter_(1, expert.long(), (-2 * dweight).to(torch.bfloat16))
+    assert torch.equal(y, want)
+    del want
+    del expert, weight, dweight
+    rows = 2 ** 28 + 5
+    x = four.repeat(rows // 4 + 1, 1)[:rows]
+    q, scale = torch.full((rows, n), 9, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn), torch.full((rows, 1), 9.0, device=DEV)
+    B.csr5_quantise(x, q, scale)
+    small_q, small_scale = torch.empty(4, n, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(4, 1, device=DEV)
+    B.csr5_quantise(four, small_q, small_scale)
+    for r in ends + [2 ** 28 - 1, 2 ** 28, 2 ** 28 + 4]:
+        assert torch.equal(q[r].view(torch.uint8), small_q[r % 4].view(torch.uint8)) and scale[r].item() == small_scale[r % 4].item()
+    assert not (scale == 9).any()

@@ -101,3 +101,18 @@ def test_tensors_that_do_not_fit_are_refused():
         B._experts(z(2, 8, 4), torch.float32, 2, 8, 5, "w")
     with pytest.raises(ValueError, match="needs"):
         B._source(None, 5, 4)
+
+
+def test_sizes_that_32_bits_do_not_count(lib):
+    big = 2 ** 31 - 1
+    assert lib.csr5_combine(1, 1, 1, big, 2, P, big, P, P, None, 0, P, big, None) == B.CSR5_ERANGE
+    assert lib.csr5_combine_backward(1, 1, 1, big, 2, P, big, P, big, P, P, P, big, P, None) == B.CSR5_ERANGE
+    for rows, n in ((big, 16), (4, big)):
+        assert lib.csr5_quantise(rows, n, 1, 2, P, n, P, n, P, 1, 1, None) == B.CSR5_ERANGE
+    for groups, rows, n, k in ((big, 8, 16, 32), (2, big, 16, 32), (2, 8, big, 32), (2, 8, 16, big)):
+        assert lib.csr5_grouped_gemm(groups, rows, n, k, 2, P, P, rows, k, None, P, k, 512, P, n, None) == B.CSR5_ERANGE
+        assert lib.csr5_grouped_gemm_dx(groups, rows, n, k, 2, P, P, n, P, k, 512, P, k, None) == B.CSR5_ERANGE
+        assert lib.csr5_grouped_gemm_dw(groups, rows, n, k, 2, P, P, n, P, rows, k, None, P, k, 512, None) == B.CSR5_ERANGE
+        assert lib.csr5_grouped_gemm_f8(groups, rows, n, k, 2, P, P, rows, k, P, 1, 1, None, P, k, 512, P, 128, 1, 1, 1, P, n, None) == B.CSR5_ERANGE
+    for m, n, k in ((big, 16, 32), (8, big, 32), (8, 16, big)):
+        assert lib.csr5_gemm_f8(m, n, k, 2, P, k, P, 1, 1, P, k, P, 128, 1, 1, P, n, None) == B.CSR5_ERANGE
