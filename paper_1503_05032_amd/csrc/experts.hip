@@ -39,6 +39,9 @@ __device__ __forceinline__ float group_sum(float v, float* part) {
 // Root-mean-square norm.  One workgroup per row, which it holds in registers between the sum of squares and the
 // output: x and the residual are read once.  8 neighbouring values per thread, so a block of 128 values that share a
 // scale is 16 neighbouring lanes; as many threads as the row has eights, up to 1024, then NV eights per thread.
+// Squares are added up in 32 bits; h is rounded for memory only, y once.  Bound by memory: 32768 x 4096 in bf16, x and the
+// residual to h and y, 173 us, 6.2 TB/s; to h and 8 bits with scales 166 us, 5.7 TB/s (a large copy: 4.8).  16 rows: 3.8 us, mostly
+// the launch.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int NORM_THREADS = 1024;
 
@@ -104,7 +107,8 @@ template <typename T, int NV, bool VEC> __global__ __launch_bounds__(NORM_THREAD
 }
 
 // Its gradients.  A workgroup takes rows by turns and keeps its share of the gain's gradient in registers; the shares
-// go to the workspace and are added up by k_columns in a fixed order.
+// go to the workspace and are added up by k_columns in a fixed order.  Bound by memory: 32768 x 4096 in bf16 with the
+// residual's gradient 213 us, 5.0 TB/s.
 constexpr int NORM_GROUPS = 1024;
 template <typename T> struct NormBackArgs {
     int rows, n;
@@ -195,7 +199,9 @@ template <typename F> void norm_shape(int n, F f) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Quantisation.  ROWS = 1: 16 lanes per block of 128 values; ROWS = 128: a workgroup per block of 128 x 128.
+// Quantisation.  ROWS = 1: 16 lanes per block of 128 values; ROWS = 128: a workgroup per block of 128 x 128.  A block stays in
+// registers between its maximum and its values, so x is read once.  Bound by memory: 32768 x 4096 in bf16 81 us with either,
+// 5.0 TB/s.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ROWS, bool VEC>
 __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, int64_t ldx, uint8_t* q, int64_t ldq, float* scale, int64_t scale_row, int64_t scale_block) {
@@ -250,7 +256,8 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
 //
 // Grouping is a counting sort, stable by pair: every workgroup counts the experts of its chunk of tokens; then each
 // adds up, per expert, the counts of all chunks and of those before it, and hands out rows to its pairs in order.
-// Tokens of one chunk: one workgroup does both.
+// Tokens of one chunk: one workgroup does both.  Both kernels wait more than they read or write: 32768 tokens, 8 of 256 in bf16
+// (20 MB, 4 us at a copy's rate) take 21 us.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int ROUTE_CHUNKS = 256;       // at most, each a workgroup
 constexpr int ROUTE_WAVES = 16;
@@ -497,7 +504,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_route_back(int to
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Back to the tokens.
+// Back to the tokens: a thread has 8 columns of a token, adds up its k rows in 32 bits and rounds once.  Bound by memory: 4 rows
+// of 4096 in bf16 for each of 8192 tokens 77 us, 5.2 TB/s.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_combine(int tokens, int k, int rows, int n, const T* z, int64_t ldz, const int32_t* place, const float* weight, const T* residual, int64_t ldr, T* y, int64_t ldy) {
@@ -518,7 +526,8 @@ __global__ __launch_bounds__(256) void k_combine(int tokens, int k, int rows, in
     store_values<8, VEC>(y + t * ldy + col, n - col, sum);
 }
 
-// A wavefront per pair: dz and the sum for dweight in one pass over the row of z.
+// A wavefront per pair: dz and the sum for dweight in one pass over the row of z.  Bound by memory: at combine's size 127 us, 4.8
+// TB/s.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_combine_back(int64_t pairs, int k, int rows, int n, const T* dy, int64_t lddy, const T* z, int64_t ldz, const int32_t* place, const float* weight, T* dz, int64_t lddz, float* dweight) {
     const int lane = threadIdx.x & 63;
