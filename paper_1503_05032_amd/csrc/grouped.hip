@@ -522,7 +522,7 @@ template <typename T, typename W> __device__ __forceinline__ void start_w(const 
 // second half of step s the tiles x s + 2 and w s + 3 are asked for, in the places of w s and x s.  So half of the loads
 // have a step to land, the others two.  Reads and loads are dealt out between the rows of products: together they held them up.
 template <typename T, int OP, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_tiles, int col_tiles) {
+__global__ __launch_bounds__(WI * WJ * 64, BI * BJ / (WI * WJ) < 64 * 64 ? 4 : 2) void k_product(Product a, int row_tiles, int col_tiles) {
     constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, TILE = BI * 128, RING = 5;
     static_assert(BI == BJ && TI >= 4 && TJ % 2 == 0, "places of a ring");
     constexpr bool X_TURNED = OP == DW, W_TURNED = OP != FWD;
@@ -569,10 +569,14 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
         else tw.template load<FAST>(q, tile, wave, int64_t(t.depth - c0) * 2);
     };
     auto load_row = [&](auto fast, int i, uint8_t* xt, uint8_t* wt, int32_t c0) __attribute__((always_inline)) {     // those beside row i: x of the step from c0 on, w of the next
+        constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
         for (int p = i * EACH; p < (i + 1) * EACH; p++) {
-            if (p < LOADS) load_x(fast, p, xt, c0);
-            else load_w(fast, p - LOADS, wt, c0 + 64);
+            if (p < LOADS) {
+                if (FAST || c0 < t.depth) load_x(fast, p, xt, c0);
+            } else {
+                if (FAST || c0 + 64 < t.depth) load_w(fast, p - LOADS, wt, c0 + 64);
+            }
         }
     };
 
@@ -636,7 +640,9 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product(Product a, int row_
         uint8_t *w_now = place[0], *x_now = place[1], *w_next = place[2], *x_next = place[3], *w_after = place[4];
         auto step = [&](auto fast, int32_t c0) __attribute__((always_inline)) {
             half(std::false_type(), fast, even, odd, x_now, w_now, 1, nullptr, nullptr, 0);
-            landed<LOADS>();                    // all but the loads of w_after
+            // all but the loads of w_after, where there are some
+            if (decltype(fast)::value || c0 + 128 < t.depth) landed<LOADS>();
+            else landed<0>();
             if constexpr (OP == DW) {
                 if (by_source) tw.here(lane, a.source_rows);
             }
@@ -938,6 +944,7 @@ template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
 //               128 x 128 tiles, with 16 rows 112 against 103; 8 bits with 6 rows 57 against 53; and where there are so few
 //               tiles that a step of their depth takes as long whatever they are: 128 rows of n = 2048 10 against 17 (10
 //               against 18), 64 of n = 8192 36 against 36 (24 against 32), 128 of n = 8192 64 against 35 (45 against 36)
+//   128 x 128   by four wavefronts, DW by eight (2048 x 2048 of 2048 rows 22 against 26; the others gain nothing by it)
 //   large tiles 256 rows and more where there are enough to go round the CUs: 4096 x 4096 x 2048 55 against 67, 2048 x 4096 x
 //               4096 78 against 61
 constexpr int FEW_ROWS16 = 12, FEW_ROWS8 = 4, FEW_AREA16 = 12288, FEW_AREA8 = 24576;
@@ -956,7 +963,7 @@ template <typename T, typename Y, int OP> int launch(Product a, hipStream_t s) {
     constexpr int BI = F8 ? 192 : 256;
     const int64_t large = (OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : a.rows / BI + (a.offset ? a.groups / 2 : 0)) * divide_up(a.cols, 256);
     if (height >= 192 && large >= LARGE_TILES) return launch_tiled<T, Y, OP, BI, 256, 2, 4>(a, s);
-    return launch_tiled<T, Y, OP, 128, 128, 2, 2>(a, s);
+    return launch_tiled<T, Y, OP, 128, 128, 2, OP == DW ? 4 : 2>(a, s);
 }
 
 bool half_type(int dtype) { return dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16; }
