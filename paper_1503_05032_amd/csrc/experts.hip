@@ -109,7 +109,6 @@ template <typename T, int NV, bool VEC> __global__ __launch_bounds__(NORM_THREAD
 // Its gradients.  A workgroup takes rows by turns and keeps its share of the gain's gradient in registers; the shares
 // go to the workspace and are added up by k_columns in a fixed order.  Bound by memory: 32768 x 4096 in bf16 with the
 // residual's gradient 213 us, 5.0 TB/s.
-constexpr int NORM_GROUPS = 1024;
 template <typename T> struct NormBackArgs {
     int rows, n;
     const T *h, *gain, *dy, *residual_grad;
@@ -191,11 +190,23 @@ __global__ __launch_bounds__(1024) void k_columns(int rows, int n, const float* 
 }
 
 // Threads of a row's workgroup, and how many times 8 values a thread holds.
+int norm_threads(int n) {
+    const int eights = divide_up(n, 8);
+    return eights >= NORM_THREADS ? NORM_THREADS : divide_up(eights, 64) * 64;
+}
 template <typename F> void norm_shape(int n, F f) {
-    const int eights = divide_up(n, 8), threads = eights >= NORM_THREADS ? NORM_THREADS : divide_up(eights, 64) * 64;
+    const int eights = divide_up(n, 8), threads = norm_threads(n);
     if (eights <= NORM_THREADS) f(threads, std::integral_constant<int, 1>());
     else if (eights <= 2 * NORM_THREADS) f(threads, std::integral_constant<int, 2>());
     else f(threads, std::integral_constant<int, 4>());
+}
+
+// Workgroups of k_rmsnorm_back.  Each writes a share of the gain's gradient, n floats, so there are no more than fill the card:
+// 4096 x 8192 with 256 of them 48 us, with 1024 69; 8191 x 2560 with 512 31, with 256 43, with 1024 35; 32768 x 1024 with
+// 1024 47, with 512 70.
+int norm_groups(int rows, int n) {
+    const int threads = norm_threads(n), fill = threads >= 512 ? 256 : threads >= 192 ? 512 : 1024;
+    return min(rows, fill);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -712,7 +723,7 @@ int csr5_rmsnorm(int32_t rows, int32_t n, int dtype, const void* x, int64_t ldx,
 
 size_t csr5_rmsnorm_workspace_bytes(int32_t rows, int32_t n) {
     if (rows < 0 || n < 0 || n > CSR5_NORM_MAX_N) return 0;
-    return size_t(rows < NORM_GROUPS ? rows : NORM_GROUPS) * size_t(n) * 4;
+    return n == 0 ? 0 : size_t(norm_groups(rows, n)) * size_t(n) * 4;
 }
 
 int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void* h, int64_t ldh, const void* gain, const float* rstd, const void* dy,
@@ -728,7 +739,7 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void* h, int
     if (reinterpret_cast<uintptr_t>(workspace) & 3) return CSR5_EINVAL;
     if (n == 0 || (rows == 0 && !dgain)) return CSR5_OK;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const int groups = rows < NORM_GROUPS ? rows : NORM_GROUPS;
+    const int groups = norm_groups(rows, n);
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
         const NormBackArgs<T> a{rows, n, static_cast<const T*>(h), static_cast<const T*>(gain), static_cast<const T*>(dy), static_cast<const T*>(residual_grad),
