@@ -794,7 +794,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int r
 // Few rows (a step of serving): bound by reading the weights once.  A workgroup of 8 wavefronts has 16 columns and 16 TI rows;
 // its wavefronts take the steps of the depth by turns, several at a time, from memory straight into the registers of the
 // matrix instructions (a load takes 64 contiguous bytes of 16 rows), and add up their sums in LDS in a fixed order.  64 rows
-// over 64 experts of 1536 x 2048 in bf16 41 us, 6.3 TB/s of the weights they name; 8 rows by 8192 x 4096 in 8 bits 9.2 us, 3.7 TB/s.
+// over 64 experts of 1536 x 2048 in bf16 41 us, 6.2 TB/s of the weights they name; 8 rows by 8192 x 4096 in 8 bits 9.2 us, 3.6 TB/s.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int FEW_WAVES = 8;
 // 8 bits: 32 columns to a workgroup where that still makes 256 of them (8 x 8192 x 4096 10.2 us against 11.2 with 16; 8 x 4096 x
