@@ -949,16 +949,19 @@ template <typename T, typename Y, int OP> bool chunks_fit(const Product& a) {
            (OP != FWD || a.source_rows > 0) && (OP == FWD ? whole(a.depth) : OP == DX ? whole(a.depth) && whole(a.cols) : whole(a.out_rows) && whole(a.cols));
 }
 
-// Which kernel.  Measured at k = 2048 and 4096, n = 1536 to 8192 (us in 16 bits, in 8):
+// Which kernel.  Measured at k = 1408 to 4096, n = 1024 to 8192 (us in 16 bits, in 8):
 //   few rows    groups of up to 12 rows on average (8 bits: 4): 64 groups of 1536 x 2048 with 10 rows each 86 against 97 in
 //               128 x 128 tiles, with 16 rows 112 against 103; 8 bits with 6 rows 57 against 53; and where there are so few
-//               tiles that a step of their depth takes as long whatever they are: 128 rows of n = 2048 10 against 17 (10
-//               against 18), 64 of n = 8192 36 against 36 (24 against 32), 128 of n = 8192 64 against 35 (45 against 36)
+//               tiles that a step of their depth takes as long whatever they are: 32 rows of n = 8192, k = 4096 21 against 34
+//               (12 against 20), 64 of them 36 against 35 (23 against 22)
+//   64 x 128    8 bits, up to 128 tiles of 128 x 128: 512 rows of 2048 x 2048 12.6 in 128 x 128, 9.8 so; 200 of 8192 x 8192 48, 41;
+//               1024 of 2048 x 4096 28, 22; with 256 tiles of 128 x 128 (1024 of 4096 x 8192) 52, 53, with 512 40, 53
 //   128 x 128   by four wavefronts, DW by eight (2048 x 2048 of 2048 rows 22 against 26; the others gain nothing by it)
 //   large tiles 256 rows and more where there are enough to go round the CUs: 4096 x 4096 x 2048 55 against 67, 2048 x 4096 x
 //               4096 78 against 61
-constexpr int FEW_ROWS16 = 12, FEW_ROWS8 = 4, FEW_AREA16 = 12288, FEW_AREA8 = 24576;
+constexpr int FEW_ROWS16 = 12, FEW_ROWS8 = 4, FEW_AREA = 12288;
 constexpr int LARGE_TILES = 192;
+constexpr int HALF_TILES = 128;
 
 template <typename T, typename Y, int OP> int launch(Product a, hipStream_t s) {
     constexpr bool F8 = is_f8<T>;
@@ -967,12 +970,14 @@ template <typename T, typename Y, int OP> int launch(Product a, hipStream_t s) {
     const int64_t height = OP == DW ? a.out_rows : a.rows / a.groups;
     if constexpr (OP == FWD) {
         const int64_t tiles = divide_up(a.rows, 32) + (a.offset ? a.groups - 1 : 0);
-        if (height <= (F8 ? FEW_ROWS8 : FEW_ROWS16) || tiles * a.cols <= (F8 ? FEW_AREA8 : FEW_AREA16))
+        if (height <= (F8 ? FEW_ROWS8 : FEW_ROWS16) || tiles * a.cols <= FEW_AREA)
             return height <= 16 ? launch_few<T, Y, 1>(a, s) : launch_few<T, Y, 2>(a, s);
     }
     constexpr int BI = F8 ? 192 : 256;
     const int64_t large = (OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, BI) : a.rows / BI + (a.offset ? a.groups / 2 : 0)) * divide_up(a.cols, 256);
     if (height >= 192 && large >= LARGE_TILES) return launch_tiled<T, Y, OP, BI, 256, 2, 4>(a, s);
+    if constexpr (F8)
+        if ((a.rows / 128 + (a.offset ? a.groups / 2 : 0)) * int64_t(divide_up(a.cols, 128)) <= HALF_TILES) return launch_tiled<T, Y, OP, 64, 128, 1, 4>(a, s);
     return launch_tiled<T, Y, OP, 128, 128, 2, OP == DW ? 4 : 2>(a, s);
 }
 

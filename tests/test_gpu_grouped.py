@@ -357,3 +357,22 @@ def test_sources_of_no_rows(sizes):
     dw = torch.ones_like(w)
     B.csr5_grouped_gemm_dw(y, w[0, :0], offsets(sizes), dw, source=source)
     assert not dw.any()
+
+
+@pytest.mark.parametrize("w_rows", [128, 1])
+@pytest.mark.parametrize("sizes,n,k", [([200], 5640, 272), ([513], 2056, 1040), ([70, 0, 130, 65], 2048, 528)])
+def test_f8_in_tiles_of_64_rows(sizes, n, k, w_rows):
+    """More rows and columns than go for few, fewer than fill the card with larger tiles."""
+    g = torch.Generator().manual_seed(n + k)
+    rows, groups = sum(sizes), len(sizes)
+    x, xs, xc = f8_operand(g, rows, k, 1, "wide")
+    operands = [f8_operand(g, n, k, w_rows, "plain") for _ in range(groups)]
+    w, ws = torch.stack([o[0] for o in operands]), torch.stack([o[1] for o in operands])
+    source = source_for(g, rows, rows)
+    for s in (None, source):
+        big, y = room(rows, n, torch.float16, "wide")
+        B.csr5_grouped_gemm_f8(x, xs, w, ws, offsets(sizes), y, w_rows=w_rows, source=None if s is None else s.to(DEV))
+        untouched(big, rows, n, "wide")
+        seen = taken(xc, s, rows)
+        for i, a, b in spans(sizes):
+            close(y[a:b], seen[a:b] @ operands[i][2].T, torch.float16, (k + 8) * EPS32 * (seen[a:b].abs() @ operands[i][2].T.abs()))
