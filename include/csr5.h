@@ -523,8 +523,8 @@ int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const 
  * Product in 8 bits: y[i][j] = sum over blocks b of 128 of
  *   x_scale(i, b) * w_scale(j / w_rows, b) * sum_{c in b} x[i][c] w[j][c],
  * each block's sum before it is scaled, the blocks' sums in 32 bits.  (With 16-byte rows
- * a block is one matrix instruction for 8 bits, which drops what is below 2^-15 or so of
- * a block's largest product; otherwise it is summed in 32 bits.)  x[m][k], w[n][k]; w_rows is 128
+ * and k >= 64 a block is one matrix instruction for 8 bits, which drops what is below
+ * 2^-15 or so of a block's largest product; otherwise it is summed in 32 bits.)  x[m][k], w[n][k]; w_rows is 128
  * (scales of csr5_quantise with block_rows 128: weights) or 1 (both operands are
  * quantised by rows, as the gradient of a weight needs it).  x_scale(i, b) is at
  * x_scale[i*xs_row + b*xs_block], w_scale at w_scale[(j/w_rows)*ws_row + b*ws_block].

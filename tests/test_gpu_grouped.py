@@ -376,3 +376,60 @@ def test_f8_in_tiles_of_64_rows(sizes, n, k, w_rows):
         seen = taken(xc, s, rows)
         for i, a, b in spans(sizes):
             close(y[a:b], seen[a:b] @ operands[i][2].T, torch.float16, (k + 8) * EPS32 * (seen[a:b].abs() @ operands[i][2].T.abs()))
+
+
+# ---------------------------------------------------------------------------------------------------------------- where steps end
+ENDS = [1, 63, 64, 65, 127, 128, 129, 0, 192, 193, 256, 257, 320, 321]
+
+
+@pytest.mark.parametrize("n,k", [(136, 264), (1024, 1032)])
+@pytest.mark.parametrize("by_source", [False, True])
+def test_dw_of_groups_that_end_about_a_step(n, k, by_source):
+    g = torch.Generator().manual_seed(n + by_source)
+    rows, groups = sum(ENDS), len(ENDS)
+    dy, x = matrix(g, rows, n, torch.bfloat16), matrix(g, rows, k, torch.bfloat16)
+    source = source_for(g, rows, rows) if by_source else None
+    big, dw = room(groups * n, k, torch.bfloat16, "wide")
+    B.csr5_grouped_gemm_dw(dy, x, offsets(ENDS), dw.unflatten(0, (groups, n)), source=None if source is None else source.to(DEV))
+    untouched(big, groups * n, k, "wide")
+    xc, dyc = taken(x, source, rows), dy.double().cpu()
+    for i, a, b in spans(ENDS):
+        close(dw[i * n:(i + 1) * n], dyc[a:b].T @ xc[a:b], torch.bfloat16, (b - a + 8) * EPS32 * (dyc[a:b].T.abs() @ xc[a:b].abs()), ENDS[i])
+
+
+@pytest.mark.parametrize("depth", [8, 56, 64, 72, 128, 136, 184, 192, 200, 256, 264, 320, 328])
+def test_depths_that_end_about_a_step(depth):
+    """y and dx of that depth, in 128 x 128 tiles and (192 of them) larger ones."""
+    g = torch.Generator().manual_seed(depth)
+    for rows, cols in ((300, 2056), (3080, 4104)):
+        offset = offsets([rows])
+        for turned in (False, True):
+            x = matrix(g, rows, depth, torch.bfloat16)
+            w = experts(g, 1, *((depth, cols) if turned else (cols, depth)), torch.bfloat16, "plain")
+            big, y = room(rows, cols, torch.bfloat16, "wide")
+            (B.csr5_grouped_gemm_dx if turned else B.csr5_grouped_gemm)(x, w, offset, y)
+            untouched(big, rows, cols, "wide")
+            xc, wc = x.double().cpu(), w[0].double().cpu() if turned else w[0].double().cpu().T
+            close(y, xc @ wc, torch.bfloat16, (depth + 8) * EPS32 * (xc.abs() @ wc.abs()), (rows, turned))
+
+
+@pytest.mark.parametrize("depth", [16, 48, 64, 112, 128, 144, 256, 272, 384, 400, 512, 528, 640])
+def test_f8_depths_that_end_about_a_step(depth):
+    """In tiles of 64 x 128, of 128 x 128 and (192 of them) of 192 x 256.  Whole numbers up to 4 with scales of powers of two:
+    every sum is exact, in the 8-bit instruction as well, so only y is rounded (not at all in float32)."""
+    g = torch.Generator().manual_seed(depth)
+
+    def operand(rows, by):
+        q = torch.randint(-4, 5, (rows, depth), generator=g).float()
+        scale = 2.0 ** torch.randint(-2, 3, (-(-rows // by), -(-depth // 128)), generator=g)
+        seen = q * scale.repeat_interleave(by, 0)[:rows].repeat_interleave(128, 1)[:, :depth]
+        return q.to(torch.float8_e4m3fn).to(DEV), scale.to(DEV), seen.double()
+
+    for rows, n in ((300, 2056), (1500, 2056), (3080, 4104)):
+        x, xs, xc = operand(rows, 1)
+        for w_rows in (128, 1):
+            w, ws, wc = operand(n, w_rows)
+            big, y = room(rows, n, torch.float32, "wide")
+            B.csr5_gemm_f8(x, xs, w, ws, y, w_rows=w_rows)
+            untouched(big, rows, n, "wide")
+            assert torch.equal(y.double().cpu(), xc @ wc.T), (rows, w_rows)
