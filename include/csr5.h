@@ -495,7 +495,8 @@ int csr5_combine_backward(int32_t tokens, int32_t k, int32_t rows, int32_t n, in
  * x[x_rows][k]; source int32[rows], or NULL: row r itself (x_rows >= rows then);
  * w[g] is n x k with row stride ldw, and begins w_group elements after w[g-1]; dw
  * likewise.  dtype BF16 or F16 for all matrices of a call.  Rows in no group are
- * left as they are; dw of an empty group is 0.
+ * left as they are; dw of an empty group is 0.  y of a row whose source is none is 0
+ * whatever w holds; in dw such a row counts as one of zeros (an infinity in dy[r] shows).
  */
 int csr5_grouped_gemm(int32_t groups, int32_t rows, int32_t n, int32_t k, int dtype, const int32_t *offset,
                       const void *x, int32_t x_rows, int64_t ldx, const int32_t *source, const void *w,

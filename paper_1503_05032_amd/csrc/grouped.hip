@@ -278,10 +278,11 @@ template <typename T, typename Y, int OP> __global__ __launch_bounds__(256) void
     for (int i = 0; i < 4; i++) {
         const int32_t row = i0 + wi + i * 16 + (lane & 15);
         if (row >= i_end) continue;
+        const bool zero = OP == FWD && source_of(a, row) < 0;       // whatever w holds
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const int32_t col = j0 + wj + j * 16 + (lane >> 4) * 4;
-            store_four<Y, false>(y + int64_t(row) * a.ldy + col, a.cols - col, acc[j][i]);
+            store_four<Y, false>(y + int64_t(row) * a.ldy + col, a.cols - col, zero ? f32x4{0, 0, 0, 0} : acc[j][i]);
         }
     }
 }
