@@ -421,7 +421,8 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
  * atomically.  Outputs must not overlap inputs unless a comment says that they may.
  *
  * Whatever offset, source and place hold, no kernel leaves the arrays: offsets are
- * clamped to [0, rows], a group that ends before it begins is empty, a source
+ * clamped to [0, rows], a group that ends before it begins is empty (where groups overlap,
+ * each value of a row of both is either's or left as it is, by timing), a source
  * outside [0, x_rows) is a row of zeros and a place outside [0, rows) is no row.
  * A size of 0 is fine: such a call writes what is left to write (or nothing).  One of
  * 2^31 - 2^16 or more is CSR5_ERANGE where a kernel counts in 32 bits.

@@ -64,7 +64,7 @@ __device__ __forceinline__ Span uniform(Span s) {
 }
 
 // The t-th tile of BM rows, counted through the groups in order; group -1: there are fewer.  The whole wavefront takes part:
-// a lane per group.  At most rows / BM + groups tiles.
+// a lane per group.  At most rows / BM + groups tiles where no groups overlap; there are no workgroups for more.
 template <int BM> __device__ __forceinline__ Span find_tile(const Product& a, int32_t t) {
     if (!a.offset) {
         const int64_t first = int64_t(t) * BM;

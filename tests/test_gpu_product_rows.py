@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from layer_util import DEV, offsets, place_in
+from layer_util import DEV, offsets, place_in, room, untouched
 from paper_1503_05032_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +50,78 @@ def test_rows_without_a_source_are_zeros_whatever_the_weights_hold(rows, n, layo
         B.csr5_grouped_gemm_f8(place_in(x.to(torch.float8_e4m3fn), layout), torch.ones(rows, 2, device=DEV), place_in(w8, layout).unflatten(0, (2, n)),
                                ws.to(DEV), offset, y, w_rows=1, source=source.to(DEV))
         check()
+
+
+# rows, n, k: few rows, 128 x 128, large tiles of y; of dx; of dw.  Four groups.
+HALVES = [(30, 32, 48, "plain"), (30, 33, 47, "odd"), (300, 1032, 72, "plain"), (1024, 8200, 72, "plain"), (1024, 72, 8200, "plain"), (100, 1800, 1800, "plain")]
+# few rows, 64 x 128, 128 x 128, large tiles
+EIGHTS = [(12, 40, 144, "plain"), (30, 33, 47, "odd"), (300, 1032, 144, "plain"), (1500, 2056, 144, "plain"), (1500, 5640, 144, "plain")]
+OUTSIDE = {
+    "past both ends": lambda r: [-4, r // 3, r // 3, r + 1000, 6],
+    "back to the beginning": lambda r: [r + 9, -7, r // 2 - 1, 2 ** 31 - 1, -2 ** 31],
+    "all past the end": lambda r: [r + 1, r + 1, r + 2, r, 2 ** 31 - 1],
+    "rows in no group": lambda r: [5, r // 4, r // 4 + 3, r // 2, r - 4],
+    "overlapping": lambda r: [0, r, 0, r, 0],
+}
+
+
+def whole(gen, rows, k):
+    return torch.randint(-2, 3, (rows, k), generator=gen).float()
+
+
+def spans(offset, rows):
+    at = [min(max(o, 0), rows) for o in offset]
+    return [(g, a, max(a, b)) for g, (a, b) in enumerate(zip(at, at[1:]))]
+
+
+def check_rows(got, product, offset, rows):
+    """Each row has its group's product, or what was there; each value of a row of two groups either's, or that."""
+    allowed = [[] for _ in range(rows)]
+    for g, a, b in spans(offset, rows):
+        if b > a:
+            out = product(g, a, b).to(got.dtype)
+            for r in range(a, b):
+                allowed[r].append(out[r - a])
+    before = torch.full_like(got[0], 77.0)
+    for r in range(rows):
+        if len(allowed[r]) != 1:
+            allowed[r].append(before)
+        assert torch.stack([got[r] == a for a in allowed[r]]).any(0).all(), r
+
+
+@pytest.mark.parametrize("offset", OUTSIDE)
+@pytest.mark.parametrize("rows,n,k,layout", HALVES)
+def test_offsets_outside_or_out_of_order(rows, n, k, layout, offset):
+    g = torch.Generator().manual_seed(rows + n)
+    offset = OUTSIDE[offset](rows)
+    o, t = torch.tensor(offset, dtype=torch.int32, device=DEV), torch.bfloat16
+    x, w, dy = whole(g, rows, k), whole(g, 4 * n, k), whole(g, rows, n)
+    xd, wd, dyd = place_in(x.to(t), layout), place_in(w.to(t), layout).unflatten(0, (4, n)), place_in(dy.to(t), layout)
+    (big_y, y), (big_x, dx), (big_w, dw) = room(rows, n, t, layout), room(rows, k, t, layout), room(4 * n, k, t, layout)
+    B.csr5_grouped_gemm(xd, wd, o, y)
+    B.csr5_grouped_gemm_dx(dyd, wd, o, dx)
+    B.csr5_grouped_gemm_dw(dyd, xd, o, dw.unflatten(0, (4, n)))
+    for big, r, c in ((big_y, rows, n), (big_x, rows, k), (big_w, 4 * n, k)):
+        untouched(big, r, c, layout)
+    w = w.unflatten(0, (4, n))
+    check_rows(y.cpu(), lambda e, a, b: x[a:b] @ w[e].T, offset, rows)
+    check_rows(dx.cpu(), lambda e, a, b: dy[a:b] @ w[e], offset, rows)
+    for e, a, b in spans(offset, rows):
+        assert torch.equal(dw[e * n:(e + 1) * n].cpu(), (dy[a:b].T @ x[a:b]).to(t)), e
+
+
+@pytest.mark.parametrize("offset", OUTSIDE)
+@pytest.mark.parametrize("w_rows", [128, 1])
+@pytest.mark.parametrize("rows,n,k,layout", EIGHTS)
+def test_offsets_outside_or_out_of_order_in_8_bits(rows, n, k, layout, w_rows, offset):
+    g = torch.Generator().manual_seed(rows + n)
+    offset, blocks = OUTSIDE[offset](rows), -(-k // 128)
+    o, f8 = torch.tensor(offset, dtype=torch.int32, device=DEV), torch.float8_e4m3fn
+    x, w = whole(g, rows, k), whole(g, 4 * n, k)
+    xs, ws = 2.0 ** torch.randint(-2, 3, (rows, blocks), generator=g), 2.0 ** torch.randint(-2, 3, (4, -(-n // w_rows), blocks), generator=g)
+    big, y = room(rows, n, torch.bfloat16, layout)
+    B.csr5_grouped_gemm_f8(place_in(x.to(f8), layout), xs.to(DEV), place_in(w.to(f8), layout).unflatten(0, (4, n)), ws.to(DEV), o, y, w_rows=w_rows)
+    untouched(big, rows, n, layout)
+    x = x * xs.repeat_interleave(128, 1)[:, :k]
+    w = w.unflatten(0, (4, n)) * ws.repeat_interleave(w_rows, 1)[:, :n].repeat_interleave(128, 2)[:, :, :k]
+    check_rows(y.cpu(), lambda e, a, b: x[a:b] @ w[e].T, offset, rows)
