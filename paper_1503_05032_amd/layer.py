@@ -37,7 +37,7 @@ class Layer:
         tokens, pairs = u.shape[0], u.shape[0] * self.k
         ints = lambda *shape: self._empty(*shape, dtype=torch.int32)
         logits = self._empty(tokens, self.experts)
-        all_rows = torch.tensor([0, tokens], dtype=torch.int32).to(u.device)
+        all_rows = torch.arange(2, dtype=torch.int32, device=u.device).mul_(tokens)       # [0, tokens], without a copy that waits
         B.csr5_grouped_gemm(u, self.router, all_rows, logits)
         expert, place, source, offset = ints(tokens, self.k), ints(tokens, self.k), ints(pairs), ints(self.experts + 1)
         weight = self._empty(tokens, self.k, dtype=torch.float32)
