@@ -71,8 +71,8 @@ public:
         }
         return v;
     }
-    // the stream: its address, a torch stream, or None: torch's current one.  Last of all, as it may have to make the device
-    // ready.
+    // the stream: its address, a torch stream, or None: torch's current one.  In a statement of its own after all others (arguments
+    // of a call are evaluated in any order), as it may have to make the device ready.
     void* stream(int i) const {
         PyObject* at = a_[i];
         PyObject* own = nullptr;
@@ -161,8 +161,11 @@ int route(const Args& a) {
     const int64_t pairs = l.rows * std::max(k, 0);
     uint8_t* const space = a.array<uint8_t>(7, "workspace", at::kByte, 0);
     const size_t bytes = a.none(7) ? 0 : size_t(a.tensor(7, "workspace").numel());
-    return csr5_route(int32_t(l.rows), int32_t(l.cols), k, dtype, l.p, l.ld, a.whole(2, "expert", pairs), a.floats(3, "weight", pairs), a.whole(4, "offset", l.cols + 1),
-                      a.whole(5, "source", pairs), a.whole(6, "place", pairs), space, bytes, a.stream(8));
+    int32_t *const expert = a.whole(2, "expert", pairs), *const offset = a.whole(4, "offset", l.cols + 1);
+    int32_t *const source = a.whole(5, "source", pairs), *const place = a.whole(6, "place", pairs);
+    float* const weight = a.floats(3, "weight", pairs);
+    void* const stream = a.stream(8);
+    return csr5_route(int32_t(l.rows), int32_t(l.cols), k, dtype, l.p, l.ld, expert, weight, offset, source, place, space, bytes, stream);
 }
 
 // z, place, y, weight, residual, stream
@@ -174,8 +177,10 @@ int combine(const Args& a) {
     const int64_t tokens = place.size(0), k = place.size(1);
     if (tokens != int32_t(tokens) || k != int32_t(k)) throw Refused("place: too large");
     const Matrix y = a.typed(2, "y", z.type, tokens, z.cols), r = a.maybe(4, "residual", z.type, tokens, z.cols);
-    return csr5_combine(int32_t(tokens), int32_t(k), int32_t(z.rows), int32_t(z.cols), dtype, z.p, z.ld, a.whole(1, "place", tokens * k), a.floats(3, "weight", tokens * k), r.p,
-                        r.ld, y.p, y.ld, a.stream(5));
+    const int32_t* const row = a.whole(1, "place", tokens * k);
+    const float* const weight = a.floats(3, "weight", tokens * k);
+    void* const stream = a.stream(5);
+    return csr5_combine(int32_t(tokens), int32_t(k), int32_t(z.rows), int32_t(z.cols), dtype, z.p, z.ld, row, weight, r.p, r.ld, y.p, y.ld, stream);
 }
 
 // x, w, offset, y, source, stream
@@ -183,8 +188,10 @@ int grouped_gemm(const Args& a) {
     const Matrix x = a.matrix(0, "x");
     const int dtype = code(x.type, "x");
     const Matrix w = a.typed(1, "w", x.type, -1, x.cols, -1), y = a.typed(3, "y", x.type, -1, w.rows);
-    return csr5_grouped_gemm(int32_t(w.groups), int32_t(y.rows), int32_t(w.rows), int32_t(x.cols), dtype, a.whole(2, "offset", w.groups + 1), x.p, int32_t(x.rows), x.ld,
-                             a.source(4, y.rows, x.rows), w.p, w.ld, w.group, y.p, y.ld, a.stream(5));
+    const int32_t *const offset = a.whole(2, "offset", w.groups + 1), *const source = a.source(4, y.rows, x.rows);
+    void* const stream = a.stream(5);
+    return csr5_grouped_gemm(int32_t(w.groups), int32_t(y.rows), int32_t(w.rows), int32_t(x.cols), dtype, offset, x.p, int32_t(x.rows), x.ld, source, w.p, w.ld, w.group, y.p,
+                             y.ld, stream);
 }
 
 // x, q, scale, block_rows, stream
@@ -193,7 +200,8 @@ int quantise(const Args& a) {
     const int dtype = code(x.type, "x");
     const int32_t by = a.number(3, "block_rows");
     const Matrix q = a.f8(1, "q", x.rows, x.cols), s = a.scales(2, "scale", by > 0 ? (x.rows + by - 1) / by : 0, blocks(x.cols));
-    return csr5_quantise(int32_t(x.rows), int32_t(x.cols), by, dtype, x.p, x.ld, as<uint8_t>(q), q.ld, as<float>(s), s.ld, s.cols, a.stream(4));
+    void* const stream = a.stream(4);
+    return csr5_quantise(int32_t(x.rows), int32_t(x.cols), by, dtype, x.p, x.ld, as<uint8_t>(q), q.ld, as<float>(s), s.ld, s.cols, stream);
 }
 
 // x, x_scale, w, w_scale, y, w_rows, stream
@@ -202,8 +210,9 @@ int gemm_f8(const Args& a) {
     const int dtype = code(y.type, "y");
     const int32_t by = a.number(5, "w_rows");
     const Matrix xs = a.scales(1, "x_scale", x.rows, blocks(x.cols)), ws = a.scales(3, "w_scale", by > 0 ? (w.rows + by - 1) / by : 0, blocks(x.cols));
+    void* const stream = a.stream(6);
     return csr5_gemm_f8(int32_t(x.rows), int32_t(w.rows), int32_t(x.cols), dtype, as<uint8_t>(x), x.ld, as<float>(xs), xs.ld, xs.cols, as<uint8_t>(w), w.ld, as<float>(ws), by, ws.ld,
-                        ws.cols, y.p, y.ld, a.stream(6));
+                        ws.cols, y.p, y.ld, stream);
 }
 
 // x, x_scale, w, w_scale, offset, y, w_rows, source, stream
@@ -214,9 +223,10 @@ int grouped_gemm_f8(const Args& a) {
     const Matrix xs = a.scales(1, "x_scale", x.rows, blocks(x.cols));
     if (w.groups == 0) return CSR5_OK;              // no scales to look at
     const Matrix ws = a.scales(3, "w_scale", by > 0 ? (w.rows + by - 1) / by : 0, blocks(x.cols), w.groups);
-    return csr5_grouped_gemm_f8(int32_t(w.groups), int32_t(y.rows), int32_t(w.rows), int32_t(x.cols), dtype, a.whole(4, "offset", w.groups + 1), as<uint8_t>(x), int32_t(x.rows), x.ld,
-                                as<float>(xs), xs.ld, xs.cols, a.source(7, y.rows, x.rows), as<uint8_t>(w), w.ld, w.group, as<float>(ws), by, ws.ld, ws.cols, ws.group, y.p, y.ld,
-                                a.stream(8));
+    const int32_t *const offset = a.whole(4, "offset", w.groups + 1), *const source = a.source(7, y.rows, x.rows);
+    void* const stream = a.stream(8);
+    return csr5_grouped_gemm_f8(int32_t(w.groups), int32_t(y.rows), int32_t(w.rows), int32_t(x.cols), dtype, offset, as<uint8_t>(x), int32_t(x.rows), x.ld, as<float>(xs), xs.ld,
+                                xs.cols, source, as<uint8_t>(w), w.ld, w.group, as<float>(ws), by, ws.ld, ws.cols, ws.group, y.p, y.ld, stream);
 }
 
 // x, gain, eps, residual, h, y, q, scale, rstd, stream
@@ -233,8 +243,10 @@ int rmsnorm(const Args& a) {
     }
     const Matrix r = a.maybe(3, "residual", x.type, x.rows, x.cols), h = a.maybe(4, "h", x.type, x.rows, x.cols), y = a.maybe(5, "y", x.type, x.rows, x.cols);
     const Matrix q = a.none(6) ? Matrix() : a.f8(6, "q", x.rows, x.cols), s = a.none(7) ? Matrix() : a.scales(7, "scale", x.rows, blocks(x.cols));
-    return csr5_rmsnorm(int32_t(x.rows), int32_t(x.cols), dtype, x.p, x.ld, r.p, r.ld, gain, float(a.real(2, "eps")), h.p, h.ld, y.p, y.ld, as<uint8_t>(q), q.ld, as<float>(s), s.ld,
-                        s.cols, a.floats(8, "rstd", x.rows), a.stream(9));
+    const float eps = float(a.real(2, "eps"));
+    float* const rstd = a.floats(8, "rstd", x.rows);
+    void* const stream = a.stream(9);
+    return csr5_rmsnorm(int32_t(x.rows), int32_t(x.cols), dtype, x.p, x.ld, r.p, r.ld, gain, eps, h.p, h.ld, y.p, y.ld, as<uint8_t>(q), q.ld, as<float>(s), s.ld, s.cols, rstd, stream);
 }
 
 template <int (*F)(const Args&), int COUNT> PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
