@@ -432,7 +432,7 @@ def csr5_read_array(h, which, wide=False):
 # ---------------------------------------------------------------------------------------------------------------------
 # Products of a layer of experts (section 5 of the header).  Matrices are 2-D tensors whose rows are contiguous (views
 # into wider ones are fine), weights of experts 3-D ones; sizes are taken from the tensors, and what the library cannot
-# see (element types, lengths) is checked here.  8-bit values are float8_e4m3fn or uint8 tensors.
+# see (element types, lengths, that they are on one GPU) is checked here.  8-bit values are float8_e4m3fn or uint8 tensors.
 # ---------------------------------------------------------------------------------------------------------------------
 _TYPE_CODES: dict = {}      # 16- and 32-bit floating types -> dtype codes; filled on first use
 _F8_TYPES: tuple = ()
@@ -475,6 +475,20 @@ def _experts(t, dtype, groups, n, k, name):
     return t.data_ptr() or None, ld if n > 1 else max(ld, k), group
 
 
+def _stream_of(stream, *tensors):
+    """The stream's address; refuses tensors of several GPUs, or of another one than the stream's (which an address does not say)."""
+    gpus = {t.get_device() for t in tensors if t is not None and not isinstance(t, int)}
+    if len(gpus) > 1:
+        raise ValueError(f"expected tensors on one GPU, got some on GPUs {sorted(gpus)}")
+    address, gpu = _stream(stream), getattr(stream, "device_index", None)
+    if stream is None:
+        import torch
+        gpu = torch.cuda.current_device()
+    if gpu is not None and gpus and gpu not in gpus:
+        raise ValueError(f"the tensors are on GPU {gpus.pop()}, the stream is one of GPU {gpu}")
+    return address
+
+
 _marshal = None     # csrc/marshal.cpp: takes the tensors of a serving step's calls apart (and makes the same checks)
 
 
@@ -514,7 +528,7 @@ def csr5_route_backward(expert, weight, dweight, dlogits, stream=None, check=Tru
     k = expert.shape[1]
     return _chk(load().csr5_route_backward(tokens, experts, k, code, _arr(expert, ["i32"], tokens * k, "expert"),
                                            _arr(weight, ["f32"], tokens * k, "weight"), _arr(dweight, ["f32"], tokens * k, "dweight"),
-                                           *_matrix(dlogits, dlogits.dtype, tokens, experts, "dlogits"), _stream(stream)),
+                                           *_matrix(dlogits, dlogits.dtype, tokens, experts, "dlogits"), _stream_of(stream, expert, weight, dweight, dlogits)),
                 "csr5_route_backward", check)
 
 
@@ -531,7 +545,7 @@ def csr5_combine_backward(dy, z, place, weight, dz, dweight, stream=None, check=
     return _chk(load().csr5_combine_backward(tokens, k, rows, n, code, *_matrix(dy, dt, tokens, n, "dy"), *_matrix(z, dt, rows, n, "z"),
                                              _arr(place, ["i32"], tokens * k, "place"), _arr(weight, ["f32"], tokens * k, "weight"),
                                              *_matrix(dz, dt, rows, n, "dz"), _arr(dweight, ["f32"], tokens * k, "dweight"),
-                                             _stream(stream)), "csr5_combine_backward", check)
+                                             _stream_of(stream, dy, z, place, weight, dz, dweight)), "csr5_combine_backward", check)
 
 
 def _source(source, rows, x_rows):
@@ -553,7 +567,7 @@ def csr5_grouped_gemm_dx(dy, w, offset, dx, stream=None, check=True):
     rows, n = dy.shape
     groups, k = w.shape[0], w.shape[2]
     return _chk(load().csr5_grouped_gemm_dx(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), *_matrix(dy, dt, rows, n, "dy"),
-                                            *_experts(w, dt, groups, n, k, "w"), *_matrix(dx, dt, rows, k, "dx"), _stream(stream)),
+                                            *_experts(w, dt, groups, n, k, "w"), *_matrix(dx, dt, rows, k, "dx"), _stream_of(stream, dy, w, offset, dx)),
                 "csr5_grouped_gemm_dx", check)
 
 
@@ -566,7 +580,7 @@ def csr5_grouped_gemm_dw(dy, x, offset, dw, source=None, stream=None, check=True
     px, ldx = _matrix(x, dt, x_rows, k, "x")
     return _chk(load().csr5_grouped_gemm_dw(groups, rows, n, k, code, _arr(offset, ["i32"], groups + 1, "offset"), *_matrix(dy, dt, rows, n, "dy"),
                                             px, x_rows, ldx, _source(source, rows, x_rows), *_experts(dw, dt, groups, n, k, "dw"),
-                                            _stream(stream)), "csr5_grouped_gemm_dw", check)
+                                            _stream_of(stream, dy, x, offset, dw, source)), "csr5_grouped_gemm_dw", check)
 
 
 def csr5_quantise(x, q, scale, block_rows=1, stream=None, check=True):
@@ -606,4 +620,4 @@ def csr5_rmsnorm_backward(h, gain, rstd, dy, dh, dgain=None, workspace=None, res
                                              _arr(rstd, ["f32"], rows, "rstd"), *_matrix(dy, dt, rows, n, "dy"),
                                              *((None, 0) if residual_grad is None else _matrix(residual_grad, dt, rows, n, "residual_grad")),
                                              *_matrix(dh, dt, rows, n, "dh"), _arr(dgain, ["f32"], n, "dgain"), *_space(workspace),
-                                             _stream(stream)), "csr5_rmsnorm_backward", check)
+                                             _stream_of(stream, h, gain, rstd, dy, dh, dgain, workspace, residual_grad)), "csr5_rmsnorm_backward", check)

@@ -1,9 +1,10 @@
 // Python's side of the calls of a serving step (the router, products, norm, quantisation, combination): takes tensors apart,
-// checks what the C library cannot see -- element types, shapes, strides, that they are on the GPU -- and calls it.  A call
+// checks what the C library cannot see -- element types, shapes, strides, that they are on one GPU -- and calls it.  A call
 // of binding.py by ctypes takes 6 us for this, as long as the kernel of a small step; here it is under one.  Every function
 // takes its arguments by position, None for what is not given, the stream's address last, and returns the C function's
 // code; what does not fit raises ValueError.
 #include <Python.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdexcept>
@@ -53,6 +54,9 @@ public:
         const at::ScalarType s = t.scalar_type();
         if (!is_f8(s) && s != at::kInt) code(s, name);          // a type of none of these calls is what to say first
         if (!t.is_cuda()) throw Refused(std::string(name) + ": expected a GPU tensor");
+        const int gpu = t.get_device();
+        if (gpu_ >= 0 && gpu != gpu_) throw Refused(std::string(name) + ": expected a tensor on GPU " + std::to_string(gpu_) + " as the others, got one on GPU " + std::to_string(gpu));
+        gpu_ = gpu;
         return t;
     }
     int32_t number(int i, const char* name) const {
@@ -72,16 +76,27 @@ public:
         return v;
     }
     // the stream: its address, a torch stream, or None: torch's current one.  In a statement of its own after all others (arguments
-    // of a call are evaluated in any order), as it may have to make the device ready.
+    // of a call are evaluated in any order), as it may have to make the device ready.  Refused where it is of another GPU than the
+    // tensors (which an address does not say).
     void* stream(int i) const {
         PyObject* at = a_[i];
         PyObject* own = nullptr;
-        if (at == Py_None) at = own = PyObject_CallObject(current_stream, nullptr);
-        else if (!PyLong_Check(at)) at = own = PyObject_GetAttrString(at, "cuda_stream");
+        int gpu = gpu_;
+        if (at == Py_None) {
+            at = own = PyObject_CallObject(current_stream, nullptr);
+            if (at) gpu = c10::impl::VirtualGuardImpl(at::kCUDA).getDevice().index();
+        } else if (!PyLong_Check(at)) {
+            PyObject* const index = PyObject_GetAttrString(at, "device_index");
+            if (index) gpu = int(PyLong_AsLong(index));
+            Py_XDECREF(index);
+            PyErr_Clear();
+            at = own = PyObject_GetAttrString(at, "cuda_stream");
+        }
         if (!at) throw Raised();
         void* const p = at == Py_None ? nullptr : PyLong_AsVoidPtr(at);
         Py_XDECREF(own);
         if (!p && PyErr_Occurred()) throw Raised();
+        if (gpu != gpu_) throw Refused("the tensors are on GPU " + std::to_string(gpu_) + ", the stream is one of GPU " + std::to_string(gpu));
         return p;
     }
     static PyObject* current_stream;        // returns the current stream's address
@@ -146,6 +161,7 @@ public:
 
 private:
     PyObject* const* a_;
+    mutable int gpu_ = -1;      // of the tensors so far
 };
 
 PyObject* Args::current_stream = nullptr;

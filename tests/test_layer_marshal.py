@@ -58,3 +58,46 @@ def test_the_stream_is_asked_for_last(native, call):
         short = shapes | {name: (dtype, *shape[:-1], shape[-1] - 1)}
         with pytest.raises(ValueError):
             getattr(native, call)(*arguments(tensors(**short)), None)
+
+
+# the calls that binding.py takes apart itself
+BACKWARD = {
+    "csr5_route_backward": dict(expert=(I32, 4, 2), weight=(F32, 4, 2), dweight=(F32, 4, 2), dlogits=(BF16, 4, 8)),
+    "csr5_combine_backward": dict(dy=(BF16, 4, 16), z=(BF16, 8, 16), place=(I32, 4, 2), weight=(F32, 4, 2), dz=(BF16, 8, 16), dweight=(F32, 4, 2)),
+    "csr5_grouped_gemm_dx": dict(dy=(BF16, 6, 16), w=(BF16, 2, 16, 32), offset=(I32, 3), dx=(BF16, 6, 32)),
+    "csr5_grouped_gemm_dw": dict(dy=(BF16, 6, 16), x=(BF16, 6, 32), offset=(I32, 3), dw=(BF16, 2, 16, 32), source=(I32, 6)),
+    "csr5_rmsnorm_backward": dict(h=(BF16, 6, 32), gain=(BF16, 32), rstd=(F32, 6), dy=(BF16, 6, 32), dh=(BF16, 6, 32), dgain=(F32, 32), workspace=(U8, 4096),
+                                  residual_grad=(BF16, 6, 32)),
+}
+
+
+class Stream:
+    cuda_stream = 4096
+
+    def __init__(self, gpu):
+        self.device_index = gpu
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_tensors_of_several_gpus_are_refused(native, call):
+    shapes, _, arguments = CALLS[call]
+    here = tensors(**shapes)
+    for name, shape in shapes.items():
+        with pytest.raises(ValueError, match="GPU"):
+            getattr(native, call)(*arguments(here | tensors("cuda:1", **{name: shape})), None)
+    with pytest.raises(ValueError, match="stream is one of GPU 1"):
+        getattr(native, call)(*arguments(here), Stream(1))
+    assert getattr(native, call)(*arguments(here), Stream(0)) == B.CSR5_EINVAL          # tensors without memory: the library's own refusal
+    assert getattr(native, call)(*arguments(here), 4096) == B.CSR5_EINVAL
+
+
+@pytest.mark.parametrize("call", BACKWARD)
+def test_tensors_of_several_gpus_are_refused_backward(call):
+    shapes = BACKWARD[call]
+    here, run = tensors(**shapes), getattr(B, call)
+    for name, shape in shapes.items():
+        with pytest.raises(ValueError, match="GPU"):
+            run(**(here | tensors("cuda:1", **{name: shape})), stream=Stream(0))
+    with pytest.raises(ValueError, match="stream is one of GPU 1"):
+        run(**here, stream=Stream(1))
+    assert run(**here, stream=Stream(0), check=False) == B.CSR5_EINVAL
