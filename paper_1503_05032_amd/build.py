@@ -1,7 +1,8 @@
-"""Builds libcsr5.so (HIP, gfx950) in-tree with hipcc, no torch involved, and next to it _marshal.so, which takes torch's
-tensors apart for the calls of a serving step."""
+"""Builds libcsr5.so (HIP, gfx950) in-tree with hipcc, no torch involved, and next to it, where torch is installed,
+_marshal.so, which takes torch's tensors apart for the calls of a serving step."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -32,7 +33,29 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
+def host_compiler() -> str:
+    """A C++ compiler: the environment's, g++, or the one that hipcc itself uses."""
+    near = os.path.join(os.path.dirname(os.path.realpath(hipcc())), "..", "lib", "llvm", "bin", "clang++")
+    for c in (os.environ.get("CXX"), shutil.which("g++"), near):
+        if c and shutil.which(c):
+            return c
+    raise RuntimeError("no C++ compiler found: set CXX")
+
+
+def torch_there() -> bool:
+    """Without torch nobody has tensors to take apart: the library alone is the build."""
+    return importlib.util.find_spec("torch") is not None
+
+
 def build(verbose: bool = True, extra=()) -> str:
+    """The library, and _marshal.so where there is torch to build it with."""
+    build_library(verbose, extra)
+    if torch_there():
+        build_marshal(verbose)
+    return OUT
+
+
+def build_library(verbose: bool = True, extra=()) -> str:
     """Compiles every source, side by side, and links them."""
     tmp = OUT + f".tmp{os.getpid()}"
     objects = [f"{tmp}.{os.path.basename(src)}.o" for src in SRC]
@@ -54,7 +77,6 @@ def build(verbose: bool = True, extra=()) -> str:
         for obj in objects:
             if os.path.exists(obj):
                 os.remove(obj)
-    build_marshal(verbose)
     return OUT
 
 
@@ -65,7 +87,7 @@ def build_marshal(verbose: bool = True) -> str:
     import torch
     t = os.path.dirname(torch.__file__)
     tmp = MARSHAL + f".tmp{os.getpid()}"
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+    cmd = [host_compiler(), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-I", INC, "-I", os.path.join(t, "include"), "-I", os.path.join(t, "include", "torch", "csrc", "api", "include"),
            "-I", sysconfig.get_paths()["include"], MARSHAL_SRC, "-o", tmp, "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
            "-L", PKG, "-l:libcsr5.so", "-Wl,-rpath,$ORIGIN"]
@@ -77,11 +99,11 @@ def build_marshal(verbose: bool = True) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(OUT) or not os.path.exists(MARSHAL):
-        return True
-    t = min(os.path.getmtime(OUT), os.path.getmtime(MARSHAL))
-    deps = SRC + HEADERS + [MARSHAL_SRC] + [os.path.join(INC, "csr5.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+    header = [os.path.join(INC, "csr5.h")]
+    made = {OUT: SRC + HEADERS + header}
+    if torch_there():
+        made[MARSHAL] = [MARSHAL_SRC] + header
+    return any(not os.path.exists(out) or any(os.path.getmtime(d) > os.path.getmtime(out) for d in deps) for out, deps in made.items())
 
 
 if __name__ == "__main__":
