@@ -641,7 +641,7 @@ int csr5_combine(int32_t tokens, int32_t k, int32_t rows, int32_t n, int dtype, 
         auto go = [&](auto v) {
             k_combine<T, decltype(v)::value><<<grid, 256, 0, s>>>(tokens, k, rows, n, static_cast<const T*>(z), ldz, place, weight, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy);
         };
-        if (aligned(z, ldz, size, 8 * size) && aligned(y, ldy, size, 8 * size) && (!residual || aligned(residual, ldr, size, 8 * size))) go(std::true_type());
+        if (aligned(z, ldz, size, 16) && aligned(y, ldy, size, 16) && (!residual || aligned(residual, ldr, size, 16))) go(std::true_type());
         else go(std::false_type());
         return launched();
     });
@@ -662,7 +662,7 @@ int csr5_combine_backward(int32_t tokens, int32_t k, int32_t rows, int32_t n, in
         auto go = [&](auto v) {
             k_combine_back<T, decltype(v)::value><<<workgroups(divide_up(pairs, 4)), 256, 0, s>>>(pairs, k, rows, n, static_cast<const T*>(dy), lddy, static_cast<const T*>(z), ldz, place, weight, static_cast<T*>(dz), lddz, dweight);
         };
-        if (aligned(z, ldz, size, 8 * size) && aligned(dy, lddy, size, 8 * size) && aligned(dz, lddz, size, 8 * size)) go(std::true_type());
+        if (aligned(z, ldz, size, 16) && aligned(dy, lddy, size, 16) && aligned(dz, lddz, size, 16)) go(std::true_type());
         else go(std::false_type());
         return launched();
     });
@@ -688,7 +688,7 @@ int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const 
             if (block_rows == 1) go(std::integral_constant<int, 1>(), v);
             else go(std::integral_constant<int, CSR5_F8_BLOCK>(), v);
         };
-        if (aligned(x, ldx, size, 8 * size) && aligned(q, ldq, 1, 8)) by(std::true_type());
+        if (aligned(x, ldx, size, 16) && aligned(q, ldq, 1, 8)) by(std::true_type());
         else by(std::false_type());
         return launched();
     });
@@ -709,7 +709,7 @@ int csr5_rmsnorm(int32_t rows, int32_t n, int dtype, const void* x, int64_t ldx,
         using T = decltype(zero);
         const NormArgs<T> a{rows, n, static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<const T*>(gain), ldx, ldr, eps,
                             static_cast<T*>(h), static_cast<T*>(y), ldh, ldy, q, ldq, scale, scale_row, scale_block, rstd};
-        const size_t wide = 8 * size;
+        const size_t wide = 16;
         const bool v = aligned(x, ldx, size, wide) && (!residual || aligned(residual, ldr, size, wide)) && aligned(gain, 0, size, wide) &&
                        (!h || aligned(h, ldh, size, wide)) && (!y || aligned(y, ldy, size, wide)) && (!q || aligned(q, ldq, 1, 8));
         norm_shape(n, [&](int threads, auto nv) {
@@ -744,7 +744,7 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void* h, int
         using T = decltype(zero);
         const NormBackArgs<T> a{rows, n, static_cast<const T*>(h), static_cast<const T*>(gain), static_cast<const T*>(dy), static_cast<const T*>(residual_grad),
                                 ldh, lddy, ldrg, rstd, static_cast<T*>(dh), lddh, dgain ? static_cast<float*>(workspace) : nullptr};
-        const size_t wide = 8 * size;
+        const size_t wide = 16;
         const bool v = aligned(h, ldh, size, wide) && aligned(dy, lddy, size, wide) && aligned(dh, lddh, size, wide) && aligned(gain, 0, size, wide) &&
                        (!residual_grad || aligned(residual_grad, ldrg, size, wide));
         if (rows > 0)

@@ -15,12 +15,18 @@ template <typename T, int N> using vec = T __attribute__((ext_vector_type(N)));
 constexpr float F8_MAX = 448.f;             // largest finite e4m3 value
 constexpr float F8_SCALE_MIN = 0x1p-126f;   // the smallest normal float: its reciprocal is finite
 
-// N values at p, of which the first `have` exist; the others are 0.  VEC: p is aligned to N values.
+// Values of a load or a store: as many of N as 16 bytes hold.
+template <typename T, int N> constexpr int PIECE = N * sizeof(T) <= 16 ? N : 16 / int(sizeof(T));
+
+// N values at p, of which the first `have` exist; the others are 0.  VEC: p is aligned to N values, or to 16 bytes where they are more.
 template <int N, bool VEC, typename T> __device__ __forceinline__ void load_values(const T* p, int have, float (&out)[N]) {
     if (VEC && have >= N) {
-        const vec<T, N> v = *reinterpret_cast<const vec<T, N>*>(p);
 #pragma unroll
-        for (int i = 0; i < N; i++) out[i] = float(v[i]);
+        for (int i = 0; i < N; i += PIECE<T, N>) {
+            const vec<T, PIECE<T, N>> v = *reinterpret_cast<const vec<T, PIECE<T, N>>*>(p + i);
+#pragma unroll
+            for (int j = 0; j < PIECE<T, N>; j++) out[i + j] = float(v[j]);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < N; i++) out[i] = i < have ? float(p[i]) : 0.f;
@@ -29,20 +35,31 @@ template <int N, bool VEC, typename T> __device__ __forceinline__ void load_valu
 
 // Eight of them as they are.
 template <bool VEC, typename T> __device__ __forceinline__ vec<T, 8> eight_values(const T* p, int have) {
-    if (VEC && have >= 8) return *reinterpret_cast<const vec<T, 8>*>(p);
     vec<T, 8> v;
+    if (VEC && have >= 8) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < have ? p[i] : T(0.f);
+        for (int i = 0; i < 8; i += PIECE<T, 8>) {
+            const vec<T, PIECE<T, 8>> part = *reinterpret_cast<const vec<T, PIECE<T, 8>>*>(p + i);
+#pragma unroll
+            for (int j = 0; j < PIECE<T, 8>; j++) v[i + j] = part[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < have ? p[i] : T(0.f);
+    }
     return v;
 }
 
 // Rounds to the nearest T, ties to even.
 template <int N, bool VEC, typename T> __device__ __forceinline__ void store_values(T* p, int have, const float (&in)[N]) {
     if (VEC && have >= N) {
-        vec<T, N> v;
 #pragma unroll
-        for (int i = 0; i < N; i++) v[i] = T(in[i]);
-        *reinterpret_cast<vec<T, N>*>(p) = v;
+        for (int i = 0; i < N; i += PIECE<T, N>) {
+            vec<T, PIECE<T, N>> v;
+#pragma unroll
+            for (int j = 0; j < PIECE<T, N>; j++) v[j] = T(in[i + j]);
+            *reinterpret_cast<vec<T, PIECE<T, N>>*>(p + i) = v;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < N; i++)
