@@ -413,12 +413,13 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
  * Matrices are row-major with a row stride in elements (ld..., at least the number
  * of columns): rows may be views into wider arrays, and no address has to be aligned to
  * more than its element; 16-byte aligned addresses and rows (ld * element size a
- * multiple of 16) get the fast kernels.  dtype names the 16- or 32-bit type of a
+ * multiple of 16; products also need k, in dx and dw n too, in whole 16 bytes, and y at
+ * four values) get the fast kernels.  dtype names the 16- or 32-bit type of a
  * call's matrices; 8-bit values are OCP e4m3 (finite, largest 448) in uint8_t.
  * Sums, softmax, norms and scales are held in 32 bits, and a result is rounded
  * once (16-bit results of products in 8 bits: see csr5_gemm_f8).  Every call only enqueues kernels on the stream, allocates nothing, waits for
  * nothing, and may be captured into a graph.  Results do not depend on timing: no call adds
- * atomically.  Outputs must not overlap inputs unless a comment says that they may.
+ * values atomically.  Outputs must not overlap inputs unless a comment says that they may.
  *
  * Whatever offset, source and place hold, no kernel leaves the arrays: offsets are
  * clamped to [0, rows], a group that ends before it begins is empty (where groups overlap,
@@ -513,9 +514,11 @@ int csr5_grouped_gemm_dw(int32_t groups, int32_t rows, int32_t n, int32_t k, int
 /*
  * 8-bit values with a scale for each block of block_rows x 128 values (block_rows 1 or
  * 128; the blocks at the right and lower edge may be smaller):
- *   scale = max(max|x| / 448, 2^-126),   q = x / scale, rounded to the nearest e4m3
- * The scale of block (i, b) is at scale[i*scale_row + b*scale_block].  A block with an
- * infinity or a NaN has such a scale.  x[rows][n] in dtype (BF16, F16, F32).
+ *   scale = max(max|x| / 448, 2^-126),   q = x / (that before its rounding to float),
+ * rounded to the nearest e4m3, ties to even.  (For 16-bit x this is 448 x / max|x| rounded
+ * once; x / scale by the float in scale[] is another value in near-ties, one in a thousand
+ * for BF16.)  The scale of block (i, b) is at scale[i*scale_row + b*scale_block].  A block
+ * with an infinity or a NaN has such a scale, and its q mean nothing.  x[rows][n] in dtype (BF16, F16, F32).
  */
 int csr5_quantise(int32_t rows, int32_t n, int32_t block_rows, int dtype, const void *x, int64_t ldx,
                   uint8_t *q, int64_t ldq, float *scale, int64_t scale_row, int64_t scale_block,

@@ -107,8 +107,9 @@ template <typename T, int NV, bool VEC> __global__ __launch_bounds__(NORM_THREAD
 }
 
 // Its gradients.  A workgroup takes rows by turns and keeps its share of the gain's gradient in registers; the shares
-// go to the workspace and are added up by k_columns in a fixed order.  Bound by memory: 32768 x 4096 in bf16 with the
-// residual's gradient 198 us, 5.4 TB/s.
+// go to the workspace and are added up by k_columns in a fixed order.  Bound by memory up to n = 16384 in 16 bits and 8192 in 32:
+// 32768 x 4096 in bf16 with the residual's gradient 194 us, 5.5 TB/s.  Longer rows do not fit the registers, and what is spilled
+// holds them up: 4096 x 32768 in bf16 892 us, 1.2 TB/s; in float32 4096 x 16384 252, 4.3, and x 32768 1749, 1.2.
 template <typename T> struct NormBackArgs {
     int rows, n;
     const T *h, *gain, *dy, *residual_grad;
@@ -261,14 +262,15 @@ __global__ __launch_bounds__(256) void k_quantise(int rows, int n, const T* x, i
 // The router.  A token's logits lie over LANES lanes, V neighbouring ones in each: 16 lanes, four tokens to a wavefront, for
 // up to 256 experts and k up to 16, otherwise all 64.  k rounds of: largest of the token, who has it first, take it out.
 // Logits are compared as whole numbers in the floats' order, 0 for what is never chosen (-inf, NaN); 16-bit ones carry their
-// expert in the low half, so that the largest is the lowest expert's of the largest and names it.  Bound by instructions:
-// 256 experts in 16 bits take about 45 a round, for four tokens (a wavefront per token: 25 for one; 32768 tokens, 8 of 256
-// experts, took 23 us).
+// expert in the low half, so that the largest is the lowest expert's of the largest and names it.  256 experts in 16 bits take
+// about 45 instructions a round, for four tokens (a wavefront per token: 25 for one; 32768 tokens, 8 of 256 experts, took 23 us).
 //
 // Grouping is a counting sort, stable by pair: every workgroup counts the experts of its chunk of tokens; then each
 // adds up, per expert, the counts of all chunks and of those before it, and hands out rows to its pairs in order.
-// Tokens of one chunk: one workgroup does both.  Both kernels wait more than they read or write: 32768 tokens, 8 of 256 in bf16
-// (20 MB, 4 us at a copy's rate) take 21 us.
+// Tokens of one chunk: one workgroup does both.  32768 tokens, 8 of 256 in bf16 (20 MB, 4 us at a copy's rate) take 21 us: about
+// 13 to choose, of which the rounds' instructions are about half and waiting the rest (four wavefronts to a SIMD, two turns each, of
+// data-parallel moves that wait for one another), and 8 to group, where every workgroup reads the counts of all chunks (64 MB from
+// the L2).
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int ROUTE_CHUNKS = 256;       // at most, each a workgroup
 constexpr int ROUTE_WAVES = 16;

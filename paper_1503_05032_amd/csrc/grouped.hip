@@ -696,8 +696,9 @@ __global__ __launch_bounds__(WI * WJ * 64, BI * BJ / (WI * WJ) < 64 * 64 ? 4 : 2
 // are read beside the last two rows.  From there on the loads of w s + 2 are asked for, then, XRING = 3, of x s + 3: that
 // half of the loads has two steps to land.  W1: a scale per row of w.
 // Bound by power as above and by what a wavefront issues beside the products (four adds for each): 8192^3 483 us, 2275
-// TFLOP/s, the matrix pipe busy 55% of the cycles; without loads 2530 TFLOP/s, without LDS reads 2880.  A scale per row of w
-// costs a fifth more.  Short depths pay for their tiles: 275 GFLOP in 64 groups of 512 rows, 2048 x 2048, 203 us.
+// TFLOP/s, the matrix pipe busy 55% of the cycles (on another card 528; 1111 with results in 32 bits); without loads 2530
+// TFLOP/s, without LDS reads 2880.  A scale per row of w costs a seventh more (603 for the 528), for the registers and LDS reads of
+// four scales instead of one.  Short depths pay for their tiles: 275 GFLOP in 64 groups of 512 rows, 2048 x 2048, 191 to 203 us.
 template <typename Y, int BI, int BJ, int WI, int WJ, int XRING, bool W1>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_product_f8(Product a, int row_tiles, int col_tiles) {
     constexpr int WAVES = WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16;

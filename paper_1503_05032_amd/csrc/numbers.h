@@ -19,6 +19,8 @@ constexpr float F8_SCALE_MIN = 0x1p-126f;   // the smallest normal float: its re
 template <typename T, int N> constexpr int PIECE = N * sizeof(T) <= 16 ? N : 16 / int(sizeof(T));
 
 // N values at p, of which the first `have` exist; the others are 0.  VEC: p is aligned to N values, or to 16 bytes where they are more.
+// (Value by value each load is waited for: 8192 x 4096 in bf16, norm 148 us against 40, its gradients 154, 52, quantisation 48, 21,
+// combination of 4 rows 197, 78, its gradients 402, 127.)
 template <int N, bool VEC, typename T> __device__ __forceinline__ void load_values(const T* p, int have, float (&out)[N]) {
     if (VEC && have >= N) {
 #pragma unroll
