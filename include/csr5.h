@@ -426,7 +426,8 @@ int csr5_baseline_csr_vector(int32_t m, int32_t nnz, const int32_t *row_ptr, con
  * each value of a row of both is either's or left as it is, by timing), a source
  * outside [0, x_rows) is a row of zeros and a place outside [0, rows) is no row.
  * A size of 0 is fine: such a call writes what is left to write (or nothing).  One of
- * 2^31 - 2^16 or more is CSR5_ERANGE where a kernel counts in 32 bits.
+ * 2^31 - 2^16 or more is CSR5_ERANGE where a kernel counts in 32 bits, and so is a product
+ * whose groups, rows and columns would take 2^32 threads (from some 10^6 groups on).
  * ========================================================================== */
 #define CSR5_DTYPE_BF16 2
 #define CSR5_DTYPE_F16 3

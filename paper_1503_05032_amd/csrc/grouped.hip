@@ -919,10 +919,13 @@ template <typename T, typename Y, int TI, int TJ, bool W1> __global__ __launch_b
 // ---------------------------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------------------------
+// A launch has fewer than 2^32 threads.
+bool threads_fit(int64_t groups, int threads) { return groups * threads <= int64_t(UINT32_MAX); }
+
 template <typename T, typename Y, int OP> int launch_plain(const Product& a, hipStream_t s) {
     const int64_t cols = divide_up(a.cols, PLAIN_TILE);
     const int64_t tiles = OP == DW ? int64_t(a.groups) * divide_up(a.out_rows, PLAIN_TILE) : int64_t(divide_up(a.rows, PLAIN_TILE)) + (a.offset ? a.groups : 0);
-    if (tiles * cols > INT32_MAX) return CSR5_ERANGE;
+    if (!threads_fit(tiles * cols, 256)) return CSR5_ERANGE;
     k_product_plain<T, Y, OP><<<uint32_t(tiles * cols), 256, 0, s>>>(a);
     return launched();
 }
@@ -931,7 +934,7 @@ template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int la
     const int64_t cols = divide_up(a.cols, BJ);
     const int64_t rows = OP == DW ? int64_t(divide_up(a.out_rows, BI)) : int64_t(divide_up(a.rows, BI)) + (a.offset ? a.groups : 0);
     const int64_t grid = (rows * cols + 7) / 8 * 8 * (OP == DW ? a.groups : 1);
-    if (grid > INT32_MAX) return CSR5_ERANGE;
+    if (!threads_fit(grid, WI * WJ * 64)) return CSR5_ERANGE;
     if constexpr (is_f8<T>) {
         constexpr int XRING = BI > 128 ? 3 : 2;         // 128 x 128: two workgroups on a CU
         if (a.w_rows == 1) k_product_f8<Y, BI, BJ, WI, WJ, XRING, true><<<uint32_t(grid), WI * WJ * 64, 0, s>>>(a, int(rows), int(cols));
@@ -944,7 +947,7 @@ template <typename T, typename Y, int OP, int BI, int BJ, int WI, int WJ> int la
 
 template <typename T, typename Y, int TI, int TJ> int launch_few(const Product& a, hipStream_t s) {
     const int64_t cols = divide_up(a.cols, 16 * TJ), rows = int64_t(divide_up(a.rows, 16 * TI)) + (a.offset ? a.groups : 0);
-    if (rows * cols > INT32_MAX) return CSR5_ERANGE;
+    if (!threads_fit(rows * cols, FEW_WAVES * 64)) return CSR5_ERANGE;
     if (is_f8<T> && a.w_rows == 1) k_product_few<T, Y, TI, TJ, is_f8<T>><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
     else k_product_few<T, Y, TI, TJ, false><<<uint32_t(rows * cols), FEW_WAVES * 64, 0, s>>>(a, int(cols));
     return launched();
