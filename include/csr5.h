@@ -582,6 +582,118 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void *h, int
                           int64_t ldrg, void *dh, int64_t lddh, float *dgain, void *workspace,
                           size_t workspace_bytes, void *hip_stream);
 
+/* ==========================================================================
+ * 6. The attention beside a layer of experts: packed sequences, a paged cache of
+ *    keys and values, rotary positions.  Sequences lie one after the other, with a row
+ *    pointer: rows [offset[s], offset[s+1]) are those of sequence s, as in CSR; the
+ *    cache is a sparse matrix of requests x tokens, whose table of pages names where
+ *    each block of `page` tokens is.
+ *
+ * What section 5 says of streams, graphs, sums in 32 bits, timing and addresses holds here.  A
+ * row has `heads` heads of d neighbouring values, at any strides (in elements); query head h
+ * goes with head h / (heads / kv_heads) of keys and values.  16-byte aligned addresses, strides of a
+ * multiple of 16 bytes and d in whole 16 bytes get the fast kernels.  An output must not overlap itself
+ * (CSR5_EINVAL).  Offsets are clamped to [0, rows] and lengths to what the table holds; a page outside
+ * [0, pages) is one of zeros where it is read, and none where it would be written.
+ * ========================================================================== */
+#define CSR5_ATTENTION_MAX_D 128
+#define CSR5_ATTENTION_MAX_HEADS 65535
+#define CSR5_ROTARY_MAX_D 512
+
+typedef struct { /* value c of head h of row i is at p[i*row + h*head + c] */
+    void *p;
+    int64_t row, head;
+} csr5_heads_t;
+typedef struct { /* value c of head h of token i of a page is at p[number*page + i*row + h*head + c] */
+    void *p;
+    int64_t page, row, head;
+} csr5_cache_t;
+
+/*
+ * The pages of one step of serving.  Request r has length[r] tokens in the cache, in the pages
+ * table[r][0 .. ceil(length / page)), and brings fresh[r] new ones, or is over (fresh[r] < 0).
+ * Free pages are a ring: pool[(state[0] + i) % ring], 0 <= i < state[1].
+ *   offset   int32[requests+1]  row pointer of the new tokens
+ *   position int32[tokens]      of each new token in its request; 0 past the last one
+ *   slot     int32[tokens]      where it goes in the cache: number of the page * page + place in it; -1
+ *                               past the last one and where its request gets no pages
+ *   length_out int32[requests]  length + fresh; length where the request gets no pages; 0 where it is over
+ *   state_out  int32[2]         the ring's free pages afterwards
+ * Requests take pages in their order: one that needs some gets them if all that it and those before it
+ * need are free (one that would pass the table's width needs none and gets none; one that needs none is served).  New pages are
+ * written into table, whose other entries stay.  The pages of a request that is over go behind the last free one, for later
+ * calls; its row of the table stays.  tokens: room in position and slot; of more new tokens than that the first are
+ * written, and offset ends at tokens.  page is a power of two.  pool and table are the only arrays that are read and written; with
+ * the same state a call gives the same again.  A length below 0 is 0, one past the table its width.
+ */
+int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int32_t tokens, const int32_t *fresh,
+               const int32_t *length, int32_t *table, int64_t ldt, int32_t *pool, const int32_t *state, int32_t *offset,
+               int32_t *position, int32_t *slot, int32_t *length_out, int32_t *state_out, void *hip_stream);
+
+/*
+ * Rotary positions: values a, b of pair i of a head become a cos - b sin, a sin + b cos of the angle
+ *   position[axis[i]][token] * frequency[i]
+ * (its negative with inverse != 0: the gradient), the product and its reduction in 64 bits.  Pair i < rot / 2 is
+ * (i, i + rot / 2), or (2i, 2i + 1) with interleaved != 0; values from rot on stay as they are.  axis NULL: all of axis 0;
+ * a pair whose axis is outside [0, axes) is not turned.
+ *   position int32[axes][tokens], row stride ldp;  frequency float[rot/2];  axis int32[rot/2]
+ *   q, q_out [tokens][heads][d];  k, k_out [tokens][kv_heads][d] in dtype (BF16, F16, F32)
+ * q_out may be q, and k_out k (with the same strides).  Instead of k_out, or beside it (k_out.p may be NULL),
+ * k goes turned, and v [tokens][kv_heads][d] as it is, to slot[token] of k_cache and v_cache: page slot / page, token slot % page;
+ * a slot outside [0, pages * page) is none.  slot NULL: no cache.  Two tokens with one slot leave either's values there.
+ */
+int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int32_t rot, int dtype, int32_t axes,
+                const int32_t *position, int64_t ldp, const float *frequency, const int32_t *axis, int interleaved,
+                int inverse, csr5_heads_t q, csr5_heads_t q_out, csr5_heads_t k, csr5_heads_t k_out, csr5_heads_t v,
+                const int32_t *slot, int32_t pages, int32_t page, csr5_cache_t k_cache, csr5_cache_t v_cache,
+                void *hip_stream);
+
+/*
+ * Attention over packed sequences: for row i of a sequence of m queries and n keys, and each head,
+ *   out = sum_j p_j v_j,  p_j = exp(scale q.k_j - lse),  lse = log sum_j exp(scale q.k_j)
+ * over all its keys, or with causal != 0 those j <= i + n - m (the last query sees every key).  A row that sees
+ * no key has out 0 and lse -inf.  Rows in no sequence are left as they are.
+ *   q, out [rows][heads][d]; k, v [k_rows][kv_heads][d] in dtype (BF16, F16); lse float[heads][rows], or NULL
+ * d <= CSR5_ATTENTION_MAX_D and heads <= CSR5_ATTENTION_MAX_HEADS, else CSR5_ERANGE; heads is a multiple
+ * of kv_heads, scale positive and finite.
+ * Softmax statistics and sums are held in 32 bits; p is rounded to dtype, relative to the largest so far, before it is
+ * multiplied by v.
+ */
+int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype,
+                   const int32_t *q_offset, const int32_t *k_offset, float scale, int causal, csr5_heads_t q,
+                   csr5_heads_t k, csr5_heads_t v, csr5_heads_t out, float *lse, void *hip_stream);
+
+/*
+ * Its gradients, from dout (of out), out and lse:
+ *   ds_ij = p_ij (dout_i . v_j - dout_i . out_i),  dq_i = scale sum_j ds_ij k_j,
+ *   dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
+ * with the sums of dk and dv over the query heads that share them.  p and ds are rounded to dtype before they are multiplied.
+ * Rows in no sequence are left as they are.  workspace: csr5_attention_backward_workspace_bytes bytes, free again after the call.
+ */
+size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads);
+int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d,
+                            int dtype, const int32_t *q_offset, const int32_t *k_offset, float scale, int causal,
+                            csr5_heads_t dout, csr5_heads_t q, csr5_heads_t k, csr5_heads_t v, csr5_heads_t out,
+                            const float *lse, csr5_heads_t dq, csr5_heads_t dk, csr5_heads_t dv, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention of new tokens over a paged cache, as csr5_attention with causal: request s has length[s] keys, its new tokens'
+ * among them (csr5_rotary has written them), in the pages table[s][0 .. width), and its rows [q_offset[s], q_offset[s+1]) of q are
+ * those of the last tokens.  One token for each request, or chunks, or both side by side.
+ *   k_cache, v_cache [pages][page][kv_heads][d] in dtype, page a power of two; table int32[sequences][width], row stride ldt
+ * A length is at most width * page; the work is split over the keys where there are few rows, by what the
+ * table could hold.  workspace: csr5_attention_paged_workspace_bytes bytes with max_length = width * page, free again after the call
+ * (0: may be NULL).
+ */
+size_t csr5_attention_paged_workspace_bytes(int32_t rows, int32_t heads, int32_t kv_heads, int32_t d, int32_t sequences,
+                                            int64_t max_length);
+int csr5_attention_paged(int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype,
+                         const int32_t *q_offset, const int32_t *length, const int32_t *table, int32_t width, int64_t ldt,
+                         int32_t pages, int32_t page, float scale, csr5_heads_t q, csr5_cache_t k_cache,
+                         csr5_cache_t v_cache, csr5_heads_t out, float *lse, void *workspace, size_t workspace_bytes,
+                         void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

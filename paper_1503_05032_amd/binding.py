@@ -42,6 +42,8 @@ SYMBOLS = [
     "csr5_route_workspace_bytes", "csr5_route", "csr5_route_backward", "csr5_combine", "csr5_combine_backward",
     "csr5_grouped_gemm", "csr5_grouped_gemm_dx", "csr5_grouped_gemm_dw", "csr5_quantise", "csr5_gemm_f8",
     "csr5_grouped_gemm_f8", "csr5_rmsnorm", "csr5_rmsnorm_workspace_bytes", "csr5_rmsnorm_backward",
+    "csr5_pages", "csr5_rotary", "csr5_attention", "csr5_attention_backward_workspace_bytes", "csr5_attention_backward",
+    "csr5_attention_paged_workspace_bytes", "csr5_attention_paged",
 ]
 
 
@@ -130,6 +132,14 @@ def load():
         "csr5_rmsnorm": [i32, i32, C.c_int, vp, i64, vp, i64, vp, C.c_float, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, vp],
         "csr5_rmsnorm_backward": [i32, i32, C.c_int, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp],
     }
+    heads, cache = Heads, Cache
+    layer.update({
+        "csr5_pages": [i32, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp],
+        "csr5_rotary": [i32, i32, i32, i32, i32, C.c_int, i32, vp, i64, vp, vp, C.c_int, C.c_int, heads, heads, heads, heads, heads, vp, i32, i32, cache, cache, vp],
+        "csr5_attention": [i32, i32, i32, i32, i32, i32, C.c_int, vp, vp, C.c_float, C.c_int, heads, heads, heads, heads, vp, vp],
+        "csr5_attention_backward": [i32, i32, i32, i32, i32, i32, C.c_int, vp, vp, C.c_float, C.c_int, heads, heads, heads, heads, heads, vp, heads, heads, heads, vp, sz, vp],
+        "csr5_attention_paged": [i32, i32, i32, i32, i32, C.c_int, vp, vp, vp, i32, i64, i32, i32, C.c_float, heads, cache, cache, heads, vp, vp, sz, vp],
+    })
     for name, argtypes in layer.items():
         getattr(lib, name).restype = C.c_int
         getattr(lib, name).argtypes = argtypes
@@ -137,10 +147,24 @@ def load():
     lib.csr5_route_workspace_bytes.argtypes = [i32, i32, i32]
     lib.csr5_rmsnorm_workspace_bytes.restype = sz
     lib.csr5_rmsnorm_workspace_bytes.argtypes = [i32, i32]
+    lib.csr5_attention_backward_workspace_bytes.restype = sz
+    lib.csr5_attention_backward_workspace_bytes.argtypes = [i32, i32]
+    lib.csr5_attention_paged_workspace_bytes.restype = sz
+    lib.csr5_attention_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i64]
     lib.csr5_strerror.restype = C.c_char_p
     lib.csr5_strerror.argtypes = [C.c_int]
     _lib = lib
     return lib
+
+
+class Heads(C.Structure):
+    """Rows of heads: csr5_heads_t."""
+    _fields_ = [("p", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class Cache(C.Structure):
+    """Pages of rows of heads: csr5_cache_t."""
+    _fields_ = [("p", C.c_void_p), ("page", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
 
 
 def _ptr(t):
@@ -621,3 +645,53 @@ def csr5_rmsnorm_backward(h, gain, rstd, dy, dh, dgain=None, workspace=None, res
                                              *((None, 0) if residual_grad is None else _matrix(residual_grad, dt, rows, n, "residual_grad")),
                                              *_matrix(dh, dt, rows, n, "dh"), _arr(dgain, ["f32"], n, "dgain"), *_space(workspace),
                                              _stream_of(stream, h, gain, rstd, dy, dh, dgain, workspace, residual_grad)), "csr5_rmsnorm_backward", check)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# The attention beside a layer of experts (section 6 of the header).  Queries, keys and values are 3-D tensors [rows, heads,
+# d] at any strides whose heads are contiguous (views of one wide product, say), caches 4-D ones [pages, page, kv_heads, d].
+# ---------------------------------------------------------------------------------------------------------------------
+def csr5_pages(fresh, length, table, pool, state, page, offset, position, slot, length_out, state_out, stream=None, check=True):
+    """The pages of a step of serving.  From fresh (new tokens; below 0: over) and length (cached ones) [requests], writes
+    offset [requests + 1], position and slot [tokens], length_out [requests] and state_out [2], new pages into table
+    [requests, width], and pages of requests that are over into the ring `pool`, whose free ones state [2] (first, count)
+    names; all int32.  `page` tokens to a page, a power of two."""
+    return _chk(_native().pages(fresh, length, table, pool, state, page, offset, position, slot, length_out, state_out, stream), "csr5_pages", check)
+
+
+def csr5_rotary(q, k, position, frequency, q_out, k_out=None, axis=None, interleaved=False, inverse=False, v=None, slot=None, k_cache=None, v_cache=None, stream=None, check=True):
+    """q [tokens, heads, d] and k [tokens, kv_heads, d] (or None) turned by position[axis[i]] * frequency[i] for pair i, backwards
+    with `inverse` (the gradient), to q_out, and to k_out or, with v as it is, to slot[token] of k_cache and v_cache [pages, page, kv_heads, d].
+    position int32 [tokens] or [axes, tokens], frequency float32 [rot / 2], axis int32 [rot / 2] (or None: all of axis 0), slot int32 [tokens]."""
+    return _chk(_native().rotary(q, k, position, frequency, q_out, k_out, axis, interleaved, inverse, v, slot, k_cache, v_cache, stream), "csr5_rotary", check)
+
+
+def _scale(scale, q):
+    return max(q.shape[-1], 1) ** -0.5 if scale is None else scale
+
+
+def csr5_attention(q, k, v, q_offset, k_offset, out, lse=None, scale=None, causal=True, stream=None, check=True):
+    """Attention over packed sequences: q and out [rows, heads, d], k and v [k_rows, kv_heads, d], q_offset and k_offset int32
+    [sequences + 1], lse float32 [heads, rows]; scale: d^-0.5 where it is None."""
+    return _chk(_native().attention(q, k, v, q_offset, k_offset, out, lse, _scale(scale, q), causal, stream), "csr5_attention", check)
+
+
+def csr5_attention_backward_workspace_bytes(rows, heads):
+    return int(load().csr5_attention_backward_workspace_bytes(int(rows), int(heads)))
+
+
+def csr5_attention_backward(dout, q, k, v, out, lse, q_offset, k_offset, dq, dk, dv, workspace, scale=None, causal=True, stream=None, check=True):
+    """Gradients dq, dk and dv of csr5_attention from dout, out and lse; `workspace` (uint8) has
+    csr5_attention_backward_workspace_bytes bytes."""
+    return _chk(_native().attention_backward(dout, q, k, v, out, lse, q_offset, k_offset, dq, dk, dv, workspace, _scale(scale, q), causal, stream), "csr5_attention_backward", check)
+
+
+def csr5_attention_paged_workspace_bytes(rows, heads, kv_heads, d, sequences, max_length):
+    return int(load().csr5_attention_paged_workspace_bytes(int(rows), int(heads), int(kv_heads), int(d), int(sequences), int(max_length)))
+
+
+def csr5_attention_paged(q, k_cache, v_cache, q_offset, length, table, out, workspace=None, lse=None, scale=None, stream=None, check=True):
+    """Causal attention of each request's last tokens, q and out [rows, heads, d], over length[s] tokens in the pages table[s] of
+    k_cache and v_cache [pages, page, kv_heads, d]; `workspace` (uint8) has csr5_attention_paged_workspace_bytes bytes, with
+    max_length = table.shape[1] * page."""
+    return _chk(_native().attention_paged(q, k_cache, v_cache, q_offset, length, table, out, workspace, lse, _scale(scale, q), stream), "csr5_attention_paged", check)

@@ -1,4 +1,5 @@
-// Python's side of the calls of a serving step (the router, products, norm, quantisation, combination): takes tensors apart,
+// Python's side of the calls of a serving step (the router, products, norm, quantisation, combination; pages, positions, attention and its
+// gradients): takes tensors apart,
 // checks what the C library cannot see -- element types, shapes, strides, that they are on one GPU -- and calls it.  A call
 // of binding.py by ctypes takes 6 us for this, as long as the kernel of a small step; here it is under one.  Every function
 // takes its arguments by position, None for what is not given, the stream's address last, and returns the C function's
@@ -151,6 +152,44 @@ public:
         if (!t.is_contiguous()) throw Refused(std::string(name) + ": expected a contiguous GPU tensor");
         return static_cast<V*>(t.data_ptr());
     }
+    // [rows, heads, d] of `type` at any strides but that of the last dimension; rows, heads, d: given, or any: -1
+    csr5_heads_t heads(int i, const char* name, at::ScalarType type, int64_t rows, int64_t heads, int64_t d) const {
+        const at::Tensor& t = shaped(i, name, type, {rows, heads, d});
+        return {t.data_ptr(), t.stride(0), t.stride(1)};
+    }
+    // [pages, page, kv_heads, d], likewise
+    csr5_cache_t cache(int i, const char* name, at::ScalarType type, int64_t pages, int64_t page, int64_t heads, int64_t d) const {
+        const at::Tensor& t = shaped(i, name, type, {pages, page, heads, d});
+        return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+    }
+    const at::Tensor& shaped(int i, const char* name, at::ScalarType type, std::initializer_list<int64_t> want) const {
+        const at::Tensor& t = tensor(i, name);
+        if (t.scalar_type() != type) throw Refused(std::string(name) + ": expected dtype " + at::toString(type) + ", got " + at::toString(t.scalar_type()));
+        bool fits = t.dim() == int64_t(want.size());
+        int64_t k = 0;
+        for (int64_t w : want) {
+            if (!fits) break;
+            fits = w < 0 || t.size(k) == w;
+            k++;
+        }
+        if (!fits) {
+            std::string got = "(";
+            for (int64_t n : t.sizes()) got += (got.size() > 1 ? ", " : "") + std::to_string(n);
+            throw Refused(std::string(name) + ": expected shape " + shape_text(want) + ", got " + got + ")");
+        }
+        for (int64_t n : t.sizes())
+            if (n != int32_t(n)) throw Refused(std::string(name) + ": too large");
+        if (t.stride(t.dim() - 1) != 1 && t.size(t.dim() - 1) > 1) throw Refused(std::string(name) + ": expected a GPU tensor with contiguous rows");
+        return t;
+    }
+    bool truth(int i, const char* name) const {
+        const int v = PyObject_IsTrue(a_[i]);
+        if (v < 0) {
+            PyErr_Clear();
+            throw Refused(std::string(name) + ": expected a truth value");
+        }
+        return v != 0;
+    }
     int32_t* whole(int i, const char* name, int64_t least) const { return array<int32_t>(i, name, at::kInt, least); }
     float* floats(int i, const char* name, int64_t least) const { return array<float>(i, name, at::kFloat, least); }
     // the source of `rows` rows, of x_rows
@@ -265,6 +304,147 @@ int rmsnorm(const Args& a) {
     return csr5_rmsnorm(int32_t(x.rows), int32_t(x.cols), dtype, x.p, x.ld, r.p, r.ld, gain, eps, h.p, h.ld, y.p, y.ld, as<uint8_t>(q), q.ld, as<float>(s), s.ld, s.cols, rstd, stream);
 }
 
+// The type of heads: 16 bits, or 32 where `f32` allows it
+int heads_code(const at::Tensor& t, const char* name, bool f32) {
+    const int dtype = code(t.scalar_type(), name);
+    if (dtype == CSR5_DTYPE_F32 && !f32) throw Refused(std::string(name) + ": expected dtype bfloat16 or float16, got Float");
+    return dtype;
+}
+
+// A row pointer, of at least one word: the sequences
+int32_t* row_pointer(const Args& a, int i, const char* name, int64_t sequences) { return a.whole(i, name, sequences + 1); }
+int64_t sequences_of(const Args& a, int i, const char* name) {
+    const at::Tensor& t = a.tensor(i, name);
+    if (t.dim() != 1 || t.numel() < 1 || t.numel() > INT32_MAX) throw Refused(std::string(name) + ": expected a 1-D tensor of one row's begin for each sequence, and the end");
+    return t.numel() - 1;
+}
+
+// fresh, length, table, pool, state, page, offset, position, slot, length_out, state_out, stream
+int pages(const Args& a) {
+    const at::Tensor& fresh = a.tensor(0, "fresh");
+    const int64_t requests = fresh.numel();
+    if (fresh.dim() != 1 || requests > INT32_MAX) throw Refused("fresh: expected a 1-D tensor");
+    const Matrix table = a.typed(2, "table", at::kInt, requests, -1);
+    const at::Tensor &pool = a.tensor(3, "pool"), &slot = a.tensor(8, "slot");
+    if (pool.numel() > INT32_MAX) throw Refused("pool: too large");
+    if (slot.numel() > INT32_MAX) throw Refused("slot: too large");
+    const int32_t page = a.number(5, "page");
+    const int32_t *const f = a.whole(0, "fresh", requests), *const length = a.whole(1, "length", requests), *const state = a.whole(4, "state", 2);
+    int32_t *const ring = a.whole(3, "pool", 0), *const offset = a.whole(6, "offset", requests + 1), *const position = a.whole(7, "position", slot.numel());
+    int32_t *const at = a.whole(8, "slot", 0), *const length_out = a.whole(9, "length_out", requests), *const state_out = a.whole(10, "state_out", 2);
+    void* const stream = a.stream(11);
+    return csr5_pages(int32_t(requests), int32_t(table.cols), int32_t(pool.numel()), page, int32_t(slot.numel()), f, length, as<int32_t>(table), table.ld, ring, state, offset, position, at,
+                      length_out, state_out, stream);
+}
+
+// q, k, position, frequency, q_out, k_out, axis, interleaved, inverse, v, slot, k_cache, v_cache, stream
+int rotary(const Args& a) {
+    const at::Tensor &q = a.tensor(0, "q"), &at_ = a.tensor(2, "position"), &frequency = a.tensor(3, "frequency");
+    const at::ScalarType type = q.scalar_type();
+    const int dtype = heads_code(q, "q", true);
+    const csr5_heads_t hq = a.heads(0, "q", type, -1, -1, -1);
+    const int64_t tokens = q.size(0), heads = q.size(1), d = q.size(2), rot = 2 * frequency.numel();
+    if (rot > d) throw Refused("frequency: expected at most " + std::to_string(d / 2) + " values, got " + std::to_string(frequency.numel()));
+    int64_t axes = 1, ldp = tokens;
+    if (at_.dim() == 2) {
+        const Matrix m = a.typed(2, "position", at::kInt, -1, tokens);
+        axes = m.rows, ldp = m.ld;
+    }
+    const int32_t* const position = at_.dim() == 2 ? static_cast<int32_t*>(at_.data_ptr()) : a.whole(2, "position", tokens);
+    const float* const f = a.floats(3, "frequency", 0);
+    const csr5_heads_t q_out = a.heads(4, "q_out", type, tokens, heads, d);
+    csr5_heads_t k{}, k_out{}, v{};
+    csr5_cache_t k_cache{}, v_cache{};
+    int64_t kv_heads = 0, n_pages = 0, page = 1;
+    if (a.none(10) != a.none(11) || a.none(10) != a.none(12) || a.none(10) != a.none(9)) throw Refused("v, slot, k_cache and v_cache: all or none");
+    if (a.none(1)) {
+        if (!a.none(5) || !a.none(10)) throw Refused("k: needed for k_out and for a cache");
+    } else {
+        k = a.heads(1, "k", type, tokens, -1, d), kv_heads = a.tensor(1, "k").size(1);
+        if (a.none(5) && a.none(10)) throw Refused("k: needs k_out or a cache");
+    }
+    if (!a.none(5)) k_out = a.heads(5, "k_out", type, tokens, kv_heads, d);
+    const int32_t* const axis = a.whole(6, "axis", frequency.numel());
+    const bool interleaved = a.truth(7, "interleaved"), inverse = a.truth(8, "inverse");
+    const int32_t* const slot = a.whole(10, "slot", tokens);
+    if (!a.none(10)) {
+        v = a.heads(9, "v", type, tokens, kv_heads, d), k_cache = a.cache(11, "k_cache", type, -1, -1, kv_heads, d);
+        n_pages = a.tensor(11, "k_cache").size(0), page = a.tensor(11, "k_cache").size(1);
+        v_cache = a.cache(12, "v_cache", type, n_pages, page, kv_heads, d);
+    }
+    void* const stream = a.stream(13);
+    return csr5_rotary(int32_t(tokens), int32_t(heads), int32_t(kv_heads), int32_t(d), int32_t(rot), dtype, int32_t(axes), position, ldp, f, axis, interleaved, inverse, hq, q_out, k, k_out, v,
+                       slot, int32_t(n_pages), int32_t(page), k_cache, v_cache, stream);
+}
+
+// What attention is asked of: sequences, rows, k_rows, heads, kv_heads, d
+struct Sizes {
+    int32_t sequences, rows, k_rows, heads, kv_heads, d;
+    at::ScalarType type;
+    int dtype;
+};
+Sizes packed(const Args& a, int q, int k, int q_offset, int k_offset) {
+    const at::Tensor &tq = a.tensor(q, "q"), &tk = a.tensor(k, "k");
+    const int dtype = heads_code(tq, "q", false);
+    const at::ScalarType type = tq.scalar_type();
+    a.heads(q, "q", type, -1, -1, -1);
+    a.heads(k, "k", type, -1, -1, tq.size(2));
+    const int64_t n = sequences_of(a, q_offset, "q_offset");
+    if (sequences_of(a, k_offset, "k_offset") != n) throw Refused("q_offset and k_offset: expected as many of one as of the other");
+    return {int32_t(n), int32_t(tq.size(0)), int32_t(tk.size(0)), int32_t(tq.size(1)), int32_t(tk.size(1)), int32_t(tq.size(2)), type, dtype};
+}
+
+// q, k, v, q_offset, k_offset, out, lse, scale, causal, stream
+int attention(const Args& a) {
+    const Sizes z = packed(a, 0, 1, 3, 4);
+    const csr5_heads_t q = a.heads(0, "q", z.type, z.rows, z.heads, z.d), k = a.heads(1, "k", z.type, z.k_rows, z.kv_heads, z.d), v = a.heads(2, "v", z.type, z.k_rows, z.kv_heads, z.d);
+    const csr5_heads_t out = a.heads(5, "out", z.type, z.rows, z.heads, z.d);
+    const int32_t *const qo = row_pointer(a, 3, "q_offset", z.sequences), *const ko = row_pointer(a, 4, "k_offset", z.sequences);
+    float* const lse = a.floats(6, "lse", int64_t(z.rows) * z.heads);
+    const float scale = float(a.real(7, "scale"));
+    const bool causal = a.truth(8, "causal");
+    void* const stream = a.stream(9);
+    return csr5_attention(z.sequences, z.rows, z.k_rows, z.heads, z.kv_heads, z.d, z.dtype, qo, ko, scale, causal, q, k, v, out, lse, stream);
+}
+
+// dout, q, k, v, out, lse, q_offset, k_offset, dq, dk, dv, workspace, scale, causal, stream
+int attention_backward(const Args& a) {
+    const Sizes z = packed(a, 1, 2, 6, 7);
+    const auto rows = [&](int i, const char* name) { return a.heads(i, name, z.type, z.rows, z.heads, z.d); };
+    const auto keys = [&](int i, const char* name) { return a.heads(i, name, z.type, z.k_rows, z.kv_heads, z.d); };
+    const csr5_heads_t dout = rows(0, "dout"), q = rows(1, "q"), k = keys(2, "k"), v = keys(3, "v"), out = rows(4, "out"), dq = rows(8, "dq"), dk = keys(9, "dk"), dv = keys(10, "dv");
+    const float* const lse = a.floats(5, "lse", int64_t(z.rows) * z.heads);
+    const int32_t *const qo = row_pointer(a, 6, "q_offset", z.sequences), *const ko = row_pointer(a, 7, "k_offset", z.sequences);
+    void* const space = a.array<uint8_t>(11, "workspace", at::kByte, 0);
+    const size_t bytes = a.none(11) ? 0 : size_t(a.tensor(11, "workspace").numel());
+    const float scale = float(a.real(12, "scale"));
+    const bool causal = a.truth(13, "causal");
+    void* const stream = a.stream(14);
+    return csr5_attention_backward(z.sequences, z.rows, z.k_rows, z.heads, z.kv_heads, z.d, z.dtype, qo, ko, scale, causal, dout, q, k, v, out, lse, dq, dk, dv, space, bytes, stream);
+}
+
+// q, k_cache, v_cache, q_offset, length, table, out, workspace, lse, scale, stream
+int attention_paged(const Args& a) {
+    const at::Tensor &tq = a.tensor(0, "q"), &tk = a.tensor(1, "k_cache");
+    const int dtype = heads_code(tq, "q", false);
+    const at::ScalarType type = tq.scalar_type();
+    const csr5_heads_t q = a.heads(0, "q", type, -1, -1, -1);
+    const int64_t rows = tq.size(0), heads = tq.size(1), d = tq.size(2);
+    const csr5_cache_t k = a.cache(1, "k_cache", type, -1, -1, -1, d);
+    const int64_t n_pages = tk.size(0), page = tk.size(1), kv_heads = tk.size(2), n = sequences_of(a, 3, "q_offset");
+    const csr5_cache_t v = a.cache(2, "v_cache", type, n_pages, page, kv_heads, d);
+    const csr5_heads_t out = a.heads(6, "out", type, rows, heads, d);
+    const Matrix table = a.typed(5, "table", at::kInt, n, -1);
+    const int32_t *const qo = row_pointer(a, 3, "q_offset", n), *const length = a.whole(4, "length", n);
+    void* const space = a.array<uint8_t>(7, "workspace", at::kByte, 0);
+    const size_t bytes = a.none(7) ? 0 : size_t(a.tensor(7, "workspace").numel());
+    float* const lse = a.floats(8, "lse", rows * heads);
+    const float scale = float(a.real(9, "scale"));
+    void* const stream = a.stream(10);
+    return csr5_attention_paged(int32_t(n), int32_t(rows), int32_t(heads), int32_t(kv_heads), int32_t(d), dtype, qo, length, as<int32_t>(table), int32_t(table.cols), table.ld, int32_t(n_pages),
+                                int32_t(page), scale, q, k, v, out, lse, space, bytes, stream);
+}
+
 template <int (*F)(const Args&), int COUNT> PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     try {
         return PyLong_FromLong(F(Args(args, n, COUNT)));
@@ -287,7 +467,7 @@ PyObject* set_current_stream(PyObject*, PyObject* f) {
 }
 
 #define ENTRY(name, count) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name, count>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(route, 9), ENTRY(combine, 6), ENTRY(grouped_gemm, 6), ENTRY(quantise, 5), ENTRY(gemm_f8, 7), ENTRY(grouped_gemm_f8, 9), ENTRY(rmsnorm, 10), {"set_current_stream", set_current_stream, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ENTRY(route, 9), ENTRY(combine, 6), ENTRY(grouped_gemm, 6), ENTRY(quantise, 5), ENTRY(gemm_f8, 7), ENTRY(grouped_gemm_f8, 9), ENTRY(rmsnorm, 10), ENTRY(pages, 12), ENTRY(rotary, 14), ENTRY(attention, 10), ENTRY(attention_backward, 15), ENTRY(attention_paged, 11), {"set_current_stream", set_current_stream, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

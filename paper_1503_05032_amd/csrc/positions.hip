@@ -1,0 +1,255 @@
+// libcsr5: what stands around the attention -- the pages of a step of serving, and rotary positions.  Bound by latency and by
+// memory; the attention itself is in attention.hip.  The C ABI is declared in include/csr5.h.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "csr5.h"
+#include "heads.h"
+#include "numbers.h"
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------------------------
+// Pages.  A request's place among the new tokens, the pages taken and the pages given back is the sum of those before it: every
+// workgroup adds all of them up (1024 requests at a time, from L2) and then writes its own share of the tokens, the new entries
+// of the tables and the ring, finding the request of each by bisection over the sums in LDS.  So there is one launch and
+// nothing to wait for between workgroups.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int PAGES_THREADS = 1024, PAGES_WAVES = PAGES_THREADS / 64;
+constexpr int PAGES_SHARE = 4096;           // tokens, or entries, of a workgroup
+
+struct PagesArgs {
+    int requests, width, ring, shift, tokens;
+    const int32_t *fresh, *length;
+    int32_t* table;
+    int64_t ldt;
+    int32_t* pool;
+    const int32_t* state;
+    int32_t *offset, *position, *slot, *length_out, *state_out;
+};
+
+// The sum of v over the threads before this one; total: over all.  part: a word per wavefront, free to be written.
+__device__ __forceinline__ int64_t sum_before(int64_t v, int64_t* part, int64_t& total) {
+    int64_t upto = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t other = __shfl_up(upto, d);
+        if (int(threadIdx.x & 63) >= d) upto += other;
+    }
+    if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = upto;
+    __syncthreads();
+    int64_t before = upto - v, all = 0;
+#pragma unroll
+    for (int w = 0; w < PAGES_WAVES; w++) {
+        if (w < int(threadIdx.x >> 6)) before += part[w];
+        all += part[w];
+    }
+    __syncthreads();
+    total = all;
+    return before;
+}
+
+// The last of the requests whose sum is at most `at`: the one that `at` lies in, as those after it without a share have a larger one.
+__device__ __forceinline__ int request_at(const int64_t* first, int count, int64_t at) {
+    int low = 0, high = count;
+    while (high - low > 1) {
+        const int mid = (low + high) / 2;
+        if (first[mid] <= at) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
+__global__ __launch_bounds__(PAGES_THREADS) void k_pages(PagesArgs a) {
+    __shared__ int64_t part[PAGES_WAVES];
+    __shared__ int64_t first_token[PAGES_THREADS], first_page[PAGES_THREADS], first_back[PAGES_THREADS];
+    __shared__ int32_t lengths[PAGES_THREADS], served[PAGES_THREADS];
+    const int t = threadIdx.x;
+    const int32_t mask = (1 << a.shift) - 1;
+    const int64_t ring = max(a.ring, 1);
+    const int64_t head = ((a.state[0] % ring) + ring) % ring, count = min(max(int64_t(a.state[1]), int64_t(0)), int64_t(a.ring));
+    const int64_t most = int64_t(a.width) << a.shift;
+    int64_t tokens = 0, asked = 0, taken = 0, back = 0;             // of the requests before these
+    for (int r0 = 0; r0 < a.requests; r0 += PAGES_THREADS) {
+        const int r = r0 + t, here = min(PAGES_THREADS, a.requests - r0);
+        const int32_t fresh = r < a.requests ? a.fresh[r] : 0;
+        const int32_t have = r < a.requests ? int32_t(min(int64_t(max(a.length[r], 0)), most)) : 0;
+        const int64_t now = int64_t(have) + max(fresh, 0), held = (int64_t(have) + mask) >> a.shift, wanted = (now + mask) >> a.shift;
+        const bool over = fresh < 0, fits = wanted <= a.width;
+        const int64_t need = fits && !over ? wanted - held : 0;
+        int64_t total_tokens, total_asked, total_taken, total_back;
+        const int64_t token = tokens + sum_before(max(fresh, 0), part, total_tokens);
+        const int64_t want = asked + sum_before(need, part, total_asked);
+        const bool ok = fits && !over && (need == 0 || want + need <= count);
+        const int64_t take = ok ? need : 0;
+        sum_before(take, part, total_taken);
+        const int64_t give = over ? held : 0;
+        const int64_t behind = back + sum_before(give, part, total_back);
+        // what is taken before a request that is served is what is asked for before it
+        first_token[t] = token, first_page[t] = want, first_back[t] = behind, lengths[t] = have, served[t] = ok;
+        if (blockIdx.x == 0 && r < a.requests) {
+            if (r == 0) a.offset[0] = 0;
+            a.offset[r + 1] = int32_t(min(token + max(fresh, 0), int64_t(a.tokens)));
+            a.length_out[r] = over ? 0 : ok ? int32_t(now) : have;
+        }
+        __syncthreads();
+        // tokens
+        const int64_t last_token = min(tokens + total_tokens, int64_t(a.tokens));
+        for (int64_t base = tokens / PAGES_SHARE * PAGES_SHARE; base < last_token; base += PAGES_SHARE) {
+            if ((base / PAGES_SHARE) % gridDim.x != blockIdx.x) continue;
+            const int64_t end = min(base + PAGES_SHARE, last_token);
+            for (int64_t i = max(base, tokens) + t; i < end; i += PAGES_THREADS) {
+                const int q = request_at(first_token, here, i);
+                const int32_t at = int32_t(int64_t(lengths[q]) + (i - first_token[q]));
+                const int32_t holds = (lengths[q] + mask) >> a.shift, p = at >> a.shift;
+                int32_t slot = -1;
+                if (served[q]) {
+                    const int32_t page = p < holds ? a.table[int64_t(r0 + q) * a.ldt + p] : a.pool[(head + first_page[q] + (p - holds)) % ring];
+                    if (page >= 0 && page <= (INT32_MAX >> a.shift)) slot = (page << a.shift) | (at & mask);       // others are no pages
+                }
+                a.position[i] = at, a.slot[i] = slot;
+            }
+        }
+        // new entries of the tables: first_page counts those of requests that are not served too, which are passed over
+        const int64_t last_page = min(asked + total_asked, count);
+        for (int64_t base = asked / PAGES_SHARE * PAGES_SHARE; base < last_page; base += PAGES_SHARE) {
+            if ((base / PAGES_SHARE) % gridDim.x != blockIdx.x) continue;
+            const int64_t end = min(base + PAGES_SHARE, last_page);
+            for (int64_t i = max(base, asked) + t; i < end; i += PAGES_THREADS) {
+                const int q = request_at(first_page, here, i);
+                if (served[q]) a.table[int64_t(r0 + q) * a.ldt + ((lengths[q] + mask) >> a.shift) + (i - first_page[q])] = a.pool[(head + i) % ring];
+            }
+        }
+        // pages that come back, behind the last free one; more than the ring has places for are not pages of it
+        const int64_t last_back = min(back + total_back, int64_t(a.ring) - count);
+        for (int64_t base = back / PAGES_SHARE * PAGES_SHARE; base < last_back; base += PAGES_SHARE) {
+            if ((base / PAGES_SHARE) % gridDim.x != blockIdx.x) continue;
+            const int64_t end = min(base + PAGES_SHARE, last_back);
+            for (int64_t i = max(base, back) + t; i < end; i += PAGES_THREADS) {
+                const int q = request_at(first_back, here, i);
+                a.pool[(head + count + i) % ring] = a.table[int64_t(r0 + q) * a.ldt + (i - first_back[q])];
+            }
+        }
+        tokens += total_tokens, asked += total_asked, taken += total_taken, back += total_back;
+        __syncthreads();
+    }
+    for (int64_t i = min(tokens, int64_t(a.tokens)) + int64_t(blockIdx.x) * PAGES_THREADS + t; i < a.tokens; i += int64_t(gridDim.x) * PAGES_THREADS)
+        a.position[i] = 0, a.slot[i] = -1;
+    if (blockIdx.x == 0 && t == 0) {
+        if (a.requests == 0) a.offset[0] = 0;
+        a.state_out[0] = int32_t((head + taken) % ring);
+        a.state_out[1] = int32_t(count - taken + min(back, int64_t(a.ring) - count));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Rotary positions.  A workgroup takes a few tokens; their angles' cosines and sines are computed once, into LDS, and serve all
+// heads.  The angle, position * frequency, is a product of whole numbers below 2^31 and floats: in 32 bits a position of 10^6 would
+// be off by 0.03 radians, so the product and its reduction to half a turn are in 64 bits, the cosine and sine of that in 32.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T> struct RotaryArgs {
+    int tokens, heads, kv_heads, d, pairs, axes;
+    const int32_t* position;
+    int64_t ldp;
+    const float* frequency;
+    const int32_t* axis;
+    bool inverse;
+    Heads<T> q, q_out, k, k_out, v;
+    const int32_t* slot;
+    int32_t pages, shift;
+    Cache<T> k_cache, v_cache;
+};
+
+constexpr int ROTARY_THREADS = 256;
+
+template <typename T, bool INTERLEAVED> __global__ __launch_bounds__(ROTARY_THREADS) void k_rotary(RotaryArgs<T> a) {
+    extern __shared__ float turn[];                     // cosines, then sines
+    const int64_t token = workgroup();
+    if (token >= a.tokens) return;
+    for (int i = threadIdx.x; i < a.pairs; i += ROTARY_THREADS) {
+        const int32_t axis = a.axis ? a.axis[i] : 0;
+        float c = 1.f, s = 0.f;
+        if (uint32_t(axis) < uint32_t(a.axes)) {
+            constexpr double TURN = 6.283185307179586476925;
+            const double angle = double(a.position[axis * a.ldp + token]) * double(a.frequency[i]);
+            sincosf(float(fma(-rint(angle / TURN), TURN, angle)), &s, &c);
+        }
+        turn[i] = c, turn[a.pairs + i] = a.inverse ? -s : s;
+    }
+    __syncthreads();
+    const int32_t slot = a.slot ? a.slot[token] : -1;
+    const int32_t page = slot >> a.shift, place = slot & ((1 << a.shift) - 1);
+    const bool cached = slot >= 0 && page < a.pages;
+    const int rest = a.d - 2 * a.pairs, each = a.pairs + rest;      // a head: its pairs, and the values that stay
+    for (int i = threadIdx.x; i < (a.heads + a.kv_heads) * each; i += ROTARY_THREADS) {
+        const int h = i / each, e = i - h * each;
+        const bool key = h >= a.heads;
+        const int hk = h - a.heads;
+        const T* const from = key ? a.k.p + token * a.k.row + hk * a.k.head : a.q.p + token * a.q.row + h * a.q.head;
+        T* const to = key ? (a.k_out.p ? a.k_out.p + token * a.k_out.row + hk * a.k_out.head : nullptr) : a.q_out.p + token * a.q_out.row + h * a.q_out.head;
+        T* const in = key && cached ? a.k_cache.p + page * a.k_cache.page + place * a.k_cache.row + hk * a.k_cache.head : nullptr;
+        if (e < a.pairs) {
+            const int x = INTERLEAVED ? 2 * e : e, y = INTERLEAVED ? 2 * e + 1 : e + a.pairs;
+            const float p = float(from[x]), q = float(from[y]), c = turn[e], s = turn[a.pairs + e];
+            const T u = T(p * c - q * s), w = T(p * s + q * c);
+            if (to) to[x] = u, to[y] = w;
+            if (in) in[x] = u, in[y] = w;
+        } else {
+            const T u = from[e + a.pairs];
+            if (to) to[e + a.pairs] = u;
+            if (in) in[e + a.pairs] = u;
+        }
+    }
+    if (cached)
+        for (int i = threadIdx.x; i < a.kv_heads * a.d; i += ROTARY_THREADS) {
+            const int h = i / a.d, e = i - h * a.d;
+            a.v_cache.p[page * a.v_cache.page + place * a.v_cache.row + h * a.v_cache.head + e] = a.v.p[token * a.v.row + h * a.v.head + e];
+        }
+}
+
+}  // namespace
+
+extern "C" {
+
+int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int32_t tokens, const int32_t* fresh, const int32_t* length, int32_t* table,
+               int64_t ldt, int32_t* pool, const int32_t* state, int32_t* offset, int32_t* position, int32_t* slot, int32_t* length_out, int32_t* state_out,
+               void* hip_stream) {
+    if (requests < 0 || width < 0 || ring < 0 || tokens < 0 || !power_of_two(page) || !state || !offset || !state_out) return CSR5_EINVAL;
+    if (requests > MOST_SIZE || tokens > MOST_SIZE) return CSR5_ERANGE;
+    if ((requests > 0 && (!fresh || !length || !length_out)) || !rows_ok(table, requests, ldt, width, 4) || (ring > 0 && !pool) || (tokens > 0 && (!position || !slot))) return CSR5_EINVAL;
+    for (const void* p : {static_cast<const void*>(fresh), static_cast<const void*>(length), static_cast<const void*>(pool), static_cast<const void*>(state), static_cast<const void*>(offset),
+                          static_cast<const void*>(position), static_cast<const void*>(slot), static_cast<const void*>(length_out), static_cast<const void*>(state_out)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return CSR5_EINVAL;
+    const PagesArgs a{requests, width, ring, __builtin_ctz(page), tokens, fresh, length, table, ldt, pool, state, offset, position, slot, length_out, state_out};
+    const int64_t shares = divide_up(int64_t(tokens), PAGES_SHARE);
+    k_pages<<<int(shares < 1 ? 1 : shares > 256 ? 256 : shares), PAGES_THREADS, 0, static_cast<hipStream_t>(hip_stream)>>>(a);
+    return launched();
+}
+
+int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int32_t rot, int dtype, int32_t axes, const int32_t* position, int64_t ldp,
+                const float* frequency, const int32_t* axis, int interleaved, int inverse, csr5_heads_t q, csr5_heads_t q_out, csr5_heads_t k, csr5_heads_t k_out,
+                csr5_heads_t v, const int32_t* slot, int32_t pages, int32_t page, csr5_cache_t k_cache, csr5_cache_t v_cache, void* hip_stream) {
+    const size_t size = dtype == CSR5_DTYPE_F32 ? 4 : dtype == CSR5_DTYPE_BF16 || dtype == CSR5_DTYPE_F16 ? 2 : 0;
+    if (!size || tokens < 0 || heads < 0 || kv_heads < 0 || d < 0 || rot < 0 || rot > d || rot % 2 || axes < 0) return CSR5_EINVAL;
+    if (d > CSR5_ROTARY_MAX_D || tokens > MOST_SIZE || int64_t(heads) + kv_heads > CSR5_ATTENTION_MAX_HEADS || axes > MOST_SIZE) return CSR5_ERANGE;
+    if (!heads_ok(q, tokens, heads, d, size) || !output_ok(q_out, tokens, heads, d, size) || !heads_ok(k, tokens, kv_heads, d, size) || (k_out.p && !output_ok(k_out, tokens, kv_heads, d, size))) return CSR5_EINVAL;
+    if (slot && (pages < 0 || !power_of_two(page) || !heads_ok(v, tokens, kv_heads, d, size) || !cache_output_ok(k_cache, pages, page, kv_heads, d, size) || !cache_output_ok(v_cache, pages, page, kv_heads, d, size))) return CSR5_EINVAL;
+    if (tokens > 0 && rot > 0 && axes > 0 && (!position || !frequency || ldp < tokens)) return CSR5_EINVAL;
+    for (const void* p : {static_cast<const void*>(position), static_cast<const void*>(frequency), static_cast<const void*>(axis), static_cast<const void*>(slot)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return CSR5_EINVAL;
+    if (tokens == 0 || d == 0 || (heads == 0 && kv_heads == 0)) return CSR5_OK;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    auto go = [&](auto zero) {
+        using T = decltype(zero);
+        const RotaryArgs<T> a{tokens, heads, kv_heads, d, rot / 2, axes, position, ldp, frequency, axis, inverse != 0, typed<T>(q), typed<T>(q_out), typed<T>(k), typed<T>(k_out),
+                              typed<T>(v), slot, slot ? pages : 0, slot ? __builtin_ctz(page) : 0, typed<T>(k_cache), typed<T>(v_cache)};
+        if (interleaved) k_rotary<T, true><<<workgroups(tokens), ROTARY_THREADS, rot * 4, s>>>(a);
+        else k_rotary<T, false><<<workgroups(tokens), ROTARY_THREADS, rot * 4, s>>>(a);
+        return launched();
+    };
+    return dtype == CSR5_DTYPE_F32 ? go(float()) : dtype == CSR5_DTYPE_F16 ? go(f16()) : go(bf16());
+}
+
+}  // extern "C"
