@@ -10,8 +10,8 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = [os.path.join(PKG, "csrc", name) for name in ("csr5.hip", "experts.hip", "grouped.hip", "attention.hip", "positions.hip")]
-HEADERS = [os.path.join(PKG, "csrc", name) for name in ("row_share.h", "far_lists.h", "numbers.h", "heads.h")]
+SRC = [os.path.join(PKG, "csrc", name) for name in ("csr5.hip", "experts.hip", "grouped.hip", "attention.hip", "attention_back.hip", "positions.hip")]
+HEADERS = [os.path.join(PKG, "csrc", name) for name in ("row_share.h", "far_lists.h", "numbers.h", "heads.h", "to_lds.h", "sequences.h")]
 INC = os.path.join(ROOT, "include")
 OUT = os.path.join(PKG, "libcsr5.so")
 MARSHAL_SRC = os.path.join(PKG, "csrc", "marshal.cpp")

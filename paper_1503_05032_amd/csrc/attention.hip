@@ -1,5 +1,8 @@
-// libcsr5: attention over packed sequences and over a paged cache of keys and values, and its gradients.  The C ABI is declared in
-// include/csr5.h.
+// libcsr5: attention over packed sequences and over a paged cache of keys and values.  Its gradients are in attention_back.hip.
+// The C ABI is declared in include/csr5.h.
+//
+// Rows are folded: the query heads that share a head of keys are rows side by side, r = token * shared + head, so that they
+// read its keys once.  A score is s = q.k in units of 1 / (scale * log2 e); softmax by a running base b, with p = 2^(c (s - b)), c = scale log2 e.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -9,57 +12,13 @@
 #include "csr5.h"
 #include "heads.h"
 #include "numbers.h"
+#include "sequences.h"
+#include "to_lds.h"
 
 namespace {
 
-// ---------------------------------------------------------------------------------------------------------------
-// Sequences
-// ---------------------------------------------------------------------------------------------------------------
-struct Span {
-    int32_t first, count;
-};
-// Rows of sequence s.  Whatever the offsets hold, these are rows that there are.
-__device__ __forceinline__ Span span_of(const int32_t* offset, int32_t s, int32_t rows) {
-    const int32_t a = min(max(offset[s], 0), rows), b = min(max(offset[s + 1], 0), rows);
-    return {a, max(b - a, 0)};
-}
-// The sequence that row i lies in, by bisection; -1: none.
-__device__ __forceinline__ int32_t sequence_of(const int32_t* offset, int32_t sequences, int32_t rows, int32_t i) {
-    int32_t low = 0, high = sequences;
-    while (high - low > 1) {
-        const int32_t mid = low + (high - low) / 2;
-        if (offset[mid] <= i) low = mid;
-        else high = mid;
-    }
-    const Span s = span_of(offset, low, rows);
-    return i >= s.first && i < s.first + s.count ? low : -1;
-}
-
-// Keys and values, packed or in a cache.
-template <typename T> struct Packed {
-    const int32_t* offset;
-    int32_t rows;
-    Heads<const T> k, v;
-    __device__ __forceinline__ Span span(int32_t s) const { return span_of(offset, s, rows); }
-    __device__ __forceinline__ const T* key(int32_t s, const Span& at, int32_t j, int h) const { return k.p + int64_t(at.first + j) * k.row + h * k.head; }
-    __device__ __forceinline__ const T* value(int32_t s, const Span& at, int32_t j, int h) const { return v.p + int64_t(at.first + j) * v.row + h * v.head; }
-};
-template <typename T> struct Paged {
-    const int32_t *length, *table;
-    int32_t width, pages, shift;
-    int64_t ldt;
-    Cache<const T> k, v;
-    __device__ __forceinline__ Span span(int32_t s) const { return {0, int32_t(min(int64_t(max(length[s], 0)), int64_t(width) << shift))}; }
-    __device__ __forceinline__ const T* row(const Cache<const T>& c, int32_t s, int32_t j, int h) const {
-        const int32_t page = table[s * ldt + (j >> shift)];
-        return uint32_t(page) < uint32_t(pages) ? c.p + page * c.page + (j & ((1 << shift) - 1)) * c.row + h * c.head : nullptr;
-    }
-    __device__ __forceinline__ const T* key(int32_t s, const Span&, int32_t j, int h) const { return row(k, s, j, h); }
-    __device__ __forceinline__ const T* value(int32_t s, const Span&, int32_t j, int h) const { return row(v, s, j, h); }
-};
-
 template <typename T, typename KV> struct Attend {
-    int32_t sequences, rows, heads, shared, d;
+    int32_t sequences, rows, heads, kv_heads, shared, d;
     const int32_t* q_offset;
     float scale;
     bool causal;
@@ -67,151 +26,515 @@ template <typename T, typename KV> struct Attend {
     KV kv;
     Heads<T> out;
     float* lse;
+    int32_t tiles;
+    int32_t chunk;          // keys of a workgroup, where the work is split over them (0: it is not)
+    float *part, *stats;    // ... and what it leaves: [chunk][row][head][d] sums, [chunk][row][head] their base and total
 };
 
-// Keys that query i of m sees, of n.
-__device__ __forceinline__ int32_t seen(bool causal, int32_t i, int32_t m, int32_t n) { return causal ? min(max(n - m + i + 1, 0), n) : n; }
+// The base rises where a score passes it by more than this many powers of two: sums are rescaled seldom, and p is at most 256.
+constexpr float RISE = 8.f;
 
-template <typename T> __device__ __forceinline__ float dot(const T* a, const T* b, int d) {
-    float sum = 0.f;
-    if (b)
-        for (int c = 0; c < d; c++) sum = fmaf(float(a[c]), float(b[c]), sum);
-    return sum;
+__device__ __forceinline__ float half_most(float v) {       // over lanes l and l ^ 32
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
 }
-__device__ __forceinline__ float wave_most(float v) {
+__device__ __forceinline__ float half_sum(float v) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(both[0]) + __uint_as_float(both[1]);
+}
+__device__ __forceinline__ float quarter_most(float v) {    // over lanes l, l ^ 16, l ^ 32, l ^ 48
+    const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return half_most(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])));
+}
+__device__ __forceinline__ float quarter_sum(float v) {
+    const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return half_sum(__uint_as_float(both[0]) + __uint_as_float(both[1]));
+}
+__device__ __forceinline__ float power(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// A row of the folded ones, its query and the keys that it sees.
+struct Row {
+    int32_t token, head, limit;
+    bool there;
+};
+__device__ __forceinline__ Row row_of(int64_t r, int32_t m, int32_t n, int32_t shared, bool causal) {
+    const int64_t count = int64_t(m) * shared, at = r < count ? r : count - 1;
+    Row x;
+    if (at >> 32) {
+        x.token = int32_t(at / shared), x.head = int32_t(at % shared);
+    } else {
+        x.token = int32_t(uint32_t(at) / uint32_t(shared)), x.head = int32_t(uint32_t(at) % uint32_t(shared));
+    }
+    x.limit = seen(causal, x.token, m, n), x.there = r < count;
+    return x;
+}
+
+// What a workgroup leaves of one row: the result, or its part of it.
+template <typename T, typename KV> struct Leave {
+    T* out;
+    float *part, *lse, *stats;
+    __device__ __forceinline__ Leave(const Attend<T, KV>& a, int32_t row, int32_t h) {
+        const int64_t at = (int64_t(blockIdx.y) * a.rows + row) * a.heads + h;
+        out = a.out.p + row * a.out.row + h * a.out.head;
+        part = a.chunk ? a.part + at * a.d : nullptr, stats = a.chunk ? a.stats + at * 2 : nullptr;
+        lse = !a.chunk && a.lse ? a.lse + int64_t(h) * a.rows + row : nullptr;
+    }
+    // four neighbouring values of the sum from c on; inverse: of the total
+    template <bool WIDE> __device__ __forceinline__ void four(int c, int d, const float (&v)[4], float inverse) const {
+        if (part) {
 #pragma unroll
-    for (int e = 1; e < 64; e *= 2) v = fmaxf(v, __shfl_xor(v, e));
-    return v;
-}
-
-// One wavefront per row and head: 64 scores at a time, a running maximum and sum.
-template <typename T, typename KV> __global__ __launch_bounds__(64) void k_attend(Attend<T, KV> a) {
-    const int64_t at = workgroup();
-    if (at >= int64_t(a.rows) * a.heads) return;
-    const int32_t row = int32_t(at / a.heads), h = int32_t(at % a.heads), hk = h / a.shared, lane = threadIdx.x;
-    const int32_t s = sequence_of(a.q_offset, a.sequences, a.rows, row);
-    if (s < 0) return;
-    const Span mine = span_of(a.q_offset, s, a.rows), keys = a.kv.span(s);
-    const int32_t n = seen(a.causal, row - mine.first, mine.count, keys.count);
-    const T* const q = a.q.p + row * a.q.row + h * a.q.head;
-    float top = -INFINITY, sum = 0.f, acc[2] = {0.f, 0.f};
-    for (int32_t j0 = 0; j0 < n; j0 += 64) {
-        const int32_t j = j0 + lane;
-        const float x = j < n ? a.scale * dot(q, a.kv.key(s, keys, j, hk), a.d) : -INFINITY;
-        const float higher = fmaxf(top, wave_most(x)), base = higher == -INFINITY ? 0.f : higher;
-        const float p = expf(x - base), less = expf(top - base);
-        top = higher, sum = sum * less + wave_sum(p);
-        acc[0] *= less, acc[1] *= less;
-        for (int e = 0; e < min(64, n - j0); e++) {
-            const float w = __shfl(p, e);
-            const T* const v = a.kv.value(s, keys, j0 + e, hk);
-            for (int i = 0; i < 2; i++)
-                if (v && i * 64 + lane < a.d) acc[i] = fmaf(w, float(v[i * 64 + lane]), acc[i]);
+            for (int e = 0; e < 4; e++)
+                if (c + e < d) part[c + e] = v[e];
+        } else {
+            const float w[4] = {v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse};
+            store_values<4, WIDE>(out + c, d - c, w);
         }
     }
-    for (int i = 0; i < 2; i++)
-        if (i * 64 + lane < a.d) a.out.p[row * a.out.row + h * a.out.head + i * 64 + lane] = T(n > 0 ? acc[i] / sum : 0.f);
-    if (a.lse && lane == 0) a.lse[int64_t(h) * a.rows + row] = n > 0 ? top + logf(sum) : -INFINITY;
-}
-
-template <typename T> struct Back {
-    int32_t sequences, rows, heads, shared, d;
-    const int32_t* q_offset;
-    float scale;
-    bool causal;
-    Heads<const T> dout, q, out;
-    Packed<T> kv;
-    const float* lse;
-    float* delta;               // [heads][rows]
-    Heads<T> dq, dk, dv;
+    __device__ __forceinline__ void total(float base, float sum, float scale) const {
+        if (stats) stats[0] = base, stats[1] = sum;
+        else if (lse) *lse = sum == 0.f ? -INFINITY : base * scale + logf(sum);
+    }
 };
 
-template <typename T> __global__ __launch_bounds__(64) void k_delta(Back<T> a) {
-    const int64_t at = workgroup() * 64 + threadIdx.x;
-    if (at >= int64_t(a.rows) * a.heads) return;
-    const int32_t row = int32_t(at % a.rows), h = int32_t(at / a.rows);
-    a.delta[at] = dot(a.dout.p + row * a.dout.row + h * a.dout.head, a.out.p + row * a.out.row + h * a.out.head, a.d);
-}
+// ---------------------------------------------------------------------------------------------------------------
+// Many rows.  128 folded rows, 32 to each of four wavefronts, which go through the keys in tiles of 64.
+// Scores are computed as keys x rows, k q^T: a lane has 32 of the 64 scores of one row, so the maximum and the sum need one exchange
+// with the lane's other half, and what it has is, rounded, the second operand of out^T = v^T p^T as it is: the order of the depth (keys) is free as
+// long as v's, which a transposing read of LDS brings, is the same.  Two tiles of keys and values are in LDS, the next one on its way.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int MANY_ROWS = 128, MANY_SHIFT = 7, MANY_KEYS = 64;
 
-// One wavefront per row and head.
-template <typename T> __global__ __launch_bounds__(64) void k_attend_dq(Back<T> a) {
-    const int64_t at = workgroup();
-    if (at >= int64_t(a.rows) * a.heads) return;
-    const int32_t row = int32_t(at / a.heads), h = int32_t(at % a.heads), hk = h / a.shared, lane = threadIdx.x;
-    const int32_t s = sequence_of(a.q_offset, a.sequences, a.rows, row);
-    if (s < 0) return;
-    const Span mine = span_of(a.q_offset, s, a.rows), keys = a.kv.span(s);
-    const int32_t n = seen(a.causal, row - mine.first, mine.count, keys.count);
-    const float lse = a.lse[int64_t(h) * a.rows + row], delta = a.delta[int64_t(h) * a.rows + row];
-    float acc[2] = {0.f, 0.f};
-    for (int32_t j0 = 0; j0 < n; j0 += 64) {
-        const int32_t j = j0 + lane;
-        float ds = 0.f;
-        if (j < n) {
-            const float p = expf(a.scale * dot(a.q.p + row * a.q.row + h * a.q.head, a.kv.key(s, keys, j, hk), a.d) - lse);
-            ds = p * (dot(a.dout.p + row * a.dout.row + h * a.dout.head, a.kv.value(s, keys, j, hk), a.d) - delta);
+// out += v^T p^T of a tile where some row does not see a key that others see, with values that are not finite among the tile's: a product
+// 0 * inf must not show.  Such values are left out, and what they do to the rows that see them is found by counting.
+template <typename T, int ND> __device__ __forceinline__ void careful(const vec<T, 8> (&p)[4], const uint32_t (&at)[ND], uint32_t row_bytes, int32_t key0, int32_t limit, f32x16 (&o)[ND]) {
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int dt = 0; dt < ND; dt++) {
+        f32x16 up = {}, down = {};
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            __builtin_amdgcn_sched_barrier(0);      // one after the other: registers count, not time
+            vec<T, 8> v = turned_from<T>(at[dt] + k * 16 * row_bytes, 8 * row_bytes), u, w, see;
+            parted<T>(v, u, w);
+#pragma unroll
+            for (int e = 0; e < 8; e++) see[e] = T(key0 + k * 16 + (e / 4) * 8 + half * 4 + e % 4 < limit ? 1.f : 0.f);
+            o[dt] = product32(v, p[k], o[dt]), up = product32(u, see, up), down = product32(w, see, down);
         }
-        for (int e = 0; e < min(64, n - j0); e++) {
-            const float w = __shfl(ds, e);
-            const T* const k = a.kv.key(s, keys, j0 + e, hk);
-            for (int i = 0; i < 2; i++)
-                if (i * 64 + lane < a.d) acc[i] = fmaf(w, float(k[i * 64 + lane]), acc[i]);
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            if (up[i] > 0.f) o[dt][i] += INFINITY;
+            if (down[i] > 0.f) o[dt][i] -= INFINITY;
         }
     }
-    for (int i = 0; i < 2; i++)
-        if (i * 64 + lane < a.d) a.dq.p[row * a.dq.row + h * a.dq.head + i * 64 + lane] = T(a.scale * acc[i]);
 }
 
-// One wavefront per key and head of keys; the query heads that share it one after the other.
-template <typename T> __global__ __launch_bounds__(64) void k_attend_dkv(Back<T> a) {
-    const int64_t at = workgroup();
-    const int32_t kv_heads = a.heads / a.shared;
-    if (at >= int64_t(a.kv.rows) * kv_heads) return;
-    const int32_t row = int32_t(at / kv_heads), hk = int32_t(at % kv_heads), lane = threadIdx.x;
-    const int32_t s = sequence_of(a.kv.offset, a.sequences, a.kv.rows, row);
-    if (s < 0) return;
-    const Span mine = span_of(a.q_offset, s, a.rows), keys = a.kv.span(s);
-    const int32_t j = row - keys.first, from = a.causal ? max(0, j - (keys.count - mine.count)) : 0;     // the first query that sees it
-    float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
-    for (int g = 0; g < a.shared; g++) {
-        const int h = hk * a.shared + g;
-        for (int32_t i0 = from; i0 < mine.count; i0 += 64) {
-            const int32_t i = i0 + lane, r = mine.first + i;
-            float p = 0.f, ds = 0.f;
-            if (i < mine.count) {
-                p = expf(a.scale * dot(a.q.p + r * a.q.row + h * a.q.head, a.kv.key(s, keys, j, hk), a.d) - a.lse[int64_t(h) * a.rows + r]);
-                ds = p * (dot(a.dout.p + r * a.dout.row + h * a.dout.head, a.kv.value(s, keys, j, hk), a.d) - a.delta[int64_t(h) * a.rows + r]);
+template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_many(Attend<T, KV> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = MANY_KEYS / EACH / 4;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int32_t hk = blockIdx.x % a.kv_heads;
+    TileOf at;
+    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, MANY_SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
+    const auto kv = a.kv.one(at.s, hk);
+    const int32_t m = at.rows.count, n = kv.count;
+    const int64_t first = at.first + wave * 32;
+    const Row row = row_of(first + (lane & 31), m, n, a.shared, a.causal);
+    // the keys that this wavefront's first and last row see, and the last of the workgroup's
+    const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
+    const int32_t all = __builtin_amdgcn_readfirstlane(row_of(at.first + MANY_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t begin = a.chunk * int32_t(blockIdx.y), end = a.chunk ? min(all, begin + a.chunk) : all;
+    if (a.chunk && begin >= end) return;
+
+    vec<T, 8> q[2 * ND];
+    {
+        const T* const from = a.q.p + (at.rows.first + row.token) * a.q.row + (hk * a.shared + row.head) * a.q.head;
+#pragma unroll
+        for (int kk = 0; kk < 2 * ND; kk++) q[kk] = eight_values<WIDE>(from + (2 * kk + half) * 8, row.there ? a.d - (2 * kk + half) * 8 : 0);
+    }
+    // which chunk of which row of a tile this lane brings
+    const int r0 = wave * EACH + lane / LANES, ck = int(chunk_at<D, BY_ROW>(r0, lane % LANES)) * 8, cv = int(chunk_at<D, BY_SEGMENT64>(r0, lane % LANES)) * 8;
+    typename decltype(kv)::Ahead ahead[LOADS];
+    auto look = [&](int32_t j0) {
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + r0 + i * 4 * EACH);
+    };
+    auto bring = [&](int32_t j0, uint8_t* to) {
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int32_t j = j0 + r0 + i * 4 * EACH;
+            const T *const k = kv.key(j, ahead[i]), *const v = kv.value(j, ahead[i]);
+            chunk_to_lds<WIDE>(k ? k + ck : k, j < n ? a.d - ck : 0, to + (i * 4 + wave) * 1024);
+            chunk_to_lds<WIDE>(v ? v + cv : v, j < n ? a.d - cv : 0, to + TILE + (i * 4 + wave) * 1024);
+        }
+    };
+    const uint32_t lds0 = lds_address(lds);
+    // where this lane reads keys (rows lane % 32) and values (rows 4 * half on, columns)
+    const int li = lane & 15, vr = half * 4 + (li >> 2);
+    uint32_t k_at[2 * ND], v_at[ND];
+#pragma unroll
+    for (int kk = 0; kk < 2 * ND; kk++) k_at[kk] = (lane & 31) * D * 2 + chunk_at<D, BY_ROW>(lane & 31, 2 * kk + half) * 16;
+#pragma unroll
+    for (int dt = 0; dt < ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, BY_SEGMENT64>(vr, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+
+    const float c = a.scale * LOG2_E, rise = RISE / c;
+    float base = -INFINITY, sum = 0.f;
+    f32x16 o[ND] = {};
+    look(begin);
+    bring(begin, lds);
+    look(begin + MANY_KEYS);
+    int now = 0;
+    for (int32_t j0 = begin; j0 < end; j0 += MANY_KEYS, now ^= 1) {
+        landed<0>();
+        if (j0 + MANY_KEYS < end) {
+            bring(j0 + MANY_KEYS, lds + (now ^ 1) * 2 * TILE);
+            look(j0 + 2 * MANY_KEYS);
+        }
+        if (j0 >= most) continue;
+        const uint32_t tile = lds0 + now * 2 * TILE;
+        f32x16 s[2] = {};
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) s[kb] = product32(chunk_from<T>(tile + k_at[kk] + kb * 32 * D * 2), q[kk], s[kb]);
+        const bool some = j0 + MANY_KEYS > least;       // some row does not see some key
+        if (some)
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (j0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4 >= row.limit) s[kb][i] = -INFINITY;
+        float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int i = 1; i < 16; i++) top = fmaxf(fmaxf(s[0][i], s[1][i]), top);
+        top = half_most(top);
+        if (__any(top > base + rise)) {
+            const float higher = fmaxf(base, top), less = higher == base ? 1.f : power((base - higher) * c);
+            base = higher, sum *= less;
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) o[dt][i] *= less;
+        }
+        const float zero = base == -INFINITY ? 0.f : base * c;
+        vec<T, 8> p[4];
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float e = power(fmaf(s[kb][i], c, -zero));
+                sum += e;
+                p[kb * 2 + i / 8][i % 8] = T(e);
             }
-            for (int e = 0; e < min(64, mine.count - i0); e++) {
-                const float w = __shfl(p, e), u = __shfl(ds, e);
-                const int64_t q = mine.first + i0 + e;
-                for (int c = lane; c < a.d; c += 64) {
-                    dv[c / 64] = fmaf(w, float(a.dout.p[q * a.dout.row + h * a.dout.head + c]), dv[c / 64]);
-                    dk[c / 64] = fmaf(u, float(a.q.p[q * a.q.row + h * a.q.head + c]), dk[c / 64]);
+        if (some && least < min(j0 + MANY_KEYS, n)) {
+            u16x2 size = {0, 0};
+            for (int i = 0; i < TILE / 1024; i++) {
+                const uint4 w = __builtin_bit_cast(uint4, chunk_from<T>(tile + TILE + i * 1024 + lane * 16));
+                most_of(size, w.x), most_of(size, w.y), most_of(size, w.z), most_of(size, w.w);
+            }
+            if (__any(not_finite<T>(size))) {
+                uint32_t from[ND];
+#pragma unroll
+                for (int dt = 0; dt < ND; dt++) from[dt] = tile + v_at[dt];
+                careful<T, ND>(p, from, D * 2, j0, row.limit, o);
+                continue;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++) o[dt] = product32(turned_from<T>(tile + v_at[dt] + k * 16 * D * 2, 8 * D * 2), p[k], o[dt]);
+    }
+    own_landed<0>();
+    sum = half_sum(sum);
+    if (!row.there) return;
+    const Leave<T, KV> leave(a, at.rows.first + row.token, hk * a.shared + row.head);
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float v[4] = {o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+            leave.template four<WIDE>(dt * 32 + i * 8 + half * 4, a.d, v, inverse);
+        }
+    if (half == 0) leave.total(base, sum, a.scale);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Few rows: 16 RB folded rows, and the keys dealt to four wavefronts in tiles of 32, each with LDS of its own and no barrier; what they
+// have of the rows is joined at the end.  Bound by the keys' and values' way from memory: 16 KB (8 where d <= 64) of each wavefront are always
+// on their way.  Products are keys x rows as above, of 16 x 16 x 32.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int FEW_KEYS = 32;
+
+template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launch_bounds__(256, 1) void k_attend_few(Attend<T, KV> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = FEW_KEYS * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = FEW_KEYS / EACH, ROWS = 16 * RB;
+    constexpr int SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, li = lane & 15;
+    const int32_t hk = blockIdx.x % a.kv_heads;
+    TileOf at;
+    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
+    const auto kv = a.kv.one(at.s, hk);
+    const int32_t m = at.rows.count, n = kv.count;
+    const int32_t least = __builtin_amdgcn_readfirstlane(row_of(at.first, m, n, a.shared, a.causal).limit);
+    const int32_t all = __builtin_amdgcn_readfirstlane(row_of(at.first + ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t begin = a.chunk * int32_t(blockIdx.y), end = a.chunk ? min(all, begin + a.chunk) : all;
+    if (a.chunk && begin >= end) return;
+
+    Row row[RB];
+    vec<T, 8> q[RB][ND];
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+        row[b] = row_of(at.first + b * 16 + li, m, n, a.shared, a.causal);
+        const T* const from = a.q.p + (at.rows.first + row[b].token) * a.q.row + (hk * a.shared + row[b].head) * a.q.head;
+#pragma unroll
+        for (int kk = 0; kk < ND; kk++) q[b][kk] = eight_values<WIDE>(from + (4 * kk + quarter) * 8, row[b].there ? a.d - (4 * kk + quarter) * 8 : 0);
+    }
+    uint8_t* const mine = lds + wave * 4 * TILE;
+    const int r0 = lane / LANES;
+    typename decltype(kv)::Ahead ahead[LOADS];
+    auto look = [&](int32_t j0) {
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + r0 + i * EACH);
+    };
+    auto bring = [&](int32_t j0, uint8_t* to) {
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int r = r0 + i * EACH;
+            const int32_t j = j0 + r;
+            const int ck = int(chunk_at<D, BY_ROW>(r, lane % LANES)) * 8, cv = int(chunk_at<D, BY_SEGMENT32>(r, lane % LANES)) * 8;
+            const T *const k = kv.key(j, ahead[i]), *const v = kv.value(j, ahead[i]);
+            chunk_to_lds<WIDE>(k ? k + ck : k, j < n ? a.d - ck : 0, to + i * 1024);
+            chunk_to_lds<WIDE>(v ? v + cv : v, j < n ? a.d - cv : 0, to + TILE + i * 1024);
+        }
+    };
+    const uint32_t lds0 = lds_address(mine);
+    const int vr = quarter * 4 + (li >> 2);
+    uint32_t k_at[ND], v_at[2 * ND];
+#pragma unroll
+    for (int kk = 0; kk < ND; kk++) k_at[kk] = li * D * 2 + chunk_at<D, BY_ROW>(li, 4 * kk + quarter) * 16;
+#pragma unroll
+    for (int dt = 0; dt < 2 * ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, BY_SEGMENT32>(vr, dt * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+
+    const float c = a.scale * LOG2_E, rise = RISE / c;
+    float base[RB], sum[RB];
+    f32x4 o[RB][2 * ND] = {};
+#pragma unroll
+    for (int b = 0; b < RB; b++) base[b] = -INFINITY, sum[b] = 0.f;
+    const int32_t start = begin + wave * FEW_KEYS;
+    if (start < end) {
+        look(start);
+        bring(start, mine);
+        look(start + 4 * FEW_KEYS);
+    }
+    int now = 0;
+    for (int32_t j0 = start; j0 < end; j0 += 4 * FEW_KEYS, now ^= 1) {
+        own_landed<0>();
+        if (j0 + 4 * FEW_KEYS < end) {
+            bring(j0 + 4 * FEW_KEYS, mine + (now ^ 1) * 2 * TILE);
+            look(j0 + 8 * FEW_KEYS);
+        }
+        const uint32_t tile = lds0 + now * 2 * TILE;
+        f32x4 s[RB][2] = {};
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int kk = 0; kk < ND; kk++) {
+                const vec<T, 8> k = chunk_from<T>(tile + k_at[kk] + kb * 16 * D * 2);
+#pragma unroll
+                for (int b = 0; b < RB; b++) s[b][kb] = product16(k, q[b][kk], s[b][kb]);
+            }
+        const bool some = j0 + FEW_KEYS > least;
+        vec<T, 8> p[RB];
+#pragma unroll
+        for (int b = 0; b < RB; b++) {
+            if (some)
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (j0 + i / 4 * 16 + quarter * 4 + i % 4 >= row[b].limit) s[b][i / 4][i % 4] = -INFINITY;
+            float top = s[b][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; i++) top = fmaxf(top, s[b][i / 4][i % 4]);
+            top = quarter_most(top);
+            if (__any(top > base[b] + rise)) {
+                const float higher = fmaxf(base[b], top), less = higher == base[b] ? 1.f : power((base[b] - higher) * c);
+                base[b] = higher, sum[b] *= less;
+#pragma unroll
+                for (int dt = 0; dt < 2 * ND; dt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) o[b][dt][i] *= less;
+            }
+            const float zero = base[b] == -INFINITY ? 0.f : base[b] * c;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float e = power(fmaf(s[b][i / 4][i % 4], c, -zero));
+                sum[b] += e;
+                p[b][i] = T(e);
+            }
+        }
+        bool bad = false;
+        if (some && least < min(j0 + FEW_KEYS, n)) {
+            u16x2 size = {0, 0};
+            for (int i = 0; i < TILE / 1024; i++) {
+                const uint4 w = __builtin_bit_cast(uint4, chunk_from<T>(tile + TILE + i * 1024 + lane * 16));
+                most_of(size, w.x), most_of(size, w.y), most_of(size, w.z), most_of(size, w.w);
+            }
+            bad = __any(not_finite<T>(size));
+        }
+        if (!bad) {
+#pragma unroll
+            for (int dt = 0; dt < 2 * ND; dt++) {
+                const vec<T, 8> v = turned_from<T>(tile + v_at[dt], 16 * D * 2);
+#pragma unroll
+                for (int b = 0; b < RB; b++) o[b][dt] = product16(v, p[b], o[b][dt]);
+            }
+        } else {                // as careful() does
+#pragma unroll
+            for (int dt = 0; dt < 2 * ND; dt++) {
+                __builtin_amdgcn_sched_barrier(0);
+                vec<T, 8> v = turned_from<T>(tile + v_at[dt], 16 * D * 2), u, w, see;
+                parted<T>(v, u, w);
+#pragma unroll
+                for (int b = 0; b < RB; b++) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) see[e] = T(j0 + e / 4 * 16 + quarter * 4 + e % 4 < row[b].limit ? 1.f : 0.f);
+                    o[b][dt] = product16(v, p[b], o[b][dt]);
+                    const f32x4 none = {}, up = product16(u, see, none), down = product16(w, see, none);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        if (up[i] > 0.f) o[b][dt][i] += INFINITY;
+                        if (down[i] > 0.f) o[b][dt][i] -= INFINITY;
+                    }
                 }
             }
         }
     }
-    for (int c = lane; c < a.d; c += 64) {
-        a.dk.p[row * a.dk.row + hk * a.dk.head + c] = T(a.scale * dk[c / 64]);
-        a.dv.p[row * a.dv.row + hk * a.dv.head + c] = T(dv[c / 64]);
+    // Joined by way of LDS: [wave][row][d], and their bases and totals.
+    own_landed<0>();
+    __syncthreads();
+    constexpr int PITCH = ND * 32 + 4;      // floats of a row: 16 rows' four values from one column on begin in other banks
+    float* const sums = reinterpret_cast<float*>(lds);
+    __shared__ float bases[4][ROWS], totals[4][ROWS];
+#pragma unroll
+    for (int b = 0; b < RB; b++) {
+        const float total = quarter_sum(sum[b]);
+        if (quarter == 0) bases[wave][b * 16 + li] = base[b], totals[wave][b * 16 + li] = total;
+#pragma unroll
+        for (int dt = 0; dt < 2 * ND; dt++) *reinterpret_cast<f32x4*>(sums + (wave * ROWS + b * 16 + li) * PITCH + dt * 16 + quarter * 4) = o[b][dt];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < ROWS * ND * 8; i += 256) {
+        const int r = i / (ND * 8), x = i % (ND * 8) * 4;
+        const Row it = row_of(at.first + r, m, n, a.shared, a.causal);
+        if (!it.there) continue;
+        float top = bases[0][r], total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 1; w < 4; w++) top = fmaxf(top, bases[w][r]);
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            // a wavefront without keys has base -inf: nothing
+            const float less = bases[w][r] == -INFINITY ? 0.f : power((bases[w][r] - top) * c);
+            if (bases[w][r] == -INFINITY && totals[w][r] == 0.f) continue;
+            total += totals[w][r] * less;
+            const f32x4 part = *reinterpret_cast<const f32x4*>(sums + (w * ROWS + r) * PITCH + x);
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] += part[e] * less;
+        }
+        const Leave<T, KV> leave(a, at.rows.first + it.token, hk * a.shared + it.head);
+        leave.template four<WIDE>(x, a.d, v, total == 0.f ? 0.f : 1.f / total);
+        if (x == 0) leave.total(top, total, a.scale);
     }
 }
 
-template <typename F> int with_half(int dtype, F f) { return dtype == CSR5_DTYPE_F16 ? f(f16()) : f(bf16()); }
-
-// What all calls ask of their sizes
-int sizes(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype, float scale) {
-    if ((dtype != CSR5_DTYPE_BF16 && dtype != CSR5_DTYPE_F16) || sequences < 0 || rows < 0 || k_rows < 0 || heads < 0 || kv_heads < 0 || d < 0) return CSR5_EINVAL;
-    if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return CSR5_EINVAL;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return CSR5_EINVAL;
-    if (sequences > MOST_SIZE || rows > MOST_SIZE || k_rows > MOST_SIZE || heads > CSR5_ATTENTION_MAX_HEADS || d > CSR5_ATTENTION_MAX_D) return CSR5_ERANGE;
-    return CSR5_OK;
+// The parts of a row that workgroups left, one for each `chunk` keys that it sees: one wavefront per row and head.
+template <typename T, typename KV> __global__ __launch_bounds__(256) void k_join(Attend<T, KV> a) {
+    const int64_t at = workgroup() * 4 + (threadIdx.x >> 6);
+    if (at >= int64_t(a.rows) * a.heads) return;
+    const int32_t row = int32_t(at / a.heads), h = int32_t(at % a.heads), lane = threadIdx.x & 63;
+    TileOf t;
+    // with tiles of one row, tile row + s is row `row` of sequence s: the sequence is found as the last that begins at or before the row
+    int32_t low = 0, high = a.sequences;
+    while (high - low > 1) {
+        const int32_t mid = low + (high - low) / 2;
+        if (begin_of(a.q_offset, mid, a.rows) <= row) low = mid;
+        else high = mid;
+    }
+    t.rows = span_of(a.q_offset, low, a.rows);
+    if (row < t.rows.first || row >= t.rows.first + t.rows.count) return;
+    const auto kv = a.kv.one(low, 0);
+    const int32_t limit = seen(a.causal, row - t.rows.first, t.rows.count, kv.count), parts = (limit + a.chunk - 1) / a.chunk;
+    const int64_t step = int64_t(a.rows) * a.heads;
+    const float* const stats = a.stats + at * 2;
+    const float* const part = a.part + at * a.d;
+    const float c = a.scale * LOG2_E;
+    float top = -INFINITY, total = 0.f, v[2] = {0.f, 0.f};
+    for (int32_t i = lane; i < parts; i += 64) top = fmaxf(top, stats[i * step * 2]);
+#pragma unroll
+    for (int e = 1; e < 64; e *= 2) top = fmaxf(top, __shfl_xor(top, e));
+    for (int32_t i = 0; i < parts; i++) {
+        const float base = stats[i * step * 2], sum = stats[i * step * 2 + 1];
+        if (base == -INFINITY && sum == 0.f) continue;
+        const float less = base == -INFINITY ? 0.f : power((base - top) * c);
+        total += sum * less;
+#pragma unroll
+        for (int e = 0; e < 2; e++)
+            if (lane + e * 64 < a.d) v[e] += part[i * step * a.d + lane + e * 64] * less;
+    }
+    const float inverse = total == 0.f ? 0.f : 1.f / total;
+    T* const out = a.out.p + row * a.out.row + h * a.out.head;
+#pragma unroll
+    for (int e = 0; e < 2; e++)
+        if (lane + e * 64 < a.d) out[lane + e * 64] = T(v[e] * inverse);
+    if (a.lse && lane == 0) a.lse[int64_t(h) * a.rows + row] = total == 0.f ? -INFINITY : top * a.scale + logf(total);
 }
-bool words(std::initializer_list<const void*> all) {
-    for (const void* p : all)
-        if (reinterpret_cast<uintptr_t>(p) & 3) return false;
-    return true;
+
+// ---------------------------------------------------------------------------------------------------------------
+// Which kernel
+// ---------------------------------------------------------------------------------------------------------------
+struct Plan {
+    int blocks;             // of 16 rows: few rows; 0: many
+    int64_t tiles, chunk, chunks;
+};
+// By the rows that a sequence has on average (the host does not know each).  The keys are split where there are not enough workgroups.
+Plan plan_of(int64_t rows, int64_t heads, int64_t kv_heads, int64_t sequences, int64_t most_keys, bool split) {
+    const int64_t shared = kv_heads ? heads / kv_heads : 1, each = (rows + sequences - 1) / sequences * shared;
+    Plan p{each <= 16 ? 1 : each <= 32 ? 2 : each <= 64 ? 4 : 0, 0, 0, 1};
+    p.tiles = tiles_at_most(sequences, rows, shared, p.blocks == 1 ? 4 : p.blocks == 2 ? 5 : p.blocks == 4 ? 6 : MANY_SHIFT);
+    if (split) {
+        const int64_t groups = p.tiles * kv_heads, least = p.blocks ? 256 : 512, unit = 128;
+        int64_t chunk = (most_keys * groups / 2048 + unit - 1) / unit * unit;
+        chunk = chunk < least ? least : chunk;
+        if (chunk < most_keys) p.chunk = chunk, p.chunks = (most_keys + chunk - 1) / chunk;
+    }
+    return p;
+}
+
+template <typename T, typename KV> int attend(Attend<T, KV> a, const Plan& p, bool wide, hipStream_t s) {
+    const int64_t groups = p.tiles * a.kv_heads;
+    if (groups > MOST_SIZE || groups * 256 > UINT32_MAX) return CSR5_ERANGE;
+    a.tiles = int32_t(p.tiles), a.chunk = int32_t(p.chunk);
+    const dim3 grid(uint32_t(groups), uint32_t(p.chunks));
+    auto go = [&](auto nd, auto w) {
+        constexpr int ND = decltype(nd)::value, TILE = (ND <= 2 ? 64 : 128) * 2;
+        constexpr bool WIDE = decltype(w)::value;
+        auto few = [&](auto rb) {
+            constexpr int RB = decltype(rb)::value, ring = 16 * FEW_KEYS * TILE, join = 4 * 16 * RB * (ND * 32 + 4) * 4;
+            k_attend_few<T, KV, ND, WIDE, RB><<<grid, 256, ring > join ? ring : join, s>>>(a);
+        };
+        if (p.blocks == 1) few(std::integral_constant<int, 1>());
+        else if (p.blocks == 2) few(std::integral_constant<int, 2>());
+        else if (p.blocks == 4) few(std::integral_constant<int, 4>());
+        else k_attend_many<T, KV, ND, WIDE><<<grid, 256, 4 * MANY_KEYS * TILE, s>>>(a);
+    };
+    auto by = [&](auto nd) {
+        if (wide) go(nd, std::true_type());
+        else go(nd, std::false_type());
+    };
+    if (a.d <= 64) by(std::integral_constant<int, 2>());
+    else if (a.d <= 96) by(std::integral_constant<int, 3>());
+    else by(std::integral_constant<int, 4>());
+    if (p.chunk) k_join<T, KV><<<workgroups((int64_t(a.rows) * a.heads + 3) / 4), 256, 0, s>>>(a);
+    return launched();
 }
 
 }  // namespace
@@ -220,53 +543,31 @@ extern "C" {
 
 int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype, const int32_t* q_offset,
                    const int32_t* k_offset, float scale, int causal, csr5_heads_t q, csr5_heads_t k, csr5_heads_t v, csr5_heads_t out, float* lse, void* hip_stream) {
-    if (const int bad = sizes(sequences, rows, k_rows, heads, kv_heads, d, dtype, scale)) return bad;
+    if (const int bad = attention_sizes(sequences, rows, k_rows, heads, kv_heads, d, dtype, scale)) return bad;
     if (!heads_ok(q, rows, heads, d, 2) || !heads_ok(k, k_rows, kv_heads, d, 2) || !heads_ok(v, k_rows, kv_heads, d, 2) || !output_ok(out, rows, heads, d, 2)) return CSR5_EINVAL;
     if (!words({q_offset, k_offset, lse})) return CSR5_EINVAL;
     if (sequences == 0 || rows == 0 || heads == 0) return CSR5_OK;
     if (!q_offset || !k_offset) return CSR5_EINVAL;
-    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const Plan p = plan_of(rows, heads, kv_heads, sequences, k_rows, false);
+    const bool w = d % 8 == 0 && wide(q, 2) && wide(k, 2) && wide(v, 2) && wide(out, 2);
     return with_half(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const Attend<T, Packed<T>> a{sequences, rows, heads, heads / kv_heads, d, q_offset, scale, causal != 0, typed<const T>(q), {k_offset, k_rows, typed<const T>(k), typed<const T>(v)}, typed<T>(out), lse};
-        k_attend<T><<<workgroups(int64_t(rows) * heads), 64, 0, s>>>(a);
-        return launched();
+        const Attend<T, Packed<T>> a{sequences, rows, heads, kv_heads, heads / kv_heads, d, q_offset, scale, causal != 0, typed<const T>(q), {k_offset, k_rows, typed<const T>(k), typed<const T>(v)},
+                                     typed<T>(out), lse, 0, 0, nullptr, nullptr};
+        return attend(a, p, w, static_cast<hipStream_t>(hip_stream));
     });
 }
 
-size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads) { return rows <= 0 || heads <= 0 ? 0 : size_t(rows) * size_t(heads) * 4; }
-
-int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype, const int32_t* q_offset,
-                            const int32_t* k_offset, float scale, int causal, csr5_heads_t dout, csr5_heads_t q, csr5_heads_t k, csr5_heads_t v, csr5_heads_t out,
-                            const float* lse, csr5_heads_t dq, csr5_heads_t dk, csr5_heads_t dv, void* workspace, size_t workspace_bytes, void* hip_stream) {
-    if (const int bad = sizes(sequences, rows, k_rows, heads, kv_heads, d, dtype, scale)) return bad;
-    if (!heads_ok(q, rows, heads, d, 2) || !heads_ok(k, k_rows, kv_heads, d, 2) || !heads_ok(v, k_rows, kv_heads, d, 2) || !heads_ok(out, rows, heads, d, 2) ||
-        !heads_ok(dout, rows, heads, d, 2) || !output_ok(dq, rows, heads, d, 2) || !output_ok(dk, k_rows, kv_heads, d, 2) || !output_ok(dv, k_rows, kv_heads, d, 2))
-        return CSR5_EINVAL;
-    if (!words({q_offset, k_offset, lse, workspace})) return CSR5_EINVAL;
-    if (sequences == 0 || heads == 0 || d == 0) return CSR5_OK;
-    if (!q_offset || !k_offset || (rows > 0 && !lse)) return CSR5_EINVAL;
-    if (rows > 0 && (!workspace || workspace_bytes < csr5_attention_backward_workspace_bytes(rows, heads))) return CSR5_ENOMEM;
-    hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    return with_half(dtype, [&](auto zero) {
-        using T = decltype(zero);
-        const Back<T> a{sequences, rows, heads, heads / kv_heads, d, q_offset, scale, causal != 0, typed<const T>(dout), typed<const T>(q), typed<const T>(out),
-                        {k_offset, k_rows, typed<const T>(k), typed<const T>(v)}, lse, static_cast<float*>(workspace), typed<T>(dq), typed<T>(dk), typed<T>(dv)};
-        if (rows > 0) {
-            k_delta<T><<<workgroups((int64_t(rows) * heads + 63) / 64), 64, 0, s>>>(a);
-            k_attend_dq<T><<<workgroups(int64_t(rows) * heads), 64, 0, s>>>(a);
-        }
-        if (k_rows > 0) k_attend_dkv<T><<<workgroups(int64_t(k_rows) * kv_heads), 64, 0, s>>>(a);
-        return launched();
-    });
+size_t csr5_attention_paged_workspace_bytes(int32_t rows, int32_t heads, int32_t kv_heads, int32_t d, int32_t sequences, int64_t max_length) {
+    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d < 0 || sequences <= 0 || max_length < 0 || max_length > MOST_SIZE) return 0;
+    const Plan p = plan_of(rows, heads, kv_heads, sequences, max_length, true);
+    return p.chunk ? size_t(p.chunks) * size_t(rows) * size_t(heads) * size_t(d + 2) * 4 : 0;
 }
-
-size_t csr5_attention_paged_workspace_bytes(int32_t rows, int32_t heads, int32_t kv_heads, int32_t d, int32_t sequences, int64_t max_length) { return 0; }
 
 int csr5_attention_paged(int32_t sequences, int32_t rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype, const int32_t* q_offset, const int32_t* length,
                          const int32_t* table, int32_t width, int64_t ldt, int32_t pages, int32_t page, float scale, csr5_heads_t q, csr5_cache_t k_cache, csr5_cache_t v_cache,
                          csr5_heads_t out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
-    if (const int bad = sizes(sequences, rows, 0, heads, kv_heads, d, dtype, scale)) return bad;
+    if (const int bad = attention_sizes(sequences, rows, 0, heads, kv_heads, d, dtype, scale)) return bad;
     if (width < 0 || pages < 0 || !power_of_two(page)) return CSR5_EINVAL;
     if (int64_t(width) * page > MOST_SIZE) return CSR5_ERANGE;
     if (!heads_ok(q, rows, heads, d, 2) || !output_ok(out, rows, heads, d, 2) || !cache_ok(k_cache, pages, page, kv_heads, d, 2) || !cache_ok(v_cache, pages, page, kv_heads, d, 2) ||
@@ -275,14 +576,18 @@ int csr5_attention_paged(int32_t sequences, int32_t rows, int32_t heads, int32_t
     if (!words({q_offset, length, lse, workspace})) return CSR5_EINVAL;
     if (sequences == 0 || rows == 0 || heads == 0) return CSR5_OK;
     if (!q_offset || !length) return CSR5_EINVAL;
-    const size_t need = csr5_attention_paged_workspace_bytes(rows, heads, kv_heads, d, sequences, int64_t(width) * page);
+    const int64_t most = int64_t(width) * page;
+    const size_t need = csr5_attention_paged_workspace_bytes(rows, heads, kv_heads, d, sequences, most);
     if (need && (!workspace || workspace_bytes < need)) return CSR5_ENOMEM;
-    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const Plan p = plan_of(rows, heads, kv_heads, sequences, most, true);
+    const bool w = d % 8 == 0 && wide(q, 2) && wide(k_cache, 2) && wide(v_cache, 2) && wide(out, 2);
+    float* const part = static_cast<float*>(workspace);
+    float* const stats = p.chunk ? part + size_t(p.chunks) * size_t(rows) * size_t(heads) * size_t(d) : nullptr;
     return with_half(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const Attend<T, Paged<T>> a{sequences, rows, heads, heads / kv_heads, d, q_offset, scale, true, typed<const T>(q), {length, table, width, pages, __builtin_ctz(page), ldt, typed<const T>(k_cache), typed<const T>(v_cache)}, typed<T>(out), lse};
-        k_attend<T><<<workgroups(int64_t(rows) * heads), 64, 0, s>>>(a);
-        return launched();
+        const Attend<T, Paged<T>> a{sequences, rows, heads, kv_heads, heads / kv_heads, d, q_offset, scale, true, typed<const T>(q),
+                                    {length, table, width, pages, __builtin_ctz(page), ldt, typed<const T>(k_cache), typed<const T>(v_cache)}, typed<T>(out), lse, 0, 0, part, stats};
+        return attend(a, p, w, static_cast<hipStream_t>(hip_stream));
     });
 }
 
