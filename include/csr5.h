@@ -598,6 +598,7 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void *h, int
  * ========================================================================== */
 #define CSR5_ATTENTION_MAX_D 128
 #define CSR5_ATTENTION_MAX_HEADS 65535
+#define CSR5_ATTENTION_MAX_ROWS (1 << 30) /* queries, and keys */
 #define CSR5_ROTARY_MAX_D 512
 
 typedef struct { /* value c of head h of row i is at p[i*row + h*head + c] */
@@ -654,8 +655,8 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
  * over all its keys, or with causal != 0 those j <= i + n - m (the last query sees every key).  A row that sees
  * no key has out 0 and lse -inf.  Rows in no sequence are left as they are.
  *   q, out [rows][heads][d]; k, v [k_rows][kv_heads][d] in dtype (BF16, F16); lse float[heads][rows], or NULL
- * d <= CSR5_ATTENTION_MAX_D and heads <= CSR5_ATTENTION_MAX_HEADS, else CSR5_ERANGE; heads is a multiple
- * of kv_heads, scale positive and finite.
+ * d <= CSR5_ATTENTION_MAX_D, heads <= CSR5_ATTENTION_MAX_HEADS, rows and k_rows <= CSR5_ATTENTION_MAX_ROWS, else
+ * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite.
  * Softmax statistics and sums are held in 32 bits; p is rounded to dtype, relative to the largest so far, before it is
  * multiplied by v.
  */

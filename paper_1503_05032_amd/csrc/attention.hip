@@ -50,25 +50,6 @@ __device__ __forceinline__ float quarter_sum(float v) {
     const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return half_sum(__uint_as_float(both[0]) + __uint_as_float(both[1]));
 }
-__device__ __forceinline__ float power(float v) { return __builtin_amdgcn_exp2f(v); }
-
-// A row of the folded ones, its query and the keys that it sees.
-struct Row {
-    int32_t token, head, limit;
-    bool there;
-};
-__device__ __forceinline__ Row row_of(int64_t r, int32_t m, int32_t n, int32_t shared, bool causal) {
-    const int64_t count = int64_t(m) * shared, at = r < count ? r : count - 1;
-    Row x;
-    if (at >> 32) {
-        x.token = int32_t(at / shared), x.head = int32_t(at % shared);
-    } else {
-        x.token = int32_t(uint32_t(at) / uint32_t(shared)), x.head = int32_t(uint32_t(at) % uint32_t(shared));
-    }
-    x.limit = seen(causal, x.token, m, n), x.there = r < count;
-    return x;
-}
-
 // What a workgroup leaves of one row: the result, or its part of it.
 template <typename T, typename KV> struct Leave {
     T* out;
@@ -104,30 +85,6 @@ template <typename T, typename KV> struct Leave {
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int MANY_ROWS = 128, MANY_SHIFT = 7, MANY_KEYS = 64;
 
-// out += v^T p^T of a tile where some row does not see a key that others see, with values that are not finite among the tile's: a product
-// 0 * inf must not show.  Such values are left out, and what they do to the rows that see them is found by counting.
-template <typename T, int ND> __device__ __forceinline__ void careful(const vec<T, 8> (&p)[4], const uint32_t (&at)[ND], uint32_t row_bytes, int32_t key0, int32_t limit, f32x16 (&o)[ND]) {
-    const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-    for (int dt = 0; dt < ND; dt++) {
-        f32x16 up = {}, down = {};
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            __builtin_amdgcn_sched_barrier(0);      // one after the other: registers count, not time
-            vec<T, 8> v = turned_from<T>(at[dt] + k * 16 * row_bytes, 8 * row_bytes), u, w, see;
-            parted<T>(v, u, w);
-#pragma unroll
-            for (int e = 0; e < 8; e++) see[e] = T(key0 + k * 16 + (e / 4) * 8 + half * 4 + e % 4 < limit ? 1.f : 0.f);
-            o[dt] = product32(v, p[k], o[dt]), up = product32(u, see, up), down = product32(w, see, down);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            if (up[i] > 0.f) o[dt][i] += INFINITY;
-            if (down[i] > 0.f) o[dt][i] -= INFINITY;
-        }
-    }
-}
-
 template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_many(Attend<T, KV> a) {
     constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = MANY_KEYS / EACH / 4;
     extern __shared__ __align__(16) uint8_t lds[];
@@ -152,7 +109,7 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
         for (int kk = 0; kk < 2 * ND; kk++) q[kk] = eight_values<WIDE>(from + (2 * kk + half) * 8, row.there ? a.d - (2 * kk + half) * 8 : 0);
     }
     // which chunk of which row of a tile this lane brings
-    const int r0 = wave * EACH + lane / LANES, ck = int(chunk_at<D, BY_ROW>(r0, lane % LANES)) * 8, cv = int(chunk_at<D, BY_SEGMENT64>(r0, lane % LANES)) * 8;
+    const int r0 = wave * EACH + lane / LANES, ck = int(chunk_at<D, false>(r0, lane % LANES)) * 8, cv = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
     typename decltype(kv)::Ahead ahead[LOADS];
     auto look = [&](int32_t j0) {
 #pragma unroll
@@ -172,9 +129,9 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
     const int li = lane & 15, vr = half * 4 + (li >> 2);
     uint32_t k_at[2 * ND], v_at[ND];
 #pragma unroll
-    for (int kk = 0; kk < 2 * ND; kk++) k_at[kk] = (lane & 31) * D * 2 + chunk_at<D, BY_ROW>(lane & 31, 2 * kk + half) * 16;
+    for (int kk = 0; kk < 2 * ND; kk++) k_at[kk] = (lane & 31) * D * 2 + chunk_at<D, false>(lane & 31, 2 * kk + half) * 16;
 #pragma unroll
-    for (int dt = 0; dt < ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, BY_SEGMENT64>(vr, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+    for (int dt = 0; dt < ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, false>(vr, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
 
     const float c = a.scale * LOG2_E, rise = RISE / c;
     float base = -INFINITY, sum = 0.f;
@@ -202,7 +159,7 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
             for (int kb = 0; kb < 2; kb++)
 #pragma unroll
                 for (int i = 0; i < 16; i++)
-                    if (j0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4 >= row.limit) s[kb][i] = -INFINITY;
+                    s[kb][i] = or_none(s[kb][i], row.limit - 1 - (j0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4));
         float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
         for (int i = 1; i < 16; i++) top = fmaxf(fmaxf(s[0][i], s[1][i]), top);
@@ -226,23 +183,18 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
                 p[kb * 2 + i / 8][i % 8] = T(e);
             }
         if (some && least < min(j0 + MANY_KEYS, n)) {
-            u16x2 size = {0, 0};
-            for (int i = 0; i < TILE / 1024; i++) {
-                const uint4 w = __builtin_bit_cast(uint4, chunk_from<T>(tile + TILE + i * 1024 + lane * 16));
-                most_of(size, w.x), most_of(size, w.y), most_of(size, w.z), most_of(size, w.w);
-            }
-            if (__any(not_finite<T>(size))) {
+            if (any_not_finite<T>(tile + TILE, TILE)) {
                 uint32_t from[ND];
 #pragma unroll
                 for (int dt = 0; dt < ND; dt++) from[dt] = tile + v_at[dt];
-                careful<T, ND>(p, from, D * 2, j0, row.limit, o);
+                careful<2, true, D, T, ND>(p, from, o, [&](int k) { return row.limit - (j0 + k); });
                 continue;
             }
         }
 #pragma unroll
         for (int k = 0; k < 4; k++)
 #pragma unroll
-            for (int dt = 0; dt < ND; dt++) o[dt] = product32(turned_from<T>(tile + v_at[dt] + k * 16 * D * 2, 8 * D * 2), p[k], o[dt]);
+            for (int dt = 0; dt < ND; dt++) o[dt] = product32(turned32<D, T>(tile + v_at[dt] + k * 16 * D * 2), p[k], o[dt]);
     }
     own_landed<0>();
     sum = half_sum(sum);
@@ -302,7 +254,7 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
         for (int i = 0; i < LOADS; i++) {
             const int r = r0 + i * EACH;
             const int32_t j = j0 + r;
-            const int ck = int(chunk_at<D, BY_ROW>(r, lane % LANES)) * 8, cv = int(chunk_at<D, BY_SEGMENT32>(r, lane % LANES)) * 8;
+            const int ck = int(chunk_at<D, true>(r, lane % LANES)) * 8, cv = int(chunk_at<D, true>(r, lane % LANES)) * 8;
             const T *const k = kv.key(j, ahead[i]), *const v = kv.value(j, ahead[i]);
             chunk_to_lds<WIDE>(k ? k + ck : k, j < n ? a.d - ck : 0, to + i * 1024);
             chunk_to_lds<WIDE>(v ? v + cv : v, j < n ? a.d - cv : 0, to + TILE + i * 1024);
@@ -312,9 +264,9 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
     const int vr = quarter * 4 + (li >> 2);
     uint32_t k_at[ND], v_at[2 * ND];
 #pragma unroll
-    for (int kk = 0; kk < ND; kk++) k_at[kk] = li * D * 2 + chunk_at<D, BY_ROW>(li, 4 * kk + quarter) * 16;
+    for (int kk = 0; kk < ND; kk++) k_at[kk] = li * D * 2 + chunk_at<D, true>(li, 4 * kk + quarter) * 16;
 #pragma unroll
-    for (int dt = 0; dt < 2 * ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, BY_SEGMENT32>(vr, dt * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+    for (int dt = 0; dt < 2 * ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, true>(vr, dt * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
 
     const float c = a.scale * LOG2_E, rise = RISE / c;
     float base[RB], sum[RB];
@@ -351,7 +303,7 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
             if (some)
 #pragma unroll
                 for (int i = 0; i < 8; i++)
-                    if (j0 + i / 4 * 16 + quarter * 4 + i % 4 >= row[b].limit) s[b][i / 4][i % 4] = -INFINITY;
+                    s[b][i / 4][i % 4] = or_none(s[b][i / 4][i % 4], row[b].limit - 1 - (j0 + i / 4 * 16 + quarter * 4 + i % 4));
             float top = s[b][0][0];
 #pragma unroll
             for (int i = 1; i < 8; i++) top = fmaxf(top, s[b][i / 4][i % 4]);
@@ -372,19 +324,11 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
                 p[b][i] = T(e);
             }
         }
-        bool bad = false;
-        if (some && least < min(j0 + FEW_KEYS, n)) {
-            u16x2 size = {0, 0};
-            for (int i = 0; i < TILE / 1024; i++) {
-                const uint4 w = __builtin_bit_cast(uint4, chunk_from<T>(tile + TILE + i * 1024 + lane * 16));
-                most_of(size, w.x), most_of(size, w.y), most_of(size, w.z), most_of(size, w.w);
-            }
-            bad = __any(not_finite<T>(size));
-        }
+        const bool bad = some && least < min(j0 + FEW_KEYS, n) && any_not_finite<T>(tile + TILE, TILE);
         if (!bad) {
 #pragma unroll
             for (int dt = 0; dt < 2 * ND; dt++) {
-                const vec<T, 8> v = turned_from<T>(tile + v_at[dt], 16 * D * 2);
+                const vec<T, 8> v = turned_from<T>(tile + v_at[dt], tile + v_at[dt] + 16 * D * 2);
 #pragma unroll
                 for (int b = 0; b < RB; b++) o[b][dt] = product16(v, p[b], o[b][dt]);
             }
@@ -392,19 +336,21 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
 #pragma unroll
             for (int dt = 0; dt < 2 * ND; dt++) {
                 __builtin_amdgcn_sched_barrier(0);
-                vec<T, 8> v = turned_from<T>(tile + v_at[dt], 16 * D * 2), u, w, see;
+                vec<T, 8> v = turned_from<T>(tile + v_at[dt], tile + v_at[dt] + 16 * D * 2), u, w;
                 parted<T>(v, u, w);
 #pragma unroll
                 for (int b = 0; b < RB; b++) {
+                    uint32_t sees[4];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) see[e] = T(j0 + e / 4 * 16 + quarter * 4 + e % 4 < row[b].limit ? 1.f : 0.f);
+                    for (int e = 0; e < 4; e++) {
+                        const int32_t j = j0 + e / 2 * 16 + quarter * 4 + e % 2 * 2;
+                        sees[e] = one_if<T>(row[b].limit - j) | one_if<T>(row[b].limit - j - 1) << 16;
+                    }
+                    const vec<T, 8> see = __builtin_bit_cast(vec<T, 8>, make_uint4(sees[0], sees[1], sees[2], sees[3]));
                     o[b][dt] = product16(v, p[b], o[b][dt]);
                     const f32x4 none = {}, up = product16(u, see, none), down = product16(w, see, none);
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        if (up[i] > 0.f) o[b][dt][i] += INFINITY;
-                        if (down[i] > 0.f) o[b][dt][i] -= INFINITY;
-                    }
+                    for (int i = 0; i < 4; i++) o[b][dt][i] += counted<true>(up[i], down[i]);
                 }
             }
         }
@@ -559,7 +505,7 @@ int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t head
 }
 
 size_t csr5_attention_paged_workspace_bytes(int32_t rows, int32_t heads, int32_t kv_heads, int32_t d, int32_t sequences, int64_t max_length) {
-    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d < 0 || sequences <= 0 || max_length < 0 || max_length > MOST_SIZE) return 0;
+    if (rows <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d < 0 || sequences <= 0 || max_length < 0 || max_length > CSR5_ATTENTION_MAX_ROWS) return 0;
     const Plan p = plan_of(rows, heads, kv_heads, sequences, max_length, true);
     return p.chunk ? size_t(p.chunks) * size_t(rows) * size_t(heads) * size_t(d + 2) * 4 : 0;
 }
@@ -569,7 +515,7 @@ int csr5_attention_paged(int32_t sequences, int32_t rows, int32_t heads, int32_t
                          csr5_heads_t out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (const int bad = attention_sizes(sequences, rows, 0, heads, kv_heads, d, dtype, scale)) return bad;
     if (width < 0 || pages < 0 || !power_of_two(page)) return CSR5_EINVAL;
-    if (int64_t(width) * page > MOST_SIZE) return CSR5_ERANGE;
+    if (int64_t(width) * page > CSR5_ATTENTION_MAX_ROWS) return CSR5_ERANGE;
     if (!heads_ok(q, rows, heads, d, 2) || !output_ok(out, rows, heads, d, 2) || !cache_ok(k_cache, pages, page, kv_heads, d, 2) || !cache_ok(v_cache, pages, page, kv_heads, d, 2) ||
         !rows_ok(table, sequences, ldt, width, 4))
         return CSR5_EINVAL;

@@ -1,123 +1,278 @@
 // libcsr5: the gradients of attention over packed sequences.  The C ABI is declared in include/csr5.h.
+//
+// With p = 2^(c q.k - lse log2 e), c = scale log2 e, and ds = p (dout.v - delta), delta = dout.out:
+//   dv = p^T dout,  dk = scale ds^T q  by workgroups that have keys and go through the queries,
+//   dq = scale ds k                    by workgroups that have queries and go through the keys,
+// so that every sum has one owner and one order; p is computed in both: seven products for the five that there are with one pass, whose dq would
+// be added up between workgroups.  p and ds are, rounded, the second operands of the next products as the lanes have them, as in attention.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "csr5.h"
 #include "heads.h"
 #include "numbers.h"
 #include "sequences.h"
+#include "to_lds.h"
 
 namespace {
 
-// The sequence that row i lies in, by bisection; -1: none.
-__device__ __forceinline__ int32_t sequence_of(const int32_t* offset, int32_t sequences, int32_t rows, int32_t i) {
-    int32_t low = 0, high = sequences;
-    while (high - low > 1) {
-        const int32_t mid = low + (high - low) / 2;
-        if (offset[mid] <= i) low = mid;
-        else high = mid;
-    }
-    const Span s = span_of(offset, low, rows);
-    return i >= s.first && i < s.first + s.count ? low : -1;
-}
-
-template <typename T> __device__ __forceinline__ float dot(const T* a, const T* b, int d) {
-    float sum = 0.f;
-    if (b)
-        for (int c = 0; c < d; c++) sum = fmaf(float(a[c]), float(b[c]), sum);
-    return sum;
-}
 template <typename T> struct Back {
-    int32_t sequences, rows, heads, shared, d;
-    const int32_t* q_offset;
+    int32_t sequences, rows, k_rows, heads, kv_heads, shared, d;
+    const int32_t *q_offset, *k_offset;
     float scale;
     bool causal;
-    Heads<const T> dout, q, out;
-    Packed<T> kv;
+    Heads<const T> dout, q, out, k, v;
     const float* lse;
-    float* delta;               // [heads][rows]
+    float *delta, *base;        // [heads][rows]: dout . out, and lse log2 e
     Heads<T> dq, dk, dv;
+    int32_t tiles;
 };
 
-template <typename T> __global__ __launch_bounds__(64) void k_delta(Back<T> a) {
-    const int64_t at = workgroup() * 64 + threadIdx.x;
-    if (at >= int64_t(a.rows) * a.heads) return;
-    const int32_t row = int32_t(at % a.rows), h = int32_t(at / a.rows);
-    a.delta[at] = dot(a.dout.p + row * a.dout.row + h * a.dout.head, a.out.p + row * a.out.row + h * a.out.head, a.d);
+// ---------------------------------------------------------------------------------------------------------------
+// delta and base: D / 8 lanes to a row and head.  Bound by memory.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T, int LANES, bool WIDE> __global__ __launch_bounds__(256) void k_delta(Back<T> a) {
+    const int64_t at = workgroup() * (256 / LANES) + threadIdx.x / LANES;
+    const int c = threadIdx.x % LANES * 8;
+    const bool there = at < int64_t(a.rows) * a.heads;
+    const int64_t row = there ? at / a.heads : 0, h = there ? at % a.heads : 0;
+    float x[8], y[8], sum = 0.f;
+    load_values<8, WIDE>(a.dout.p + row * a.dout.row + h * a.dout.head + c, there ? a.d - c : 0, x);
+    load_values<8, WIDE>(a.out.p + row * a.out.row + h * a.out.head + c, there ? a.d - c : 0, y);
+#pragma unroll
+    for (int e = 0; e < 8; e++) sum = fmaf(x[e], y[e], sum);
+    sum = lanes_sum<LANES>(sum);
+    if (there && c == 0) a.delta[h * a.rows + row] = sum, a.base[h * a.rows + row] = a.lse[h * a.rows + row] * LOG2_E;
 }
 
-// One wavefront per row and head.
-template <typename T> __global__ __launch_bounds__(64) void k_attend_dq(Back<T> a) {
-    const int64_t at = workgroup();
-    if (at >= int64_t(a.rows) * a.heads) return;
-    const int32_t row = int32_t(at / a.heads), h = int32_t(at % a.heads), hk = h / a.shared, lane = threadIdx.x;
-    const int32_t s = sequence_of(a.q_offset, a.sequences, a.rows, row);
-    if (s < 0) return;
-    const Span mine = span_of(a.q_offset, s, a.rows), keys = span_of(a.kv.offset, s, a.kv.rows);
-    const int32_t n = seen(a.causal, row - mine.first, mine.count, keys.count);
-    const float lse = a.lse[int64_t(h) * a.rows + row], delta = a.delta[int64_t(h) * a.rows + row];
-    float acc[2] = {0.f, 0.f};
-    for (int32_t j0 = 0; j0 < n; j0 += 64) {
-        const int32_t j = j0 + lane;
-        float ds = 0.f;
-        if (j < n) {
-            const float p = expf(a.scale * dot(a.q.p + row * a.q.row + h * a.q.head, (a.kv.k.p + (keys.first + j) * a.kv.k.row + hk * a.kv.k.head), a.d) - lse);
-            ds = p * (dot(a.dout.p + row * a.dout.row + h * a.dout.head, (a.kv.v.p + (keys.first + j) * a.kv.v.row + hk * a.kv.v.head), a.d) - delta);
+// Where a wavefront reads tiles of 64 rows of LDS for products of 32 x 32 x 16: rows as first operands, and turned.
+template <int ND> struct Read {
+    static constexpr int D = ND <= 2 ? 64 : 128;
+    uint32_t row[2 * ND], turned[ND];
+    __device__ __forceinline__ Read() {
+        const int lane = threadIdx.x & 63, half = lane >> 5, li = lane & 15, r = half * 4 + (li >> 2);
+#pragma unroll
+        for (int kk = 0; kk < 2 * ND; kk++) row[kk] = (lane & 31) * D * 2 + chunk_at<D, false>(lane & 31, 2 * kk + half) * 16;
+#pragma unroll
+        for (int dt = 0; dt < ND; dt++) turned[dt] = r * D * 2 + chunk_at<D, false>(r, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+    }
+};
+
+// A head's values of this lane's column, for second operands.
+template <int ND, bool WIDE, typename T> __device__ __forceinline__ void column(vec<T, 8> (&to)[2 * ND], const T* from, bool there, int d) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int kk = 0; kk < 2 * ND; kk++) to[kk] = eight_values<WIDE>(from + (2 * kk + half) * 8, there ? d - (2 * kk + half) * 8 : 0);
+}
+// A column of a result that lies as [values][columns].
+template <int ND, bool WIDE, typename T> __device__ __forceinline__ void leave(T* to, const f32x16 (&acc)[ND], float scale, int d) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int c = dt * 32 + i * 8 + half * 4;
+            const float v[4] = {acc[dt][4 * i] * scale, acc[dt][4 * i + 1] * scale, acc[dt][4 * i + 2] * scale, acc[dt][4 * i + 3] * scale};
+            store_values<4, WIDE>(to + c, d - c, v);
         }
-        for (int e = 0; e < min(64, n - j0); e++) {
-            const float w = __shfl(ds, e);
-            const T* const k = a.kv.k.p + (keys.first + j0 + e) * a.kv.k.row + hk * a.kv.k.head;
-            for (int i = 0; i < 2; i++)
-                if (i * 64 + lane < a.d) acc[i] = fmaf(w, float(k[i * 64 + lane]), acc[i]);
+}
+
+constexpr int BACK_ROWS = 128, BACK_SHIFT = 7, BACK_STEP = 64;
+
+// ---------------------------------------------------------------------------------------------------------------
+// dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 64.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = BACK_STEP * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = BACK_STEP / EACH / 4;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int32_t hk = blockIdx.x % a.kv_heads;
+    TileOf at;
+    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, BACK_SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
+    const Span keys = span_of(a.k_offset, at.s, a.k_rows);
+    const int32_t m = at.rows.count, n = keys.count;
+    const Row row = row_of(at.first + wave * 32 + (lane & 31), m, n, a.shared, a.causal);
+    const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
+    const int32_t end = __builtin_amdgcn_readfirstlane(row_of(at.first + BACK_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int64_t token = at.rows.first + row.token;
+    const int h = hk * a.shared + row.head;
+    vec<T, 8> q[2 * ND], dout[2 * ND];
+    column<ND, WIDE>(q, a.q.p + token * a.q.row + h * a.q.head, row.there, a.d);
+    column<ND, WIDE>(dout, a.dout.p + token * a.dout.row + h * a.dout.head, row.there, a.d);
+    const float delta = a.delta[int64_t(h) * a.rows + token], base = a.base[int64_t(h) * a.rows + token], c = a.scale * LOG2_E;
+
+    const int r0 = wave * EACH + lane / LANES, chunk = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
+    const T *const k0 = same(a.k.p + keys.first * a.k.row + hk * a.k.head), *const v0 = same(a.v.p + keys.first * a.v.row + hk * a.v.head);
+    auto bring = [&](int32_t j0, uint8_t* to) {
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int32_t j = j0 + r0 + i * 4 * EACH;
+            const int have = j < n ? a.d - chunk : 0;
+            chunk_to_lds<WIDE>(k0 + j * a.k.row + chunk, have, to + (i * 4 + wave) * 1024);
+            chunk_to_lds<WIDE>(v0 + j * a.v.row + chunk, have, to + TILE + (i * 4 + wave) * 1024);
+        }
+    };
+    const uint32_t lds0 = lds_address(lds);
+    const Read<ND> read;
+    f32x16 dq[ND] = {};
+    bring(0, lds);
+    int now = 0;
+    for (int32_t j0 = 0; j0 < end; j0 += BACK_STEP, now ^= 1) {
+        landed<0>();
+        if (j0 + BACK_STEP < end) bring(j0 + BACK_STEP, lds + (now ^ 1) * 2 * TILE);
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) {
+            const int32_t j = j0 + kb * 32;
+            if (j >= most) break;
+            const uint32_t tile = lds0 + now * 2 * TILE + kb * 32 * D * 2;
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), q[kk], s);
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), dout[kk], dp);
+            const bool some = j + 32 > least;       // some row does not see some key
+            vec<T, 8> ds[2];
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                s[i] = power(fmaf(s[i], c, -base)) * (dp[i] - delta);
+            }
+            if (some) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (j + 8 * (i / 4) + 4 * half + i % 4));
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++) ds[i / 8][i % 8] = T(s[i]);
+            if (some && least < min(j + 32, n) && any_not_finite<T>(tile, 32 * D * 2)) {
+                uint32_t from[ND];
+#pragma unroll
+                for (int dt = 0; dt < ND; dt++) from[dt] = tile + read.turned[dt];
+                careful<1, false, D, T, ND>(ds, from, dq, [&](int k) { return row.limit - (j + k); });
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+#pragma unroll
+                    for (int dt = 0; dt < ND; dt++) dq[dt] = product32(turned32<D, T>(tile + read.turned[dt] + k * 16 * D * 2), ds[k], dq[dt]);
+            }
         }
     }
-    for (int i = 0; i < 2; i++)
-        if (i * 64 + lane < a.d) a.dq.p[row * a.dq.row + h * a.dq.head + i * 64 + lane] = T(a.scale * acc[i]);
+    own_landed<0>();
+    if (row.there) leave<ND, WIDE>(a.dq.p + token * a.dq.row + h * a.dq.head, dq, a.scale, a.d);
 }
 
-// One wavefront per key and head of keys; the query heads that share it one after the other.
-template <typename T> __global__ __launch_bounds__(64) void k_attend_dkv(Back<T> a) {
-    const int64_t at = workgroup();
-    const int32_t kv_heads = a.heads / a.shared;
-    if (at >= int64_t(a.kv.rows) * kv_heads) return;
-    const int32_t row = int32_t(at / kv_heads), hk = int32_t(at % kv_heads), lane = threadIdx.x;
-    const int32_t s = sequence_of(a.kv.offset, a.sequences, a.kv.rows, row);
-    if (s < 0) return;
-    const Span mine = span_of(a.q_offset, s, a.rows), keys = span_of(a.kv.offset, s, a.kv.rows);
-    const int32_t j = row - keys.first, from = a.causal ? max(0, j - (keys.count - mine.count)) : 0;     // the first query that sees it
-    float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
-    for (int g = 0; g < a.shared; g++) {
-        const int h = hk * a.shared + g;
-        for (int32_t i0 = from; i0 < mine.count; i0 += 64) {
-            const int32_t i = i0 + lane, r = mine.first + i;
-            float p = 0.f, ds = 0.f;
-            if (i < mine.count) {
-                p = expf(a.scale * dot(a.q.p + r * a.q.row + h * a.q.head, (a.kv.k.p + (keys.first + j) * a.kv.k.row + hk * a.kv.k.head), a.d) - a.lse[int64_t(h) * a.rows + r]);
-                ds = p * (dot(a.dout.p + r * a.dout.row + h * a.dout.head, (a.kv.v.p + (keys.first + j) * a.kv.v.row + hk * a.kv.v.head), a.d) - a.delta[int64_t(h) * a.rows + r]);
-            }
-            for (int e = 0; e < min(64, mine.count - i0); e++) {
-                const float w = __shfl(p, e), u = __shfl(ds, e);
-                const int64_t q = mine.first + i0 + e;
-                for (int c = lane; c < a.d; c += 64) {
-                    dv[c / 64] = fmaf(w, float(a.dout.p[q * a.dout.row + h * a.dout.head + c]), dv[c / 64]);
-                    dk[c / 64] = fmaf(u, float(a.q.p[q * a.q.row + h * a.q.head + c]), dk[c / 64]);
+// ---------------------------------------------------------------------------------------------------------------
+// dk and dv: 128 keys, 32 to each wavefront, which go through the queries that see them in tiles of 64, head by head of those that share the
+// keys.  Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
+// ---------------------------------------------------------------------------------------------------------------
+template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) void k_attend_dkv(Back<T> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = BACK_STEP * D * 2, STAGE = 2 * TILE + 512, LANES = D / 8, EACH = 64 / LANES, LOADS = BACK_STEP / EACH / 4;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int32_t hk = blockIdx.x % a.kv_heads;
+    TileOf at;
+    if (!tile_of(a.k_offset, a.sequences, a.k_rows, 1, BACK_SHIFT, blockIdx.x / a.kv_heads, at)) return;
+    const Span mine = span_of(a.q_offset, at.s, a.rows);
+    const int32_t m = mine.count, n = at.rows.count, first = int32_t(at.first) + wave * 32, key = first + (lane & 31);
+    const bool there = key < n;
+    const int64_t token = at.rows.first + min(key, n - 1);
+    vec<T, 8> k[2 * ND], v[2 * ND];
+    column<ND, WIDE>(k, a.k.p + token * a.k.row + hk * a.k.head, there, a.d);
+    column<ND, WIDE>(v, a.v.p + token * a.v.row + hk * a.v.head, there, a.d);
+    const float c = a.scale * LOG2_E;
+    // query i sees key j where j <= i + ahead
+    const int32_t ahead = a.causal ? n - m : n;         // sums of two are below 2^31
+    const int32_t start = max(0, int32_t(at.first) - ahead) / BACK_STEP * BACK_STEP, steps = m > start ? (m - start + BACK_STEP - 1) / BACK_STEP : 0;
+
+    const int r0 = wave * EACH + lane / LANES, chunk = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
+    auto bring = [&](int32_t step, uint8_t* to) {
+        const int h = hk * a.shared + step / steps;
+        const int32_t i0 = start + step % steps * BACK_STEP;
+        const T *const q0 = a.q.p + mine.first * a.q.row + h * a.q.head, *const o0 = a.dout.p + mine.first * a.dout.row + h * a.dout.head;
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int32_t r = i0 + r0 + i * 4 * EACH;
+            const int have = r < m ? a.d - chunk : 0;
+            chunk_to_lds<WIDE>(q0 + r * a.q.row + chunk, have, to + (i * 4 + wave) * 1024);
+            chunk_to_lds<WIDE>(o0 + r * a.dout.row + chunk, have, to + TILE + (i * 4 + wave) * 1024);
+        }
+        if (wave < 2) {
+            const float* const from = (wave ? a.delta : a.base) + int64_t(h) * a.rows + mine.first + i0 + lane;
+            word_to_lds(i0 + lane < m ? static_cast<const void*>(from) : &ZEROS, to + 2 * TILE + wave * 256);
+        }
+    };
+    const uint32_t lds0 = lds_address(lds);
+    const Read<ND> read;
+    f32x16 dk[ND] = {}, dv[ND] = {};
+    const int32_t total = steps * a.shared;
+    if (total > 0) bring(0, lds);
+    int now = 0;
+    int32_t i0 = start;
+    for (int32_t step = 0; step < total; step++, now ^= 1, i0 = i0 + BACK_STEP < m ? i0 + BACK_STEP : start) {
+        landed<0>();
+        if (step + 1 < total) bring(step + 1, lds + (now ^ 1) * STAGE);
+#pragma unroll
+        for (int rb = 0; rb < 2; rb++) {
+            const int32_t i = i0 + rb * 32;
+            if (i >= m || i + 31 + ahead < first) continue;         // no query, or none that sees one of these keys
+            const uint32_t tile = lds0 + now * STAGE + rb * 32 * D * 2, words = lds0 + now * STAGE + 2 * TILE + rb * 128 + half * 16;
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), k[kk], s);
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), v[kk], dp);
+            const bool hidden = i + ahead < first + 31, some = hidden || i + 32 > m;      // some query does not see some key; or there is none
+            vec<T, 8> p[2], ds[2];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const f32x4 base = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + e * 32), delta = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + 256 + e * 32);
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    const int w = e * 4 + u;
+                    s[w] = power(fmaf(s[w], c, -base[u])), dp[w] = s[w] * (dp[w] - delta[u]);
                 }
             }
+            if (some) {
+#pragma unroll
+                for (int w = 0; w < 16; w++) {
+                    const int32_t r = i + 8 * (w / 4) + 4 * half + w % 4, unseen = (m - 1 - r) | (r + ahead - key);
+                    s[w] = or_zero(s[w], unseen), dp[w] = or_zero(dp[w], unseen);
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < 16; w++) p[w / 8][w % 8] = T(s[w]), ds[w / 8][w % 8] = T(dp[w]);
+            if (hidden && (any_not_finite<T>(tile, 32 * D * 2) || any_not_finite<T>(tile + TILE, 32 * D * 2))) {
+                uint32_t from[ND];
+                auto see = [&](int r) { return min(m - (i + r), i + r + ahead - key + 1); };
+#pragma unroll
+                for (int dt = 0; dt < ND; dt++) from[dt] = tile + TILE + read.turned[dt];
+                careful<1, true, D, T, ND>(p, from, dv, see);
+#pragma unroll
+                for (int dt = 0; dt < ND; dt++) from[dt] = tile + read.turned[dt];
+                careful<1, false, D, T, ND>(ds, from, dk, see);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int dt = 0; dt < ND; dt++) {
+                        dv[dt] = product32(turned32<D, T>(tile + TILE + read.turned[dt] + x * 16 * D * 2), p[x], dv[dt]);
+                        dk[dt] = product32(turned32<D, T>(tile + read.turned[dt] + x * 16 * D * 2), ds[x], dk[dt]);
+                    }
+            }
         }
     }
-    for (int c = lane; c < a.d; c += 64) {
-        a.dk.p[row * a.dk.row + hk * a.dk.head + c] = T(a.scale * dk[c / 64]);
-        a.dv.p[row * a.dv.row + hk * a.dv.head + c] = T(dv[c / 64]);
-    }
+    own_landed<0>();
+    if (!there) return;
+    leave<ND, WIDE>(a.dk.p + token * a.dk.row + hk * a.dk.head, dk, a.scale, a.d);
+    leave<ND, WIDE>(a.dv.p + token * a.dv.row + hk * a.dv.head, dv, 1.f, a.d);
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads) { return rows <= 0 || heads <= 0 ? 0 : size_t(rows) * size_t(heads) * 4; }
+size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads) { return rows <= 0 || heads <= 0 ? 0 : size_t(rows) * size_t(heads) * 8; }
 
 int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype, const int32_t* q_offset,
                             const int32_t* k_offset, float scale, int causal, csr5_heads_t dout, csr5_heads_t q, csr5_heads_t k, csr5_heads_t v, csr5_heads_t out,
@@ -127,19 +282,34 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
         !heads_ok(dout, rows, heads, d, 2) || !output_ok(dq, rows, heads, d, 2) || !output_ok(dk, k_rows, kv_heads, d, 2) || !output_ok(dv, k_rows, kv_heads, d, 2))
         return CSR5_EINVAL;
     if (!words({q_offset, k_offset, lse, workspace})) return CSR5_EINVAL;
-    if (sequences == 0 || heads == 0 || d == 0) return CSR5_OK;
+    if (sequences == 0 || heads == 0 || d == 0 || (rows == 0 && k_rows == 0)) return CSR5_OK;
     if (!q_offset || !k_offset || (rows > 0 && !lse)) return CSR5_EINVAL;
     if (rows > 0 && (!workspace || workspace_bytes < csr5_attention_backward_workspace_bytes(rows, heads))) return CSR5_ENOMEM;
+    const int64_t q_tiles = tiles_at_most(sequences, rows, heads / kv_heads, BACK_SHIFT), k_tiles = tiles_at_most(sequences, k_rows, 1, BACK_SHIFT);
+    if (q_tiles * kv_heads * 256 > UINT32_MAX || k_tiles * kv_heads * 256 > UINT32_MAX) return CSR5_ERANGE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const bool w = d % 8 == 0 && wide(q, 2) && wide(k, 2) && wide(v, 2) && wide(out, 2) && wide(dout, 2) && wide(dq, 2) && wide(dk, 2) && wide(dv, 2);
     return with_half(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const Back<T> a{sequences, rows, heads, heads / kv_heads, d, q_offset, scale, causal != 0, typed<const T>(dout), typed<const T>(q), typed<const T>(out),
-                        {k_offset, k_rows, typed<const T>(k), typed<const T>(v)}, lse, static_cast<float*>(workspace), typed<T>(dq), typed<T>(dk), typed<T>(dv)};
-        if (rows > 0) {
-            k_delta<T><<<workgroups((int64_t(rows) * heads + 63) / 64), 64, 0, s>>>(a);
-            k_attend_dq<T><<<workgroups(int64_t(rows) * heads), 64, 0, s>>>(a);
-        }
-        if (k_rows > 0) k_attend_dkv<T><<<workgroups(int64_t(k_rows) * kv_heads), 64, 0, s>>>(a);
+        float* const delta = static_cast<float*>(workspace);
+        const Back<T> a{sequences, rows, k_rows, heads, kv_heads, heads / kv_heads, d, q_offset, k_offset, scale, causal != 0, typed<const T>(dout), typed<const T>(q), typed<const T>(out),
+                        typed<const T>(k), typed<const T>(v), lse, delta, delta + size_t(rows) * size_t(heads), typed<T>(dq), typed<T>(dk), typed<T>(dv), int32_t(q_tiles)};
+        auto go = [&](auto nd, auto is_wide) {
+            constexpr int ND = decltype(nd)::value, D = ND <= 2 ? 64 : 128;
+            constexpr bool WIDE = decltype(is_wide)::value;
+            if (rows > 0) {
+                k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
+                k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2, s>>>(a);
+            }
+            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2 + 1024, s>>>(a);
+        };
+        auto by = [&](auto nd) {
+            if (w) go(nd, std::true_type());
+            else go(nd, std::false_type());
+        };
+        if (d <= 64) by(std::integral_constant<int, 2>());
+        else if (d <= 96) by(std::integral_constant<int, 3>());
+        else by(std::integral_constant<int, 4>());
         return launched();
     });
 }

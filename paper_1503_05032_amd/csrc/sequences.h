@@ -109,6 +109,25 @@ template <typename T> struct Paged {
 // Keys that query i of m sees, of n.
 __device__ __forceinline__ int32_t seen(bool causal, int32_t i, int32_t m, int32_t n) { return causal ? min(max(n - m + i + 1, 0), n) : n; }
 
+__device__ __forceinline__ float power(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// A row of the folded ones, its query and the keys that it sees.
+struct Row {
+    int32_t token, head, limit;
+    bool there;
+};
+__device__ __forceinline__ Row row_of(int64_t r, int32_t m, int32_t n, int32_t shared, bool causal) {
+    const int64_t count = int64_t(m) * shared, at = r < count ? r : count - 1;
+    Row x;
+    if (at >> 32) {
+        x.token = int32_t(at / shared), x.head = int32_t(at % shared);
+    } else {
+        x.token = int32_t(uint32_t(at) / uint32_t(shared)), x.head = int32_t(uint32_t(at) % uint32_t(shared));
+    }
+    x.limit = seen(causal, x.token, m, n), x.there = r < count;
+    return x;
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // Matrix instructions, 16 bits in and 32 out.  Of 32 x 32 x 16 (16 x 16 x 32) a lane has row (column) lane % 32 (16) of the first
 // (second) operand, values 8 * (lane / 32 (16)) to + 7 of the depth; of the result column lane % 32 (16), and rows 8 * (i / 4) + 4 * (lane / 32) + i % 4
@@ -121,29 +140,32 @@ __device__ __forceinline__ f32x4 product16(vec<f16, 8> a, vec<f16, 8> b, f32x4 c
 
 // ---------------------------------------------------------------------------------------------------------------
 // Tiles in LDS: rows of D values (64 or 128), 16-byte chunks c of row r swizzled so that the 64 banks are read evenly.
-//   rows are read (the first operand of a product over d, 16 or 32 rows' chunk c): c ^ r over 256 bytes
-//   columns are read (over the rows: transposing reads of 4 rows x 16 values by 16 lanes): segments of 64 bytes (32 x 32 x 16: half
-//   a wavefront reads 4 rows' segment) or 32 bytes (16 x 16 x 32: 8 rows' segment), segment g ^ r over 256 bytes
+//   rows are read (the first operand of a product over d): 16 rows' chunk c has to be in 16 places
+//   columns are read (over the rows: transposing reads of 4 rows x 16 values by 16 lanes): for 32 x 32 x 16 half a wavefront reads 64 bytes
+//   of 4 rows, chunks 4g to 4g + 3; for 16 x 16 x 32 32 bytes of 8 rows, chunks 2g and 2g + 1
+// SMALL false: c ^ (r % 4, r / 4 % 4) (as four bits) is both, for 32 x 32 x 16; true: c ^ (r % 8, r / 8 % 2), for 16 x 16 x 32.  Rows of 128 bytes have
+// r / 2 for r, and the two of a pair are next to each other.
 // ---------------------------------------------------------------------------------------------------------------
-enum { BY_ROW, BY_SEGMENT64, BY_SEGMENT32 };
-template <int D, int HOW> __device__ __forceinline__ uint32_t chunk_at(int r, int c) {      // where chunk c is in row r, in chunks; its own inverse
-    if (HOW == BY_ROW) return D == 128 ? c ^ (r & 15) : c ^ (r >> 1 & 7);
-    if (HOW == BY_SEGMENT64) return D == 128 ? c ^ ((r & 3) << 2) : c ^ ((r >> 1 & 1) << 2);
-    return D == 128 ? c ^ ((r & 7) << 1) : c ^ ((r >> 1 & 3) << 1);
+template <int D, bool SMALL> __device__ __forceinline__ uint32_t chunk_at(int r, int c) {      // where chunk c is in row r, in chunks; its own inverse
+    if (D == 128) return SMALL ? c ^ ((r & 7) << 1 | (r >> 3 & 1)) : c ^ ((r & 3) << 2 | (r >> 2 & 3));
+    return SMALL ? c ^ ((r >> 1 & 3) << 1 | (r >> 3 & 1)) : c ^ ((r >> 1 & 1) << 2 | (r >> 2 & 3));
 }
 
 template <typename T> __device__ __forceinline__ vec<T, 8> chunk_from(uint32_t at) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(vec<T, 8>, *(const __attribute__((address_space(3))) u32x4*)uintptr_t(at));
 }
-// Rows `at` and those `further` bytes on, four rows each of 16 columns, as a lane's eight values of one column.
-template <typename T> __device__ __forceinline__ vec<T, 8> turned_from(uint32_t at, uint32_t further) {
+// The rows at `at` and those at `other`, four rows each of 16 columns, as a lane's eight values of one column.
+template <typename T> __device__ __forceinline__ vec<T, 8> turned_from(uint32_t at, uint32_t other) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-    const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at)), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at + further));
+    const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(at)), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)uintptr_t(other));
     const uint2 a = __builtin_bit_cast(uint2, low), b = __builtin_bit_cast(uint2, high);
     return __builtin_bit_cast(vec<T, 8>, make_uint4(a.x, a.y, b.x, b.y));
 }
+
+// For 32 x 32 x 16: columns of four rows and of those 8 rows on, where bit 1 of a chunk's place is the other one.
+template <int D, typename T> __device__ __forceinline__ vec<T, 8> turned32(uint32_t at) { return turned_from<T>(at, (at ^ 32) + 8 * D * 2); }
 
 // One wavefront's load into LDS: 1024 bytes, lane by lane 16 of them; `from` NULL, or values from `have` on: zeros.
 template <bool WIDE, typename T> __device__ __forceinline__ void chunk_to_lds(const T* from, int have, uint8_t* to) {
@@ -160,19 +182,69 @@ __device__ __forceinline__ void most_of(u16x2& most, uint32_t w) {
 }
 template <typename T> __device__ __forceinline__ bool not_finite(u16x2 most) { return most[0] >= NOT_FINITE<T> || most[1] >= NOT_FINITE<T>; }
 
-// v without what is not finite; up: 1 where it is +inf or NaN, down: where it is -inf or NaN.
-// (By whole vectors of words: a bit cast of one element takes the first one for all with this compiler.)
+template <typename T> constexpr uint32_t ONE = std::is_same<T, f16>::value ? 0x3c00u : 0x3f80u;
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+// v without what is not finite; up: 1 where it is +inf or NaN, down: where it is -inf or NaN.  (By packed arithmetic: comparisons would need
+// a register of the scalar file each.)
 template <typename T> __device__ __forceinline__ void parted(vec<T, 8>& v, vec<T, 8>& up, vec<T, 8>& down) {
-    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-    u16x8 w = __builtin_bit_cast(u16x8, v);
+    const u16x8 w = __builtin_bit_cast(u16x8, v), size = w & uint16_t(0x7fff), finite = uint16_t(NOT_FINITE<T> - 1), inf = uint16_t(NOT_FINITE<T>), one = 1;
+    const u16x8 bad = __builtin_elementwise_min(__builtin_elementwise_max(size, finite) - finite, one), nan = __builtin_elementwise_min(__builtin_elementwise_max(size, inf) - inf, one);
+    const u16x8 minus = w >> 15;
+    up = __builtin_bit_cast(vec<T, 8>, u16x8((bad & (nan | (minus ^ one))) * uint16_t(ONE<T>)));
+    down = __builtin_bit_cast(vec<T, 8>, u16x8((bad & (nan | minus)) * uint16_t(ONE<T>)));
+    v = __builtin_bit_cast(vec<T, 8>, u16x8(w & (bad - one)));
+}
+// 1 where `margin` is positive
+template <typename T> __device__ __forceinline__ uint32_t one_if(int32_t margin) { return uint32_t(min(max(margin, 0), 1)) * ONE<T>; }
+// x, and 0 (-inf) where `hidden` is negative
+__device__ __forceinline__ float or_zero(float x, int32_t hidden) { return __uint_as_float(__float_as_uint(x) & ~uint32_t(hidden >> 31)); }
+__device__ __forceinline__ float or_none(float x, int32_t hidden) {
+    const uint32_t mask = uint32_t(hidden >> 31);
+    return __uint_as_float((__float_as_uint(x) & ~mask) | (mask & 0xff800000u));
+}
+
+// What counts of values that are not finite do to a sum: a count becomes 0 or infinity (no contraction: a fused product would stay below it).
+template <bool SIGNED> __device__ __forceinline__ float counted(float up, float down) {
+#pragma clang fp contract(off)
+    const float x = up * 0x1p127f * 0x1p127f, y = down * 0x1p127f * 0x1p127f;
+    return SIGNED ? x - y : (x - x) + (y - y);
+}
+
+// acc += v p over a depth of 32 K for products of 32 x 32 x 16, v turned on the way (at[i]: where this lane reads the first four rows of columns 32 i on),
+// p the second operand, where some p are 0 because the mask hides that depth from that column and v has values that are not finite: a product
+// 0 * inf must not show.  Such values are left out, and what they do to the columns that see them is found by counting; see(k): positive where
+// this lane's column sees depth k.  SIGNED: p is positive, so their sign is the sum's; else they make it NaN.
+template <int K, bool SIGNED, int D, typename T, int ND, typename See> __device__ __forceinline__ void careful(const vec<T, 8>* p, const uint32_t (&at)[ND], f32x16 (&acc)[ND], See see) {
+    const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        const uint32_t word = w[e], size = word & 0x7fff;
-        const bool bad = size >= NOT_FINITE<T>, nan = size > NOT_FINITE<T>, minus = word & 0x8000;
-        up[e] = T(bad && (nan || !minus) ? 1.f : 0.f), down[e] = T(bad && (nan || minus) ? 1.f : 0.f);
-        if (bad) w[e] = 0;
+    for (int dt = 0; dt < ND; dt++) {
+        f32x16 up = {}, down = {};
+#pragma unroll
+        for (int k = 0; k < 2 * K; k++) {
+            __builtin_amdgcn_sched_barrier(0);      // one after the other: registers count here, not time
+            vec<T, 8> v = turned32<D, T>(at[dt] + k * 16 * D * 2), u, w;
+            parted<T>(v, u, w);
+            uint32_t sees[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int at_k = k * 16 + (e / 2) * 8 + half * 4 + e % 2 * 2;
+                sees[e] = one_if<T>(see(at_k)) | one_if<T>(see(at_k + 1)) << 16;
+            }
+            const vec<T, 8> s = __builtin_bit_cast(vec<T, 8>, make_uint4(sees[0], sees[1], sees[2], sees[3]));
+            acc[dt] = product32(v, p[k], acc[dt]), up = product32(u, s, up), down = product32(w, s, down);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) acc[dt][i] += counted<SIGNED>(up[i], down[i]);
     }
-    v = __builtin_bit_cast(vec<T, 8>, w);
+}
+// Whether `bytes` of LDS have a value that is not finite, by all lanes of a wavefront.
+template <typename T> __device__ __forceinline__ bool any_not_finite(uint32_t at, int bytes) {
+    u16x2 size = {0, 0};
+    for (int i = (threadIdx.x & 63) * 16; i < bytes; i += 1024) {
+        const uint4 w = __builtin_bit_cast(uint4, chunk_from<T>(at + i));
+        most_of(size, w.x), most_of(size, w.y), most_of(size, w.z), most_of(size, w.w);
+    }
+    return __any(not_finite<T>(size));
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -184,7 +256,7 @@ inline int attention_sizes(int32_t sequences, int32_t rows, int32_t k_rows, int3
     if ((dtype != CSR5_DTYPE_BF16 && dtype != CSR5_DTYPE_F16) || sequences < 0 || rows < 0 || k_rows < 0 || heads < 0 || kv_heads < 0 || d < 0) return CSR5_EINVAL;
     if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return CSR5_EINVAL;
     if (!(scale > 0.f) || !std::isfinite(scale)) return CSR5_EINVAL;
-    if (sequences > MOST_SIZE || rows > MOST_SIZE || k_rows > MOST_SIZE || heads > CSR5_ATTENTION_MAX_HEADS || d > CSR5_ATTENTION_MAX_D) return CSR5_ERANGE;
+    if (sequences > MOST_SIZE || rows > CSR5_ATTENTION_MAX_ROWS || k_rows > CSR5_ATTENTION_MAX_ROWS || heads > CSR5_ATTENTION_MAX_HEADS || d > CSR5_ATTENTION_MAX_D) return CSR5_ERANGE;
     return CSR5_OK;
 }
 inline bool words(std::initializer_list<const void*> all) {

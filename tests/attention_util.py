@@ -2,7 +2,7 @@
 
 Bounds.  A score, a sum of d products in 32 bits, is off by delta = (d + 8) * 2^-23 * scale * sum |q||k|.  So p = exp(score - c) is
 off by eps_p = delta + 2^-21 + 2^-21 * (|score| + |c|) relatively: the score's error, an exponential within 2^-21, and its argument
-in 32 bits.  One rounding to the type adds U (2^-8 in BF16, 2^-11 in F16; there also 2^-25 absolutely, below the smallest
+in 32 bits; one below 2^-126, the smallest normal number of 32 bits, may be 0, which is 2^-126 absolutely.  One rounding to the type adds U (2^-8 in BF16, 2^-11 in F16; there also 2^-25 absolutely, below the smallest
 normal number), and a sum of n terms n * 2^-23 of their magnitudes, joined parts and rescaling by factors within 2^-21 among them."""
 import math
 
@@ -75,11 +75,11 @@ def gradients_of(q, k, v, dout, out, lse, scale, causal, dtype):
     p = torch.where(see, torch.exp(score - base), 0.0)
     dp, delta = dout @ v.T, (dout * out).sum(1, keepdim=True)
     ds = torch.where(see, p * (dp - delta), 0.0)
-    tiny = 2.0 ** -25 if dtype is torch.float16 else 0.0
+    tiny = TINY16[dtype]
     eps = (d + 8) * EPS32 * scale * (q.abs() @ k.abs().T) + 2.0 ** -21 + 2.0 ** -21 * (torch.where(see, score.abs(), 0.0) + base.abs())
     eps_dp = (d + 8) * EPS32 * (dout.abs() @ v.abs().T + (dout.abs() * out.abs()).sum(1, keepdim=True))
     err_p = torch.where(see, p * (eps + U[dtype]) + tiny, 0.0)
-    err_ds = torch.where(see, p * eps_dp * (1 + U[dtype]) + ds.abs() * (eps + U[dtype] + 2.0 ** -21) + tiny, 0.0)
+    err_ds = torch.where(see, p * eps_dp * (1 + U[dtype]) + ds.abs() * (eps + U[dtype] + 2.0 ** -21) + tiny + 2.0 ** -126 * (dp - delta).abs(), 0.0)
     more = lambda count: (count + 64) * EPS32                           # noqa: E731  a sum's own error
     dq, dq_slack = scale * (ds @ k), scale * ((err_ds + more(n) * ds.abs()) @ k.abs())
     dk, dk_slack = scale * (ds.T @ q), scale * ((err_ds + more(m * 16) * ds.abs()).T @ q.abs())
