@@ -162,27 +162,35 @@ template <typename T> struct RotaryArgs {
     Cache<T> k_cache, v_cache;
 };
 
-constexpr int ROTARY_THREADS = 256;
+constexpr int ROTARY_THREADS = 256, ROTARY_MANY = 1024;     // from so many tokens on a workgroup has four
 
-template <typename T, bool INTERLEAVED> __global__ __launch_bounds__(ROTARY_THREADS) void k_rotary(RotaryArgs<T> a) {
-    extern __shared__ float turn[];                     // cosines, then sines
-    const int64_t token = workgroup();
-    if (token >= a.tokens) return;
-    for (int i = threadIdx.x; i < a.pairs; i += ROTARY_THREADS) {
-        const int32_t axis = a.axis ? a.axis[i] : 0;
+// Cosines and sines of TOKENS tokens, in LDS: [token][pairs], then the sines.
+template <int TOKENS, typename T> __device__ __forceinline__ void turns(const RotaryArgs<T>& a, int64_t token0, float* turn) {
+    for (int i = threadIdx.x; i < TOKENS * a.pairs; i += ROTARY_THREADS) {
+        const int t = TOKENS == 1 ? 0 : i / a.pairs, p = i - t * a.pairs;
+        const int64_t token = min(token0 + t, int64_t(a.tokens - 1));
+        const int32_t axis = a.axis ? a.axis[p] : 0;
         float c = 1.f, s = 0.f;
         if (uint32_t(axis) < uint32_t(a.axes)) {
             constexpr double TURN = 6.283185307179586476925;
-            const double angle = double(a.position[axis * a.ldp + token]) * double(a.frequency[i]);
-            sincosf(float(fma(-rint(angle / TURN), TURN, angle)), &s, &c);
+            const double angle = double(a.position[axis * a.ldp + token]) * double(a.frequency[p]);
+            sincosf(float(fma(-rint(angle * (1 / TURN)), TURN, angle)), &s, &c);
         }
-        turn[i] = c, turn[a.pairs + i] = a.inverse ? -s : s;
+        turn[i] = c, turn[TOKENS * a.pairs + i] = a.inverse ? -s : s;
     }
     __syncthreads();
+}
+
+// Value by value, for rows of any addresses.
+template <typename T, bool INTERLEAVED> __global__ __launch_bounds__(ROTARY_THREADS) void k_rotary(RotaryArgs<T> a) {
+    extern __shared__ float turn[];
+    const int64_t token = workgroup();
+    if (token >= a.tokens) return;
+    turns<1>(a, token, turn);
     const int32_t slot = a.slot ? a.slot[token] : -1;
     const int32_t page = slot >> a.shift, place = slot & ((1 << a.shift) - 1);
     const bool cached = slot >= 0 && page < a.pages;
-    const int rest = a.d - 2 * a.pairs, each = a.pairs + rest;      // a head: its pairs, and the values that stay
+    const int each = a.d - a.pairs;                                 // a head: its pairs, and the values that stay
     for (int i = threadIdx.x; i < (a.heads + a.kv_heads) * each; i += ROTARY_THREADS) {
         const int h = i / each, e = i - h * each;
         const bool key = h >= a.heads;
@@ -207,6 +215,86 @@ template <typename T, bool INTERLEAVED> __global__ __launch_bounds__(ROTARY_THRE
             const int h = i / a.d, e = i - h * a.d;
             a.v_cache.p[page * a.v_cache.page + place * a.v_cache.row + h * a.v_cache.head + e] = a.v.p[token * a.v.row + h * a.v.head + e];
         }
+}
+
+// 16 bytes at a time.  A unit is 16 bytes of a head, or two times 16 whose values are pairs; a head has `units` of them (values have none to turn, and
+// take the same number of places).  A workgroup's threads go through the units of its tokens.
+template <typename T, bool INTERLEAVED, int TOKENS> __global__ __launch_bounds__(ROTARY_THREADS) void k_rotary_wide(RotaryArgs<T> a, int units, uint32_t inverse_units, int all_heads) {
+    constexpr int V = 16 / sizeof(T), N = INTERLEAVED ? V / 2 : V;       // pairs of a unit
+    extern __shared__ __align__(16) float turn[];
+    const int64_t token0 = workgroup() * TOKENS;
+    if (token0 >= a.tokens) return;
+    turns<TOKENS>(a, token0, turn);
+    const int tokens = int(min(int64_t(TOKENS), a.tokens - token0));
+    const int total = all_heads * units, split = a.pairs / N;       // units that are turned
+    int32_t page[TOKENS], place[TOKENS];
+    bool cached[TOKENS];
+#pragma unroll
+    for (int t = 0; t < TOKENS; t++) {
+        const int32_t slot = a.slot && t < tokens ? a.slot[token0 + t] : -1;
+        page[t] = slot >> a.shift, place[t] = slot & ((1 << a.shift) - 1), cached[t] = slot >= 0 && page[t] < a.pages;
+    }
+    for (int i = threadIdx.x; i < total; i += ROTARY_THREADS) {
+        const int h = units == 1 ? i : int(__umulhi(uint32_t(i), inverse_units)), u = i - h * units;
+        const int hk = h - a.heads;
+        if (hk >= a.kv_heads) {                                     // values, as they are
+            const int hv = hk - a.kv_heads;
+#pragma unroll
+            for (int t = 0; t < TOKENS; t++) {
+                if (!cached[t]) continue;
+                const T* const from = a.v.p + (token0 + t) * a.v.row + hv * a.v.head;
+                T* const in = a.v_cache.p + page[t] * a.v_cache.page + place[t] * a.v_cache.row + hv * a.v_cache.head;
+                for (int c = u * V; c < a.d; c += units * V) *reinterpret_cast<uint4*>(in + c) = *reinterpret_cast<const uint4*>(from + c);
+            }
+            continue;
+        }
+        const bool key = hk >= 0, pair = u < split;
+        // where the unit is: one place, or two
+        const int c0 = INTERLEAVED || pair ? u * V : (u + split) * V, c1 = pair && !INTERLEAVED ? c0 + a.pairs : c0;
+        const Heads<T> source = key ? a.k : a.q, result = key ? a.k_out : a.q_out;
+        const int64_t from = (key ? hk : h) * source.head, to = (key ? hk : h) * result.head, in = hk * a.k_cache.head;
+        vec<T, V> x[TOKENS], y[TOKENS];
+#pragma unroll
+        for (int t = 0; t < TOKENS; t++)
+            if (t < tokens) {
+                const T* const p = source.p + (token0 + t) * source.row + from;
+                x[t] = *reinterpret_cast<const vec<T, V>*>(p + c0);
+                if (!INTERLEAVED) y[t] = *reinterpret_cast<const vec<T, V>*>(p + c1);
+            }
+        if (pair) {
+#pragma unroll
+            for (int t = 0; t < TOKENS; t++)
+                if (t < tokens) {
+                    float c[N], s[N];
+                    load_values<N, true>(turn + t * a.pairs + u * N, N, c);
+                    load_values<N, true>(turn + (TOKENS + t) * a.pairs + u * N, N, s);
+#pragma unroll
+                    for (int e = 0; e < N; e++) {
+                        if (INTERLEAVED) {
+                            const float p = float(x[t][2 * e]), q = float(x[t][2 * e + 1]);
+                            x[t][2 * e] = T(p * c[e] - q * s[e]), x[t][2 * e + 1] = T(p * s[e] + q * c[e]);
+                        } else {
+                            const float p = float(x[t][e]), q = float(y[t][e]);
+                            x[t][e] = T(p * c[e] - q * s[e]), y[t][e] = T(p * s[e] + q * c[e]);
+                        }
+                    }
+                }
+        }
+#pragma unroll
+        for (int t = 0; t < TOKENS; t++)
+            if (t < tokens) {
+                if (!key || a.k_out.p) {
+                    T* const p = result.p + (token0 + t) * result.row + to;
+                    *reinterpret_cast<vec<T, V>*>(p + c0) = x[t];
+                    if (!INTERLEAVED && pair) *reinterpret_cast<vec<T, V>*>(p + c1) = y[t];
+                }
+                if (key && cached[t]) {
+                    T* const p = a.k_cache.p + page[t] * a.k_cache.page + place[t] * a.k_cache.row + in;
+                    *reinterpret_cast<vec<T, V>*>(p + c0) = x[t];
+                    if (!INTERLEAVED && pair) *reinterpret_cast<vec<T, V>*>(p + c1) = y[t];
+                }
+            }
+    }
 }
 
 }  // namespace
@@ -241,15 +329,26 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
         if (reinterpret_cast<uintptr_t>(p) & 3) return CSR5_EINVAL;
     if (tokens == 0 || d == 0 || (heads == 0 && kv_heads == 0)) return CSR5_OK;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    auto go = [&](auto zero) {
+    auto typed_call = [&](auto zero) {
         using T = decltype(zero);
         const RotaryArgs<T> a{tokens, heads, kv_heads, d, rot / 2, axes, position, ldp, frequency, axis, inverse != 0, typed<T>(q), typed<T>(q_out), typed<T>(k), typed<T>(k_out),
                               typed<T>(v), slot, slot ? pages : 0, slot ? __builtin_ctz(page) : 0, typed<T>(k_cache), typed<T>(v_cache)};
-        if (interleaved) k_rotary<T, true><<<workgroups(tokens), ROTARY_THREADS, rot * 4, s>>>(a);
-        else k_rotary<T, false><<<workgroups(tokens), ROTARY_THREADS, rot * 4, s>>>(a);
+        constexpr int V = 16 / sizeof(T);
+        const int pairs = rot / 2, units = (interleaved ? d : d - pairs) / V, all_heads = heads + (slot ? 2 : 1) * kv_heads;
+        const bool w = d % V == 0 && (interleaved ? rot : pairs) % V == 0 && units > 0 && int64_t(all_heads) * units < (1 << 22) && wide(q, size) && wide(q_out, size) && wide(k, size) &&
+                       wide(k_out, size) && (!slot || (wide(v, size) && wide(k_cache, size) && wide(v_cache, size)));
+        auto go = [&](auto inter) {
+            constexpr bool I = decltype(inter)::value;
+            const uint32_t inverse_units = units > 1 ? uint32_t(((uint64_t(1) << 32) + units - 1) / units) : 0;     // exact for what is below 2^32 / units
+            if (!w) k_rotary<T, I><<<workgroups(tokens), ROTARY_THREADS, rot * 4, s>>>(a);
+            else if (tokens >= ROTARY_MANY) k_rotary_wide<T, I, 4><<<workgroups(divide_up(tokens, 4)), ROTARY_THREADS, rot * 16, s>>>(a, units, inverse_units, all_heads);
+            else k_rotary_wide<T, I, 1><<<workgroups(tokens), ROTARY_THREADS, rot * 4, s>>>(a, units, inverse_units, all_heads);
+        };
+        if (interleaved) go(std::true_type());
+        else go(std::false_type());
         return launched();
     };
-    return dtype == CSR5_DTYPE_F32 ? go(float()) : dtype == CSR5_DTYPE_F16 ? go(f16()) : go(bf16());
+    return dtype == CSR5_DTYPE_F32 ? typed_call(float()) : dtype == CSR5_DTYPE_F16 ? typed_call(f16()) : typed_call(bf16());
 }
 
 }  // extern "C"
