@@ -13,12 +13,12 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------------------------
 // Pages.  A request's place among the new tokens, the pages taken and the pages given back is the sum of those before it: every
-// workgroup adds all of them up (1024 requests at a time, from L2) and then writes its own share of the tokens, the new entries
-// of the tables and the ring, finding the request of each by bisection over the sums in LDS.  So there is one launch and
+// workgroup adds all of them up (256 or 1024 requests at a time) and then writes its own share of the tokens, the new entries
+// of the tables and the ring, finding the request of each by bisection over the sums in LDS; tokens, new entries and the ring are three workgroups', as each waits
+// for memory.  So there is one launch and
 // nothing to wait for between workgroups.
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int PAGES_THREADS = 1024, PAGES_WAVES = PAGES_THREADS / 64;
-constexpr int PAGES_SHARE = 4096;           // tokens, or entries, of a workgroup
+constexpr int PAGES_SHARE = 1024;           // tokens, or entries, of a workgroup
 
 struct PagesArgs {
     int requests, width, ring, shift, tokens;
@@ -30,29 +30,39 @@ struct PagesArgs {
     int32_t *offset, *position, *slot, *length_out, *state_out;
 };
 
-// The sum of v over the threads before this one; total: over all.  part: a word per wavefront, free to be written.
-__device__ __forceinline__ int64_t sum_before(int64_t v, int64_t* part, int64_t& total) {
-    int64_t upto = v;
+// Sums of three values over the threads before this one, and over all.
+struct Sums {
+    int64_t before[3], all[3];
+};
+template <int WAVES> __device__ __forceinline__ Sums sums_of(const int64_t (&v)[3], int64_t (&part)[3][WAVES]) {
+    int64_t upto[3] = {v[0], v[1], v[2]};
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const int64_t other = __shfl_up(upto, d);
-        if (int(threadIdx.x & 63) >= d) upto += other;
-    }
-    if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = upto;
-    __syncthreads();
-    int64_t before = upto - v, all = 0;
+        int64_t other[3];
 #pragma unroll
-    for (int w = 0; w < PAGES_WAVES; w++) {
-        if (w < int(threadIdx.x >> 6)) before += part[w];
-        all += part[w];
+        for (int k = 0; k < 3; k++) other[k] = __shfl_up(upto[k], d);
+#pragma unroll
+        for (int k = 0; k < 3; k++)
+            if (lane >= d) upto[k] += other[k];
     }
+    if (lane == 63) part[0][wave] = upto[0], part[1][wave] = upto[1], part[2][wave] = upto[2];
     __syncthreads();
-    total = all;
-    return before;
+    Sums s;
+#pragma unroll
+    for (int k = 0; k < 3; k++) {
+        s.before[k] = upto[k] - v[k], s.all[k] = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; i++) {
+            if (i < wave) s.before[k] += part[k][i];
+            s.all[k] += part[k][i];
+        }
+    }
+    return s;
 }
 
 // The last of the requests whose sum is at most `at`: the one that `at` lies in, as those after it without a share have a larger one.
-__device__ __forceinline__ int request_at(const int64_t* first, int count, int64_t at) {
+__device__ __forceinline__ int request_at(const int32_t* first, int count, int32_t at) {
     int low = 0, high = count;
     while (high - low > 1) {
         const int mid = (low + high) / 2;
@@ -62,84 +72,89 @@ __device__ __forceinline__ int request_at(const int64_t* first, int count, int64
     return low;
 }
 
-__global__ __launch_bounds__(PAGES_THREADS) void k_pages(PagesArgs a) {
-    __shared__ int64_t part[PAGES_WAVES];
-    __shared__ int64_t first_token[PAGES_THREADS], first_page[PAGES_THREADS], first_back[PAGES_THREADS];
-    __shared__ int32_t lengths[PAGES_THREADS], served[PAGES_THREADS];
+template <int THREADS> __global__ __launch_bounds__(THREADS) void k_pages(PagesArgs a) {
+    __shared__ int64_t part[3][THREADS / 64];
+    __shared__ int32_t first[THREADS];                              // of what this workgroup writes; as far as there is room for it
+    __shared__ int32_t wants[THREADS];                              // pages asked for before
+    __shared__ int32_t lengths[THREADS], held_pages[THREADS];       // held_pages: -1 where a request is not served
+    const int task = blockIdx.x % 3, group = blockIdx.x / 3, groups = gridDim.x / 3;     // tokens, new pages, pages that come back
     const int t = threadIdx.x;
     const int32_t mask = (1 << a.shift) - 1;
     const int64_t ring = max(a.ring, 1);
-    const int64_t head = ((a.state[0] % ring) + ring) % ring, count = min(max(int64_t(a.state[1]), int64_t(0)), int64_t(a.ring));
+    const int32_t state = a.state[0];
+    const int64_t head = state >= 0 && state < ring ? state : ((state % ring) + ring) % ring, count = min(max(int64_t(a.state[1]), int64_t(0)), int64_t(a.ring));
+    const auto around = [&](int64_t i) { return i < ring ? i : i - ring; };         // of what is below 2 ring
     const int64_t most = int64_t(a.width) << a.shift;
     int64_t tokens = 0, asked = 0, taken = 0, back = 0;             // of the requests before these
-    for (int r0 = 0; r0 < a.requests; r0 += PAGES_THREADS) {
-        const int r = r0 + t, here = min(PAGES_THREADS, a.requests - r0);
+    // this workgroup's part of `begin` to `last` of all
+    const auto share = [&](int64_t begin, int64_t last, auto f) {
+        if (begin >= last) return;                      // both are below 2^31 then
+        const int32_t from = int32_t(begin), to = int32_t(last), skip = (group + groups - from / PAGES_SHARE % groups) % groups;
+        for (int32_t base = from / PAGES_SHARE + skip; base <= (to - 1) / PAGES_SHARE; base += groups) {
+            const int32_t end = base < to / PAGES_SHARE ? (base + 1) * PAGES_SHARE : to;
+            for (int32_t i = max(base * PAGES_SHARE, from) + t; i < end; i += THREADS) f(i);
+        }
+    };
+    const int64_t rooms[3] = {a.tokens, count, a.ring - count};
+    const int64_t room = rooms[task];
+    for (int r0 = 0; r0 < a.requests; r0 += THREADS) {
+        const int r = r0 + t, here = min(THREADS, a.requests - r0);
         const int32_t fresh = r < a.requests ? a.fresh[r] : 0;
         const int32_t have = r < a.requests ? int32_t(min(int64_t(max(a.length[r], 0)), most)) : 0;
         const int64_t now = int64_t(have) + max(fresh, 0), held = (int64_t(have) + mask) >> a.shift, wanted = (now + mask) >> a.shift;
-        const bool over = fresh < 0, fits = wanted <= a.width;
-        const int64_t need = fits && !over ? wanted - held : 0;
-        int64_t total_tokens, total_asked, total_taken, total_back;
-        const int64_t token = tokens + sum_before(max(fresh, 0), part, total_tokens);
-        const int64_t want = asked + sum_before(need, part, total_asked);
-        const bool ok = fits && !over && (need == 0 || want + need <= count);
-        const int64_t take = ok ? need : 0;
-        sum_before(take, part, total_taken);
-        const int64_t give = over ? held : 0;
-        const int64_t behind = back + sum_before(give, part, total_back);
-        // what is taken before a request that is served is what is asked for before it
-        first_token[t] = token, first_page[t] = want, first_back[t] = behind, lengths[t] = have, served[t] = ok;
+        const bool over = fresh < 0, fits = wanted <= a.width && !over;
+        const int64_t need = fits ? wanted - held : 0;
+        // what is served is what all that is asked for up to it leaves room for: the pages taken are the most that fits so
+        const int64_t v[3] = {max(fresh, 0), need, over ? held : 0};
+        if (r0 > 0) __syncthreads();
+        const Sums s = sums_of<THREADS / 64>(v, part);
+        const int64_t token = tokens + s.before[0], want = asked + s.before[1];
+        const bool ok = fits && (need == 0 || want + need <= count);
+        first[t] = int32_t(min(room, task == 0 ? token : task == 1 ? want : back + s.before[2])), lengths[t] = have, held_pages[t] = ok ? int32_t(held) : -1;
+        wants[t] = int32_t(min(want, count));
         if (blockIdx.x == 0 && r < a.requests) {
             if (r == 0) a.offset[0] = 0;
             a.offset[r + 1] = int32_t(min(token + max(fresh, 0), int64_t(a.tokens)));
             a.length_out[r] = over ? 0 : ok ? int32_t(now) : have;
         }
+        if (ok && need > 0) taken = want + need;
         __syncthreads();
-        // tokens
-        const int64_t last_token = min(tokens + total_tokens, int64_t(a.tokens));
-        for (int64_t base = tokens / PAGES_SHARE * PAGES_SHARE; base < last_token; base += PAGES_SHARE) {
-            if ((base / PAGES_SHARE) % gridDim.x != blockIdx.x) continue;
-            const int64_t end = min(base + PAGES_SHARE, last_token);
-            for (int64_t i = max(base, tokens) + t; i < end; i += PAGES_THREADS) {
-                const int q = request_at(first_token, here, i);
-                const int32_t at = int32_t(int64_t(lengths[q]) + (i - first_token[q]));
-                const int32_t holds = (lengths[q] + mask) >> a.shift, p = at >> a.shift;
+        if (task == 0)
+            share(tokens, min(tokens + s.all[0], room), [&](int32_t i) {
+                const int q = request_at(first, here, i);
+                const int32_t at = lengths[q] + (i - first[q]), holds = held_pages[q], p = at >> a.shift;
                 int32_t slot = -1;
-                if (served[q]) {
-                    const int32_t page = p < holds ? a.table[int64_t(r0 + q) * a.ldt + p] : a.pool[(head + first_page[q] + (p - holds)) % ring];
+                if (holds >= 0) {
+                    const int32_t page = p < holds ? a.table[int64_t(r0 + q) * a.ldt + p] : a.pool[around(head + wants[q] + (p - holds))];
                     if (page >= 0 && page <= (INT32_MAX >> a.shift)) slot = (page << a.shift) | (at & mask);       // others are no pages
                 }
                 a.position[i] = at, a.slot[i] = slot;
-            }
-        }
-        // new entries of the tables: first_page counts those of requests that are not served too, which are passed over
-        const int64_t last_page = min(asked + total_asked, count);
-        for (int64_t base = asked / PAGES_SHARE * PAGES_SHARE; base < last_page; base += PAGES_SHARE) {
-            if ((base / PAGES_SHARE) % gridDim.x != blockIdx.x) continue;
-            const int64_t end = min(base + PAGES_SHARE, last_page);
-            for (int64_t i = max(base, asked) + t; i < end; i += PAGES_THREADS) {
-                const int q = request_at(first_page, here, i);
-                if (served[q]) a.table[int64_t(r0 + q) * a.ldt + ((lengths[q] + mask) >> a.shift) + (i - first_page[q])] = a.pool[(head + i) % ring];
-            }
-        }
-        // pages that come back, behind the last free one; more than the ring has places for are not pages of it
-        const int64_t last_back = min(back + total_back, int64_t(a.ring) - count);
-        for (int64_t base = back / PAGES_SHARE * PAGES_SHARE; base < last_back; base += PAGES_SHARE) {
-            if ((base / PAGES_SHARE) % gridDim.x != blockIdx.x) continue;
-            const int64_t end = min(base + PAGES_SHARE, last_back);
-            for (int64_t i = max(base, back) + t; i < end; i += PAGES_THREADS) {
-                const int q = request_at(first_back, here, i);
-                a.pool[(head + count + i) % ring] = a.table[int64_t(r0 + q) * a.ldt + (i - first_back[q])];
-            }
-        }
-        tokens += total_tokens, asked += total_asked, taken += total_taken, back += total_back;
-        __syncthreads();
+            });
+        else if (task == 1)             // requests that are not served count here too, and are passed over
+            share(asked, min(asked + s.all[1], room), [&](int32_t i) {
+                const int q = request_at(first, here, i);
+                if (held_pages[q] >= 0) a.table[int64_t(r0 + q) * a.ldt + held_pages[q] + (i - first[q])] = a.pool[around(head + i)];
+            });
+        else                            // behind the last free one; more than the ring has places for are not pages of it
+            share(back, min(back + s.all[2], room), [&](int32_t i) {
+                const int q = request_at(first, here, i);
+                a.pool[around(around(head + count) + i)] = a.table[int64_t(r0 + q) * a.ldt + (i - first[q])];
+            });
+        tokens += s.all[0], asked += s.all[1], back += s.all[2];
     }
-    for (int64_t i = min(tokens, int64_t(a.tokens)) + int64_t(blockIdx.x) * PAGES_THREADS + t; i < a.tokens; i += int64_t(gridDim.x) * PAGES_THREADS)
-        a.position[i] = 0, a.slot[i] = -1;
-    if (blockIdx.x == 0 && t == 0) {
+    if (task == 0)
+        for (int64_t i = min(tokens, int64_t(a.tokens)) + int64_t(group) * THREADS + t; i < a.tokens; i += int64_t(groups) * THREADS) a.position[i] = 0, a.slot[i] = -1;
+    if (blockIdx.x != 0) return;
+    // the pages taken are those asked for up to the last request that got some: the most of all threads'
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) taken = max(taken, int64_t(__shfl_xor(taken, d)));
+    __syncthreads();
+    if ((t & 63) == 0) part[0][t >> 6] = taken;
+    __syncthreads();
+    if (t == 0) {
+        for (int w = 1; w < THREADS / 64; w++) taken = max(taken, part[0][w]);
         if (a.requests == 0) a.offset[0] = 0;
-        a.state_out[0] = int32_t((head + taken) % ring);
+        a.state_out[0] = int32_t(around(head + taken));
         a.state_out[1] = int32_t(count - taken + min(back, int64_t(a.ring) - count));
     }
 }
@@ -312,7 +327,10 @@ int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int3
         if (reinterpret_cast<uintptr_t>(p) & 3) return CSR5_EINVAL;
     const PagesArgs a{requests, width, ring, __builtin_ctz(page), tokens, fresh, length, table, ldt, pool, state, offset, position, slot, length_out, state_out};
     const int64_t shares = divide_up(int64_t(tokens), PAGES_SHARE);
-    k_pages<<<int(shares < 1 ? 1 : shares > 256 ? 256 : shares), PAGES_THREADS, 0, static_cast<hipStream_t>(hip_stream)>>>(a);
+    const int groups = int(shares < 1 ? 1 : shares > 256 ? 256 : shares) * 3;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (requests <= 256) k_pages<256><<<groups, 256, 0, s>>>(a);
+    else k_pages<1024><<<groups, 1024, 0, s>>>(a);
     return launched();
 }
 
