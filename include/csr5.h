@@ -624,7 +624,8 @@ typedef struct { /* value c of head h of token i of a page is at p[number*page +
  * need are free (one that would pass the table's width needs none and gets none; one that needs none is served).  New pages are
  * written into table, whose other entries stay.  The pages of a request that is over go behind the last free one, for later
  * calls; its row of the table stays.  tokens: room in position and slot; of more new tokens than that the first are
- * written, and offset ends at tokens.  page is a power of two.  pool and table are the only arrays that are read and written; with
+ * written, and offset ends at tokens.  page is a power of two, and width * page is below
+ * 2^31, as is the number of requests and of tokens (else CSR5_ERANGE).  pool and table are the only arrays that are read and written; with
  * the same state a call gives the same again.  A length below 0 is 0, one past the table its width.
  */
 int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int32_t tokens, const int32_t *fresh,

@@ -18,7 +18,7 @@ namespace {
 // for memory.  So there is one launch and
 // nothing to wait for between workgroups.
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int PAGES_SHARE = 1024;           // tokens, or entries, of a workgroup
+constexpr int PAGES_THREADS = 256, PAGES_SHARE = 1024;      // tokens, or entries, of a workgroup
 
 struct PagesArgs {
     int requests, width, ring, shift, tokens;
@@ -72,11 +72,12 @@ __device__ __forceinline__ int request_at(const int32_t* first, int count, int32
     return low;
 }
 
-template <int THREADS> __global__ __launch_bounds__(THREADS) void k_pages(PagesArgs a) {
+template <int EACH> __global__ __launch_bounds__(PAGES_THREADS) void k_pages(PagesArgs a) {
+    constexpr int THREADS = PAGES_THREADS, MANY = THREADS * EACH;     // requests at a time
     __shared__ int64_t part[3][THREADS / 64];
-    __shared__ int32_t first[THREADS];                              // of what this workgroup writes; as far as there is room for it
-    __shared__ int32_t wants[THREADS];                              // pages asked for before
-    __shared__ int32_t lengths[THREADS], held_pages[THREADS];       // held_pages: -1 where a request is not served
+    __shared__ int32_t first[MANY];                                 // of what this workgroup writes; as far as there is room for it
+    __shared__ int32_t wants[MANY];                                 // pages asked for before
+    __shared__ int32_t lengths[MANY], held_pages[MANY];       // held_pages: -1 where a request is not served
     const int task = blockIdx.x % 3, group = blockIdx.x / 3, groups = gridDim.x / 3;     // tokens, new pages, pages that come back
     const int t = threadIdx.x;
     const int32_t mask = (1 << a.shift) - 1;
@@ -97,27 +98,42 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_pages(PagesA
     };
     const int64_t rooms[3] = {a.tokens, count, a.ring - count};
     const int64_t room = rooms[task];
-    for (int r0 = 0; r0 < a.requests; r0 += THREADS) {
-        const int r = r0 + t, here = min(THREADS, a.requests - r0);
-        const int32_t fresh = r < a.requests ? a.fresh[r] : 0;
-        const int32_t have = r < a.requests ? int32_t(min(int64_t(max(a.length[r], 0)), most)) : 0;
-        const int64_t now = int64_t(have) + max(fresh, 0), held = (int64_t(have) + mask) >> a.shift, wanted = (now + mask) >> a.shift;
-        const bool over = fresh < 0, fits = wanted <= a.width && !over;
-        const int64_t need = fits ? wanted - held : 0;
-        // what is served is what all that is asked for up to it leaves room for: the pages taken are the most that fits so
-        const int64_t v[3] = {max(fresh, 0), need, over ? held : 0};
+    for (int r0 = 0; r0 < a.requests; r0 += MANY) {
+        const int here = min(MANY, a.requests - r0);
+        int32_t fresh[EACH], have[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; e++) {
+            const int r = r0 + t * EACH + e;
+            fresh[e] = r < a.requests ? a.fresh[r] : 0, have[e] = r < a.requests ? a.length[r] : 0;
+        }
+        int64_t v[3] = {0, 0, 0}, held[EACH], need[EACH];
+        bool fits[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; e++) {
+            have[e] = int32_t(min(int64_t(max(have[e], 0)), most));
+            const int64_t wanted = (int64_t(have[e]) + max(fresh[e], 0) + mask) >> a.shift;
+            held[e] = (int64_t(have[e]) + mask) >> a.shift;
+            fits[e] = wanted <= a.width && fresh[e] >= 0;
+            need[e] = fits[e] ? wanted - held[e] : 0;
+            v[0] += max(fresh[e], 0), v[1] += need[e], v[2] += fresh[e] < 0 ? held[e] : 0;
+        }
         if (r0 > 0) __syncthreads();
         const Sums s = sums_of<THREADS / 64>(v, part);
-        const int64_t token = tokens + s.before[0], want = asked + s.before[1];
-        const bool ok = fits && (need == 0 || want + need <= count);
-        first[t] = int32_t(min(room, task == 0 ? token : task == 1 ? want : back + s.before[2])), lengths[t] = have, held_pages[t] = ok ? int32_t(held) : -1;
-        wants[t] = int32_t(min(want, count));
-        if (blockIdx.x == 0 && r < a.requests) {
-            if (r == 0) a.offset[0] = 0;
-            a.offset[r + 1] = int32_t(min(token + max(fresh, 0), int64_t(a.tokens)));
-            a.length_out[r] = over ? 0 : ok ? int32_t(now) : have;
+        int64_t token = tokens + s.before[0], want = asked + s.before[1], behind = back + s.before[2];
+#pragma unroll
+        for (int e = 0; e < EACH; e++) {
+            const int r = r0 + t * EACH + e, i = t * EACH + e;
+            // what is served is what all that is asked for up to it leaves room for
+            const bool ok = fits[e] && (need[e] == 0 || want + need[e] <= count);
+            first[i] = int32_t(min(room, task == 0 ? token : task == 1 ? want : behind)), wants[i] = int32_t(min(want, count)), lengths[i] = have[e], held_pages[i] = ok ? int32_t(held[e]) : -1;
+            token += max(fresh[e], 0), want += need[e], behind += fresh[e] < 0 ? held[e] : 0;
+            if (blockIdx.x == 0 && r < a.requests) {
+                if (r == 0) a.offset[0] = 0;
+                a.offset[r + 1] = int32_t(min(token, int64_t(a.tokens)));
+                a.length_out[r] = fresh[e] < 0 ? 0 : ok ? have[e] + fresh[e] : have[e];
+            }
+            if (ok && need[e] > 0) taken = want;
         }
-        if (ok && need > 0) taken = want + need;
         __syncthreads();
         if (task == 0)
             share(tokens, min(tokens + s.all[0], room), [&](int32_t i) {
@@ -320,7 +336,7 @@ int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int3
                int64_t ldt, int32_t* pool, const int32_t* state, int32_t* offset, int32_t* position, int32_t* slot, int32_t* length_out, int32_t* state_out,
                void* hip_stream) {
     if (requests < 0 || width < 0 || ring < 0 || tokens < 0 || !power_of_two(page) || !state || !offset || !state_out) return CSR5_EINVAL;
-    if (requests > MOST_SIZE || tokens > MOST_SIZE) return CSR5_ERANGE;
+    if (requests > MOST_SIZE || tokens > MOST_SIZE || int64_t(width) * page > INT32_MAX) return CSR5_ERANGE;
     if ((requests > 0 && (!fresh || !length || !length_out)) || !rows_ok(table, requests, ldt, width, 4) || (ring > 0 && !pool) || (tokens > 0 && (!position || !slot))) return CSR5_EINVAL;
     for (const void* p : {static_cast<const void*>(fresh), static_cast<const void*>(length), static_cast<const void*>(pool), static_cast<const void*>(state), static_cast<const void*>(offset),
                           static_cast<const void*>(position), static_cast<const void*>(slot), static_cast<const void*>(length_out), static_cast<const void*>(state_out)})
@@ -329,8 +345,8 @@ int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int3
     const int64_t shares = divide_up(int64_t(tokens), PAGES_SHARE);
     const int groups = int(shares < 1 ? 1 : shares > 256 ? 256 : shares) * 3;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (requests <= 256) k_pages<256><<<groups, 256, 0, s>>>(a);
-    else k_pages<1024><<<groups, 1024, 0, s>>>(a);
+    if (requests <= PAGES_THREADS) k_pages<1><<<groups, PAGES_THREADS, 0, s>>>(a);
+    else k_pages<4><<<groups, PAGES_THREADS, 0, s>>>(a);
     return launched();
 }
 
