@@ -71,6 +71,10 @@ template <typename T, typename KV> struct Leave {
             store_values<4, WIDE>(out + c, d - c, w);
         }
     }
+    __device__ __forceinline__ void more(int c, float v) const {
+        if (part) part[c] += v;
+        else out[c] = T(float(out[c]) + v);
+    }
     __device__ __forceinline__ void total(float base, float sum, float scale) const {
         if (stats) stats[0] = base, stats[1] = sum;
         else if (lse) *lse = sum == 0.f ? -INFINITY : base * scale + logf(sum);
@@ -85,9 +89,50 @@ template <typename T, typename KV> struct Leave {
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int MANY_ROWS = 128, MANY_SHIFT = 7, MANY_KEYS = 64;
 
+// What this lane asks for of the rows of a load: they lie side by side from one address on, or each is looked for.
+template <typename T, int D, bool WIDE, bool SMALL> struct Bring {
+    static constexpr int LANES = D / 8, EACH = 64 / LANES;      // lanes of a row, rows of a load
+    int row, chunk;             // this lane's, in a load
+    uint32_t k_off, v_off;      // in bytes, from the load's first row
+    bool near;                  // every lane's chunk is in the row, and no offset passes 32 bits
+    // first: the row of a tile that this lane has in its first load (in others a multiple of 16 further)
+    template <typename One> __device__ __forceinline__ Bring(const One& kv, int first, int d) {
+        row = (threadIdx.x & 63) / LANES, chunk = int(chunk_at<D, SMALL>(first, threadIdx.x % LANES)) * 8;
+        // where d ends within a chunk that is read, or beside it, there are zeros to be had; a chunk that is not read may be another one
+        near = WIDE && (d == D || (D == 128 && d == 96)) && (EACH * kv.k_row | EACH * kv.v_row) < (1 << 28);
+        const int c = chunk < d ? chunk : 0;
+        k_off = uint32_t(row * kv.k_row + c) * 2, v_off = uint32_t(row * kv.v_row + c) * 2;
+    }
+    // rows j (a multiple of EACH, the same in every lane) on, to k and v
+    template <typename One> __device__ __forceinline__ void operator()(const One& kv, int32_t j, typename One::Ahead ahead, int d, uint8_t* k, uint8_t* v) const {
+        if (near && j + EACH <= kv.count && kv.template together<EACH>(ahead)) {
+            to_lds(kv.key(j, ahead), k_off, k), to_lds(kv.value(j, ahead), v_off, v);
+        } else {
+            const bool there = j + row < kv.count;
+            const T *const from = there ? kv.any_key(j + row) : nullptr, *const of = there ? kv.any_value(j + row) : nullptr;
+            chunk_to_lds<WIDE>(from ? from + chunk : from, d - chunk, k), chunk_to_lds<WIDE>(of ? of + chunk : of, d - chunk, v);
+        }
+    }
+};
+
+// What a lane left of a row (values c = dt * 32 + i * 8 + half * 4 on) sees of keys [from, to), whose values that are not finite were left out.
+template <int ND, typename T, typename KV, typename One> __device__ __forceinline__ void repair(const Leave<T, KV>& leave, const One& kv, int32_t from, int32_t to, int d) {
+    for (int32_t j = from; j < to; j++) {
+        const T* const v = kv.any_value(j);
+        if (!v) continue;
+        for (int i = 0; i < 4 * ND; i++)
+            for (int e = 0; e < 4; e++) {
+                const int c = i * 8 + ((threadIdx.x >> 5) & 1) * 4 + e;
+                if (c < d && !finite(float(v[c]))) leave.more(c, float(v[c]));
+            }
+    }
+}
+
 template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_many(Attend<T, KV> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = MANY_KEYS / EACH / 4;
-    extern __shared__ __align__(16) uint8_t lds[];
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2, LOADS = TILE / 4096;
+    typedef Bring<T, D, WIDE, false> B;
+    extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
+    int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
@@ -96,11 +141,13 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
     const int32_t m = at.rows.count, n = kv.count;
     const int64_t first = at.first + wave * 32;
     const Row row = row_of(first + (lane & 31), m, n, a.shared, a.causal);
-    // the keys that this wavefront's first and last row see, and the last of the workgroup's
+    // the keys that this wavefront's first and last row see, and the workgroup's
     const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
     const int32_t all = __builtin_amdgcn_readfirstlane(row_of(at.first + MANY_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t fewest = __builtin_amdgcn_readfirstlane(row_of(at.first, m, n, a.shared, a.causal).limit);
     const int32_t begin = a.chunk * int32_t(blockIdx.y), end = a.chunk ? min(all, begin + a.chunk) : all;
     if (a.chunk && begin >= end) return;
+    if (threadIdx.x == 0) cleansed = 0;
 
     vec<T, 8> q[2 * ND];
     {
@@ -108,21 +155,15 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 #pragma unroll
         for (int kk = 0; kk < 2 * ND; kk++) q[kk] = eight_values<WIDE>(from + (2 * kk + half) * 8, row.there ? a.d - (2 * kk + half) * 8 : 0);
     }
-    // which chunk of which row of a tile this lane brings
-    const int r0 = wave * EACH + lane / LANES, ck = int(chunk_at<D, false>(r0, lane % LANES)) * 8, cv = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
+    const B bring(kv, wave * B::EACH + lane / B::LANES, a.d);
     typename decltype(kv)::Ahead ahead[LOADS];
     auto look = [&](int32_t j0) {
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + r0 + i * 4 * EACH);
+        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + (i * 4 + wave) * B::EACH);
     };
-    auto bring = [&](int32_t j0, uint8_t* to) {
+    auto load = [&](int32_t j0, uint8_t* to) {
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const int32_t j = j0 + r0 + i * 4 * EACH;
-            const T *const k = kv.key(j, ahead[i]), *const v = kv.value(j, ahead[i]);
-            chunk_to_lds<WIDE>(k ? k + ck : k, j < n ? a.d - ck : 0, to + (i * 4 + wave) * 1024);
-            chunk_to_lds<WIDE>(v ? v + cv : v, j < n ? a.d - cv : 0, to + TILE + (i * 4 + wave) * 1024);
-        }
+        for (int i = 0; i < LOADS; i++) bring(kv, j0 + (i * 4 + wave) * B::EACH, ahead[i], a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
     };
     const uint32_t lds0 = lds_address(lds);
     // where this lane reads keys (rows lane % 32) and values (rows 4 * half on, columns)
@@ -137,13 +178,17 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
     float base = -INFINITY, sum = 0.f;
     f32x16 o[ND] = {};
     look(begin);
-    bring(begin, lds);
+    load(begin, lds);
     look(begin + MANY_KEYS);
     int now = 0;
     for (int32_t j0 = begin; j0 < end; j0 += MANY_KEYS, now ^= 1) {
         landed<0>();
+        if (j0 + MANY_KEYS > fewest && fewest < n) {        // some row does not see some key
+            if (cleanse<T>(lds + now * 2 * TILE + TILE, TILE, threadIdx.x, 256)) cleansed = 1;
+            __syncthreads();
+        }
         if (j0 + MANY_KEYS < end) {
-            bring(j0 + MANY_KEYS, lds + (now ^ 1) * 2 * TILE);
+            load(j0 + MANY_KEYS, lds + (now ^ 1) * 2 * TILE);
             look(j0 + 2 * MANY_KEYS);
         }
         if (j0 >= most) continue;
@@ -153,13 +198,12 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
         for (int kb = 0; kb < 2; kb++)
 #pragma unroll
             for (int kk = 0; kk < 2 * ND; kk++) s[kb] = product32(chunk_from<T>(tile + k_at[kk] + kb * 32 * D * 2), q[kk], s[kb]);
-        const bool some = j0 + MANY_KEYS > least;       // some row does not see some key
-        if (some)
+        if (j0 + MANY_KEYS > least) {
 #pragma unroll
             for (int kb = 0; kb < 2; kb++)
 #pragma unroll
-                for (int i = 0; i < 16; i++)
-                    s[kb][i] = or_none(s[kb][i], row.limit - 1 - (j0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4));
+                for (int i = 0; i < 16; i++) s[kb][i] = or_none(s[kb][i], row.limit - 1 - (j0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4));
+        }
         float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
         for (int i = 1; i < 16; i++) top = fmaxf(fmaxf(s[0][i], s[1][i]), top);
@@ -182,21 +226,13 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
                 sum += e;
                 p[kb * 2 + i / 8][i % 8] = T(e);
             }
-        if (some && least < min(j0 + MANY_KEYS, n)) {
-            if (any_not_finite<T>(tile + TILE, TILE)) {
-                uint32_t from[ND];
-#pragma unroll
-                for (int dt = 0; dt < ND; dt++) from[dt] = tile + v_at[dt];
-                careful<2, true, D, T, ND>(p, from, o, [&](int k) { return row.limit - (j0 + k); });
-                continue;
-            }
-        }
 #pragma unroll
         for (int k = 0; k < 4; k++)
 #pragma unroll
             for (int dt = 0; dt < ND; dt++) o[dt] = product32(turned32<D, T>(tile + v_at[dt] + k * 16 * D * 2), p[k], o[dt]);
     }
     own_landed<0>();
+    __syncthreads();
     sum = half_sum(sum);
     if (!row.there) return;
     const Leave<T, KV> leave(a, at.rows.first + row.token, hk * a.shared + row.head);
@@ -209,6 +245,8 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
             leave.template four<WIDE>(dt * 32 + i * 8 + half * 4, a.d, v, inverse);
         }
     if (half == 0) leave.total(base, sum, a.scale);
+    // the tiles that were cleansed begin with the first that some row does not see whole
+    if (cleansed) repair<ND>(leave, kv, max(begin, fewest / MANY_KEYS * MANY_KEYS), min(row.limit, end), a.d);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -219,9 +257,11 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 constexpr int FEW_KEYS = 32;
 
 template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launch_bounds__(256, 1) void k_attend_few(Attend<T, KV> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = FEW_KEYS * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = FEW_KEYS / EACH, ROWS = 16 * RB;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = FEW_KEYS * D * 2, LOADS = TILE / 1024, ROWS = 16 * RB;
+    typedef Bring<T, D, WIDE, true> B;
     constexpr int SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
     extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ int32_t cleansed[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, li = lane & 15;
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
@@ -243,21 +283,19 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
         for (int kk = 0; kk < ND; kk++) q[b][kk] = eight_values<WIDE>(from + (4 * kk + quarter) * 8, row[b].there ? a.d - (4 * kk + quarter) * 8 : 0);
     }
     uint8_t* const mine = lds + wave * 4 * TILE;
-    const int r0 = lane / LANES;
+    // rows 8 and more apart have other swizzles: two loads in turn
+    const B even(kv, lane / B::LANES, a.d), odd(kv, 8 + lane / B::LANES, a.d), next(kv, 4 + lane / B::LANES, a.d), last(kv, 12 + lane / B::LANES, a.d);
     typename decltype(kv)::Ahead ahead[LOADS];
     auto look = [&](int32_t j0) {
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + r0 + i * EACH);
+        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + i * B::EACH);
     };
-    auto bring = [&](int32_t j0, uint8_t* to) {
+    auto load = [&](int32_t j0, uint8_t* to) {
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
-            const int r = r0 + i * EACH;
-            const int32_t j = j0 + r;
-            const int ck = int(chunk_at<D, true>(r, lane % LANES)) * 8, cv = int(chunk_at<D, true>(r, lane % LANES)) * 8;
-            const T *const k = kv.key(j, ahead[i]), *const v = kv.value(j, ahead[i]);
-            chunk_to_lds<WIDE>(k ? k + ck : k, j < n ? a.d - ck : 0, to + i * 1024);
-            chunk_to_lds<WIDE>(v ? v + cv : v, j < n ? a.d - cv : 0, to + TILE + i * 1024);
+            const int r = i * B::EACH % 16;
+            const B& bring = r == 0 ? even : r == 4 ? next : r == 8 ? odd : last;
+            bring(kv, j0 + i * B::EACH, ahead[i], a.d, to + i * 1024, to + TILE + i * 1024);
         }
     };
     const uint32_t lds0 = lds_address(mine);
@@ -276,14 +314,15 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
     const int32_t start = begin + wave * FEW_KEYS;
     if (start < end) {
         look(start);
-        bring(start, mine);
+        load(start, mine);
         look(start + 4 * FEW_KEYS);
     }
     int now = 0;
+    bool found = false;
     for (int32_t j0 = start; j0 < end; j0 += 4 * FEW_KEYS, now ^= 1) {
         own_landed<0>();
         if (j0 + 4 * FEW_KEYS < end) {
-            bring(j0 + 4 * FEW_KEYS, mine + (now ^ 1) * 2 * TILE);
+            load(j0 + 4 * FEW_KEYS, mine + (now ^ 1) * 2 * TILE);
             look(j0 + 8 * FEW_KEYS);
         }
         const uint32_t tile = lds0 + now * 2 * TILE;
@@ -297,6 +336,10 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
                 for (int b = 0; b < RB; b++) s[b][kb] = product16(k, q[b][kk], s[b][kb]);
             }
         const bool some = j0 + FEW_KEYS > least;
+        if (some && least < n) {
+            found = __any(cleanse<T>(mine + now * 2 * TILE + TILE, TILE, lane, 64)) || found;
+            wave_order();
+        }
         vec<T, 8> p[RB];
 #pragma unroll
         for (int b = 0; b < RB; b++) {
@@ -324,35 +367,11 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
                 p[b][i] = T(e);
             }
         }
-        const bool bad = some && least < min(j0 + FEW_KEYS, n) && any_not_finite<T>(tile + TILE, TILE);
-        if (!bad) {
 #pragma unroll
-            for (int dt = 0; dt < 2 * ND; dt++) {
-                const vec<T, 8> v = turned_from<T>(tile + v_at[dt], tile + v_at[dt] + 16 * D * 2);
+        for (int dt = 0; dt < 2 * ND; dt++) {
+            const vec<T, 8> v = turned_from<T>(tile + v_at[dt], tile + v_at[dt] + 16 * D * 2);
 #pragma unroll
-                for (int b = 0; b < RB; b++) o[b][dt] = product16(v, p[b], o[b][dt]);
-            }
-        } else {                // as careful() does
-#pragma unroll
-            for (int dt = 0; dt < 2 * ND; dt++) {
-                __builtin_amdgcn_sched_barrier(0);
-                vec<T, 8> v = turned_from<T>(tile + v_at[dt], tile + v_at[dt] + 16 * D * 2), u, w;
-                parted<T>(v, u, w);
-#pragma unroll
-                for (int b = 0; b < RB; b++) {
-                    uint32_t sees[4];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const int32_t j = j0 + e / 2 * 16 + quarter * 4 + e % 2 * 2;
-                        sees[e] = one_if<T>(row[b].limit - j) | one_if<T>(row[b].limit - j - 1) << 16;
-                    }
-                    const vec<T, 8> see = __builtin_bit_cast(vec<T, 8>, make_uint4(sees[0], sees[1], sees[2], sees[3]));
-                    o[b][dt] = product16(v, p[b], o[b][dt]);
-                    const f32x4 none = {}, up = product16(u, see, none), down = product16(w, see, none);
-#pragma unroll
-                    for (int i = 0; i < 4; i++) o[b][dt][i] += counted<true>(up[i], down[i]);
-                }
-            }
+            for (int b = 0; b < RB; b++) o[b][dt] = product16(v, p[b], o[b][dt]);
         }
     }
     // Joined by way of LDS: [wave][row][d], and their bases and totals.
@@ -361,6 +380,7 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
     constexpr int PITCH = ND * 32 + 4;      // floats of a row: 16 rows' four values from one column on begin in other banks
     float* const sums = reinterpret_cast<float*>(lds);
     __shared__ float bases[4][ROWS], totals[4][ROWS];
+    if (lane == 0) cleansed[wave] = found;
 #pragma unroll
     for (int b = 0; b < RB; b++) {
         const float total = quarter_sum(sum[b]);
@@ -389,6 +409,12 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
         const Leave<T, KV> leave(a, at.rows.first + it.token, hk * a.shared + it.head);
         leave.template four<WIDE>(x, a.d, v, total == 0.f ? 0.f : 1.f / total);
         if (x == 0) leave.total(top, total, a.scale);
+        if (cleansed[0] | cleansed[1] | cleansed[2] | cleansed[3])
+            for (int32_t j = max(begin, least / FEW_KEYS * FEW_KEYS); j < min(it.limit, end); j++) {
+                const T* const from = kv.any_value(j);
+                for (int e = 0; from && e < 4; e++)
+                    if (x + e < a.d && !finite(float(from[x + e]))) leave.more(x + e, float(from[x + e]));
+            }
     }
 }
 
@@ -470,7 +496,7 @@ template <typename T, typename KV> int attend(Attend<T, KV> a, const Plan& p, bo
         if (p.blocks == 1) few(std::integral_constant<int, 1>());
         else if (p.blocks == 2) few(std::integral_constant<int, 2>());
         else if (p.blocks == 4) few(std::integral_constant<int, 4>());
-        else k_attend_many<T, KV, ND, WIDE><<<grid, 256, 4 * MANY_KEYS * TILE, s>>>(a);
+        else k_attend_many<T, KV, ND, WIDE><<<grid, 256, 4 * MANY_KEYS * TILE + 16, s>>>(a);
     };
     auto by = [&](auto nd) {
         if (wide) go(nd, std::true_type());

@@ -87,7 +87,8 @@ constexpr int BACK_ROWS = 128, BACK_SHIFT = 7, BACK_STEP = 64;
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
     constexpr int D = ND <= 2 ? 64 : 128, TILE = BACK_STEP * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = BACK_STEP / EACH / 4;
-    extern __shared__ __align__(16) uint8_t lds[];
+    extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
+    int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
@@ -97,6 +98,8 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     const Row row = row_of(at.first + wave * 32 + (lane & 31), m, n, a.shared, a.causal);
     const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
     const int32_t end = __builtin_amdgcn_readfirstlane(row_of(at.first + BACK_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t fewest = __builtin_amdgcn_readfirstlane(row_of(at.first, m, n, a.shared, a.causal).limit);
+    if (threadIdx.x == 0) cleansed = 0;
     const int64_t token = at.rows.first + row.token;
     const int h = hk * a.shared + row.head;
     vec<T, 8> q[2 * ND], dout[2 * ND];
@@ -122,6 +125,10 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     int now = 0;
     for (int32_t j0 = 0; j0 < end; j0 += BACK_STEP, now ^= 1) {
         landed<0>();
+        if (j0 + BACK_STEP > fewest && fewest < n) {        // some row does not see some key
+            if (cleanse<T>(lds + now * 2 * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
+            __syncthreads();
+        }
         if (j0 + BACK_STEP < end) bring(j0 + BACK_STEP, lds + (now ^ 1) * 2 * TILE);
 #pragma unroll
         for (int kb = 0; kb < 2; kb++) {
@@ -145,21 +152,24 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
             }
 #pragma unroll
             for (int i = 0; i < 16; i++) ds[i / 8][i % 8] = T(s[i]);
-            if (some && least < min(j + 32, n) && any_not_finite<T>(tile, 32 * D * 2)) {
-                uint32_t from[ND];
 #pragma unroll
-                for (int dt = 0; dt < ND; dt++) from[dt] = tile + read.turned[dt];
-                careful<1, false, D, T, ND>(ds, from, dq, [&](int k) { return row.limit - (j + k); });
-            } else {
+            for (int k = 0; k < 2; k++)
 #pragma unroll
-                for (int k = 0; k < 2; k++)
-#pragma unroll
-                    for (int dt = 0; dt < ND; dt++) dq[dt] = product32(turned32<D, T>(tile + read.turned[dt] + k * 16 * D * 2), ds[k], dq[dt]);
-            }
+                for (int dt = 0; dt < ND; dt++) dq[dt] = product32(turned32<D, T>(tile + read.turned[dt] + k * 16 * D * 2), ds[k], dq[dt]);
         }
     }
     own_landed<0>();
-    if (row.there) leave<ND, WIDE>(a.dq.p + token * a.dq.row + h * a.dq.head, dq, a.scale, a.d);
+    __syncthreads();
+    if (!row.there) return;
+    T* const to = a.dq.p + token * a.dq.row + h * a.dq.head;
+    leave<ND, WIDE>(to, dq, a.scale, a.d);
+    // a key that is not finite makes the values of dq not finite that it has so; the others are by way of lse
+    if (cleansed)
+        for (int32_t j = fewest / BACK_STEP * BACK_STEP; j < row.limit; j++)
+            for (int i = 0; i < 16 * ND; i++) {
+                const int x = i / 4 * 8 + half * 4 + i % 4;
+                if (x < a.d && !finite(float(k0[j * a.k.row + x]))) to[x] = T(NAN);
+            }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -168,7 +178,8 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) void k_attend_dkv(Back<T> a) {
     constexpr int D = ND <= 2 ? 64 : 128, TILE = BACK_STEP * D * 2, STAGE = 2 * TILE + 512, LANES = D / 8, EACH = 64 / LANES, LOADS = BACK_STEP / EACH / 4;
-    extern __shared__ __align__(16) uint8_t lds[];
+    extern __shared__ __align__(16) uint8_t lds[];          // begins at 0
+    int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 2 * STAGE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
@@ -183,6 +194,8 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
     const float c = a.scale * LOG2_E;
     // query i sees key j where j <= i + ahead
     const int32_t ahead = a.causal ? n - m : n;         // sums of two are below 2^31
+    const int32_t whole = max(0, int32_t(at.first) + BACK_ROWS - 1 - ahead);      // the first query that sees all of the workgroup's keys
+    if (threadIdx.x == 0) cleansed = 0;
     const int32_t start = max(0, int32_t(at.first) - ahead) / BACK_STEP * BACK_STEP, steps = m > start ? (m - start + BACK_STEP - 1) / BACK_STEP : 0;
 
     const int r0 = wave * EACH + lane / LANES, chunk = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
@@ -211,6 +224,10 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
     int32_t i0 = start;
     for (int32_t step = 0; step < total; step++, now ^= 1, i0 = i0 + BACK_STEP < m ? i0 + BACK_STEP : start) {
         landed<0>();
+        if (i0 < whole && i0 + ahead < n - 1) {             // some query does not see some key
+            if (cleanse<T>(lds + now * STAGE, 2 * TILE, threadIdx.x, 256)) cleansed = 1;
+            __syncthreads();
+        }
         if (step + 1 < total) bring(step + 1, lds + (now ^ 1) * STAGE);
 #pragma unroll
         for (int rb = 0; rb < 2; rb++) {
@@ -222,7 +239,7 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
             for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), k[kk], s);
 #pragma unroll
             for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), v[kk], dp);
-            const bool hidden = i + ahead < first + 31, some = hidden || i + 32 > m;      // some query does not see some key; or there is none
+            const bool some = i + ahead < first + 31 || i + 32 > m;         // some query does not see some key; or there is none
             vec<T, 8> p[2], ds[2];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
@@ -242,30 +259,37 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
             }
 #pragma unroll
             for (int w = 0; w < 16; w++) p[w / 8][w % 8] = T(s[w]), ds[w / 8][w % 8] = T(dp[w]);
-            if (hidden && (any_not_finite<T>(tile, 32 * D * 2) || any_not_finite<T>(tile + TILE, 32 * D * 2))) {
-                uint32_t from[ND];
-                auto see = [&](int r) { return min(m - (i + r), i + r + ahead - key + 1); };
 #pragma unroll
-                for (int dt = 0; dt < ND; dt++) from[dt] = tile + TILE + read.turned[dt];
-                careful<1, true, D, T, ND>(p, from, dv, see);
+            for (int x = 0; x < 2; x++)
 #pragma unroll
-                for (int dt = 0; dt < ND; dt++) from[dt] = tile + read.turned[dt];
-                careful<1, false, D, T, ND>(ds, from, dk, see);
-            } else {
-#pragma unroll
-                for (int x = 0; x < 2; x++)
-#pragma unroll
-                    for (int dt = 0; dt < ND; dt++) {
-                        dv[dt] = product32(turned32<D, T>(tile + TILE + read.turned[dt] + x * 16 * D * 2), p[x], dv[dt]);
-                        dk[dt] = product32(turned32<D, T>(tile + read.turned[dt] + x * 16 * D * 2), ds[x], dk[dt]);
-                    }
-            }
+                for (int dt = 0; dt < ND; dt++) {
+                    dv[dt] = product32(turned32<D, T>(tile + TILE + read.turned[dt] + x * 16 * D * 2), p[x], dv[dt]);
+                    dk[dt] = product32(turned32<D, T>(tile + read.turned[dt] + x * 16 * D * 2), ds[x], dk[dt]);
+                }
         }
     }
     own_landed<0>();
+    __syncthreads();
     if (!there) return;
-    leave<ND, WIDE>(a.dk.p + token * a.dk.row + hk * a.dk.head, dk, a.scale, a.d);
-    leave<ND, WIDE>(a.dv.p + token * a.dv.row + hk * a.dv.head, dv, 1.f, a.d);
+    T *const to_k = a.dk.p + token * a.dk.row + hk * a.dk.head, *const to_v = a.dv.p + token * a.dv.row + hk * a.dv.head;
+    leave<ND, WIDE>(to_k, dk, a.scale, a.d);
+    leave<ND, WIDE>(to_v, dv, 1.f, a.d);
+    if (!cleansed) return;
+    // a query that is not finite makes all of dk and dv so of the keys that it sees, a dout that is not all of dk, and the values of dv that it has so
+    for (int g = 0; g < a.shared; g++)
+        for (int32_t i = max(start, key - ahead); i < min(m, start + (whole - start + BACK_STEP - 1) / BACK_STEP * BACK_STEP); i++) {
+            const T *const q = a.q.p + (mine.first + i) * a.q.row + (hk * a.shared + g) * a.q.head, *const o = a.dout.p + (mine.first + i) * a.dout.row + (hk * a.shared + g) * a.dout.head;
+            bool bad_q = false, bad_o = false;
+            for (int x = 0; x < a.d; x++) bad_q = bad_q || !finite(float(q[x])), bad_o = bad_o || !finite(float(o[x]));
+            if (!bad_q && !bad_o) continue;
+            for (int e = 0; e < 16 * ND; e++) {
+                const int x = e / 4 * 8 + half * 4 + e % 4;
+                if (x >= a.d) continue;
+                to_k[x] = T(NAN);
+                if (bad_q) to_v[x] = T(NAN);
+                else if (!finite(float(o[x]))) to_v[x] = T(float(to_v[x]) + float(o[x]));
+            }
+        }
 }
 
 }  // namespace
@@ -299,9 +323,9 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
             constexpr bool WIDE = decltype(is_wide)::value;
             if (rows > 0) {
                 k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
-                k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2, s>>>(a);
+                k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2 + 16, s>>>(a);
             }
-            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2 + 1024, s>>>(a);
+            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2 + 1024 + 16, s>>>(a);
         };
         auto by = [&](auto nd) {
             if (w) go(nd, std::true_type());

@@ -62,7 +62,8 @@ __device__ __forceinline__ bool tile_of(const int32_t* offset, int32_t sequences
     return out.first >= 0 && out.first < int64_t(out.rows.count) * times;
 }
 
-// Keys and values of one sequence and head, packed or in a cache: where row j of either is.
+// Keys and values of one sequence and head, packed or in a cache: where row j of either is, and whether rows from j on (a multiple of
+// their number) lie side by side, so that one address serves a wavefront's load.
 template <typename T> struct Packed {
     const int32_t* offset;
     int32_t rows;
@@ -71,15 +72,17 @@ template <typename T> struct Packed {
         const T *k, *v;
         int64_t k_row, v_row;
         int32_t count;
-        // What is looked up ahead of a row's loads (a packed row needs nothing).
-        struct Ahead {};
-        __device__ __forceinline__ Ahead ahead(int32_t) const { return {}; }
+        typedef int Ahead;          // what is looked up ahead of a load (for packed rows nothing)
+        __device__ __forceinline__ Ahead ahead(int32_t) const { return 0; }
+        template <int ROWS> __device__ __forceinline__ bool together(Ahead) const { return true; }
         __device__ __forceinline__ const T* key(int32_t j, Ahead) const { return k + j * k_row; }
         __device__ __forceinline__ const T* value(int32_t j, Ahead) const { return v + j * v_row; }
+        __device__ __forceinline__ const T* any_key(int32_t j) const { return k + j * k_row; }
+        __device__ __forceinline__ const T* any_value(int32_t j) const { return v + j * v_row; }
     };
     __device__ __forceinline__ One one(int32_t s, int32_t h) const {
         const Span at = span_of(offset, s, rows);
-        return {same(k.p + at.first * k.row + h * k.head), same(v.p + at.first * v.row + h * v.head), k.row, v.row, at.count};
+        return {same(k.p + at.first * k.row + h * k.head), same(v.p + at.first * v.row + h * v.head), k.row, v.row, __builtin_amdgcn_readfirstlane(at.count)};
     }
 };
 template <typename T> struct Paged {
@@ -93,16 +96,28 @@ template <typename T> struct Paged {
         const T *k, *v;
         int64_t k_page, k_row, v_page, v_row;
         int32_t count;
-        typedef int32_t Ahead;      // the page; -1: a row of zeros
+        typedef int32_t Ahead;      // the page of a row that is the same in every lane; -1: none
         __device__ __forceinline__ int32_t ahead(int32_t j) const {
-            const int32_t page = j < count ? table[j >> shift] : -1;
+            typedef const __attribute__((address_space(4))) int32_t* constant;      // a scalar load
+            const int32_t page = j < count ? ((constant)(uintptr_t)table)[j >> shift] : -1;
             return uint32_t(page) < uint32_t(pages) ? page : -1;
         }
-        __device__ __forceinline__ const T* key(int32_t j, int32_t page) const { return page < 0 ? nullptr : k + page * k_page + (j & ((1 << shift) - 1)) * k_row; }
-        __device__ __forceinline__ const T* value(int32_t j, int32_t page) const { return page < 0 ? nullptr : v + page * v_page + (j & ((1 << shift) - 1)) * v_row; }
+        template <int ROWS> __device__ __forceinline__ bool together(int32_t page) const { return page >= 0 && (1 << shift) >= ROWS; }
+        __device__ __forceinline__ const T* key(int32_t j, int32_t page) const { return k + page * k_page + (j & ((1 << shift) - 1)) * k_row; }
+        __device__ __forceinline__ const T* value(int32_t j, int32_t page) const { return v + page * v_page + (j & ((1 << shift) - 1)) * v_row; }
+        // of any row, j < count, which may be another one in every lane; NULL: a row of zeros
+        __device__ __forceinline__ const T* any_key(int32_t j) const {
+            const int32_t page = table[j >> shift];
+            return uint32_t(page) < uint32_t(pages) ? key(j, page) : nullptr;
+        }
+        __device__ __forceinline__ const T* any_value(int32_t j) const {
+            const int32_t page = table[j >> shift];
+            return uint32_t(page) < uint32_t(pages) ? value(j, page) : nullptr;
+        }
     };
     __device__ __forceinline__ One one(int32_t s, int32_t h) const {
-        return {same(table + s * ldt), pages, shift, same(k.p + h * k.head), same(v.p + h * v.head), k.page, k.row, v.page, v.row, int32_t(min(int64_t(max(length[s], 0)), int64_t(width) << shift))};
+        const int32_t count = int32_t(min(int64_t(max(length[s], 0)), int64_t(width) << shift));
+        return {same(table + s * ldt), pages, shift, same(k.p + h * k.head), same(v.p + h * v.head), k.page, k.row, v.page, v.row, __builtin_amdgcn_readfirstlane(count)};
     }
 };
 
@@ -167,35 +182,12 @@ template <typename T> __device__ __forceinline__ vec<T, 8> turned_from(uint32_t 
 // For 32 x 32 x 16: columns of four rows and of those 8 rows on, where bit 1 of a chunk's place is the other one.
 template <int D, typename T> __device__ __forceinline__ vec<T, 8> turned32(uint32_t at) { return turned_from<T>(at, (at ^ 32) + 8 * D * 2); }
 
-// One wavefront's load into LDS: 1024 bytes, lane by lane 16 of them; `from` NULL, or values from `have` on: zeros.
+// One wavefront's load into LDS, from an address of each lane: 1024 bytes, lane by lane 16 of them; `from` NULL, or values from `have` on: zeros.
 template <bool WIDE, typename T> __device__ __forceinline__ void chunk_to_lds(const T* from, int have, uint8_t* to) {
     if (WIDE) to_lds(from && have > 0 ? static_cast<const void*>(from) : &ZEROS, to);
     else *reinterpret_cast<vec<T, 8>*>(to + (threadIdx.x & 63) * 16) = eight_values<false>(from, from ? have : 0);
 }
 
-// The largest magnitude of 16-bit values, in pairs of them: whether one is not finite.
-template <typename T> constexpr uint32_t NOT_FINITE = std::is_same<T, f16>::value ? 0x7c00u : 0x7f80u;
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void most_of(u16x2& most, uint32_t w) {
-    const u16x2 v = __builtin_bit_cast(u16x2, w & 0x7fff7fffu);
-    most = __builtin_elementwise_max(most, v);
-}
-template <typename T> __device__ __forceinline__ bool not_finite(u16x2 most) { return most[0] >= NOT_FINITE<T> || most[1] >= NOT_FINITE<T>; }
-
-template <typename T> constexpr uint32_t ONE = std::is_same<T, f16>::value ? 0x3c00u : 0x3f80u;
-typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-// v without what is not finite; up: 1 where it is +inf or NaN, down: where it is -inf or NaN.  (By packed arithmetic: comparisons would need
-// a register of the scalar file each.)
-template <typename T> __device__ __forceinline__ void parted(vec<T, 8>& v, vec<T, 8>& up, vec<T, 8>& down) {
-    const u16x8 w = __builtin_bit_cast(u16x8, v), size = w & uint16_t(0x7fff), finite = uint16_t(NOT_FINITE<T> - 1), inf = uint16_t(NOT_FINITE<T>), one = 1;
-    const u16x8 bad = __builtin_elementwise_min(__builtin_elementwise_max(size, finite) - finite, one), nan = __builtin_elementwise_min(__builtin_elementwise_max(size, inf) - inf, one);
-    const u16x8 minus = w >> 15;
-    up = __builtin_bit_cast(vec<T, 8>, u16x8((bad & (nan | (minus ^ one))) * uint16_t(ONE<T>)));
-    down = __builtin_bit_cast(vec<T, 8>, u16x8((bad & (nan | minus)) * uint16_t(ONE<T>)));
-    v = __builtin_bit_cast(vec<T, 8>, u16x8(w & (bad - one)));
-}
-// 1 where `margin` is positive
-template <typename T> __device__ __forceinline__ uint32_t one_if(int32_t margin) { return uint32_t(min(max(margin, 0), 1)) * ONE<T>; }
 // x, and 0 (-inf) where `hidden` is negative
 __device__ __forceinline__ float or_zero(float x, int32_t hidden) { return __uint_as_float(__float_as_uint(x) & ~uint32_t(hidden >> 31)); }
 __device__ __forceinline__ float or_none(float x, int32_t hidden) {
@@ -203,49 +195,25 @@ __device__ __forceinline__ float or_none(float x, int32_t hidden) {
     return __uint_as_float((__float_as_uint(x) & ~mask) | (mask & 0xff800000u));
 }
 
-// What counts of values that are not finite do to a sum: a count becomes 0 or infinity (no contraction: a fused product would stay below it).
-template <bool SIGNED> __device__ __forceinline__ float counted(float up, float down) {
-#pragma clang fp contract(off)
-    const float x = up * 0x1p127f * 0x1p127f, y = down * 0x1p127f * 0x1p127f;
-    return SIGNED ? x - y : (x - x) + (y - y);
-}
-
-// acc += v p over a depth of 32 K for products of 32 x 32 x 16, v turned on the way (at[i]: where this lane reads the first four rows of columns 32 i on),
-// p the second operand, where some p are 0 because the mask hides that depth from that column and v has values that are not finite: a product
-// 0 * inf must not show.  Such values are left out, and what they do to the columns that see them is found by counting; see(k): positive where
-// this lane's column sees depth k.  SIGNED: p is positive, so their sign is the sum's; else they make it NaN.
-template <int K, bool SIGNED, int D, typename T, int ND, typename See> __device__ __forceinline__ void careful(const vec<T, 8>* p, const uint32_t (&at)[ND], f32x16 (&acc)[ND], See see) {
-    const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-    for (int dt = 0; dt < ND; dt++) {
-        f32x16 up = {}, down = {};
-#pragma unroll
-        for (int k = 0; k < 2 * K; k++) {
-            __builtin_amdgcn_sched_barrier(0);      // one after the other: registers count here, not time
-            vec<T, 8> v = turned32<D, T>(at[dt] + k * 16 * D * 2), u, w;
-            parted<T>(v, u, w);
-            uint32_t sees[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int at_k = k * 16 + (e / 2) * 8 + half * 4 + e % 2 * 2;
-                sees[e] = one_if<T>(see(at_k)) | one_if<T>(see(at_k + 1)) << 16;
-            }
-            const vec<T, 8> s = __builtin_bit_cast(vec<T, 8>, make_uint4(sees[0], sees[1], sees[2], sees[3]));
-            acc[dt] = product32(v, p[k], acc[dt]), up = product32(u, s, up), down = product32(w, s, down);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i++) acc[dt][i] += counted<SIGNED>(up[i], down[i]);
+// Where a mask hides some depth of a product from some columns, their p are 0, and a value there that is not finite must not show, as 0 * inf would.
+// So a tile with such values, seldom as they are, is cleansed of them in LDS before it is read, and what they do to the columns that do see them is
+// added to the results in the end, from memory.  (A second way through the products for such tiles would take the first one's registers: the attention of
+// 3 sequences up to 8001 took 985 us with it.)  Bytes [from, to) of this tile by lanes that have `lane` of `lanes`; whether there were some.
+template <typename T> __device__ __forceinline__ bool cleanse(uint8_t* tile, int bytes, int lane, int lanes) {
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+    constexpr uint16_t LARGEST = std::is_same<T, f16>::value ? 0x7bff : 0x7f7f;
+    bool found = false;
+    for (int i = lane * 16; i < bytes; i += lanes * 16) {
+        u16x8* const at = reinterpret_cast<u16x8*>(tile + i);
+        const u16x8 w = *at, over = __builtin_elementwise_max(w & uint16_t(0x7fff), u16x8(LARGEST)) - LARGEST;     // 0: finite
+        const uint4 some = __builtin_bit_cast(uint4, over);
+        if (!(some.x | some.y | some.z | some.w)) continue;
+        *at = w & (__builtin_elementwise_min(over, u16x8(1)) - uint16_t(1));
+        found = true;
     }
+    return found;
 }
-// Whether `bytes` of LDS have a value that is not finite, by all lanes of a wavefront.
-template <typename T> __device__ __forceinline__ bool any_not_finite(uint32_t at, int bytes) {
-    u16x2 size = {0, 0};
-    for (int i = (threadIdx.x & 63) * 16; i < bytes; i += 1024) {
-        const uint4 w = __builtin_bit_cast(uint4, chunk_from<T>(at + i));
-        most_of(size, w.x), most_of(size, w.y), most_of(size, w.z), most_of(size, w.w);
-    }
-    return __any(not_finite<T>(size));
-}
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 
 // ---------------------------------------------------------------------------------------------------------------
 // What calls ask of their sizes
