@@ -82,38 +82,12 @@ template <typename T, typename KV> struct Leave {
 };
 
 // ---------------------------------------------------------------------------------------------------------------
-// Many rows.  128 folded rows, 32 to each of four wavefronts, which go through the keys in tiles of 64.
-// Scores are computed as keys x rows, k q^T: a lane has 32 of the 64 scores of one row, so the maximum and the sum need one exchange
+// Many rows.  128 folded rows, 32 to each of four wavefronts, which go through the keys in tiles of 32.
+// Scores are computed as keys x rows, k q^T: a lane has 16 of the 32 scores of one row, so the maximum and the sum need one exchange
 // with the lane's other half, and what it has is, rounded, the second operand of out^T = v^T p^T as it is: the order of the depth (keys) is free as
 // long as v's, which a transposing read of LDS brings, is the same.  Two tiles of keys and values are in LDS, the next one on its way.
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int MANY_ROWS = 128, MANY_SHIFT = 7, MANY_KEYS = 64;
-
-// What this lane asks for of the rows of a load: they lie side by side from one address on, or each is looked for.
-template <typename T, int D, bool WIDE, bool SMALL> struct Bring {
-    static constexpr int LANES = D / 8, EACH = 64 / LANES;      // lanes of a row, rows of a load
-    int row, chunk;             // this lane's, in a load
-    uint32_t k_off, v_off;      // in bytes, from the load's first row
-    bool near;                  // every lane's chunk is in the row, and no offset passes 32 bits
-    // first: the row of a tile that this lane has in its first load (in others a multiple of 16 further)
-    template <typename One> __device__ __forceinline__ Bring(const One& kv, int first, int d) {
-        row = (threadIdx.x & 63) / LANES, chunk = int(chunk_at<D, SMALL>(first, threadIdx.x % LANES)) * 8;
-        // where d ends within a chunk that is read, or beside it, there are zeros to be had; a chunk that is not read may be another one
-        near = WIDE && (d == D || (D == 128 && d == 96)) && (EACH * kv.k_row | EACH * kv.v_row) < (1 << 28);
-        const int c = chunk < d ? chunk : 0;
-        k_off = uint32_t(row * kv.k_row + c) * 2, v_off = uint32_t(row * kv.v_row + c) * 2;
-    }
-    // rows j (a multiple of EACH, the same in every lane) on, to k and v
-    template <typename One> __device__ __forceinline__ void operator()(const One& kv, int32_t j, typename One::Ahead ahead, int d, uint8_t* k, uint8_t* v) const {
-        if (near && j + EACH <= kv.count && kv.template together<EACH>(ahead)) {
-            to_lds(kv.key(j, ahead), k_off, k), to_lds(kv.value(j, ahead), v_off, v);
-        } else {
-            const bool there = j + row < kv.count;
-            const T *const from = there ? kv.any_key(j + row) : nullptr, *const of = there ? kv.any_value(j + row) : nullptr;
-            chunk_to_lds<WIDE>(from ? from + chunk : from, d - chunk, k), chunk_to_lds<WIDE>(of ? of + chunk : of, d - chunk, v);
-        }
-    }
-};
+constexpr int MANY_ROWS = 128, MANY_SHIFT = 7, MANY_KEYS = 32;
 
 // What a lane left of a row (values c = dt * 32 + i * 8 + half * 4 on) sees of keys [from, to), whose values that are not finite were left out.
 template <int ND, typename T, typename KV, typename One> __device__ __forceinline__ void repair(const Leave<T, KV>& leave, const One& kv, int32_t from, int32_t to, int d) {
@@ -128,7 +102,7 @@ template <int ND, typename T, typename KV, typename One> __device__ __forceinlin
     }
 }
 
-template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_many(Attend<T, KV> a) {
+template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 3) void k_attend_many(Attend<T, KV> a) {
     constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2, LOADS = TILE / 4096;
     typedef Bring<T, D, WIDE, false> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
@@ -193,20 +167,18 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
         }
         if (j0 >= most) continue;
         const uint32_t tile = lds0 + now * 2 * TILE;
-        f32x16 s[2] = {};
+        f32x16 s = {};
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) s[kb] = product32(chunk_from<T>(tile + k_at[kk] + kb * 32 * D * 2), q[kk], s[kb]);
+        for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + k_at[kk]), q[kk], s);
         if (j0 + MANY_KEYS > least) {
 #pragma unroll
-            for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) s[kb][i] = or_none(s[kb][i], row.limit - 1 - (j0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4));
+            for (int i = 0; i < 16; i++) s[i] = or_none(s[i], row.limit - 1 - (j0 + 8 * (i / 4) + 4 * half + i % 4));
         }
-        float top = fmaxf(s[0][0], s[1][0]);
+        __builtin_amdgcn_s_setprio(0);
+        float top = s[0];
 #pragma unroll
-        for (int i = 1; i < 16; i++) top = fmaxf(fmaxf(s[0][i], s[1][i]), top);
+        for (int i = 1; i < 16; i++) top = fmaxf(s[i], top);
         top = half_most(top);
         if (__any(top > base + rise)) {
             const float higher = fmaxf(base, top), less = higher == base ? 1.f : power((base - higher) * c);
@@ -217,19 +189,19 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
                 for (int i = 0; i < 16; i++) o[dt][i] *= less;
         }
         const float zero = base == -INFINITY ? 0.f : base * c;
-        vec<T, 8> p[4];
+        vec<T, 8> p[2];
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++)
+        for (int i = 0; i < 16; i++) {
+            const float e = power(fmaf(s[i], c, -zero));
+            sum += e;
+            p[i / 8][i % 8] = T(e);
+        }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const float e = power(fmaf(s[kb][i], c, -zero));
-                sum += e;
-                p[kb * 2 + i / 8][i % 8] = T(e);
-            }
-#pragma unroll
-        for (int k = 0; k < 4; k++)
+        for (int k = 0; k < 2; k++)
 #pragma unroll
             for (int dt = 0; dt < ND; dt++) o[dt] = product32(turned32<D, T>(tile + v_at[dt] + k * 16 * D * 2), p[k], o[dt]);
+        __builtin_amdgcn_s_setprio(0);
     }
     own_landed<0>();
     __syncthreads();

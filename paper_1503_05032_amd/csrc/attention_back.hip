@@ -80,24 +80,26 @@ template <int ND, bool WIDE, typename T> __device__ __forceinline__ void leave(T
         }
 }
 
-constexpr int BACK_ROWS = 128, BACK_SHIFT = 7, BACK_STEP = 64;
+constexpr int DQ_ROWS = 128, DQ_SHIFT = 7, DQ_STEP = 64;
+constexpr int DKV_KEYS = 64, DKV_SHIFT = 6, DKV_STEP = 64;
 
 // ---------------------------------------------------------------------------------------------------------------
 // dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 64.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = BACK_STEP * D * 2, LANES = D / 8, EACH = 64 / LANES, LOADS = BACK_STEP / EACH / 4;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = DQ_STEP * D * 2, LOADS = TILE / 4096;
+    typedef Bring<T, D, WIDE, false> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
-    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, BACK_SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
+    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, DQ_SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
     const Span keys = span_of(a.k_offset, at.s, a.k_rows);
     const int32_t m = at.rows.count, n = keys.count;
     const Row row = row_of(at.first + wave * 32 + (lane & 31), m, n, a.shared, a.causal);
     const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
-    const int32_t end = __builtin_amdgcn_readfirstlane(row_of(at.first + BACK_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t end = __builtin_amdgcn_readfirstlane(row_of(at.first + DQ_ROWS - 1, m, n, a.shared, a.causal).limit);
     const int32_t fewest = __builtin_amdgcn_readfirstlane(row_of(at.first, m, n, a.shared, a.causal).limit);
     if (threadIdx.x == 0) cleansed = 0;
     const int64_t token = at.rows.first + row.token;
@@ -107,29 +109,24 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     column<ND, WIDE>(dout, a.dout.p + token * a.dout.row + h * a.dout.head, row.there, a.d);
     const float delta = a.delta[int64_t(h) * a.rows + token], base = a.base[int64_t(h) * a.rows + token], c = a.scale * LOG2_E;
 
-    const int r0 = wave * EACH + lane / LANES, chunk = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
-    const T *const k0 = same(a.k.p + keys.first * a.k.row + hk * a.k.head), *const v0 = same(a.v.p + keys.first * a.v.row + hk * a.v.head);
-    auto bring = [&](int32_t j0, uint8_t* to) {
+    const typename Packed<T>::One kv{same(a.k.p + keys.first * a.k.row + hk * a.k.head), same(a.v.p + keys.first * a.v.row + hk * a.v.head), a.k.row, a.v.row, __builtin_amdgcn_readfirstlane(n)};
+    const B bring(kv, wave * B::EACH + lane / B::LANES, a.d);
+    auto load = [&](int32_t j0, uint8_t* to) {
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const int32_t j = j0 + r0 + i * 4 * EACH;
-            const int have = j < n ? a.d - chunk : 0;
-            chunk_to_lds<WIDE>(k0 + j * a.k.row + chunk, have, to + (i * 4 + wave) * 1024);
-            chunk_to_lds<WIDE>(v0 + j * a.v.row + chunk, have, to + TILE + (i * 4 + wave) * 1024);
-        }
+        for (int i = 0; i < LOADS; i++) bring(kv, j0 + (i * 4 + wave) * B::EACH, 0, a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
     };
     const uint32_t lds0 = lds_address(lds);
     const Read<ND> read;
     f32x16 dq[ND] = {};
-    bring(0, lds);
+    load(0, lds);
     int now = 0;
-    for (int32_t j0 = 0; j0 < end; j0 += BACK_STEP, now ^= 1) {
+    for (int32_t j0 = 0; j0 < end; j0 += DQ_STEP, now ^= 1) {
         landed<0>();
-        if (j0 + BACK_STEP > fewest && fewest < n) {        // some row does not see some key
+        if (j0 + DQ_STEP > fewest && fewest < n) {        // some row does not see some key
             if (cleanse<T>(lds + now * 2 * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
-        if (j0 + BACK_STEP < end) bring(j0 + BACK_STEP, lds + (now ^ 1) * 2 * TILE);
+        if (j0 + DQ_STEP < end) load(j0 + DQ_STEP, lds + (now ^ 1) * 2 * TILE);
 #pragma unroll
         for (int kb = 0; kb < 2; kb++) {
             const int32_t j = j0 + kb * 32;
@@ -165,27 +162,30 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     leave<ND, WIDE>(to, dq, a.scale, a.d);
     // a key that is not finite makes the values of dq not finite that it has so; the others are by way of lse
     if (cleansed)
-        for (int32_t j = fewest / BACK_STEP * BACK_STEP; j < row.limit; j++)
+        for (int32_t j = fewest / DQ_STEP * DQ_STEP; j < row.limit; j++)
             for (int i = 0; i < 16 * ND; i++) {
                 const int x = i / 4 * 8 + half * 4 + i % 4;
-                if (x < a.d && !finite(float(k0[j * a.k.row + x]))) to[x] = T(NAN);
+                if (x < a.d && !finite(float(kv.any_key(j)[x]))) to[x] = T(NAN);
             }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// dk and dv: 128 keys, 32 to each wavefront, which go through the queries that see them in tiles of 64, head by head of those that share the
-// keys.  Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
+// dk and dv: 64 keys to a workgroup, which go through the queries that see them in tiles of 64, head by head of those that share the keys: each wavefront
+// has 32 of the keys and takes 32 of the queries, and what two have of the same keys is added up in the end.  (With 128 keys, 32 to a
+// wavefront and all queries, there are half as many workgroups and the first keys' are twice as long: 5 sequences up to 2801, 20 heads of 128 557 us.)
+// Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) void k_attend_dkv(Back<T> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = BACK_STEP * D * 2, STAGE = 2 * TILE + 512, LANES = D / 8, EACH = 64 / LANES, LOADS = BACK_STEP / EACH / 4;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = DKV_STEP * D * 2, STAGE = 2 * TILE + 512, LOADS = TILE / 4096;
+    typedef Bring<T, D, WIDE, false> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 2 * STAGE);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, rb = wave >> 1;
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
-    if (!tile_of(a.k_offset, a.sequences, a.k_rows, 1, BACK_SHIFT, blockIdx.x / a.kv_heads, at)) return;
+    if (!tile_of(a.k_offset, a.sequences, a.k_rows, 1, DKV_SHIFT, blockIdx.x / a.kv_heads, at)) return;
     const Span mine = span_of(a.q_offset, at.s, a.rows);
-    const int32_t m = mine.count, n = at.rows.count, first = int32_t(at.first) + wave * 32, key = first + (lane & 31);
+    const int32_t m = mine.count, n = at.rows.count, first = int32_t(at.first) + (wave & 1) * 32, key = first + (lane & 31);
     const bool there = key < n;
     const int64_t token = at.rows.first + min(key, n - 1);
     vec<T, 8> k[2 * ND], v[2 * ND];
@@ -194,22 +194,19 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
     const float c = a.scale * LOG2_E;
     // query i sees key j where j <= i + ahead
     const int32_t ahead = a.causal ? n - m : n;         // sums of two are below 2^31
-    const int32_t whole = max(0, int32_t(at.first) + BACK_ROWS - 1 - ahead);      // the first query that sees all of the workgroup's keys
+    const int32_t whole = max(0, int32_t(at.first) + DKV_KEYS - 1 - ahead);      // the first query that sees all of the workgroup's keys
     if (threadIdx.x == 0) cleansed = 0;
-    const int32_t start = max(0, int32_t(at.first) - ahead) / BACK_STEP * BACK_STEP, steps = m > start ? (m - start + BACK_STEP - 1) / BACK_STEP : 0;
+    const int32_t start = max(0, int32_t(at.first) - ahead) / DKV_STEP * DKV_STEP, steps = m > start ? (m - start + DKV_STEP - 1) / DKV_STEP : 0;
 
-    const int r0 = wave * EACH + lane / LANES, chunk = int(chunk_at<D, false>(r0, lane % LANES)) * 8;
-    auto bring = [&](int32_t step, uint8_t* to) {
-        const int h = hk * a.shared + step / steps;
-        const int32_t i0 = start + step % steps * BACK_STEP;
-        const T *const q0 = a.q.p + mine.first * a.q.row + h * a.q.head, *const o0 = a.dout.p + mine.first * a.dout.row + h * a.dout.head;
+    // the queries of a head, and their dout, as rows side by side
+    auto of = [&](int h) {
+        return typename Packed<T>::One{same(a.q.p + mine.first * a.q.row + h * a.q.head), same(a.dout.p + mine.first * a.dout.row + h * a.dout.head), a.q.row, a.dout.row, __builtin_amdgcn_readfirstlane(m)};
+    };
+    const B bring(of(hk * a.shared), wave * B::EACH + lane / B::LANES, a.d);
+    auto load = [&](int h, int32_t i0, uint8_t* to) {
+        const auto rows = of(h);
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const int32_t r = i0 + r0 + i * 4 * EACH;
-            const int have = r < m ? a.d - chunk : 0;
-            chunk_to_lds<WIDE>(q0 + r * a.q.row + chunk, have, to + (i * 4 + wave) * 1024);
-            chunk_to_lds<WIDE>(o0 + r * a.dout.row + chunk, have, to + TILE + (i * 4 + wave) * 1024);
-        }
+        for (int i = 0; i < LOADS; i++) bring(rows, i0 + (i * 4 + wave) * B::EACH, 0, a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
         if (wave < 2) {
             const float* const from = (wave ? a.delta : a.base) + int64_t(h) * a.rows + mine.first + i0 + lane;
             word_to_lds(i0 + lane < m ? static_cast<const void*>(from) : &ZEROS, to + 2 * TILE + wave * 256);
@@ -218,66 +215,83 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
     const uint32_t lds0 = lds_address(lds);
     const Read<ND> read;
     f32x16 dk[ND] = {}, dv[ND] = {};
+    // the step that is loaded next
+    int h = hk * a.shared;
+    int32_t i1 = start;
     const int32_t total = steps * a.shared;
-    if (total > 0) bring(0, lds);
+    auto load_next = [&](uint8_t* to) {
+        load(h, i1, to);
+        if ((i1 += DKV_STEP) >= m) i1 = start, h++;
+    };
+    if (total > 0) load_next(lds);
     int now = 0;
     int32_t i0 = start;
-    for (int32_t step = 0; step < total; step++, now ^= 1, i0 = i0 + BACK_STEP < m ? i0 + BACK_STEP : start) {
+    for (int32_t step = 0; step < total; step++, now ^= 1, i0 = i0 + DKV_STEP < m ? i0 + DKV_STEP : start) {
         landed<0>();
         if (i0 < whole && i0 + ahead < n - 1) {             // some query does not see some key
             if (cleanse<T>(lds + now * STAGE, 2 * TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
-        if (step + 1 < total) bring(step + 1, lds + (now ^ 1) * STAGE);
+        if (step + 1 < total) load_next(lds + (now ^ 1) * STAGE);
+        const int32_t i = i0 + rb * 32;
+        if (i >= m || i + 31 + ahead < first) continue;         // no query, or none that sees one of these keys
+        const uint32_t tile = lds0 + now * STAGE + rb * 32 * D * 2, words = lds0 + now * STAGE + 2 * TILE + rb * 128 + half * 16;
+        f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int rb = 0; rb < 2; rb++) {
-            const int32_t i = i0 + rb * 32;
-            if (i >= m || i + 31 + ahead < first) continue;         // no query, or none that sees one of these keys
-            const uint32_t tile = lds0 + now * STAGE + rb * 32 * D * 2, words = lds0 + now * STAGE + 2 * TILE + rb * 128 + half * 16;
-            f32x16 s = {}, dp = {};
+        for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), k[kk], s);
 #pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), k[kk], s);
+        for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), v[kk], dp);
+        const bool some = i + ahead < first + 31 || i + 32 > m;         // some query does not see some key; or there is none
+        vec<T, 8> p[2], ds[2];
 #pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), v[kk], dp);
-            const bool some = i + ahead < first + 31 || i + 32 > m;         // some query does not see some key; or there is none
-            vec<T, 8> p[2], ds[2];
+        for (int e = 0; e < 4; e++) {
+            const f32x4 base = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + e * 32), delta = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + 256 + e * 32);
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const f32x4 base = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + e * 32), delta = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + 256 + e * 32);
-#pragma unroll
-                for (int u = 0; u < 4; u++) {
-                    const int w = e * 4 + u;
-                    s[w] = power(fmaf(s[w], c, -base[u])), dp[w] = s[w] * (dp[w] - delta[u]);
-                }
+            for (int u = 0; u < 4; u++) {
+                const int w = e * 4 + u;
+                s[w] = power(fmaf(s[w], c, -base[u])), dp[w] = s[w] * (dp[w] - delta[u]);
             }
-            if (some) {
-#pragma unroll
-                for (int w = 0; w < 16; w++) {
-                    const int32_t r = i + 8 * (w / 4) + 4 * half + w % 4, unseen = (m - 1 - r) | (r + ahead - key);
-                    s[w] = or_zero(s[w], unseen), dp[w] = or_zero(dp[w], unseen);
-                }
-            }
-#pragma unroll
-            for (int w = 0; w < 16; w++) p[w / 8][w % 8] = T(s[w]), ds[w / 8][w % 8] = T(dp[w]);
-#pragma unroll
-            for (int x = 0; x < 2; x++)
-#pragma unroll
-                for (int dt = 0; dt < ND; dt++) {
-                    dv[dt] = product32(turned32<D, T>(tile + TILE + read.turned[dt] + x * 16 * D * 2), p[x], dv[dt]);
-                    dk[dt] = product32(turned32<D, T>(tile + read.turned[dt] + x * 16 * D * 2), ds[x], dk[dt]);
-                }
         }
+        if (some) {
+#pragma unroll
+            for (int w = 0; w < 16; w++) {
+                const int32_t r = i + 8 * (w / 4) + 4 * half + w % 4, unseen = (m - 1 - r) | (r + ahead - key);
+                s[w] = or_zero(s[w], unseen), dp[w] = or_zero(dp[w], unseen);
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 16; w++) p[w / 8][w % 8] = T(s[w]), ds[w / 8][w % 8] = T(dp[w]);
+#pragma unroll
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++) {
+                dv[dt] = product32(turned32<D, T>(tile + TILE + read.turned[dt] + x * 16 * D * 2), p[x], dv[dt]);
+                dk[dt] = product32(turned32<D, T>(tile + read.turned[dt] + x * 16 * D * 2), ds[x], dk[dt]);
+            }
     }
     own_landed<0>();
     __syncthreads();
-    if (!there) return;
+    // two wavefronts' sums by way of LDS
+    float* const sums = reinterpret_cast<float*>(lds) + (wave & 1) * (ND * 2048) + lane;
+    if (rb == 1) {
+#pragma unroll
+        for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) sums[(dt * 16 + i) * 64] = dk[dt][i], sums[(dt * 16 + i) * 64 + ND * 1024] = dv[dt][i];
+    }
+    __syncthreads();
+    if (rb == 1 || !there) return;
+#pragma unroll
+    for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) dk[dt][i] += sums[(dt * 16 + i) * 64], dv[dt][i] += sums[(dt * 16 + i) * 64 + ND * 1024];
     T *const to_k = a.dk.p + token * a.dk.row + hk * a.dk.head, *const to_v = a.dv.p + token * a.dv.row + hk * a.dv.head;
     leave<ND, WIDE>(to_k, dk, a.scale, a.d);
     leave<ND, WIDE>(to_v, dv, 1.f, a.d);
     if (!cleansed) return;
     // a query that is not finite makes all of dk and dv so of the keys that it sees, a dout that is not all of dk, and the values of dv that it has so
     for (int g = 0; g < a.shared; g++)
-        for (int32_t i = max(start, key - ahead); i < min(m, start + (whole - start + BACK_STEP - 1) / BACK_STEP * BACK_STEP); i++) {
+        for (int32_t i = max(start, key - ahead); i < min(m, start + (whole - start + DKV_STEP - 1) / DKV_STEP * DKV_STEP); i++) {
             const T *const q = a.q.p + (mine.first + i) * a.q.row + (hk * a.shared + g) * a.q.head, *const o = a.dout.p + (mine.first + i) * a.dout.row + (hk * a.shared + g) * a.dout.head;
             bool bad_q = false, bad_o = false;
             for (int x = 0; x < a.d; x++) bad_q = bad_q || !finite(float(q[x])), bad_o = bad_o || !finite(float(o[x]));
@@ -309,7 +323,7 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
     if (sequences == 0 || heads == 0 || d == 0 || (rows == 0 && k_rows == 0)) return CSR5_OK;
     if (!q_offset || !k_offset || (rows > 0 && !lse)) return CSR5_EINVAL;
     if (rows > 0 && (!workspace || workspace_bytes < csr5_attention_backward_workspace_bytes(rows, heads))) return CSR5_ENOMEM;
-    const int64_t q_tiles = tiles_at_most(sequences, rows, heads / kv_heads, BACK_SHIFT), k_tiles = tiles_at_most(sequences, k_rows, 1, BACK_SHIFT);
+    const int64_t q_tiles = tiles_at_most(sequences, rows, heads / kv_heads, DQ_SHIFT), k_tiles = tiles_at_most(sequences, k_rows, 1, DKV_SHIFT);
     if (q_tiles * kv_heads * 256 > UINT32_MAX || k_tiles * kv_heads * 256 > UINT32_MAX) return CSR5_ERANGE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const bool w = d % 8 == 0 && wide(q, 2) && wide(k, 2) && wide(v, 2) && wide(out, 2) && wide(dout, 2) && wide(dq, 2) && wide(dk, 2) && wide(dv, 2);
@@ -323,9 +337,9 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
             constexpr bool WIDE = decltype(is_wide)::value;
             if (rows > 0) {
                 k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
-                k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2 + 16, s>>>(a);
+                k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * DQ_STEP * D * 2 + 16, s>>>(a);
             }
-            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * BACK_STEP * D * 2 + 1024 + 16, s>>>(a);
+            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * DKV_STEP * D * 2 + 1024 + 16, s>>>(a);
         };
         auto by = [&](auto nd) {
             if (w) go(nd, std::true_type());

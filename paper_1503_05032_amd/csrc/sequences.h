@@ -188,6 +188,32 @@ template <bool WIDE, typename T> __device__ __forceinline__ void chunk_to_lds(co
     else *reinterpret_cast<vec<T, 8>*>(to + (threadIdx.x & 63) * 16) = eight_values<false>(from, from ? have : 0);
 }
 
+// What this lane asks for of the rows of a load: they lie side by side from one address on, or each is looked for.
+template <typename T, int D, bool WIDE, bool SMALL> struct Bring {
+    static constexpr int LANES = D / 8, EACH = 64 / LANES;      // lanes of a row, rows of a load
+    int row, chunk;             // this lane's, in a load
+    uint32_t k_off, v_off;      // in bytes, from the load's first row
+    bool near;                  // every lane's chunk is in the row, and no offset passes 32 bits
+    // first: the row of a tile that this lane has in its first load (in others a multiple of 16 further)
+    template <typename One> __device__ __forceinline__ Bring(const One& kv, int first, int d) {
+        row = (threadIdx.x & 63) / LANES, chunk = int(chunk_at<D, SMALL>(first, threadIdx.x % LANES)) * 8;
+        // where d ends within a chunk that is read, or beside it, there are zeros to be had; a chunk that is not read may be another one
+        near = WIDE && (d == D || (D == 128 && d == 96)) && (EACH * kv.k_row | EACH * kv.v_row) < (1 << 28);
+        const int c = chunk < d ? chunk : 0;
+        k_off = uint32_t(row * kv.k_row + c) * 2, v_off = uint32_t(row * kv.v_row + c) * 2;
+    }
+    // rows j (a multiple of EACH, the same in every lane) on, to k and v
+    template <typename One> __device__ __forceinline__ void operator()(const One& kv, int32_t j, typename One::Ahead ahead, int d, uint8_t* k, uint8_t* v) const {
+        if (near && j + EACH <= kv.count && kv.template together<EACH>(ahead)) {
+            to_lds(kv.key(j, ahead), k_off, k), to_lds(kv.value(j, ahead), v_off, v);
+        } else {
+            const bool there = j + row < kv.count;
+            const T *const from = there ? kv.any_key(j + row) : nullptr, *const of = there ? kv.any_value(j + row) : nullptr;
+            chunk_to_lds<WIDE>(from ? from + chunk : from, d - chunk, k), chunk_to_lds<WIDE>(of ? of + chunk : of, d - chunk, v);
+        }
+    }
+};
+
 // x, and 0 (-inf) where `hidden` is negative
 __device__ __forceinline__ float or_zero(float x, int32_t hidden) { return __uint_as_float(__float_as_uint(x) & ~uint32_t(hidden >> 31)); }
 __device__ __forceinline__ float or_none(float x, int32_t hidden) {
