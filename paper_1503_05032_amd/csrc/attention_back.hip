@@ -48,17 +48,18 @@ template <typename T, int LANES, bool WIDE> __global__ __launch_bounds__(256) vo
     if (there && c == 0) a.delta[h * a.rows + row] = sum, a.base[h * a.rows + row] = a.lse[h * a.rows + row] * LOG2_E;
 }
 
-// Where a wavefront reads tiles of 64 rows of LDS for products of 32 x 32 x 16: rows as first operands, and turned.
+// Where a wavefront reads rows of LDS for products of 32 x 32 x 16: rows as first operands (chunks 2 kk on), and turned (columns 32 dt on).  Tiles begin at
+// multiples of 256 bytes, so other chunks are other patterns in bits 5 to 7: one register for all of them.
 template <int ND> struct Read {
     static constexpr int D = ND <= 2 ? 64 : 128;
-    uint32_t row[2 * ND], turned[ND];
+    uint32_t row_, turned_;
     __device__ __forceinline__ Read() {
         const int lane = threadIdx.x & 63, half = lane >> 5, li = lane & 15, r = half * 4 + (li >> 2);
-#pragma unroll
-        for (int kk = 0; kk < 2 * ND; kk++) row[kk] = (lane & 31) * D * 2 + chunk_at<D, false>(lane & 31, 2 * kk + half) * 16;
-#pragma unroll
-        for (int dt = 0; dt < ND; dt++) turned[dt] = r * D * 2 + chunk_at<D, false>(r, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+        row_ = (lane & 31) * D * 2 + chunk_at<D, false>(lane & 31, half) * 16;
+        turned_ = r * D * 2 + chunk_at<D, false>(r, ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
     }
+    __device__ __forceinline__ uint32_t row(uint32_t tile, int kk) const { return (tile + row_) ^ (kk * 32); }
+    __device__ __forceinline__ uint32_t turned(uint32_t tile, int dt) const { return (tile + turned_) ^ (dt * 64); }
 };
 
 // A head's values of this lane's column, for second operands.
@@ -134,9 +135,9 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
             const uint32_t tile = lds0 + now * 2 * TILE + kb * 32 * D * 2;
             f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), q[kk], s);
+            for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(read.row(tile, kk)), q[kk], s);
 #pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), dout[kk], dp);
+            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(read.row(tile + TILE, kk)), dout[kk], dp);
             const bool some = j + 32 > least;       // some row does not see some key
             vec<T, 8> ds[2];
 #pragma unroll
@@ -152,7 +153,7 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
 #pragma unroll
             for (int k = 0; k < 2; k++)
 #pragma unroll
-                for (int dt = 0; dt < ND; dt++) dq[dt] = product32(turned32<D, T>(tile + read.turned[dt] + k * 16 * D * 2), ds[k], dq[dt]);
+                for (int dt = 0; dt < ND; dt++) dq[dt] = product32(turned32<D, T>(read.turned(tile + k * 16 * D * 2, dt)), ds[k], dq[dt]);
         }
     }
     own_landed<0>();
@@ -175,8 +176,8 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
 // wavefront and all queries, there are half as many workgroups and the first keys' are twice as long: 5 sequences up to 2801, 20 heads of 128 557 us.)
 // Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
 // ---------------------------------------------------------------------------------------------------------------
-template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) void k_attend_dkv(Back<T> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = DKV_STEP * D * 2, STAGE = 2 * TILE + 512, LOADS = TILE / 4096;
+template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dkv(Back<T> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = DKV_STEP * D * 2, STAGE = 2 * TILE + DKV_STEP * 8, LOADS = TILE / 4096;
     typedef Bring<T, D, WIDE, false> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 2 * STAGE);
@@ -207,10 +208,8 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
         const auto rows = of(h);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) bring(rows, i0 + (i * 4 + wave) * B::EACH, 0, a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
-        if (wave < 2) {
-            const float* const from = (wave ? a.delta : a.base) + int64_t(h) * a.rows + mine.first + i0 + lane;
-            word_to_lds(i0 + lane < m ? static_cast<const void*>(from) : &ZEROS, to + 2 * TILE + wave * 256);
-        }
+        const int32_t i = i0 + lane;
+        if (wave < 2) word_to_lds(i < m ? static_cast<const void*>((wave ? a.delta : a.base) + int64_t(h) * a.rows + mine.first + i) : &ZEROS, to + 2 * TILE + wave * 256);
     };
     const uint32_t lds0 = lds_address(lds);
     const Read<ND> read;
@@ -234,25 +233,26 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
         }
         if (step + 1 < total) load_next(lds + (now ^ 1) * STAGE);
         const int32_t i = i0 + rb * 32;
-        if (i >= m || i + 31 + ahead < first) continue;         // no query, or none that sees one of these keys
+        if (i >= m || i + 31 + ahead < first) continue;     // no query, or none that sees one of these keys
         const uint32_t tile = lds0 + now * STAGE + rb * 32 * D * 2, words = lds0 + now * STAGE + 2 * TILE + rb * 128 + half * 16;
         f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + read.row[kk]), k[kk], s);
+        for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(read.row(tile, kk)), k[kk], s);
 #pragma unroll
-        for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(tile + TILE + read.row[kk]), v[kk], dp);
-        const bool some = i + ahead < first + 31 || i + 32 > m;         // some query does not see some key; or there is none
+        for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(read.row(tile + TILE, kk)), v[kk], dp);
+        // all 256 registers are in use: without these borders, loads that are moved up put 45 of them into memory
+        __builtin_amdgcn_sched_barrier(0);
         vec<T, 8> p[2], ds[2];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            const f32x4 base = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + e * 32), delta = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + 256 + e * 32);
+            const f32x4 base = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + e * 32), delta = *(const __attribute__((address_space(3))) f32x4*)uintptr_t(words + DKV_STEP * 4 + e * 32);
 #pragma unroll
             for (int u = 0; u < 4; u++) {
                 const int w = e * 4 + u;
                 s[w] = power(fmaf(s[w], c, -base[u])), dp[w] = s[w] * (dp[w] - delta[u]);
             }
         }
-        if (some) {
+        if (i + ahead < first + 31 || i + 32 > m) {         // some query does not see some key; or there is none
 #pragma unroll
             for (int w = 0; w < 16; w++) {
                 const int32_t r = i + 8 * (w / 4) + 4 * half + w % 4, unseen = (m - 1 - r) | (r + ahead - key);
@@ -261,12 +261,13 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 1) vo
         }
 #pragma unroll
         for (int w = 0; w < 16; w++) p[w / 8][w % 8] = T(s[w]), ds[w / 8][w % 8] = T(dp[w]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int x = 0; x < 2; x++)
 #pragma unroll
             for (int dt = 0; dt < ND; dt++) {
-                dv[dt] = product32(turned32<D, T>(tile + TILE + read.turned[dt] + x * 16 * D * 2), p[x], dv[dt]);
-                dk[dt] = product32(turned32<D, T>(tile + read.turned[dt] + x * 16 * D * 2), ds[x], dk[dt]);
+                dv[dt] = product32(turned32<D, T>(read.turned(tile + TILE + x * 16 * D * 2, dt)), p[x], dv[dt]);
+                dk[dt] = product32(turned32<D, T>(read.turned(tile + x * 16 * D * 2, dt)), ds[x], dk[dt]);
             }
     }
     own_landed<0>();
@@ -339,7 +340,7 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
                 k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
                 k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * DQ_STEP * D * 2 + 16, s>>>(a);
             }
-            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * DKV_STEP * D * 2 + 1024 + 16, s>>>(a);
+            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * DKV_STEP * D * 2 + 16 * DKV_STEP + 16, s>>>(a);
         };
         auto by = [&](auto nd) {
             if (w) go(nd, std::true_type());
