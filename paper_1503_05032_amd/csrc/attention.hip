@@ -223,12 +223,12 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 
 // ---------------------------------------------------------------------------------------------------------------
 // Few rows: 16 RB folded rows, and the keys dealt to four wavefronts in tiles of 32, each with LDS of its own and no barrier; what they
-// have of the rows is joined at the end.  Bound by the keys' and values' way from memory: 16 KB (8 where d <= 64) of each wavefront are always
-// on their way.  Products are keys x rows as above, of 16 x 16 x 32.
+// have of the rows is joined at the end.  Bound by the keys' and values' way from memory: 16 KB (8 where d <= 64) of each wavefront, eight of them on a
+// CU, are on their way but for the moment in which it reads what has come into registers.  Products are keys x rows as above, of 16 x 16 x 32.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int FEW_KEYS = 32;
 
-template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launch_bounds__(256, 1) void k_attend_few(Attend<T, KV> a) {
+template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launch_bounds__(256, RB <= 2 ? 2 : 1) void k_attend_few(Attend<T, KV> a) {
     constexpr int D = ND <= 2 ? 64 : 128, TILE = FEW_KEYS * D * 2, LOADS = TILE / 1024, ROWS = 16 * RB;
     typedef Bring<T, D, WIDE, true> B;
     constexpr int SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
@@ -254,7 +254,7 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
 #pragma unroll
         for (int kk = 0; kk < ND; kk++) q[b][kk] = eight_values<WIDE>(from + (4 * kk + quarter) * 8, row[b].there ? a.d - (4 * kk + quarter) * 8 : 0);
     }
-    uint8_t* const mine = lds + wave * 4 * TILE;
+    uint8_t* const mine = lds + wave * 2 * TILE;
     // rows 8 and more apart have other swizzles: two loads in turn
     const B even(kv, lane / B::LANES, a.d), odd(kv, 8 + lane / B::LANES, a.d), next(kv, 4 + lane / B::LANES, a.d), last(kv, 12 + lane / B::LANES, a.d);
     typename decltype(kv)::Ahead ahead[LOADS];
@@ -289,29 +289,34 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
         load(start, mine);
         look(start + 4 * FEW_KEYS);
     }
-    int now = 0;
     bool found = false;
-    for (int32_t j0 = start; j0 < end; j0 += 4 * FEW_KEYS, now ^= 1) {
+    for (int32_t j0 = start; j0 < end; j0 += 4 * FEW_KEYS) {
         own_landed<0>();
+        const bool some = j0 + FEW_KEYS > least;
+        if (some && least < n) {
+            found = __any(cleanse<T>(mine + TILE, TILE, lane, 64)) || found;
+            wave_order();
+        }
+        // everything of the tile into registers, and the next one on its way before this one's products
+        vec<T, 8> k[2][ND], v[2 * ND];
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int kk = 0; kk < ND; kk++) k[kb][kk] = chunk_from<T>(lds0 + k_at[kk] + kb * 16 * D * 2);
+#pragma unroll
+        for (int dt = 0; dt < 2 * ND; dt++) v[dt] = turned_from<T>(lds0 + v_at[dt], lds0 + v_at[dt] + 16 * D * 2);
         if (j0 + 4 * FEW_KEYS < end) {
-            load(j0 + 4 * FEW_KEYS, mine + (now ^ 1) * 2 * TILE);
+            own_read();
+            load(j0 + 4 * FEW_KEYS, mine);
             look(j0 + 8 * FEW_KEYS);
         }
-        const uint32_t tile = lds0 + now * 2 * TILE;
         f32x4 s[RB][2] = {};
 #pragma unroll
         for (int kb = 0; kb < 2; kb++)
 #pragma unroll
-            for (int kk = 0; kk < ND; kk++) {
-                const vec<T, 8> k = chunk_from<T>(tile + k_at[kk] + kb * 16 * D * 2);
+            for (int kk = 0; kk < ND; kk++)
 #pragma unroll
-                for (int b = 0; b < RB; b++) s[b][kb] = product16(k, q[b][kk], s[b][kb]);
-            }
-        const bool some = j0 + FEW_KEYS > least;
-        if (some && least < n) {
-            found = __any(cleanse<T>(mine + now * 2 * TILE + TILE, TILE, lane, 64)) || found;
-            wave_order();
-        }
+                for (int b = 0; b < RB; b++) s[b][kb] = product16(k[kb][kk], q[b][kk], s[b][kb]);
         vec<T, 8> p[RB];
 #pragma unroll
         for (int b = 0; b < RB; b++) {
@@ -340,11 +345,9 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
             }
         }
 #pragma unroll
-        for (int dt = 0; dt < 2 * ND; dt++) {
-            const vec<T, 8> v = turned_from<T>(tile + v_at[dt], tile + v_at[dt] + 16 * D * 2);
+        for (int dt = 0; dt < 2 * ND; dt++)
 #pragma unroll
-            for (int b = 0; b < RB; b++) o[b][dt] = product16(v, p[b], o[b][dt]);
-        }
+            for (int b = 0; b < RB; b++) o[b][dt] = product16(v[dt], p[b], o[b][dt]);
     }
     // Joined by way of LDS: [wave][row][d], and their bases and totals.
     own_landed<0>();
@@ -394,35 +397,39 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
 template <typename T, typename KV> __global__ __launch_bounds__(256) void k_join(Attend<T, KV> a) {
     const int64_t at = workgroup() * 4 + (threadIdx.x >> 6);
     if (at >= int64_t(a.rows) * a.heads) return;
-    const int32_t row = int32_t(at / a.heads), h = int32_t(at % a.heads), lane = threadIdx.x & 63;
-    TileOf t;
-    // with tiles of one row, tile row + s is row `row` of sequence s: the sequence is found as the last that begins at or before the row
-    int32_t low = 0, high = a.sequences;
-    while (high - low > 1) {
-        const int32_t mid = low + (high - low) / 2;
-        if (begin_of(a.q_offset, mid, a.rows) <= row) low = mid;
-        else high = mid;
-    }
-    t.rows = span_of(a.q_offset, low, a.rows);
-    if (row < t.rows.first || row >= t.rows.first + t.rows.count) return;
-    const auto kv = a.kv.one(low, 0);
-    const int32_t limit = seen(a.causal, row - t.rows.first, t.rows.count, kv.count), parts = (limit + a.chunk - 1) / a.chunk;
+    const int32_t row = __builtin_amdgcn_readfirstlane(int32_t(at / a.heads)), h = __builtin_amdgcn_readfirstlane(int32_t(at % a.heads)), lane = threadIdx.x & 63;
+    Span rows;
+    const int32_t s = last_of(a.q_offset, a.sequences, a.rows, rows, [&](int32_t begin, int32_t) { return begin <= row; });
+    if (s < 0 || row >= rows.first + rows.count) return;
+    const auto kv = a.kv.one(s, 0);
+    const int32_t limit = seen(a.causal, row - rows.first, rows.count, kv.count), parts = (limit + a.chunk - 1) / a.chunk;
     const int64_t step = int64_t(a.rows) * a.heads;
     const float* const stats = a.stats + at * 2;
     const float* const part = a.part + at * a.d;
     const float c = a.scale * LOG2_E;
     float top = -INFINITY, total = 0.f, v[2] = {0.f, 0.f};
-    for (int32_t i = lane; i < parts; i += 64) top = fmaxf(top, stats[i * step * 2]);
+    // 64 parts at a time: their bases and totals by the lanes, what they count by then one after the other
+    for (int32_t i0 = 0; i0 < parts; i0 += 64) {
+        const int32_t have = min(parts - i0, 64);
+        const float base = lane < have ? stats[(i0 + lane) * step * 2] : -INFINITY, sum = lane < have ? stats[(i0 + lane) * step * 2 + 1] : 0.f;
+        float higher = fmaxf(top, base);
 #pragma unroll
-    for (int e = 1; e < 64; e *= 2) top = fmaxf(top, __shfl_xor(top, e));
-    for (int32_t i = 0; i < parts; i++) {
-        const float base = stats[i * step * 2], sum = stats[i * step * 2 + 1];
-        if (base == -INFINITY && sum == 0.f) continue;
-        const float less = base == -INFINITY ? 0.f : power((base - top) * c);
-        total += sum * less;
+        for (int e = 1; e < 64; e *= 2) higher = fmaxf(higher, __shfl_xor(higher, e));
+        const float less = top == higher ? 1.f : power((top - higher) * c), weight = lane >= have ? 0.f : base == higher ? 1.f : power((base - higher) * c);
+        top = higher, total = total * less + wave_sum(sum * weight), v[0] *= less, v[1] *= less;
+        for (int32_t i = 0; i < have; i += 8) {
+            float from[8][2];
 #pragma unroll
-        for (int e = 0; e < 2; e++)
-            if (lane + e * 64 < a.d) v[e] += part[i * step * a.d + lane + e * 64] * less;
+            for (int u = 0; u < 8; u++)
+#pragma unroll
+                for (int e = 0; e < 2; e++) from[u][e] = lane + e * 64 < a.d ? part[(i0 + min(i + u, have - 1)) * step * a.d + lane + e * 64] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 8; u++) {
+                const float w = i + u < have ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), i + u)) : 0.f;
+#pragma unroll
+                for (int e = 0; e < 2; e++) v[e] = fmaf(from[u][e], w, v[e]);
+            }
+        }
     }
     const float inverse = total == 0.f ? 0.f : 1.f / total;
     T* const out = a.out.p + row * a.out.row + h * a.out.head;
@@ -462,7 +469,7 @@ template <typename T, typename KV> int attend(Attend<T, KV> a, const Plan& p, bo
         constexpr int ND = decltype(nd)::value, TILE = (ND <= 2 ? 64 : 128) * 2;
         constexpr bool WIDE = decltype(w)::value;
         auto few = [&](auto rb) {
-            constexpr int RB = decltype(rb)::value, ring = 16 * FEW_KEYS * TILE, join = 4 * 16 * RB * (ND * 32 + 4) * 4;
+            constexpr int RB = decltype(rb)::value, ring = 8 * FEW_KEYS * TILE, join = 4 * 16 * RB * (ND * 32 + 4) * 4;
             k_attend_few<T, KV, ND, WIDE, RB><<<grid, 256, ring > join ? ring : join, s>>>(a);
         };
         if (p.blocks == 1) few(std::integral_constant<int, 1>());

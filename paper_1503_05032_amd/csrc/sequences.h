@@ -43,21 +43,29 @@ struct TileOf {
     Span rows;
     int64_t first;          // of rows.count * times
 };
-__device__ __forceinline__ bool tile_of(const int32_t* offset, int32_t sequences, int32_t rows, int64_t times, int shift, int64_t t, TileOf& out) {
+// The last of the sequences for which f(its first row, its number) holds, where it holds for those before too, and its rows; -1: none.
+template <typename F> __device__ __forceinline__ int32_t last_of(const int32_t* offset, int32_t sequences, int32_t rows, Span& span, F f) {
     const int lane = threadIdx.x & 63;
     int32_t low = 0, count = sequences;
     for (;;) {
         const int32_t step = (count + 63) / 64;
         const int64_t i = int64_t(low) + int64_t(lane) * step;
-        const bool before = int64_t(lane) * step < count && (int64_t(begin_of(offset, int32_t(i), rows)) * times >> shift) + i <= t;
-        const uint64_t votes = __ballot(before);
-        if (!votes) return false;
+        const int32_t begin = i <= sequences ? begin_of(offset, int32_t(i), rows) : rows;
+        const uint64_t votes = __ballot(int64_t(lane) * step < count && f(begin, int32_t(i)));
+        if (!votes) return -1;
         const int last = 63 - __builtin_clzll(votes);
+        if (step == 1) {
+            const int32_t s = low + last, first = __builtin_amdgcn_readlane(begin, last);
+            const int32_t end = last < 63 ? __builtin_amdgcn_readlane(begin, last + 1) : begin_of(offset, s + 1, rows);
+            span = {first, max(end - first, 0)};
+            return __builtin_amdgcn_readfirstlane(s);
+        }
         low += last * step, count = min(step, count - last * step);
-        if (step == 1) break;
     }
-    out.s = __builtin_amdgcn_readfirstlane(low);
-    out.rows = span_of(offset, out.s, rows);
+}
+__device__ __forceinline__ bool tile_of(const int32_t* offset, int32_t sequences, int32_t rows, int64_t times, int shift, int64_t t, TileOf& out) {
+    out.s = last_of(offset, sequences, rows, out.rows, [&](int32_t begin, int32_t i) { return (int64_t(begin) * times >> shift) + i <= t; });
+    if (out.s < 0) return false;
     out.first = (t - ((int64_t(out.rows.first) * times >> shift) + out.s)) << shift;
     return out.first >= 0 && out.first < int64_t(out.rows.count) * times;
 }

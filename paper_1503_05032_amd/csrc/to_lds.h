@@ -54,6 +54,11 @@ template <int LATER> __device__ __forceinline__ void own_landed() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
 }
 
+// This wavefront's reads of LDS have returned: it may be loaded anew.
+__device__ __forceinline__ void own_read() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
 }  // namespace
 
 #endif
