@@ -103,8 +103,8 @@ template <int ND, typename T, typename KV, typename One> __device__ __forceinlin
 }
 
 template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 3) void k_attend_many(Attend<T, KV> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2, LOADS = TILE / 4096;
-    typedef Bring<T, D, WIDE, false> B;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2;
+    typedef Bring<T, D, WIDE, false, MANY_KEYS, 4> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -129,48 +129,31 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 #pragma unroll
         for (int kk = 0; kk < 2 * ND; kk++) q[kk] = eight_values<WIDE>(from + (2 * kk + half) * 8, row.there ? a.d - (2 * kk + half) * 8 : 0);
     }
-    const B bring(kv, wave * B::EACH + lane / B::LANES, a.d);
-    typename decltype(kv)::Ahead ahead[LOADS];
-    auto look = [&](int32_t j0) {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + (i * 4 + wave) * B::EACH);
-    };
-    auto load = [&](int32_t j0, uint8_t* to) {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) bring(kv, j0 + (i * 4 + wave) * B::EACH, ahead[i], a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
-    };
+    // LDS: two tiles of keys, then two of values
     const uint32_t lds0 = lds_address(lds);
-    // where this lane reads keys (rows lane % 32) and values (rows 4 * half on, columns)
-    const int li = lane & 15, vr = half * 4 + (li >> 2);
-    uint32_t k_at[2 * ND], v_at[ND];
-#pragma unroll
-    for (int kk = 0; kk < 2 * ND; kk++) k_at[kk] = (lane & 31) * D * 2 + chunk_at<D, false>(lane & 31, 2 * kk + half) * 16;
-#pragma unroll
-    for (int dt = 0; dt < ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, false>(vr, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+    const B bring(kv, wave, a.d);
+    typename decltype(kv)::Ahead ahead[B::LOADS];
+    const ReadFixed<ND> read(lds0);
 
     const float c = a.scale * LOG2_E, rise = RISE / c;
     float base = -INFINITY, sum = 0.f;
     f32x16 o[ND] = {};
-    look(begin);
-    load(begin, lds);
-    look(begin + MANY_KEYS);
-    int now = 0;
-    for (int32_t j0 = begin; j0 < end; j0 += MANY_KEYS, now ^= 1) {
+    auto tile = [&](auto at_place, int32_t j0) {
+        constexpr int NOW = decltype(at_place)::value;
         landed<0>();
         if (j0 + MANY_KEYS > fewest && fewest < n) {        // some row does not see some key
-            if (cleanse<T>(lds + now * 2 * TILE + TILE, TILE, threadIdx.x, 256)) cleansed = 1;
+            if (cleanse<T>(lds + (2 + NOW) * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
         if (j0 + MANY_KEYS < end) {
-            load(j0 + MANY_KEYS, lds + (now ^ 1) * 2 * TILE);
-            look(j0 + 2 * MANY_KEYS);
+            bring(kv, j0 + MANY_KEYS, ahead, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
+            bring.look(kv, j0 + 2 * MANY_KEYS, ahead);
         }
-        if (j0 >= most) continue;
-        const uint32_t tile = lds0 + now * 2 * TILE;
+        if (j0 >= most) return;
         f32x16 s = {};
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(tile + k_at[kk]), q[kk], s);
+        for (int kk = 0; kk < 2 * ND; kk++) s = product32(read.template row<T>(NOW * TILE, kk), q[kk], s);
         if (j0 + MANY_KEYS > least) {
 #pragma unroll
             for (int i = 0; i < 16; i++) s[i] = or_none(s[i], row.limit - 1 - (j0 + 8 * (i / 4) + 4 * half + i % 4));
@@ -200,8 +183,17 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 #pragma unroll
         for (int k = 0; k < 2; k++)
 #pragma unroll
-            for (int dt = 0; dt < ND; dt++) o[dt] = product32(turned32<D, T>(tile + v_at[dt] + k * 16 * D * 2), p[k], o[dt]);
+            for (int dt = 0; dt < ND; dt++) o[dt] = product32(read.template turned<T>((2 + NOW) * TILE + k * 16 * D * 2, dt), p[k], o[dt]);
         __builtin_amdgcn_s_setprio(0);
+    };
+    if (begin < end) {
+        bring.look(kv, begin, ahead);
+        bring(kv, begin, ahead, a.d, lds0, lds0 + 2 * TILE);
+        bring.look(kv, begin + MANY_KEYS, ahead);
+    }
+    for (int32_t j0 = begin; j0 < end; j0 += 2 * MANY_KEYS) {
+        tile(std::integral_constant<int, 0>(), j0);
+        if (j0 + MANY_KEYS < end) tile(std::integral_constant<int, 1>(), j0 + MANY_KEYS);
     }
     own_landed<0>();
     __syncthreads();
@@ -229,8 +221,8 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 constexpr int FEW_KEYS = 32;
 
 template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launch_bounds__(256, RB <= 2 ? 2 : 1) void k_attend_few(Attend<T, KV> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = FEW_KEYS * D * 2, LOADS = TILE / 1024, ROWS = 16 * RB;
-    typedef Bring<T, D, WIDE, true> B;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = FEW_KEYS * D * 2, ROWS = 16 * RB;
+    typedef Bring<T, D, WIDE, true, FEW_KEYS, 1> B;
     constexpr int SHIFT = RB == 1 ? 4 : RB == 2 ? 5 : 6;
     extern __shared__ __align__(16) uint8_t lds[];
     __shared__ int32_t cleansed[4];
@@ -255,21 +247,8 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
         for (int kk = 0; kk < ND; kk++) q[b][kk] = eight_values<WIDE>(from + (4 * kk + quarter) * 8, row[b].there ? a.d - (4 * kk + quarter) * 8 : 0);
     }
     uint8_t* const mine = lds + wave * 2 * TILE;
-    // rows 8 and more apart have other swizzles: two loads in turn
-    const B even(kv, lane / B::LANES, a.d), odd(kv, 8 + lane / B::LANES, a.d), next(kv, 4 + lane / B::LANES, a.d), last(kv, 12 + lane / B::LANES, a.d);
-    typename decltype(kv)::Ahead ahead[LOADS];
-    auto look = [&](int32_t j0) {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + i * B::EACH);
-    };
-    auto load = [&](int32_t j0, uint8_t* to) {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            const int r = i * B::EACH % 16;
-            const B& bring = r == 0 ? even : r == 4 ? next : r == 8 ? odd : last;
-            bring(kv, j0 + i * B::EACH, ahead[i], a.d, to + i * 1024, to + TILE + i * 1024);
-        }
-    };
+    const B bring(kv, 0, a.d);
+    typename decltype(kv)::Ahead ahead[B::LOADS];
     const uint32_t lds0 = lds_address(mine);
     const int vr = quarter * 4 + (li >> 2);
     uint32_t k_at[ND], v_at[2 * ND];
@@ -285,9 +264,9 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
     for (int b = 0; b < RB; b++) base[b] = -INFINITY, sum[b] = 0.f;
     const int32_t start = begin + wave * FEW_KEYS;
     if (start < end) {
-        look(start);
-        load(start, mine);
-        look(start + 4 * FEW_KEYS);
+        bring.look(kv, start, ahead);
+        bring(kv, start, ahead, a.d, lds0, lds0 + TILE);
+        bring.look(kv, start + 4 * FEW_KEYS, ahead);
     }
     bool found = false;
     for (int32_t j0 = start; j0 < end; j0 += 4 * FEW_KEYS) {
@@ -307,8 +286,8 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
         for (int dt = 0; dt < 2 * ND; dt++) v[dt] = turned_from<T>(lds0 + v_at[dt], lds0 + v_at[dt] + 16 * D * 2);
         if (j0 + 4 * FEW_KEYS < end) {
             own_read();
-            load(j0 + 4 * FEW_KEYS, mine);
-            look(j0 + 8 * FEW_KEYS);
+            bring(kv, j0 + 4 * FEW_KEYS, ahead, a.d, lds0, lds0 + TILE);
+            bring.look(kv, j0 + 8 * FEW_KEYS, ahead);
         }
         f32x4 s[RB][2] = {};
 #pragma unroll

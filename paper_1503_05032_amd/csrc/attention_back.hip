@@ -81,15 +81,15 @@ template <int ND, bool WIDE, typename T> __device__ __forceinline__ void leave(T
         }
 }
 
-constexpr int DQ_ROWS = 128, DQ_SHIFT = 7, DQ_STEP = 64;
-constexpr int DKV_KEYS = 64, DKV_SHIFT = 6, DKV_STEP = 64;
+constexpr int DQ_ROWS = 128, DQ_SHIFT = 7, DQ_STEP = 32;
+constexpr int DKV_KEYS = 64, DKV_SHIFT = 6;
 
 // ---------------------------------------------------------------------------------------------------------------
-// dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 64.
+// dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 32.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = DQ_STEP * D * 2, LOADS = TILE / 4096;
-    typedef Bring<T, D, WIDE, false> B;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = DQ_STEP * D * 2;
+    typedef Bring<T, D, WIDE, false, DQ_STEP, 4> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -111,50 +111,44 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     const float delta = a.delta[int64_t(h) * a.rows + token], base = a.base[int64_t(h) * a.rows + token], c = a.scale * LOG2_E;
 
     const typename Packed<T>::One kv{same(a.k.p + keys.first * a.k.row + hk * a.k.head), same(a.v.p + keys.first * a.v.row + hk * a.v.head), a.k.row, a.v.row, __builtin_amdgcn_readfirstlane(n)};
-    const B bring(kv, wave * B::EACH + lane / B::LANES, a.d);
-    auto load = [&](int32_t j0, uint8_t* to) {
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) bring(kv, j0 + (i * 4 + wave) * B::EACH, 0, a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
-    };
+    const B bring(kv, wave, a.d);
+    const int none[B::LOADS] = {};
+    // LDS: two tiles of keys, then two of values
     const uint32_t lds0 = lds_address(lds);
-    const Read<ND> read;
+    const ReadFixed<ND> read(lds0);
     f32x16 dq[ND] = {};
-    load(0, lds);
-    int now = 0;
-    for (int32_t j0 = 0; j0 < end; j0 += DQ_STEP, now ^= 1) {
+    auto tile = [&](auto at_place, int32_t j0) {
+        constexpr int NOW = decltype(at_place)::value;
         landed<0>();
-        if (j0 + DQ_STEP > fewest && fewest < n) {        // some row does not see some key
-            if (cleanse<T>(lds + now * 2 * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
+        if (j0 + DQ_STEP > fewest && fewest < n) {          // some row does not see some key
+            if (cleanse<T>(lds + NOW * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
-        if (j0 + DQ_STEP < end) load(j0 + DQ_STEP, lds + (now ^ 1) * 2 * TILE);
+        if (j0 + DQ_STEP < end) bring(kv, j0 + DQ_STEP, none, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
+        if (j0 >= most) return;
+        f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++) {
-            const int32_t j = j0 + kb * 32;
-            if (j >= most) break;
-            const uint32_t tile = lds0 + now * 2 * TILE + kb * 32 * D * 2;
-            f32x16 s = {}, dp = {};
+        for (int kk = 0; kk < 2 * ND; kk++) s = product32(read.template row<T>(NOW * TILE, kk), q[kk], s);
 #pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) s = product32(chunk_from<T>(read.row(tile, kk)), q[kk], s);
+        for (int kk = 0; kk < 2 * ND; kk++) dp = product32(read.template row<T>((2 + NOW) * TILE, kk), dout[kk], dp);
 #pragma unroll
-            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(chunk_from<T>(read.row(tile + TILE, kk)), dout[kk], dp);
-            const bool some = j + 32 > least;       // some row does not see some key
-            vec<T, 8> ds[2];
+        for (int i = 0; i < 16; i++) s[i] = power(fmaf(s[i], c, -base)) * (dp[i] - delta);
+        if (j0 + DQ_STEP > least) {
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                s[i] = power(fmaf(s[i], c, -base)) * (dp[i] - delta);
-            }
-            if (some) {
-#pragma unroll
-                for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (j + 8 * (i / 4) + 4 * half + i % 4));
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i++) ds[i / 8][i % 8] = T(s[i]);
-#pragma unroll
-            for (int k = 0; k < 2; k++)
-#pragma unroll
-                for (int dt = 0; dt < ND; dt++) dq[dt] = product32(turned32<D, T>(read.turned(tile + k * 16 * D * 2, dt)), ds[k], dq[dt]);
+            for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (j0 + 8 * (i / 4) + 4 * half + i % 4));
         }
+        vec<T, 8> ds[2];
+#pragma unroll
+        for (int i = 0; i < 16; i++) ds[i / 8][i % 8] = T(s[i]);
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++) dq[dt] = product32(read.template turned<T>(NOW * TILE + k * 16 * D * 2, dt), ds[k], dq[dt]);
+    };
+    if (end > 0) bring(kv, 0, none, a.d, lds0, lds0 + 2 * TILE);
+    for (int32_t j0 = 0; j0 < end; j0 += 2 * DQ_STEP) {
+        tile(std::integral_constant<int, 0>(), j0);
+        if (j0 + DQ_STEP < end) tile(std::integral_constant<int, 1>(), j0 + DQ_STEP);
     }
     own_landed<0>();
     __syncthreads();
@@ -171,14 +165,15 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// dk and dv: 64 keys to a workgroup, which go through the queries that see them in tiles of 64, head by head of those that share the keys: each wavefront
-// has 32 of the keys and takes 32 of the queries, and what two have of the same keys is added up in the end.  (With 128 keys, 32 to a
+// dk and dv: 64 keys to a workgroup, which go through the queries that see them in tiles of 32 RG, head by head of those that share the keys: each
+// wavefront has 32 of the keys and takes 32 of the queries, and what RG of them have of the same keys is added up in the end.  (With 128 keys, 32 to a
 // wavefront and all queries, there are half as many workgroups and the first keys' are twice as long: 5 sequences up to 2801, 20 heads of 128 557 us.)
 // Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
 // ---------------------------------------------------------------------------------------------------------------
-template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dkv(Back<T> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = DKV_STEP * D * 2, STAGE = 2 * TILE + DKV_STEP * 8, LOADS = TILE / 4096;
-    typedef Bring<T, D, WIDE, false> B;
+template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(128 * RG, 2) void k_attend_dkv(Back<T> a) {
+    constexpr int DKV_STEP = 32 * RG, WAVES = 2 * RG;
+    constexpr int D = ND <= 2 ? 64 : 128, TILE = DKV_STEP * D * 2, STAGE = 2 * TILE + DKV_STEP * 8;
+    typedef Bring<T, D, WIDE, false, DKV_STEP, WAVES> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 2 * STAGE);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, rb = wave >> 1;
@@ -203,35 +198,35 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     auto of = [&](int h) {
         return typename Packed<T>::One{same(a.q.p + mine.first * a.q.row + h * a.q.head), same(a.dout.p + mine.first * a.dout.row + h * a.dout.head), a.q.row, a.dout.row, __builtin_amdgcn_readfirstlane(m)};
     };
-    const B bring(of(hk * a.shared), wave * B::EACH + lane / B::LANES, a.d);
-    auto load = [&](int h, int32_t i0, uint8_t* to) {
-        const auto rows = of(h);
-#pragma unroll
-        for (int i = 0; i < LOADS; i++) bring(rows, i0 + (i * 4 + wave) * B::EACH, 0, a.d, to + (i * 4 + wave) * 1024, to + TILE + (i * 4 + wave) * 1024);
-        const int32_t i = i0 + lane;
-        if (wave < 2) word_to_lds(i < m ? static_cast<const void*>((wave ? a.delta : a.base) + int64_t(h) * a.rows + mine.first + i) : &ZEROS, to + 2 * TILE + wave * 256);
-    };
+    const B bring(of(hk * a.shared), wave, a.d);
+    const int none[B::LOADS] = {};
     const uint32_t lds0 = lds_address(lds);
+    auto load = [&](int h, int32_t i0, uint32_t to) {
+        bring(of(h), i0, none, a.d, to, to + TILE);
+        // base, and delta: a wavefront for each 64
+        const int32_t i = i0 + wave % (RG / 2) * 64 + lane;
+        if (wave < RG) word_to_lds(i < m ? static_cast<const void*>((wave < RG / 2 ? a.base : a.delta) + int64_t(h) * a.rows + mine.first + i) : &ZEROS, lds + (to - lds0) + 2 * TILE + wave * 256);
+    };
     const Read<ND> read;
     f32x16 dk[ND] = {}, dv[ND] = {};
     // the step that is loaded next
     int h = hk * a.shared;
     int32_t i1 = start;
     const int32_t total = steps * a.shared;
-    auto load_next = [&](uint8_t* to) {
+    auto load_next = [&](uint32_t to) {
         load(h, i1, to);
         if ((i1 += DKV_STEP) >= m) i1 = start, h++;
     };
-    if (total > 0) load_next(lds);
+    if (total > 0) load_next(lds0);
     int now = 0;
     int32_t i0 = start;
     for (int32_t step = 0; step < total; step++, now ^= 1, i0 = i0 + DKV_STEP < m ? i0 + DKV_STEP : start) {
         landed<0>();
         if (i0 < whole && i0 + ahead < n - 1) {             // some query does not see some key
-            if (cleanse<T>(lds + now * STAGE, 2 * TILE, threadIdx.x, 256)) cleansed = 1;
+            if (cleanse<T>(lds + now * STAGE, 2 * TILE, threadIdx.x, 128 * RG)) cleansed = 1;
             __syncthreads();
         }
-        if (step + 1 < total) load_next(lds + (now ^ 1) * STAGE);
+        if (step + 1 < total) load_next(lds0 + (now ^ 1) * STAGE);
         const int32_t i = i0 + rb * 32;
         if (i >= m || i + 31 + ahead < first) continue;     // no query, or none that sees one of these keys
         const uint32_t tile = lds0 + now * STAGE + rb * 32 * D * 2, words = lds0 + now * STAGE + 2 * TILE + rb * 128 + half * 16;
@@ -272,20 +267,26 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     }
     own_landed<0>();
     __syncthreads();
-    // two wavefronts' sums by way of LDS
-    float* const sums = reinterpret_cast<float*>(lds) + (wave & 1) * (ND * 2048) + lane;
-    if (rb == 1) {
+    // the sums of the wavefronts that have the same keys by way of LDS: the upper half's to the lower's, until one has them all
 #pragma unroll
-        for (int dt = 0; dt < ND; dt++)
+    for (int more = RG / 2; more > 0; more /= 2) {
+        float* const sums = reinterpret_cast<float*>(lds) + ((wave & 1) + rb % more * 2) * (ND * 2048) + lane;
+        if (rb >= more && rb < 2 * more) {
 #pragma unroll
-            for (int i = 0; i < 16; i++) sums[(dt * 16 + i) * 64] = dk[dt][i], sums[(dt * 16 + i) * 64 + ND * 1024] = dv[dt][i];
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) sums[(dt * 16 + i) * 64] = dk[dt][i], sums[(dt * 16 + i) * 64 + ND * 1024] = dv[dt][i];
+        }
+        __syncthreads();
+        if (rb < more) {
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) dk[dt][i] += sums[(dt * 16 + i) * 64], dv[dt][i] += sums[(dt * 16 + i) * 64 + ND * 1024];
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    if (rb == 1 || !there) return;
-#pragma unroll
-    for (int dt = 0; dt < ND; dt++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) dk[dt][i] += sums[(dt * 16 + i) * 64], dv[dt][i] += sums[(dt * 16 + i) * 64 + ND * 1024];
+    if (rb > 0 || !there) return;
     T *const to_k = a.dk.p + token * a.dk.row + hk * a.dk.head, *const to_v = a.dv.p + token * a.dv.row + hk * a.dv.head;
     leave<ND, WIDE>(to_k, dk, a.scale, a.d);
     leave<ND, WIDE>(to_v, dv, 1.f, a.d);
@@ -340,7 +341,16 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
                 k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
                 k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * DQ_STEP * D * 2 + 16, s>>>(a);
             }
-            if (k_rows > 0) k_attend_dkv<T, ND, WIDE><<<uint32_t(k_tiles * kv_heads), 256, 4 * DKV_STEP * D * 2 + 16 * DKV_STEP + 16, s>>>(a);
+            auto keys = [&](auto rg) {
+                constexpr int RG = decltype(rg)::value, STEP = 32 * RG;
+                k_attend_dkv<T, ND, WIDE, RG><<<uint32_t(k_tiles * kv_heads), 128 * RG, 4 * STEP * D * 2 + 16 * STEP + 16, s>>>(a);
+            };
+            if (k_rows > 0) {
+                // long sequences of few workgroups: what the longest takes counts (5 sequences up to 2801, 5 heads of keys: 618 us for 657, all gradients; 9 up
+                // to 1025, 12 heads: 128 for 121)
+                if (rows > 96 * int64_t(sequences) && k_tiles * kv_heads <= 768) keys(std::integral_constant<int, 4>());
+                else keys(std::integral_constant<int, 2>());
+            }
         };
         auto by = [&](auto nd) {
             if (w) go(nd, std::true_type());

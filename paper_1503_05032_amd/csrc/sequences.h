@@ -80,6 +80,7 @@ template <typename T> struct Packed {
         const T *k, *v;
         int64_t k_row, v_row;
         int32_t count;
+        static constexpr bool PACKED = true;
         typedef int Ahead;          // what is looked up ahead of a load (for packed rows nothing)
         __device__ __forceinline__ Ahead ahead(int32_t) const { return 0; }
         template <int ROWS> __device__ __forceinline__ bool together(Ahead) const { return true; }
@@ -104,6 +105,7 @@ template <typename T> struct Paged {
         const T *k, *v;
         int64_t k_page, k_row, v_page, v_row;
         int32_t count;
+        static constexpr bool PACKED = false;
         typedef int32_t Ahead;      // the page of a row that is the same in every lane; -1: none
         __device__ __forceinline__ int32_t ahead(int32_t j) const {
             typedef const __attribute__((address_space(4))) int32_t* constant;      // a scalar load
@@ -190,34 +192,86 @@ template <typename T> __device__ __forceinline__ vec<T, 8> turned_from(uint32_t 
 // For 32 x 32 x 16: columns of four rows and of those 8 rows on, where bit 1 of a chunk's place is the other one.
 template <int D, typename T> __device__ __forceinline__ vec<T, 8> turned32(uint32_t at) { return turned_from<T>(at, (at ^ 32) + 8 * D * 2); }
 
+// Where a wavefront reads tiles for products of 32 x 32 x 16: rows as first operands (chunks 2 kk on), and turned (columns 32 dt on).  Tiles begin at
+// multiples of 256 bytes.  Other chunks are other patterns in bits 5 to 7: with a register for each, a tile at a fixed place needs no arithmetic; with one
+// register for all, one instruction a read.
+template <int ND> struct ReadFixed {
+    static constexpr int D = ND <= 2 ? 64 : 128;
+    uint32_t rows[2 * ND], first[ND], second[ND];
+    __device__ __forceinline__ ReadFixed(uint32_t lds) {
+        const int lane = threadIdx.x & 63, half = lane >> 5, li = lane & 15, r = half * 4 + (li >> 2);
+#pragma unroll
+        for (int kk = 0; kk < 2 * ND; kk++) rows[kk] = lds + (lane & 31) * D * 2 + chunk_at<D, false>(lane & 31, 2 * kk + half) * 16;
+#pragma unroll
+        for (int dt = 0; dt < ND; dt++) {
+            first[dt] = lds + r * D * 2 + chunk_at<D, false>(r, dt * 4 + ((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
+            second[dt] = (first[dt] ^ 32) + 8 * D * 2;
+        }
+    }
+    template <typename T> __device__ __forceinline__ vec<T, 8> row(int tile, int kk) const { return chunk_from<T>(rows[kk] + tile); }
+    template <typename T> __device__ __forceinline__ vec<T, 8> turned(int tile, int dt) const { return turned_from<T>(first[dt] + tile, second[dt] + tile); }
+};
+
 // One wavefront's load into LDS, from an address of each lane: 1024 bytes, lane by lane 16 of them; `from` NULL, or values from `have` on: zeros.
-template <bool WIDE, typename T> __device__ __forceinline__ void chunk_to_lds(const T* from, int have, uint8_t* to) {
-    if (WIDE) to_lds(from && have > 0 ? static_cast<const void*>(from) : &ZEROS, to);
-    else *reinterpret_cast<vec<T, 8>*>(to + (threadIdx.x & 63) * 16) = eight_values<false>(from, from ? have : 0);
+template <bool WIDE, typename T> __device__ __forceinline__ void chunk_to_lds(const T* from, int have, uint32_t to) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    if (WIDE) to_lds_at(from && have > 0 ? static_cast<const void*>(from) : &ZEROS, to);
+    else *(__attribute__((address_space(3))) u32x4*)uintptr_t(to + (threadIdx.x & 63) * 16) = __builtin_bit_cast(u32x4, eight_values<false>(from, from ? have : 0));
 }
 
-// What this lane asks for of the rows of a load: they lie side by side from one address on, or each is looked for.
-template <typename T, int D, bool WIDE, bool SMALL> struct Bring {
+// A tile of keys and one of values (or of any two arrays with the same rows) into LDS by WAVES wavefronts, each LOADS times a load of EACH rows of both: where
+// they lie side by side from one address on, that and one offset of each lane serve a load; else each lane looks for its row.
+template <typename T, int D, bool WIDE, bool SMALL, int ROWS, int WAVES> struct Bring {
     static constexpr int LANES = D / 8, EACH = 64 / LANES;      // lanes of a row, rows of a load
-    int row, chunk;             // this lane's, in a load
-    uint32_t k_off, v_off;      // in bytes, from the load's first row
-    bool near;                  // every lane's chunk is in the row, and no offset passes 32 bits
-    // first: the row of a tile that this lane has in its first load (in others a multiple of 16 further)
-    template <typename One> __device__ __forceinline__ Bring(const One& kv, int first, int d) {
-        row = (threadIdx.x & 63) / LANES, chunk = int(chunk_at<D, SMALL>(first, threadIdx.x % LANES)) * 8;
+    static constexpr int LOADS = ROWS / EACH / WAVES;
+    // Rows that all loads of a lane have the swizzle of; where WAVES is 1, loads differ in it.
+    static constexpr int KINDS = WAVES * EACH >= 16 ? 1 : 16 / (WAVES * EACH);
+    int wave, row;                                  // this lane's row of a load
+    int chunk[KINDS];
+    uint32_t k_off[LOADS], v_off[LOADS];            // in bytes: packed, from the tile's first row; else from the load's
+    bool near;                                      // every lane's chunk is in the row, and no offset passes 32 bits
+    template <typename One> __device__ __forceinline__ Bring(const One& kv, int wave, int d) : wave(wave) {
+        const int lane = threadIdx.x & 63;
+        row = lane / LANES;
         // where d ends within a chunk that is read, or beside it, there are zeros to be had; a chunk that is not read may be another one
-        near = WIDE && (d == D || (D == 128 && d == 96)) && (EACH * kv.k_row | EACH * kv.v_row) < (1 << 28);
-        const int c = chunk < d ? chunk : 0;
-        k_off = uint32_t(row * kv.k_row + c) * 2, v_off = uint32_t(row * kv.v_row + c) * 2;
+        near = WIDE && (d == D || (D == 128 && d == 96)) && (ROWS * kv.k_row | ROWS * kv.v_row) < (1 << 28);
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int r = (i * WAVES + wave) * EACH + row, from = One::PACKED ? r : row;
+            const int c = int(chunk_at<D, SMALL>(r, lane % LANES)) * 8, in = c < d ? c : 0;
+            chunk[i % KINDS] = c;
+            k_off[i] = uint32_t(from * kv.k_row + in) * 2, v_off[i] = uint32_t(from * kv.v_row + in) * 2;
+        }
     }
-    // rows j (a multiple of EACH, the same in every lane) on, to k and v
-    template <typename One> __device__ __forceinline__ void operator()(const One& kv, int32_t j, typename One::Ahead ahead, int d, uint8_t* k, uint8_t* v) const {
-        if (near && j + EACH <= kv.count && kv.template together<EACH>(ahead)) {
-            to_lds(kv.key(j, ahead), k_off, k), to_lds(kv.value(j, ahead), v_off, v);
-        } else {
-            const bool there = j + row < kv.count;
-            const T *const from = there ? kv.any_key(j + row) : nullptr, *const of = there ? kv.any_value(j + row) : nullptr;
-            chunk_to_lds<WIDE>(from ? from + chunk : from, d - chunk, k), chunk_to_lds<WIDE>(of ? of + chunk : of, d - chunk, v);
+    // The loads' pages, of the tile from j0 on.
+    template <typename One> __device__ __forceinline__ void look(const One& kv, int32_t j0, typename One::Ahead (&ahead)[LOADS]) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) ahead[i] = kv.ahead(j0 + (i * WAVES + wave) * EACH);
+    }
+    // k, v: where the tiles are in LDS
+    template <typename One> __device__ __forceinline__ void operator()(const One& kv, int32_t j0, const typename One::Ahead (&ahead)[LOADS], int d, uint32_t k, uint32_t v) const {
+        const bool whole = near && j0 + ROWS <= kv.count;
+        if (One::PACKED && whole) {
+            const T *const from = kv.key(j0, ahead[0]), *const of = kv.value(j0, ahead[0]);
+#pragma unroll
+            for (int i = 0; i < LOADS; i++) {
+                to_lds_at(from, k_off[i], k + (i * WAVES + wave) * 1024);
+                to_lds_at(of, v_off[i], v + (i * WAVES + wave) * 1024);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; i++) {
+            const int32_t j = j0 + (i * WAVES + wave) * EACH;
+            const uint32_t to = (i * WAVES + wave) * 1024;
+            if (!One::PACKED && whole && kv.template together<EACH>(ahead[i])) {
+                to_lds_at(kv.key(j, ahead[i]), k_off[i], k + to), to_lds_at(kv.value(j, ahead[i]), v_off[i], v + to);
+            } else {
+                const bool there = j + row < kv.count;
+                const T *const from = there ? kv.any_key(j + row) : nullptr, *const of = there ? kv.any_value(j + row) : nullptr;
+                const int c = chunk[i % KINDS];
+                chunk_to_lds<WIDE>(from ? from + c : from, d - c, k + to), chunk_to_lds<WIDE>(of ? of + c : of, d - c, v + to);
+            }
         }
     }
 };
