@@ -1,0 +1,135 @@
+"""Attention with a layer of experts behind it: values and gradients against torch in 64 bits, serving against training (GPU)."""
+import pytest
+import torch
+
+from paper_1503_05032_amd.attention import Attention, Cache, train
+from paper_1503_05032_amd.layer import Layer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+# A value passes through at most twelve roundings to bfloat16 (2^-8 each, relative), and what follows each lets its error
+# grow to at most twice: norm of the error over the norm.
+CHAIN = 12 * 2 * 2.0 ** -8
+
+
+def plain(a, x, residual, lengths):
+    """The attention in 64 bits on the CPU, of leaves that take gradients."""
+    leaf = lambda t: t.detach().double().cpu().requires_grad_()  # noqa: E731
+    p = {name: leaf(t) for name, t in a.parameters().items()}
+    xs, rs = leaf(x), leaf(residual)
+    h = xs + rs
+    u = h / (h.square().mean(dim=1, keepdim=True) + a.eps).sqrt() * p["gain"]
+    q, k, v = (u @ p["into"][0].T).view(-1, a.heads + 2 * a.kv_heads, a.d).split([a.heads, a.kv_heads, a.kv_heads], dim=1)
+    outs, at = [], 0
+    for n in lengths:
+        rows = slice(at, at + n)
+        angle = torch.arange(n).double()[:, None, None] * a.frequency.double().cpu()
+        c, s = torch.cos(angle), torch.sin(angle)
+
+        def turn(t):
+            low, high = t[rows].chunk(2, dim=-1)
+            return torch.cat([low * c - high * s, low * s + high * c], dim=-1)
+        kk, vv = (t.repeat_interleave(a.heads // a.kv_heads, dim=1) for t in (turn(k), v[rows]))
+        score = torch.einsum("ihd,jhd->hij", turn(q), kk) * a.d ** -0.5
+        score = score.masked_fill(torch.ones(n, n).triu(1).bool(), float("-inf"))
+        outs.append(torch.einsum("hij,jhd->ihd", torch.softmax(score, -1), vv).reshape(n, -1))
+        at += n
+    return torch.cat(outs) @ p["back"][0].T, h, xs, rs, p
+
+
+def near(got, want, what):
+    off = float((got.double().cpu() - want).norm() / want.norm())
+    assert off <= CHAIN, (what, off)
+
+
+def packed(lengths):
+    offset = torch.tensor([sum(lengths[:i]) for i in range(len(lengths) + 1)], dtype=torch.int32, device=DEV)
+    return offset, torch.cat([torch.arange(n, dtype=torch.int32) for n in lengths]).to(DEV)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,lengths", [(4, 2, 64, [40, 1, 77]), (6, 1, 32, [130]), (3, 3, 80, [5, 5, 60])])
+def test_values_and_gradients(heads, kv_heads, d, lengths):
+    g = torch.Generator().manual_seed(d)
+    a = Attention(width=256, heads=heads, kv_heads=kv_heads, d=d, generator=g)
+    offset, position = packed(lengths)
+    x, residual, dz, dh = (torch.randn(sum(lengths), 256, generator=g).to(DEV, a.dtype) for _ in range(4))
+    z, s = a.forward(x, offset, position, residual)
+    want, h, xs, rs, p = plain(a, x, residual, lengths)
+    near(z, want.detach(), "z")
+    near(s["h"], h.detach(), "h")
+    dx, grads = a.backward(dz, s, dh)
+    (want * dz.double().cpu()).sum().add((h * dh.double().cpu()).sum()).backward()
+    near(dx, xs.grad, "dx")
+    near(dx, rs.grad, "residual")
+    for name, got in grads.items():
+        near(got, p[name].grad, name)
+
+
+def test_served_in_chunks_and_single_tokens_as_trained():
+    """Two layers of attention and experts; three requests that come, go on, end and make room for others."""
+    g = torch.Generator().manual_seed(3)
+    blocks = [(Attention(width=256, heads=4, kv_heads=2, d=64, generator=g), Layer(width=256, inner=128, experts=4, k=2, generator=g)) for _ in range(2)]
+    cache = Cache(layers=2, pages=14, page=16, requests=3, width=6, kv_heads=2, d=64)
+    text = {name: torch.randn(90, 256, generator=g).to(DEV, torch.bfloat16) for name in "abcd"}
+
+    def trained(x):
+        offset, position = packed([x.shape[0]])
+        h = None
+        for attention, layer in blocks:
+            z, s = attention.forward(x, offset, position, h)
+            x, h = layer.forward(z, residual=s["h"])[0], None
+        return x
+
+    def served(x):
+        h = None
+        for i, (attention, layer) in enumerate(blocks):
+            z, hh = attention.serve(x, cache, i, h)
+            x = layer.forward(z, residual=hh)[0]
+        return x
+    whole = {name: trained(t) for name, t in text.items()}
+    done = dict.fromkeys("abcd", 0)
+    # what each request brings in each step: its text and how much; None: it is over
+    for step in ([("a", 50), ("b", 7), ("c", 1)], [("a", 1), ("b", 1), ("c", 33)], [("a", 39), None, ("c", 1)], [None, ("d", 20), ("c", 1)], [("", 0), ("d", 1), ("c", 50)]):
+        fresh = [-1 if s is None else s[1] for s in step]
+        parts = [(s[0], done[s[0]], s[1]) for s in step if s and s[1]]
+        x = torch.cat([text[name][at:at + n] for name, at, n in parts])
+        cache.step(torch.tensor(fresh, dtype=torch.int32, device=DEV), x.shape[0])
+        assert bool((cache.slot >= 0).all())
+        got, row = served(x), 0
+        for name, at, n in parts:
+            near(got[row:row + n], whole[name][at:at + n].double().cpu(), (name, at, n))
+            row, done[name] = row + n, at + n
+    assert cache.length.tolist() == [0, 21, 86] and int(cache.state[1]) == 14 - 2 - 6
+
+
+def test_a_step_of_serving_captured_and_replayed():
+    g = torch.Generator().manual_seed(4)
+    a = Attention(width=128, heads=4, kv_heads=2, d=32, generator=g)
+    eager, played = (Cache(layers=1, pages=40, page=4, requests=5, width=12, kv_heads=2, d=32) for _ in range(2))
+    x, fresh = torch.zeros(5, 128, dtype=a.dtype, device=DEV), torch.ones(5, dtype=torch.int32, device=DEV)
+
+    def step(cache):
+        cache.step(fresh, 5)
+        return a.serve(x, cache, 0)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(Cache(layers=1, pages=40, page=4, requests=5, width=12, kv_heads=2, d=32))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(played)
+    for _ in range(10):
+        x.copy_(torch.randn(5, 128, generator=g))
+        want = step(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want, out) and torch.equal(eager.k, played.k) and torch.equal(eager.length, played.length) and torch.equal(eager.table, played.table)
+
+
+def test_training_runs():
+    g = torch.Generator().manual_seed(5)
+    make = lambda: (Attention(width=128, heads=4, kv_heads=2, d=32, generator=g), Layer(width=128, inner=64, experts=4, k=2, generator=g))  # noqa: E731
+    losses = train(make(), make(), steps=3, tokens=60, generator=g)
+    assert len(losses) == 3 and all(loss == loss and loss < float("inf") for loss in losses)
