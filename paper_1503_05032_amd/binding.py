@@ -666,14 +666,10 @@ def csr5_rotary(q, k, position, frequency, q_out, k_out=None, axis=None, interle
     return _chk(_native().rotary(q, k, position, frequency, q_out, k_out, axis, interleaved, inverse, v, slot, k_cache, v_cache, stream), "csr5_rotary", check)
 
 
-def _scale(scale, q):
-    return max(q.shape[-1], 1) ** -0.5 if scale is None else scale
-
-
 def csr5_attention(q, k, v, q_offset, k_offset, out, lse=None, scale=None, causal=True, stream=None, check=True):
     """Attention over packed sequences: q and out [rows, heads, d], k and v [k_rows, kv_heads, d], q_offset and k_offset int32
     [sequences + 1], lse float32 [heads, rows]; scale: d^-0.5 where it is None."""
-    return _chk(_native().attention(q, k, v, q_offset, k_offset, out, lse, _scale(scale, q), causal, stream), "csr5_attention", check)
+    return _chk(_native().attention(q, k, v, q_offset, k_offset, out, lse, scale, causal, stream), "csr5_attention", check)
 
 
 def csr5_attention_backward_workspace_bytes(rows, heads):
@@ -683,7 +679,7 @@ def csr5_attention_backward_workspace_bytes(rows, heads):
 def csr5_attention_backward(dout, q, k, v, out, lse, q_offset, k_offset, dq, dk, dv, workspace, scale=None, causal=True, stream=None, check=True):
     """Gradients dq, dk and dv of csr5_attention from dout, out and lse; `workspace` (uint8) has
     csr5_attention_backward_workspace_bytes bytes."""
-    return _chk(_native().attention_backward(dout, q, k, v, out, lse, q_offset, k_offset, dq, dk, dv, workspace, _scale(scale, q), causal, stream), "csr5_attention_backward", check)
+    return _chk(_native().attention_backward(dout, q, k, v, out, lse, q_offset, k_offset, dq, dk, dv, workspace, scale, causal, stream), "csr5_attention_backward", check)
 
 
 def csr5_attention_paged_workspace_bytes(rows, heads, kv_heads, d, sequences, max_length):
@@ -694,4 +690,4 @@ def csr5_attention_paged(q, k_cache, v_cache, q_offset, length, table, out, work
     """Causal attention of each request's last tokens, q and out [rows, heads, d], over length[s] tokens in the pages table[s] of
     k_cache and v_cache [pages, page, kv_heads, d]; `workspace` (uint8) has csr5_attention_paged_workspace_bytes bytes, with
     max_length = table.shape[1] * page."""
-    return _chk(_native().attention_paged(q, k_cache, v_cache, q_offset, length, table, out, workspace, lse, _scale(scale, q), stream), "csr5_attention_paged", check)
+    return _chk(_native().attention_paged(q, k_cache, v_cache, q_offset, length, table, out, workspace, lse, scale, stream), "csr5_attention_paged", check)

@@ -8,6 +8,7 @@
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <stdexcept>
 #include <string>
 
@@ -394,6 +395,8 @@ Sizes packed(const Args& a, int q, int k, int q_offset, int k_offset) {
     return {int32_t(n), int32_t(tq.size(0)), int32_t(tk.size(0)), int32_t(tq.size(1)), int32_t(tk.size(1)), int32_t(tq.size(2)), type, dtype};
 }
 
+float scale_of(const Args& a, int i, int64_t d) { return a.none(i) ? 1.f / std::sqrt(float(std::max<int64_t>(d, 1))) : float(a.real(i, "scale")); }
+
 // q, k, v, q_offset, k_offset, out, lse, scale, causal, stream
 int attention(const Args& a) {
     const Sizes z = packed(a, 0, 1, 3, 4);
@@ -401,7 +404,7 @@ int attention(const Args& a) {
     const csr5_heads_t out = a.heads(5, "out", z.type, z.rows, z.heads, z.d);
     const int32_t *const qo = row_pointer(a, 3, "q_offset", z.sequences), *const ko = row_pointer(a, 4, "k_offset", z.sequences);
     float* const lse = a.floats(6, "lse", int64_t(z.rows) * z.heads);
-    const float scale = float(a.real(7, "scale"));
+    const float scale = scale_of(a, 7, z.d);
     const bool causal = a.truth(8, "causal");
     void* const stream = a.stream(9);
     return csr5_attention(z.sequences, z.rows, z.k_rows, z.heads, z.kv_heads, z.d, z.dtype, qo, ko, scale, causal, q, k, v, out, lse, stream);
@@ -417,7 +420,7 @@ int attention_backward(const Args& a) {
     const int32_t *const qo = row_pointer(a, 6, "q_offset", z.sequences), *const ko = row_pointer(a, 7, "k_offset", z.sequences);
     void* const space = a.array<uint8_t>(11, "workspace", at::kByte, 0);
     const size_t bytes = a.none(11) ? 0 : size_t(a.tensor(11, "workspace").numel());
-    const float scale = float(a.real(12, "scale"));
+    const float scale = scale_of(a, 12, z.d);
     const bool causal = a.truth(13, "causal");
     void* const stream = a.stream(14);
     return csr5_attention_backward(z.sequences, z.rows, z.k_rows, z.heads, z.kv_heads, z.d, z.dtype, qo, ko, scale, causal, dout, q, k, v, out, lse, dq, dk, dv, space, bytes, stream);
@@ -439,7 +442,7 @@ int attention_paged(const Args& a) {
     void* const space = a.array<uint8_t>(7, "workspace", at::kByte, 0);
     const size_t bytes = a.none(7) ? 0 : size_t(a.tensor(7, "workspace").numel());
     float* const lse = a.floats(8, "lse", rows * heads);
-    const float scale = float(a.real(9, "scale"));
+    const float scale = scale_of(a, 9, d);
     void* const stream = a.stream(10);
     return csr5_attention_paged(int32_t(n), int32_t(rows), int32_t(heads), int32_t(kv_heads), int32_t(d), dtype, qo, length, as<int32_t>(table), int32_t(table.cols), table.ld, int32_t(n_pages),
                                 int32_t(page), scale, q, k, v, out, lse, space, bytes, stream);

@@ -156,7 +156,7 @@ def test_rotary_takes_a_cache_or_rows(lib):
     with pytest.raises(ValueError, match="frequency"):
         run("csr5_rotary", here | tensors(frequency=(F32, 33)), {})
     with pytest.raises(ValueError):
-        run("csr5_rotary", here, {"interleaved": None, "inverse": object()} | {"axis": 3})
+        run("csr5_rotary", here | {"axis": 3}, {})
 
 
 def test_scale_is_a_number(lib):
