@@ -592,7 +592,7 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void *h, int
  * What section 5 says of streams, graphs, sums in 32 bits, timing and addresses holds here.  A
  * row has `heads` heads of d neighbouring values, at any strides (in elements); query head h
  * goes with head h / (heads / kv_heads) of keys and values.  16-byte aligned addresses, strides of a
- * multiple of 16 bytes and d in whole 16 bytes get the fast kernels.  An output must not overlap itself
+ * multiple of 16 bytes and d in whole 16 bytes get the fast kernels (attention: the fastest loads with d of 64, 96 or 128).  An output must not overlap itself
  * (CSR5_EINVAL).  Offsets are clamped to [0, rows] and lengths to what the table holds; a page outside
  * [0, pages) is one of zeros where it is read, and none where it would be written.
  * ========================================================================== */
@@ -658,8 +658,9 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
  *   q, out [rows][heads][d]; k, v [k_rows][kv_heads][d] in dtype (BF16, F16); lse float[heads][rows], or NULL
  * d <= CSR5_ATTENTION_MAX_D, heads <= CSR5_ATTENTION_MAX_HEADS, rows and k_rows <= CSR5_ATTENTION_MAX_ROWS, else
  * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite.
- * Softmax statistics and sums are held in 32 bits; p is rounded to dtype, relative to the largest so far, before it is
- * multiplied by v.
+ * Softmax statistics and sums are held in 32 bits; exp(scale q.k_j - b) is rounded to dtype before it is multiplied by v,
+ * b a running base that the largest score so far passes by 8 ln 2 at most.  What a row does not see has no part in it,
+ * whatever it holds; a value that is infinite where it is seen counts with its sign, also where its p is too small for dtype.
  */
 int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype,
                    const int32_t *q_offset, const int32_t *k_offset, float scale, int causal, csr5_heads_t q,
@@ -669,7 +670,9 @@ int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t head
  * Its gradients, from dout (of out), out and lse:
  *   ds_ij = p_ij (dout_i . v_j - dout_i . out_i),  dq_i = scale sum_j ds_ij k_j,
  *   dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
- * with the sums of dk and dv over the query heads that share them.  p and ds are rounded to dtype before they are multiplied.
+ * with the sums of dk and dv over the query heads that share them.  p and ds are rounded to dtype before they are multiplied (F16:
+ * a ds past 65504 becomes infinite).  A query that is not finite, or whose dout is not, has a part in the gradients of the keys that it sees
+ * only, and a key that is not in those of the queries that see it.
  * Rows in no sequence are left as they are.  workspace: csr5_attention_backward_workspace_bytes bytes, free again after the call.
  */
 size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads);

