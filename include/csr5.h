@@ -660,7 +660,7 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
  * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite.
  * Softmax statistics and sums are held in 32 bits; exp(scale q.k_j - b) is rounded to dtype before it is multiplied by v,
  * b a running base that the largest score so far passes by 8 ln 2 at most.  What a row does not see has no part in it,
- * whatever it holds; a value that is infinite where it is seen counts with its sign, also where its p is too small for dtype.
+ * whatever it holds; a value that is not finite where it is seen makes the result not finite.
  */
 int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype,
                    const int32_t *q_offset, const int32_t *k_offset, float scale, int causal, csr5_heads_t q,
