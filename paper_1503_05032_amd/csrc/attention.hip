@@ -107,22 +107,23 @@ template <int ND, typename T, typename KV, typename One> __device__ __forceinlin
     }
 }
 
-template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds__(256, 3) void k_attend_many(Attend<T, KV> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = MANY_KEYS * D * 2;
-    typedef Bring<T, D, WIDE, false, MANY_KEYS, 4> B;
+template <typename T, typename KV, int ND, bool WIDE, int KG> __global__ __launch_bounds__(256, KG == 1 ? 3 : 2) void k_attend_many(Attend<T, KV> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, KEYS = MANY_KEYS * KG, TILE = KEYS * D * 2, ROWS = MANY_ROWS / KG;
+    constexpr int SHIFT = KG == 1 ? MANY_SHIFT : KG == 2 ? MANY_SHIFT - 1 : MANY_SHIFT - 2;
+    typedef Bring<T, D, WIDE, false, KEYS, 4> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, kg = KG == 1 ? 0 : wave / (4 / KG);
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
-    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, MANY_SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
+    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
     const auto kv = a.kv.one(at.s, hk);
     const int32_t m = at.rows.count, n = kv.count;
-    const int64_t first = at.first + wave * 32;
+    const int64_t first = at.first + wave % (4 / KG) * 32;
     const Row row = row_of(first + (lane & 31), m, n, a.shared, a.causal);
     // the keys that this wavefront's first and last row see, and the workgroup's
     const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
-    const int32_t all = __builtin_amdgcn_readfirstlane(row_of(at.first + MANY_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t all = __builtin_amdgcn_readfirstlane(row_of(at.first + ROWS - 1, m, n, a.shared, a.causal).limit);
     const int32_t fewest = __builtin_amdgcn_readfirstlane(row_of(at.first, m, n, a.shared, a.causal).limit);
     const int32_t begin = a.chunk * int32_t(blockIdx.y), end = a.chunk ? min(all, begin + a.chunk) : all;
     if (a.chunk && begin >= end) return;
@@ -138,7 +139,7 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
     const uint32_t lds0 = lds_address(lds);
     const B bring(kv, wave, a.d);
     typename decltype(kv)::Ahead ahead[B::LOADS];
-    const ReadFixed<ND> read(lds0);
+    const ReadFixed<ND> read(lds0 + kg * MANY_KEYS * D * 2);      // its 32 keys of a tile
 
     const float c = a.scale * LOG2_E, rise = RISE / c;
     float base = -INFINITY, sum = 0.f;
@@ -146,22 +147,23 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
     auto tile = [&](auto at_place, int32_t j0) {
         constexpr int NOW = decltype(at_place)::value;
         landed<0>();
-        if (j0 + MANY_KEYS > fewest && fewest < n) {        // some row does not see some key
+        if (j0 + KEYS > fewest && fewest < n) {        // some row does not see some key
             if (cleanse<T>(lds + (2 + NOW) * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
-        if (j0 + MANY_KEYS < end) {
-            bring(kv, j0 + MANY_KEYS, ahead, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
-            bring.look(kv, j0 + 2 * MANY_KEYS, ahead);
+        if (j0 + KEYS < end) {
+            bring(kv, j0 + KEYS, ahead, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
+            bring.look(kv, j0 + 2 * KEYS, ahead);
         }
-        if (j0 >= most) return;
+        const int32_t mine = j0 + kg * MANY_KEYS;           // this wavefront's keys
+        if (mine >= most) return;
         f32x16 s = {};
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int kk = 0; kk < 2 * ND; kk++) s = product32(read.template row<T>(NOW * TILE, kk), q[kk], s);
-        if (j0 + MANY_KEYS > least) {
+        if (mine + MANY_KEYS > least) {
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[i] = or_none(s[i], row.limit - 1 - (j0 + 8 * (i / 4) + 4 * half + i % 4));
+            for (int i = 0; i < 16; i++) s[i] = or_none(s[i], row.limit - 1 - (mine + 8 * (i / 4) + 4 * half + i % 4));
         }
         __builtin_amdgcn_s_setprio(0);
         float top = s[0];
@@ -194,16 +196,39 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
     if (begin < end) {
         bring.look(kv, begin, ahead);
         bring(kv, begin, ahead, a.d, lds0, lds0 + 2 * TILE);
-        bring.look(kv, begin + MANY_KEYS, ahead);
+        bring.look(kv, begin + KEYS, ahead);
     }
-    for (int32_t j0 = begin; j0 < end; j0 += 2 * MANY_KEYS) {
+    for (int32_t j0 = begin; j0 < end; j0 += 2 * KEYS) {
         tile(std::integral_constant<int, 0>(), j0);
-        if (j0 + MANY_KEYS < end) tile(std::integral_constant<int, 1>(), j0 + MANY_KEYS);
+        if (j0 + KEYS < end) tile(std::integral_constant<int, 1>(), j0 + KEYS);
     }
     own_landed<0>();
     __syncthreads();
     sum = half_sum(sum);
-    if (!row.there) return;
+    // the sums of the wavefronts that have the same rows by way of LDS: the upper half's to the lower's, until one has them all
+#pragma unroll
+    for (int more = KG / 2; more > 0; more /= 2) {
+        float* const place = reinterpret_cast<float*>(lds) + (wave % (4 / KG) + kg % more * (4 / KG)) * (ND * 1024 + 128) + lane;
+        if (kg >= more && kg < 2 * more) {
+            place[0] = base, place[64] = sum;
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) place[(2 + dt * 16 + i) * 64] = o[dt][i];
+        }
+        __syncthreads();
+        if (kg < more) {
+            const float other = place[0], higher = fmaxf(base, other);
+            const float less = base == higher ? 1.f : power((base - higher) * c), weight = other == higher ? 1.f : power((other - higher) * c);
+            base = higher, sum = sum * less + place[64] * weight;
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) o[dt][i] = o[dt][i] * less + place[(2 + dt * 16 + i) * 64] * weight;
+        }
+        __syncthreads();
+    }
+    if (kg > 0 || !row.there) return;
     const Leave<T, KV> leave(a, at.rows.first + row.token, hk * a.shared + row.head);
     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
@@ -215,7 +240,7 @@ template <typename T, typename KV, int ND, bool WIDE> __global__ __launch_bounds
         }
     if (half == 0) leave.total(base, sum, a.scale);
     // the tiles that were cleansed begin with the first that some row does not see whole
-    if (cleansed) repair<ND>(leave, kv, max(begin, fewest / MANY_KEYS * MANY_KEYS), min(row.limit, end), a.d);
+    if (cleansed) repair<ND>(leave, kv, max(begin, fewest / KEYS * KEYS), min(row.limit, end), a.d);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -429,6 +454,7 @@ template <typename T, typename KV> __global__ __launch_bounds__(256) void k_join
 // ---------------------------------------------------------------------------------------------------------------
 struct Plan {
     int blocks;             // of 16 rows: few rows; 0: many
+    int sides;              // many rows: wavefronts that share a row's keys, 128 / sides rows to a workgroup
     int64_t tiles, chunk, chunks;
 };
 // By the rows that a sequence has on average (the host does not know each): 64 are where few rows' kernel ends (sequences of 131 to 420 rows
@@ -437,8 +463,13 @@ struct Plan {
 // and 4096, 527 for 8192; parts of 128 for 8 short ones: 23.7 against 18.6).
 Plan plan_of(int64_t rows, int64_t heads, int64_t kv_heads, int64_t sequences, int64_t most_keys, bool split) {
     const int64_t shared = kv_heads ? heads / kv_heads : 1, each = (rows + sequences - 1) / sequences * shared;
-    Plan p{each <= 16 ? 1 : each <= 32 ? 2 : each <= 64 ? 4 : 0, 0, 0, 1};
+    Plan p{each <= 16 ? 1 : each <= 32 ? 2 : each <= 64 ? 4 : 0, 1, 0, 0, 1};
     p.tiles = tiles_at_most(sequences, rows, shared, p.blocks == 1 ? 4 : p.blocks == 2 ? 5 : p.blocks == 4 ? 6 : MANY_SHIFT);
+    if (p.blocks == 0) {
+        const int64_t groups = p.tiles * kv_heads;
+        p.sides = sides_of(groups);
+        if (p.sides > 1) p.tiles = tiles_at_most(sequences, rows, shared, p.sides == 2 ? MANY_SHIFT - 1 : MANY_SHIFT - 2);
+    }
     if (split) {
         const int64_t groups = p.tiles * kv_heads, least = p.blocks ? 256 : 512, unit = 128;
         int64_t chunk = (most_keys * groups / 2048 + unit - 1) / unit * unit;
@@ -463,7 +494,15 @@ template <typename T, typename KV> int attend(Attend<T, KV> a, const Plan& p, bo
         if (p.blocks == 1) few(std::integral_constant<int, 1>());
         else if (p.blocks == 2) few(std::integral_constant<int, 2>());
         else if (p.blocks == 4) few(std::integral_constant<int, 4>());
-        else k_attend_many<T, KV, ND, WIDE><<<grid, 256, 4 * MANY_KEYS * TILE + 16, s>>>(a);
+        else {
+            auto many = [&](auto kg) {
+                constexpr int KG = decltype(kg)::value;
+                k_attend_many<T, KV, ND, WIDE, KG><<<grid, 256, 4 * KG * MANY_KEYS * TILE + 16, s>>>(a);
+            };
+            if (p.sides == 4) many(std::integral_constant<int, 4>());
+            else if (p.sides == 2) many(std::integral_constant<int, 2>());
+            else many(std::integral_constant<int, 1>());
+        }
     };
     auto by = [&](auto nd) {
         if (wide) go(nd, std::true_type());

@@ -29,6 +29,7 @@ template <typename T> struct Back {
     float *delta, *base;        // [heads][rows]: dout . out, and lse log2 e
     Heads<T> dq, dk, dv;
     int32_t tiles;
+    float* part;                // sums of dk, then of dv, by workgroups that have some of the heads only: [part][2][k_rows][kv_heads][d]; NULL: there are none
 };
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -88,20 +89,20 @@ constexpr int DKV_KEYS = 64, DKV_SHIFT = 6;
 // dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 32.
 // 5 sequences up to 2801, 20 heads of 128 with 5 of keys: 167 us, 730 TFLOP/s of its three products.
 // ---------------------------------------------------------------------------------------------------------------
-template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
-    constexpr int D = ND <= 2 ? 64 : 128, TILE = DQ_STEP * D * 2;
-    typedef Bring<T, D, WIDE, false, DQ_STEP, 4> B;
+template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
+    constexpr int D = ND <= 2 ? 64 : 128, KEYS = DQ_STEP * KG, TILE = KEYS * D * 2, ROWS = DQ_ROWS / KG;
+    typedef Bring<T, D, WIDE, false, KEYS, 4> B;
     extern __shared__ __align__(16) uint8_t lds[];          // begins at 0: nothing else is in LDS, so bits of addresses can be turned over
     int32_t& cleansed = *reinterpret_cast<int32_t*>(lds + 4 * TILE);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, kg = KG == 1 ? 0 : wave / (4 / KG);
     const int32_t hk = blockIdx.x % a.kv_heads;
     TileOf at;
-    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, DQ_SHIFT, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
+    if (!tile_of(a.q_offset, a.sequences, a.rows, a.shared, KG == 1 ? DQ_SHIFT : KG == 2 ? DQ_SHIFT - 1 : DQ_SHIFT - 2, a.tiles - 1 - int32_t(blockIdx.x / a.kv_heads), at)) return;
     const Span keys = span_of(a.k_offset, at.s, a.k_rows);
     const int32_t m = at.rows.count, n = keys.count;
-    const Row row = row_of(at.first + wave * 32 + (lane & 31), m, n, a.shared, a.causal);
+    const Row row = row_of(at.first + wave % (4 / KG) * 32 + (lane & 31), m, n, a.shared, a.causal);
     const int32_t least = __builtin_amdgcn_readfirstlane(row.limit), most = __builtin_amdgcn_readlane(row.limit, 31);
-    const int32_t end = __builtin_amdgcn_readfirstlane(row_of(at.first + DQ_ROWS - 1, m, n, a.shared, a.causal).limit);
+    const int32_t end = __builtin_amdgcn_readfirstlane(row_of(at.first + ROWS - 1, m, n, a.shared, a.causal).limit);
     const int32_t fewest = __builtin_amdgcn_readfirstlane(row_of(at.first, m, n, a.shared, a.causal).limit);
     if (threadIdx.x == 0) cleansed = 0;
     const int64_t token = at.rows.first + row.token;
@@ -116,17 +117,18 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
     const int none[B::LOADS] = {};
     // LDS: two tiles of keys, then two of values
     const uint32_t lds0 = lds_address(lds);
-    const ReadFixed<ND> read(lds0);
+    const ReadFixed<ND> read(lds0 + kg * DQ_STEP * D * 2);        // its 32 keys of a tile
     f32x16 dq[ND] = {};
     auto tile = [&](auto at_place, int32_t j0) {
         constexpr int NOW = decltype(at_place)::value;
         landed<0>();
-        if (j0 + DQ_STEP > fewest && fewest < n) {          // some row does not see some key
+        if (j0 + KEYS > fewest && fewest < n) {          // some row does not see some key
             if (cleanse<T>(lds + NOW * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
-        if (j0 + DQ_STEP < end) bring(kv, j0 + DQ_STEP, none, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
-        if (j0 >= most) return;
+        if (j0 + KEYS < end) bring(kv, j0 + KEYS, none, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
+        const int32_t mine = j0 + kg * DQ_STEP;             // this wavefront's keys
+        if (mine >= most) return;
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int kk = 0; kk < 2 * ND; kk++) s = product32(read.template row<T>(NOW * TILE, kk), q[kk], s);
@@ -134,9 +136,9 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
         for (int kk = 0; kk < 2 * ND; kk++) dp = product32(read.template row<T>((2 + NOW) * TILE, kk), dout[kk], dp);
 #pragma unroll
         for (int i = 0; i < 16; i++) s[i] = power(fmaf(s[i], c, -base)) * (dp[i] - delta);
-        if (j0 + DQ_STEP > least) {
+        if (mine + DQ_STEP > least) {
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (j0 + 8 * (i / 4) + 4 * half + i % 4));
+            for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (mine + 8 * (i / 4) + 4 * half + i % 4));
         }
         vec<T, 8> ds[2];
 #pragma unroll
@@ -147,18 +149,37 @@ template <typename T, int ND, bool WIDE> __global__ __launch_bounds__(256, 2) vo
             for (int dt = 0; dt < ND; dt++) dq[dt] = product32(read.template turned<T>(NOW * TILE + k * 16 * D * 2, dt), ds[k], dq[dt]);
     };
     if (end > 0) bring(kv, 0, none, a.d, lds0, lds0 + 2 * TILE);
-    for (int32_t j0 = 0; j0 < end; j0 += 2 * DQ_STEP) {
+    for (int32_t j0 = 0; j0 < end; j0 += 2 * KEYS) {
         tile(std::integral_constant<int, 0>(), j0);
-        if (j0 + DQ_STEP < end) tile(std::integral_constant<int, 1>(), j0 + DQ_STEP);
+        if (j0 + KEYS < end) tile(std::integral_constant<int, 1>(), j0 + KEYS);
     }
     own_landed<0>();
     __syncthreads();
-    if (!row.there) return;
+    // the sums of the wavefronts that have the same rows by way of LDS, as in attention.hip
+#pragma unroll
+    for (int more = KG / 2; more > 0; more /= 2) {
+        float* const place = reinterpret_cast<float*>(lds) + (wave % (4 / KG) + kg % more * (4 / KG)) * (ND * 1024) + lane;
+        if (kg >= more && kg < 2 * more) {
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) place[(dt * 16 + i) * 64] = dq[dt][i];
+        }
+        __syncthreads();
+        if (kg < more) {
+#pragma unroll
+            for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) dq[dt][i] += place[(dt * 16 + i) * 64];
+        }
+        __syncthreads();
+    }
+    if (kg > 0 || !row.there) return;
     T* const to = a.dq.p + token * a.dq.row + h * a.dq.head;
     leave<ND, WIDE>(to, dq, a.scale, a.d);
     // a key that is not finite makes the values of dq not finite that it has so; the others are by way of lse
     if (cleansed)
-        for (int32_t j = fewest / DQ_STEP * DQ_STEP; j < row.limit; j++)
+        for (int32_t j = fewest / KEYS * KEYS; j < row.limit; j++)
             for (int i = 0; i < 16 * ND; i++) {
                 const int x = i / 4 * 8 + half * 4 + i % 4;
                 if (x < a.d && !finite(float(kv.any_key(j)[x]))) to[x] = T(NAN);
@@ -196,6 +217,8 @@ template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(12
     if (threadIdx.x == 0) cleansed = 0;
     const int32_t start = max(0, int32_t(at.first) - ahead) / DKV_STEP * DKV_STEP, steps = m > start ? (m - start + DKV_STEP - 1) / DKV_STEP : 0;
 
+    // the heads of this workgroup, of those that share the keys
+    const int first_head = int(int64_t(blockIdx.y) * a.shared / gridDim.y), last_head = int(int64_t(blockIdx.y + 1) * a.shared / gridDim.y);
     // the queries of a head, and their dout, as rows side by side
     auto of = [&](int h) {
         return typename Packed<T>::One{same(a.q.p + mine.first * a.q.row + h * a.q.head), same(a.dout.p + mine.first * a.dout.row + h * a.dout.head), a.q.row, a.dout.row, __builtin_amdgcn_readfirstlane(m)};
@@ -212,9 +235,9 @@ template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(12
     const Read<ND> read;
     f32x16 dk[ND] = {}, dv[ND] = {};
     // the step that is loaded next
-    int h = hk * a.shared;
+    int h = hk * a.shared + first_head;
     int32_t i1 = start;
-    const int32_t total = steps * a.shared;
+    const int32_t total = steps * (last_head - first_head);
     auto load_next = [&](uint32_t to) {
         load(h, i1, to);
         if ((i1 += DKV_STEP) >= m) i1 = start, h++;
@@ -290,11 +313,23 @@ template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(12
     }
     if (rb > 0 || !there) return;
     T *const to_k = a.dk.p + token * a.dk.row + hk * a.dk.head, *const to_v = a.dv.p + token * a.dv.row + hk * a.dv.head;
-    leave<ND, WIDE>(to_k, dk, a.scale, a.d);
-    leave<ND, WIDE>(to_v, dv, 1.f, a.d);
+    const int64_t step = int64_t(a.k_rows) * a.kv_heads * a.d;
+    float* const part = a.part ? a.part + blockIdx.y * 2 * step + (token * a.kv_heads + hk) * a.d : nullptr;
+    if (part) {
+#pragma unroll
+        for (int dt = 0; dt < ND; dt++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int x = dt * 32 + i / 4 * 8 + half * 4 + i % 4;
+                if (x < a.d) part[x] = dk[dt][i], part[step + x] = dv[dt][i];
+            }
+    } else {
+        leave<ND, WIDE>(to_k, dk, a.scale, a.d);
+        leave<ND, WIDE>(to_v, dv, 1.f, a.d);
+    }
     if (!cleansed) return;
     // a query that is not finite makes all of dk and dv so of the keys that it sees, a dout that is not all of dk, and the values of dv that it has so
-    for (int g = 0; g < a.shared; g++)
+    for (int g = first_head; g < last_head; g++)
         for (int32_t i = max(start, key - ahead); i < min(m, start + (whole - start + DKV_STEP - 1) / DKV_STEP * DKV_STEP); i++) {
             const T *const q = a.q.p + (mine.first + i) * a.q.row + (hk * a.shared + g) * a.q.head, *const o = a.dout.p + (mine.first + i) * a.dout.row + (hk * a.shared + g) * a.dout.head;
             bool bad_q = false, bad_o = false;
@@ -303,18 +338,50 @@ template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(12
             for (int e = 0; e < 16 * ND; e++) {
                 const int x = e / 4 * 8 + half * 4 + e % 4;
                 if (x >= a.d) continue;
-                to_k[x] = T(NAN);
-                if (bad_q) to_v[x] = T(NAN);
-                else if (!finite(float(o[x]))) to_v[x] = T(float(to_v[x]) + float(o[x]));
+                const float more = bad_q ? NAN : finite(float(o[x])) ? 0.f : float(o[x]);
+                if (part) part[x] = NAN, part[step + x] += more;
+                else to_k[x] = T(NAN), to_v[x] = T(float(to_v[x]) + more);
             }
         }
+}
+
+// The parts of dk and dv, added up in their order: a wavefront for each key and head.
+template <typename T> __global__ __launch_bounds__(256) void k_add(Back<T> a, int parts) {
+    const int64_t at = workgroup() * 4 + (threadIdx.x >> 6);
+    if (at >= int64_t(a.k_rows) * a.kv_heads) return;
+    const int32_t row = __builtin_amdgcn_readfirstlane(int32_t(at / a.kv_heads)), hk = __builtin_amdgcn_readfirstlane(int32_t(at % a.kv_heads)), lane = threadIdx.x & 63;
+    Span keys;
+    const int32_t s = last_of(a.k_offset, a.sequences, a.k_rows, keys, [&](int32_t begin, int32_t) { return begin <= row; });
+    if (s < 0 || row >= keys.first + keys.count) return;
+    const int64_t step = int64_t(a.k_rows) * a.kv_heads * a.d;
+    for (int x = lane; x < a.d; x += 64) {
+        float dk = 0.f, dv = 0.f;
+        for (int p = 0; p < parts; p++) dk += a.part[p * 2 * step + at * a.d + x], dv += a.part[(p * 2 + 1) * step + at * a.d + x];
+        a.dk.p[row * a.dk.row + hk * a.dk.head + x] = T(dk * a.scale), a.dv.p[row * a.dv.row + hk * a.dv.head + x] = T(dv);
+    }
+}
+
+// Workgroups that have the same keys and some of the heads each, where there are few workgroups and many heads share keys: dk and dv are then added up
+// from their parts, in 32 bits in the workspace.  (One sequence of 3549, 16 heads with one of keys, 57 workgroups of 450 steps: all
+// gradients and the attention 1275 us, 497 in nine parts.)
+constexpr size_t MOST_PARTS = size_t(32) << 20;
+int parts_of(int64_t groups, int64_t shared, int64_t k_values, size_t room) {
+    if (groups > 256 || groups == 0 || shared < 2 || k_values == 0) return 1;
+    int64_t parts = (512 + groups - 1) / groups;
+    const int64_t fit = int64_t(room) / (k_values * 8);
+    parts = parts < shared ? parts : shared, parts = parts < fit ? parts : fit;
+    return parts < 2 ? 1 : int(parts);
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads) { return rows <= 0 || heads <= 0 ? 0 : size_t(rows) * size_t(heads) * 8; }
+size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads) {
+    if (rows <= 0 || heads <= 0) return 0;
+    const size_t all = size_t(rows) * size_t(heads), parts = all * 1024;        // of all heads, with as many keys as queries and 128 values to a head
+    return all * 8 + (parts < MOST_PARTS ? parts : MOST_PARTS);
+}
 
 int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype, const int32_t* q_offset,
                             const int32_t* k_offset, float scale, int causal, csr5_heads_t dout, csr5_heads_t q, csr5_heads_t k, csr5_heads_t v, csr5_heads_t out,
@@ -327,31 +394,43 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
     if (sequences == 0 || heads == 0 || d == 0 || (rows == 0 && k_rows == 0)) return CSR5_OK;
     if (!q_offset || !k_offset || (rows > 0 && !lse)) return CSR5_EINVAL;
     if (rows > 0 && (!workspace || workspace_bytes < csr5_attention_backward_workspace_bytes(rows, heads))) return CSR5_ENOMEM;
-    const int64_t q_tiles = tiles_at_most(sequences, rows, heads / kv_heads, DQ_SHIFT), k_tiles = tiles_at_most(sequences, k_rows, 1, DKV_SHIFT);
+    const int64_t wide_tiles = tiles_at_most(sequences, rows, heads / kv_heads, DQ_SHIFT);
+    const int sides = sides_of(wide_tiles * kv_heads);
+    const int64_t q_tiles = tiles_at_most(sequences, rows, heads / kv_heads, sides == 1 ? DQ_SHIFT : sides == 2 ? DQ_SHIFT - 1 : DQ_SHIFT - 2), k_tiles = tiles_at_most(sequences, k_rows, 1, DKV_SHIFT);
     if (q_tiles * kv_heads * 256 > UINT32_MAX || k_tiles * kv_heads * 256 > UINT32_MAX) return CSR5_ERANGE;
+    const size_t room = csr5_attention_backward_workspace_bytes(rows, heads) - size_t(rows) * size_t(heads) * 8;
+    const int parts = rows == 0 ? 1 : parts_of(k_tiles * kv_heads, heads / kv_heads, int64_t(k_rows) * kv_heads * d, room);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const bool w = d % 8 == 0 && wide(q, 2) && wide(k, 2) && wide(v, 2) && wide(out, 2) && wide(dout, 2) && wide(dq, 2) && wide(dk, 2) && wide(dv, 2);
     return with_half(dtype, [&](auto zero) {
         using T = decltype(zero);
         float* const delta = static_cast<float*>(workspace);
         const Back<T> a{sequences, rows, k_rows, heads, kv_heads, heads / kv_heads, d, q_offset, k_offset, scale, causal != 0, typed<const T>(dout), typed<const T>(q), typed<const T>(out),
-                        typed<const T>(k), typed<const T>(v), lse, delta, delta + size_t(rows) * size_t(heads), typed<T>(dq), typed<T>(dk), typed<T>(dv), int32_t(q_tiles)};
+                        typed<const T>(k), typed<const T>(v), lse, delta, delta + size_t(rows) * size_t(heads), typed<T>(dq), typed<T>(dk), typed<T>(dv), int32_t(q_tiles),
+                        parts > 1 ? delta + 2 * size_t(rows) * size_t(heads) : nullptr};
         auto go = [&](auto nd, auto is_wide) {
             constexpr int ND = decltype(nd)::value, D = ND <= 2 ? 64 : 128;
             constexpr bool WIDE = decltype(is_wide)::value;
             if (rows > 0) {
                 k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
-                k_attend_dq<T, ND, WIDE><<<uint32_t(q_tiles * kv_heads), 256, 4 * DQ_STEP * D * 2 + 16, s>>>(a);
+                auto queries = [&](auto kg) {
+                    constexpr int KG = decltype(kg)::value;
+                    k_attend_dq<T, ND, WIDE, KG><<<uint32_t(q_tiles * kv_heads), 256, 4 * KG * DQ_STEP * D * 2 + 16, s>>>(a);
+                };
+                if (sides == 4) queries(std::integral_constant<int, 4>());
+                else if (sides == 2) queries(std::integral_constant<int, 2>());
+                else queries(std::integral_constant<int, 1>());
             }
             auto keys = [&](auto rg) {
                 constexpr int RG = decltype(rg)::value, STEP = 32 * RG;
-                k_attend_dkv<T, ND, WIDE, RG><<<uint32_t(k_tiles * kv_heads), 128 * RG, 4 * STEP * D * 2 + 16 * STEP + 16, s>>>(a);
+                k_attend_dkv<T, ND, WIDE, RG><<<dim3(uint32_t(k_tiles * kv_heads), parts), 128 * RG, 4 * STEP * D * 2 + 16 * STEP + 16, s>>>(a);
             };
             if (k_rows > 0) {
                 // long sequences of few workgroups: what the longest takes counts (5 sequences up to 2801, 5 heads of keys: 618 us for 657, all gradients; 9 up
                 // to 1025, 12 heads: 128 for 121)
-                if (rows > 96 * int64_t(sequences) && k_tiles * kv_heads <= 768) keys(std::integral_constant<int, 4>());
+                if (rows > 96 * int64_t(sequences) && k_tiles * kv_heads * parts <= 768) keys(std::integral_constant<int, 4>());
                 else keys(std::integral_constant<int, 2>());
+                if (parts > 1) k_add<T><<<workgroups((int64_t(k_rows) * kv_heads + 3) / 4), 256, 0, s>>>(a, parts);
             }
         };
         auto by = [&](auto nd) {

@@ -84,6 +84,22 @@ def test_heads_that_share(heads, kv):
     backward(p, True)
 
 
+# Few workgroups: their wavefronts share rows' keys, four or two of them; more: none do.  Short sequences, and few heads that share keys or many, have kernels
+# of their own in the gradients of keys.
+EVERY = [("one wavefront to a row", [(700, 700), (300, 300), (520, 600), (64, 64), (33, 1)], 16, 16), ("two", [(700, 700), (300, 300), (520, 600), (64, 64), (33, 1)], 8, 8),
+         ("four", [(450, 450), (129, 300)], 2, 2), ("short ones", [(90, 90)] * 21 + [(5, 200), (70, 3)], 8, 2), ("many heads to one", [(260, 260), (31, 64)], 16, 1),
+         ("five heads to one", [(130, 131), (64, 64)], 10, 2)]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F16, 64), (BF16, 96), (F16, 88)])
+@pytest.mark.parametrize("name,lengths,heads,kv", EVERY, ids=[e[0] for e in EVERY])
+def test_every_kernel(name, lengths, heads, kv, dtype, d, causal):
+    p = packed(lengths, heads, kv, d, dtype, seed=17)
+    forward(p, causal)
+    backward(p, causal)
+
+
 @pytest.mark.parametrize("scale", [1e-3, 0.5, 4.0])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_scales(scale, dtype):
@@ -109,6 +125,34 @@ def test_scores_that_grow_and_are_far_apart():
         forward(p, False)
         forward(p, True)
         backward(p, True)
+
+
+@pytest.mark.parametrize("heads,kv", [(4, 2), (16, 8), (32, 16), (3, 3)])
+@pytest.mark.parametrize("bad", [math.nan, -math.inf])
+def test_what_the_mask_hides_does_not_show_in_any_kernel(bad, heads, kv):
+    """As below, with more workgroups: 150 rows and 20 short sequences."""
+    m, d = 150, 128
+    lengths = [(m, m)] + [(30, 30)] * 20
+    for at in (70, 149):
+        clean, p = (packed(lengths, heads, kv, d, BF16, seed=5) for _ in range(2))
+        p["k"][at], p["v"][at] = bad, bad
+        for x in (clean, p):
+            B.csr5_attention(x["q"], x["k"], x["v"], x["qo"], x["ko"], x["out"], lse=x["lse"])
+        other = [i for i in range(m + 600) if not at <= i < m]
+        assert torch.equal(p["out"][other], clean["out"][other]) and torch.equal(p["lse"][:, other], clean["lse"][:, other])
+        grads = []
+        for x, k, q in ((clean, clean["k"], clean["q"]), (clean, p["k"], clean["q"]), (clean, clean["k"], clean["q"].clone())):
+            if len(grads) == 2:
+                q[at] = bad
+            dout = A.heads(torch.Generator().manual_seed(9), x["rows"], heads, d, BF16)
+            dq, dk, dv = (A.heads(x["gen"], r, h, d, BF16, fill=0.0) for r, h in ((x["rows"], heads), (x["k_rows"], kv), (x["k_rows"], kv)))
+            space = torch.full((B.csr5_attention_backward_workspace_bytes(x["rows"], heads),), 255, dtype=torch.uint8, device=DEV)
+            B.csr5_attention_backward(dout, q, k, x["v"], x["out"], x["lse"], x["qo"], x["ko"], dq, dk, dv, space)
+            grads.append((dq, dk, dv))
+        (dq, dk, dv), (eq, ek, ev), (fq, fk, fv) = grads
+        assert torch.equal(dq[other], eq[other]) and not bool(torch.isfinite(eq[at:m].float()).any())          # a key: the rows before it, and other sequences
+        keys = [i for i in range(m + 600) if not (i <= at)]
+        assert torch.equal(dk[keys], fk[keys]) and torch.equal(dv[keys], fv[keys]) and not bool(torch.isfinite(fk[:at + 1].float()).any())      # a query: the keys after it
 
 
 @pytest.mark.parametrize("d", [64, 80, 128])

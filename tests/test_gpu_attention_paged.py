@@ -61,6 +61,14 @@ def test_sizes_of_heads_and_strides(d, layout):
     check(batch([(1, 70), (70, 130), (1, 3)], 6, 3, d, F16 if d % 2 else BF16, 8, layout, seed=d))
 
 
+@pytest.mark.parametrize("heads,kv", [(16, 16), (8, 8), (4, 2)])
+@pytest.mark.parametrize("page", [1, 16, 64])
+def test_chunks_by_every_kernel(page, heads, kv):
+    """One, two or four wavefronts to a row, pages of less than a load's rows, of some of them and of whole tiles; the keys split and not."""
+    check(batch([(500, 900), (1, 700), (300, 300), (129, 1500), (64, 64)], heads, kv, 128, BF16, page, seed=9))
+    check(batch([(260, 400), (1, 70), (300, 300)], heads, kv, 64, F16, page, seed=10))
+
+
 @pytest.mark.parametrize("width", [40, 400, 5000])
 def test_tables_much_wider_than_the_histories(width):
     check(batch([(1, 600), (4, 130), (1, 0), (1, 1), (2, 639)], 16, 2, 64, BF16, 16, seed=1, width=width))
