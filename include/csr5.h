@@ -592,7 +592,7 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void *h, int
  * What section 5 says of streams, graphs, sums in 32 bits, timing and addresses holds here.  A
  * row has `heads` heads of d neighbouring values, at any strides (in elements); query head h
  * goes with head h / (heads / kv_heads) of keys and values.  16-byte aligned addresses, strides of a
- * multiple of 16 bytes and d in whole 16 bytes get the fast kernels (attention: the fastest loads with d of 64, 96 or 128).  An output must not overlap itself
+ * multiple of 16 bytes and d in whole 16 bytes get the fast kernels.  An output must not overlap itself
  * (CSR5_EINVAL).  Offsets are clamped to [0, rows] and lengths to what the table holds; a page outside
  * [0, pages) is one of zeros where it is read, and none where it would be written.
  * ========================================================================== */

@@ -193,6 +193,10 @@ template <typename T, typename KV, int ND, bool WIDE, int KG> __global__ __launc
             for (int dt = 0; dt < ND; dt++) o[dt] = product32(read.template turned<T>((2 + NOW) * TILE + k * 16 * D * 2, dt), p[k], o[dt]);
         __builtin_amdgcn_s_setprio(0);
     };
+    if (bring.ragged) {
+        zeros_to(lds0, 4 * TILE, threadIdx.x, 256);
+        landed<0>();
+    }
     if (begin < end) {
         bring.look(kv, begin, ahead);
         bring(kv, begin, ahead, a.d, lds0, lds0 + 2 * TILE);
@@ -294,6 +298,10 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
 #pragma unroll
     for (int b = 0; b < RB; b++) base[b] = -INFINITY, sum[b] = 0.f;
     const int32_t start = begin + wave * FEW_KEYS;
+    if (bring.ragged) {
+        zeros_to(lds0, 2 * TILE, lane, 64);
+        own_read();
+    }
     if (start < end) {
         bring.look(kv, start, ahead);
         bring(kv, start, ahead, a.d, lds0, lds0 + TILE);

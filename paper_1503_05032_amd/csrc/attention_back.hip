@@ -148,6 +148,10 @@ template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(25
 #pragma unroll
             for (int dt = 0; dt < ND; dt++) dq[dt] = product32(read.template turned<T>(NOW * TILE + k * 16 * D * 2, dt), ds[k], dq[dt]);
     };
+    if (bring.ragged) {
+        zeros_to(lds0, 4 * TILE, threadIdx.x, 256);
+        landed<0>();
+    }
     if (end > 0) bring(kv, 0, none, a.d, lds0, lds0 + 2 * TILE);
     for (int32_t j0 = 0; j0 < end; j0 += 2 * KEYS) {
         tile(std::integral_constant<int, 0>(), j0);
@@ -242,6 +246,10 @@ template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(12
         load(h, i1, to);
         if ((i1 += DKV_STEP) >= m) i1 = start, h++;
     };
+    if (bring.ragged) {
+        zeros_to(lds0, 2 * STAGE, threadIdx.x, 128 * RG);
+        landed<0>();
+    }
     if (total > 0) load_next(lds0);
     int now = 0;
     int32_t i0 = start;

@@ -223,8 +223,15 @@ template <bool WIDE, typename T> __device__ __forceinline__ void chunk_to_lds(co
     else *(__attribute__((address_space(3))) u32x4*)uintptr_t(to + (threadIdx.x & 63) * 16) = __builtin_bit_cast(u32x4, eight_values<false>(from, from ? have : 0));
 }
 
+// Zeros to `bytes` of LDS, by `lanes` lanes of which this is one.
+__device__ __forceinline__ void zeros_to(uint32_t at, int bytes, int lane, int lanes) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    for (int i = lane * 16; i < bytes; i += lanes * 16) *(__attribute__((address_space(3))) u32x4*)uintptr_t(at + i) = u32x4{0, 0, 0, 0};
+}
+
 // A tile of keys and one of values (or of any two arrays with the same rows) into LDS by WAVES wavefronts, each LOADS times a load of EACH rows of both: where
-// they lie side by side from one address on, that and one offset of each lane serve a load; else each lane looks for its row.
+// they lie side by side from one address on, that and one offset of each lane serve a load; else each lane looks for its row (heads of 80 over pages of 16,
+// 32 single tokens over 4000 to 8000: 262 us so, 135 by offsets).
 template <typename T, int D, bool WIDE, bool SMALL, int ROWS, int WAVES> struct Bring {
     static constexpr int LANES = D / 8, EACH = 64 / LANES;      // lanes of a row, rows of a load
     static constexpr int LOADS = ROWS / EACH / WAVES;
@@ -233,12 +240,14 @@ template <typename T, int D, bool WIDE, bool SMALL, int ROWS, int WAVES> struct 
     int wave, row;                                  // this lane's row of a load
     int chunk[KINDS];
     uint32_t k_off[LOADS], v_off[LOADS];            // in bytes: packed, from the tile's first row; else from the load's
-    bool near;                                      // every lane's chunk is in the row, and no offset passes 32 bits
+    bool near;                                      // 16-byte rows, and no offset passes 32 bits
+    bool ragged;                                    // lanes whose chunk is beside the row, but is read, ask for nothing: their place has zeros from the beginning
     template <typename One> __device__ __forceinline__ Bring(const One& kv, int wave, int d) : wave(wave) {
         const int lane = threadIdx.x & 63;
         row = lane / LANES;
-        // where d ends within a chunk that is read, or beside it, there are zeros to be had; a chunk that is not read may be another one
-        near = WIDE && (d == D || (D == 128 && d == 96)) && (ROWS * kv.k_row | ROWS * kv.v_row) < (1 << 28);
+        // a chunk that is not read may be another one
+        ragged = d != D && !(D == 128 && d == 96);
+        near = WIDE && (ROWS * kv.k_row | ROWS * kv.v_row) < (1 << 28);
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
             const int r = (i * WAVES + wave) * EACH + row, from = One::PACKED ? r : row;
@@ -259,6 +268,7 @@ template <typename T, int D, bool WIDE, bool SMALL, int ROWS, int WAVES> struct 
             const T *const from = kv.key(j0, ahead[0]), *const of = kv.value(j0, ahead[0]);
 #pragma unroll
             for (int i = 0; i < LOADS; i++) {
+                if (ragged && chunk[i % KINDS] >= d) continue;
                 to_lds_at(from, k_off[i], k + (i * WAVES + wave) * 1024);
                 to_lds_at(of, v_off[i], v + (i * WAVES + wave) * 1024);
             }
@@ -269,6 +279,7 @@ template <typename T, int D, bool WIDE, bool SMALL, int ROWS, int WAVES> struct 
             const int32_t j = j0 + (i * WAVES + wave) * EACH;
             const uint32_t to = (i * WAVES + wave) * 1024;
             if (!One::PACKED && whole && kv.template together<EACH>(ahead[i])) {
+                if (ragged && chunk[i % KINDS] >= d) continue;
                 to_lds_at(kv.key(j, ahead[i]), k_off[i], k + to), to_lds_at(kv.value(j, ahead[i]), v_off[i], v + to);
             } else {
                 const bool there = j + row < kv.count;

@@ -37,11 +37,11 @@ __device__ __forceinline__ void to_lds(const void* base, uint32_t offset, const 
 }
 // To an LDS address that is the same in every lane.
 __device__ __forceinline__ void to_lds_at(const void* from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uint32_t(__builtin_amdgcn_readfirstlane(lds))), "v"(from) : "memory", "m0");
 }
 __device__ __forceinline__ void to_lds_at(const void* base, uint32_t offset, uint32_t lds) {
     const void* at;
-    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(at) : "s"(lds), "v"(offset), "s"(same(base)) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(at) : "s"(uint32_t(__builtin_amdgcn_readfirstlane(lds))), "v"(offset), "s"(same(base)) : "memory", "m0");
 }
 __device__ __forceinline__ void word_to_lds(const void* from, const void* lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(lds)), "v"(from) : "memory", "m0");
