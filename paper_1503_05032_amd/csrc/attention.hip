@@ -467,7 +467,7 @@ struct Plan {
 };
 // By the rows that a sequence has on average (the host does not know each): 64 are where few rows' kernel ends (sequences of 131 to 420 rows
 // by it 38 -> 138 us, by 32 rows to a workgroup 86).  The keys are split where there are not enough workgroups, into parts of 256 or 512 and more, for about 2048
-// of them (chunks up to 700 over 2000 to 12000 tokens: 457 us unsplit, 453 for 1024, 407 for 2048, 441 for 3072; 48 single tokens over long histories: 519 for 2048
+// of them (chunks up to 700 over 2000 to 12000 tokens: 457 us unsplit, 453 for 1024, 407 for 2048; 48 single tokens over long histories: 519 for 2048
 // and 4096, 527 for 8192; parts of 128 for 8 short ones: 23.7 against 18.6).
 Plan plan_of(int64_t rows, int64_t heads, int64_t kv_heads, int64_t sequences, int64_t most_keys, bool split) {
     const int64_t shared = kv_heads ? heads / kv_heads : 1, each = (rows + sequences - 1) / sequences * shared;
