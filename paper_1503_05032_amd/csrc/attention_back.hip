@@ -87,7 +87,7 @@ constexpr int DKV_KEYS = 64, DKV_SHIFT = 6;
 
 // ---------------------------------------------------------------------------------------------------------------
 // dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 32.
-// 5 sequences up to 2801, 20 heads of 128 with 5 of keys: 169 us, 720 TFLOP/s of its three products.
+// 5 sequences up to 2801, 20 heads of 128 with 5 of keys: 169 us, 720 TFLOP/s of its three products.  Keys are cleansed between the scores and dq's product: 1 us.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
     constexpr int D = ND <= 2 ? 64 : 128, KEYS = DQ_STEP * KG, TILE = KEYS * D * 2, ROWS = DQ_ROWS / KG;
@@ -122,27 +122,32 @@ template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(25
     auto tile = [&](auto at_place, int32_t j0) {
         constexpr int NOW = decltype(at_place)::value;
         landed<0>();
-        if (j0 + KEYS > fewest && fewest < n) {          // some row does not see some key
+        if (j0 + KEYS < end) bring(kv, j0 + KEYS, none, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
+        const int32_t mine = j0 + kg * DQ_STEP;             // this wavefront's keys
+        const bool some = mine < most;
+        vec<T, 8> ds[2];
+        if (some) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) s = product32(read.template row<T>(NOW * TILE, kk), q[kk], s);
+#pragma unroll
+            for (int kk = 0; kk < 2 * ND; kk++) dp = product32(read.template row<T>((2 + NOW) * TILE, kk), dout[kk], dp);
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[i] = power(fmaf(s[i], c, -base)) * (dp[i] - delta);
+            if (mine + DQ_STEP > least) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (mine + 8 * (i / 4) + 4 * half + i % 4));
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++) ds[i / 8][i % 8] = T(s[i]);
+        }
+        // Some row does not see some key: cleansed after the scores, which a key's values decide as they are (one of -inf may make its p 0).
+        if (j0 + KEYS > fewest && fewest < n) {
+            __syncthreads();
             if (cleanse<T>(lds + NOW * TILE, TILE, threadIdx.x, 256)) cleansed = 1;
             __syncthreads();
         }
-        if (j0 + KEYS < end) bring(kv, j0 + KEYS, none, a.d, lds0 + (1 - NOW) * TILE, lds0 + (3 - NOW) * TILE);
-        const int32_t mine = j0 + kg * DQ_STEP;             // this wavefront's keys
-        if (mine >= most) return;
-        f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int kk = 0; kk < 2 * ND; kk++) s = product32(read.template row<T>(NOW * TILE, kk), q[kk], s);
-#pragma unroll
-        for (int kk = 0; kk < 2 * ND; kk++) dp = product32(read.template row<T>((2 + NOW) * TILE, kk), dout[kk], dp);
-#pragma unroll
-        for (int i = 0; i < 16; i++) s[i] = power(fmaf(s[i], c, -base)) * (dp[i] - delta);
-        if (mine + DQ_STEP > least) {
-#pragma unroll
-            for (int i = 0; i < 16; i++) s[i] = or_zero(s[i], row.limit - 1 - (mine + 8 * (i / 4) + 4 * half + i % 4));
-        }
-        vec<T, 8> ds[2];
-#pragma unroll
-        for (int i = 0; i < 16; i++) ds[i / 8][i % 8] = T(s[i]);
+        if (!some) return;
 #pragma unroll
         for (int k = 0; k < 2; k++)
 #pragma unroll
@@ -181,7 +186,7 @@ template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(25
     if (kg > 0 || !row.there) return;
     T* const to = a.dq.p + token * a.dq.row + h * a.dq.head;
     leave<ND, WIDE>(to, dq, a.scale, a.d);
-    // a key that is not finite makes the values of dq not finite that it has so; the others are by way of lse
+    // a key that is not finite makes the values of dq not finite that it has so; the others have had it by way of the scores
     if (cleansed)
         for (int32_t j = fewest / KEYS * KEYS; j < row.limit; j++)
             for (int i = 0; i < 16 * ND; i++) {

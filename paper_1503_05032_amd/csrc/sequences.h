@@ -299,7 +299,7 @@ __device__ __forceinline__ float or_none(float x, int32_t hidden) {
 }
 
 // Where a mask hides some depth of a product from some columns, their p are 0, and a value there that is not finite must not show, as 0 * inf would.
-// So a tile with such values, seldom as they are, is cleansed of them in LDS before it is read, and what they do to the columns that do see them is
+// So a tile with such values, seldom as they are, is cleansed of them in LDS before it is read so (keys after the scores, which their values decide as they are), and what they do to the columns that do see them is
 // added to the results in the end, from memory.  (A second way through the products for such tiles would take the first one's registers: the attention of
 // 3 sequences up to 8001 took 985 us with it.)  Bytes [from, to) of this tile by lanes that have `lane` of `lanes`; whether there were some.
 template <typename T> __device__ __forceinline__ bool cleanse(uint8_t* tile, int bytes, int lane, int lanes) {
