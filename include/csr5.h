@@ -660,7 +660,8 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
  * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite.
  * Softmax statistics and sums are held in 32 bits; exp(scale q.k_j - b) is rounded to dtype before it is multiplied by v,
  * b a running base that the largest score so far passes by 8 ln 2 at most.  What a row does not see has no part in it,
- * whatever it holds; a value that is not finite where it is seen makes the result not finite.
+ * whatever it holds.  A score of -inf (of a key of -inf, say) has weight 0, and a row all of whose scores are -inf is as one that sees no
+ * key; a score that is NaN or +inf, or a value of v that is not finite, makes the result not finite where it is seen.
  */
 int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d, int dtype,
                    const int32_t *q_offset, const int32_t *k_offset, float scale, int causal, csr5_heads_t q,
@@ -672,7 +673,8 @@ int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t head
  *   dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
  * with the sums of dk and dv over the query heads that share them.  p and ds are rounded to dtype before they are multiplied (F16:
  * a ds past 65504 becomes infinite).  A query that is not finite, or whose dout is not, has a part in the gradients of the keys that it sees
- * only, and a key that is not in those of the queries that see it.
+ * only, and a key that is not in those of the queries that see it; weights of scores of -inf are 0 here too, also in a row of nothing else, and
+ * only the values of a sum with 0 times infinity are not finite then.
  * Rows in no sequence are left as they are.  workspace: csr5_attention_backward_workspace_bytes bytes, free again after the call.
  */
 size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads);

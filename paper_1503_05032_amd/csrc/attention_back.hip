@@ -26,7 +26,7 @@ template <typename T> struct Back {
     bool causal;
     Heads<const T> dout, q, out, k, v;
     const float* lse;
-    float *delta, *base;        // [heads][rows]: dout . out, and lse log2 e
+    float *delta, *base;        // [heads][rows]: dout . out, and lse log2 e (infinity where lse is -inf)
     Heads<T> dq, dk, dv;
     int32_t tiles;
     float* part;                // sums of dk, then of dv, by workgroups that have some of the heads only: [part][2][k_rows][kv_heads][d]; NULL: there are none
@@ -46,7 +46,11 @@ template <typename T, int LANES, bool WIDE> __global__ __launch_bounds__(256) vo
 #pragma unroll
     for (int e = 0; e < 8; e++) sum = fmaf(x[e], y[e], sum);
     sum = lanes_sum<LANES>(sum);
-    if (there && c == 0) a.delta[h * a.rows + row] = sum, a.base[h * a.rows + row] = a.lse[h * a.rows + row] * LOG2_E;
+    if (there && c == 0) {
+        const float lse = a.lse[h * a.rows + row];
+        // a row whose scores are all -inf: with this base its weights are 0, as in its result
+        a.delta[h * a.rows + row] = sum, a.base[h * a.rows + row] = lse == -INFINITY ? INFINITY : lse * LOG2_E;
+    }
 }
 
 // Where a wavefront reads rows of LDS for products of 32 x 32 x 16: rows as first operands (chunks 2 kk on), and turned (columns 32 dt on).  Tiles begin at
@@ -341,19 +345,22 @@ template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(12
         leave<ND, WIDE>(to_v, dv, 1.f, a.d);
     }
     if (!cleansed) return;
-    // a query that is not finite makes all of dk and dv so of the keys that it sees, a dout that is not all of dk, and the values of dv that it has so
+    // a query that is not finite makes all of dk and dv so of the keys that it sees (where its scores are all -inf: the values of dk that it has so), a dout that is not all
+    // of dk, and the values of dv that it has so
     for (int g = first_head; g < last_head; g++)
         for (int32_t i = max(start, key - ahead); i < min(m, start + (whole - start + DKV_STEP - 1) / DKV_STEP * DKV_STEP); i++) {
             const T *const q = a.q.p + (mine.first + i) * a.q.row + (hk * a.shared + g) * a.q.head, *const o = a.dout.p + (mine.first + i) * a.dout.row + (hk * a.shared + g) * a.dout.head;
             bool bad_q = false, bad_o = false;
             for (int x = 0; x < a.d; x++) bad_q = bad_q || !finite(float(q[x])), bad_o = bad_o || !finite(float(o[x]));
             if (!bad_q && !bad_o) continue;
+            const bool none = a.base[int64_t(hk * a.shared + g) * a.rows + mine.first + i] == INFINITY;      // all its weights are 0
             for (int e = 0; e < 16 * ND; e++) {
                 const int x = e / 4 * 8 + half * 4 + e % 4;
                 if (x >= a.d) continue;
-                const float more = bad_q ? NAN : finite(float(o[x])) ? 0.f : float(o[x]);
-                if (part) part[x] = NAN, part[step + x] += more;
-                else to_k[x] = T(NAN), to_v[x] = T(float(to_v[x]) + more);
+                const float of_v = bad_q && !none ? NAN : finite(float(o[x])) ? 0.f : none ? NAN : float(o[x]);
+                const float of_k = bad_o || !none || !finite(float(q[x])) ? NAN : 0.f;
+                if (part) part[x] += of_k, part[step + x] += of_v;
+                else to_k[x] = T(float(to_k[x]) + of_k), to_v[x] = T(float(to_v[x]) + of_v);
             }
         }
 }

@@ -97,3 +97,27 @@ def test_keys_with_one_value_of_minus_infinity(name, dtype, d, causal):
     assert not case.nothing
     case.check_forward(causal)
     case.check_backward(causal, [i for i in range(190) if (i >= 3 if i < 150 else i >= 160) or not causal], [])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_rows_that_see_such_keys_only(name, dtype, d, causal):
+    """The first rows under the mask, and all of a sequence: they have no part in any gradient."""
+    case = Case(name, dtype, d, 0.0, gone=[0, 1, 2, *range(150, 190)])
+    case.run(causal)
+    assert case.nothing == [*(range(3) if causal else []), *range(150, 190)]
+    case.check_forward(causal)
+    case.check_backward(causal, range(190), [])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_queries_with_one_value_of_minus_infinity(name, dtype, d, causal):
+    """All their scores are -inf, in tiles with a mask and without."""
+    case = Case(name, dtype, d, 0.5, lost=[2, 40, 101, 170])
+    case.run(causal)
+    assert case.nothing == [2, 40, 101, 170]
+    case.check_forward(causal)
+    case.check_backward(causal, [], [j for j in range(190) if (j <= 101 if j < 150 else j <= 170) or not causal])
