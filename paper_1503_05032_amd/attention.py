@@ -49,12 +49,15 @@ class Attention:
         return qkv.view(-1, self.heads + 2 * self.kv_heads, self.d).split([self.heads, self.kv_heads, self.kv_heads], dim=1)
 
     def forward(self, x, offset, position, residual=None):
-        """Causal attention within each sequence [offset[s], offset[s + 1]) of x [tokens, width], and what `backward` needs; s["h"] is x + residual."""
+        """Causal attention within each sequence [offset[s], offset[s + 1]) of x [tokens, width], and what `backward` needs; s["h"] is x + residual.
+        Tokens in no sequence (before offset[0], or behind the last) get z = 0 and, in `backward`, the gradient of h alone; they have no part in the parameters'."""
         s = self._queries(x, residual)
         q, k, v = self._split(s["qkv"])
         B.csr5_rotary(q, k, position, self.frequency, q, k_out=k)
         tokens = x.shape[0]
-        out, lse, z = self._empty(tokens, self.heads, self.d), self._empty(self.heads, tokens, dtype=torch.float32), self._empty(tokens, self.width)
+        # the attention leaves rows in no sequence as they are, and the products go over all
+        out = torch.zeros(tokens, self.heads, self.d, dtype=self.dtype, device=x.device)
+        lse, z = self._empty(self.heads, tokens, dtype=torch.float32), self._empty(tokens, self.width)
         B.csr5_attention(q, k, v, offset, offset, out, lse=lse)
         B.csr5_grouped_gemm(out.view(tokens, -1), self.back, s["rows"], z)
         s.update(offset=offset, position=position, out=out, lse=lse)
@@ -66,7 +69,7 @@ class Attention:
         dout, dback = self._empty(tokens, self.heads * self.d), torch.empty_like(self.back)
         B.csr5_grouped_gemm_dx(dz, self.back, s["rows"], dout)
         B.csr5_grouped_gemm_dw(dz, s["out"].view(tokens, -1), s["rows"], dback)
-        dqkv = torch.empty_like(s["qkv"])
+        dqkv = torch.zeros_like(s["qkv"])                   # as `out`
         (q, k, v), (dq, dk, dv) = self._split(s["qkv"]), self._split(dqkv)
         space = self._empty(B.csr5_attention_backward_workspace_bytes(tokens, self.heads), dtype=torch.uint8)
         B.csr5_attention_backward(dout.view(tokens, self.heads, self.d), q, k, v, s["out"], s["lse"], s["offset"], s["offset"], dq, dk, dv, space)

@@ -133,3 +133,38 @@ def test_training_runs():
     make = lambda: (Attention(width=128, heads=4, kv_heads=2, d=32, generator=g), Layer(width=128, inner=64, experts=4, k=2, generator=g))  # noqa: E731
     losses = train(make(), make(), steps=3, tokens=60, generator=g)
     assert len(losses) == 3 and all(loss == loss and loss < float("inf") for loss in losses)
+
+
+@pytest.fixture
+def filled_memory():
+    """What torch allocates is NaN (whole numbers: the largest) until it is written."""
+    before = torch.are_deterministic_algorithms_enabled(), torch.utils.deterministic.fill_uninitialized_memory
+    torch.use_deterministic_algorithms(True, warn_only=True)
+    torch.utils.deterministic.fill_uninitialized_memory = True
+    yield
+    torch.use_deterministic_algorithms(before[0])
+    torch.utils.deterministic.fill_uninitialized_memory = before[1]
+
+
+@pytest.mark.parametrize("before,behind", [(0, 9), (5, 0), (7, 70)])
+def test_tokens_in_no_sequence(before, behind, filled_memory):
+    """A padded batch: such tokens' z is 0, the gradient of x is that of h, and the parameters' gradients are those of the sequences alone."""
+    g = torch.Generator().manual_seed(6)
+    lengths = [40, 1, 77]
+    a = Attention(width=256, heads=4, kv_heads=2, d=64, generator=g)
+    offset, position = packed(lengths)
+    tokens = before + sum(lengths) + behind
+    x, residual, dz, dh = (torch.randn(tokens, 256, generator=g).to(DEV, a.dtype) for _ in range(4))
+    inside = slice(before, before + sum(lengths))
+    at = torch.zeros(tokens, dtype=torch.int32, device=DEV)
+    at[inside] = position
+    z, s = a.forward(x, offset + before, at, residual)
+    dx, grads = a.backward(dz, s, dh)
+    want, h, xs, rs, p = plain(a, x[inside], residual[inside], lengths)
+    (want * dz[inside].double().cpu()).sum().add((h * dh[inside].double().cpu()).sum()).backward()
+    near(z[inside], want.detach(), "z")
+    near(dx[inside], xs.grad, "dx")
+    for name, got in grads.items():
+        near(got, p[name].grad, name)
+    for rows in (slice(0, before), slice(before + sum(lengths), tokens)):
+        assert bool((z[rows] == 0).all()) and torch.equal(dx[rows], dh[rows])
