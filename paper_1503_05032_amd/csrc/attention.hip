@@ -33,6 +33,8 @@ template <typename T, typename KV> struct Attend {
 
 // The base rises where a score passes it by more than this many powers of two: sums are rescaled seldom, and p is at most 256.
 constexpr float RISE = 8.f;
+// The same in scores; finite (the smallest scales would make it infinite), so that the first score, from a base of -inf, passes it.
+__device__ __forceinline__ float rise_of(float c) { return fminf(RISE / c, 0x1.fffffep127f); }
 
 __device__ __forceinline__ float half_most(float v) {       // over lanes l and l ^ 32
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -141,7 +143,7 @@ template <typename T, typename KV, int ND, bool WIDE, int KG> __global__ __launc
     typename decltype(kv)::Ahead ahead[B::LOADS];
     const ReadFixed<ND> read(lds0 + kg * MANY_KEYS * D * 2);      // its 32 keys of a tile
 
-    const float c = a.scale * LOG2_E, rise = RISE / c;
+    const float c = a.scale * LOG2_E, rise = rise_of(c);
     float base = -INFINITY, sum = 0.f;
     f32x16 o[ND] = {};
     auto tile = [&](auto at_place, int32_t j0) {
@@ -292,7 +294,7 @@ template <typename T, typename KV, int ND, bool WIDE, int RB> __global__ __launc
 #pragma unroll
     for (int dt = 0; dt < 2 * ND; dt++) v_at[dt] = TILE + vr * D * 2 + chunk_at<D, true>(vr, dt * 2 + ((li & 3) >> 1)) * 16 + (li & 1) * 8;
 
-    const float c = a.scale * LOG2_E, rise = RISE / c;
+    const float c = a.scale * LOG2_E, rise = rise_of(c);
     float base[RB], sum[RB];
     f32x4 o[RB][2 * ND] = {};
 #pragma unroll

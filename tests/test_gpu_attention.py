@@ -303,3 +303,12 @@ def test_nothing_to_do():
     B.csr5_attention_backward(e(0, 4, 64), e(0, 4, 64), e(6, 2, 64), e(6, 2, 64), e(0, 4, 64), e(4, 0, dtype=torch.float32), two[:2], torch.tensor([0, 6], dtype=torch.int32, device=DEV),
                               e(0, 4, 64), dk, dv, None)                                     # six keys, no query
     assert bool((dk == 0).all()) and bool((dv == 0).all())
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1.5e-38, 2.0 ** -126, 2.0 ** -140, 2.0 ** -149])
+@pytest.mark.parametrize("lengths,heads,kv", [([(1, 90), (2, 400)], 4, 2), ([(150, 150)], 4, 2), ([(150, 150)] + [(40, 40)] * 20, 8, 8), ([(150, 150)] + [(40, 40)] * 20, 32, 16)])
+def test_the_smallest_scales(lengths, heads, kv, scale):
+    """Scores that are all but 0 in units of which 8 powers of two are past the largest number: means of the values."""
+    p = packed(lengths, heads, kv, 64, BF16, seed=12)
+    forward(p, True, scale)
+    backward(p, True, scale=scale)

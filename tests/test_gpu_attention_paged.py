@@ -171,3 +171,13 @@ def test_another_stream_twice_the_same_and_replayed():
         for x, (out, lse) in zip((p, q), want):
             end = int(x["qo"][-1])
             assert torch.equal(x["out"][:end], out[:end]) and torch.equal(x["lse"][:, :end], lse[:, :end])
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** -126, 2.0 ** -149])
+@pytest.mark.parametrize("lengths", [[(1, 1500), (3, 700), (1, 1)], [(300, 1500), (100, 100)]])
+def test_the_smallest_scales(lengths, scale):
+    """Scores of which 8 powers of two are past the largest number, with the keys split."""
+    p = batch(lengths, 8, 4, 64, BF16, 16, seed=12)
+    assert space(p).numel() > 0
+    call(p, scale=scale)
+    A.check_forward(p["q"], p["k"], p["v"], A.sequences(p["qo"]), p["spans"], p["out"], p["lse"], scale, True)
