@@ -657,7 +657,8 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
  * no key has out 0 and lse -inf.  Rows in no sequence are left as they are.
  *   q, out [rows][heads][d]; k, v [k_rows][kv_heads][d] in dtype (BF16, F16); lse float[heads][rows], or NULL
  * d <= CSR5_ATTENTION_MAX_D, heads <= CSR5_ATTENTION_MAX_HEADS, rows and k_rows <= CSR5_ATTENTION_MAX_ROWS, else
- * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite.
+ * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite, also times log2 e (else CSR5_EINVAL): scores are held times
+ * log2 e in 32 bits, and one past 2^128 is infinite.
  * Softmax statistics and sums are held in 32 bits; exp(scale q.k_j - b) is rounded to dtype before it is multiplied by v,
  * b a running base that the largest score so far passes by 8 ln 2 at most.  What a row does not see has no part in it,
  * whatever it holds.  A score of -inf (of a key of -inf, say) has weight 0, and a row all of whose scores are -inf is as one that sees no

@@ -164,3 +164,15 @@ def test_scale_is_a_number(lib):
     here = tensors(**shapes)
     with pytest.raises(ValueError, match="scale"):
         run("csr5_attention", here, {"scale": "much"})
+
+
+def test_scales_past_the_range_of_scores(lib):
+    """Scores are held times log2 e: a scale that is past 2^128 in that is refused."""
+    K = B.Heads(P, 256, 128)
+    top = 2.0 ** 128 * (1 - 2.0 ** -24)
+    past, below = top / 1.4426, top / 1.4427
+    assert lib.csr5_attention(2, 3, 5, 4, 2, 128, B.CSR5_DTYPE_BF16, P, P, past, 1, H, K, K, H, P, None) == B.CSR5_EINVAL
+    assert lib.csr5_attention(0, 3, 5, 4, 2, 128, B.CSR5_DTYPE_BF16, P, P, below, 1, H, K, K, H, P, None) == B.CSR5_OK
+    assert lib.csr5_attention_backward(2, 3, 5, 4, 2, 128, B.CSR5_DTYPE_F16, P, P, past, 1, H, H, K, K, H, P, H, K, K, P, 1 << 20, None) == B.CSR5_EINVAL
+    cache = B.Cache(P, 4096, 256, 128)
+    assert lib.csr5_attention_paged(2, 3, 4, 2, 128, B.CSR5_DTYPE_BF16, P, P, P, 6, 6, 9, 16, past, H, cache, cache, H, P, None, 0, None) == B.CSR5_EINVAL
