@@ -656,7 +656,7 @@ int csr5_rotary(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int3
  * over all its keys, or with causal != 0 those j <= i + n - m (the last query sees every key).  A row that sees
  * no key has out 0 and lse -inf.  Rows in no sequence are left as they are.
  *   q, out [rows][heads][d]; k, v [k_rows][kv_heads][d] in dtype (BF16, F16); lse float[heads][rows], or NULL
- * d <= CSR5_ATTENTION_MAX_D, heads <= CSR5_ATTENTION_MAX_HEADS, rows and k_rows <= CSR5_ATTENTION_MAX_ROWS, else
+ * d <= CSR5_ATTENTION_MAX_D, heads and kv_heads <= CSR5_ATTENTION_MAX_HEADS, rows and k_rows <= CSR5_ATTENTION_MAX_ROWS, else
  * CSR5_ERANGE; heads is a multiple of kv_heads, scale positive and finite, also times log2 e (else CSR5_EINVAL): scores are held times
  * log2 e in 32 bits, and one past 2^128 is infinite.
  * Softmax statistics and sums are held in 32 bits; exp(scale q.k_j - b) is rounded to dtype before it is multiplied by v,
@@ -676,7 +676,7 @@ int csr5_attention(int32_t sequences, int32_t rows, int32_t k_rows, int32_t head
  * a ds past 65504 becomes infinite).  A query that is not finite, or whose dout is not, has a part in the gradients of the keys that it sees
  * only, and a key that is not in those of the queries that see it; weights of scores of -inf are 0 here too, also in a row of nothing else, and
  * only the values of a sum with 0 times infinity are not finite then.
- * Rows in no sequence are left as they are.  workspace: csr5_attention_backward_workspace_bytes bytes, free again after the call.
+ * Rows in no sequence are left as they are; without queries (rows or heads 0) dk and dv are 0.  workspace: csr5_attention_backward_workspace_bytes bytes, free again after the call.
  */
 size_t csr5_attention_backward_workspace_bytes(int32_t rows, int32_t heads);
 int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int32_t heads, int32_t kv_heads, int32_t d,

@@ -411,15 +411,16 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
         !heads_ok(dout, rows, heads, d, 2) || !output_ok(dq, rows, heads, d, 2) || !output_ok(dk, k_rows, kv_heads, d, 2) || !output_ok(dv, k_rows, kv_heads, d, 2))
         return CSR5_EINVAL;
     if (!words({q_offset, k_offset, lse, workspace})) return CSR5_EINVAL;
-    if (sequences == 0 || heads == 0 || d == 0 || (rows == 0 && k_rows == 0)) return CSR5_OK;
-    if (!q_offset || !k_offset || (rows > 0 && !lse)) return CSR5_EINVAL;
-    if (rows > 0 && (!workspace || workspace_bytes < csr5_attention_backward_workspace_bytes(rows, heads))) return CSR5_ENOMEM;
+    if (sequences == 0 || kv_heads == 0 || d == 0 || (rows == 0 && k_rows == 0)) return CSR5_OK;
+    const bool queries_there = rows > 0 && heads > 0;        // without them dk and dv are 0
+    if (!q_offset || !k_offset || (queries_there && !lse)) return CSR5_EINVAL;
+    if (queries_there && (!workspace || workspace_bytes < csr5_attention_backward_workspace_bytes(rows, heads))) return CSR5_ENOMEM;
     const int64_t wide_tiles = tiles_at_most(sequences, rows, heads / kv_heads, DQ_SHIFT);
     const int sides = sides_of(wide_tiles * kv_heads);
     const int64_t q_tiles = tiles_at_most(sequences, rows, heads / kv_heads, sides == 1 ? DQ_SHIFT : sides == 2 ? DQ_SHIFT - 1 : DQ_SHIFT - 2), k_tiles = tiles_at_most(sequences, k_rows, 1, DKV_SHIFT);
     if (q_tiles * kv_heads * 256 > UINT32_MAX || k_tiles * kv_heads * 256 > UINT32_MAX) return CSR5_ERANGE;
     const size_t room = csr5_attention_backward_workspace_bytes(rows, heads) - size_t(rows) * size_t(heads) * 8;
-    const int parts = rows == 0 ? 1 : parts_of(k_tiles * kv_heads, heads / kv_heads, int64_t(k_rows) * kv_heads * d, room);
+    const int parts = !queries_there ? 1 : parts_of(k_tiles * kv_heads, heads / kv_heads, int64_t(k_rows) * kv_heads * d, room);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const bool w = d % 8 == 0 && wide(q, 2) && wide(k, 2) && wide(v, 2) && wide(out, 2) && wide(dout, 2) && wide(dq, 2) && wide(dk, 2) && wide(dv, 2);
     return with_half(dtype, [&](auto zero) {
@@ -431,7 +432,7 @@ int csr5_attention_backward(int32_t sequences, int32_t rows, int32_t k_rows, int
         auto go = [&](auto nd, auto is_wide) {
             constexpr int ND = decltype(nd)::value, D = ND <= 2 ? 64 : 128;
             constexpr bool WIDE = decltype(is_wide)::value;
-            if (rows > 0) {
+            if (queries_there) {
                 k_delta<T, D / 8, WIDE><<<workgroups((int64_t(rows) * heads + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
                 auto queries = [&](auto kg) {
                     constexpr int KG = decltype(kg)::value;

@@ -327,7 +327,7 @@ inline int attention_sizes(int32_t sequences, int32_t rows, int32_t k_rows, int3
     if ((dtype != CSR5_DTYPE_BF16 && dtype != CSR5_DTYPE_F16) || sequences < 0 || rows < 0 || k_rows < 0 || heads < 0 || kv_heads < 0 || d < 0) return CSR5_EINVAL;
     if (kv_heads == 0 ? heads != 0 : heads % kv_heads != 0) return CSR5_EINVAL;
     if (!(scale > 0.f) || !std::isfinite(scale * LOG2_E)) return CSR5_EINVAL;       // infinite, it would make a score of 0 NaN
-    if (sequences > MOST_SIZE || rows > CSR5_ATTENTION_MAX_ROWS || k_rows > CSR5_ATTENTION_MAX_ROWS || heads > CSR5_ATTENTION_MAX_HEADS || d > CSR5_ATTENTION_MAX_D) return CSR5_ERANGE;
+    if (sequences > MOST_SIZE || rows > CSR5_ATTENTION_MAX_ROWS || k_rows > CSR5_ATTENTION_MAX_ROWS || heads > CSR5_ATTENTION_MAX_HEADS || kv_heads > CSR5_ATTENTION_MAX_HEADS || d > CSR5_ATTENTION_MAX_D) return CSR5_ERANGE;
     return CSR5_OK;
 }
 inline bool words(std::initializer_list<const void*> all) {

@@ -176,3 +176,9 @@ def test_scales_past_the_range_of_scores(lib):
     assert lib.csr5_attention_backward(2, 3, 5, 4, 2, 128, B.CSR5_DTYPE_F16, P, P, past, 1, H, H, K, K, H, P, H, K, K, P, 1 << 20, None) == B.CSR5_EINVAL
     cache = B.Cache(P, 4096, 256, 128)
     assert lib.csr5_attention_paged(2, 3, 4, 2, 128, B.CSR5_DTYPE_BF16, P, P, P, 6, 6, 9, 16, past, H, cache, cache, H, P, None, 0, None) == B.CSR5_EINVAL
+
+
+def test_heads_of_keys_without_queries(lib):
+    K, N = B.Heads(P, 256, 128), B.Heads(None, 0, 0)
+    back = lambda n, kv, ko=P, dk=K: lib.csr5_attention_backward(n, 3, 5, 0, kv, 128, B.CSR5_DTYPE_F16, P, ko, 0.1, 1, N, N, K, K, N, None, N, dk, K, None, 0, None)  # noqa: E731
+    assert back(0, 2) == B.CSR5_OK and back(2, 2, ko=None) == B.CSR5_EINVAL and back(2, 2, dk=N) == B.CSR5_EINVAL and back(2, 65536, dk=B.Heads(P, 2 ** 24, 128)) == B.CSR5_ERANGE

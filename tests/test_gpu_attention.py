@@ -312,3 +312,14 @@ def test_the_smallest_scales(lengths, heads, kv, scale):
     p = packed(lengths, heads, kv, 64, BF16, seed=12)
     forward(p, True, scale)
     backward(p, True, scale=scale)
+
+
+def test_no_query_heads():
+    """Keys that no head of queries shares have gradients of 0, as those that no query sees."""
+    e = lambda *shape, dtype=BF16: torch.empty(*shape, dtype=dtype, device=DEV)  # noqa: E731
+    dk = e(150, 2, 64).fill_(3)
+    dv = dk.clone()
+    offset, k_offset = torch.tensor([0, 5, 7], dtype=torch.int32, device=DEV), torch.tensor([0, 90, 140], dtype=torch.int32, device=DEV)
+    none = e(7, 0, 64)
+    B.csr5_attention_backward(none, none, e(150, 2, 64), e(150, 2, 64), none, e(0, 7, dtype=torch.float32), offset, k_offset, none, dk, dv, None)
+    assert bool((dk[:140] == 0).all()) and bool((dv[:140] == 0).all()) and bool((dk[140:] == 3).all()) and bool((dv[140:] == 3).all())
