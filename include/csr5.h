@@ -593,7 +593,7 @@ int csr5_rmsnorm_backward(int32_t rows, int32_t n, int dtype, const void *h, int
  * row has `heads` heads of d neighbouring values, at any strides (in elements); query head h
  * goes with head h / (heads / kv_heads) of keys and values.  16-byte aligned addresses, strides of a
  * multiple of 16 bytes and d in whole 16 bytes get the fast kernels.  An output must not overlap itself
- * (CSR5_EINVAL).  Offsets are clamped to [0, rows] and lengths to what the table holds; a page outside
+ * (CSR5_EINVAL), nor another array of the call unless a comment says that it may.  Offsets are clamped to [0, rows] and lengths to what the table holds; a page outside
  * [0, pages) is one of zeros where it is read, and none where it would be written.
  * ========================================================================== */
 #define CSR5_ATTENTION_MAX_D 128
@@ -625,8 +625,8 @@ typedef struct { /* value c of head h of token i of a page is at p[number*page +
  * written into table, whose other entries stay.  The pages of a request that is over go behind the last free one, for later
  * calls; its row of the table stays.  tokens: room in position and slot; of more new tokens than that the first are
  * written, and offset ends at tokens.  page is a power of two, and width * page is below
- * 2^31, as is the number of requests and of tokens (else CSR5_ERANGE).  pool and table are the only arrays that are read and written; with
- * the same state a call gives the same again.  A length below 0 is 0, one past the table its width.
+ * 2^31, as is the number of requests and of tokens (else CSR5_ERANGE).  pool and table are the only arrays that are read and written, and no
+ * array that is written may share a word with another one of the call (CSR5_EINVAL); with the same state a call gives the same again.  A length below 0 is 0, one past the table its width.
  */
 int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int32_t tokens, const int32_t *fresh,
                const int32_t *length, int32_t *table, int64_t ldt, int32_t *pool, const int32_t *state, int32_t *offset,

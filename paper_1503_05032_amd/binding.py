@@ -655,7 +655,7 @@ def csr5_pages(fresh, length, table, pool, state, page, offset, position, slot, 
     """The pages of a step of serving.  From fresh (new tokens; below 0: over) and length (cached ones) [requests], writes
     offset [requests + 1], position and slot [tokens], length_out [requests] and state_out [2], new pages into table
     [requests, width], and pages of requests that are over into the ring `pool`, whose free ones state [2] (first, count)
-    names; all int32.  `page` tokens to a page, a power of two."""
+    names; all int32, and none that is written a part of another.  `page` tokens to a page, a power of two."""
     return _chk(_native().pages(fresh, length, table, pool, state, page, offset, position, slot, length_out, state_out, stream), "csr5_pages", check)
 
 

@@ -331,6 +331,23 @@ template <typename T, bool INTERLEAVED, int TOKENS> __global__ __launch_bounds__
     }
 }
 
+// Arrays of whole numbers of 32 bits: `rows` of `words`, ld apart.
+struct Words {
+    const void* p;
+    int64_t words, rows = 1, ld = 0;
+};
+// Whether a, of one row, has a word that b has too.
+bool share_words(const Words& a, const Words& b) {
+    if (a.words == 0 || b.words == 0 || b.rows == 0) return false;
+    const uint64_t from = reinterpret_cast<uintptr_t>(a.p), to = from + uint64_t(a.words) * 4, first = reinterpret_cast<uintptr_t>(b.p), row_bytes = uint64_t(b.words) * 4;
+    if (to <= first) return false;
+    const uint64_t begin = from > first ? from - first : 0, end = to - first;
+    if (b.rows == 1) return begin < row_bytes;
+    const uint64_t pitch = uint64_t(b.ld < (int64_t(1) << 60) ? b.ld : int64_t(1) << 60) * 4, row = begin / pitch;
+    if (row >= uint64_t(b.rows)) return false;
+    return begin - row * pitch < row_bytes || (row + 1 < uint64_t(b.rows) && end > (row + 1) * pitch);         // in the row, or as far as the next
+}
+
 }  // namespace
 
 extern "C" {
@@ -344,6 +361,15 @@ int csr5_pages(int32_t requests, int32_t width, int32_t ring, int32_t page, int3
     for (const void* p : {static_cast<const void*>(fresh), static_cast<const void*>(length), static_cast<const void*>(pool), static_cast<const void*>(state), static_cast<const void*>(offset),
                           static_cast<const void*>(position), static_cast<const void*>(slot), static_cast<const void*>(length_out), static_cast<const void*>(state_out)})
         if (reinterpret_cast<uintptr_t>(p) & 3) return CSR5_EINVAL;
+    // workgroups read the inputs, in no order, while others write
+    const Words rows{table, width, requests, ldt};
+    const Words one[] = {{pool, ring}, {offset, int64_t(requests) + 1}, {position, tokens}, {slot, tokens}, {length_out, requests}, {state_out, 2}, {fresh, requests}, {length, requests}, {state, 2}};
+    constexpr int ALL = sizeof one / sizeof one[0], WRITTEN = 6;
+    for (int i = 0; i < ALL; i++) {
+        if (share_words(one[i], rows)) return CSR5_EINVAL;
+        for (int j = i + 1; j < ALL && i < WRITTEN; j++)
+            if (share_words(one[i], one[j])) return CSR5_EINVAL;
+    }
     const PagesArgs a{requests, width, ring, __builtin_ctz(page), tokens, fresh, length, table, ldt, pool, state, offset, position, slot, length_out, state_out};
     const int64_t shares = divide_up(int64_t(tokens), PAGES_SHARE);
     const int groups = int(shares < 1 ? 1 : shares > 256 ? 256 : shares) * 3;

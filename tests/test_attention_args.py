@@ -182,3 +182,22 @@ def test_heads_of_keys_without_queries(lib):
     K, N = B.Heads(P, 256, 128), B.Heads(None, 0, 0)
     back = lambda n, kv, ko=P, dk=K: lib.csr5_attention_backward(n, 3, 5, 0, kv, 128, B.CSR5_DTYPE_F16, P, ko, 0.1, 1, N, N, K, K, N, None, N, dk, K, None, 0, None)  # noqa: E731
     assert back(0, 2) == B.CSR5_OK and back(2, 2, ko=None) == B.CSR5_EINVAL and back(2, 2, dk=N) == B.CSR5_EINVAL and back(2, 65536, dk=B.Heads(P, 2 ** 24, 128)) == B.CSR5_ERANGE
+
+
+def test_pages_outputs_that_overlap(lib):
+    """No output of a step may be another array of it, or share a word with one: workgroups read the inputs while others write."""
+    sizes = dict(fresh=3, length=3, table=12, pool=8, state=2, offset=4, position=5, slot=5, length_out=3, state_out=2)
+    place, at = {}, P
+    for name, words in sizes.items():
+        place[name] = at
+        at += 4 * words
+    written = ("table", "pool", "offset", "position", "slot", "length_out", "state_out")
+
+    def rc(**over):
+        p = place | over
+        return lib.csr5_pages(3, 4, 8, 16, 5, p["fresh"], p["length"], p["table"], 4, p["pool"], p["state"], p["offset"], p["position"], p["slot"], p["length_out"], p["state_out"], None)
+    for name in written:
+        for other in sizes:
+            if other != name:
+                for shift in (0, 4 * (sizes[other] - 1), -4 * (sizes[name] - 1)):
+                    assert rc(**{name: place[other] + shift}) == B.CSR5_EINVAL, (name, other, shift)

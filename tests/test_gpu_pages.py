@@ -128,3 +128,22 @@ def test_replayed_while_requests_go_on():
         assert [t.tolist() for t in (offset, position, slot, length_out, state_out, table, pool)] == [list(w) for w in want]
         length.copy_(length_out), state.copy_(state_out)
         host = dict(length=want[3], state=want[4], table=want[5], pool=want[6])
+
+
+def test_arrays_side_by_side():
+    """All arrays of a step in one, without a word between them, and one of them between the rows of the table."""
+    rng = random.Random(77)
+    fresh, length, table, pool, state, page, tokens = serving(rng, 5, 16, 40, 90, over=0.2, slack=2.0)
+    want = step(fresh, length, table, pool, state, page, tokens)
+    n, width = len(fresh), len(table[0])
+    sizes = dict(fresh=n, slot=tokens, length=n, offset=n + 1, pool=len(pool), state_out=2, position=tokens, state=2, table=n * (width + n))
+    words = torch.full((sum(sizes.values()),), -7, dtype=torch.int32, device=DEV)
+    at = dict(zip(sizes, words.split(list(sizes.values()))))
+    wide = at["table"].view(n, width + n)
+    here = at | dict(table=wide[:, :width], length_out=wide[2, width:])
+    for name, values in dict(fresh=fresh, length=length, table=table, pool=pool, state=state).items():
+        here[name].copy_(torch.tensor(values, dtype=torch.int32))
+    B.csr5_pages(here["fresh"], here["length"], here["table"], here["pool"], here["state"], page, *(here[name] for name in ("offset", "position", "slot", "length_out", "state_out")))
+    assert [here[name].tolist() for name in ("offset", "position", "slot", "length_out", "state_out", "table", "pool")] == [list(w) for w in want]
+    assert here["fresh"].tolist() == fresh and here["length"].tolist() == length and here["state"].tolist() == state
+    assert bool((wide[[0, 1, 3, 4], width:] == -7).all())
