@@ -159,3 +159,25 @@ def paged(gen, k, v, k_spans, page, layout="plain", spare=3, width=None):
             k_cache[int(table[s, p]), :rows] = k[a + p * page:a + p * page + rows]
             v_cache[int(table[s, p]), :rows] = v[a + p * page:a + p * page + rows]
     return k_cache, v_cache, table.to(DEV), torch.tensor(lengths, dtype=torch.int32, device=DEV)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Which kernel a call takes: the library's rule (plan_of in attention.hip, csr5_attention_backward), so that a test can say which one it means
+# ---------------------------------------------------------------------------------------------------------------------
+def sides(rows, n, heads_, kv):
+    """Wavefronts that share a row's keys, in the kernels for many rows."""
+    groups = ((rows * (heads_ // kv) >> 7) + n) * kv
+    return 4 if groups <= 128 else 2 if groups <= 320 else 1
+
+
+def forward_kernel(rows, n, heads_, kv):
+    each = -(-rows // n) * (heads_ // kv)
+    return ("few", 1 if each <= 16 else 2 if each <= 32 else 4) if each <= 64 else ("many", sides(rows, n, heads_, kv))
+
+
+def is_split(rows, n, heads_, kv, most):
+    """Whether the attention over a cache takes its keys by parts; most: what the table could hold."""
+    kind, size = forward_kernel(rows, n, heads_, kv)
+    shift = {("few", 1): 4, ("few", 2): 5, ("few", 4): 6, ("many", 1): 7, ("many", 2): 6, ("many", 4): 5}[kind, size]
+    groups = ((rows * (heads_ // kv) >> shift) + n) * kv
+    return max(-(-(most * groups // 2048) // 128) * 128, 256 if kind == "few" else 512) < most

@@ -155,3 +155,40 @@ def test_nothing_to_do():
     out = e(3, 4, 64)
     B.csr5_rotary(q, None, torch.zeros(3, dtype=I32, device=DEV), e(0, dtype=F32), out)
     assert torch.equal(q, out) and U and math.pi
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,kv,d,rot,axes,dtype,layout", [
+    (1024, 4, 2, 128, 128, 1, BF16, "plain"), (1025, 3, 1, 128, 96, 3, BF16, "beside"), (1027, 2, 2, 64, 64, 2, F16, "major"), (2050, 5, 1, 80, 80, 2, F32, "plain"), (1030, 2, 1, 512, 512, 1, F32, "plain"),
+    (1999, 1, 1, 40, 16, 1, F16, "plain"), (1026, 2, 2, 33, 20, 1, F32, "odd"),
+])
+def test_prompts(tokens, heads, kv, d, rot, axes, dtype, layout, interleaved):
+    """From 1024 tokens on, of which four are a workgroup's: to rows, in place, back, and into the cache."""
+    gen, q, k, v, position, frequency, axis = case(tokens, heads, kv, d, rot, axes, dtype, layout, seed=5)
+    wants = {inverse: [turned(x, position, frequency, axis, interleaved, inverse) for x in (q, k)] for inverse in (False, True)}
+    for inverse in (False, True):
+        q_out, k_out = A.heads(gen, tokens, heads, d, dtype, layout, fill=77.0), A.heads(gen, tokens, kv, d, dtype, layout, fill=77.0)
+        B.csr5_rotary(q, k, position, frequency, q_out, k_out=k_out, axis=axis, interleaved=interleaved, inverse=inverse)
+        for y, (want, slack) in zip((q_out, k_out), wants[inverse]):
+            A.bounded(y, want, slack, dtype, ("turned", inverse))
+            y.fill_(77.0)
+            rest = A.whole(y)
+            assert bool(((rest == 77) | rest.isnan()).all())
+    page, pages = 16, tokens // 16 + 9
+    caches = [torch.full((pages, page, kv, d), 77.0, dtype=dtype, device=DEV) for _ in range(2)]
+    slot = torch.randperm(pages * page, generator=gen)[:tokens].to(I32)
+    for i, none in ((0, -1), (5, pages * page), (1000, 2 ** 31 - 1), (tokens - 1, -2 ** 31), (tokens - 2, -7)):
+        slot[i] = none
+    slot = slot.to(DEV)
+    q_before = q.clone()
+    B.csr5_rotary(q, k, position, frequency, q, axis=axis, interleaved=interleaved, v=v, slot=slot, k_cache=caches[0], v_cache=caches[1])
+    A.bounded(q, *wants[False][0], dtype, "in place")
+    q.copy_(q_before)
+    there = (slot >= 0) & (slot < pages * page)
+    at = slot[there].long()
+    want, slack = wants[False][1]
+    A.bounded(caches[0][at // page, at % page], want[there], slack[there], dtype, "keys")
+    assert torch.equal(caches[1][at // page, at % page], v[there])
+    for c in caches:
+        c[at // page, at % page] = 77.0
+        assert bool((c == 77).all())
