@@ -134,3 +134,23 @@ def test_offsets_out_of_order_write_within_their_sequences(heads, kv):
         for view, whole in ((out, out_all), (dq, dq_all), (dk, dk_all), (dv, dv_all), (lse, lse_all)):
             view.fill_(77.0)
             assert bool((whole == 77).all())
+
+
+FORMS = {("few", 1): ([(5, 70), (1, 300), (8, 8), (3, 131)], 4, 2), ("few", 2): ([(13, 70), (11, 300), (16, 16)], 4, 2), ("few", 4): ([(30, 70), (25, 300), (31, 31)], 4, 2),
+         ("many", 4): ([(130, 200), (65, 65)], 4, 2), ("many", 2): ([(130, 200), (65, 65)], 60, 60), ("many", 1): ([(130, 200), (65, 65)], 128, 128)}
+
+
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("form", list(FORMS), ids=lambda f: f"{f[0]} {f[1]}")
+def test_every_form(form, dtype, d, layout):
+    """Each compiled kernel once: by rows and wavefronts, type, size of heads, rows in 16 bytes or not, packed and paged."""
+    lengths, heads, kv = FORMS[form]
+    p = packed_tests.packed(lengths, heads, kv, d, dtype, layout, seed=39)
+    assert A.forward_kernel(p["rows"], len(lengths), heads, kv) == form
+    packed_tests.forward(p, True)
+    packed_tests.backward(p, True, layout)
+    p = paged_tests.batch(lengths, heads, kv, d, dtype, 16, layout, seed=40)
+    assert A.forward_kernel(p["q"].shape[0], len(lengths), heads, kv) == form
+    paged_tests.check(p)
