@@ -521,7 +521,8 @@ template <typename T, typename KV> int attend(Attend<T, KV> a, const Plan& p, bo
     if (a.d <= 64) by(std::integral_constant<int, 2>());
     else if (a.d <= 96) by(std::integral_constant<int, 3>());
     else by(std::integral_constant<int, 4>());
-    if (p.chunk) k_join<T, KV><<<workgroups((int64_t(a.rows) * a.heads + 3) / 4), 256, 0, s>>>(a);
+    if constexpr (!KV::One::PACKED)         // packed keys are not split
+        if (p.chunk) k_join<T, KV><<<workgroups((int64_t(a.rows) * a.heads + 3) / 4), 256, 0, s>>>(a);
     return launched();
 }
 
