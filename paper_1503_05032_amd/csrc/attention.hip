@@ -89,8 +89,8 @@ template <typename T, typename KV> struct Leave {
 // with the lane's other half, and what it has is, rounded, the second operand of out^T = v^T p^T as it is: the order of the depth (keys) is free as
 // long as v's, which a transposing read of LDS brings, is the same.  Two tiles of keys and of values are in LDS, the next on its way, at fixed places, so
 // that the reads' addresses need no arithmetic.  170 registers at most: three workgroups to a CU, whose products and powers go on side by side.
-// Bound by power and by what products and powers take of each other: 3 sequences up to 8001, 32 heads of 128 with 8 of keys, 790 us, 922 TFLOP/s
-// (a library product of 8192^3: 1371), the matrix units busy 48 % of the time at 1.85 GHz.  Without powers it takes 700 us, without loads 645, with products alone 545.
+// Bound by power and by what products and powers take of each other: 3 sequences up to 8001, 32 heads of 128 with 8 of keys, 794 us, 916 TFLOP/s
+// (a library product of 8192^3: 1598), the matrix units busy 48 % of the time at 1.85 GHz.  Without powers it takes 700 us, without loads 645, with products alone 545.
 // Tiles of 64 and two workgroups: 775 against 740; the next scores beside this tile's powers in one stream of instructions: 908; eight wavefronts to 256
 // rows: 874 against 775; rings of three and four tiles: no change.
 // ---------------------------------------------------------------------------------------------------------------
@@ -253,7 +253,7 @@ template <typename T, typename KV, int ND, bool WIDE, int KG> __global__ __launc
 // Few rows: 16 RB folded rows, and the keys dealt to four wavefronts in tiles of 32, each with LDS of its own and no barrier; what they
 // have of the rows is joined at the end.  Bound by the keys' and values' way from memory: 16 KB (8 where d <= 64) of each wavefront, eight of them on a
 // CU, are on their way but for the moment in which it reads what has come into registers.  48 single tokens of 64 heads with 8 of keys over 3000 to
-// 24000 tokens 517 us, 5.1 TB/s (two tiles to a wavefront and one workgroup to a CU: 551); 8 over 200 to 2200 15 us and 4.5 to join the parts.  Products are keys x rows as above, of 16 x 16 x 32.
+// 24000 tokens 519 us, 5.1 TB/s (two tiles to a wavefront and one workgroup to a CU: 551); 8 over 200 to 2200 15 us and 4.5 to join the parts.  Products are keys x rows as above, of 16 x 16 x 32.
 // ---------------------------------------------------------------------------------------------------------------
 constexpr int FEW_KEYS = 32;
 

@@ -91,7 +91,7 @@ constexpr int DKV_KEYS = 64, DKV_SHIFT = 6;
 
 // ---------------------------------------------------------------------------------------------------------------
 // dq: 128 folded rows (as in attention.hip), 32 to each wavefront, which go through keys and values in tiles of 32.
-// 5 sequences up to 2801, 20 heads of 128 with 5 of keys: 169 us, 720 TFLOP/s of its three products.  Keys are cleansed between the scores and dq's product: 1 us.
+// 5 sequences up to 2801, 20 heads of 128 with 5 of keys: 171 us, 711 TFLOP/s of its three products.  Keys are cleansed between the scores and dq's product: 1 us.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(256, 2) void k_attend_dq(Back<T> a) {
     constexpr int D = ND <= 2 ? 64 : 128, KEYS = DQ_STEP * KG, TILE = KEYS * D * 2, ROWS = DQ_ROWS / KG;
@@ -202,8 +202,8 @@ template <typename T, int ND, bool WIDE, int KG> __global__ __launch_bounds__(25
 // ---------------------------------------------------------------------------------------------------------------
 // dk and dv: 64 keys to a workgroup, which go through the queries that see them in tiles of 32 RG, head by head of those that share the keys: each
 // wavefront has 32 of the keys and takes 32 of the queries, and what RG of them have of the same keys is added up in the end.  (With 128 keys, 32 to a
-// wavefront and all queries, there are half as many workgroups and the first keys' are twice as long.)  5 sequences up to 2801, 20 heads of 128 with 5 of keys: 340 us,
-// 475 TFLOP/s of its four products; 557 with 128 keys and one wavefront to a SIMD, whose accumulators went to and fro between the two halves of the registers.
+// wavefront and all queries, there are half as many workgroups and the first keys' are twice as long.)  5 sequences up to 2801, 20 heads of 128 with 5 of keys: 330 us,
+// 489 TFLOP/s of its four products; 557 with 128 keys and one wavefront to a SIMD, whose accumulators went to and fro between the two halves of the registers.
 // Scores are computed as queries x keys, so that a lane has a key's column of p and ds.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T, int ND, bool WIDE, int RG> __global__ __launch_bounds__(128 * RG, 2) void k_attend_dkv(Back<T> a) {
@@ -382,8 +382,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_add(Back<T> a, in
 }
 
 // Workgroups that have the same keys and some of the heads each, where there are few workgroups and many heads share keys: dk and dv are then added up
-// from their parts, in 32 bits in the workspace.  (One sequence of 3549, 16 heads of 80 with one of keys, 57 workgroups: all
-// gradients and the attention 1275 us, 464 in nine parts.)
+// from their parts, in 32 bits in the workspace.  (One sequence of 3549, 16 heads of 80 with one of keys, 56 workgroups: all
+// gradients and the attention 1275 us, 464 in ten parts.)
 constexpr size_t MOST_PARTS = size_t(32) << 20;
 int parts_of(int64_t groups, int64_t shared, int64_t k_values, size_t room) {
     if (groups > 256 || groups == 0 || shared < 2 || k_values == 0) return 1;

@@ -15,7 +15,7 @@ namespace {
 // Pages.  A request's place among the new tokens, the pages taken and the pages given back is the sum of those before it: every
 // workgroup adds all of them up (256 or 1024 requests at a time) and then writes its own share of the tokens, the new entries
 // of the tables and the ring, finding the request of each by bisection over the sums in LDS; tokens, new entries and the ring are three workgroups', as each waits
-// for memory.  Bound by the launch and four accesses to memory in turn: 48 requests 4.5 us, 700 that bring 30154 tokens 8.9 (one workgroup for everything
+// for memory.  Bound by the launch and four accesses to memory in turn: 48 requests 4.6 us, 700 that bring 30154 tokens 9.0 (one workgroup for everything
 // 12.4 and 18.9; an empty launch 3.4).  So there is one launch and
 // nothing to wait for between workgroups.
 // ---------------------------------------------------------------------------------------------------------------
@@ -181,7 +181,7 @@ template <int EACH> __global__ __launch_bounds__(PAGES_THREADS) void k_pages(Pag
 // heads.  The angle, position * frequency, is a product of whole numbers below 2^31 and floats: in 32 bits a position of 10^6 would
 // be off by 0.03 radians, so the product and its reduction to half a turn are in 64 bits, the cosine and sine of that in 32.
 // Bound by memory: 16384 tokens of 28 + 4 heads of 128, three axes, 59 us (4.6 TB/s; value by value 177); 8191 of 16 + 16 heads of 64, backwards, 13.5 us (5.0; a
-// large copy: 5.0); 24 tokens into the cache 4.5 us, a launch.
+// large copy: 5.0); 24 tokens into the cache 3.7 us, a launch.
 // ---------------------------------------------------------------------------------------------------------------
 template <typename T> struct RotaryArgs {
     int tokens, heads, kv_heads, d, pairs, axes;

@@ -37,7 +37,7 @@ __device__ __forceinline__ Span span_of(const int32_t* offset, int32_t s, int32_
 inline int64_t tiles_at_most(int64_t sequences, int64_t rows, int64_t times, int shift) { return (rows * times >> shift) + sequences; }
 
 // Where there are few workgroups of 128 rows, two or four wavefronts share a row's keys instead, and workgroups have 64 rows or 32 (one sequence
-// of 861, 7 heads: 47 workgroups, attention 32 us for 19; above some 500 of them it is the other way round, as keys are brought more often).
+// of 861, 7 heads with one of keys: 48 workgroups, attention 32 us for 19; above some 500 of them it is the other way round, as keys are brought more often).
 inline int sides_of(int64_t groups) { return groups <= 128 ? 4 : groups <= 320 ? 2 : 1; }
 
 // The sequence that has tile t and where in it the tile begins, by all lanes of a wavefront: 64 sequences at a time are looked at.
